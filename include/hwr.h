@@ -65,7 +65,9 @@ typedef enum {
     HWR_ERR_UNSUPPORTED = 7  /* valid request outside this build's limits */
 } hwr_status;
 
-typedef enum { HWR_F32 = 0, HWR_BF16 = 1 } hwr_dtype;
+/* HWR_F16 is a type of the operators in hwr_ops.h; routing contexts take the
+ * other two. */
+typedef enum { HWR_F32 = 0, HWR_BF16 = 1, HWR_F16 = 2 } hwr_dtype;
 
 /* Flags of hwr_route_batch. */
 #define HWR_SEQUENTIAL   (1u << 0) /* in-batch queue update, see route_batch */

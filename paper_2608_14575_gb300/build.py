@@ -27,6 +27,9 @@ SOURCES = {
     "k_simt.cu": ["--fmad=false"],
     "k_tc.cu": [],
     "hwr_noalloc.cu": [],
+    "ops_api.cu": [],
+    "k_group.cu": [],
+    "k_ops.cu": [],
 }
 
 

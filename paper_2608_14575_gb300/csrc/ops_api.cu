@@ -1,0 +1,637 @@
+// C-ABI host code of the operators that follow a routing decision
+// (declarations in include/hwr_ops.h): argument checks, the workspace, tensor
+// maps, and the launches of each call on the context's stream.
+#include <cudaTypedefs.h>
+#include <math.h>
+#include <stdarg.h>
+#include <stdio.h>
+#include <stdlib.h>
+#include <string.h>
+
+#include <new>
+#include <string>
+
+#include <nvtx3/nvToolsExt.h>
+
+#include "ops_internal.cuh"
+
+using namespace hwr;
+
+namespace {
+
+thread_local std::string g_create_error;
+PFN_cuTensorMapEncodeTiled_v12000 g_encode = nullptr;
+
+struct ApiRange {
+    explicit ApiRange(const char *name) { nvtxRangePushA(name); }
+    ~ApiRange() { nvtxRangePop(); }
+    ApiRange(const ApiRange &) = delete;
+    ApiRange &operator=(const ApiRange &) = delete;
+};
+
+}  // namespace
+
+struct hwr_ops {
+    cudaStream_t stream = nullptr;
+    bool own_stream = false, broken = false;
+    int nsm = 1;
+    std::string err;
+    char *ws = nullptr;
+    size_t ws_cap = 0;
+    float *part = nullptr;       // partial tiles of the grouped products
+    uint32_t *count = nullptr;   // their arrivals (zeroed once, self-resetting)
+    double *sums = nullptr;      // partial sums of squares
+    int sums_cap = 0;
+    int32_t *status_h = nullptr, *status_d = nullptr;   // mapped: bounded waits that ran out
+    long fail_at = 0, allocs = 0;                        // HWR_TEST_FAIL_ALLOC
+};
+
+static hwr_status fail(hwr_ops *c, hwr_status s, const char *fmt, ...) {
+    char buf[512];
+    va_list ap;
+    va_start(ap, fmt);
+    vsnprintf(buf, sizeof buf, fmt, ap);
+    va_end(ap);
+    if (c) {
+        c->err = buf;
+        if (s == HWR_ERR_CUDA || s == HWR_ERR_TIMEOUT) c->broken = true;
+    } else {
+        g_create_error = buf;
+    }
+    return s;
+}
+
+static hwr_status cuda_fail(hwr_ops *c, cudaError_t e, const char *what) {
+    return fail(c, e == cudaErrorMemoryAllocation ? HWR_ERR_OOM : HWR_ERR_CUDA, "%s: %s", what,
+                cudaGetErrorString(e));
+}
+
+#define CK(ctx, call, what)                                     \
+    do {                                                        \
+        cudaError_t e_ = (call);                                \
+        if (e_ != cudaSuccess) return cuda_fail(ctx, e_, what); \
+    } while (0)
+#define OK(call)                              \
+    do {                                      \
+        const hwr_status s_ = (call);         \
+        if (s_ != HWR_OK) return s_;          \
+    } while (0)
+
+static hwr_status ready(hwr_ops *c) {
+    if (c->broken) return fail(c, HWR_ERR_STATE, "context unusable after an earlier failure");
+    if (*(volatile int32_t *)c->status_h != ST_OK)
+        return fail(c, HWR_ERR_TIMEOUT, "a device-side wait of an earlier call gave up");
+    return HWR_OK;
+}
+
+template <class T>
+static hwr_status alloc(hwr_ops *c, T **p, size_t n) {
+    *p = nullptr;
+    if (c->fail_at > 0 && ++c->allocs == c->fail_at)
+        return fail(c, HWR_ERR_OOM, "allocation %ld failed (test hook)", c->allocs);
+    const cudaError_t e = cudaMalloc((void **)p, n * sizeof(T));
+    if (e != cudaSuccess) {
+        cudaGetLastError();
+        *p = nullptr;
+        return fail(c, HWR_ERR_OOM, "cudaMalloc(%zu): %s", n * sizeof(T), cudaGetErrorString(e));
+    }
+    return HWR_OK;
+}
+
+static hwr_status reserve(hwr_ops *c, size_t bytes) {
+    if (bytes <= c->ws_cap) return HWR_OK;
+    if (c->ws) {
+        CK(c, cudaStreamSynchronize(c->stream), "synchronize before regrow");
+        cudaFree(c->ws);
+        c->ws = nullptr;
+        c->ws_cap = 0;
+    }
+    const size_t want = bytes + bytes / 8;
+    OK(alloc(c, &c->ws, want));
+    c->ws_cap = want;
+    return HWR_OK;
+}
+
+extern "C" hwr_status hwr_ops_create(void *cuda_stream, hwr_ops **out) {
+    if (!out) return fail(nullptr, HWR_ERR_INVALID_ARG, "out is NULL");
+    *out = nullptr;
+    hwr_ops *c = new (std::nothrow) hwr_ops;
+    if (!c) return fail(nullptr, HWR_ERR_OOM, "host allocation failed");
+    if (const char *e = getenv("HWR_TEST_FAIL_ALLOC")) c->fail_at = atol(e);
+    auto body = [&]() -> hwr_status {
+        int dev = 0;
+        CK(c, cudaGetDevice(&dev), "cudaGetDevice");
+        CK(c, cudaDeviceGetAttribute(&c->nsm, cudaDevAttrMultiProcessorCount, dev), "device attribute");
+        if (!g_encode) {
+            void *fn = nullptr;
+            cudaDriverEntryPointQueryResult qr;
+            CK(c, cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &qr),
+               "cuTensorMapEncodeTiled");
+            if (qr != cudaDriverEntryPointSuccess || !fn)
+                return fail(c, HWR_ERR_CUDA, "the driver has no cuTensorMapEncodeTiled");
+            g_encode = (PFN_cuTensorMapEncodeTiled_v12000)fn;
+        }
+        CK(c, group_prepare(), "kernel attributes");
+        CK(c, ops_prepare(), "kernel attributes");
+        if (cuda_stream) {
+            c->stream = (cudaStream_t)cuda_stream;
+        } else {
+            CK(c, cudaStreamCreateWithFlags(&c->stream, cudaStreamNonBlocking), "stream");
+            c->own_stream = true;
+        }
+        CK(c, cudaHostAlloc((void **)&c->status_h, 64, cudaHostAllocMapped), "status word");
+        memset(c->status_h, 0, 64);
+        CK(c, cudaHostGetDevicePointer((void **)&c->status_d, c->status_h, 0), "status word");
+        OK(alloc(c, &c->part, group_part_floats(c->nsm)));
+        OK(alloc(c, &c->count, c->nsm));
+        c->sums_cap = clip_blocks(INT64_MAX, c->nsm);
+        OK(alloc(c, &c->sums, c->sums_cap));
+        CK(c, cudaMemsetAsync(c->count, 0, c->nsm * sizeof(uint32_t), c->stream), "memset");
+        return HWR_OK;
+    };
+    const hwr_status s = body();
+    if (s != HWR_OK) {
+        g_create_error = c->err;
+        hwr_ops_destroy(c);
+        return s;
+    }
+    *out = c;
+    return HWR_OK;
+}
+
+extern "C" hwr_status hwr_ops_destroy(hwr_ops *c) {
+    if (!c) return HWR_OK;
+    if (c->stream) cudaStreamSynchronize(c->stream);
+    cudaFree(c->ws);
+    cudaFree(c->part);
+    cudaFree(c->count);
+    cudaFree(c->sums);
+    if (c->status_h) cudaFreeHost(c->status_h);
+    if (c->own_stream) cudaStreamDestroy(c->stream);
+    cudaGetLastError();
+    delete c;
+    return HWR_OK;
+}
+
+extern "C" hwr_status hwr_ops_synchronize(hwr_ops *c) {
+    if (!c) return HWR_ERR_INVALID_ARG;
+    if (c->broken) return fail(c, HWR_ERR_STATE, "context unusable after an earlier failure");
+    CK(c, cudaStreamSynchronize(c->stream), "synchronize");
+    return ready(c);
+}
+
+extern "C" const char *hwr_ops_last_error(const hwr_ops *c) {
+    return c ? c->err.c_str() : g_create_error.c_str();
+}
+
+extern "C" hwr_status hwr_ops_reserve(hwr_ops *c, uint64_t bytes) {
+    if (!c) return HWR_ERR_INVALID_ARG;
+    OK(ready(c));
+    return reserve(c, bytes);
+}
+
+// ---------------------------------------------------------------------------
+
+extern "C" hwr_status hwr_dispatch(hwr_ops *c, int32_t rows, int32_t groups, const int32_t *choice,
+                                   int32_t *offsets, int32_t *order) {
+    if (!c) return HWR_ERR_INVALID_ARG;
+    ApiRange range("hwr_dispatch");
+    OK(ready(c));
+    if (rows < 0 || groups < 1) return fail(c, HWR_ERR_INVALID_ARG, "rows %d, groups %d", rows, groups);
+    if (groups > OPS_MAX_GROUPS)
+        return fail(c, HWR_ERR_UNSUPPORTED, "groups %d > %d", groups, OPS_MAX_GROUPS);
+    if (!offsets || (rows && (!choice || !order))) return fail(c, HWR_ERR_INVALID_ARG, "NULL array");
+    const size_t ints = dispatch_scratch_ints(rows, groups, c->nsm);
+    OK(reserve(c, ints * 4));
+    CK(c, launch_dispatch(rows, groups, choice, offsets, order, (int32_t *)c->ws, c->nsm, c->stream),
+       "dispatch kernel");
+    return HWR_OK;
+}
+
+// ---------------------------------------------------------------------------
+// Operands of the products: nz matrices of rows x cols 16-bit elements.
+
+namespace {
+
+struct Operand {
+    const void *p = nullptr;
+    int64_t ld = 0, z = 0, nz = 1, rows = 0;
+    int cols = 0;
+    bool pad = false;
+    size_t off = 0;      // of the padded copy in the workspace
+};
+
+int64_t up(int64_t v, int64_t m) { return (v + m - 1) / m * m; }
+bool on16(const void *p, int64_t ld, int64_t z, int64_t nz) {
+    return ((uintptr_t)p & 15) == 0 && ld % 8 == 0 && (nz == 1 || z % 8 == 0);
+}
+
+// What a call takes from the workspace, in the order it is asked for.
+struct Carver {
+    size_t at = 0;
+    size_t take(size_t bytes) {
+        const size_t o = at;
+        at = (size_t)up((int64_t)(at + bytes), 1024);
+        return o;
+    }
+    // an operand that TMA cannot read in place gets a padded copy
+    Operand operand(const void *p, int64_t ld, int64_t rows, int cols, int64_t z = 0, int64_t nz = 1) {
+        Operand o;
+        o.p = p;
+        o.ld = ld;
+        o.rows = rows;
+        o.cols = cols;
+        o.nz = nz;
+        o.z = nz > 1 ? z : 0;
+        o.pad = !on16(p, ld, z, nz);
+        if (o.pad) o.off = take((size_t)(nz * rows * up(cols, 8) * 2));
+        return o;
+    }
+};
+
+}  // namespace
+
+static hwr_status settle(hwr_ops *c, Operand *o) {
+    if (!o->pad) {
+        if (o->nz == 1) o->z = up(o->ld * o->rows, 8);
+        return HWR_OK;
+    }
+    const int64_t ld = up(o->cols, 8);
+    CK(c, launch_pad(c->ws + o->off, ld, o->p, o->ld, o->z, o->nz, o->rows, o->cols, c->nsm, c->stream),
+       "padding copy");
+    o->p = c->ws + o->off;
+    o->ld = ld;
+    o->z = ld * o->rows;
+    return HWR_OK;
+}
+
+static hwr_status encode(hwr_ops *c, CUtensorMap *m, bool f16, const Operand &o, int rank, int box0, int box1) {
+    const cuuint64_t dims[3] = {(cuuint64_t)o.cols, (cuuint64_t)o.rows, (cuuint64_t)o.nz};
+    const cuuint64_t strides[2] = {(cuuint64_t)o.ld * 2, (cuuint64_t)o.z * 2};
+    const cuuint32_t box[3] = {(cuuint32_t)box0, (cuuint32_t)box1, 1};
+    const cuuint32_t estr[3] = {1, 1, 1};
+    const CUresult r = g_encode(
+        m, f16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, rank, const_cast<void *>(o.p),
+        dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+        box0 == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+        CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r != CUDA_SUCCESS)
+        return fail(c, HWR_ERR_INVALID_ARG, "operand of %lld x %lld x %d (stride %lld) cannot be mapped",
+                    (long long)o.nz, (long long)o.rows, o.cols, (long long)o.ld);
+    return HWR_OK;
+}
+
+// Rows of the result scattered or not: 16-byte stores where the rows allow them.
+static int vec_ok(const void *p, int64_t ld, int64_t z) { return on16(p, ld, z, 2); }
+
+static GroupProduct product(hwr_ops *c, const hwr_rows *r) {
+    GroupProduct p;
+    p.rows = r->rows;
+    p.groups = r->groups;
+    p.offsets = r->offsets;
+    p.order = r->order;
+    p.f16 = r->dtype == HWR_F16;
+    p.part = c->part;
+    p.count = c->count;
+    p.status = c->status_d;
+    return p;
+}
+
+// Columns of a tile: n in as few tiles of at most `most` as it takes, evenly.
+static int even_tiles(int n, int most) {
+    const int tiles = (n + most - 1) / most;
+    return (int)up((n + tiles - 1) / tiles, 16);
+}
+
+// out[t] = W[g(t)] x[t] (b K-major: [out][in]) or W[g(t)]^T x[t] (b_mn).
+static hwr_status rows_product(hwr_ops *c, GroupProduct p, const Operand &x, const Operand &b, bool b_mn, int k,
+                               int n, const Operand *u, const Operand *eb) {
+    p.k = k;
+    p.n = n;
+    p.b_mn = b_mn;
+    p.ext_b_mn = b_mn;
+    // few rows a group: the weights' bytes bound the product, and narrower
+    // tiles spread them more evenly over the SMs
+    const int64_t per = p.rows / p.groups;
+    p.bn = even_tiles(n, per < 48 && p.out_kind != GP_OUT_PACK ? 128 : GP_MAX_BN);
+    p.mma_n = p.bn;
+    group_plan(&p);
+    if (((int64_t)p.rows / GP_BM + 1) * p.groups * p.ntiles > INT32_MAX)
+        return fail(c, HWR_ERR_UNSUPPORTED, "rows %d x groups %d x columns %d is too large", p.rows, p.groups, n);
+    GroupMaps m;
+    memset(&m, 0, sizeof m);
+    OK(encode(c, &m.a, p.f16, x, 2, 64, 1));
+    OK(encode(c, &m.b, p.f16, b, 3, 64, b_mn ? 64 : p.bn));
+    if (u) {
+        OK(encode(c, &m.u, p.f16, *u, 2, 64, 1));
+        OK(b_mn ? encode(c, &m.eb, p.f16, *eb, 3, 64, GP_RC) : encode(c, &m.eb, p.f16, *eb, 3, GP_RC, p.bn));
+    }
+    CK(c, launch_group(p, m, c->nsm, c->stream), "grouped product kernel");
+    return HWR_OK;
+}
+
+// out[g] = sum over the rows of g of l[t] r[t]^T.
+static hwr_status grad_product(hwr_ops *c, GroupProduct p, const Operand &l, const Operand &r) {
+    p.wgrad = 1;
+    p.m = l.cols;
+    p.n = r.cols;
+    p.bn = p.out_kind == GP_OUT_GROUP ? even_tiles(p.n, GP_MAX_BN) : p.n < GP_MAX_BN ? p.n : GP_MAX_BN;
+    p.mma_n = p.bn;
+    group_plan(&p);
+    if ((int64_t)p.groups * p.mtiles * p.ntiles > INT32_MAX)
+        return fail(c, HWR_ERR_UNSUPPORTED, "groups %d x %d x %d is too large", p.groups, p.m, p.n);
+    GroupMaps m;
+    memset(&m, 0, sizeof m);
+    OK(encode(c, &m.a, p.f16, l, 2, 64, 1));
+    OK(encode(c, &m.b, p.f16, r, 2, 64, 1));
+    CK(c, launch_group(p, m, c->nsm, c->stream), "weight gradient kernel");
+    return HWR_OK;
+}
+
+static hwr_status check_rows(hwr_ops *c, const hwr_rows *r, bool need_x, bool need_w, bool grouped) {
+    if (!r) return fail(c, HWR_ERR_INVALID_ARG, "NULL rows");
+    if (r->rows < 0 || r->groups < 1 || r->n_in < 1 || r->n_out < 1)
+        return fail(c, HWR_ERR_INVALID_ARG, "rows %d, groups %d, n_in %d, n_out %d", r->rows, r->groups, r->n_in,
+                    r->n_out);
+    if (r->groups > OPS_MAX_GROUPS) return fail(c, HWR_ERR_UNSUPPORTED, "groups %d > %d", r->groups, OPS_MAX_GROUPS);
+    if (r->dtype != HWR_BF16 && r->dtype != HWR_F16)
+        return fail(c, HWR_ERR_DTYPE, "dtype %d: products take bf16 or fp16", (int)r->dtype);
+    if (r->rows && (!r->offsets || !r->order || (need_x && !r->x) || (need_w && !r->w)))
+        return fail(c, HWR_ERR_INVALID_ARG, "NULL array");
+    if (need_x && r->x_ld < r->n_in) return fail(c, HWR_ERR_INVALID_ARG, "x_ld %lld < n_in", (long long)r->x_ld);
+    if (r->w_ld < r->n_in) return fail(c, HWR_ERR_INVALID_ARG, "w_ld %lld < n_in", (long long)r->w_ld);
+    if (grouped && r->groups > 1 && r->w_group < r->w_ld * (r->n_out - 1) + r->n_in)
+        return fail(c, HWR_ERR_INVALID_ARG, "w_group %lld: groups overlap", (long long)r->w_group);
+    return HWR_OK;
+}
+
+static hwr_status check_out(hwr_ops *c, const hwr_rows *r, const void *p, int64_t ld, int width, const char *name) {
+    if (r->rows && !p) return fail(c, HWR_ERR_INVALID_ARG, "%s is NULL", name);
+    if (ld < width) return fail(c, HWR_ERR_INVALID_ARG, "%s_ld %lld < %d", name, (long long)ld, width);
+    return HWR_OK;
+}
+
+extern "C" hwr_status hwr_grouped_forward(hwr_ops *c, const hwr_rows *r, void *y, int64_t y_ld) {
+    if (!c) return HWR_ERR_INVALID_ARG;
+    ApiRange range("hwr_grouped_forward");
+    OK(ready(c));
+    OK(check_rows(c, r, true, true, true));
+    OK(check_out(c, r, y, y_ld, r->n_out, "y"));
+    if (r->rows == 0) return HWR_OK;
+    Carver cv;
+    Operand x = cv.operand(r->x, r->x_ld, r->rows, r->n_in);
+    Operand w = cv.operand(r->w, r->w_ld, r->n_out, r->n_in, r->w_group, r->groups);
+    OK(reserve(c, cv.at));
+    OK(settle(c, &x));
+    OK(settle(c, &w));
+    GroupProduct p = product(c, r);
+    p.out_kind = GP_OUT_ROWS;
+    p.out = y;
+    p.ld = y_ld;
+    p.vec = vec_ok(y, y_ld, 0);
+    return rows_product(c, p, x, w, false, r->n_in, r->n_out, nullptr, nullptr);
+}
+
+extern "C" hwr_status hwr_grouped_backward(hwr_ops *c, const hwr_rows *r, const void *dy, int64_t dy_ld, void *dx,
+                                           int64_t dx_ld, void *dw) {
+    if (!c) return HWR_ERR_INVALID_ARG;
+    ApiRange range("hwr_grouped_backward");
+    OK(ready(c));
+    OK(check_rows(c, r, dw != nullptr, dx != nullptr, true));
+    OK(check_out(c, r, dy, dy_ld, r->n_out, "dy"));
+    if (dx) OK(check_out(c, r, dx, dx_ld, r->n_in, "dx"));
+    if (r->rows == 0) {
+        for (int g = 0; dw && g < r->groups; ++g)
+            CK(c, cudaMemset2DAsync((uint16_t *)dw + g * (r->groups > 1 ? r->w_group : 0), r->w_ld * 2, 0,
+                                    (size_t)r->n_in * 2, r->n_out, c->stream), "memset");
+        return HWR_OK;
+    }
+    Carver cv;
+    Operand d = cv.operand(dy, dy_ld, r->rows, r->n_out), x, w;
+    if (dw) x = cv.operand(r->x, r->x_ld, r->rows, r->n_in);
+    if (dx) w = cv.operand(r->w, r->w_ld, r->n_out, r->n_in, r->w_group, r->groups);
+    OK(reserve(c, cv.at));
+    OK(settle(c, &d));
+    if (dx) {
+        OK(settle(c, &w));
+        GroupProduct p = product(c, r);
+        p.out_kind = GP_OUT_ROWS;
+        p.out = dx;
+        p.ld = dx_ld;
+        p.vec = vec_ok(dx, dx_ld, 0);
+        OK(rows_product(c, p, d, w, true, r->n_out, r->n_in, nullptr, nullptr));
+    }
+    if (dw) {
+        OK(settle(c, &x));
+        GroupProduct p = product(c, r);
+        p.out_kind = GP_OUT_GROUP;
+        p.out = dw;
+        p.ld = r->w_ld;
+        p.gstride = r->groups > 1 ? r->w_group : 0;
+        p.vec = vec_ok(dw, r->w_ld, p.gstride);
+        OK(grad_product(c, p, d, x));
+    }
+    return HWR_OK;
+}
+
+static hwr_status check_adapters(hwr_ops *c, const hwr_rows *r, const hwr_adapters *ad) {
+    if (!ad) return fail(c, HWR_ERR_INVALID_ARG, "NULL adapters");
+    if (ad->rank < 1) return fail(c, HWR_ERR_INVALID_ARG, "rank %d", ad->rank);
+    if (ad->rank > OPS_MAX_RANK) return fail(c, HWR_ERR_UNSUPPORTED, "rank %d > %d", ad->rank, OPS_MAX_RANK);
+    if (r->rows && (!ad->a || !ad->b || !ad->scale)) return fail(c, HWR_ERR_INVALID_ARG, "NULL array");
+    return HWR_OK;
+}
+
+// scale[g] x[t] M[g] per row, as two 16-bit terms: [rows][32-rank chunks][high, low].
+static hwr_status low_rank(hwr_ops *c, const hwr_rows *r, const hwr_adapters *ad, const Operand &x,
+                           const Operand &m, bool m_mn, int k, const Operand &u) {
+    GroupProduct p = product(c, r);
+    p.out_kind = GP_OUT_PACK;
+    p.out = const_cast<void *>(u.p);
+    p.ld = u.ld;
+    p.vec = 1;
+    p.scale = ad->scale;
+    return rows_product(c, p, x, m, m_mn, k, ad->rank, nullptr, nullptr);
+}
+
+// The packed inner product's place in the workspace.
+static Operand packed(Carver &cv, const hwr_rows *r, const hwr_adapters *ad) {
+    Operand u;
+    u.cols = (int)up(ad->rank, GP_RC) * 2;
+    u.ld = u.cols;
+    u.rows = r->rows;
+    u.off = cv.take((size_t)u.rows * u.ld * 2);
+    return u;
+}
+
+extern "C" hwr_status hwr_adapter_forward(hwr_ops *c, const hwr_rows *r, const hwr_adapters *ad, void *y,
+                                          int64_t y_ld) {
+    if (!c) return HWR_ERR_INVALID_ARG;
+    ApiRange range("hwr_adapter_forward");
+    OK(ready(c));
+    OK(check_rows(c, r, true, true, false));
+    OK(check_adapters(c, r, ad));
+    OK(check_out(c, r, y, y_ld, r->n_out, "y"));
+    if (r->rows == 0) return HWR_OK;
+    const int K = r->n_in, N = r->n_out, R = ad->rank, G = r->groups;
+    Carver cv;
+    Operand x = cv.operand(r->x, r->x_ld, r->rows, K);
+    Operand w = cv.operand(r->w, r->w_ld, N, K);
+    Operand a = cv.operand(ad->a, K, R, K, (int64_t)R * K, G);
+    Operand b = cv.operand(ad->b, R, N, R, (int64_t)N * R, G);
+    Operand u = packed(cv, r, ad);
+    OK(reserve(c, cv.at));
+    u.p = c->ws + u.off;
+    OK(settle(c, &x));
+    OK(settle(c, &a));
+    OK(low_rank(c, r, ad, x, a, false, K, u));
+    OK(settle(c, &w));
+    OK(settle(c, &b));
+    GroupProduct p = product(c, r);
+    p.shared = 1;
+    p.groups = 1;
+    p.ext_groups = G;
+    p.rank = R;
+    p.out_kind = GP_OUT_ROWS;
+    p.out = y;
+    p.ld = y_ld;
+    p.vec = vec_ok(y, y_ld, 0);
+    return rows_product(c, p, x, w, false, K, N, &u, &b);
+}
+
+extern "C" hwr_status hwr_adapter_backward(hwr_ops *c, const hwr_rows *r, const hwr_adapters *ad, const void *dy,
+                                           int64_t dy_ld, void *dx, int64_t dx_ld, void *da, void *db) {
+    if (!c) return HWR_ERR_INVALID_ARG;
+    ApiRange range("hwr_adapter_backward");
+    OK(ready(c));
+    OK(check_rows(c, r, da || db, dx != nullptr, false));
+    OK(check_adapters(c, r, ad));
+    OK(check_out(c, r, dy, dy_ld, r->n_out, "dy"));
+    if (dx) OK(check_out(c, r, dx, dx_ld, r->n_in, "dx"));
+    const int K = r->n_in, N = r->n_out, R = ad->rank, G = r->groups;
+    if (r->rows == 0) {
+        if (da) CK(c, cudaMemsetAsync(da, 0, (size_t)G * R * K * 2, c->stream), "memset");
+        if (db) CK(c, cudaMemsetAsync(db, 0, (size_t)G * N * R * 2, c->stream), "memset");
+        return HWR_OK;
+    }
+    if (!dx && !da && !db) return HWR_OK;
+    Carver cv;
+    Operand d = cv.operand(dy, dy_ld, r->rows, N), x, w, a, b, u, v;
+    if (da || db) x = cv.operand(r->x, r->x_ld, r->rows, K);
+    if (dx) w = cv.operand(r->w, r->w_ld, N, K);
+    if (dx || db) a = cv.operand(ad->a, K, R, K, (int64_t)R * K, G);
+    if (dx || da) {
+        b = cv.operand(ad->b, R, N, R, (int64_t)N * R, G);
+        v = packed(cv, r, ad);
+    }
+    if (db) u = packed(cv, r, ad);
+    OK(reserve(c, cv.at));
+    OK(settle(c, &d));
+    if (dx || da) {
+        OK(settle(c, &b));
+        v.p = c->ws + v.off;
+        OK(low_rank(c, r, ad, d, b, true, N, v));
+    }
+    if (dx || db) OK(settle(c, &a));
+    if (dx) {
+        OK(settle(c, &w));
+        GroupProduct p = product(c, r);
+        p.shared = 1;
+        p.groups = 1;
+        p.ext_groups = G;
+        p.rank = R;
+        p.out_kind = GP_OUT_ROWS;
+        p.out = dx;
+        p.ld = dx_ld;
+        p.vec = vec_ok(dx, dx_ld, 0);
+        OK(rows_product(c, p, d, w, true, N, K, &v, &a));
+    }
+    if (da || db) OK(settle(c, &x));
+    if (da) {
+        GroupProduct p = product(c, r);
+        p.out_kind = GP_OUT_LOW_T;
+        p.out = da;
+        p.ld = K;
+        p.gstride = (int64_t)R * K;
+        p.rank_out = R;
+        OK(grad_product(c, p, x, v));
+    }
+    if (db) {
+        u.p = c->ws + u.off;
+        OK(low_rank(c, r, ad, x, a, false, K, u));
+        GroupProduct p = product(c, r);
+        p.out_kind = GP_OUT_LOW;
+        p.out = db;
+        p.ld = R;
+        p.gstride = (int64_t)N * R;
+        p.rank_out = R;
+        p.vec = vec_ok(db, R, p.gstride);
+        OK(grad_product(c, p, d, u));
+    }
+    return HWR_OK;
+}
+
+// ---------------------------------------------------------------------------
+
+extern "C" hwr_status hwr_clip_gradients(hwr_ops *c, int32_t n, const hwr_gradient *grads, float max_norm,
+                                         float *norm) {
+    if (!c) return HWR_ERR_INVALID_ARG;
+    ApiRange range("hwr_clip_gradients");
+    OK(ready(c));
+    if (n < 0 || (n && !grads) || !norm) return fail(c, HWR_ERR_INVALID_ARG, "n %d or a NULL array", n);
+    if (!(max_norm > 0.f)) return fail(c, HWR_ERR_INVALID_ARG, "max_norm %g", max_norm);
+    for (int i = 0; i < n; ++i) {
+        const hwr_gradient &g = grads[i];
+        if (g.n < 0 || (g.n && (!g.in || !g.out))) return fail(c, HWR_ERR_INVALID_ARG, "gradient %d: n %lld or a NULL array", i, (long long)g.n);
+        if (g.dtype != HWR_F32 && g.dtype != HWR_BF16 && g.dtype != HWR_F16)
+            return fail(c, HWR_ERR_DTYPE, "gradient %d: dtype %d", i, (int)g.dtype);
+        const uintptr_t mask = g.dtype == HWR_F32 ? 3 : 1;
+        if (((uintptr_t)g.in | (uintptr_t)g.out) & mask) return fail(c, HWR_ERR_INVALID_ARG, "gradient %d is not aligned to its elements", i);
+        if (clip_chunks(g.n, g.dtype) > INT32_MAX / 2) return fail(c, HWR_ERR_UNSUPPORTED, "gradient %d has %lld elements", i, (long long)g.n);
+    }
+    // tables of up to CLIP_TABLE tensors; each has its blocks' partial sums
+    int nparts = 0;
+    for (int pass = 0; pass < 2; ++pass) {
+        int first = 0;
+        for (int i = 0; i < n || i == 0;) {
+            ClipTable t;
+            t.n = 0;
+            t.first_block = first;
+            int64_t chunks = 0;
+            for (; i < n && t.n < CLIP_TABLE; ++i) {
+                const hwr_gradient &g = grads[i];
+                const int64_t k = clip_chunks(g.n, g.dtype);
+                if (k == 0) continue;
+                if (chunks + k > INT32_MAX) break;
+                t.in[t.n] = g.in;
+                t.out[t.n] = g.out;
+                t.count[t.n] = g.n;
+                t.dtype[t.n] = (uint8_t)g.dtype;
+                t.chunk0[t.n++] = (int32_t)chunks;
+                chunks += k;
+            }
+            t.chunk0[t.n] = (int32_t)chunks;
+            const int blocks = clip_blocks(chunks, c->nsm);
+            if (pass == 0) {
+                if (first + blocks > c->sums_cap) {
+                    CK(c, cudaStreamSynchronize(c->stream), "synchronize before regrow");
+                    double *more = nullptr;
+                    const int cap = 2 * (first + blocks);
+                    OK(alloc(c, &more, cap));
+                    CK(c, cudaMemcpyAsync(more, c->sums, first * sizeof(double), cudaMemcpyDeviceToDevice, c->stream), "copy");
+                    CK(c, cudaStreamSynchronize(c->stream), "synchronize");
+                    cudaFree(c->sums);
+                    c->sums = more;
+                    c->sums_cap = cap;
+                }
+                CK(c, launch_square_sums(t, blocks, c->sums, c->stream), "norm kernel");
+            } else {
+                CK(c, launch_clip(t, blocks, c->sums, nparts, max_norm, norm, c->stream), "clip kernel");
+            }
+            first += blocks;
+            if (n == 0) break;
+        }
+        nparts = first;
+    }
+    return HWR_OK;
+}
