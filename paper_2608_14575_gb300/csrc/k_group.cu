@@ -1,24 +1,35 @@
-// Products with ragged groups of rows on the tensor cores (TMA + tcgen05), fp32
-// accumulation in TMEM.  One kernel serves
-//   rows products   out[t] = W[g(t)] x[t] (W K-major) or W[g(t)]^T x[t] (W
-//                   MN-major): a tile is up to 128 rows of one group, gathered
-//                   by their indices, times bn columns;
-//   weight gradients  out[g] = sum over the group's rows of l[t] r[t]^T: both
-//                   operands are gathered rows, MN-major, and the contraction
-//                   runs over the group's rows.
-// A rows product may carry a low-rank extension: after the contraction, for
-// each group g with rows in the tile, the tile's rows of u (two 16-bit terms
-// a value) times the group's [n][rank] matrix, accumulated only into the
-// lanes of that group's rows (the MMA's lane mask), so that no value of one
-// group's matrix ever meets another group's rows.
+// Products with ragged groups of rows on the tensor cores, fp32 accumulation in
+// TMEM.  One kernel serves
+//   grouped products   out[t] = W[g(t)] x[t], or W[g(t)]^T x[t] (W MN-major);
+//   shared products    out[t] = W x[t] + a low-rank term of t's group;
+//   weight gradients   out[g] = sum over the group's rows of l[t] r[t]^T.
 //
-// The iterations (64-deep stages of the contraction) of all tiles are dealt
-// evenly: whole tiles first, one to a CTA a round, then the tiles of the last
-// rounds as one line of iterations cut into equal pieces.  The pieces of a tile
-// leave fp32 partials; the last to arrive adds them in the order of the
-// contraction, so the result does not depend on who that is.
+// A pair of CTAs (cta_group::2) computes a tile of 256 x up to 256: per 64-deep
+// stage each CTA holds 128 rows of the A side and half of the B side, which
+// halves the B bytes that every SM takes from L2.  W comes by TMA, and so do
+// the rows of x once they lie by place; of a few rows, which need no copy, each
+// is picked by its index with 16-byte cp.async.  (Large products on picked rows
+// were bound by the picking: 434 us with cp.async and 650 us with TMA's row
+// gather for 65,536 x 1024 x 2048 over 64 groups.)
+//
+// In a grouped product the rows of x are the B side, whose extent moves in
+// steps of 16: a group's last rows cost no whole tile, and a few rows of a
+// decode step cost 16.  In a shared product they are the A side, because the
+// low-rank extension must keep groups apart: after the contraction, for each
+// group with rows in the tile, the tile's rows of u (two 16-bit terms a value)
+// times the group's [n][rank] matrix are accumulated with the MMA's row mask
+// into that group's rows only; no value of one group's matrix ever meets
+// another group's rows.
+//
+// The iterations (stages of the contraction) of all tiles are dealt evenly:
+// whole tiles first, one to a pair a round, then the tiles of the last rounds
+// as one line of iterations cut into equal pieces.  The pieces of a tile leave
+// fp32 partials; the last to arrive adds them in the order of the contraction,
+// so the result does not depend on who that is.
 #include "ops_internal.cuh"
 #include "umma.cuh"
+
+#include <stddef.h>
 
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -28,24 +39,51 @@ namespace {
 
 using namespace umma;
 
-constexpr int THREADS = 192;       // warps 0-3 epilogue, 4 TMA producer, 5 MMA issuer
-constexpr int A_BYTES = GP_BM * GP_BK * 2;
+// warps 0-3 epilogue, 4-7 epilogue too (sorted rows) or picking rows, 8 TMA, 9
+// MMA (even CTA) or relay (odd CTA)
+constexpr int THREADS = 320;
+constexpr int GATHER_WARPS = 4;
+constexpr int A_BYTES = 128 * GP_BK * 2;
 constexpr int MAX_STAGES = 12;
 constexpr int SMEM_MAX = 227 * 1024;
 constexpr int MIN_PIECE = 4;       // iterations of the smallest piece of a cut tile
 
+constexpr int OUT_PITCH = 64;      // bytes of a staged output row (32 columns)
+constexpr int OUT_BYTES = 32 * OUT_PITCH;   // of a warp
+// Staged rows keep their four 16-byte units in an order of their own, so that
+// neither writing a row a lane nor reading a row by 4 lanes meets a bank twice.
+__device__ __forceinline__ int staged_at(int row, int unit) {
+    return row * OUT_PITCH + ((unit ^ ((row >> 1) & 3)) << 4);
+}
+
+// What a kernel is compiled for (the epilogue's registers are those of its kind).
+enum : int { K_GROUPED = 0, K_SHARED = 1, K_PACK = 2, K_GRAD = 3, K_LOW = 4 };
+
+// Shared memory behind the stages: this, then the group tables.
 struct Tables {
-    int64_t iter0[OPS_MAX_GROUPS + 1];   // first iteration of each group (weight gradients)
-    int32_t offs[OPS_MAX_GROUPS + 1];    // first row of each group, clamped
-    int32_t eoffs[OPS_MAX_GROUPS + 1];   // the same of the extension's groups
-    int32_t tile0[OPS_MAX_GROUPS + 1];   // first tile of each group
-    uint64_t full[MAX_STAGES], empty[MAX_STAGES], accf[2], acce[2], done;
+    // per stage: full (even CTA: both CTAs' bytes, and the odd CTA's word), rows
+    // (this CTA's picked rows have landed), empty
+    uint64_t full[MAX_STAGES], rowsf[MAX_STAGES], empty[MAX_STAGES], accf[2], acce[2], done;
+    alignas(16) uint8_t out[8][OUT_BYTES];   // epilogue staging, a warp each
+    int32_t rows[GP_TILE];               // the tile's rows of the output (epilogue)
     uint32_t tmem;
     int abort_f;
-    int last;
+    int last, go;        // epilogue: this piece writes the tile; the accumulator is there
+    // group tables: ng groups of the tiles, and the extension's
+    int ng;
+    int64_t *iter0;      // [ng + 1] first iteration of each group (gradients)
+    int32_t *offs;       // [ng + 1] first place of each group, clamped
+    int32_t *tile0;      // [ng + 1] first tile of each group (rows products)
+    int32_t *eoffs;      // [groups + 1] first place of each of the extension's groups
 };
 
-constexpr int STAGE_ROOM = SMEM_MAX - 1024 - (int)((sizeof(Tables) + 1023) / 1024 * 1024);
+static_assert(OUT_PITCH % 16 == 0 && OUT_BYTES % 16 == 0 && offsetof(Tables, out) % 16 == 0 && sizeof(Tables) % 16 == 0,
+              "staged rows are read and written 16 bytes at a time");
+
+__host__ __device__ inline int table_bytes(const GroupProduct &p) {
+    const int g = p.plan.groups + 1;
+    return (int)sizeof(Tables) + (p.mode == GP_WGRAD ? g * 12 : p.shared ? g * 4 + 16 : g * 8);
+}
 
 // Waits of the unwinding (copies in flight, MMAs issued): bounded, no flags.
 __device__ __forceinline__ void drain(uint64_t *bar, uint32_t parity) {
@@ -54,41 +92,69 @@ __device__ __forceinline__ void drain(uint64_t *bar, uint32_t parity) {
         if (clock64() - t0 > WAIT_CYCLES) return;
 }
 
-struct Work {
-    int g, mt, nt;        // group, row tile (or result-row tile) and column tile within it
-    int k0, k1, ki;       // iterations of this piece, and of the tile
-    int c0, c1;           // first and last CTA with a piece of the tile
+__host__ __device__ inline int up16(int v) { return (v + 15) & ~15; }
+
+// A place in the ring of stages (a division a stage would cost what an MMA does).
+struct Ring {
+    int s = 0, stages;
+    uint32_t ph = 0, n = 0;       // phase, steps in all
+    __device__ explicit Ring(int stages_) : stages(stages_) {}
+    __device__ void step() {
+        ++n;
+        if (++s == stages) {
+            s = 0;
+            ph ^= 1;
+        }
+    }
 };
 
-// The pieces of this CTA, in order.
+struct Work {
+    int g, xt, ot;        // group; tile of rows (gradients: of result rows); tile of columns
+    int k0, k1, ki;       // iterations of this piece, and of the tile
+    int c0, c1;           // first and last pair with a piece of the tile
+    int first, count;     // places of the tile (gradients: of the group)
+};
+
+// a * b / c; 32-bit where that holds (a 64-bit division costs some 100 instructions)
+__device__ __forceinline__ int64_t mul_div(int64_t a, int b, int c) {
+    const uint64_t v = (uint64_t)a * (uint32_t)b;
+    if (v >> 32) return (int64_t)(v / (uint32_t)c);
+    return (uint32_t)v / (uint32_t)c;
+}
+__device__ __forceinline__ int64_t div_small(int64_t a, int64_t b) {
+    if ((a | b) >> 32) return a / b;
+    return (uint32_t)a / (uint32_t)b;
+}
+
+// The pieces of this pair, in order.
 struct Walk {
     const GroupProduct &p;
     const Tables &t;
-    int tiles, dp, kiters, ctas;
-    int next_tile;
+    int me, pairs, dp, kiters, cutters, next_tile;
     int64_t rest, pos, end;
 
     __device__ Walk(const GroupProduct &p_, const Tables &t_) : p(p_), t(t_) {
-        tiles = t.tile0[p.groups];
+        const bool grad = p.mode == GP_WGRAD;
+        const int tiles = grad ? 0 : t.tile0[t.ng];
+        me = blockIdx.x >> 1;
+        pairs = gridDim.x >> 1;
         kiters = (p.k + GP_BK - 1) / GP_BK;
-        const int P = gridDim.x;
-        dp = 0;
-        if (!p.wgrad && tiles >= 2 * P) dp = (tiles / P - 1) * P;
-        rest = p.wgrad ? t.iter0[p.groups] : (int64_t)(tiles - dp) * kiters;
+        dp = !grad && tiles >= 2 * pairs ? (tiles / pairs - 1) * pairs : 0;
+        rest = grad ? t.iter0[t.ng] : (int64_t)(tiles - dp) * kiters;
         const int64_t most = rest / MIN_PIECE;
-        ctas = most < 1 ? 1 : most < P ? (int)most : P;
-        next_tile = blockIdx.x;
+        cutters = most < 1 ? 1 : most < pairs ? (int)most : pairs;
+        next_tile = me;
         pos = end = 0;
-        if ((int)blockIdx.x < ctas) {
-            pos = first(blockIdx.x);
-            end = first(blockIdx.x + 1);
+        if (me < cutters) {
+            pos = mul_div(rest, me, cutters);
+            end = mul_div(rest, me + 1, cutters);
         }
     }
-    __device__ int64_t first(int c) const { return rest * c / ctas; }
-    // the CTA whose piece holds iteration i
-    __device__ int owner(int64_t i) const { return (int)(((i + 1) * ctas - 1) / rest); }
+    // the pair whose piece holds iteration i
+    __device__ int owner(int64_t i) const { return (int)div_small((i + 1) * cutters - 1, rest); }
 
-    __device__ static int find(const int32_t *v, int n, int x) {   // last g with v[g] <= x
+    template <class T>
+    __device__ static int find(const T *v, int n, T x) {   // last g with v[g] <= x
         int lo = 0, hi = n - 1;
         while (lo < hi) {
             const int m = (lo + hi + 1) >> 1;
@@ -98,43 +164,42 @@ struct Walk {
         return lo;
     }
     __device__ void place(Work &w, int tile) const {
-        w.g = find(t.tile0, p.groups, tile);
+        w.g = find(t.tile0, t.ng, tile);
         const int local = tile - t.tile0[w.g];
-        const int mts = (t.tile0[w.g + 1] - t.tile0[w.g]) / p.ntiles;
-        // bands of 64 row tiles, column by column: the CTAs at work share
+        const int n = t.offs[w.g + 1] - t.offs[w.g], xts = (n + GP_TILE - 1) / GP_TILE;
+        // bands of 32 row tiles, column by column: the pairs at work share
         // columns of W and the band's rows stay in L2
-        const int band = local / (64 * p.ntiles), in = local - band * 64 * p.ntiles;
-        const int h = min(64, mts - band * 64);
-        w.nt = in / h;
-        w.mt = band * 64 + (in - w.nt * h);
+        const int band = local / (32 * p.ntiles), in = local - band * 32 * p.ntiles;
+        const int h = min(32, xts - band * 32);
+        w.ot = in / h;
+        w.xt = band * 32 + (in - w.ot * h);
+        // rows on the B side: tiles of about equal extent
+        const int width = p.mode == GP_GROUPED && xts <= 8 ? up16((n + xts - 1) / xts) : GP_TILE;
+        w.first = t.offs[w.g] + w.xt * width;
+        w.count = min(width, n - w.xt * width);
     }
     __device__ bool next(Work &w) {
         if (next_tile < dp) {
             place(w, next_tile);
-            next_tile += gridDim.x;
+            next_tile += pairs;
             w.k0 = 0;
             w.k1 = w.ki = kiters;
-            w.c0 = w.c1 = blockIdx.x;
+            w.c0 = w.c1 = me;
             return true;
         }
         if (pos >= end) return false;
         int64_t start;
-        if (p.wgrad) {
-            int lo = 0, hi = p.groups - 1;
-            while (lo < hi) {
-                const int m = (lo + hi + 1) >> 1;
-                if (t.iter0[m] <= pos) lo = m;
-                else hi = m - 1;
-            }
-            w.g = lo;
-            const int per = t.tile0[lo + 1] - t.tile0[lo];
-            w.ki = (int)((t.iter0[lo + 1] - t.iter0[lo]) / per);
-            const int local = (int)((pos - t.iter0[lo]) / w.ki);
-            start = t.iter0[lo] + (int64_t)local * w.ki;
-            w.nt = local / p.mtiles;
-            w.mt = local - w.nt * p.mtiles;
+        if (p.mode == GP_WGRAD) {
+            w.g = find(t.iter0, t.ng, pos);
+            w.first = t.offs[w.g];
+            w.count = max(0, t.offs[w.g + 1] - w.first);
+            w.ki = max(1, (w.count + GP_BK - 1) / GP_BK);
+            const int local = (int)div_small(pos - t.iter0[w.g], w.ki);
+            start = t.iter0[w.g] + (int64_t)local * w.ki;
+            w.ot = local / p.mtiles;
+            w.xt = local - w.ot * p.mtiles;
         } else {
-            const int i = (int)(pos / kiters);
+            const int i = (int)div_small(pos, kiters);
             w.ki = kiters;
             start = (int64_t)i * kiters;
             place(w, dp + i);
@@ -155,22 +220,22 @@ struct Ext {
     const GroupProduct &p;
     const Tables &t;
     int p0, p1, g, r0, a, b;
-    __device__ Ext(const GroupProduct &p_, const Tables &t_, int first, int last)
-        : p(p_), t(t_), p0(first), p1(last) {
-        g = Walk::find(t.eoffs, p.ext_groups, first);   // eoffs[g] <= first, or g = 0
+    __device__ Ext(const GroupProduct &p_, const Tables &t_, const Work &w)
+        : p(p_), t(t_), p0(w.first), p1(w.first + w.count) {
+        g = Walk::find(t.eoffs, p.plan.groups, p0);   // eoffs[g] <= first, or g = 0
         r0 = 0;
         settle();
     }
     __device__ void settle() {
-        for (; g < p.ext_groups; ++g) {
+        for (; g < p.plan.groups; ++g) {
             a = max(t.eoffs[g], p0);
             b = min(t.eoffs[g + 1], p1);
             if (a < b) return;
             if (t.eoffs[g] >= p1) break;
         }
-        g = p.ext_groups;
+        g = p.plan.groups;
     }
-    __device__ bool more() const { return g < p.ext_groups; }
+    __device__ bool more() const { return g < p.plan.groups; }
     __device__ void step() {
         r0 += GP_RC;
         if (r0 >= p.rank) {
@@ -200,13 +265,6 @@ __device__ __forceinline__ float widen(uint16_t v) {
 // n consecutive 16-bit values of v (32 at most) to dst.
 template <bool F16>
 __device__ __forceinline__ void store_row(uint16_t *dst, const float (&v)[32], int n, bool vec) {
-    if (vec && n == 32) {
-#pragma unroll
-        for (int j = 0; j < 32; j += 8)
-            *(uint4 *)(dst + j) = make_uint4(pack2<F16>(v[j], v[j + 1]), pack2<F16>(v[j + 2], v[j + 3]),
-                                             pack2<F16>(v[j + 4], v[j + 5]), pack2<F16>(v[j + 6], v[j + 7]));
-        return;
-    }
 #pragma unroll
     for (int j = 0; j < 32; j += 8) {
         if (vec && j + 8 <= n)
@@ -219,455 +277,652 @@ __device__ __forceinline__ void store_row(uint16_t *dst, const float (&v)[32], i
     }
 }
 
-template <bool F16>
-__global__ void __launch_bounds__(THREADS, 1)
+// Index of the row at a place of the order, -1 where there is none.
+__device__ __forceinline__ int row_at(const GroupProduct &p, int place) {
+    const int r = p.plan.order[place];
+    return (uint32_t)r < (uint32_t)p.plan.rows ? r : -1;
+}
+
+// ---- picked rows ------------------------------------------------------------------
+//
+// A stage's rows are 64 columns K-major in the 128-byte swizzle: the 16-byte
+// unit c of smem row r lies at unit c ^ (r mod 8).  Eight lanes copy one row's
+// 128 bytes.
+
+__device__ void pick_rows(const GroupProduct &p, Tables &t, uint8_t *sm, int rank) {
+    Walk walk(p, t);
+    Work w;
+    Ring at(p.stages);
+    bool ok = true;
+    const int tid = threadIdx.x & 127, sub = tid >> 3, c = tid & 7;
+    const uint32_t dst = (p.mode == GP_GROUPED ? A_BYTES : 0) + sub * 128 + ((c ^ (sub & 7)) << 4);
+    while (ok && walk.next(w)) {
+        // this CTA's rows of the tile: its 128 of the A side, or its half of the B side
+        const int half = p.mode == GP_GROUPED ? up16(w.count) >> 1 : 128;
+        const int mine = min(half, w.count - rank * half);
+        const uint16_t *row[8];     // 16 rows apart: 2,048 bytes of smem
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int q = sub + i * 16, r = q < mine ? row_at(p, w.first + rank * half + q) : -1;
+            row[i] = r < 0 ? nullptr : p.x + r * p.x_ld;
+        }
+        int stages = w.k1 - w.k0;
+        if (p.rank && w.k1 == w.ki)
+            for (Ext e(p, t, w); e.more(); e.step()) ++stages;   // of these only the arrival is due
+        for (int i0 = 0; i0 < stages; ++i0, at.step()) {
+            const int kb = w.k0 + i0;
+            ok = mbar_wait(&t.empty[at.s], at.ph ^ 1, &t.abort_f, p.status);
+            ok = __all_sync(0xffffffffu, ok);
+            if (!ok) break;
+            if (kb < w.k1) {
+                const uint32_t st = smem_u32(sm + (size_t)at.s * p.stage_bytes) + dst;
+                const int col = kb * GP_BK + c * 8, left = p.k - col;
+                const uint32_t bytes = left >= 8 ? 16 : left > 0 ? left * 2 : 0;   // beyond: zeros
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (row[i]) cp_async16(st + i * 2048, row[i] + (bytes ? col : 0), bytes);
+            }
+            cp_async_arrive(&t.rowsf[at.s]);
+        }
+    }
+    cp_async_wait_all();
+}
+
+// ---- the kernel -------------------------------------------------------------------
+
+template <bool F16, int KIND>
+__global__ void __launch_bounds__(THREADS, 1) __cluster_dims__(2, 1, 1)
 k_group(const __grid_constant__ GroupMaps maps, const __grid_constant__ GroupProduct p) {
     extern __shared__ uint8_t smem_raw[];
     uint8_t *sm = (uint8_t *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
     Tables &t = *(Tables *)(sm + (size_t)p.stages * p.stage_bytes);
     volatile int *abort_f = &t.abort_f;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = cluster_rank();
+    constexpr bool grad = KIND == K_GRAD || KIND == K_LOW;
+    constexpr bool grouped = KIND == K_GROUPED, shared = KIND == K_SHARED, low = KIND == K_LOW, pack = KIND == K_PACK;
+    constexpr int CS = GP_TILE;      // TMEM columns of one of the two accumulators
 
-    // Group tables.  Offsets are the caller's: clamped here, so that no value
-    // of theirs reads or writes outside the arrays.
-    {
-        const int ng = p.shared ? p.ext_groups : p.groups;
-        int32_t *dst = p.shared ? t.eoffs : t.offs;
-        for (int i = threadIdx.x; i <= ng; i += THREADS) {
-            const int v = p.offsets[i];
-            dst[i] = v < 0 ? 0 : v > p.rows ? p.rows : v;
-        }
-        if (p.shared && threadIdx.x == 0) {
-            t.offs[0] = 0;
-            t.offs[1] = p.rows;
-        }
-    }
     if (threadIdx.x == 0) {
         for (int s = 0; s < p.stages; ++s) {
-            mbar_init(&t.full[s], 1);
+            mbar_init(&t.full[s], p.sorted ? 1 : 2);
+            mbar_init(&t.rowsf[s], 32 * GATHER_WARPS);
             mbar_init(&t.empty[s], 1);
         }
         for (int b = 0; b < 2; ++b) {
             mbar_init(&t.accf[b], 1);
-            mbar_init(&t.acce[b], 128);
+            mbar_init(&t.acce[b], p.sorted ? 16 : 8);
         }
         mbar_init(&t.done, 1);
         t.abort_f = 0;
+        t.ng = shared ? 1 : p.plan.groups;
+        // the tables of 8-byte values come first
+        t.iter0 = (int64_t *)(&t + 1);
+        t.offs = (int32_t *)(&t + 1) + (grad ? 2 * (t.ng + 1) : 0);
+        t.tile0 = t.offs + t.ng + 1;
+        t.eoffs = t.tile0 + t.ng + 1;
         fence_mbar_init();
     }
-    const uint32_t cs = (p.bn + 31) & ~31;      // TMEM columns of one of the two accumulators
-    uint32_t tcols = 64;
-    while (tcols < 2 * cs) tcols *= 2;
-    if (warp == 5) {
-        tmem_alloc(&t.tmem, tcols);
-        tmem_relinquish();
+    if (warp == 9) {
+        tmem_alloc_pair(&t.tmem, 2 * CS);
+        tmem_relinquish_pair();
+    }
+    if (warp == 8 && lane == 0) {
+        if (!grad) tma_prefetch_desc(&maps.w);
+        if (p.sorted) tma_prefetch_desc(&maps.x);
+        if (shared) tma_prefetch_desc(&maps.eb);
+    }
+    // everything above overlaps the kernel before; everything below may read
+    // what it wrote
+    grid_launch_dependents();
+    grid_dependency_wait();
+    __syncthreads();
+    // Group tables.  Offsets are the caller's: clamped here, so that no value
+    // of theirs reads or writes outside the arrays.
+    {
+        int32_t *dst = shared ? t.eoffs : t.offs;
+        for (int i = threadIdx.x; i <= p.plan.groups; i += THREADS) {
+            const int v = p.plan.offsets[i];
+            dst[i] = v < 0 ? 0 : v > p.plan.places ? p.plan.places : v;
+        }
+        if (shared && threadIdx.x == 0) {
+            const int v = p.plan.padded ? p.plan.offsets[p.plan.groups + 1] : p.plan.rows;
+            t.offs[0] = 0;
+            t.offs[1] = v < 0 ? 0 : v > p.plan.places ? p.plan.places : v;
+        }
     }
     __syncthreads();
     if (warp == 0) {
-        // first tile (and iteration) of each group: a running sum over 32 groups at a time
-        int tile = 0;
-        int64_t iter = 0;
-        for (int g0 = 0; g0 < p.groups; g0 += 32) {
+        // first tile (or iteration) of each group: a running sum over 32 groups at a time
+        int64_t run = 0;
+        for (int g0 = 0; g0 < t.ng; g0 += 32) {
             const int g = g0 + lane;
-            int nt = 0, ki = 0;
-            if (g < p.groups) {
+            int64_t v = 0;
+            if (g < t.ng) {
                 const int n = max(0, t.offs[g + 1] - t.offs[g]);
-                if (p.wgrad) {
-                    nt = p.mtiles * p.ntiles;
-                    ki = max(1, (n + GP_BK - 1) / GP_BK);   // an empty group's zeros are written too
-                } else {
-                    nt = (n + GP_BM - 1) / GP_BM * p.ntiles;
-                }
+                // (an empty group's zero gradient is written too)
+                v = grad ? (int64_t)p.mtiles * p.ntiles * max(1, (n + GP_BK - 1) / GP_BK)
+                         : (int64_t)((n + GP_TILE - 1) / GP_TILE) * p.ntiles;
             }
-            int st = nt;
-            int64_t si = (int64_t)nt * ki;
+#pragma unroll
             for (int d = 1; d < 32; d *= 2) {
-                const int a = __shfl_up_sync(0xffffffffu, st, d);
-                const int64_t b = __shfl_up_sync(0xffffffffu, si, d);
-                if (lane >= d) {
-                    st += a;
-                    si += b;
-                }
+                const int64_t o = __shfl_up_sync(0xffffffffu, v, d);
+                if (lane >= d) v += o;
             }
-            if (g < p.groups) {
-                t.tile0[g + 1] = tile + st;
-                t.iter0[g + 1] = iter + si;
+            if (g < t.ng) {
+                if (grad) t.iter0[g + 1] = run + v;
+                else t.tile0[g + 1] = (int)(run + v);
             }
-            tile += __shfl_sync(0xffffffffu, st, 31);
-            iter += __shfl_sync(0xffffffffu, si, 31);
+            run += __shfl_sync(0xffffffffu, v, 31);
         }
         if (lane == 0) {
-            t.tile0[0] = 0;
-            t.iter0[0] = 0;
+            if (grad) t.iter0[0] = 0;
+            else t.tile0[0] = 0;
         }
     }
     tc_fence_before();
     __syncthreads();
+    cluster_sync();          // the other CTA's barriers and TMEM are there
     tc_fence_after();
     const uint32_t tmem = t.tmem;
-    const int bblocks = (p.bn + 63) / 64;
-    const uint32_t b_bytes = p.wgrad || p.b_mn ? bblocks * 8192 : p.bn * 128;
 
-    if (warp == 4) {
-        // producer: gathers 4 rows a lane, one lane loads the W tiles
-        uint32_t n = 0;
-        bool ok = true;
-        Walk walk(p, t);
-        Work w;
-        while (ok && walk.next(w)) {
-            if (p.wgrad) {
-                const int first = t.offs[w.g], last = t.offs[w.g + 1];
-                // 16 lanes hold the rows of the stage; each gathers its four
-                // rows into every block of 64 columns, shared between the two halves
-                const int mblocks = min(2, (p.m - w.mt * GP_BM + 63) / 64);
-                const int nb = min(bblocks, (p.n - w.nt * p.bn + 63) / 64);
-                const uint32_t bytes = (uint32_t)(mblocks + nb) * 8192;
-                int next[4];
-                auto rows_of = [&](int kb) {
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const int pos = first + kb * GP_BK + 4 * (lane & 15) + j;
-                        int r = p.rows;
-                        if (kb < w.k1 && pos < last) r = p.order ? p.order[pos] : pos;
-                        next[j] = (uint32_t)r < (uint32_t)p.rows ? r : p.rows;
-                    }
-                };
-                rows_of(w.k0);
-                for (int kb = w.k0; kb < w.k1; ++kb, ++n) {
-                    int idx[4];
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) idx[j] = next[j];
-                    rows_of(kb + 1);
-                    const int s = n % p.stages;
-                    ok = mbar_wait(&t.empty[s], ((n / p.stages) & 1) ^ 1, abort_f, p.status);
-                    ok = __all_sync(0xffffffffu, ok);
-                    if (!ok) break;
-                    uint8_t *st = sm + (size_t)s * p.stage_bytes + (lane & 15) * 512;
-                    if (lane == 0) mbar_arrive_expect_tx(&t.full[s], bytes);
-                    __syncwarp();
-                    for (int b = lane >> 4; b < mblocks + nb; b += 2)
-                        if (b < mblocks)
-                            tma_gather4(st + b * 8192, &maps.a, &t.full[s], w.mt * GP_BM + b * 64, idx);
-                        else
-                            tma_gather4(st + A_BYTES + (b - mblocks) * 8192, &maps.b, &t.full[s],
-                                        w.nt * p.bn + (b - mblocks) * 64, idx);
-                }
-            } else {
-                const int first = t.offs[w.g] + w.mt * GP_BM;
-                const int last = min(first + GP_BM, t.offs[w.g + 1]);
-                const int na = (last - first + 3) / 4;     // lanes with rows
-                int idx[4];
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const int pos = first + 4 * lane + j;
-                    int r = p.rows;
-                    if (pos < last) r = p.order ? p.order[pos] : pos;
-                    idx[j] = (uint32_t)r < (uint32_t)p.rows ? r : p.rows;
-                }
-                const int n0 = w.nt * p.bn;
-                const int nb = min(bblocks, (p.n - n0 + 63) / 64);
-                const uint32_t bytes = (p.b_mn ? nb * 8192 : b_bytes) + na * 512;
-                for (int kb = w.k0; kb < w.k1; ++kb, ++n) {
-                    const int s = n % p.stages;
-                    ok = mbar_wait(&t.empty[s], ((n / p.stages) & 1) ^ 1, abort_f, p.status);
-                    ok = __all_sync(0xffffffffu, ok);
-                    if (!ok) break;
-                    uint8_t *st = sm + (size_t)s * p.stage_bytes;
-                    if (lane == 0) {
-                        mbar_arrive_expect_tx(&t.full[s], bytes);
-                        if (p.b_mn)
-                            for (int b = 0; b < nb; ++b)
-                                tma_load_3d(st + A_BYTES + b * 8192, &maps.b, &t.full[s], n0 + b * 64,
-                                            kb * GP_BK, w.g);
-                        else
-                            tma_load_3d(st + A_BYTES, &maps.b, &t.full[s], kb * GP_BK, n0, w.g);
-                    }
-                    __syncwarp();
-                    if (lane < na) tma_gather4(st + lane * 512, &maps.a, &t.full[s], kb * GP_BK, idx);
-                }
-                if (ok && p.rank && w.k1 == w.ki) {
-                    const uint32_t ebytes =
-                        (p.ext_b_mn ? nb * 4096 : p.bn * 64) + na * 512;
-                    for (Ext e(p, t, first, last); e.more(); e.step(), ++n) {
-                        const int s = n % p.stages;
-                        ok = mbar_wait(&t.empty[s], ((n / p.stages) & 1) ^ 1, abort_f, p.status);
-                        ok = __all_sync(0xffffffffu, ok);
-                        if (!ok) break;
-                        uint8_t *st = sm + (size_t)s * p.stage_bytes;
-                        if (lane == 0) {
-                            mbar_arrive_expect_tx(&t.full[s], ebytes);
-                            if (p.ext_b_mn)
-                                for (int b = 0; b < nb; ++b)
-                                    tma_load_3d(st + A_BYTES + b * 4096, &maps.eb, &t.full[s],
-                                                n0 + b * 64, e.r0, e.g);
-                            else
-                                tma_load_3d(st + A_BYTES, &maps.eb, &t.full[s], e.r0, n0, e.g);
-                        }
-                        __syncwarp();
-                        if (lane < na) tma_gather4(st + lane * 512, &maps.u, &t.full[s], e.r0 * 2, idx);
-                    }
-                }
-            }
-        }
-        // the loads still in flight land before the CTA can exit
-        const uint32_t f = n > (uint32_t)p.stages ? n - p.stages : 0;
-        if (lane == 0)
-            for (uint32_t j = f; j < n; ++j) drain(&t.full[j % p.stages], (j / p.stages) & 1);
-        __syncwarp();
-    } else if (warp == 5) {
+    if (!p.sorted && warp >= 4 && warp < 8) {
+        pick_rows(p, t, sm, rank);
+    } else if (warp == 8) {
+        // TMA: W (each CTA its 128 rows of the A side or its half of the B side),
+        // sorted rows, the extension's operands, a gradient's two sides.  All bytes
+        // count on the even CTA's barrier.
         if (lane == 0) {
-            uint32_t n = 0, lt = 0;
+            Ring at(p.stages);
             bool ok = true;
             Walk walk(p, t);
             Work w;
-            const uint32_t idesc = idesc_16bit(GP_BM, p.mma_n, F16, p.wgrad, p.wgrad || p.b_mn);
-            const uint32_t eidesc = idesc_16bit(GP_BM, p.mma_n, F16, false, p.ext_b_mn);
-            // per 16-deep MMA: two rows of 8 K indices further (MN-major) or 32 bytes (K-major)
-            const uint32_t astep = p.wgrad ? 2048 >> 4 : 2, bstep = p.wgrad || p.b_mn ? 2048 >> 4 : 2;
+            const int half = grouped ? 128 : p.bn >> 1;           // of the dense operand
+            const int blocks = (half + 63) >> 6;                  // MN-major blocks of 64
+            const uint32_t dbytes = p.dense_mn ? blocks * 8192 : half * 128;
+            const uint32_t ebytes = p.dense_mn ? blocks * 4096 : half * 64;
+            const uint32_t dside = grouped ? 0 : A_BYTES, xside = grouped ? A_BYTES : 0;
+            const uint32_t full0 = smem_of(&t.full[0], 0);
+            auto claim = [&](uint32_t bytes) {
+                ok = mbar_wait(&t.empty[at.s], at.ph ^ 1, abort_f, p.status);
+                if (ok && rank == 0) mbar_arrive_expect_tx(&t.full[at.s], bytes);
+                return ok;
+            };
+            while (ok && walk.next(w)) {
+                if (grad) {
+                    const int l0 = w.xt * GP_TILE + rank * 128, r0 = w.ot * p.bn + rank * half;
+                    for (int kb = w.k0; kb < w.k1; ++kb, at.step()) {
+                        if (!claim(2 * (2 + blocks) * 8192)) break;
+                        uint8_t *st = sm + (size_t)at.s * p.stage_bytes;
+                        const int row = w.first + kb * GP_BK;
+                        for (int b = 0; b < 2; ++b)
+                            tma_load_3d_pair(st + b * 8192, &maps.x, full0 + at.s * 8, l0 + b * 64, row, 0);
+                        for (int b = 0; b < blocks; ++b)
+                            tma_load_3d_pair(st + A_BYTES + b * 8192, &maps.w, full0 + at.s * 8, r0 + b * 64, row, 0);
+                    }
+                    continue;
+                }
+                const int o0 = w.ot * (grouped ? GP_TILE : p.bn) + rank * half;
+                // boxes of rows: this CTA's, and both CTAs'
+                const int xhalf = grouped ? up16(w.count) >> 1 : 128;
+                const int x0 = w.first + rank * xhalf;
+                const int c0 = min(xhalf, w.count), c1 = max(0, w.count - xhalf);
+                const int boxes = ((rank ? c1 : c0) + GP_ROW_BOX - 1) / GP_ROW_BOX;
+                const uint32_t xbytes = ((c0 + GP_ROW_BOX - 1) / GP_ROW_BOX + (c1 + GP_ROW_BOX - 1) / GP_ROW_BOX) *
+                                        GP_ROW_BOX * 128;
+                for (int kb = w.k0; kb < w.k1; ++kb, at.step()) {
+                    if (!claim(2 * dbytes + (p.sorted ? xbytes : 0))) break;
+                    uint8_t *st = sm + (size_t)at.s * p.stage_bytes;
+                    if (p.sorted && boxes == 4)
+                        tma_load_3d_pair(st + xside, &maps.xx, full0 + at.s * 8, kb * GP_BK, x0, 0);
+                    else if (p.sorted)
+                        for (int b = 0; b < boxes; ++b)
+                            tma_load_3d_pair(st + xside + b * GP_ROW_BOX * 128, &maps.x, full0 + at.s * 8, kb * GP_BK,
+                                             x0 + b * GP_ROW_BOX, 0);
+                    if (p.dense_mn)
+                        for (int b = 0; b < blocks; ++b)
+                            tma_load_3d_pair(st + dside + b * 8192, &maps.w, full0 + at.s * 8, o0 + b * 64, kb * GP_BK, w.g);
+                    else
+                        tma_load_3d_pair(st + dside, &maps.w, full0 + at.s * 8, kb * GP_BK, o0, w.g);
+                }
+                if (shared && ok && w.k1 == w.ki)
+                    for (Ext e(p, t, w); e.more(); e.step(), at.step()) {
+                        if (!claim(2 * ebytes + xbytes)) break;
+                        uint8_t *st = sm + (size_t)at.s * p.stage_bytes;
+                        for (int b = 0; b < boxes; ++b)
+                            tma_load_3d_pair(st + b * GP_ROW_BOX * 128, &maps.u, full0 + at.s * 8, e.r0 * 2,
+                                             x0 + b * GP_ROW_BOX, 0);
+                        if (p.dense_mn)
+                            for (int b = 0; b < blocks; ++b)
+                                tma_load_3d_pair(st + A_BYTES + b * 4096, &maps.eb, full0 + at.s * 8, o0 + b * 64, e.r0, e.g);
+                        else
+                            tma_load_3d_pair(st + A_BYTES, &maps.eb, full0 + at.s * 8, e.r0, o0, e.g);
+                    }
+            }
+            // the loads still in flight land before the pair can exit
+            if (rank == 0)
+                for (uint32_t j = at.n > (uint32_t)p.stages ? at.n - p.stages : 0; j < at.n; ++j)
+                    drain(&t.full[j % p.stages], (j / p.stages) & 1);
+        }
+        __syncwarp();
+    } else if (warp == 9) {
+        if (lane == 0 && rank == 0) {
+            uint32_t lt = 0;
+            Ring at(p.stages);
+            bool ok = true;
+            Walk walk(p, t);
+            Work w;
+            const bool a_mn = grad || (grouped && p.dense_mn);
+            const bool b_mn = grad || (!grad && !grouped && p.dense_mn);
+            // both CTAs' operands have landed; picked rows, copied by threads, are
+            // made visible to the tensor cores' proxy here (and by the odd CTA's relay)
+            auto stage_ready = [&]() {
+                if (!p.sorted && !mbar_wait(&t.rowsf[at.s], at.ph, abort_f, p.status)) return false;
+                if (!mbar_wait(&t.full[at.s], at.ph, abort_f, p.status)) return false;
+                if (!p.sorted) fence_proxy_async_smem();
+                tc_fence_after();
+                return true;
+            };
+            // per 16-deep MMA: 16 rows of 128 bytes further (MN-major), or 32 bytes (K-major)
+            const uint32_t astep = a_mn ? 2048 >> 4 : 2, bstep = b_mn ? 2048 >> 4 : 2;
             for (; ok && walk.next(w); ++lt) {
                 const int b = lt & 1;
-                const uint32_t d = tmem + b * cs;
+                const uint32_t d = tmem + b * CS;
+                const int N = grouped ? up16(w.count) : p.bn;
+                const uint32_t idesc = idesc_16bit(GP_TILE, N, F16, a_mn, b_mn);
                 ok = mbar_wait(&t.acce[b], ((lt >> 1) & 1) ^ 1, abort_f, p.status);
                 if (!ok) break;
                 tc_fence_after();
-                for (int kb = w.k0; kb < w.k1; ++kb, ++n) {
-                    const int s = n % p.stages;
-                    ok = mbar_wait(&t.full[s], (n / p.stages) & 1, abort_f, p.status);
+                for (int kb = w.k0; kb < w.k1; ++kb, at.step()) {
+                    ok = stage_ready();
                     if (!ok) break;
-                    tc_fence_after();
-                    const uint32_t st = smem_u32(sm + (size_t)s * p.stage_bytes);
+                    const uint32_t st = smem_u32(sm + (size_t)at.s * p.stage_bytes);
                     const uint64_t ad = sdesc(st, 8192, 1024, 2), bd = sdesc(st + A_BYTES, 8192, 1024, 2);
+                    // a gradient's last stage: whole 16s of rows, the group's padding
+                    // among them (zeros), nothing of the next group
+                    const int steps = grad ? min(4, max(1, (w.count - kb * GP_BK + 15) >> 4)) : 4;
 #pragma unroll
                     for (int k = 0; k < 4; ++k)
-                        mma_bf16(d, ad + astep * k, bd + bstep * k, idesc, (kb > w.k0) | k);
-                    mma_commit(&t.empty[s]);
+                        if (k < steps) mma_pair(d, ad + astep * k, bd + bstep * k, idesc, (kb > w.k0) | k);
+                    mma_commit_pair(&t.empty[at.s]);
                 }
                 if (!ok) break;
-                if (p.rank && w.k1 == w.ki) {
-                    const int first = t.offs[w.g] + w.mt * GP_BM;
-                    const int last = min(first + GP_BM, t.offs[w.g + 1]);
-                    for (Ext e(p, t, first, last); e.more(); e.step(), ++n) {
-                        uint32_t off[4];
+                if (shared && w.k1 == w.ki) {
+                    const uint32_t eidesc = idesc_16bit(GP_TILE, p.bn, F16, false, p.dense_mn);
+                    for (Ext e(p, t, w); e.more(); e.step(), at.step()) {
+                        uint32_t off[8];
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const int a = min(max(e.a - first - 32 * i, 0), 32);
-                            const int z = min(max(e.b - first - 32 * i, 0), 32);
-                            // lanes [a, z) of this word take part
+                        for (int i = 0; i < 8; ++i) {
+                            const int a = min(max(e.a - w.first - 32 * i, 0), 32);
+                            const int z = min(max(e.b - w.first - 32 * i, 0), 32);
+                            // rows [a, z) of this word take part
                             const uint32_t below = a == 32 ? 0xffffffffu : (1u << a) - 1;
                             const uint32_t upto = z == 32 ? 0xffffffffu : (1u << z) - 1;
                             off[i] = ~(upto & ~below);
                         }
-                        const int s = n % p.stages;
-                        ok = mbar_wait(&t.full[s], (n / p.stages) & 1, abort_f, p.status);
+                        ok = stage_ready();
                         if (!ok) break;
-                        tc_fence_after();
-                        const uint32_t st = smem_u32(sm + (size_t)s * p.stage_bytes);
+                        const uint32_t st = smem_u32(sm + (size_t)at.s * p.stage_bytes);
                         const uint64_t ad = sdesc(st, 0, 1024, 2);
-                        const uint64_t bd = p.ext_b_mn ? sdesc(st + A_BYTES, 4096, 1024, 2)
+                        const uint64_t bd = p.dense_mn ? sdesc(st + A_BYTES, 4096, 1024, 2)
                                                        : sdesc(st + A_BYTES, 0, 512, 4);
                         const int steps = min(GP_RC, p.rank - e.r0) > 16 ? 2 : 1;
-                        const uint32_t eb = p.ext_b_mn ? 2048 >> 4 : 2;
+                        const uint32_t eb = p.dense_mn ? 2048 >> 4 : 2;
                         for (int k = 0; k < steps; ++k) {
-                            mma_16bit_lanes(d, ad + 2 * k, bd + eb * k, eidesc, off, 1);
-                            mma_16bit_lanes(d, ad + 4 + 2 * k, bd + eb * k, eidesc, off, 1);
+                            mma_pair_rows(d, ad + 2 * k, bd + eb * k, eidesc, off);
+                            mma_pair_rows(d, ad + 4 + 2 * k, bd + eb * k, eidesc, off);
                         }
-                        mma_commit(&t.empty[s]);
+                        mma_commit_pair(&t.empty[at.s]);
                     }
                     if (!ok) break;
                 }
-                mma_commit(&t.accf[b]);
+                mma_commit_pair(&t.accf[b]);
             }
-            mma_commit(&t.done);
+            mma_commit_pair(&t.done);
             drain(&t.done, 0);
+        } else if (lane == 0 && !p.sorted) {
+            // odd CTA: passes on to the even one that a stage's rows are here
+            const uint32_t full0 = smem_of(&t.full[0], 0);
+            Ring at(p.stages);
+            bool ok = true;
+            Walk walk(p, t);
+            Work w;
+            while (ok && walk.next(w)) {
+                int stages = w.k1 - w.k0;
+                if (shared && w.k1 == w.ki)
+                    for (Ext e(p, t, w); e.more(); e.step()) ++stages;
+                for (; stages > 0; --stages, at.step()) {
+                    ok = mbar_wait(&t.rowsf[at.s], at.ph, abort_f, p.status);
+                    if (!ok) break;
+                    fence_proxy_async_smem();
+                    mbar_arrive_cluster(full0 + at.s * 8);
+                }
+            }
         }
         __syncwarp();
     } else {
-        // epilogue: thread = TMEM lane = row of the tile
-        const int row = threadIdx.x;
-        const uint32_t lane_base = (uint32_t)(warp * 32) << 16;
-        const int P = gridDim.x;
-        if (p.out_kind == GP_OUT_ROWS && !p.shared) {
+        // epilogue: thread = TMEM lane = row of the A side; with eight warps, two
+        // take every other 32 columns of the same rows
+        const int row = threadIdx.x & 127, quad = warp & 3, half = warp >> 2;
+        const int halves = p.sorted ? 2 : 1, threads = 128 * halves;
+        const uint32_t lane_base = (uint32_t)(quad * 32) << 16;
+        const uint32_t acce0 = smem_of(&t.acce[0], 0);
+        uint16_t *const out0 = (uint16_t *)p.out;
+        uint8_t *const stage = t.out[warp];
+        if (grouped) {
             // rows without a group: zeros
-            for (int64_t pos = (int64_t)t.offs[p.groups] + blockIdx.x * 4 + warp; pos < p.rows;
-                 pos += (int64_t)P * 4) {
-                const int r = p.order ? p.order[pos] : (int)pos;
-                if ((uint32_t)r >= (uint32_t)p.rows) continue;
-                uint16_t *dst = (uint16_t *)p.out + (int64_t)r * p.ld;
+            const int total = p.plan.padded ? p.plan.offsets[p.plan.groups + 1] : p.plan.rows;
+            for (int64_t pos = (int64_t)t.offs[t.ng] + blockIdx.x * (4 * halves) + warp; pos < min(total, p.plan.places);
+                 pos += (int64_t)gridDim.x * (4 * halves)) {
+                const int r = row_at(p, (int)pos);
+                if (r < 0) continue;
+                uint16_t *dst = out0 + (int64_t)r * p.ld;
                 if (p.vec)
                     for (int j = lane * 8; j + 8 <= p.n; j += 256) *(uint4 *)(dst + j) = make_uint4(0, 0, 0, 0);
                 for (int j = (p.vec ? p.n & ~7 : 0) + lane; j < p.n; j += 32) dst[j] = 0;
             }
         }
         uint32_t lt = 0;
-        bool ok = true;
         Walk walk(p, t);
         Work w;
         for (; walk.next(w); ++lt) {
             const int b = lt & 1;
-            int64_t orow = -1;     // this lane's row of the output
-            int nrows = GP_BM;
-            float sc = 1.f;
-            if (p.wgrad) {
-                nrows = min(GP_BM, p.m - w.mt * GP_BM);
-                orow = w.mt * GP_BM + row;
+            int nrows;                 // rows of the A side that count
+            int cols;                  // columns that count
+            if (grad) {
+                nrows = min(128, p.m - w.xt * GP_TILE - (int)rank * 128);
+                cols = min(p.bn, p.n - w.ot * p.bn);
+            } else if (grouped) {
+                nrows = min(128, p.n - w.ot * GP_TILE - (int)rank * 128);
+                cols = w.count;
+                for (int i = threadIdx.x; i < w.count; i += threads) t.rows[i] = row_at(p, w.first + i);
             } else {
-                const int first = t.offs[w.g] + w.mt * GP_BM;
-                nrows = min(GP_BM, t.offs[w.g + 1] - first);
-                if (row < nrows) orow = p.order ? p.order[first + row] : first + row;
-                if (p.scale) sc = p.scale[w.g];
+                nrows = min(128, w.count - (int)rank * 128);
+                cols = min(p.bn, p.n - w.ot * p.bn);
+                if (half == 0 && row < nrows) t.rows[row] = row_at(p, w.first + rank * 128 + row);
             }
-            const bool mine = row < nrows && (p.wgrad || (uint64_t)orow < (uint64_t)p.rows);
-            ok = mbar_wait(&t.accf[b], (lt >> 1) & 1, abort_f, p.status);
-            ok = __all_sync(0xffffffffu, ok);
-            if (!ok) break;
+            // one warp waits for all: they go on, or give up, together
+            if (warp == 0) {
+                bool ok = mbar_wait(&t.accf[b], (lt >> 1) & 1, abort_f, p.status);
+                ok = __all_sync(0xffffffffu, ok);
+                if (lane == 0) t.go = ok;
+            }
+            named_bar_sync(1, threads);
+            if (!*(volatile int *)&t.go) break;
             tc_fence_after();
             const bool cut = w.c0 != w.c1;
             bool write = true;
-            const int cols = (p.mma_n + 31) & ~31;
-            const uint32_t acc = tmem + lane_base + b * cs;
+            const uint32_t acc = tmem + lane_base + b * CS;
+            auto release = [&]() {     // this warp has read its part of the accumulator
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive_cluster(acce0 + b * 8);
+            };
             if (cut) {
                 // leave this piece's sums (slot 1: the tile's first piece, which
-                // ends its CTA's line; slot 0: a later one, which begins it); the
+                // ends its pair's line; slot 0: a later one, which begins it); the
                 // last of the tile's pieces to arrive adds them all
                 const int slot = 2 * blockIdx.x + (w.k0 == 0);
-                float4 *dst = (float4 *)(p.part + (size_t)slot * GP_BM * GP_MAX_BN) + row;
-                for (int c = 0; c < cols; c += 32) {
+                float4 *dst = (float4 *)(p.part + (size_t)slot * 128 * GP_TILE) + row;
+                for (int c = half * 32; c < cols; c += 32 * halves) {
                     uint32_t v[32];
                     tmem_ld32(acc + c, v);
                     tmem_wait_ld32(v);
                     if (row < nrows)
 #pragma unroll
                         for (int j = 0; j < 32; j += 4)
-                            __stcg(dst + (c + j) / 4 * GP_BM,
-                                   make_float4(__uint_as_float(v[j]), __uint_as_float(v[j + 1]),
-                                               __uint_as_float(v[j + 2]), __uint_as_float(v[j + 3])));
+                            if (c + j < cols)
+                                __stcg(dst + (c + j) / 4 * 128,
+                                       make_float4(__uint_as_float(v[j]), __uint_as_float(v[j + 1]),
+                                                   __uint_as_float(v[j + 2]), __uint_as_float(v[j + 3])));
                 }
+                release();
                 __threadfence();
-                named_bar_sync(1, 128);
+                named_bar_sync(1, threads);
                 if (threadIdx.x == 0) {
-                    const uint32_t before = atomicAdd(&p.count[w.c0], 1u);
-                    t.last = before == (uint32_t)(w.c1 - w.c0);
-                    if (t.last) p.count[w.c0] = 0;
+                    uint32_t *count = p.count + 2 * w.c0 + rank;
+                    t.last = atomicAdd(count, 1u) == (uint32_t)(w.c1 - w.c0);
+                    if (t.last) *count = 0;
                     __threadfence();
                 }
-                named_bar_sync(1, 128);
+                named_bar_sync(1, threads);
                 write = *(volatile int *)&t.last != 0;
             }
-            // 32 columns of the tile from column c on: from TMEM, or the pieces' sum
-            auto values = [&](int c, float (&v)[32]) {
-                if (!cut) {
-                    uint32_t u[32];
-                    tmem_ld32(acc + c, u);
-                    tmem_wait_ld32(u);
-#pragma unroll
-                    for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(u[j]);
-                    return;
-                }
-#pragma unroll
-                for (int j = 0; j < 32; ++j) v[j] = 0.f;
-                if (row >= nrows) return;
-                for (int o = w.c0; o <= w.c1; ++o) {
-                    const int slot = 2 * o + (o == w.c0);
-                    const float4 *src = (const float4 *)(p.part + (size_t)slot * GP_BM * GP_MAX_BN) + row;
-#pragma unroll
-                    for (int j = 0; j < 32; j += 4) {
-                        const float4 x = __ldcg(src + (c + j) / 4 * GP_BM);
-                        v[j] += x.x;
-                        v[j + 1] += x.y;
-                        v[j + 2] += x.z;
-                        v[j + 3] += x.w;
-                    }
-                }
+            auto out_row = [&](int r) -> uint16_t * {     // of the A side: null where there is none
+                if (r >= nrows) return nullptr;
+                if (grad) return out0 + w.g * p.gstride + (int64_t)(w.xt * GP_TILE + rank * 128 + r) * p.ld;
+                const int at = t.rows[r];
+                return at < 0 ? nullptr : out0 + (int64_t)at * p.ld;
             };
-            if (write) {
-                const int n0 = w.nt * p.bn;
-                uint16_t *out = (uint16_t *)p.out;
-                if (p.out_kind == GP_OUT_ROWS || p.out_kind == GP_OUT_GROUP) {
-                    if (p.out_kind == GP_OUT_GROUP) out += w.g * p.gstride;
-                    const int width = min(p.bn, p.n - n0);
-                    for (int c = 0; c < width; c += 32) {
-                        float v[32];
-                        values(c, v);
-                        if (mine) store_row<F16>(out + orow * p.ld + n0 + c, v, min(32, width - c), p.vec);
-                    }
-                } else if (p.out_kind == GP_OUT_PACK) {
-                    // value = high + low, to about twice the type's precision; an
-                    // infinite high term takes a zero low one (not inf - inf)
-                    for (int c = 0; c < cols && n0 + c < p.n; c += 32) {
-                        float v[32], lo[32];
-                        values(c, v);
+            // Chunks of 32 columns of this thread's row.  A joined tile of a few
+            // rows is dealt to all threads instead, a row's chunk at a time.
+            const int chunks = pack ? (p.n + 63) / 64 * 2 : low ? (cols + 63) / 64 * 2 : (cols + 31) / 32;
+            const bool dealt = !grad && !grouped && cut && nrows <= 32;
+            const int items = !write ? 0 : dealt ? nrows * chunks : chunks;
+            // (low: both chunks of a pair in one warp)
+            auto column = [&](int i) {
+                return (low ? (i >> 1) * 2 * halves + half * 2 + (i & 1) : i * halves + half) * 32;
+            };
+            // staged rows go out 64 bytes each, by 4 lanes: this lane's 4 rows
+            const bool staged = !low && !pack && p.vec && !dealt;
+            const int piece = (lane & 3) * 8;
+            uint16_t *base[4];
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) {
-                            v[j] = n0 + c + j < p.n ? v[j] * sc : 0.f;
-                            const float hi = widen<F16>((uint16_t)pack2<F16>(v[j], 0.f));
-                            lo[j] = isinf(hi) ? 0.f : v[j] - hi;
-                        }
-                        if (mine) {
-                            store_row<F16>(out + orow * p.ld + (n0 + c) * 2, v, 32, true);
-                            store_row<F16>(out + orow * p.ld + (n0 + c) * 2 + 32, lo, 32, true);
+            for (int q = 0; q < 4; ++q)
+                base[q] = staged && !grouped ? out_row(quad * 32 + q * 8 + (lane >> 2)) : nullptr;
+            float prev[32];
+            uint32_t u[32];
+            const bool tm = !cut && write;
+            bool held = tm;
+            if (tm && column(0) < chunks * 32) tmem_ld32(acc + column(0), u);
+            for (int i = dealt ? threadIdx.x : 0; dealt ? i < items : column(i) < items * 32; i += dealt ? threads : 1) {
+                const int r = dealt ? i % nrows : row, c = dealt ? i / nrows * 32 : column(i);
+                const bool mine = r < nrows;
+                float v[32];
+                if (cut) {
+                    // the pieces' sum, in the order of the contraction
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) v[j] = 0.f;
+#pragma unroll 2
+                    for (int o = w.c0; o <= (mine ? w.c1 : -1); ++o) {
+                        const int slot = 2 * (2 * o + rank) + (o == w.c0);
+                        const float4 *src = (const float4 *)(p.part + (size_t)slot * 128 * GP_TILE) + r;
+                        float4 x[8];
+#pragma unroll
+                        for (int j = 0; j < 8; ++j)
+                            x[j] = c + 4 * j < cols ? __ldcg(src + (c / 4 + j) * 128) : make_float4(0, 0, 0, 0);
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) {
+                            v[4 * j] += x[j].x;
+                            v[4 * j + 1] += x[j].y;
+                            v[4 * j + 2] += x[j].z;
+                            v[4 * j + 3] += x[j].w;
                         }
                     }
                 } else {
-                    // blocks of 64 columns: the products with the high terms of 32
-                    // ranks, then those with the low terms
-                    out += w.g * p.gstride;
-                    for (int c = 0; c < cols; c += 64) {
-                        const int r = (n0 + c) / 2, left = p.rank_out - r;
-                        if (left <= 0) break;
-                        float v[32], lo[32];
-                        values(c, v);
-                        values(c + 32, lo);
+                    // (a gradient without rows: its stage held the next group's)
+                    const bool none = grad && w.count == 0;
+                    tmem_wait_ld32(u);
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) v[j] += lo[j];
-                        if (!mine) continue;
-                        if (p.out_kind == GP_OUT_LOW)
-                            store_row<F16>(out + orow * p.ld + r, v, min(32, left), p.vec);
-                        else
-#pragma unroll
-                            for (int j = 0; j < 32; ++j)
-                                if (j < left) out[(r + j) * p.ld + orow] = (uint16_t)pack2<F16>(v[j], 0.f);
+                    for (int j = 0; j < 32; ++j) v[j] = none ? 0.f : __uint_as_float(u[j]);
+                    if (column(i + 1) < items * 32) {
+                        tmem_ld32(acc + column(i + 1), u);       // while this chunk goes out
+                    } else {
+                        release();
+                        held = false;
                     }
                 }
+                if (staged) {
+                    // 32 x 32 values through shared memory, rows of the output as rows.
+                    // Grouped: lane = result column, TMEM column = row of x
+                    if (grouped) {
+#pragma unroll
+                        for (int j = 0; j < 32; ++j)
+                            *(uint16_t *)(stage + staged_at(j, lane >> 3) + (lane & 7) * 2) = (uint16_t)pack2<F16>(v[j], 0.f);
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 4; ++j)
+                            *(uint4 *)(stage + staged_at(lane, j)) =
+                                make_uint4(pack2<F16>(v[8 * j], v[8 * j + 1]), pack2<F16>(v[8 * j + 2], v[8 * j + 3]),
+                                           pack2<F16>(v[8 * j + 4], v[8 * j + 5]), pack2<F16>(v[8 * j + 6], v[8 * j + 7]));
+                    }
+                    __syncwarp();
+                    const int n = grouped ? w.ot * GP_TILE + rank * 128 + quad * 32 + piece : w.ot * p.bn + c + piece;
+                    const int left = p.n - n;
+                    uint16_t *dst[4];
+                    uint4 d[4];
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const int j = q * 8 + (lane >> 2);
+                        d[q] = *(const uint4 *)(stage + staged_at(j, lane & 3));
+                        dst[q] = base[q];
+                        if (grouped) {
+                            const int at = c + j < cols ? t.rows[c + j] : -1;
+                            dst[q] = at < 0 ? nullptr : out0 + (int64_t)at * p.ld;
+                        }
+                    }
+                    if (left >= 8 && (grouped || c + piece < cols)) {
+#pragma unroll
+                        for (int q = 0; q < 4; ++q)
+                            if (dst[q]) *(uint4 *)(dst[q] + n) = d[q];
+                    } else if (left > 0 && (grouped || c + piece < cols)) {
+#pragma unroll
+                        for (int q = 0; q < 4; ++q)
+                            if (dst[q])
+                                for (int k = 0; k < left; ++k)
+                                    dst[q][n + k] = ((const uint16_t *)(stage + staged_at(q * 8 + (lane >> 2), lane & 3)))[k];
+                    }
+                    __syncwarp();
+                } else if (grouped) {
+                    const int n = w.ot * GP_TILE + rank * 128 + row;
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) {
+                        const int at = mine && c + j < cols ? t.rows[c + j] : -1;
+                        if (at >= 0) out0[(int64_t)at * p.ld + n] = (uint16_t)pack2<F16>(v[j], 0.f);
+                    }
+                } else if (low) {
+                    // blocks of 64 columns: the products with the high terms of 32
+                    // ranks, then those with the low terms
+                    const int r0 = (w.ot * p.bn + c) >> 6 << 5, left = p.rank_out - r0;
+                    if (c & 32) {
+                        uint16_t *out = out0 + w.g * p.gstride;
+                        const int64_t m = w.xt * GP_TILE + rank * 128 + row;
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) v[j] += prev[j];
+                        if (mine && left > 0) {
+                            if (p.out_kind == GP_OUT_LOW)
+                                store_row<F16>(out + m * p.ld + r0, v, min(32, left), p.vec);
+                            else
+#pragma unroll
+                                for (int j = 0; j < 32; ++j)
+                                    if (j < left) out[(r0 + j) * p.ld + m] = (uint16_t)pack2<F16>(v[j], 0.f);
+                        }
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) prev[j] = v[j];
+                    }
+                } else if (pack) {
+                    // 32 ranks of an inner product: value = high + low term, to about
+                    // twice the type's precision; an infinite high term takes a zero
+                    // low one (not inf - inf)
+                    const float sc = p.scale[w.g];
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) {
+                        v[j] = c + j < p.n ? v[j] * sc : 0.f;
+                        const float hi = widen<F16>((uint16_t)pack2<F16>(v[j], 0.f));
+                        prev[j] = isinf(hi) ? 0.f : v[j] - hi;
+                    }
+                    if (mine) {
+                        uint16_t *dst = out0 + (int64_t)(w.first + rank * 128 + r) * p.ld + c * 2;
+                        store_row<F16>(dst, v, 32, true);
+                        store_row<F16>(dst + 32, prev, 32, true);
+                    }
+                } else {
+                    uint16_t *dst = out_row(r);
+                    if (dst) store_row<F16>(dst + w.ot * p.bn + c, v, min(32, cols - c), p.vec);
+                }
             }
-            tc_fence_before();
-            mbar_arrive(&t.acce[b]);
+            if (held) release();                // (no chunk was this warp's)
+            named_bar_sync(1, threads);         // t.rows and t.go may be written again
         }
     }
     tc_fence_before();
     __syncthreads();
-    if (warp == 5) {
-        __syncwarp();
+    cluster_sync();          // no MMA reads this CTA's memory, no arrival is on its way
+    if (warp == 9) {
         tc_fence_after();
-        tmem_dealloc(tmem, tcols);
+        tmem_dealloc_pair(tmem, 2 * CS);
     }
+}
+
+using Kernel = void (*)(GroupMaps, GroupProduct);
+
+Kernel kernel_of(int f16, int kind) {
+    static const Kernel all[2][5] = {
+        {k_group<false, 0>, k_group<false, 1>, k_group<false, 2>, k_group<false, 3>, k_group<false, 4>},
+        {k_group<true, 0>, k_group<true, 1>, k_group<true, 2>, k_group<true, 3>, k_group<true, 4>}};
+    return all[f16][kind];
+}
+
+int kind_of(const GroupProduct &p) {
+    if (p.mode == GP_GROUPED) return K_GROUPED;
+    if (p.mode == GP_ROWS) return p.shared ? K_SHARED : K_PACK;
+    return p.out_kind == GP_OUT_GROUP ? K_GRAD : K_LOW;
 }
 
 }  // namespace
 
-cudaError_t group_prepare() {
-    const auto attr = cudaFuncAttributeMaxDynamicSharedMemorySize;
-    cudaError_t e = cudaFuncSetAttribute(k_group<false>, attr, SMEM_MAX);
-    if (e == cudaSuccess) e = cudaFuncSetAttribute(k_group<true>, attr, SMEM_MAX);
+cudaError_t group_prepare(int nsm, int *ctas) {
+    cudaError_t e = cudaSuccess;
+    for (int kind = 0; kind < 5 && e == cudaSuccess; ++kind)
+        for (int f16 = 0; f16 < 2 && e == cudaSuccess; ++f16)
+            e = cudaFuncSetAttribute((const void *)kernel_of(f16, kind), cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                     SMEM_MAX);
+    if (e != cudaSuccess) return e;
+    // the pairs that run at once: the walk deals its pieces to that many
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = 2;
+    at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+    cfg.gridDim = dim3((unsigned)nsm / 2 * 2);
+    cfg.blockDim = dim3(THREADS);
+    cfg.dynamicSmemBytes = SMEM_MAX;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    int pairs = 0;
+    e = cudaOccupancyMaxActiveClusters(&pairs, (const void *)kernel_of(0, K_SHARED), &cfg);
+    if (e == cudaSuccess && pairs < 1) e = cudaErrorLaunchOutOfResources;
+    *ctas = 2 * (pairs < nsm / 2 ? pairs : nsm / 2);
     return e;
 }
 
-size_t group_part_floats(int nsm) { return (size_t)nsm * 2 * GP_BM * GP_MAX_BN; }
+size_t group_part_floats(int ctas) { return (size_t)ctas * 2 * 128 * GP_TILE; }
 
 void group_plan(GroupProduct *p) {
-    const int bb = p->wgrad || p->b_mn ? (p->bn + 63) / 64 * 8192 : p->bn * 128;
-    // an extension stage holds bn x 32 ranks: never more than an ordinary one
-    p->stage_bytes = A_BYTES + bb;
-    const int fit = STAGE_ROOM / p->stage_bytes;
+    // B side: whole 1 KB; MN-major operands come in blocks of 64 columns
+    int b = (p->sorted ? (p->bn / 2 + GP_ROW_BOX - 1) / GP_ROW_BOX * GP_ROW_BOX : p->bn / 2) * 128;
+    if (p->mode == GP_WGRAD || (p->mode == GP_ROWS && p->dense_mn)) b = (p->bn / 2 + 63) / 64 * 8192;
+    p->stage_bytes = A_BYTES + (b + 1023) / 1024 * 1024;
+    const int fit = (SMEM_MAX - 1024 - table_bytes(*p)) / p->stage_bytes;
     p->stages = fit < MAX_STAGES ? fit : MAX_STAGES;
-    p->ntiles = (p->n + p->bn - 1) / p->bn;
-    p->mtiles = (p->m + GP_BM - 1) / GP_BM;
+    p->smem = 1024 + p->stages * p->stage_bytes + table_bytes(*p);
+    p->ntiles = (p->n + (p->mode == GP_GROUPED ? GP_TILE : p->bn) - 1) / (p->mode == GP_GROUPED ? GP_TILE : p->bn);
+    p->mtiles = (p->m + GP_TILE - 1) / GP_TILE;
 }
 
-cudaError_t launch_group(const GroupProduct &p, const GroupMaps &maps, int nsm, cudaStream_t s) {
-    const size_t smem = 1024 + (size_t)p.stages * p.stage_bytes + sizeof(Tables);
-    if (p.f16) k_group<true><<<nsm, THREADS, smem, s>>>(maps, p);
-    else k_group<false><<<nsm, THREADS, smem, s>>>(maps, p);
-    return cudaGetLastError();
+cudaError_t launch_group(const GroupProduct &p, const GroupMaps &maps, int ctas, cudaStream_t s) {
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.gridDim = dim3((unsigned)ctas);
+    cfg.blockDim = dim3(THREADS);
+    cfg.dynamicSmemBytes = (size_t)p.smem;
+    cfg.stream = s;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel_of(p.f16 != 0, kind_of(p)), maps, p);
 }
 
 }  // namespace hwr

@@ -157,6 +157,81 @@ k_dispatch_place(int rows, int G, int64_t per_block, const int32_t *choice, cons
 size_t place_smem(int G) { return (size_t)(DP_WARPS + 3) * (G + 1) * 4; }
 
 // ---------------------------------------------------------------------------
+// Rows by place: a warp copies a row (reads and writes of 512 bytes at a time).
+
+constexpr int SR_THREADS = 256;
+
+__global__ void __launch_bounds__(SR_THREADS)
+k_sort_rows(const __grid_constant__ GroupPlan plan, const __grid_constant__ SortRows m, int places,
+            int32_t *padded_offsets, int32_t *padded_order) {
+    extern __shared__ int32_t sh[];
+    const int G = plan.groups, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    int32_t *offs = sh, *pad = sh + G + 1;       // first place of each group, in either plan
+    int total = plan.rows;
+    if (padded_offsets) {
+        for (int i = threadIdx.x; i <= G; i += SR_THREADS) {
+            const int v = plan.offsets[i];
+            offs[i] = v < 0 ? 0 : v > plan.rows ? plan.rows : v;
+        }
+        __syncthreads();
+        if (warp == 0) {
+            int run = 0;
+            for (int g0 = 0; g0 < G; g0 += 32) {
+                const int g = g0 + lane;
+                int v = g < G ? (max(0, offs[g + 1] - offs[g]) + 15) & ~15 : 0;
+                const int own = v;
+#pragma unroll
+                for (int d = 1; d < 32; d *= 2) {
+                    const int o = __shfl_up_sync(0xffffffffu, v, d);
+                    if (lane >= d) v += o;
+                }
+                if (g < G) pad[g] = run + v - own;
+                run += __shfl_sync(0xffffffffu, v, 31);
+            }
+            if (lane == 0) pad[G] = run;
+        }
+        __syncthreads();
+        total = min(pad[G] + plan.rows - offs[G], places);
+        if (blockIdx.x == 0) {
+            for (int i = threadIdx.x; i <= G; i += SR_THREADS) padded_offsets[i] = pad[i];
+            if (threadIdx.x == 0) padded_offsets[G + 1] = total;
+        }
+    }
+    for (int64_t at = blockIdx.x * (SR_THREADS / 32) + warp; at < total; at += (int64_t)gridDim.x * (SR_THREADS / 32)) {
+        int place = (int)at;
+        if (padded_offsets) {
+            int lo = 0, hi = G;
+            while (lo < hi) {                    // last group that begins at or before the place
+                const int mid = (lo + hi + 1) >> 1;
+                if (pad[mid] <= at) lo = mid;
+                else hi = mid - 1;
+            }
+            place = offs[lo] + (int)(at - pad[lo]);
+            if (lo < G && place >= offs[lo + 1]) place = -1;
+        }
+        int r = place >= 0 && place < plan.rows ? plan.order[place] : -1;
+        if ((uint32_t)r >= (uint32_t)plan.rows) r = -1;
+        if (padded_offsets && lane == 0) padded_order[at] = r;
+        for (int k = 0; k < m.n; ++k) {
+            uint4 *dst = (uint4 *)(m.dst[k] + at * m.dst_ld[k]);
+            const int units = (int)(m.dst_ld[k] / 8), cols = m.cols[k];
+            const uint16_t *src = r < 0 ? nullptr : m.src[k] + r * m.src_ld[k];
+            if (src && ((uintptr_t)src & 15) == 0 && cols % 8 == 0) {
+#pragma unroll 4
+                for (int i = lane; i < units; i += 32) dst[i] = __ldg((const uint4 *)src + i);
+                continue;
+            }
+            for (int i = lane; i < units; i += 32) {
+                uint32_t v[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] = src && i * 8 + j < cols ? src[i * 8 + j] : 0;
+                dst[i] = make_uint4(v[0] | v[1] << 16, v[2] | v[3] << 16, v[4] | v[5] << 16, v[6] | v[7] << 16);
+            }
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------
 // Padding copy of 16-bit elements.
 
 __global__ void __launch_bounds__(256)
@@ -393,6 +468,14 @@ cudaError_t launch_dispatch(int rows, int groups, const int32_t *choice, int32_t
         k_dispatch_count<<<b, DP_THREADS, (groups + 1) * 4, s>>>(rows, groups, per, choice, scratch);
     k_dispatch_place<<<b, DP_THREADS, place_smem(groups), s>>>(rows, groups, per, choice,
                                                               b > 1 ? scratch : nullptr, offsets, order);
+    return cudaGetLastError();
+}
+
+cudaError_t launch_sort_rows(const GroupPlan &plan, const SortRows &m, int places, int32_t *padded_offsets,
+                             int32_t *padded_order, int nsm, cudaStream_t s) {
+    const int64_t want = ((int64_t)places + SR_THREADS / 32 - 1) / (SR_THREADS / 32), most = (int64_t)nsm * 8;
+    k_sort_rows<<<(int)(want < most ? want : most), SR_THREADS, (plan.groups + 1) * 8, s>>>(plan, m, places, padded_offsets,
+                                                                                            padded_order);
     return cudaGetLastError();
 }
 

@@ -34,7 +34,7 @@ struct ApiRange {
 struct hwr_ops {
     cudaStream_t stream = nullptr;
     bool own_stream = false, broken = false;
-    int nsm = 1;
+    int nsm = 1, ctas = 2;       // SMs; CTAs of the grouped products
     std::string err;
     char *ws = nullptr;
     size_t ws_cap = 0;
@@ -131,7 +131,7 @@ extern "C" hwr_status hwr_ops_create(void *cuda_stream, hwr_ops **out) {
                 return fail(c, HWR_ERR_CUDA, "the driver has no cuTensorMapEncodeTiled");
             g_encode = (PFN_cuTensorMapEncodeTiled_v12000)fn;
         }
-        CK(c, group_prepare(), "kernel attributes");
+        CK(c, group_prepare(c->nsm, &c->ctas), "kernel attributes");
         CK(c, ops_prepare(), "kernel attributes");
         if (cuda_stream) {
             c->stream = (cudaStream_t)cuda_stream;
@@ -142,11 +142,11 @@ extern "C" hwr_status hwr_ops_create(void *cuda_stream, hwr_ops **out) {
         CK(c, cudaHostAlloc((void **)&c->status_h, 64, cudaHostAllocMapped), "status word");
         memset(c->status_h, 0, 64);
         CK(c, cudaHostGetDevicePointer((void **)&c->status_d, c->status_h, 0), "status word");
-        OK(alloc(c, &c->part, group_part_floats(c->nsm)));
-        OK(alloc(c, &c->count, c->nsm));
+        OK(alloc(c, &c->part, group_part_floats(c->ctas)));
+        OK(alloc(c, &c->count, c->ctas));
         c->sums_cap = clip_blocks(INT64_MAX, c->nsm);
         OK(alloc(c, &c->sums, c->sums_cap));
-        CK(c, cudaMemsetAsync(c->count, 0, c->nsm * sizeof(uint32_t), c->stream), "memset");
+        CK(c, cudaMemsetAsync(c->count, 0, c->ctas * sizeof(uint32_t), c->stream), "memset");
         return HWR_OK;
     };
     const hwr_status s = body();
@@ -265,13 +265,14 @@ static hwr_status settle(hwr_ops *c, Operand *o) {
     return HWR_OK;
 }
 
-static hwr_status encode(hwr_ops *c, CUtensorMap *m, bool f16, const Operand &o, int rank, int box0, int box1) {
+// A map over nz matrices: boxes of box0 columns (64: 128-byte swizzle, 32: 64-byte) x box1 rows.
+static hwr_status encode(hwr_ops *c, CUtensorMap *m, bool f16, const Operand &o, int box0, int box1) {
     const cuuint64_t dims[3] = {(cuuint64_t)o.cols, (cuuint64_t)o.rows, (cuuint64_t)o.nz};
     const cuuint64_t strides[2] = {(cuuint64_t)o.ld * 2, (cuuint64_t)o.z * 2};
     const cuuint32_t box[3] = {(cuuint32_t)box0, (cuuint32_t)box1, 1};
     const cuuint32_t estr[3] = {1, 1, 1};
     const CUresult r = g_encode(
-        m, f16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, rank, const_cast<void *>(o.p),
+        m, f16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void *>(o.p),
         dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
         box0 == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
         CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
@@ -281,15 +282,83 @@ static hwr_status encode(hwr_ops *c, CUtensorMap *m, bool f16, const Operand &o,
     return HWR_OK;
 }
 
-// Rows of the result scattered or not: 16-byte stores where the rows allow them.
+// 16-byte stores where the rows of the result allow them.
 static int vec_ok(const void *p, int64_t ld, int64_t z) { return on16(p, ld, z, 2); }
 
-static GroupProduct product(hwr_ops *c, const hwr_rows *r) {
+// What the products of a call share: the plan and the rows of its inputs, by
+// place (copied to the workspace) or where the caller has them.
+struct Rows {
+    GroupPlan plan;
+    bool sorted = false;
+    Operand x, dy;
+    size_t offsets_off = 0, order_off = 0;     // padded plan
+};
+
+// Rows that are few are picked by index: they cost no copy, and the weights'
+// bytes bound the product (64 rows x 12 groups, 1024 -> 4096: 42 us picked).
+// More of them are copied by place once.
+constexpr int PICK_ROWS = 256;
+
+// contracted: a gradient contracts over the rows, which takes the padded plan.
+static Rows plan_rows(Carver &cv, const hwr_rows *r, const void *dy, int64_t dy_ld, bool need_x, bool contracted) {
+    Rows s;
+    s.plan.rows = s.plan.places = r->rows;
+    s.plan.groups = r->groups;
+    s.plan.offsets = r->offsets;
+    s.plan.order = r->order;
+    auto operand = [&](const void *p, int64_t ld, int cols) {
+        Operand o;
+        o.p = p;
+        o.ld = ld;
+        o.rows = r->rows;
+        o.cols = cols;
+        return o;
+    };
+    if (need_x) s.x = operand(r->x, r->x_ld, r->n_in);
+    if (dy) s.dy = operand(dy, dy_ld, r->n_out);
+    s.sorted = contracted || r->rows > PICK_ROWS || (need_x && !on16(r->x, r->x_ld, 0, 1)) ||
+               (dy && !on16(dy, dy_ld, 0, 1));
+    if (!s.sorted) return s;
+    if (contracted) {
+        s.plan.padded = 1;
+        s.plan.places = r->rows + 15 * (r->rows < r->groups ? r->rows : r->groups);
+        s.offsets_off = cv.take((size_t)(r->groups + 2) * 4);
+        s.order_off = cv.take((size_t)s.plan.places * 4);
+    }
+    if (need_x) s.x.off = cv.take((size_t)s.plan.places * up(r->n_in, 8) * 2);
+    if (dy) s.dy.off = cv.take((size_t)s.plan.places * up(r->n_out, 8) * 2);
+    return s;
+}
+
+static hwr_status sort_rows(hwr_ops *c, Rows *s) {
+    if (!s->sorted) return HWR_OK;
+    SortRows m;
+    for (Operand *o : {&s->x, &s->dy}) {
+        if (!o->p) continue;
+        m.src[m.n] = (const uint16_t *)o->p;
+        m.src_ld[m.n] = o->ld;
+        m.cols[m.n] = o->cols;
+        o->p = c->ws + o->off;
+        o->ld = up(o->cols, 8);
+        o->rows = s->plan.places;
+        m.dst[m.n] = (uint16_t *)(c->ws + o->off);
+        m.dst_ld[m.n++] = o->ld;
+    }
+    int32_t *offsets = s->plan.padded ? (int32_t *)(c->ws + s->offsets_off) : nullptr;
+    int32_t *order = s->plan.padded ? (int32_t *)(c->ws + s->order_off) : nullptr;
+    CK(c, launch_sort_rows(s->plan, m, s->plan.places, offsets, order, c->nsm, c->stream), "row copy");
+    if (s->plan.padded) {
+        s->plan.offsets = offsets;
+        s->plan.order = order;
+    }
+    for (Operand *o : {&s->x, &s->dy}) o->z = up(o->ld * o->rows, 8);
+    return HWR_OK;
+}
+
+static GroupProduct product(hwr_ops *c, const hwr_rows *r, const Rows &s) {
     GroupProduct p;
-    p.rows = r->rows;
-    p.groups = r->groups;
-    p.offsets = r->offsets;
-    p.order = r->order;
+    p.plan = s.plan;
+    p.sorted = s.sorted;
     p.f16 = r->dtype == HWR_F16;
     p.part = c->part;
     p.count = c->count;
@@ -303,48 +372,56 @@ static int even_tiles(int n, int most) {
     return (int)up((n + tiles - 1) / tiles, 16);
 }
 
-// out[t] = W[g(t)] x[t] (b K-major: [out][in]) or W[g(t)]^T x[t] (b_mn).
-static hwr_status rows_product(hwr_ops *c, GroupProduct p, const Operand &x, const Operand &b, bool b_mn, int k,
-                               int n, const Operand *u, const Operand *eb) {
-    p.k = k;
+static hwr_status check_tiles(hwr_ops *c, const GroupProduct &p) {
+    if (((int64_t)p.plan.places / GP_TILE + 1) * p.plan.groups * p.ntiles > INT32_MAX)
+        return fail(c, HWR_ERR_UNSUPPORTED, "rows %d x groups %d x columns %d is too large", p.plan.rows, p.plan.groups,
+                    p.n);
+    return HWR_OK;
+}
+
+// out[t] = W[g(t)] x[t] (w K-major: [out][in]) or W[g(t)]^T x[t] (w_mn).
+static hwr_status rows_product(hwr_ops *c, GroupProduct p, const Operand &x, const Operand &w, bool w_mn, int n,
+                               const Operand *u, const Operand *eb) {
+    p.k = x.cols;
     p.n = n;
-    p.b_mn = b_mn;
-    p.ext_b_mn = b_mn;
-    // few rows a group: the weights' bytes bound the product, and narrower
-    // tiles spread them more evenly over the SMs
-    const int64_t per = p.rows / p.groups;
-    p.bn = even_tiles(n, per < 48 && p.out_kind != GP_OUT_PACK ? 128 : GP_MAX_BN);
-    p.mma_n = p.bn;
+    p.dense_mn = w_mn;
+    if (!p.sorted) {
+        p.x = (const uint16_t *)x.p;
+        p.x_ld = x.ld;
+    }
+    if (p.mode == GP_GROUPED) p.bn = (int)up(p.plan.places < GP_TILE ? p.plan.places : GP_TILE, 16);
+    else p.bn = even_tiles(n, GP_TILE);
     group_plan(&p);
-    if (((int64_t)p.rows / GP_BM + 1) * p.groups * p.ntiles > INT32_MAX)
-        return fail(c, HWR_ERR_UNSUPPORTED, "rows %d x groups %d x columns %d is too large", p.rows, p.groups, n);
+    OK(check_tiles(c, p));
     GroupMaps m;
     memset(&m, 0, sizeof m);
-    OK(encode(c, &m.a, p.f16, x, 2, 64, 1));
-    OK(encode(c, &m.b, p.f16, b, 3, 64, b_mn ? 64 : p.bn));
-    if (u) {
-        OK(encode(c, &m.u, p.f16, *u, 2, 64, 1));
-        OK(b_mn ? encode(c, &m.eb, p.f16, *eb, 3, 64, GP_RC) : encode(c, &m.eb, p.f16, *eb, 3, GP_RC, p.bn));
+    if (p.sorted) {
+        OK(encode(c, &m.x, p.f16, x, 64, GP_ROW_BOX));
+        OK(encode(c, &m.xx, p.f16, x, 64, 128));
     }
-    CK(c, launch_group(p, m, c->nsm, c->stream), "grouped product kernel");
+    OK(encode(c, &m.w, p.f16, w, 64, w_mn ? 64 : p.mode == GP_GROUPED ? 128 : p.bn / 2));
+    if (u) {
+        OK(encode(c, &m.u, p.f16, *u, 64, GP_ROW_BOX));
+        OK(w_mn ? encode(c, &m.eb, p.f16, *eb, 64, GP_RC) : encode(c, &m.eb, p.f16, *eb, GP_RC, p.bn / 2));
+    }
+    CK(c, launch_group(p, m, c->ctas, c->stream), "product kernel");
     return HWR_OK;
 }
 
 // out[g] = sum over the rows of g of l[t] r[t]^T.
 static hwr_status grad_product(hwr_ops *c, GroupProduct p, const Operand &l, const Operand &r) {
-    p.wgrad = 1;
+    p.mode = GP_WGRAD;
     p.m = l.cols;
     p.n = r.cols;
-    p.bn = p.out_kind == GP_OUT_GROUP ? even_tiles(p.n, GP_MAX_BN) : p.n < GP_MAX_BN ? p.n : GP_MAX_BN;
-    p.mma_n = p.bn;
+    p.bn = p.out_kind == GP_OUT_GROUP ? even_tiles(p.n, GP_TILE) : p.n < GP_TILE ? p.n : GP_TILE;
     group_plan(&p);
-    if ((int64_t)p.groups * p.mtiles * p.ntiles > INT32_MAX)
-        return fail(c, HWR_ERR_UNSUPPORTED, "groups %d x %d x %d is too large", p.groups, p.m, p.n);
+    if ((int64_t)p.plan.groups * p.mtiles * p.ntiles > INT32_MAX)
+        return fail(c, HWR_ERR_UNSUPPORTED, "groups %d x %d x %d is too large", p.plan.groups, p.m, p.n);
     GroupMaps m;
     memset(&m, 0, sizeof m);
-    OK(encode(c, &m.a, p.f16, l, 2, 64, 1));
-    OK(encode(c, &m.b, p.f16, r, 2, 64, 1));
-    CK(c, launch_group(p, m, c->nsm, c->stream), "weight gradient kernel");
+    OK(encode(c, &m.x, p.f16, l, 64, GP_BK));
+    OK(encode(c, &m.w, p.f16, r, 64, GP_BK));
+    CK(c, launch_group(p, m, c->ctas, c->stream), "weight gradient kernel");
     return HWR_OK;
 }
 
@@ -379,17 +456,18 @@ extern "C" hwr_status hwr_grouped_forward(hwr_ops *c, const hwr_rows *r, void *y
     OK(check_out(c, r, y, y_ld, r->n_out, "y"));
     if (r->rows == 0) return HWR_OK;
     Carver cv;
-    Operand x = cv.operand(r->x, r->x_ld, r->rows, r->n_in);
+    Rows rows = plan_rows(cv, r, nullptr, 0, true, false);
     Operand w = cv.operand(r->w, r->w_ld, r->n_out, r->n_in, r->w_group, r->groups);
     OK(reserve(c, cv.at));
-    OK(settle(c, &x));
+    OK(sort_rows(c, &rows));
     OK(settle(c, &w));
-    GroupProduct p = product(c, r);
+    GroupProduct p = product(c, r, rows);
+    p.mode = GP_GROUPED;
     p.out_kind = GP_OUT_ROWS;
     p.out = y;
     p.ld = y_ld;
     p.vec = vec_ok(y, y_ld, 0);
-    return rows_product(c, p, x, w, false, r->n_in, r->n_out, nullptr, nullptr);
+    return rows_product(c, p, rows.x, w, false, r->n_out, nullptr, nullptr);
 }
 
 extern "C" hwr_status hwr_grouped_backward(hwr_ops *c, const hwr_rows *r, const void *dy, int64_t dy_ld, void *dx,
@@ -406,30 +484,31 @@ extern "C" hwr_status hwr_grouped_backward(hwr_ops *c, const hwr_rows *r, const 
                                     (size_t)r->n_in * 2, r->n_out, c->stream), "memset");
         return HWR_OK;
     }
+    if (!dx && !dw) return HWR_OK;
     Carver cv;
-    Operand d = cv.operand(dy, dy_ld, r->rows, r->n_out), x, w;
-    if (dw) x = cv.operand(r->x, r->x_ld, r->rows, r->n_in);
+    Rows rows = plan_rows(cv, r, dy, dy_ld, dw != nullptr, dw != nullptr);
+    Operand w;
     if (dx) w = cv.operand(r->w, r->w_ld, r->n_out, r->n_in, r->w_group, r->groups);
     OK(reserve(c, cv.at));
-    OK(settle(c, &d));
+    OK(sort_rows(c, &rows));
     if (dx) {
         OK(settle(c, &w));
-        GroupProduct p = product(c, r);
+        GroupProduct p = product(c, r, rows);
+        p.mode = GP_GROUPED;
         p.out_kind = GP_OUT_ROWS;
         p.out = dx;
         p.ld = dx_ld;
         p.vec = vec_ok(dx, dx_ld, 0);
-        OK(rows_product(c, p, d, w, true, r->n_out, r->n_in, nullptr, nullptr));
+        OK(rows_product(c, p, rows.dy, w, true, r->n_in, nullptr, nullptr));
     }
     if (dw) {
-        OK(settle(c, &x));
-        GroupProduct p = product(c, r);
+        GroupProduct p = product(c, r, rows);
         p.out_kind = GP_OUT_GROUP;
         p.out = dw;
         p.ld = r->w_ld;
         p.gstride = r->groups > 1 ? r->w_group : 0;
         p.vec = vec_ok(dw, r->w_ld, p.gstride);
-        OK(grad_product(c, p, d, x));
+        OK(grad_product(c, p, rows.dy, rows.x));
     }
     return HWR_OK;
 }
@@ -442,26 +521,44 @@ static hwr_status check_adapters(hwr_ops *c, const hwr_rows *r, const hwr_adapte
     return HWR_OK;
 }
 
-// scale[g] x[t] M[g] per row, as two 16-bit terms: [rows][32-rank chunks][high, low].
-static hwr_status low_rank(hwr_ops *c, const hwr_rows *r, const hwr_adapters *ad, const Operand &x,
-                           const Operand &m, bool m_mn, int k, const Operand &u) {
-    GroupProduct p = product(c, r);
+// scale[g] M[g] x[t] (or M[g]^T x[t]) by place, as two 16-bit terms: [places]
+// [32-rank chunks][high, low], an even number of chunks.
+static hwr_status low_rank(hwr_ops *c, const hwr_rows *r, const hwr_adapters *ad, const Rows &rows, const Operand &x,
+                           const Operand &m, bool m_mn, const Operand &u) {
+    GroupProduct p = product(c, r, rows);
+    p.mode = GP_ROWS;
     p.out_kind = GP_OUT_PACK;
     p.out = const_cast<void *>(u.p);
     p.ld = u.ld;
     p.vec = 1;
     p.scale = ad->scale;
-    return rows_product(c, p, x, m, m_mn, k, ad->rank, nullptr, nullptr);
+    return rows_product(c, p, x, m, m_mn, ad->rank, nullptr, nullptr);
 }
 
-// The packed inner product's place in the workspace.
-static Operand packed(Carver &cv, const hwr_rows *r, const hwr_adapters *ad) {
+// The packed inner products' place in the workspace.
+static Operand packed(Carver &cv, const Rows &rows, const hwr_adapters *ad) {
     Operand u;
-    u.cols = (int)up(ad->rank, GP_RC) * 2;
+    u.cols = (int)up(ad->rank, 2 * GP_RC) * 2;
     u.ld = u.cols;
-    u.rows = r->rows;
+    u.rows = rows.plan.places;
+    u.z = up(u.ld * u.rows, 8);
     u.off = cv.take((size_t)u.rows * u.ld * 2);
     return u;
+}
+
+// W x[t] (or W^T x[t]) and the extension of t's group.
+static hwr_status shared_product(hwr_ops *c, const hwr_rows *r, const hwr_adapters *ad, const Rows &rows,
+                                 const Operand &x, const Operand &w, bool w_mn, const Operand &u, const Operand &eb,
+                                 void *out, int64_t ld, int n) {
+    GroupProduct p = product(c, r, rows);
+    p.mode = GP_ROWS;
+    p.shared = 1;
+    p.rank = ad->rank;
+    p.out_kind = GP_OUT_ROWS;
+    p.out = out;
+    p.ld = ld;
+    p.vec = vec_ok(out, ld, 0);
+    return rows_product(c, p, x, w, w_mn, n, &u, &eb);
 }
 
 extern "C" hwr_status hwr_adapter_forward(hwr_ops *c, const hwr_rows *r, const hwr_adapters *ad, void *y,
@@ -475,28 +572,19 @@ extern "C" hwr_status hwr_adapter_forward(hwr_ops *c, const hwr_rows *r, const h
     if (r->rows == 0) return HWR_OK;
     const int K = r->n_in, N = r->n_out, R = ad->rank, G = r->groups;
     Carver cv;
-    Operand x = cv.operand(r->x, r->x_ld, r->rows, K);
+    Rows rows = plan_rows(cv, r, nullptr, 0, true, false);
     Operand w = cv.operand(r->w, r->w_ld, N, K);
     Operand a = cv.operand(ad->a, K, R, K, (int64_t)R * K, G);
     Operand b = cv.operand(ad->b, R, N, R, (int64_t)N * R, G);
-    Operand u = packed(cv, r, ad);
+    Operand u = packed(cv, rows, ad);
     OK(reserve(c, cv.at));
     u.p = c->ws + u.off;
-    OK(settle(c, &x));
+    OK(sort_rows(c, &rows));
     OK(settle(c, &a));
-    OK(low_rank(c, r, ad, x, a, false, K, u));
     OK(settle(c, &w));
     OK(settle(c, &b));
-    GroupProduct p = product(c, r);
-    p.shared = 1;
-    p.groups = 1;
-    p.ext_groups = G;
-    p.rank = R;
-    p.out_kind = GP_OUT_ROWS;
-    p.out = y;
-    p.ld = y_ld;
-    p.vec = vec_ok(y, y_ld, 0);
-    return rows_product(c, p, x, w, false, K, N, &u, &b);
+    OK(low_rank(c, r, ad, rows, rows.x, a, false, u));
+    return shared_product(c, r, ad, rows, rows.x, w, false, u, b, y, y_ld, N);
 }
 
 extern "C" hwr_status hwr_adapter_backward(hwr_ops *c, const hwr_rows *r, const hwr_adapters *ad, const void *dy,
@@ -516,57 +604,45 @@ extern "C" hwr_status hwr_adapter_backward(hwr_ops *c, const hwr_rows *r, const 
     }
     if (!dx && !da && !db) return HWR_OK;
     Carver cv;
-    Operand d = cv.operand(dy, dy_ld, r->rows, N), x, w, a, b, u, v;
-    if (da || db) x = cv.operand(r->x, r->x_ld, r->rows, K);
+    Rows rows = plan_rows(cv, r, dy, dy_ld, da || db, da || db);
+    Operand w, a, b, u, v;
     if (dx) w = cv.operand(r->w, r->w_ld, N, K);
     if (dx || db) a = cv.operand(ad->a, K, R, K, (int64_t)R * K, G);
     if (dx || da) {
         b = cv.operand(ad->b, R, N, R, (int64_t)N * R, G);
-        v = packed(cv, r, ad);
+        v = packed(cv, rows, ad);
     }
-    if (db) u = packed(cv, r, ad);
+    if (db) u = packed(cv, rows, ad);
     OK(reserve(c, cv.at));
-    OK(settle(c, &d));
+    u.p = c->ws + u.off;
+    v.p = c->ws + v.off;
+    OK(sort_rows(c, &rows));
+    if (dx) OK(settle(c, &w));
+    if (dx || db) OK(settle(c, &a));
     if (dx || da) {
         OK(settle(c, &b));
-        v.p = c->ws + v.off;
-        OK(low_rank(c, r, ad, d, b, true, N, v));
+        OK(low_rank(c, r, ad, rows, rows.dy, b, true, v));
     }
-    if (dx || db) OK(settle(c, &a));
-    if (dx) {
-        OK(settle(c, &w));
-        GroupProduct p = product(c, r);
-        p.shared = 1;
-        p.groups = 1;
-        p.ext_groups = G;
-        p.rank = R;
-        p.out_kind = GP_OUT_ROWS;
-        p.out = dx;
-        p.ld = dx_ld;
-        p.vec = vec_ok(dx, dx_ld, 0);
-        OK(rows_product(c, p, d, w, true, N, K, &v, &a));
-    }
-    if (da || db) OK(settle(c, &x));
+    if (db) OK(low_rank(c, r, ad, rows, rows.x, a, false, u));
+    if (dx) OK(shared_product(c, r, ad, rows, rows.dy, w, true, v, a, dx, dx_ld, K));
     if (da) {
-        GroupProduct p = product(c, r);
+        GroupProduct p = product(c, r, rows);
         p.out_kind = GP_OUT_LOW_T;
         p.out = da;
         p.ld = K;
         p.gstride = (int64_t)R * K;
         p.rank_out = R;
-        OK(grad_product(c, p, x, v));
+        OK(grad_product(c, p, rows.x, v));
     }
     if (db) {
-        u.p = c->ws + u.off;
-        OK(low_rank(c, r, ad, x, a, false, K, u));
-        GroupProduct p = product(c, r);
+        GroupProduct p = product(c, r, rows);
         p.out_kind = GP_OUT_LOW;
         p.out = db;
         p.ld = R;
         p.gstride = (int64_t)N * R;
         p.rank_out = R;
         p.vec = vec_ok(db, R, p.gstride);
-        OK(grad_product(c, p, d, u));
+        OK(grad_product(c, p, rows.dy, u));
     }
     return HWR_OK;
 }

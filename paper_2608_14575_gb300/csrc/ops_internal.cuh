@@ -17,40 +17,58 @@ constexpr int OPS_MAX_RANK = HWR_OPS_MAX_RANK;
 
 // ---- products with ragged groups of rows (k_group.cu) -----------------------
 
-constexpr int GP_BM = 128;         // rows of a tile (TMEM lanes)
-constexpr int GP_MAX_BN = 256;     // columns of a tile
+constexpr int GP_TILE = 256;       // rows of a tile's A side; B side: up to 256 in steps of 16
 constexpr int GP_BK = 64;          // contraction of a pipeline stage
-constexpr int GP_RC = 32;          // ranks of an extension stage (high and low halves: 64 columns)
+constexpr int GP_RC = 32;          // ranks of an extension stage (high and low terms: 64 columns)
+
+// Which operand holds the rows of x.
+enum : int {
+    GP_GROUPED = 0,    // B side: out^T tile = W[g] tile (A) x rows (B): a ragged group costs
+                       // whole 16s of rows
+    GP_ROWS = 1,       // A side: out tile = rows x W tile
+    GP_WGRAD = 2,      // contraction: both sides are columns of gathered rows
+};
 
 // What a tile's values become.
 enum : int {
     GP_OUT_ROWS = 0,   // out[order[p]][n], rows scattered back to their places
-    GP_OUT_PACK = 1,   // scale[g] * value as two 16-bit terms, rows as above
+    GP_OUT_PACK = 1,   // scale[g] * value as two 16-bit terms, a row per place
     GP_OUT_GROUP = 2,  // out[g][m][n]
     GP_OUT_LOW = 3,    // out[g][m][r]: columns j and j + 32 of each 64 added
     GP_OUT_LOW_T = 4,  // out[g][r][m]: the same, transposed
 };
 
+// A plan as the products read it.  The places of its order hold the groups one
+// after the other, then the rows without a group; a padded plan (sort_rows)
+// starts every group at a multiple of 16 places, with no row (-1) at the rest.
+struct GroupPlan {
+    int rows = 0;                     // rows of x and of the output
+    int places = 0;                   // upper bound of the places
+    int groups = 0;
+    const int32_t *offsets = nullptr; // [groups + 1] (padded: and the number of places)
+    const int32_t *order = nullptr;   // [places]
+    int padded = 0;
+};
+
 struct GroupProduct {
-    // rows and their groups
-    int rows = 0, groups = 0;         // tiles lie within one of `groups` groups
-    int shared = 0;                   // 1: one group of all rows (groups = 1)
-    const int32_t *offsets = nullptr; // [groups or ext_groups + 1]
-    const int32_t *order = nullptr;   // [rows]
-    // shape: contraction length (rows products), columns of the result, and
-    // for gradients (wgrad) the result's rows per group
-    int wgrad = 0;
-    int k = 0, n = 0, m = 0;
-    int bn = 0, ntiles = 0, mtiles = 0;
-    int mma_n = 0;
-    int b_mn = 0;                     // B is MN-major
+    int mode = 0;
+    GroupPlan plan;
+    int shared = 0;                   // one W for all places; the plan's groups are the extension's
+    // x (rows products) by place, through the tensor map of sorted rows, or
+    // picked by index
+    int sorted = 0;
+    const uint16_t *x = nullptr;
+    int64_t x_ld = 0;
+    int k = 0, n = 0, m = 0;          // contraction (rows products), result columns, rows (gradients)
+    int dense_mn = 0;                 // W is MN-major
+    int bn = 0;                       // B-side extent of a tile (GP_GROUPED: at most)
+    int ntiles = 0, mtiles = 0;       // column tiles; row tiles of a gradient
     int f16 = 0;
-    int stages = 0, stage_bytes = 0;
-    // low-rank extension of a shared product
-    int rank = 0, ext_groups = 0;
-    int ext_b_mn = 0;
+    int stages = 0, stage_bytes = 0, smem = 0;
+    int rank = 0;                     // of the low-rank extension of a shared product
     // output
-    int out_kind = 0, vec = 0;
+    int out_kind = 0;
+    int vec = 0;                      // 16-byte stores
     void *out = nullptr;
     int64_t ld = 0, gstride = 0;
     int rank_out = 0;                 // GP_OUT_LOW*: ranks written
@@ -61,15 +79,19 @@ struct GroupProduct {
     int32_t *status = nullptr;
 };
 
+// x: the rows by place (or l and r of a gradient: the A and B side); w: the
+// dense operand; u, eb: the extension's.
 struct GroupMaps {
-    CUtensorMap a, b, u, eb;
+    CUtensorMap x, xx, w, u, eb;      // xx: x in boxes of 128 rows
 };
 
-cudaError_t group_prepare();
-// Pipeline stages that fit beside the tables, for a tile of bn columns.
+constexpr int GP_ROW_BOX = 32;     // rows of a box of x and u
+
+cudaError_t group_prepare(int nsm, int *ctas);
+// Pipeline stages that fit beside the tables, and the counts of tiles.
 void group_plan(GroupProduct *p);
-size_t group_part_floats(int nsm);
-cudaError_t launch_group(const GroupProduct &p, const GroupMaps &maps, int nsm, cudaStream_t s);
+size_t group_part_floats(int ctas);
+cudaError_t launch_group(const GroupProduct &p, const GroupMaps &maps, int ctas, cudaStream_t s);
 
 // ---- dispatch, clipping, padding (k_ops.cu) ---------------------------------
 
@@ -77,6 +99,21 @@ cudaError_t ops_prepare();
 size_t dispatch_scratch_ints(int rows, int groups, int nsm);
 cudaError_t launch_dispatch(int rows, int groups, const int32_t *choice, int32_t *offsets,
                             int32_t *order, int32_t *scratch, int nsm, cudaStream_t s);
+
+// Rows of up to two matrices by place: dst[p] = src[order[p]], zeros where the
+// order holds no row.  With padded_offsets (groups + 2 ints) the places are
+// those of the padded plan, which is written there and to padded_order (places
+// of its ints); without, those of the plan itself.
+struct SortRows {
+    int n = 0;                        // matrices
+    const uint16_t *src[2];
+    int64_t src_ld[2];
+    int cols[2];
+    uint16_t *dst[2];
+    int64_t dst_ld[2];                // whole 16-byte units
+};
+cudaError_t launch_sort_rows(const GroupPlan &plan, const SortRows &m, int places, int32_t *padded_offsets,
+                             int32_t *padded_order, int nsm, cudaStream_t s);
 
 // dst [z][rows][dst_ld] = src [z][rows][cols] (strides in elements, 16-bit
 // elements; columns up to dst_ld are zeroed).
