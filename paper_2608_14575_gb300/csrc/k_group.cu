@@ -71,6 +71,7 @@ struct Tables {
     int last, go;        // epilogue: this piece writes the tile; the accumulator is there
     // group tables: ng groups of the tiles, and the extension's
     int ng;
+    int ext;             // stages of the extension, where all places are in one tile (else -1)
     int64_t *iter0;      // [ng + 1] first iteration of each group (gradients)
     int32_t *offs;       // [ng + 1] first place of each group, clamped
     int32_t *tile0;      // [ng + 1] first tile of each group (rows products)
@@ -113,6 +114,7 @@ struct Work {
     int k0, k1, ki;       // iterations of this piece, and of the tile
     int c0, c1;           // first and last pair with a piece of the tile
     int first, count;     // places of the tile (gradients: of the group)
+    int e0, e1;           // stages of the extension that go with the piece
 };
 
 // a * b / c; 32-bit where that holds (a 64-bit division costs some 100 instructions)
@@ -131,16 +133,23 @@ struct Walk {
     const GroupProduct &p;
     const Tables &t;
     int me, pairs, dp, kiters, cutters, next_tile;
-    int64_t rest, pos, end;
+    int64_t base, rest, pos, end;    // the line of iterations: where it begins, its length; this pair's
 
     __device__ Walk(const GroupProduct &p_, const Tables &t_) : p(p_), t(t_) {
         const bool grad = p.mode == GP_WGRAD;
-        const int tiles = grad ? 0 : t.tile0[t.ng];
+        const int per = p.mtiles * p.ntiles, tiles = grad ? t.ng * per : t.tile0[t.ng];
         me = blockIdx.x >> 1;
         pairs = gridDim.x >> 1;
         kiters = (p.k + GP_BK - 1) / GP_BK;
-        dp = !grad && tiles >= 2 * pairs ? (tiles / pairs - 1) * pairs : 0;
-        rest = grad ? t.iter0[t.ng] : (int64_t)(tiles - dp) * kiters;
+        dp = tiles >= 2 * pairs ? (tiles / pairs - 1) * pairs : 0;
+        base = 0;
+        if (grad) {
+            const int g = dp / per;       // (dp < tiles: the group exists)
+            base = t.iter0[g] + (int64_t)(dp - g * per) * cost(g);
+            rest = t.iter0[t.ng] - base;
+        } else {
+            rest = (int64_t)(tiles - dp) * kiters;
+        }
         const int64_t most = rest / MIN_PIECE;
         cutters = most < 1 ? 1 : most < pairs ? (int)most : pairs;
         next_tile = me;
@@ -150,8 +159,20 @@ struct Walk {
             end = mul_div(rest, me + 1, cutters);
         }
     }
-    // the pair whose piece holds iteration i
+    // the pair whose piece holds iteration i of the line
     __device__ int owner(int64_t i) const { return (int)div_small((i + 1) * cutters - 1, rest); }
+    // Iterations that a gradient's tile counts for: its own, or what writing it takes.
+    __device__ int cost(int g) const {
+        return max(MIN_PIECE, (max(0, t.offs[g + 1] - t.offs[g]) + GP_BK - 1) / GP_BK);
+    }
+    __device__ void place_grad(Work &w, int g, int local) const {
+        w.g = g;
+        w.first = t.offs[g];
+        w.count = max(0, t.offs[g + 1] - w.first);
+        w.ki = max(1, (w.count + GP_BK - 1) / GP_BK);
+        w.ot = local / p.mtiles;
+        w.xt = local - w.ot * p.mtiles;
+    }
 
     template <class T>
     __device__ static int find(const T *v, int n, T x) {   // last g with v[g] <= x
@@ -179,70 +200,101 @@ struct Walk {
         w.count = min(width, n - w.xt * width);
     }
     __device__ bool next(Work &w) {
+        const bool grad = p.mode == GP_WGRAD;
         if (next_tile < dp) {
-            place(w, next_tile);
+            if (grad) {
+                const int per = p.mtiles * p.ntiles, g = next_tile / per;
+                place_grad(w, g, next_tile - g * per);
+            } else {
+                place(w, next_tile);
+                w.ki = kiters;
+            }
             next_tile += pairs;
             w.k0 = 0;
-            w.k1 = w.ki = kiters;
+            w.k1 = w.ki;
             w.c0 = w.c1 = me;
+            w.e0 = 0;
+            w.e1 = INT32_MAX;
             return true;
         }
-        if (pos >= end) return false;
-        int64_t start;
-        if (p.mode == GP_WGRAD) {
-            w.g = find(t.iter0, t.ng, pos);
-            w.first = t.offs[w.g];
-            w.count = max(0, t.offs[w.g + 1] - w.first);
-            w.ki = max(1, (w.count + GP_BK - 1) / GP_BK);
-            const int local = (int)div_small(pos - t.iter0[w.g], w.ki);
-            start = t.iter0[w.g] + (int64_t)local * w.ki;
-            w.ot = local / p.mtiles;
-            w.xt = local - w.ot * p.mtiles;
-        } else {
-            const int i = (int)div_small(pos, kiters);
-            w.ki = kiters;
-            start = (int64_t)i * kiters;
-            place(w, dp + i);
+        while (pos < end) {
+            int64_t start, stop;      // of the tile, on the line
+            if (grad) {
+                const int g = find(t.iter0, t.ng, base + pos), c = cost(g);
+                const int local = (int)div_small(base + pos - t.iter0[g], c);
+                place_grad(w, g, local);
+                start = t.iter0[g] + (int64_t)local * c - base;
+                stop = start + c;
+            } else {
+                const int i = (int)div_small(pos, kiters);
+                place(w, dp + i);
+                w.ki = kiters;
+                start = (int64_t)i * kiters;
+                stop = start + kiters;
+            }
+            const int64_t upto = stop < end ? stop : end;
+            w.k0 = (int)(pos - start);
+            w.k1 = min((int)(upto - start), w.ki);
+            pos = upto;
+            if (w.k0 >= w.k1) continue;       // (of a gradient: nothing but what writing counts for)
+            w.c0 = owner(start);
+            w.c1 = owner(start + w.ki - 1);
+            w.e0 = 0;
+            w.e1 = INT32_MAX;
+            if (p.rank && w.c0 != w.c1) {
+                // a piece takes its share of the extension
+                const int all = t.ext >= 0 ? t.ext : ext_stages(w);
+                w.e0 = (int)mul_div(all, w.k0, w.ki);
+                w.e1 = (int)mul_div(all, w.k1, w.ki);
+            }
+            return true;
         }
-        w.k0 = (int)(pos - start);
-        const int64_t stop = start + w.ki < end ? start + w.ki : end;
-        w.k1 = (int)(stop - start);
-        w.c0 = owner(start);
-        w.c1 = owner(start + w.ki - 1);
-        pos = stop;
-        return true;
+        return false;
+    }
+    // Stages of the extension of a tile (see Ext).
+    __device__ int ext_stages(const Work &w) const {
+        int n = 0;
+        for (int g = find(t.eoffs, p.plan.groups, w.first); g < p.plan.groups && t.eoffs[g] < w.first + w.count; ++g)
+            n += max(t.eoffs[g], w.first) < min(t.eoffs[g + 1], w.first + w.count);
+        return n * ((p.rank + GP_RC - 1) / GP_RC);
     }
 };
 
-// The extension's stages of a tile: for each group with rows in the tile, the
-// rank in steps of GP_RC.
+// The extension's stages of a piece, out of the tile's: for each group with rows
+// in the tile, the rank in steps of GP_RC.
 struct Ext {
     const GroupProduct &p;
     const Tables &t;
-    int p0, p1, g, r0, a, b;
+    int p0, p1, g, r0, a, b, left;
     __device__ Ext(const GroupProduct &p_, const Tables &t_, const Work &w)
         : p(p_), t(t_), p0(w.first), p1(w.first + w.count) {
         g = Walk::find(t.eoffs, p.plan.groups, p0);   // eoffs[g] <= first, or g = 0
         r0 = 0;
+        left = w.e1 - w.e0;
         settle();
+        for (int i = 0; i < w.e0 && g < p.plan.groups; ++i) advance();
     }
     __device__ void settle() {
         for (; g < p.plan.groups; ++g) {
+            if (t.eoffs[g] >= p1) break;
             a = max(t.eoffs[g], p0);
             b = min(t.eoffs[g + 1], p1);
             if (a < b) return;
-            if (t.eoffs[g] >= p1) break;
         }
         g = p.plan.groups;
     }
-    __device__ bool more() const { return g < p.plan.groups; }
-    __device__ void step() {
+    __device__ void advance() {
         r0 += GP_RC;
         if (r0 >= p.rank) {
             r0 = 0;
             ++g;
             settle();
         }
+    }
+    __device__ bool more() const { return left > 0 && g < p.plan.groups; }
+    __device__ void step() {
+        --left;
+        advance();
     }
 };
 
@@ -307,7 +359,7 @@ __device__ void pick_rows(const GroupProduct &p, Tables &t, uint8_t *sm, int ran
             row[i] = r < 0 ? nullptr : p.x + r * p.x_ld;
         }
         int stages = w.k1 - w.k0;
-        if (p.rank && w.k1 == w.ki)
+        if (p.rank)
             for (Ext e(p, t, w); e.more(); e.step()) ++stages;   // of these only the arrival is due
         for (int i0 = 0; i0 < stages; ++i0, at.step()) {
             const int kb = w.k0 + i0;
@@ -400,8 +452,8 @@ k_group(const __grid_constant__ GroupMaps maps, const __grid_constant__ GroupPro
             int64_t v = 0;
             if (g < t.ng) {
                 const int n = max(0, t.offs[g + 1] - t.offs[g]);
-                // (an empty group's zero gradient is written too)
-                v = grad ? (int64_t)p.mtiles * p.ntiles * max(1, (n + GP_BK - 1) / GP_BK)
+                // (an empty group's zero gradient is written too: see Walk::cost)
+                v = grad ? (int64_t)p.mtiles * p.ntiles * max(MIN_PIECE, (n + GP_BK - 1) / GP_BK)
                          : (int64_t)((n + GP_TILE - 1) / GP_TILE) * p.ntiles;
             }
 #pragma unroll
@@ -419,6 +471,12 @@ k_group(const __grid_constant__ GroupMaps maps, const __grid_constant__ GroupPro
             if (grad) t.iter0[0] = 0;
             else t.tile0[0] = 0;
         }
+    }
+    if (shared && warp == 1) {
+        int n = 0;
+        for (int g = lane; g < p.plan.groups; g += 32) n += t.eoffs[g] < t.eoffs[g + 1];
+        n = __reduce_add_sync(0xffffffffu, n);
+        if (lane == 0) t.ext = t.offs[1] <= GP_TILE ? n * ((p.rank + GP_RC - 1) / GP_RC) : -1;
     }
     tc_fence_before();
     __syncthreads();
@@ -485,7 +543,7 @@ k_group(const __grid_constant__ GroupMaps maps, const __grid_constant__ GroupPro
                     else
                         tma_load_3d_pair(st + dside, &maps.w, full0 + at.s * 8, kb * GP_BK, o0, w.g);
                 }
-                if (shared && ok && w.k1 == w.ki)
+                if (shared && ok)
                     for (Ext e(p, t, w); e.more(); e.step(), at.step()) {
                         if (!claim(2 * ebytes + xbytes)) break;
                         uint8_t *st = sm + (size_t)at.s * p.stage_bytes;
@@ -547,7 +605,7 @@ k_group(const __grid_constant__ GroupMaps maps, const __grid_constant__ GroupPro
                     mma_commit_pair(&t.empty[at.s]);
                 }
                 if (!ok) break;
-                if (shared && w.k1 == w.ki) {
+                if (shared) {
                     const uint32_t eidesc = idesc_16bit(GP_TILE, p.bn, F16, false, p.dense_mn);
                     for (Ext e(p, t, w); e.more(); e.step(), at.step()) {
                         uint32_t off[8];
@@ -589,7 +647,7 @@ k_group(const __grid_constant__ GroupMaps maps, const __grid_constant__ GroupPro
             Work w;
             while (ok && walk.next(w)) {
                 int stages = w.k1 - w.k0;
-                if (shared && w.k1 == w.ki)
+                if (shared)
                     for (Ext e(p, t, w); e.more(); e.step()) ++stages;
                 for (; stages > 0; --stages, at.step()) {
                     ok = mbar_wait(&t.rowsf[at.s], at.ph, abort_f, p.status);

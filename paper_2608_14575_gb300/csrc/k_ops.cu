@@ -232,6 +232,109 @@ k_sort_rows(const __grid_constant__ GroupPlan plan, const __grid_constant__ Sort
 }
 
 // ---------------------------------------------------------------------------
+// Low-rank inner products of a few rows: u[place] = scale[g] A[g] x[order[place]]
+// as two 16-bit terms a value, in the layout of the tensor-core kernel.  A few
+// rows read all of A once and compute little: a block takes a row and four
+// ranks, its eight warps an eighth of the columns each, so that every load of
+// the call is in flight at once.
+
+constexpr int LF_THREADS = 256, LF_WARPS = LF_THREADS / 32, LF_RANKS = 4;
+
+template <bool F16>
+__device__ __forceinline__ void widen8(const uint4 &u, float (&f)[8]) {
+    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if (F16) {
+            const float2 v = __half22float2(*(const __half2 *)&w[i]);
+            f[2 * i] = v.x;
+            f[2 * i + 1] = v.y;
+        } else {
+            f[2 * i] = __uint_as_float(w[i] << 16);
+            f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+        }
+    }
+}
+
+// Eight elements from column c on of a row of n, zeros beyond it.
+__device__ __forceinline__ uint4 row8(const uint16_t *row, int c, int n) {
+    if (c + 8 <= n) return __ldg((const uint4 *)(row + c));
+    uint32_t v[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = c + j < n ? row[c + j] : 0;
+    return make_uint4(v[0] | v[1] << 16, v[2] | v[3] << 16, v[4] | v[5] << 16, v[6] | v[7] << 16);
+}
+
+template <bool F16>
+__global__ void __launch_bounds__(LF_THREADS)
+k_low_few(const __grid_constant__ LowFew p) {
+    __shared__ float part[LF_WARPS][LF_RANKS];
+    __shared__ int group;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int place = blockIdx.x, r0 = blockIdx.y * LF_RANKS;
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const int row = p.plan.order[place];
+    if (warp == 0) {
+        // the place's group: how many groups end at or before it
+        int n = 0;
+        for (int g = lane; g < p.plan.groups; g += 32) n += p.plan.offsets[g + 1] <= place;
+        n = __reduce_add_sync(0xffffffffu, n);
+        if (lane == 0) group = n;
+    }
+    __syncthreads();
+    const int g = group, ranks = min(LF_RANKS, p.rank - r0);
+    float acc[LF_RANKS] = {};
+    if (g < p.plan.groups && (uint32_t)row < (uint32_t)p.plan.rows && ranks > 0) {
+        const uint16_t *x = p.x + row * p.x_ld;
+        const uint16_t *a = p.a + g * p.a_z + (int64_t)r0 * p.a_ld;
+#pragma unroll 2
+        for (int c = (warp * 32 + lane) * 8; c < p.k; c += LF_THREADS * 8) {
+            const uint4 xv = row8(x, c, p.k);
+            uint4 av[LF_RANKS];
+#pragma unroll
+            for (int r = 0; r < LF_RANKS; ++r)
+                av[r] = r < ranks ? row8(a + r * p.a_ld, c, p.k) : make_uint4(0, 0, 0, 0);
+            float xf[8];
+            widen8<F16>(xv, xf);
+#pragma unroll
+            for (int r = 0; r < LF_RANKS; ++r) {
+                float af[8];
+                widen8<F16>(av[r], af);
+                if (r < ranks)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) acc[r] = fmaf(xf[j], af[j], acc[r]);
+            }
+        }
+    }
+#pragma unroll
+    for (int r = 0; r < LF_RANKS; ++r) {
+        for (int d = 16; d; d /= 2) acc[r] += __shfl_down_sync(0xffffffffu, acc[r], d);
+        if (lane == 0) part[warp][r] = acc[r];
+    }
+    __syncthreads();
+    if (threadIdx.x < LF_RANKS) {
+        const int r = r0 + threadIdx.x;
+        float v = 0.f;
+        for (int w = 0; w < LF_WARPS; ++w) v += part[w][threadIdx.x];
+        v = r < p.rank && g < p.plan.groups ? v * p.scale[g] : 0.f;
+        // high and low terms (an infinite high one takes a zero low one)
+        uint16_t *u = p.u + (int64_t)place * p.u_ld + r / GP_RC * (2 * GP_RC) + r % GP_RC;
+        if (F16) {
+            const __half h = __float2half_rn(v);
+            const float f = __half2float(h);
+            u[0] = __half_as_ushort(h);
+            u[GP_RC] = __half_as_ushort(__float2half_rn(isinf(f) ? 0.f : v - f));
+        } else {
+            const __nv_bfloat16 h = __float2bfloat16_rn(v);
+            const float f = __bfloat162float(h);
+            u[0] = __bfloat16_as_ushort(h);
+            u[GP_RC] = __bfloat16_as_ushort(__float2bfloat16_rn(isinf(f) ? 0.f : v - f));
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------
 // Padding copy of 16-bit elements.
 
 __global__ void __launch_bounds__(256)
@@ -477,6 +580,19 @@ cudaError_t launch_sort_rows(const GroupPlan &plan, const SortRows &m, int place
     k_sort_rows<<<(int)(want < most ? want : most), SR_THREADS, (plan.groups + 1) * 8, s>>>(plan, m, places, padded_offsets,
                                                                                             padded_order);
     return cudaGetLastError();
+}
+
+cudaError_t launch_low_few(const LowFew &p, bool f16, cudaStream_t s) {
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.gridDim = dim3((unsigned)p.plan.rows, (unsigned)((p.rank + 2 * GP_RC - 1) / (2 * GP_RC) * (2 * GP_RC / LF_RANKS)));
+    cfg.blockDim = dim3(LF_THREADS);
+    cfg.stream = s;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    return f16 ? cudaLaunchKernelEx(&cfg, k_low_few<true>, p) : cudaLaunchKernelEx(&cfg, k_low_few<false>, p);
 }
 
 cudaError_t launch_pad(void *dst, int64_t dst_ld, const void *src, int64_t src_ld, int64_t src_z, int64_t nz,

@@ -298,6 +298,7 @@ struct Rows {
 // bytes bound the product (64 rows x 12 groups, 1024 -> 4096: 42 us picked).
 // More of them are copied by place once.
 constexpr int PICK_ROWS = 256;
+constexpr int64_t LOW_FEW_VALUES = 16 << 20;   // values of the adapters read by a few rows
 
 // contracted: a gradient contracts over the rows, which takes the padded plan.
 static Rows plan_rows(Carver &cv, const hwr_rows *r, const void *dy, int64_t dy_ld, bool need_x, bool contracted) {
@@ -525,6 +526,24 @@ static hwr_status check_adapters(hwr_ops *c, const hwr_rows *r, const hwr_adapte
 // [32-rank chunks][high, low], an even number of chunks.
 static hwr_status low_rank(hwr_ops *c, const hwr_rows *r, const hwr_adapters *ad, const Rows &rows, const Operand &x,
                            const Operand &m, bool m_mn, const Operand &u) {
+    // a row reads its adapter's matrix once: few enough bytes need no tensor
+    // cores (64 rows, rank 16, 4,096 columns: 27 us on them, 5 us without)
+    if (!rows.sorted && !m_mn && (int64_t)r->rows * ad->rank * x.cols <= LOW_FEW_VALUES) {
+        LowFew f;
+        f.plan = rows.plan;
+        f.k = x.cols;
+        f.rank = ad->rank;
+        f.x = (const uint16_t *)x.p;
+        f.x_ld = x.ld;
+        f.a = (const uint16_t *)m.p;
+        f.a_ld = m.ld;
+        f.a_z = m.z;
+        f.scale = ad->scale;
+        f.u = (uint16_t *)const_cast<void *>(u.p);
+        f.u_ld = u.ld;
+        CK(c, launch_low_few(f, r->dtype == HWR_F16, c->stream), "low-rank kernel");
+        return HWR_OK;
+    }
     GroupProduct p = product(c, r, rows);
     p.mode = GP_ROWS;
     p.out_kind = GP_OUT_PACK;

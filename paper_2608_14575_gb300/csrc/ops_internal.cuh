@@ -115,6 +115,19 @@ struct SortRows {
 cudaError_t launch_sort_rows(const GroupPlan &plan, const SortRows &m, int places, int32_t *padded_offsets,
                              int32_t *padded_order, int nsm, cudaStream_t s);
 
+// u[place] = scale[g] a[g] x[order[place]] as GP_OUT_PACK leaves it, for a few
+// rows (a 16-byte aligned, rows of x too).
+struct LowFew {
+    GroupPlan plan;
+    int k, rank;
+    const uint16_t *x, *a;
+    int64_t x_ld, a_ld, a_z;
+    const float *scale;
+    uint16_t *u;
+    int64_t u_ld;
+};
+cudaError_t launch_low_few(const LowFew &p, bool f16, cudaStream_t s);
+
 // dst [z][rows][dst_ld] = src [z][rows][cols] (strides in elements, 16-bit
 // elements; columns up to dst_ld are zeroed).
 cudaError_t launch_pad(void *dst, int64_t dst_ld, const void *src, int64_t src_ld, int64_t src_z,
