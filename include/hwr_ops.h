@@ -11,6 +11,7 @@
  *   hwr_adapter_forward     y[t] = W x[t] + scale[c] B[c] (A[c] x[t])
  *   hwr_adapter_backward    dx, dA, dB of the same (W is left as it is)
  *   hwr_clip_gradients      global norm of many tensors, and clipping
+ *   hwr_gradients_clip      the same over a list that is laid out once
  *
  * Conventions (those of hwr.h, and)
  *   - A context of its own (hwr_ops): one CUDA stream, one workspace.  Calls
@@ -134,6 +135,18 @@ typedef struct {
  */
 hwr_status hwr_clip_gradients(hwr_ops *ops, int32_t n, const hwr_gradient *grads, float max_norm,
                               float *norm);
+
+/*
+ * The same for gradients that stay where they are from step to step: create
+ * lays their table out in device memory once (synchronises the stream); clip
+ * reads and writes the arrays as they are at the call, which must still be
+ * there.  destroy synchronises; NULL is fine.
+ */
+typedef struct hwr_gradients hwr_gradients;
+hwr_status hwr_gradients_create(hwr_ops *ops, int32_t n, const hwr_gradient *grads,
+                                hwr_gradients **out);
+hwr_status hwr_gradients_clip(hwr_ops *ops, const hwr_gradients *list, float max_norm, float *norm);
+hwr_status hwr_gradients_destroy(hwr_ops *ops, hwr_gradients *list);
 
 #ifdef __cplusplus
 }

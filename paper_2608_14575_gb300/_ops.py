@@ -31,7 +31,8 @@ HWR_OPS_MAX_RANK = 256
 OPS_EXPORTS = ("hwr_ops_create", "hwr_ops_destroy", "hwr_ops_synchronize",
                "hwr_ops_last_error", "hwr_ops_reserve", "hwr_dispatch",
                "hwr_grouped_forward", "hwr_grouped_backward", "hwr_adapter_forward",
-               "hwr_adapter_backward", "hwr_clip_gradients")
+               "hwr_adapter_backward", "hwr_clip_gradients", "hwr_gradients_create",
+               "hwr_gradients_clip", "hwr_gradients_destroy")
 
 
 class hwr_rows(ct.Structure):
@@ -71,6 +72,9 @@ def load_ops():
         lib.hwr_adapter_forward.argtypes = [P, P, P, P, L]
         lib.hwr_adapter_backward.argtypes = [P, P, P, P, L, P, L, P, P]
         lib.hwr_clip_gradients.argtypes = [P, I, P, ct.c_float, P]
+        lib.hwr_gradients_create.argtypes = [P, I, P, ct.POINTER(P)]
+        lib.hwr_gradients_clip.argtypes = [P, P, ct.c_float, P]
+        lib.hwr_gradients_destroy.argtypes = [P, P]
         for n in OPS_EXPORTS:
             getattr(lib, n).restype = ct.c_int
         lib.hwr_ops_last_error.restype = ct.c_char_p
@@ -89,9 +93,25 @@ class Plan:
 
 
 class GradientList:
-    """The gradients of one clipping call, for callers that clip the same
-    buffers again and again: made by ``Operators.gradient_list``."""
-    __slots__ = ("grads", "out", "table", "n", "ref")
+    """The gradients of a training loop, laid out once for ``clip_gradients``:
+    made by ``Operators.gradient_list``."""
+
+    def __init__(self, ops, grads, out):
+        self.ops, self.grads, self.out = ops, grads, out     # (the tensors stay alive)
+        self.handle = ct.c_void_p()
+        ops._call(ops.lib.hwr_gradients_create, len(grads), ops._gradients(grads, out),
+                  ct.byref(self.handle))
+
+    def close(self):
+        if self.handle and self.ops.ctx:
+            self.ops.lib.hwr_gradients_destroy(self.ops.ctx, self.handle)
+        self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
 
 
 class Operators:
@@ -271,18 +291,11 @@ class Operators:
                    da.data_ptr() if need_dab else None, db.data_ptr() if need_dab else None)
         return dx, da, db
 
-    def gradient_list(self, grads, out=None) -> GradientList:
-        """The gradients of ``clip_gradients`` as a list to be used again: its
-        tensors are read and written where they are at each call.  ``out``: where
-        the clipped ones go (default: in place)."""
-        grads = list(grads)
-        out = grads if out is None else list(out)
+    def _gradients(self, grads, out):
         if len(out) != len(grads):
             raise ValueError(f"{len(out)} outputs for {len(grads)} gradients")
-        l = GradientList()
-        l.grads, l.out, l.n = grads, out, len(grads)
-        l.table = (hwr_gradient * max(1, l.n))()
-        for e, g, o in zip(l.table, grads, out):
+        table = (hwr_gradient * max(1, len(grads)))()
+        for e, g, o in zip(table, grads, out):
             code = self._grad_dtypes.get(g.dtype)
             if code is None:
                 raise TypeError(f"gradient: {g.dtype}, want float32, bfloat16 or float16")
@@ -292,16 +305,29 @@ class Operators:
                 if t.device != self.device or not t.is_contiguous():
                     raise ValueError(f"want contiguous gradients on {self.device}")
             e.in_, e.out, e.n, e.dtype = g.data_ptr(), o.data_ptr(), g.numel(), code
-        l.ref = ct.cast(l.table, ct.c_void_p)
-        return l
+        return table
+
+    def gradient_list(self, grads, out=None) -> GradientList:
+        """Lay out gradients that stay where they are for ``clip_gradients`` at
+        every step.  ``out``: where the clipped ones go (default: in place)."""
+        grads = list(grads)
+        return GradientList(self, grads, grads if out is None else list(out))
 
     def clip_gradients(self, grads, max_norm: float, out=None):
         """Scale the gradients by min(1, max_norm / (norm + 1e-6)); returns the
         norm over all of them before that, a scalar tensor on the device.
-        ``grads``: tensors, or a ``gradient_list``."""
-        l = grads if isinstance(grads, GradientList) else self.gradient_list(grads, out)
+        ``grads``: tensors (``out``: where the clipped ones go, default in
+        place), or a ``gradient_list``."""
         norm = self.torch.empty((), dtype=self.torch.float32, device=self.device)
-        self._call(self.lib.hwr_clip_gradients, l.n, l.ref, float(max_norm), norm.data_ptr())
+        if isinstance(grads, GradientList):
+            if out is not None or grads.ops is not self or not grads.handle:
+                raise ValueError("a gradient list has its outputs, its context, and is open")
+            self._call(self.lib.hwr_gradients_clip, grads.handle, float(max_norm), norm.data_ptr())
+        else:
+            grads = list(grads)
+            self._call(self.lib.hwr_clip_gradients, len(grads),
+                       self._gradients(grads, grads if out is None else list(out)),
+                       float(max_norm), norm.data_ptr())
         return norm
 
     def reserve(self, nbytes: int):

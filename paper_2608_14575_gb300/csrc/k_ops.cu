@@ -15,11 +15,21 @@ namespace {
 // warp holds DP_PER x 32 consecutive rows in registers.  The rows of a warp
 // that share a key find each other by a match over the warp, so a row's place
 // is its key's first place (over the blocks, rounds and warps before it) plus
-// the peers in lower lanes: no atomics decide an order.
+// the peers in lower lanes: no atomics decide an order.  What the blocks before
+// hold of each key comes from shared memory within a cluster (up to DP_CLUSTER
+// blocks, one launch) or from a counting pass before (more).  All of it is
+// bound by latency: 4 MB of choices are read and written in 1.2 us.
 
-constexpr int DP_THREADS = 1024, DP_WARPS = DP_THREADS / 32;
+constexpr int DP_THREADS = 512, DP_WARPS = DP_THREADS / 32;
 constexpr int DP_PER = 8;
 constexpr int DP_ROWS = DP_THREADS * DP_PER;
+constexpr int DP_CLUSTER = 8;
+constexpr int DP_FEW = 512;      // rows whose places are counted row against row
+
+__device__ __forceinline__ void pdl_begin() {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+}
 
 __device__ __forceinline__ int key_of(const int32_t *choice, int64_t row, int64_t end, int G) {
     if (row >= end) return G + 1;            // no row
@@ -27,11 +37,42 @@ __device__ __forceinline__ int key_of(const int32_t *choice, int64_t row, int64_
     return (uint32_t)c < (uint32_t)G ? c : G;
 }
 
+// A few rows: a row's place is the number of rows that come before it.
+__global__ void __launch_bounds__(DP_FEW)
+k_dispatch_few(int rows, int G, const int32_t *choice, int32_t *offsets, int32_t *order) {
+    __shared__ __align__(16) int32_t key[DP_FEW];
+    const int tid = threadIdx.x, n4 = (rows + 3) / 4;
+    pdl_begin();
+    key[tid] = tid < rows ? key_of(choice, tid, rows, G) : G + 1;
+    __syncthreads();
+    const int4 *k4 = (const int4 *)key;
+    if (tid < rows) {
+        const int k = key[tid];
+        int place = 0;
+        for (int j = 0; j < n4; ++j) {
+            const int4 v = k4[j];
+            place += (v.x < k) + (v.y < k) + (v.z < k) + (v.w < k);
+            place += (v.x == k && 4 * j < tid) + (v.y == k && 4 * j + 1 < tid) + (v.z == k && 4 * j + 2 < tid) +
+                     (v.w == k && 4 * j + 3 < tid);
+        }
+        order[place] = tid;
+    }
+    for (int g = tid; g <= G; g += DP_FEW) {
+        int n = 0;
+        for (int j = 0; j < n4; ++j) {
+            const int4 v = k4[j];
+            n += (v.x < g) + (v.y < g) + (v.z < g) + (v.w < g);
+        }
+        offsets[g] = n;
+    }
+}
+
 // Rows of each key in each block: hist [blocks][G + 1].
 __global__ void __launch_bounds__(DP_THREADS)
 k_dispatch_count(int rows, int G, int64_t per_block, const int32_t *choice, int32_t *hist) {
     extern __shared__ int32_t sh[];
     for (int i = threadIdx.x; i <= G; i += DP_THREADS) sh[i] = 0;
+    pdl_begin();
     __syncthreads();
     const int64_t begin = blockIdx.x * per_block;
     const int64_t end = begin + per_block < rows ? begin + per_block : rows;
@@ -50,12 +91,25 @@ k_dispatch_count(int rows, int G, int64_t per_block, const int32_t *choice, int3
     for (int i = threadIdx.x; i <= G; i += DP_THREADS) hist[(int64_t)blockIdx.x * (G + 1) + i] = sh[i];
 }
 
-// hist: counts per block of k_dispatch_count, or null with a single block.
+__device__ __forceinline__ int remote_int(const int32_t *p, int rank) {
+    uint32_t a;
+    int v;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"((uint32_t)__cvta_generic_to_shared(p)), "r"(rank));
+    asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
+    return v;
+}
+
+__device__ __forceinline__ void cluster_barrier() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+
+// hist: counts per block of k_dispatch_count; null with one block, or with one
+// cluster of blocks of a round each.
 __global__ void __launch_bounds__(DP_THREADS)
 k_dispatch_place(int rows, int G, int64_t per_block, const int32_t *choice, const int32_t *hist,
                  int32_t *offsets, int32_t *order) {
     extern __shared__ int32_t sh[];
-    const int G1 = G + 1, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int G1 = G + 1, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, nb = gridDim.x;
     int32_t *wh = sh;                        // [DP_WARPS][G1] counts, then first places
     int32_t *base = sh + DP_WARPS * G1;      // [G1] next place of each key
     int32_t *total = base + G1;              // [G1] rows of each key in all
@@ -65,6 +119,8 @@ k_dispatch_place(int rows, int G, int64_t per_block, const int32_t *choice, cons
     const int64_t end = begin + per_block < rows ? begin + per_block : rows;
 
     for (int i = tid; i < G1; i += DP_THREADS) base[i] = total[i] = 0;
+    // after the counting pass the choices are known to be there, its counts are not
+    if (!hist) pdl_begin();
     for (int64_t r0 = begin; r0 < end || r0 == begin; r0 += DP_ROWS) {
         int key[DP_PER];
 #pragma unroll
@@ -72,21 +128,6 @@ k_dispatch_place(int rows, int G, int64_t per_block, const int32_t *choice, cons
             key[i] = key_of(choice, r0 + (warp * DP_PER + i) * 32 + lane, end, G);
         for (int i = tid; i < DP_WARPS * G1; i += DP_THREADS) wh[i] = 0;
         __syncthreads();
-        if (hist && r0 == begin) {
-            // rows of each key in the blocks before this one, and in all
-            const int subs = max(1, DP_THREADS / G1), nb = gridDim.x;
-            for (int j = tid; j < G1 * subs; j += DP_THREADS) {
-                const int g = j % G1, sub = j / G1;
-                int before = 0, all = 0;
-                for (int b = sub; b < nb; b += subs) {
-                    const int c = hist[(int64_t)b * G1 + g];
-                    all += c;
-                    if (b < (int)blockIdx.x) before += c;
-                }
-                atomicAdd(&base[g], before);
-                atomicAdd(&total[g], all);
-            }
-        }
         // counts of each warp's rows
         int rank[DP_PER];
 #pragma unroll
@@ -102,22 +143,54 @@ k_dispatch_place(int rows, int G, int64_t per_block, const int32_t *choice, cons
             rank[i] = c + __popc(peers & ((1u << lane) - 1));
             __syncwarp();
         }
+        if (hist && r0 == begin) {
+            // rows of each key in the blocks before this one, and in all
+            pdl_begin();
+            const int subs = max(1, DP_THREADS / G1);
+            for (int j = tid; j < G1 * subs; j += DP_THREADS) {
+                const int g = j % G1, sub = j / G1;
+                int before = 0, all = 0;
+#pragma unroll 8
+                for (int b = sub; b < nb; b += subs) {
+                    const int c = hist[(int64_t)b * G1 + g];
+                    all += c;
+                    before += b < (int)blockIdx.x ? c : 0;
+                }
+                atomicAdd(&base[g], before);
+                atomicAdd(&total[g], all);
+            }
+        }
         __syncthreads();
         // over the warps: counts become first places within the round
         for (int g = tid; g < G1; g += DP_THREADS) {
             int sum = 0;
+#pragma unroll
             for (int w = 0; w < DP_WARPS; ++w) {
                 const int c = wh[w * G1 + g];
                 wh[w * G1 + g] = sum;
                 sum += c;
             }
-            if (!hist) total[g] = sum;      // a single block has a single round
             round[g] = sum;
+            if (!hist && nb == 1) total[g] = sum;
+        }
+        if (!hist && nb > 1) {
+            cluster_barrier();
+            for (int g = tid; g < G1; g += DP_THREADS) {
+                int before = 0, all = 0;
+                for (int b = 0; b < nb; ++b) {
+                    const int c = remote_int(&round[g], b);
+                    all += c;
+                    before += b < (int)blockIdx.x ? c : 0;
+                }
+                base[g] = before;
+                total[g] = all;
+            }
         }
         __syncthreads();
         if (r0 == begin) {
-            // first place of each key: a running sum of the totals
-            int v = tid < G ? total[tid] : 0, s = v;
+            // first place of each key: a running sum of the totals, two keys a thread
+            const int a = 2 * tid < G ? total[2 * tid] : 0, b = 2 * tid + 1 < G ? total[2 * tid + 1] : 0;
+            int s = a + b;
 #pragma unroll
             for (int d = 1; d < 32; d *= 2) {
                 const int o = __shfl_up_sync(0xffffffffu, s, d);
@@ -125,21 +198,19 @@ k_dispatch_place(int rows, int G, int64_t per_block, const int32_t *choice, cons
             }
             if (lane == 31) wsum[warp] = s;
             __syncthreads();
-            if (warp == 0) {
-                int x = wsum[lane];
+            int before = 0, all = 0;
 #pragma unroll
-                for (int d = 1; d < 32; d *= 2) {
-                    const int o = __shfl_up_sync(0xffffffffu, x, d);
-                    if (lane >= d) x += o;
-                }
-                wsum[lane] = x;
+            for (int w = 0; w < DP_WARPS; ++w) {
+                before += w < warp ? wsum[w] : 0;
+                all += wsum[w];
             }
-            __syncthreads();
-            const int upto = s + (warp ? wsum[warp - 1] : 0);
-            if (tid < G) base[tid] += upto - v;
-            if (tid == 0) base[G] += wsum[DP_WARPS - 1];
+            const int upto = before + s;
+            if (2 * tid < G) base[2 * tid] += upto - a - b;
+            if (2 * tid + 1 < G) base[2 * tid + 1] += upto - b;
+            if (tid == 0) base[G] += all;
             if (blockIdx.x == 0) {
-                if (tid < G) offsets[tid + 1] = upto;
+                if (2 * tid < G) offsets[2 * tid + 1] = upto - b;
+                if (2 * tid + 1 < G) offsets[2 * tid + 2] = upto;
                 if (tid == 0) offsets[0] = 0;
             }
             __syncthreads();
@@ -152,6 +223,7 @@ k_dispatch_place(int rows, int G, int64_t per_block, const int32_t *choice, cons
         __syncthreads();
         for (int g = tid; g < G1; g += DP_THREADS) base[g] += round[g];
     }
+    if (!hist && nb > 1) cluster_barrier();      // the others may still read this block's counts
 }
 
 size_t place_smem(int G) { return (size_t)(DP_WARPS + 3) * (G + 1) * 4; }
@@ -168,6 +240,7 @@ k_sort_rows(const __grid_constant__ GroupPlan plan, const __grid_constant__ Sort
     const int G = plan.groups, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     int32_t *offs = sh, *pad = sh + G + 1;       // first place of each group, in either plan
     int total = plan.rows;
+    pdl_begin();
     if (padded_offsets) {
         for (int i = threadIdx.x; i <= G; i += SR_THREADS) {
             const int v = plan.offsets[i];
@@ -272,8 +345,7 @@ k_low_few(const __grid_constant__ LowFew p) {
     __shared__ int group;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int place = blockIdx.x, r0 = blockIdx.y * LF_RANKS;
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    asm volatile("griddepcontrol.wait;" ::: "memory");
+    pdl_begin();
     const int row = p.plan.order[place];
     if (warp == 0) {
         // the place's group: how many groups end at or before it
@@ -355,21 +427,18 @@ k_pad(uint16_t *dst, int64_t dst_ld, const uint16_t *src, int64_t src_ld, int64_
 
 // ---------------------------------------------------------------------------
 // Gradient clipping: one pass sums the squares, one scales.  Both are bound by
-// HBM; a block's chunks lie a grid apart, so that the whole GPU walks the
-// tensors in order, and the second pass walks them backwards: it begins with
-// what the first left in L2.
+// HBM.  The tensors are cut into chunks of 16 KB, named by a table in device
+// memory (read from kernel parameters, the table's cache misses cost more than
+// the chunks of a small set of gradients); a block's chunks lie a grid apart,
+// so that the whole GPU walks the tensors in order, and the second pass walks
+// them backwards: it begins with what the first left in L2.
 
 constexpr int CL_THREADS = 256;
-constexpr int CL_BYTES = 16;                         // of one access
-constexpr int CL_PER = 8;                            // accesses of a thread in a chunk
+constexpr int CL_PER = CLIP_CHUNK_BYTES / 16 / CL_THREADS;   // 16-byte accesses of a thread in a chunk
 
-__host__ __device__ inline int dtype_size(int d) { return d == HWR_F32 ? 4 : 2; }
-__host__ __device__ inline int chunk_elems(int d) { return CL_THREADS * CL_PER * CL_BYTES / dtype_size(d); }
-
-// Eight 16-byte units (or the ragged, unaligned rest) of a chunk as floats.
 template <int DT>
 struct Vec {
-    static constexpr int N = DT == HWR_F32 ? 4 : 8;
+    static constexpr int N = DT == HWR_F32 ? 4 : 8;      // values of 16 bytes
     __device__ static void unpack(const uint4 &u, float (&f)[N]) {
         const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
@@ -402,45 +471,41 @@ struct Vec {
         }
         return make_uint4(w[0], w[1], w[2], w[3]);
     }
+    __device__ static float load(const void *p, int i) {
+        if (DT == HWR_F32) return ((const float *)p)[i];
+        if (DT == HWR_BF16) return __bfloat162float(((const __nv_bfloat16 *)p)[i]);
+        return __half2float(((const __half *)p)[i]);
+    }
+    __device__ static void store(void *p, int i, float v) {
+        if (DT == HWR_F32) ((float *)p)[i] = v;
+        else if (DT == HWR_BF16) ((__nv_bfloat16 *)p)[i] = __float2bfloat16_rn(v);
+        else ((__half *)p)[i] = __float2half_rn(v);
+    }
+    static constexpr int FULL = CLIP_CHUNK_BYTES / (DT == HWR_F32 ? 4 : 2);
 };
 
+// The squares of a thread's share of a chunk once more, in 64 bits: where
+// their fp32 sum left the range that fp32 holds well.
 template <int DT>
-__device__ __forceinline__ float load1(const void *p, int64_t i) {
-    if (DT == HWR_F32) return ((const float *)p)[i];
-    if (DT == HWR_BF16) return __bfloat162float(((const __nv_bfloat16 *)p)[i]);
-    return __half2float(((const __half *)p)[i]);
-}
-template <int DT>
-__device__ __forceinline__ void store1(void *p, int64_t i, float v) {
-    if (DT == HWR_F32) ((float *)p)[i] = v;
-    else if (DT == HWR_BF16) ((__nv_bfloat16 *)p)[i] = __float2bfloat16_rn(v);
-    else ((__half *)p)[i] = __float2half_rn(v);
-}
-
-// Adds the squares of some values, s their fp32 sum: into `acc` where fp32
-// holds it well, else (squares near fp32's limits) into `wide`, exactly
-// enough.  NaN and infinite values go the ordinary way.
-template <int N>
-__device__ __forceinline__ void add_squares(const float (&f)[N], float &acc, double &wide) {
-    float s = 0.f, m = 0.f;
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-        s = fmaf(f[i], f[i], s);
-        m = fmaxf(m, fabsf(f[i]));
-    }
-    if ((s > 1e30f && m <= 3.4028234e38f) || (s < 1e-30f && m > 0.f)) {
-        for (int i = 0; i < N; ++i) wide += (double)f[i] * f[i];
-        return;
-    }
-    acc += s;
+__device__ __noinline__ double wide_squares(const void *in, int n, bool vec) {
+    double s = 0;
+    auto add = [&](float f) { s += (double)f * f; };
+    constexpr int N = Vec<DT>::N;
+    if (vec)
+        for (int i = 0; i < CL_PER; ++i)
+            for (int j = 0; j < N; ++j) add(Vec<DT>::load(in, (i * CL_THREADS + threadIdx.x) * N + j));
+    else
+        for (int i = threadIdx.x; i < n; i += CL_THREADS) add(Vec<DT>::load(in, i));
+    return s;
 }
 
 template <int DT>
-__device__ __forceinline__ void sum_chunk(const void *in, int64_t e0, int64_t n, float &acc, double &wide) {
-    constexpr int N = Vec<DT>::N, SZ = DT == HWR_F32 ? 4 : 2;
-    const int64_t left = n - e0;
-    if (left >= chunk_elems(DT) && ((uintptr_t)in & 15) == 0) {
-        const uint4 *v = (const uint4 *)((const char *)in + e0 * SZ) + threadIdx.x;
+__device__ __forceinline__ void sum_chunk(const ClipChunk &c, float &acc, double &wide) {
+    constexpr int N = Vec<DT>::N;
+    const bool vec = c.n == Vec<DT>::FULL && ((uintptr_t)c.in & 15) == 0;
+    float s = 0.f;
+    if (vec) {
+        const uint4 *v = (const uint4 *)c.in + threadIdx.x;
         uint4 u[CL_PER];
 #pragma unroll
         for (int i = 0; i < CL_PER; ++i) u[i] = v[i * CL_THREADS];
@@ -448,24 +513,33 @@ __device__ __forceinline__ void sum_chunk(const void *in, int64_t e0, int64_t n,
         for (int i = 0; i < CL_PER; ++i) {
             float f[N];
             Vec<DT>::unpack(u[i], f);
-            add_squares(f, acc, wide);
+#pragma unroll
+            for (int j = 0; j < N; ++j) s = fmaf(f[j], f[j], s);
         }
-        return;
+        // all zeros: nothing was lost
+        uint32_t any = 0;
+#pragma unroll
+        for (int i = 0; i < CL_PER; ++i) any |= u[i].x | u[i].y | u[i].z | u[i].w;
+        if (any == 0) return;
+    } else {
+        bool any = false;
+        for (int i = threadIdx.x; i < c.n; i += CL_THREADS) {
+            const float f = Vec<DT>::load(c.in, i);
+            any |= f != 0.f;
+            s = fmaf(f, f, s);
+        }
+        if (!any) return;
     }
-    const int64_t stop = left < chunk_elems(DT) ? left : chunk_elems(DT);
-    for (int64_t i = threadIdx.x; i < stop; i += CL_THREADS) {
-        float f[1] = {load1<DT>(in, e0 + i)};
-        add_squares(f, acc, wide);
-    }
+    if (s >= 1e-30f && s <= 1e30f) acc += s;
+    else wide += wide_squares<DT>(c.in, c.n, vec);      // NaN and infinities too
 }
 
 template <int DT>
-__device__ __forceinline__ void scale_chunk(const void *in, void *out, int64_t e0, int64_t n, float k) {
-    constexpr int N = Vec<DT>::N, SZ = DT == HWR_F32 ? 4 : 2;
-    const int64_t left = n - e0;
-    if (left >= chunk_elems(DT) && (((uintptr_t)in | (uintptr_t)out) & 15) == 0) {
-        const uint4 *v = (const uint4 *)((const char *)in + e0 * SZ) + threadIdx.x;
-        uint4 *o = (uint4 *)((char *)out + e0 * SZ) + threadIdx.x;
+__device__ __forceinline__ void scale_chunk(const ClipChunk &c, float k) {
+    constexpr int N = Vec<DT>::N;
+    if (c.n == Vec<DT>::FULL && (((uintptr_t)c.in | (uintptr_t)c.out) & 15) == 0) {
+        const uint4 *v = (const uint4 *)c.in + threadIdx.x;
+        uint4 *o = (uint4 *)c.out + threadIdx.x;
         uint4 u[CL_PER];
 #pragma unroll
         for (int i = 0; i < CL_PER; ++i) u[i] = v[i * CL_THREADS];
@@ -479,19 +553,7 @@ __device__ __forceinline__ void scale_chunk(const void *in, void *out, int64_t e
         }
         return;
     }
-    const int64_t stop = left < chunk_elems(DT) ? left : chunk_elems(DT);
-    for (int64_t i = threadIdx.x; i < stop; i += CL_THREADS)
-        store1<DT>(out, e0 + i, load1<DT>(in, e0 + i) * k);
-}
-
-__device__ __forceinline__ int tensor_of(const ClipTable &t, int chunk) {
-    int lo = 0, hi = t.n - 1;
-    while (lo < hi) {
-        const int m = (lo + hi + 1) >> 1;
-        if (t.chunk0[m] <= chunk) lo = m;
-        else hi = m - 1;
-    }
-    return lo;
+    for (int i = threadIdx.x; i < c.n; i += CL_THREADS) Vec<DT>::store(c.out, i, Vec<DT>::load(c.in, i) * k);
 }
 
 __device__ __forceinline__ double block_sum(double v) {
@@ -504,40 +566,59 @@ __device__ __forceinline__ double block_sum(double v) {
     return s;
 }
 
+// The table's entries of up to CLIP_TABLE tensors (kernel parameters), from
+// chunk `at` on: for lists that are used once.
 __global__ void __launch_bounds__(CL_THREADS)
-k_square_sums(const __grid_constant__ ClipTable t, double *part) {
-    float acc = 0.f;
-    double wide = 0;
-    const int chunks = t.chunk0[t.n];
-    for (int c = blockIdx.x; c < chunks; c += gridDim.x) {
-        const int k = tensor_of(t, c);
-        const int64_t n = t.count[k];
-        const int64_t e0 = (int64_t)(c - t.chunk0[k]) * chunk_elems(t.dtype[k]);
-        if (t.dtype[k] == HWR_F32) sum_chunk<HWR_F32>(t.in[k], e0, n, acc, wide);
-        else if (t.dtype[k] == HWR_BF16) sum_chunk<HWR_BF16>(t.in[k], e0, n, acc, wide);
-        else sum_chunk<HWR_F16>(t.in[k], e0, n, acc, wide);
+k_clip_table(const __grid_constant__ ClipTable t, ClipChunk *table) {
+    const int i = blockIdx.x * CL_THREADS + threadIdx.x;
+    if (i >= t.chunk0[t.n]) return;
+    int lo = 0, hi = t.n - 1;
+    while (lo < hi) {
+        const int m = (lo + hi + 1) >> 1;
+        if (t.chunk0[m] <= i) lo = m;
+        else hi = m - 1;
     }
-    const double s = block_sum((double)acc + wide);
-    if (threadIdx.x == 0) part[t.first_block + blockIdx.x] = s;
+    table[t.at + i] = clip_chunk(t.in[lo], t.out[lo], t.count[lo], t.dtype[lo], i - t.chunk0[lo]);
 }
 
 __global__ void __launch_bounds__(CL_THREADS)
-k_clip(const __grid_constant__ ClipTable t, const double *part, int nparts, float max_norm, float *norm) {
+k_square_sums(const ClipChunk *table, int chunks, double *part) {
+    float acc = 0.f;
+    double wide = 0;
+    pdl_begin();
+    int i = blockIdx.x;
+    ClipChunk c;
+    if (i < chunks) c = table[i];
+    for (; i < chunks; i += gridDim.x) {
+        const ClipChunk now = c;
+        if (i + gridDim.x < chunks) c = table[i + gridDim.x];
+        if (now.dtype == HWR_F32) sum_chunk<HWR_F32>(now, acc, wide);
+        else if (now.dtype == HWR_BF16) sum_chunk<HWR_BF16>(now, acc, wide);
+        else sum_chunk<HWR_F16>(now, acc, wide);
+    }
+    const double s = block_sum((double)acc + wide);
+    if (threadIdx.x == 0) part[blockIdx.x] = s;
+}
+
+__global__ void __launch_bounds__(CL_THREADS)
+k_clip(const ClipChunk *table, int chunks, const double *part, int nparts, float max_norm, float *norm) {
+    pdl_begin();
+    int i = chunks - 1 - (int)blockIdx.x;
+    ClipChunk c;
+    if (i >= 0) c = table[i];
     double s = 0;
-    for (int i = threadIdx.x; i < nparts; i += CL_THREADS) s += part[i];
+    for (int j = threadIdx.x; j < nparts; j += CL_THREADS) s += part[j];
     const float total = (float)sqrt(block_sum(s));
-    if (blockIdx.x == 0 && t.first_block == 0 && threadIdx.x == 0) *norm = total;
+    if (blockIdx.x == 0 && threadIdx.x == 0) *norm = total;
     float k = max_norm / (total + 1e-6f);
     if (k > 1.f || isinf(max_norm)) k = 1.f;        // NaN stays
-    const int chunks = t.chunk0[t.n];
-    for (int c = chunks - 1 - blockIdx.x; c >= 0; c -= gridDim.x) {
-        const int i = tensor_of(t, c);
-        if (k == 1.f && t.in[i] == t.out[i]) continue;
-        const int64_t n = t.count[i];
-        const int64_t e0 = (int64_t)(c - t.chunk0[i]) * chunk_elems(t.dtype[i]);
-        if (t.dtype[i] == HWR_F32) scale_chunk<HWR_F32>(t.in[i], t.out[i], e0, n, k);
-        else if (t.dtype[i] == HWR_BF16) scale_chunk<HWR_BF16>(t.in[i], t.out[i], e0, n, k);
-        else scale_chunk<HWR_F16>(t.in[i], t.out[i], e0, n, k);
+    for (; i >= 0; i -= gridDim.x) {
+        const ClipChunk now = c;
+        if (i >= (int)gridDim.x) c = table[i - gridDim.x];
+        if (k == 1.f && now.in == now.out) continue;
+        if (now.dtype == HWR_F32) scale_chunk<HWR_F32>(now, k);
+        else if (now.dtype == HWR_BF16) scale_chunk<HWR_BF16>(now, k);
+        else scale_chunk<HWR_F16>(now, k);
     }
 }
 
@@ -548,10 +629,10 @@ cudaError_t ops_prepare() {
     return cudaFuncSetAttribute(k_dispatch_place, attr, (int)place_smem(OPS_MAX_GROUPS));
 }
 
-// Blocks and rows per block of a dispatch: whole rounds, a block an SM at most.
+// Blocks and rows per block of a dispatch: whole rounds, two blocks an SM at most.
 static int dispatch_blocks(int rows, int nsm, int64_t *per_block) {
     const int64_t rounds = ((int64_t)rows + DP_ROWS - 1) / DP_ROWS;
-    const int64_t each = (rounds + nsm - 1) / nsm;
+    const int64_t each = (rounds + 2 * nsm - 1) / (2 * nsm);
     *per_block = (each < 1 ? 1 : each) * DP_ROWS;
     const int64_t b = (rows + *per_block - 1) / *per_block;
     return b < 1 ? 1 : (int)b;
@@ -560,38 +641,60 @@ static int dispatch_blocks(int rows, int nsm, int64_t *per_block) {
 size_t dispatch_scratch_ints(int rows, int groups, int nsm) {
     int64_t per;
     const int b = dispatch_blocks(rows, nsm, &per);
-    return b > 1 ? (size_t)b * (groups + 1) : 0;
+    return b > DP_CLUSTER ? (size_t)b * (groups + 1) : 0;
+}
+
+// A launch that may begin while the kernel before it ends (it waits by itself).
+static cudaLaunchConfig_t relaxed(int grid, int block, size_t smem, cudaStream_t s, cudaLaunchAttribute *at) {
+    cudaLaunchConfig_t cfg = {};
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.gridDim = dim3((unsigned)grid);
+    cfg.blockDim = dim3((unsigned)block);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    return cfg;
 }
 
 cudaError_t launch_dispatch(int rows, int groups, const int32_t *choice, int32_t *offsets, int32_t *order,
                             int32_t *scratch, int nsm, cudaStream_t s) {
+    cudaLaunchAttribute at[2];
+    if (rows <= DP_FEW) {
+        const cudaLaunchConfig_t cfg = relaxed(1, DP_FEW, 0, s, at);
+        return cudaLaunchKernelEx(&cfg, k_dispatch_few, rows, groups, choice, offsets, order);
+    }
     int64_t per;
     const int b = dispatch_blocks(rows, nsm, &per);
-    if (b > 1)
-        k_dispatch_count<<<b, DP_THREADS, (groups + 1) * 4, s>>>(rows, groups, per, choice, scratch);
-    k_dispatch_place<<<b, DP_THREADS, place_smem(groups), s>>>(rows, groups, per, choice,
-                                                              b > 1 ? scratch : nullptr, offsets, order);
-    return cudaGetLastError();
+    const int32_t *hist = b > DP_CLUSTER ? scratch : nullptr;
+    if (hist) {
+        const cudaLaunchConfig_t cfg = relaxed(b, DP_THREADS, (groups + 1) * 4, s, at);
+        const cudaError_t e = cudaLaunchKernelEx(&cfg, k_dispatch_count, rows, groups, per, choice, scratch);
+        if (e != cudaSuccess) return e;
+    }
+    cudaLaunchConfig_t cfg = relaxed(b, DP_THREADS, place_smem(groups), s, at);
+    if (!hist && b > 1) {
+        at[1].id = cudaLaunchAttributeClusterDimension;
+        at[1].val.clusterDim.x = b;
+        at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
+        cfg.numAttrs = 2;
+    }
+    return cudaLaunchKernelEx(&cfg, k_dispatch_place, rows, groups, per, choice, hist, offsets, order);
 }
 
 cudaError_t launch_sort_rows(const GroupPlan &plan, const SortRows &m, int places, int32_t *padded_offsets,
                              int32_t *padded_order, int nsm, cudaStream_t s) {
     const int64_t want = ((int64_t)places + SR_THREADS / 32 - 1) / (SR_THREADS / 32), most = (int64_t)nsm * 8;
-    k_sort_rows<<<(int)(want < most ? want : most), SR_THREADS, (plan.groups + 1) * 8, s>>>(plan, m, places, padded_offsets,
-                                                                                            padded_order);
-    return cudaGetLastError();
+    cudaLaunchAttribute at[1];
+    const cudaLaunchConfig_t cfg = relaxed((int)(want < most ? want : most), SR_THREADS, (plan.groups + 1) * 8, s, at);
+    return cudaLaunchKernelEx(&cfg, k_sort_rows, plan, m, places, padded_offsets, padded_order);
 }
 
 cudaError_t launch_low_few(const LowFew &p, bool f16, cudaStream_t s) {
-    cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute at[1];
-    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.gridDim = dim3((unsigned)p.plan.rows, (unsigned)((p.rank + 2 * GP_RC - 1) / (2 * GP_RC) * (2 * GP_RC / LF_RANKS)));
-    cfg.blockDim = dim3(LF_THREADS);
-    cfg.stream = s;
-    cfg.attrs = at;
-    cfg.numAttrs = 1;
+    cudaLaunchConfig_t cfg = relaxed(p.plan.rows, LF_THREADS, 0, s, at);
+    cfg.gridDim.y = (unsigned)((p.rank + 2 * GP_RC - 1) / (2 * GP_RC) * (2 * GP_RC / LF_RANKS));
     return f16 ? cudaLaunchKernelEx(&cfg, k_low_few<true>, p) : cudaLaunchKernelEx(&cfg, k_low_few<false>, p);
 }
 
@@ -610,17 +713,21 @@ int clip_blocks(int64_t chunks, int nsm) {
     return (int)(chunks < 1 ? 1 : chunks < most ? chunks : most);
 }
 
-int64_t clip_chunks(int64_t n, int dtype) { return (n + chunk_elems(dtype) - 1) / chunk_elems(dtype); }
-
-cudaError_t launch_square_sums(const ClipTable &t, int blocks, double *part, cudaStream_t s) {
-    k_square_sums<<<blocks, CL_THREADS, 0, s>>>(t, part);
+cudaError_t launch_clip_table(const ClipTable &t, ClipChunk *table, cudaStream_t s) {
+    const int chunks = t.chunk0[t.n];
+    if (chunks) k_clip_table<<<(chunks + CL_THREADS - 1) / CL_THREADS, CL_THREADS, 0, s>>>(t, table);
     return cudaGetLastError();
 }
 
-cudaError_t launch_clip(const ClipTable &t, int blocks, const double *part, int nparts, float max_norm,
-                        float *norm, cudaStream_t s) {
-    k_clip<<<blocks, CL_THREADS, 0, s>>>(t, part, nparts, max_norm, norm);
-    return cudaGetLastError();
+cudaError_t launch_clip(const ClipChunk *table, int chunks, int nsm, double *part, float max_norm, float *norm,
+                        cudaStream_t s) {
+    const int blocks = clip_blocks(chunks, nsm);
+    cudaLaunchAttribute at[1];
+    const cudaLaunchConfig_t cfg = relaxed(blocks, CL_THREADS, 0, s, at);
+    cudaError_t e = cudaLaunchKernelEx(&cfg, k_square_sums, table, chunks, part);
+    if (e == cudaSuccess)
+        e = cudaLaunchKernelEx(&cfg, k_clip, table, chunks, (const double *)part, blocks, max_norm, norm);
+    return e;
 }
 
 }  // namespace hwr

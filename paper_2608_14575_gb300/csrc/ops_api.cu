@@ -41,7 +41,6 @@ struct hwr_ops {
     float *part = nullptr;       // partial tiles of the grouped products
     uint32_t *count = nullptr;   // their arrivals (zeroed once, self-resetting)
     double *sums = nullptr;      // partial sums of squares
-    int sums_cap = 0;
     int32_t *status_h = nullptr, *status_d = nullptr;   // mapped: bounded waits that ran out
     long fail_at = 0, allocs = 0;                        // HWR_TEST_FAIL_ALLOC
 };
@@ -144,8 +143,7 @@ extern "C" hwr_status hwr_ops_create(void *cuda_stream, hwr_ops **out) {
         CK(c, cudaHostGetDevicePointer((void **)&c->status_d, c->status_h, 0), "status word");
         OK(alloc(c, &c->part, group_part_floats(c->ctas)));
         OK(alloc(c, &c->count, c->ctas));
-        c->sums_cap = clip_blocks(INT64_MAX, c->nsm);
-        OK(alloc(c, &c->sums, c->sums_cap));
+        OK(alloc(c, &c->sums, clip_blocks(INT64_MAX, c->nsm)));
         CK(c, cudaMemsetAsync(c->count, 0, c->ctas * sizeof(uint32_t), c->stream), "memset");
         return HWR_OK;
     };
@@ -668,65 +666,110 @@ extern "C" hwr_status hwr_adapter_backward(hwr_ops *c, const hwr_rows *r, const 
 
 // ---------------------------------------------------------------------------
 
+struct hwr_gradients {
+    ClipChunk *table = nullptr;
+    int chunks = 0;
+};
+
+static hwr_status check_gradients(hwr_ops *c, int32_t n, const hwr_gradient *grads, int64_t *chunks) {
+    if (n < 0 || (n && !grads)) return fail(c, HWR_ERR_INVALID_ARG, "n %d or a NULL array", n);
+    *chunks = 0;
+    for (int i = 0; i < n; ++i) {
+        const hwr_gradient &g = grads[i];
+        if (g.n < 0 || (g.n && (!g.in || !g.out)))
+            return fail(c, HWR_ERR_INVALID_ARG, "gradient %d: n %lld or a NULL array", i, (long long)g.n);
+        if (g.dtype != HWR_F32 && g.dtype != HWR_BF16 && g.dtype != HWR_F16)
+            return fail(c, HWR_ERR_DTYPE, "gradient %d: dtype %d", i, (int)g.dtype);
+        const uintptr_t mask = g.dtype == HWR_F32 ? 3 : 1;
+        if (((uintptr_t)g.in | (uintptr_t)g.out) & mask)
+            return fail(c, HWR_ERR_INVALID_ARG, "gradient %d is not aligned to its elements", i);
+        *chunks += g.n > INT64_MAX / 8 ? INT32_MAX : clip_chunks(g.n, g.dtype);
+        if (*chunks >= INT32_MAX) return fail(c, HWR_ERR_UNSUPPORTED, "too many elements");
+    }
+    return HWR_OK;
+}
+
+static hwr_status check_norm(hwr_ops *c, float max_norm, const float *norm) {
+    if (!norm) return fail(c, HWR_ERR_INVALID_ARG, "norm is NULL");
+    if (!(max_norm > 0.f)) return fail(c, HWR_ERR_INVALID_ARG, "max_norm %g", max_norm);
+    return HWR_OK;
+}
+
 extern "C" hwr_status hwr_clip_gradients(hwr_ops *c, int32_t n, const hwr_gradient *grads, float max_norm,
                                          float *norm) {
     if (!c) return HWR_ERR_INVALID_ARG;
     ApiRange range("hwr_clip_gradients");
     OK(ready(c));
-    if (n < 0 || (n && !grads) || !norm) return fail(c, HWR_ERR_INVALID_ARG, "n %d or a NULL array", n);
-    if (!(max_norm > 0.f)) return fail(c, HWR_ERR_INVALID_ARG, "max_norm %g", max_norm);
+    int64_t chunks;
+    OK(check_gradients(c, n, grads, &chunks));
+    OK(check_norm(c, max_norm, norm));
+    OK(reserve(c, (size_t)chunks * sizeof(ClipChunk)));
+    ClipChunk *table = (ClipChunk *)c->ws;
+    ClipTable t;
+    t.n = t.at = 0;
+    t.chunk0[0] = 0;
     for (int i = 0; i < n; ++i) {
         const hwr_gradient &g = grads[i];
-        if (g.n < 0 || (g.n && (!g.in || !g.out))) return fail(c, HWR_ERR_INVALID_ARG, "gradient %d: n %lld or a NULL array", i, (long long)g.n);
-        if (g.dtype != HWR_F32 && g.dtype != HWR_BF16 && g.dtype != HWR_F16)
-            return fail(c, HWR_ERR_DTYPE, "gradient %d: dtype %d", i, (int)g.dtype);
-        const uintptr_t mask = g.dtype == HWR_F32 ? 3 : 1;
-        if (((uintptr_t)g.in | (uintptr_t)g.out) & mask) return fail(c, HWR_ERR_INVALID_ARG, "gradient %d is not aligned to its elements", i);
-        if (clip_chunks(g.n, g.dtype) > INT32_MAX / 2) return fail(c, HWR_ERR_UNSUPPORTED, "gradient %d has %lld elements", i, (long long)g.n);
+        t.in[t.n] = g.in;
+        t.out[t.n] = g.out;
+        t.count[t.n] = g.n;
+        t.dtype[t.n] = (uint8_t)g.dtype;
+        t.chunk0[t.n + 1] = t.chunk0[t.n] + (int32_t)clip_chunks(g.n, g.dtype);
+        if (++t.n < CLIP_TABLE && i + 1 < n) continue;
+        CK(c, launch_clip_table(t, table, c->stream), "gradient table kernel");
+        t.at += t.chunk0[t.n];
+        t.n = 0;
     }
-    // tables of up to CLIP_TABLE tensors; each has its blocks' partial sums
-    int nparts = 0;
-    for (int pass = 0; pass < 2; ++pass) {
-        int first = 0;
-        for (int i = 0; i < n || i == 0;) {
-            ClipTable t;
-            t.n = 0;
-            t.first_block = first;
-            int64_t chunks = 0;
-            for (; i < n && t.n < CLIP_TABLE; ++i) {
-                const hwr_gradient &g = grads[i];
-                const int64_t k = clip_chunks(g.n, g.dtype);
-                if (k == 0) continue;
-                if (chunks + k > INT32_MAX) break;
-                t.in[t.n] = g.in;
-                t.out[t.n] = g.out;
-                t.count[t.n] = g.n;
-                t.dtype[t.n] = (uint8_t)g.dtype;
-                t.chunk0[t.n++] = (int32_t)chunks;
-                chunks += k;
-            }
-            t.chunk0[t.n] = (int32_t)chunks;
-            const int blocks = clip_blocks(chunks, c->nsm);
-            if (pass == 0) {
-                if (first + blocks > c->sums_cap) {
-                    CK(c, cudaStreamSynchronize(c->stream), "synchronize before regrow");
-                    double *more = nullptr;
-                    const int cap = 2 * (first + blocks);
-                    OK(alloc(c, &more, cap));
-                    CK(c, cudaMemcpyAsync(more, c->sums, first * sizeof(double), cudaMemcpyDeviceToDevice, c->stream), "copy");
-                    CK(c, cudaStreamSynchronize(c->stream), "synchronize");
-                    cudaFree(c->sums);
-                    c->sums = more;
-                    c->sums_cap = cap;
-                }
-                CK(c, launch_square_sums(t, blocks, c->sums, c->stream), "norm kernel");
-            } else {
-                CK(c, launch_clip(t, blocks, c->sums, nparts, max_norm, norm, c->stream), "clip kernel");
-            }
-            first += blocks;
-            if (n == 0) break;
-        }
-        nparts = first;
+    CK(c, launch_clip(table, (int)chunks, c->nsm, c->sums, max_norm, norm, c->stream), "clip kernel");
+    return HWR_OK;
+}
+
+extern "C" hwr_status hwr_gradients_create(hwr_ops *c, int32_t n, const hwr_gradient *grads, hwr_gradients **out) {
+    if (!c) return HWR_ERR_INVALID_ARG;
+    ApiRange range("hwr_gradients_create");
+    if (!out) return fail(c, HWR_ERR_INVALID_ARG, "out is NULL");
+    *out = nullptr;
+    OK(ready(c));
+    int64_t chunks;
+    OK(check_gradients(c, n, grads, &chunks));
+    hwr_gradients *l = new (std::nothrow) hwr_gradients;
+    ClipChunk *host = new (std::nothrow) ClipChunk[chunks ? chunks : 1];
+    hwr_status s = l && host ? HWR_OK : fail(c, HWR_ERR_OOM, "host allocation failed");
+    if (s == HWR_OK) s = alloc(c, &l->table, chunks ? chunks : 1);
+    if (s == HWR_OK) {
+        for (int i = 0; i < n; ++i)
+            for (int64_t k = 0, m = clip_chunks(grads[i].n, grads[i].dtype); k < m; ++k)
+                host[l->chunks++] = clip_chunk(grads[i].in, grads[i].out, grads[i].n, grads[i].dtype, k);
+        cudaError_t e = cudaMemcpyAsync(l->table, host, chunks * sizeof(ClipChunk), cudaMemcpyHostToDevice, c->stream);
+        if (e == cudaSuccess) e = cudaStreamSynchronize(c->stream);
+        if (e != cudaSuccess) s = cuda_fail(c, e, "gradient table");
     }
+    delete[] host;
+    if (s != HWR_OK) {
+        if (l) cudaFree(l->table);
+        delete l;
+        return s;
+    }
+    *out = l;
+    return HWR_OK;
+}
+
+extern "C" hwr_status hwr_gradients_clip(hwr_ops *c, const hwr_gradients *l, float max_norm, float *norm) {
+    if (!c) return HWR_ERR_INVALID_ARG;
+    ApiRange range("hwr_gradients_clip");
+    OK(ready(c));
+    if (!l) return fail(c, HWR_ERR_INVALID_ARG, "NULL list");
+    OK(check_norm(c, max_norm, norm));
+    CK(c, launch_clip(l->table, l->chunks, c->nsm, c->sums, max_norm, norm, c->stream), "clip kernel");
+    return HWR_OK;
+}
+
+extern "C" hwr_status hwr_gradients_destroy(hwr_ops *c, hwr_gradients *l) {
+    if (!l) return HWR_OK;
+    if (!c) return HWR_ERR_INVALID_ARG;
+    cudaStreamSynchronize(c->stream);
+    cudaFree(l->table);
+    cudaGetLastError();
+    delete l;
     return HWR_OK;
 }

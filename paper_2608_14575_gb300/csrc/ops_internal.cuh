@@ -133,21 +133,37 @@ cudaError_t launch_low_few(const LowFew &p, bool f16, cudaStream_t s);
 cudaError_t launch_pad(void *dst, int64_t dst_ld, const void *src, int64_t src_ld, int64_t src_z,
                        int64_t nz, int64_t rows, int cols, int nsm, cudaStream_t s);
 
-constexpr int CLIP_TABLE = 512;   // tensors of one launch (kernel parameters)
+constexpr int CLIP_CHUNK_BYTES = 16384;
+struct alignas(16) ClipChunk {
+    const void *in;
+    void *out;
+    int32_t n, dtype;
+    int64_t unused;
+};
+inline __host__ __device__ int clip_elems(int dtype) { return CLIP_CHUNK_BYTES / (dtype == HWR_F32 ? 4 : 2); }
+inline __host__ __device__ int64_t clip_chunks(int64_t n, int dtype) { return (n + clip_elems(dtype) - 1) / clip_elems(dtype); }
+inline __host__ __device__ ClipChunk clip_chunk(const void *in, void *out, int64_t n, int dtype, int64_t i) {
+    ClipChunk c;
+    const int64_t left = n - i * clip_elems(dtype);
+    c.in = (const char *)in + i * CLIP_CHUNK_BYTES;
+    c.out = (char *)out + i * CLIP_CHUNK_BYTES;
+    c.n = (int32_t)(left < clip_elems(dtype) ? left : clip_elems(dtype));
+    c.dtype = dtype;
+    c.unused = 0;
+    return c;
+}
+constexpr int CLIP_TABLE = 256;       // tensors of one launch of the table's kernel
 struct ClipTable {
-    int n;
-    int first_block;              // of this launch, among all partial sums
+    int n, at;                        // tensors; first chunk of them in the table
     const void *in[CLIP_TABLE];
     void *out[CLIP_TABLE];
     int64_t count[CLIP_TABLE];
     int32_t chunk0[CLIP_TABLE + 1];   // first chunk of each tensor
     uint8_t dtype[CLIP_TABLE];
 };
-
-int clip_blocks(int64_t chunks, int nsm);
-int64_t clip_chunks(int64_t n, int dtype);
-cudaError_t launch_square_sums(const ClipTable &t, int blocks, double *part, cudaStream_t s);
-cudaError_t launch_clip(const ClipTable &t, int blocks, const double *part, int nparts, float max_norm,
-                        float *norm, cudaStream_t s);
+int clip_blocks(int64_t chunks, int nsm);    // partial sums of a call
+cudaError_t launch_clip_table(const ClipTable &t, ClipChunk *table, cudaStream_t s);
+cudaError_t launch_clip(const ClipChunk *table, int chunks, int nsm, double *part, float max_norm, float *norm,
+                        cudaStream_t s);
 
 }  // namespace hwr

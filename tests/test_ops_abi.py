@@ -47,6 +47,9 @@ def test_calls_without_a_context(lib):
     assert lib.hwr_adapter_forward(None, ct.byref(r), ct.byref(a), None, 0) == bad
     assert lib.hwr_adapter_backward(None, ct.byref(r), ct.byref(a), None, 0, None, 0, None, None) == bad
     assert lib.hwr_clip_gradients(None, 0, None, 1.0, ct.byref(f)) == bad
+    assert lib.hwr_gradients_create(None, 0, None, None) == bad
+    assert lib.hwr_gradients_clip(None, None, 1.0, ct.byref(f)) == bad
+    assert lib.hwr_gradients_destroy(None, None) == _hwr.HWR_OK
     assert lib.hwr_ops_destroy(None) == _hwr.HWR_OK
 
 

@@ -415,6 +415,13 @@ def test_clip(ops, dt, sizes, factor):
     for g, o in zip(keep, out):
         want = g.double() * k
         assert ((o.double() - want).abs() <= want.abs() * (unit + 516 * 2.0 ** -24) + floor).all()
+    once = ops.gradient_list(grads, [o.zero_() for o in out])
+    for _ in range(2):
+        assert float(ops.clip_gradients(once, limit)) == float(got)
+    for g, o in zip(keep, out):
+        want = g.double() * k
+        assert ((o.double() - want).abs() <= want.abs() * (unit + 516 * 2.0 ** -24) + floor).all()
+    once.close()
     again = ops.clip_gradients(grads, limit)                 # in place
     assert float(again) == float(got)
     assert all(torch.equal(a, b) for a, b in zip(grads, out))
