@@ -44,7 +44,7 @@ using namespace umma;
 constexpr int THREADS = 320;
 constexpr int GATHER_WARPS = 4;
 constexpr int A_BYTES = 128 * GP_BK * 2;
-constexpr int MAX_STAGES = 12;
+constexpr int MAX_STAGES = 24;
 constexpr int SMEM_MAX = 227 * 1024;
 constexpr int MIN_PIECE = 4;       // iterations of the smallest piece of a cut tile
 
@@ -80,6 +80,12 @@ struct Tables {
 
 static_assert(OUT_PITCH % 16 == 0 && OUT_BYTES % 16 == 0 && offsetof(Tables, out) % 16 == 0 && sizeof(Tables) % 16 == 0,
               "staged rows are read and written 16 bytes at a time");
+
+// A group's matrix in an extension stage of one CTA: 32 ranks of blocks of 64
+// columns (MN-major), or rows of 32 or, with a small rank, 16 ranks.
+__host__ __device__ inline int ext_bytes(const GroupProduct &p) {
+    return p.dense_mn ? (p.bn / 2 + 63) / 64 * 4096 : p.bn / 2 * (p.rank <= 16 ? 32 : 64);
+}
 
 __host__ __device__ inline int table_bytes(const GroupProduct &p) {
     const int g = p.plan.groups + 1;
@@ -126,6 +132,11 @@ __device__ __forceinline__ int64_t mul_div(int64_t a, int b, int c) {
 __device__ __forceinline__ int64_t div_small(int64_t a, int64_t b) {
     if ((a | b) >> 32) return a / b;
     return (uint32_t)a / (uint32_t)b;
+}
+
+// Stages of the extension for n groups.
+__device__ __forceinline__ int ext_steps(const GroupProduct &p, int n) {
+    return p.ext_pack > 1 ? (n + p.ext_pack - 1) / p.ext_pack : n * ((p.rank + GP_RC - 1) / GP_RC);
 }
 
 // The pieces of this pair, in order.
@@ -256,12 +267,14 @@ struct Walk {
         int n = 0;
         for (int g = find(t.eoffs, p.plan.groups, w.first); g < p.plan.groups && t.eoffs[g] < w.first + w.count; ++g)
             n += max(t.eoffs[g], w.first) < min(t.eoffs[g + 1], w.first + w.count);
-        return n * ((p.rank + GP_RC - 1) / GP_RC);
+        return ext_steps(p, n);
     }
 };
 
 // The extension's stages of a piece, out of the tile's: for each group with rows
-// in the tile, the rank in steps of GP_RC.
+// in the tile, the rank in steps of GP_RC.  Where one step holds the whole rank,
+// the tile's rows of u are the same for all groups, and a stage takes up to
+// p.ext_pack groups' matrices beside them.
 struct Ext {
     const GroupProduct &p;
     const Tables &t;
@@ -272,7 +285,8 @@ struct Ext {
         r0 = 0;
         left = w.e1 - w.e0;
         settle();
-        for (int i = 0; i < w.e0 && g < p.plan.groups; ++i) advance();
+        for (int i = 0; i < w.e0 && g < p.plan.groups; ++i)
+            for (int q = 0; q < p.ext_pack; ++q) advance();
     }
     __device__ void settle() {
         for (; g < p.plan.groups; ++g) {
@@ -283,7 +297,9 @@ struct Ext {
         }
         g = p.plan.groups;
     }
-    __device__ void advance() {
+    __device__ bool here() const { return g < p.plan.groups; }
+    __device__ void advance() {          // the next group's matrix (or ranks)
+        if (!here()) return;
         r0 += GP_RC;
         if (r0 >= p.rank) {
             r0 = 0;
@@ -291,10 +307,14 @@ struct Ext {
             settle();
         }
     }
-    __device__ bool more() const { return left > 0 && g < p.plan.groups; }
-    __device__ void step() {
+    // stages: while (e.more()) { up to p.ext_pack times, while here(): ...; advance() }
+    __device__ bool more() {
+        if (left <= 0 || !here()) return false;
         --left;
-        advance();
+        return true;
+    }
+    __device__ void skip() {             // a whole stage
+        for (int q = 0; q < p.ext_pack; ++q) advance();
     }
 };
 
@@ -347,7 +367,7 @@ __device__ void pick_rows(const GroupProduct &p, Tables &t, uint8_t *sm, int ran
     Ring at(p.stages);
     bool ok = true;
     const int tid = threadIdx.x & 127, sub = tid >> 3, c = tid & 7;
-    const uint32_t dst = (p.mode == GP_GROUPED ? A_BYTES : 0) + sub * 128 + ((c ^ (sub & 7)) << 4);
+    const uint32_t dst = (p.mode == GP_GROUPED ? p.b_off : 0) + sub * 128 + ((c ^ (sub & 7)) << 4);
     while (ok && walk.next(w)) {
         // this CTA's rows of the tile: its 128 of the A side, or its half of the B side
         const int half = p.mode == GP_GROUPED ? up16(w.count) >> 1 : 128;
@@ -358,24 +378,26 @@ __device__ void pick_rows(const GroupProduct &p, Tables &t, uint8_t *sm, int ran
             const int q = sub + i * 16, r = q < mine ? row_at(p, w.first + rank * half + q) : -1;
             row[i] = r < 0 ? nullptr : p.x + r * p.x_ld;
         }
-        int stages = w.k1 - w.k0;
-        if (p.rank)
-            for (Ext e(p, t, w); e.more(); e.step()) ++stages;   // of these only the arrival is due
-        for (int i0 = 0; i0 < stages; ++i0, at.step()) {
-            const int kb = w.k0 + i0;
+        for (int kb = w.k0; kb < w.k1; ++kb, at.step()) {
             ok = mbar_wait(&t.empty[at.s], at.ph ^ 1, &t.abort_f, p.status);
             ok = __all_sync(0xffffffffu, ok);
             if (!ok) break;
-            if (kb < w.k1) {
-                const uint32_t st = smem_u32(sm + (size_t)at.s * p.stage_bytes) + dst;
-                const int col = kb * GP_BK + c * 8, left = p.k - col;
-                const uint32_t bytes = left >= 8 ? 16 : left > 0 ? left * 2 : 0;   // beyond: zeros
+            const uint32_t st = smem_u32(sm + (size_t)at.s * p.stage_bytes) + dst;
+            const int col = kb * GP_BK + c * 8, left = p.k - col;
+            const uint32_t bytes = left >= 8 ? 16 : left > 0 ? left * 2 : 0;   // beyond: zeros
 #pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    if (row[i]) cp_async16(st + i * 2048, row[i] + (bytes ? col : 0), bytes);
-            }
+            for (int i = 0; i < 8; ++i)
+                if (row[i]) cp_async16(st + i * 2048, row[i] + (bytes ? col : 0), bytes);
             cp_async_arrive(&t.rowsf[at.s]);
         }
+        // of the extension's stages only the arrival is due
+        if (p.rank && ok)
+            for (Ext e(p, t, w); e.more(); e.skip(), at.step()) {
+                ok = mbar_wait(&t.empty[at.s], at.ph ^ 1, &t.abort_f, p.status);
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+                cp_async_arrive(&t.rowsf[at.s]);
+            }
     }
     cp_async_wait_all();
 }
@@ -476,7 +498,7 @@ k_group(const __grid_constant__ GroupMaps maps, const __grid_constant__ GroupPro
         int n = 0;
         for (int g = lane; g < p.plan.groups; g += 32) n += t.eoffs[g] < t.eoffs[g + 1];
         n = __reduce_add_sync(0xffffffffu, n);
-        if (lane == 0) t.ext = t.offs[1] <= GP_TILE ? n * ((p.rank + GP_RC - 1) / GP_RC) : -1;
+        if (lane == 0) t.ext = t.offs[1] <= GP_TILE ? ext_steps(p, n) : -1;
     }
     tc_fence_before();
     __syncthreads();
@@ -498,8 +520,8 @@ k_group(const __grid_constant__ GroupMaps maps, const __grid_constant__ GroupPro
             const int half = grouped ? 128 : p.bn >> 1;           // of the dense operand
             const int blocks = (half + 63) >> 6;                  // MN-major blocks of 64
             const uint32_t dbytes = p.dense_mn ? blocks * 8192 : half * 128;
-            const uint32_t ebytes = p.dense_mn ? blocks * 4096 : half * 64;
-            const uint32_t dside = grouped ? 0 : A_BYTES, xside = grouped ? A_BYTES : 0;
+            const uint32_t ebytes = ext_bytes(p);
+            const uint32_t dside = grouped ? 0 : p.b_off, xside = grouped ? p.b_off : 0;
             const uint32_t full0 = smem_of(&t.full[0], 0);
             auto claim = [&](uint32_t bytes) {
                 ok = mbar_wait(&t.empty[at.s], at.ph ^ 1, abort_f, p.status);
@@ -544,17 +566,23 @@ k_group(const __grid_constant__ GroupMaps maps, const __grid_constant__ GroupPro
                         tma_load_3d_pair(st + dside, &maps.w, full0 + at.s * 8, kb * GP_BK, o0, w.g);
                 }
                 if (shared && ok)
-                    for (Ext e(p, t, w); e.more(); e.step(), at.step()) {
-                        if (!claim(2 * ebytes + xbytes)) break;
+                    for (Ext e(p, t, w); e.more(); at.step()) {
+                        Ext f = e;
+                        int n = 0;
+                        for (; n < p.ext_pack && f.here(); ++n) f.advance();
+                        if (!claim(2 * n * ebytes + xbytes)) break;
                         uint8_t *st = sm + (size_t)at.s * p.stage_bytes;
                         for (int b = 0; b < boxes; ++b)
                             tma_load_3d_pair(st + b * GP_ROW_BOX * 128, &maps.u, full0 + at.s * 8, e.r0 * 2,
                                              x0 + b * GP_ROW_BOX, 0);
-                        if (p.dense_mn)
-                            for (int b = 0; b < blocks; ++b)
-                                tma_load_3d_pair(st + A_BYTES + b * 4096, &maps.eb, full0 + at.s * 8, o0 + b * 64, e.r0, e.g);
-                        else
-                            tma_load_3d_pair(st + A_BYTES, &maps.eb, full0 + at.s * 8, e.r0, o0, e.g);
+                        for (int q = 0; q < n; ++q, e.advance()) {
+                            uint8_t *eb = st + p.b_off + q * ebytes;
+                            if (p.dense_mn)
+                                for (int b = 0; b < blocks; ++b)
+                                    tma_load_3d_pair(eb + b * 4096, &maps.eb, full0 + at.s * 8, o0 + b * 64, e.r0, e.g);
+                            else
+                                tma_load_3d_pair(eb, &maps.eb, full0 + at.s * 8, e.r0, o0, e.g);
+                        }
                     }
             }
             // the loads still in flight land before the pair can exit
@@ -595,7 +623,7 @@ k_group(const __grid_constant__ GroupMaps maps, const __grid_constant__ GroupPro
                     ok = stage_ready();
                     if (!ok) break;
                     const uint32_t st = smem_u32(sm + (size_t)at.s * p.stage_bytes);
-                    const uint64_t ad = sdesc(st, 8192, 1024, 2), bd = sdesc(st + A_BYTES, 8192, 1024, 2);
+                    const uint64_t ad = sdesc(st, 8192, 1024, 2), bd = sdesc(st + p.b_off, 8192, 1024, 2);
                     // a gradient's last stage: whole 16s of rows, the group's padding
                     // among them (zeros), nothing of the next group
                     const int steps = grad ? min(4, max(1, (w.count - kb * GP_BK + 15) >> 4)) : 4;
@@ -607,28 +635,31 @@ k_group(const __grid_constant__ GroupMaps maps, const __grid_constant__ GroupPro
                 if (!ok) break;
                 if (shared) {
                     const uint32_t eidesc = idesc_16bit(GP_TILE, p.bn, F16, false, p.dense_mn);
-                    for (Ext e(p, t, w); e.more(); e.step(), at.step()) {
-                        uint32_t off[8];
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            const int a = min(max(e.a - w.first - 32 * i, 0), 32);
-                            const int z = min(max(e.b - w.first - 32 * i, 0), 32);
-                            // rows [a, z) of this word take part
-                            const uint32_t below = a == 32 ? 0xffffffffu : (1u << a) - 1;
-                            const uint32_t upto = z == 32 ? 0xffffffffu : (1u << z) - 1;
-                            off[i] = ~(upto & ~below);
-                        }
+                    for (Ext e(p, t, w); e.more(); at.step()) {
                         ok = stage_ready();
                         if (!ok) break;
                         const uint32_t st = smem_u32(sm + (size_t)at.s * p.stage_bytes);
                         const uint64_t ad = sdesc(st, 0, 1024, 2);
-                        const uint64_t bd = p.dense_mn ? sdesc(st + A_BYTES, 4096, 1024, 2)
-                                                       : sdesc(st + A_BYTES, 0, 512, 4);
-                        const int steps = min(GP_RC, p.rank - e.r0) > 16 ? 2 : 1;
-                        const uint32_t eb = p.dense_mn ? 2048 >> 4 : 2;
-                        for (int k = 0; k < steps; ++k) {
-                            mma_pair_rows(d, ad + 2 * k, bd + eb * k, eidesc, off);
-                            mma_pair_rows(d, ad + 4 + 2 * k, bd + eb * k, eidesc, off);
+                        for (int q = 0; q < p.ext_pack && e.here(); ++q, e.advance()) {
+                            uint32_t off[8];
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) {
+                                const int a = min(max(e.a - w.first - 32 * i, 0), 32);
+                                const int z = min(max(e.b - w.first - 32 * i, 0), 32);
+                                // rows [a, z) of this word take part
+                                const uint32_t below = a == 32 ? 0xffffffffu : (1u << a) - 1;
+                                const uint32_t upto = z == 32 ? 0xffffffffu : (1u << z) - 1;
+                                off[i] = ~(upto & ~below);
+                            }
+                            const uint32_t eb = st + p.b_off + q * ext_bytes(p);
+                            const uint64_t bd = p.dense_mn ? sdesc(eb, 4096, 1024, 2)
+                                                : p.rank <= 16 ? sdesc(eb, 0, 256, 6) : sdesc(eb, 0, 512, 4);
+                            const int steps = min(GP_RC, p.rank - e.r0) > 16 ? 2 : 1;
+                            for (int k = 0; k < steps; ++k) {
+                                const uint64_t bk = bd + (p.dense_mn ? (2048 >> 4) * k : 2 * k);
+                                mma_pair_rows(d, ad + 2 * k, bk, eidesc, off);
+                                mma_pair_rows(d, ad + 4 + 2 * k, bk, eidesc, off);
+                            }
                         }
                         mma_commit_pair(&t.empty[at.s]);
                     }
@@ -646,15 +677,19 @@ k_group(const __grid_constant__ GroupMaps maps, const __grid_constant__ GroupPro
             Walk walk(p, t);
             Work w;
             while (ok && walk.next(w)) {
-                int stages = w.k1 - w.k0;
-                if (shared)
-                    for (Ext e(p, t, w); e.more(); e.step()) ++stages;
-                for (; stages > 0; --stages, at.step()) {
+                auto pass = [&]() {
                     ok = mbar_wait(&t.rowsf[at.s], at.ph, abort_f, p.status);
-                    if (!ok) break;
+                    if (!ok) return false;
                     fence_proxy_async_smem();
                     mbar_arrive_cluster(full0 + at.s * 8);
-                }
+                    at.step();
+                    return true;
+                };
+                for (int kb = w.k0; kb < w.k1; ++kb)
+                    if (!pass()) break;
+                if (shared && ok)
+                    for (Ext e(p, t, w); e.more(); e.skip())
+                        if (!pass()) break;
             }
         }
         __syncwarp();
@@ -958,10 +993,20 @@ cudaError_t group_prepare(int nsm, int *ctas) {
 size_t group_part_floats(int ctas) { return (size_t)ctas * 2 * 128 * GP_TILE; }
 
 void group_plan(GroupProduct *p) {
-    // B side: whole 1 KB; MN-major operands come in blocks of 64 columns
-    int b = (p->sorted ? (p->bn / 2 + GP_ROW_BOX - 1) / GP_ROW_BOX * GP_ROW_BOX : p->bn / 2) * 128;
+    // B side: whole 1 KB; MN-major operands come in blocks of 64 columns.  Few
+    // picked rows take the room of their own groups of 8 on the A side: the MMA
+    // reads on into the B side for the rows that do not count
+    int a = A_BYTES, b = (p->sorted ? (p->bn / 2 + GP_ROW_BOX - 1) / GP_ROW_BOX * GP_ROW_BOX : p->bn / 2) * 128;
     if (p->mode == GP_WGRAD || (p->mode == GP_ROWS && p->dense_mn)) b = (p->bn / 2 + 63) / 64 * 8192;
-    p->stage_bytes = A_BYTES + (b + 1023) / 1024 * 1024;
+    if (p->mode == GP_ROWS && !p->sorted && p->plan.rows < 128) a = (p->plan.rows + GP_ROW_BOX - 1) / GP_ROW_BOX * GP_ROW_BOX * 128;
+    b = (b + 1023) / 1024 * 1024;
+    p->b_off = a;
+    p->stage_bytes = a + b;
+    p->ext_pack = 1;
+    if (p->rank && p->rank <= GP_RC) {
+        const int fits = b / ext_bytes(*p);
+        p->ext_pack = fits < 1 ? 1 : fits;
+    }
     const int fit = (SMEM_MAX - 1024 - table_bytes(*p)) / p->stage_bytes;
     p->stages = fit < MAX_STAGES ? fit : MAX_STAGES;
     p->smem = 1024 + p->stages * p->stage_bytes + table_bytes(*p);

@@ -13,7 +13,7 @@ namespace {
 //
 // A block takes a run of consecutive rows in rounds of DP_ROWS; in a round each
 // warp holds DP_PER x 32 consecutive rows in registers.  The rows of a warp
-// that share a key find each other by a match over the warp, so a row's place
+// that share a key find each other by votes over the warp, so a row's place
 // is its key's first place (over the blocks, rounds and warps before it) plus
 // the peers in lower lanes: no atomics decide an order.  What the blocks before
 // hold of each key comes from shared memory within a cluster (up to DP_CLUSTER
@@ -35,6 +35,18 @@ __device__ __forceinline__ int key_of(const int32_t *choice, int64_t row, int64_
     if (row >= end) return G + 1;            // no row
     const int c = choice[row];
     return (uint32_t)c < (uint32_t)G ? c : G;
+}
+
+// Lanes of the warp with the same key (of nbits bits): a vote per bit.  (A match
+// over the warp takes a step per distinct key.)
+__device__ __forceinline__ uint32_t peers_of(int key, int nbits) {
+    uint32_t peers = 0xffffffffu;
+    for (int b = 0; b < nbits; ++b) {
+        const bool on = (key >> b) & 1;
+        const uint32_t v = __ballot_sync(0xffffffffu, on);
+        peers &= on ? v : ~v;
+    }
+    return peers;
 }
 
 // A few rows: a row's place is the number of rows that come before it.
@@ -76,14 +88,14 @@ k_dispatch_count(int rows, int G, int64_t per_block, const int32_t *choice, int3
     __syncthreads();
     const int64_t begin = blockIdx.x * per_block;
     const int64_t end = begin + per_block < rows ? begin + per_block : rows;
-    const int lane = threadIdx.x & 31;
+    const int lane = threadIdx.x & 31, nbits = 32 - __clz(G + 1);
     for (int64_t r0 = begin; r0 < end; r0 += DP_ROWS) {
         int key[DP_PER];
 #pragma unroll
         for (int i = 0; i < DP_PER; ++i) key[i] = key_of(choice, r0 + i * DP_THREADS + threadIdx.x, end, G);
 #pragma unroll
         for (int i = 0; i < DP_PER; ++i) {
-            const uint32_t peers = __match_any_sync(0xffffffffu, key[i]);
+            const uint32_t peers = peers_of(key[i], nbits);
             if (key[i] <= G && lane == __ffs(peers) - 1) atomicAdd(&sh[key[i]], __popc(peers));
         }
     }
@@ -110,6 +122,7 @@ k_dispatch_place(int rows, int G, int64_t per_block, const int32_t *choice, cons
                  int32_t *offsets, int32_t *order) {
     extern __shared__ int32_t sh[];
     const int G1 = G + 1, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, nb = gridDim.x;
+    const int nbits = 32 - __clz(G + 1);
     int32_t *wh = sh;                        // [DP_WARPS][G1] counts, then first places
     int32_t *base = sh + DP_WARPS * G1;      // [G1] next place of each key
     int32_t *total = base + G1;              // [G1] rows of each key in all
@@ -132,7 +145,7 @@ k_dispatch_place(int rows, int G, int64_t per_block, const int32_t *choice, cons
         int rank[DP_PER];
 #pragma unroll
         for (int i = 0; i < DP_PER; ++i) {
-            const uint32_t peers = __match_any_sync(0xffffffffu, key[i]);
+            const uint32_t peers = peers_of(key[i], nbits);
             const int leader = __ffs(peers) - 1;
             int c = 0;
             if (key[i] <= G && lane == leader) {
@@ -556,13 +569,15 @@ __device__ __forceinline__ void scale_chunk(const ClipChunk &c, float k) {
     for (int i = threadIdx.x; i < c.n; i += CL_THREADS) Vec<DT>::store(c.out, i, Vec<DT>::load(c.in, i) * k);
 }
 
-__device__ __forceinline__ double block_sum(double v) {
-    __shared__ double w[CL_THREADS / 32];
+// Sum of fp32 values over the warp, in lane 0 as a double.  (The GPU has few
+// 64-bit units: a reduction of doubles by every warp cost more than the reads.)
+__device__ __forceinline__ double warp_sum(float v, double wide) {
     for (int d = 16; d; d /= 2) v += __shfl_down_sync(0xffffffffu, v, d);
-    if ((threadIdx.x & 31) == 0) w[threadIdx.x >> 5] = v;
-    __syncthreads();
-    double s = 0;
-    for (int i = 0; i < CL_THREADS / 32; ++i) s += w[i];
+    double s = v;
+    if (__any_sync(0xffffffffu, wide != 0.0)) {
+        for (int d = 16; d; d /= 2) wide += __shfl_down_sync(0xffffffffu, wide, d);
+        s += wide;
+    }
     return s;
 }
 
@@ -581,8 +596,13 @@ k_clip_table(const __grid_constant__ ClipTable t, ClipChunk *table) {
     table[t.at + i] = clip_chunk(t.in[lo], t.out[lo], t.count[lo], t.dtype[lo], i - t.chunk0[lo]);
 }
 
+// The last block to finish adds the blocks' sums, in their order, and leaves
+// the norm and the factor.
 __global__ void __launch_bounds__(CL_THREADS)
-k_square_sums(const ClipChunk *table, int chunks, double *part) {
+k_square_sums(const ClipChunk *table, int chunks, ClipSums sums, float max_norm, float *norm) {
+    __shared__ double w[CL_THREADS / 32];
+    __shared__ bool last;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     float acc = 0.f;
     double wide = 0;
     pdl_begin();
@@ -596,22 +616,42 @@ k_square_sums(const ClipChunk *table, int chunks, double *part) {
         else if (now.dtype == HWR_BF16) sum_chunk<HWR_BF16>(now, acc, wide);
         else sum_chunk<HWR_F16>(now, acc, wide);
     }
-    const double s = block_sum((double)acc + wide);
-    if (threadIdx.x == 0) part[blockIdx.x] = s;
+    const double s = warp_sum(acc, wide);
+    if (lane == 0) w[warp] = s;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        double b = 0;
+        for (int k = 0; k < CL_THREADS / 32; ++k) b += w[k];
+        sums.part[blockIdx.x] = b;
+        __threadfence();
+        last = atomicAdd(sums.count, 1u) == gridDim.x - 1;
+        if (last) *sums.count = 0;
+        __threadfence();
+    }
+    __syncthreads();
+    if (!last) return;
+    double v = 0;
+    for (int k = threadIdx.x; k < gridDim.x; k += CL_THREADS) v += __ldcg(&sums.part[k]);
+    for (int d = 16; d; d /= 2) v += __shfl_down_sync(0xffffffffu, v, d);
+    if (lane == 0) w[warp] = v;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        double b = 0;
+        for (int k = 0; k < CL_THREADS / 32; ++k) b += w[k];
+        const float total = (float)sqrt(b);
+        const float k = max_norm / (total + 1e-6f);
+        *norm = total;
+        *sums.factor = k > 1.f || isinf(max_norm) ? 1.f : k;       // NaN stays
+    }
 }
 
 __global__ void __launch_bounds__(CL_THREADS)
-k_clip(const ClipChunk *table, int chunks, const double *part, int nparts, float max_norm, float *norm) {
+k_clip(const ClipChunk *table, int chunks, const float *factor) {
     pdl_begin();
     int i = chunks - 1 - (int)blockIdx.x;
     ClipChunk c;
     if (i >= 0) c = table[i];
-    double s = 0;
-    for (int j = threadIdx.x; j < nparts; j += CL_THREADS) s += part[j];
-    const float total = (float)sqrt(block_sum(s));
-    if (blockIdx.x == 0 && threadIdx.x == 0) *norm = total;
-    float k = max_norm / (total + 1e-6f);
-    if (k > 1.f || isinf(max_norm)) k = 1.f;        // NaN stays
+    const float k = *factor;
     for (; i >= 0; i -= gridDim.x) {
         const ClipChunk now = c;
         if (i >= (int)gridDim.x) c = table[i - gridDim.x];
@@ -719,14 +759,13 @@ cudaError_t launch_clip_table(const ClipTable &t, ClipChunk *table, cudaStream_t
     return cudaGetLastError();
 }
 
-cudaError_t launch_clip(const ClipChunk *table, int chunks, int nsm, double *part, float max_norm, float *norm,
-                        cudaStream_t s) {
+cudaError_t launch_clip(const ClipChunk *table, int chunks, int nsm, const ClipSums &sums, float max_norm,
+                        float *norm, cudaStream_t s) {
     const int blocks = clip_blocks(chunks, nsm);
     cudaLaunchAttribute at[1];
     const cudaLaunchConfig_t cfg = relaxed(blocks, CL_THREADS, 0, s, at);
-    cudaError_t e = cudaLaunchKernelEx(&cfg, k_square_sums, table, chunks, part);
-    if (e == cudaSuccess)
-        e = cudaLaunchKernelEx(&cfg, k_clip, table, chunks, (const double *)part, blocks, max_norm, norm);
+    cudaError_t e = cudaLaunchKernelEx(&cfg, k_square_sums, table, chunks, sums, max_norm, norm);
+    if (e == cudaSuccess && chunks) e = cudaLaunchKernelEx(&cfg, k_clip, table, chunks, (const float *)sums.factor);
     return e;
 }
 

@@ -40,7 +40,7 @@ struct hwr_ops {
     size_t ws_cap = 0;
     float *part = nullptr;       // partial tiles of the grouped products
     uint32_t *count = nullptr;   // their arrivals (zeroed once, self-resetting)
-    double *sums = nullptr;      // partial sums of squares
+    double *sums = nullptr;      // partial sums of squares; then their arrivals and the factor
     int32_t *status_h = nullptr, *status_d = nullptr;   // mapped: bounded waits that ran out
     long fail_at = 0, allocs = 0;                        // HWR_TEST_FAIL_ALLOC
 };
@@ -143,7 +143,8 @@ extern "C" hwr_status hwr_ops_create(void *cuda_stream, hwr_ops **out) {
         CK(c, cudaHostGetDevicePointer((void **)&c->status_d, c->status_h, 0), "status word");
         OK(alloc(c, &c->part, group_part_floats(c->ctas)));
         OK(alloc(c, &c->count, c->ctas));
-        OK(alloc(c, &c->sums, clip_blocks(INT64_MAX, c->nsm)));
+        OK(alloc(c, &c->sums, clip_blocks(INT64_MAX, c->nsm) + 1));
+        CK(c, cudaMemsetAsync(c->sums, 0, (clip_blocks(INT64_MAX, c->nsm) + 1) * sizeof(double), c->stream), "memset");
         CK(c, cudaMemsetAsync(c->count, 0, c->ctas * sizeof(uint32_t), c->stream), "memset");
         return HWR_OK;
     };
@@ -263,7 +264,8 @@ static hwr_status settle(hwr_ops *c, Operand *o) {
     return HWR_OK;
 }
 
-// A map over nz matrices: boxes of box0 columns (64: 128-byte swizzle, 32: 64-byte) x box1 rows.
+// A map over nz matrices: boxes of box0 columns (64, 32 or 16: swizzled over their
+// 128, 64 or 32 bytes) x box1 rows.
 static hwr_status encode(hwr_ops *c, CUtensorMap *m, bool f16, const Operand &o, int box0, int box1) {
     const cuuint64_t dims[3] = {(cuuint64_t)o.cols, (cuuint64_t)o.rows, (cuuint64_t)o.nz};
     const cuuint64_t strides[2] = {(cuuint64_t)o.ld * 2, (cuuint64_t)o.z * 2};
@@ -272,7 +274,10 @@ static hwr_status encode(hwr_ops *c, CUtensorMap *m, bool f16, const Operand &o,
     const CUresult r = g_encode(
         m, f16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void *>(o.p),
         dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-        box0 == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+        box0 == 64   ? CU_TENSOR_MAP_SWIZZLE_128B
+        : box0 == 32 ? CU_TENSOR_MAP_SWIZZLE_64B
+                     : CU_TENSOR_MAP_SWIZZLE_32B,
+        CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
         CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     if (r != CUDA_SUCCESS)
         return fail(c, HWR_ERR_INVALID_ARG, "operand of %lld x %lld x %d (stride %lld) cannot be mapped",
@@ -296,6 +301,9 @@ struct Rows {
 // bytes bound the product (64 rows x 12 groups, 1024 -> 4096: 42 us picked).
 // More of them are copied by place once.
 constexpr int PICK_ROWS = 256;
+// Their shared product takes narrower tiles: more pairs have a tile of their own,
+// and a tile has fewer pieces to join.
+constexpr int FEW_BN = 128;
 constexpr int64_t LOW_FEW_VALUES = 16 << 20;   // values of the adapters read by a few rows
 
 // contracted: a gradient contracts over the rows, which takes the padded plan.
@@ -389,7 +397,7 @@ static hwr_status rows_product(hwr_ops *c, GroupProduct p, const Operand &x, con
         p.x_ld = x.ld;
     }
     if (p.mode == GP_GROUPED) p.bn = (int)up(p.plan.places < GP_TILE ? p.plan.places : GP_TILE, 16);
-    else p.bn = even_tiles(n, GP_TILE);
+    else p.bn = even_tiles(n, p.sorted || !p.shared ? GP_TILE : FEW_BN);
     group_plan(&p);
     OK(check_tiles(c, p));
     GroupMaps m;
@@ -401,7 +409,8 @@ static hwr_status rows_product(hwr_ops *c, GroupProduct p, const Operand &x, con
     OK(encode(c, &m.w, p.f16, w, 64, w_mn ? 64 : p.mode == GP_GROUPED ? 128 : p.bn / 2));
     if (u) {
         OK(encode(c, &m.u, p.f16, *u, 64, GP_ROW_BOX));
-        OK(w_mn ? encode(c, &m.eb, p.f16, *eb, 64, GP_RC) : encode(c, &m.eb, p.f16, *eb, GP_RC, p.bn / 2));
+        OK(w_mn ? encode(c, &m.eb, p.f16, *eb, 64, GP_RC)
+                : encode(c, &m.eb, p.f16, *eb, p.rank <= 16 ? 16 : GP_RC, p.bn / 2));
     }
     CK(c, launch_group(p, m, c->ctas, c->stream), "product kernel");
     return HWR_OK;
@@ -689,6 +698,14 @@ static hwr_status check_gradients(hwr_ops *c, int32_t n, const hwr_gradient *gra
     return HWR_OK;
 }
 
+static ClipSums clip_sums(const hwr_ops *c) {
+    ClipSums s;
+    s.part = c->sums;
+    s.count = (uint32_t *)(c->sums + clip_blocks(INT64_MAX, c->nsm));
+    s.factor = (float *)(s.count + 1);
+    return s;
+}
+
 static hwr_status check_norm(hwr_ops *c, float max_norm, const float *norm) {
     if (!norm) return fail(c, HWR_ERR_INVALID_ARG, "norm is NULL");
     if (!(max_norm > 0.f)) return fail(c, HWR_ERR_INVALID_ARG, "max_norm %g", max_norm);
@@ -720,7 +737,7 @@ extern "C" hwr_status hwr_clip_gradients(hwr_ops *c, int32_t n, const hwr_gradie
         t.at += t.chunk0[t.n];
         t.n = 0;
     }
-    CK(c, launch_clip(table, (int)chunks, c->nsm, c->sums, max_norm, norm, c->stream), "clip kernel");
+    CK(c, launch_clip(table, (int)chunks, c->nsm, clip_sums(c), max_norm, norm, c->stream), "clip kernel");
     return HWR_OK;
 }
 
@@ -760,7 +777,7 @@ extern "C" hwr_status hwr_gradients_clip(hwr_ops *c, const hwr_gradients *l, flo
     OK(ready(c));
     if (!l) return fail(c, HWR_ERR_INVALID_ARG, "NULL list");
     OK(check_norm(c, max_norm, norm));
-    CK(c, launch_clip(l->table, l->chunks, c->nsm, c->sums, max_norm, norm, c->stream), "clip kernel");
+    CK(c, launch_clip(l->table, l->chunks, c->nsm, clip_sums(c), max_norm, norm, c->stream), "clip kernel");
     return HWR_OK;
 }
 

@@ -65,7 +65,9 @@ struct GroupProduct {
     int ntiles = 0, mtiles = 0;       // column tiles; row tiles of a gradient
     int f16 = 0;
     int stages = 0, stage_bytes = 0, smem = 0;
+    int b_off = 0;                    // of the B side in a stage
     int rank = 0;                     // of the low-rank extension of a shared product
+    int ext_pack = 1;                 // groups in one of its stages
     // output
     int out_kind = 0;
     int vec = 0;                      // 16-byte stores
@@ -163,7 +165,12 @@ struct ClipTable {
 };
 int clip_blocks(int64_t chunks, int nsm);    // partial sums of a call
 cudaError_t launch_clip_table(const ClipTable &t, ClipChunk *table, cudaStream_t s);
-cudaError_t launch_clip(const ClipChunk *table, int chunks, int nsm, double *part, float max_norm, float *norm,
-                        cudaStream_t s);
+struct ClipSums {
+    double *part;                     // [clip_blocks]
+    uint32_t *count;                  // blocks that have finished (zeroed once, self-resetting)
+    float *factor;                    // what the gradients are scaled by
+};
+cudaError_t launch_clip(const ClipChunk *table, int chunks, int nsm, const ClipSums &sums, float max_norm,
+                        float *norm, cudaStream_t s);
 
 }  // namespace hwr
