@@ -3,15 +3,19 @@
 Each .cu file of csrc/ is compiled to an object in parallel, then linked into
 one shared library with the CUDA runtime linked statically, so that loading
 it needs no libcudart on the library path.  The output goes to
-``_build/libhwr_<machine>.so`` next to this file (git-ignored).
+``_build/libhwr_<machine>.so`` next to this file (git-ignored).  The torch
+binding of the operators (csrc/ops_torch.cpp, g++) is compiled beside it into
+``_build/hwr_torch_<machine>.so``, which links the library.
 """
 from __future__ import annotations
 
+import importlib.util
 import os
 import platform
 import shutil
 import subprocess
 import sys
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
@@ -37,6 +41,28 @@ def lib_path() -> str:
     return os.path.join(OUT_DIR, f"libhwr_{platform.machine()}.so")
 
 
+def torch_path() -> str:
+    return os.path.join(OUT_DIR, f"hwr_torch_{platform.machine()}.so")
+
+
+def _torch_commands(out: str):
+    """Compile and link commands of the torch binding."""
+    spec = importlib.util.find_spec("torch")
+    if spec is None or not spec.submodule_search_locations:
+        raise RuntimeError("torch not found: the operators' binding needs its headers")
+    torch = list(spec.submodule_search_locations)[0]
+    obj = os.path.join(OUT_DIR, f"ops_torch_{platform.machine()}.o")
+    compile_ = ["g++", "-O2", "-std=c++17", "-fPIC", "-fvisibility=hidden", "-I", INCLUDE,
+                "-isystem", os.path.join(torch, "include"),
+                "-isystem", os.path.join(torch, "include", "torch", "csrc", "api", "include"),
+                "-isystem", sysconfig.get_paths()["include"],
+                "-c", os.path.join(CSRC, "ops_torch.cpp"), "-o", obj]
+    lib = os.path.join(torch, "lib")
+    link = ["g++", "-shared", obj, "-o", out, lib_path(), "-L", lib, "-ltorch_python",
+            "-ltorch_cpu", "-lc10", "-Wl,-rpath,$ORIGIN"]
+    return compile_, link
+
+
 def _nvcc() -> str:
     p = shutil.which("nvcc") or "/usr/local/cuda/bin/nvcc"
     if not os.path.exists(p):
@@ -45,9 +71,9 @@ def _nvcc() -> str:
 
 
 def _stale(out: str) -> bool:
-    if not os.path.exists(out):
+    if not os.path.exists(out) or not os.path.exists(torch_path()):
         return True
-    t = os.path.getmtime(out)
+    t = min(os.path.getmtime(out), os.path.getmtime(torch_path()))
     deps = [os.path.join(CSRC, f) for f in os.listdir(CSRC)]
     deps += [os.path.join(INCLUDE, f) for f in os.listdir(INCLUDE)]
     deps.append(os.path.abspath(__file__))
@@ -75,6 +101,10 @@ def build(force: bool = False, verbose: bool = False, ptxas_info: bool = False) 
             print(" ".join(cmd), flush=True)
         procs.append((src, subprocess.Popen(cmd, stdout=subprocess.PIPE,
                                             stderr=subprocess.STDOUT, text=True)))
+    torch_out = torch_path() + ".tmp"
+    torch_compile, torch_link = _torch_commands(torch_out)
+    procs.append(("ops_torch.cpp", subprocess.Popen(torch_compile, stdout=subprocess.PIPE,
+                                                    stderr=subprocess.STDOUT, text=True)))
     errors = []
     for src, p in procs:
         text, _ = p.communicate()
@@ -88,6 +118,8 @@ def build(force: bool = False, verbose: bool = False, ptxas_info: bool = False) 
     link = [nvcc, "-shared", *ARCH, "-cudart", "static", *objs, "-o", tmp]
     subprocess.run(link, check=True)
     os.replace(tmp, out)
+    subprocess.run(torch_link, check=True)
+    os.replace(torch_out, torch_path())
     return out
 
 

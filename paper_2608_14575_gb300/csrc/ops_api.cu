@@ -42,6 +42,7 @@ struct hwr_ops {
     uint32_t *count = nullptr;   // their arrivals (zeroed once, self-resetting)
     double *sums = nullptr;      // partial sums of squares; then their arrivals and the factor
     int32_t *status_h = nullptr, *status_d = nullptr;   // mapped: bounded waits that ran out
+    cudaEvent_t event = nullptr;                         // hwr_ops_after / before
     long fail_at = 0, allocs = 0;                        // HWR_TEST_FAIL_ALLOC
 };
 
@@ -166,6 +167,7 @@ extern "C" hwr_status hwr_ops_destroy(hwr_ops *c) {
     cudaFree(c->count);
     cudaFree(c->sums);
     if (c->status_h) cudaFreeHost(c->status_h);
+    if (c->event) cudaEventDestroy(c->event);
     if (c->own_stream) cudaStreamDestroy(c->stream);
     cudaGetLastError();
     delete c;
@@ -181,6 +183,27 @@ extern "C" hwr_status hwr_ops_synchronize(hwr_ops *c) {
 
 extern "C" const char *hwr_ops_last_error(const hwr_ops *c) {
     return c ? c->err.c_str() : g_create_error.c_str();
+}
+
+static hwr_status order_streams(hwr_ops *c, cudaStream_t first, cudaStream_t then) {
+    if (!c->event) CK(c, cudaEventCreateWithFlags(&c->event, cudaEventDisableTiming), "event");
+    CK(c, cudaEventRecord(c->event, first), "event record");
+    CK(c, cudaStreamWaitEvent(then, c->event, 0), "stream wait");
+    return HWR_OK;
+}
+
+extern "C" hwr_status hwr_ops_after(hwr_ops *c, void *stream) {
+    if (!c) return HWR_ERR_INVALID_ARG;
+    OK(ready(c));
+    if (!stream) return fail(c, HWR_ERR_INVALID_ARG, "NULL stream");
+    return order_streams(c, (cudaStream_t)stream, c->stream);
+}
+
+extern "C" hwr_status hwr_ops_before(hwr_ops *c, void *stream) {
+    if (!c) return HWR_ERR_INVALID_ARG;
+    OK(ready(c));
+    if (!stream) return fail(c, HWR_ERR_INVALID_ARG, "NULL stream");
+    return order_streams(c, c->stream, (cudaStream_t)stream);
 }
 
 extern "C" hwr_status hwr_ops_reserve(hwr_ops *c, uint64_t bytes) {

@@ -41,6 +41,7 @@ def test_calls_without_a_context(lib):
     assert lib.hwr_ops_create(None, None) == bad
     assert lib.hwr_ops_synchronize(None) == bad
     assert lib.hwr_ops_reserve(None, 1) == bad
+    assert lib.hwr_ops_after(None, None) == bad and lib.hwr_ops_before(None, None) == bad
     assert lib.hwr_dispatch(None, 1, 1, None, None, None) == bad
     assert lib.hwr_grouped_forward(None, ct.byref(r), None, 0) == bad
     assert lib.hwr_grouped_backward(None, ct.byref(r), None, 0, None, 0, None) == bad
