@@ -40,13 +40,15 @@ namespace {
 using namespace umma;
 
 // warps 0-3 epilogue, 4-7 epilogue too (sorted rows) or picking rows, 8 TMA, 9
-// MMA (even CTA) or relay (odd CTA)
-constexpr int THREADS = 320;
+// MMA (even CTA) or relay (odd CTA), 10 dealing the pieces
+constexpr int THREADS = 352;
+constexpr int PIECES = 4;          // pieces dealt ahead
 constexpr int GATHER_WARPS = 4;
 constexpr int A_BYTES = 128 * GP_BK * 2;
 constexpr int MAX_STAGES = 24;
 constexpr int SMEM_MAX = 227 * 1024;
-constexpr int MIN_PIECE = 4;       // iterations of the smallest piece of a cut tile
+constexpr int MIN_PIECE = 6 * GP_BK;   // columns of the smallest piece of a cut tile (joining costs about as much)
+constexpr int WRITE_COST = 4;      // iterations that writing a gradient's tile counts for
 
 constexpr int OUT_PITCH = 64;      // bytes of a staged output row (32 columns)
 constexpr int OUT_BYTES = 32 * OUT_PITCH;   // of a warp
@@ -59,6 +61,14 @@ __device__ __forceinline__ int staged_at(int row, int unit) {
 // What a kernel is compiled for (the epilogue's registers are those of its kind).
 enum : int { K_GROUPED = 0, K_SHARED = 1, K_PACK = 2, K_GRAD = 3, K_LOW = 4 };
 
+struct Work {
+    int g, xt, ot;        // group; tile of rows (gradients: of result rows); tile of columns
+    int k0, k1, ki;       // iterations of this piece, and of the tile
+    int c0, c1;           // first and last pair with a piece of the tile
+    int first, count;     // places of the tile (gradients: of the group)
+    int e0, e1;           // stages of the extension that go with the piece
+};
+
 // Shared memory behind the stages: this, then the group tables.
 struct Tables {
     // per stage: full (even CTA: both CTAs' bytes, and the odd CTA's word), rows
@@ -66,9 +76,15 @@ struct Tables {
     uint64_t full[MAX_STAGES], rowsf[MAX_STAGES], empty[MAX_STAGES], accf[2], acce[2], done;
     alignas(16) uint8_t out[8][OUT_BYTES];   // epilogue staging, a warp each
     int32_t rows[GP_TILE];               // the tile's rows of the output (epilogue)
+    // pieces dealt, for the warps that work on them
+    Work work[PIECES];
+    uint64_t dealt[PIECES], taken[PIECES];
     uint32_t tmem;
     int abort_f;
-    int last, go;        // epilogue: this piece writes the tile; the accumulator is there
+    // epilogue: its piece and whether there is one, the accumulator is there, this
+    // piece writes the tile
+    Work mine;
+    int go, ready, last;
     // group tables: ng groups of the tiles, and the extension's
     int ng;
     int ext;             // stages of the extension, where all places are in one tile (else -1)
@@ -115,14 +131,6 @@ struct Ring {
     }
 };
 
-struct Work {
-    int g, xt, ot;        // group; tile of rows (gradients: of result rows); tile of columns
-    int k0, k1, ki;       // iterations of this piece, and of the tile
-    int c0, c1;           // first and last pair with a piece of the tile
-    int first, count;     // places of the tile (gradients: of the group)
-    int e0, e1;           // stages of the extension that go with the piece
-};
-
 // a * b / c; 32-bit where that holds (a 64-bit division costs some 100 instructions)
 __device__ __forceinline__ int64_t mul_div(int64_t a, int b, int c) {
     const uint64_t v = (uint64_t)a * (uint32_t)b;
@@ -139,135 +147,169 @@ __device__ __forceinline__ int ext_steps(const GroupProduct &p, int n) {
     return p.ext_pack > 1 ? (n + p.ext_pack - 1) / p.ext_pack : n * ((p.rank + GP_RC - 1) / GP_RC);
 }
 
-// The pieces of this pair, in order.
+template <class T>
+__device__ __forceinline__ int find(const T *v, int n, T x) {   // last g with v[g] <= x
+    int lo = 0, hi = n - 1;
+    while (lo < hi) {
+        const int m = (lo + hi + 1) >> 1;
+        if (v[m] <= x) lo = m;
+        else hi = m - 1;
+    }
+    return lo;
+}
+
+// Iterations that a gradient's tile counts for: its own, or what writing it takes.
+__device__ __forceinline__ int grad_cost(const Tables &t, int g) {
+    return max(WRITE_COST, (max(0, t.offs[g + 1] - t.offs[g]) + GP_BK - 1) / GP_BK);
+}
+
+// How the iterations of all tiles are dealt: the first dp tiles whole, one to a
+// pair a round, the others as one line cut into `cutters` equal pieces.
 struct Walk {
     const GroupProduct &p;
     const Tables &t;
     int me, pairs, dp, kiters, cutters, next_tile;
-    int64_t base, rest, pos, end;    // the line of iterations: where it begins, its length; this pair's
+    int64_t base, rest;       // where the line begins (gradients), and its length
+    int64_t pos, end;         // of this pair's piece of it, what is left
 
     __device__ Walk(const GroupProduct &p_, const Tables &t_) : p(p_), t(t_) {
         const bool grad = p.mode == GP_WGRAD;
         const int per = p.mtiles * p.ntiles, tiles = grad ? t.ng * per : t.tile0[t.ng];
-        me = blockIdx.x >> 1;
+        me = next_tile = blockIdx.x >> 1;
         pairs = gridDim.x >> 1;
-        kiters = (p.k + GP_BK - 1) / GP_BK;
+        const int deep = GP_BK * p.kk;
+        kiters = (p.k + deep - 1) / deep;
         dp = tiles >= 2 * pairs ? (tiles / pairs - 1) * pairs : 0;
         base = 0;
         if (grad) {
-            const int g = dp / per;       // (dp < tiles: the group exists)
-            base = t.iter0[g] + (int64_t)(dp - g * per) * cost(g);
+            const int g = dp / per;           // (dp < tiles: the group exists)
+            base = t.iter0[g] + (int64_t)(dp - g * per) * grad_cost(t, g);
             rest = t.iter0[t.ng] - base;
         } else {
             rest = (int64_t)(tiles - dp) * kiters;
         }
-        const int64_t most = rest / MIN_PIECE;
+        const int64_t most = max(div_small(rest, max(1, MIN_PIECE / deep)), (int64_t)(tiles - dp));
         cutters = most < 1 ? 1 : most < pairs ? (int)most : pairs;
-        next_tile = me;
         pos = end = 0;
         if (me < cutters) {
             pos = mul_div(rest, me, cutters);
             end = mul_div(rest, me + 1, cutters);
         }
     }
-    // the pair whose piece holds iteration i of the line
-    __device__ int owner(int64_t i) const { return (int)div_small((i + 1) * cutters - 1, rest); }
-    // Iterations that a gradient's tile counts for: its own, or what writing it takes.
-    __device__ int cost(int g) const {
-        return max(MIN_PIECE, (max(0, t.offs[g + 1] - t.offs[g]) + GP_BK - 1) / GP_BK);
-    }
-    __device__ void place_grad(Work &w, int g, int local) const {
-        w.g = g;
-        w.first = t.offs[g];
-        w.count = max(0, t.offs[g + 1] - w.first);
-        w.ki = max(1, (w.count + GP_BK - 1) / GP_BK);
-        w.ot = local / p.mtiles;
-        w.xt = local - w.ot * p.mtiles;
-    }
-
-    template <class T>
-    __device__ static int find(const T *v, int n, T x) {   // last g with v[g] <= x
-        int lo = 0, hi = n - 1;
-        while (lo < hi) {
-            const int m = (lo + hi + 1) >> 1;
-            if (v[m] <= x) lo = m;
-            else hi = m - 1;
-        }
-        return lo;
-    }
-    __device__ void place(Work &w, int tile) const {
-        w.g = find(t.tile0, t.ng, tile);
-        const int local = tile - t.tile0[w.g];
-        const int n = t.offs[w.g + 1] - t.offs[w.g], xts = (n + GP_TILE - 1) / GP_TILE;
-        // bands of 32 row tiles, column by column: the pairs at work share
-        // columns of W and the band's rows stay in L2
-        const int band = local / (32 * p.ntiles), in = local - band * 32 * p.ntiles;
-        const int h = min(32, xts - band * 32);
-        w.ot = in / h;
-        w.xt = band * 32 + (in - w.ot * h);
-        // rows on the B side: tiles of about equal extent
-        const int width = p.mode == GP_GROUPED && xts <= 8 ? up16((n + xts - 1) / xts) : GP_TILE;
-        w.first = t.offs[w.g] + w.xt * width;
-        w.count = min(width, n - w.xt * width);
-    }
     __device__ bool next(Work &w) {
         const bool grad = p.mode == GP_WGRAD;
-        if (next_tile < dp) {
-            if (grad) {
-                const int per = p.mtiles * p.ntiles, g = next_tile / per;
-                place_grad(w, g, next_tile - g * per);
+        w.e0 = 0;
+        w.e1 = INT32_MAX;
+        while (true) {
+            int tile = next_tile, cost = kiters;
+            int64_t start = 0;       // of the tile, on the line
+            const bool whole = tile < dp;
+            if (whole) {
+                next_tile += pairs;
             } else {
-                place(w, next_tile);
+                if (pos >= end) return false;
+                if (grad) {
+                    const int g = find(t.iter0, t.ng, base + pos);
+                    cost = grad_cost(t, g);
+                    const int local = (int)div_small(base + pos - t.iter0[g], cost);
+                    start = t.iter0[g] + (int64_t)local * cost - base;
+                    tile = g * p.mtiles * p.ntiles + local;
+                } else {
+                    const int i = (int)div_small(pos, kiters);
+                    start = (int64_t)i * kiters;
+                    tile = dp + i;
+                }
+            }
+            if (grad) {
+                const int per = p.mtiles * p.ntiles, local = tile % per;
+                w.g = tile / per;
+                w.first = t.offs[w.g];
+                w.count = max(0, t.offs[w.g + 1] - w.first);
+                w.ki = max(1, (w.count + GP_BK - 1) / GP_BK);
+                w.ot = local / p.mtiles;
+                w.xt = local - w.ot * p.mtiles;
+            } else {
+                w.g = find(t.tile0, t.ng, tile);
+                const int local = tile - t.tile0[w.g];
+                const int n = t.offs[w.g + 1] - t.offs[w.g], xts = (n + GP_TILE - 1) / GP_TILE;
+                // bands of 32 row tiles, column by column: the pairs at work share
+                // columns of W and the band's rows stay in L2
+                const int band = local / (32 * p.ntiles), in = local - band * 32 * p.ntiles;
+                const int h = min(32, xts - band * 32);
+                w.ot = in / h;
+                w.xt = band * 32 + (in - w.ot * h);
+                // rows on the B side: tiles of about equal extent
+                const int width = p.mode == GP_GROUPED && xts <= 8 ? up16((n + xts - 1) / xts) : GP_TILE;
+                w.first = t.offs[w.g] + w.xt * width;
+                w.count = min(width, n - w.xt * width);
                 w.ki = kiters;
             }
-            next_tile += pairs;
-            w.k0 = 0;
-            w.k1 = w.ki;
-            w.c0 = w.c1 = me;
-            w.e0 = 0;
-            w.e1 = INT32_MAX;
-            return true;
-        }
-        while (pos < end) {
-            int64_t start, stop;      // of the tile, on the line
-            if (grad) {
-                const int g = find(t.iter0, t.ng, base + pos), c = cost(g);
-                const int local = (int)div_small(base + pos - t.iter0[g], c);
-                place_grad(w, g, local);
-                start = t.iter0[g] + (int64_t)local * c - base;
-                stop = start + c;
-            } else {
-                const int i = (int)div_small(pos, kiters);
-                place(w, dp + i);
-                w.ki = kiters;
-                start = (int64_t)i * kiters;
-                stop = start + kiters;
+            if (whole) {
+                w.k0 = 0;
+                w.k1 = w.ki;
+                w.c0 = w.c1 = me;
+                return true;
             }
-            const int64_t upto = stop < end ? stop : end;
+            const int64_t stop = start + cost < end ? start + cost : end;
             w.k0 = (int)(pos - start);
-            w.k1 = min((int)(upto - start), w.ki);
-            pos = upto;
+            w.k1 = min((int)(stop - start), w.ki);
+            pos = stop;
             if (w.k0 >= w.k1) continue;       // (of a gradient: nothing but what writing counts for)
-            w.c0 = owner(start);
-            w.c1 = owner(start + w.ki - 1);
-            w.e0 = 0;
-            w.e1 = INT32_MAX;
+            // the pairs with the tile's first and last iteration
+            w.c0 = (int)div_small((start + 1) * cutters - 1, rest);
+            w.c1 = (int)div_small((start + w.ki) * cutters - 1, rest);
             if (p.rank && w.c0 != w.c1) {
                 // a piece takes its share of the extension
-                const int all = t.ext >= 0 ? t.ext : ext_stages(w);
+                int all = t.ext;
+                if (all < 0) {
+                    int n = 0;
+                    for (int g = find(t.eoffs, p.plan.groups, w.first);
+                         g < p.plan.groups && t.eoffs[g] < w.first + w.count; ++g)
+                        n += max(t.eoffs[g], w.first) < min(t.eoffs[g + 1], w.first + w.count);
+                    all = ext_steps(p, n);
+                }
                 w.e0 = (int)mul_div(all, w.k0, w.ki);
                 w.e1 = (int)mul_div(all, w.k1, w.ki);
             }
             return true;
         }
-        return false;
     }
-    // Stages of the extension of a tile (see Ext).
-    __device__ int ext_stages(const Work &w) const {
-        int n = 0;
-        for (int g = find(t.eoffs, p.plan.groups, w.first); g < p.plan.groups && t.eoffs[g] < w.first + w.count; ++g)
-            n += max(t.eoffs[g], w.first) < min(t.eoffs[g + 1], w.first + w.count);
-        return ext_steps(p, n);
+};
+
+// Warp 10's thread: deals the pair's pieces to the warps of its CTA, a few
+// ahead of them.  (Every warp for itself, they took 3 to 5 us before the first
+// load, in code fetched five times, and a bubble a tile.)
+__device__ void deal(const GroupProduct &p, Tables &t) {
+    Walk walk(p, t);
+    Work w;
+    for (int i = 0;; ++i) {
+        const bool more = walk.next(w);
+        const int s = i % PIECES;
+        if (!mbar_wait(&t.taken[s], ((i / PIECES) & 1) ^ 1, &t.abort_f, p.status)) return;
+        if (!more) w.g = -1;
+        t.work[s] = w;
+        mbar_arrive(&t.dealt[s]);
+        if (!more) return;
+    }
+}
+
+// The pieces as a warp takes them: all its lanes, or (ALONE) its first lane.
+template <bool ALONE>
+struct Pieces {
+    const GroupProduct &p;
+    Tables &t;
+    int i = 0;
+    __device__ Pieces(const GroupProduct &p_, Tables &t_) : p(p_), t(t_) {}
+    __device__ bool next(Work &w) {
+        const int s = i % PIECES;
+        bool ok = mbar_wait(&t.dealt[s], (i / PIECES) & 1, &t.abort_f, p.status);
+        if (!ALONE) ok = __all_sync(0xffffffffu, ok);
+        if (!ok) return false;
+        w = t.work[s];
+        if (!ALONE) __syncwarp();
+        if (ALONE || (threadIdx.x & 31) == 0) mbar_arrive(&t.taken[s]);
+        ++i;
+        return w.g >= 0;
     }
 };
 
@@ -281,7 +323,7 @@ struct Ext {
     int p0, p1, g, r0, a, b, left;
     __device__ Ext(const GroupProduct &p_, const Tables &t_, const Work &w)
         : p(p_), t(t_), p0(w.first), p1(w.first + w.count) {
-        g = Walk::find(t.eoffs, p.plan.groups, p0);   // eoffs[g] <= first, or g = 0
+        g = find(t.eoffs, p.plan.groups, p0);   // eoffs[g] <= first, or g = 0
         r0 = 0;
         left = w.e1 - w.e0;
         settle();
@@ -362,15 +404,17 @@ __device__ __forceinline__ int row_at(const GroupProduct &p, int place) {
 // 128 bytes.
 
 __device__ void pick_rows(const GroupProduct &p, Tables &t, uint8_t *sm, int rank) {
-    Walk walk(p, t);
     Work w;
     Ring at(p.stages);
     bool ok = true;
     const int tid = threadIdx.x & 127, sub = tid >> 3, c = tid & 7;
-    const uint32_t dst = (p.mode == GP_GROUPED ? p.b_off : 0) + sub * 128 + ((c ^ (sub & 7)) << 4);
-    while (ok && walk.next(w)) {
+    const bool grouped = p.mode == GP_GROUPED;
+    const uint32_t dst = (grouped ? p.b_off : 0) + sub * 128 + ((c ^ (sub & 7)) << 4);
+    const uint32_t block = grouped ? p.b_sub : p.a_sub;
+    Pieces<false> pieces(p, t);
+    while (ok && pieces.next(w)) {
         // this CTA's rows of the tile: its 128 of the A side, or its half of the B side
-        const int half = p.mode == GP_GROUPED ? up16(w.count) >> 1 : 128;
+        const int half = grouped ? up16(w.count) >> 1 : 128;
         const int mine = min(half, w.count - rank * half);
         const uint16_t *row[8];     // 16 rows apart: 2,048 bytes of smem
 #pragma unroll
@@ -383,11 +427,13 @@ __device__ void pick_rows(const GroupProduct &p, Tables &t, uint8_t *sm, int ran
             ok = __all_sync(0xffffffffu, ok);
             if (!ok) break;
             const uint32_t st = smem_u32(sm + (size_t)at.s * p.stage_bytes) + dst;
-            const int col = kb * GP_BK + c * 8, left = p.k - col;
-            const uint32_t bytes = left >= 8 ? 16 : left > 0 ? left * 2 : 0;   // beyond: zeros
+            for (int j = 0; j < p.kk; ++j) {
+                const int col = (kb * p.kk + j) * GP_BK + c * 8, left = p.k - col;
+                const uint32_t bytes = left >= 8 ? 16 : left > 0 ? left * 2 : 0;   // beyond: zeros
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (row[i]) cp_async16(st + i * 2048, row[i] + (bytes ? col : 0), bytes);
+                for (int i = 0; i < 8; ++i)
+                    if (row[i]) cp_async16(st + j * block + i * 2048, row[i] + (bytes ? col : 0), bytes);
+            }
             cp_async_arrive(&t.rowsf[at.s]);
         }
         // of the extension's stages only the arrival is due
@@ -428,6 +474,11 @@ k_group(const __grid_constant__ GroupMaps maps, const __grid_constant__ GroupPro
             mbar_init(&t.acce[b], p.sorted ? 16 : 8);
         }
         mbar_init(&t.done, 1);
+        for (int i = 0; i < PIECES; ++i) {
+            mbar_init(&t.dealt[i], 1);
+            // the epilogue, the picking warps, TMA, MMA or relay
+            mbar_init(&t.taken[i], p.sorted ? 2 + (rank == 0) : 3 + GATHER_WARPS);
+        }
         t.abort_f = 0;
         t.ng = shared ? 1 : p.plan.groups;
         // the tables of 8-byte values come first
@@ -474,8 +525,8 @@ k_group(const __grid_constant__ GroupMaps maps, const __grid_constant__ GroupPro
             int64_t v = 0;
             if (g < t.ng) {
                 const int n = max(0, t.offs[g + 1] - t.offs[g]);
-                // (an empty group's zero gradient is written too: see Walk::cost)
-                v = grad ? (int64_t)p.mtiles * p.ntiles * max(MIN_PIECE, (n + GP_BK - 1) / GP_BK)
+                // (an empty group's zero gradient is written too: see grad_cost)
+                v = grad ? (int64_t)p.mtiles * p.ntiles * max(WRITE_COST, (n + GP_BK - 1) / GP_BK)
                          : (int64_t)((n + GP_TILE - 1) / GP_TILE) * p.ntiles;
             }
 #pragma unroll
@@ -506,7 +557,10 @@ k_group(const __grid_constant__ GroupMaps maps, const __grid_constant__ GroupPro
     tc_fence_after();
     const uint32_t tmem = t.tmem;
 
-    if (!p.sorted && warp >= 4 && warp < 8) {
+    if (warp == 10) {
+        if (lane == 0) deal(p, t);
+        __syncwarp();
+    } else if (!p.sorted && warp >= 4 && warp < 8) {
         pick_rows(p, t, sm, rank);
     } else if (warp == 8) {
         // TMA: W (each CTA its 128 rows of the A side or its half of the B side),
@@ -515,7 +569,6 @@ k_group(const __grid_constant__ GroupMaps maps, const __grid_constant__ GroupPro
         if (lane == 0) {
             Ring at(p.stages);
             bool ok = true;
-            Walk walk(p, t);
             Work w;
             const int half = grouped ? 128 : p.bn >> 1;           // of the dense operand
             const int blocks = (half + 63) >> 6;                  // MN-major blocks of 64
@@ -528,7 +581,8 @@ k_group(const __grid_constant__ GroupMaps maps, const __grid_constant__ GroupPro
                 if (ok && rank == 0) mbar_arrive_expect_tx(&t.full[at.s], bytes);
                 return ok;
             };
-            while (ok && walk.next(w)) {
+            Pieces<true> pieces(p, t);
+            while (ok && pieces.next(w)) {
                 if (grad) {
                     const int l0 = w.xt * GP_TILE + rank * 128, r0 = w.ot * p.bn + rank * half;
                     for (int kb = w.k0; kb < w.k1; ++kb, at.step()) {
@@ -551,19 +605,25 @@ k_group(const __grid_constant__ GroupMaps maps, const __grid_constant__ GroupPro
                 const uint32_t xbytes = ((c0 + GP_ROW_BOX - 1) / GP_ROW_BOX + (c1 + GP_ROW_BOX - 1) / GP_ROW_BOX) *
                                         GP_ROW_BOX * 128;
                 for (int kb = w.k0; kb < w.k1; ++kb, at.step()) {
-                    if (!claim(2 * dbytes + (p.sorted ? xbytes : 0))) break;
+                    if (!claim(2 * p.kk * dbytes + (p.sorted ? xbytes : 0))) break;
                     uint8_t *st = sm + (size_t)at.s * p.stage_bytes;
+                    // (sorted rows: kk = 1)
                     if (p.sorted && boxes == 4)
                         tma_load_3d_pair(st + xside, &maps.xx, full0 + at.s * 8, kb * GP_BK, x0, 0);
                     else if (p.sorted)
                         for (int b = 0; b < boxes; ++b)
                             tma_load_3d_pair(st + xside + b * GP_ROW_BOX * 128, &maps.x, full0 + at.s * 8, kb * GP_BK,
                                              x0 + b * GP_ROW_BOX, 0);
-                    if (p.dense_mn)
-                        for (int b = 0; b < blocks; ++b)
-                            tma_load_3d_pair(st + dside + b * 8192, &maps.w, full0 + at.s * 8, o0 + b * 64, kb * GP_BK, w.g);
-                    else
-                        tma_load_3d_pair(st + dside, &maps.w, full0 + at.s * 8, kb * GP_BK, o0, w.g);
+                    auto dense = [&](uint8_t *dst, int k) {
+                        if (p.dense_mn)
+                            for (int b = 0; b < blocks; ++b)
+                                tma_load_3d_pair(dst + b * 8192, &maps.w, full0 + at.s * 8, o0 + b * 64, k, w.g);
+                        else
+                            tma_load_3d_pair(dst, &maps.w, full0 + at.s * 8, k, o0, w.g);
+                    };
+                    dense(st + dside, kb * p.kk * GP_BK);
+                    for (int j = 1; j < p.kk; ++j)
+                        dense(st + dside + j * (grouped ? p.a_sub : p.b_sub), (kb * p.kk + j) * GP_BK);
                 }
                 if (shared && ok)
                     for (Ext e(p, t, w); e.more(); at.step()) {
@@ -596,7 +656,6 @@ k_group(const __grid_constant__ GroupMaps maps, const __grid_constant__ GroupPro
             uint32_t lt = 0;
             Ring at(p.stages);
             bool ok = true;
-            Walk walk(p, t);
             Work w;
             const bool a_mn = grad || (grouped && p.dense_mn);
             const bool b_mn = grad || (!grad && !grouped && p.dense_mn);
@@ -611,7 +670,8 @@ k_group(const __grid_constant__ GroupMaps maps, const __grid_constant__ GroupPro
             };
             // per 16-deep MMA: 16 rows of 128 bytes further (MN-major), or 32 bytes (K-major)
             const uint32_t astep = a_mn ? 2048 >> 4 : 2, bstep = b_mn ? 2048 >> 4 : 2;
-            for (; ok && walk.next(w); ++lt) {
+            Pieces<true> pieces(p, t);
+            for (; ok && pieces.next(w); ++lt) {
                 const int b = lt & 1;
                 const uint32_t d = tmem + b * CS;
                 const int N = grouped ? up16(w.count) : p.bn;
@@ -623,13 +683,17 @@ k_group(const __grid_constant__ GroupMaps maps, const __grid_constant__ GroupPro
                     ok = stage_ready();
                     if (!ok) break;
                     const uint32_t st = smem_u32(sm + (size_t)at.s * p.stage_bytes);
-                    const uint64_t ad = sdesc(st, 8192, 1024, 2), bd = sdesc(st + p.b_off, 8192, 1024, 2);
                     // a gradient's last stage: whole 16s of rows, the group's padding
                     // among them (zeros), nothing of the next group
                     const int steps = grad ? min(4, max(1, (w.count - kb * GP_BK + 15) >> 4)) : 4;
+                    auto block = [&](uint32_t a, uint32_t bb, bool add) {
+                        const uint64_t ad = sdesc(a, 8192, 1024, 2), bd = sdesc(bb, 8192, 1024, 2);
 #pragma unroll
-                    for (int k = 0; k < 4; ++k)
-                        if (k < steps) mma_pair(d, ad + astep * k, bd + bstep * k, idesc, (kb > w.k0) | k);
+                        for (int k = 0; k < 4; ++k)
+                            if (k < steps) mma_pair(d, ad + astep * k, bd + bstep * k, idesc, add || k);
+                    };
+                    block(st, st + p.b_off, kb > w.k0);
+                    for (int j = 1; j < p.kk; ++j) block(st + j * p.a_sub, st + p.b_off + j * p.b_sub, true);
                     mma_commit_pair(&t.empty[at.s]);
                 }
                 if (!ok) break;
@@ -674,9 +738,9 @@ k_group(const __grid_constant__ GroupMaps maps, const __grid_constant__ GroupPro
             const uint32_t full0 = smem_of(&t.full[0], 0);
             Ring at(p.stages);
             bool ok = true;
-            Walk walk(p, t);
             Work w;
-            while (ok && walk.next(w)) {
+            Pieces<true> pieces(p, t);
+            while (ok && pieces.next(w)) {
                 auto pass = [&]() {
                     ok = mbar_wait(&t.rowsf[at.s], at.ph, abort_f, p.status);
                     if (!ok) return false;
@@ -716,9 +780,21 @@ k_group(const __grid_constant__ GroupMaps maps, const __grid_constant__ GroupPro
             }
         }
         uint32_t lt = 0;
-        Walk walk(p, t);
         Work w;
-        for (; walk.next(w); ++lt) {
+        Pieces<false> pieces(p, t);
+        for (;; ++lt) {
+            // one warp waits for all, here and for the accumulator: they go on, or
+            // give up, together
+            if (warp == 0) {
+                const bool more = pieces.next(w);
+                if (lane == 0) {
+                    t.go = more;
+                    t.mine = w;
+                }
+            }
+            named_bar_sync(1, threads);
+            if (!*(volatile int *)&t.go) break;
+            w = t.mine;
             const int b = lt & 1;
             int nrows;                 // rows of the A side that count
             int cols;                  // columns that count
@@ -734,14 +810,13 @@ k_group(const __grid_constant__ GroupMaps maps, const __grid_constant__ GroupPro
                 cols = min(p.bn, p.n - w.ot * p.bn);
                 if (half == 0 && row < nrows) t.rows[row] = row_at(p, w.first + rank * 128 + row);
             }
-            // one warp waits for all: they go on, or give up, together
             if (warp == 0) {
                 bool ok = mbar_wait(&t.accf[b], (lt >> 1) & 1, abort_f, p.status);
                 ok = __all_sync(0xffffffffu, ok);
-                if (lane == 0) t.go = ok;
+                if (lane == 0) t.ready = ok;
             }
             named_bar_sync(1, threads);
-            if (!*(volatile int *)&t.go) break;
+            if (!*(volatile int *)&t.ready) break;
             tc_fence_after();
             const bool cut = w.c0 != w.c1;
             bool write = true;
@@ -936,7 +1011,7 @@ k_group(const __grid_constant__ GroupMaps maps, const __grid_constant__ GroupPro
                 }
             }
             if (held) release();                // (no chunk was this warp's)
-            named_bar_sync(1, threads);         // t.rows and t.go may be written again
+            named_bar_sync(1, threads);         // what the warps share may be written again
         }
     }
     tc_fence_before();
@@ -1000,14 +1075,21 @@ void group_plan(GroupProduct *p) {
     if (p->mode == GP_WGRAD || (p->mode == GP_ROWS && p->dense_mn)) b = (p->bn / 2 + 63) / 64 * 8192;
     if (p->mode == GP_ROWS && !p->sorted && p->plan.rows < 128) a = (p->plan.rows + GP_ROW_BOX - 1) / GP_ROW_BOX * GP_ROW_BOX * 128;
     b = (b + 1023) / 1024 * 1024;
-    p->b_off = a;
-    p->stage_bytes = a + b;
+    const int room = SMEM_MAX - 1024 - table_bytes(*p), deep = (p->k + GP_BK - 1) / GP_BK;
+    // picked rows: stages of up to 256 columns, as the words and fences of a
+    // stage (about 0.5 us) outlast its few bytes
+    p->kk = 1;
+    while (!p->sorted && p->kk < 4 && 2 * p->kk <= deep && room / ((a + b) * 2 * p->kk) >= 4) p->kk *= 2;
+    p->a_sub = a;
+    p->b_sub = b;
+    p->b_off = a * p->kk;
+    p->stage_bytes = (a + b) * p->kk;
     p->ext_pack = 1;
     if (p->rank && p->rank <= GP_RC) {
-        const int fits = b / ext_bytes(*p);
+        const int fits = b * p->kk / ext_bytes(*p);
         p->ext_pack = fits < 1 ? 1 : fits;
     }
-    const int fit = (SMEM_MAX - 1024 - table_bytes(*p)) / p->stage_bytes;
+    const int fit = room / p->stage_bytes;
     p->stages = fit < MAX_STAGES ? fit : MAX_STAGES;
     p->smem = 1024 + p->stages * p->stage_bytes + table_bytes(*p);
     p->ntiles = (p->n + (p->mode == GP_GROUPED ? GP_TILE : p->bn) - 1) / (p->mode == GP_GROUPED ? GP_TILE : p->bn);

@@ -65,6 +65,8 @@ struct GroupProduct {
     int ntiles = 0, mtiles = 0;       // column tiles; row tiles of a gradient
     int f16 = 0;
     int stages = 0, stage_bytes = 0, smem = 0;
+    int kk = 1;                       // blocks of 64 columns of the contraction in a stage
+    int a_sub = 0, b_sub = 0;         // bytes of a block's A and B side
     int b_off = 0;                    // of the B side in a stage
     int rank = 0;                     // of the low-rank extension of a shared product
     int ext_pack = 1;                 // groups in one of its stages
