@@ -47,7 +47,8 @@ constexpr int GATHER_WARPS = 4;
 constexpr int A_BYTES = 128 * GP_BK * 2;
 constexpr int MAX_STAGES = 24;
 constexpr int SMEM_MAX = 227 * 1024;
-constexpr int MIN_PIECE = 6 * GP_BK;   // columns of the smallest piece of a cut tile (joining costs about as much)
+constexpr int MIN_PIECE = 6 * GP_BK;   // columns of the smallest piece of a cut tile
+constexpr int JOIN_COST = 8 * GP_BK;   // columns that joining the pieces of tiles costs (about 4 us)
 constexpr int WRITE_COST = 4;      // iterations that writing a gradient's tile counts for
 
 constexpr int OUT_PITCH = 64;      // bytes of a staged output row (32 columns)
@@ -187,6 +188,13 @@ struct Walk {
             rest = t.iter0[t.ng] - base;
         } else {
             rest = (int64_t)(tiles - dp) * kiters;
+        }
+        // Cut only where evening out the last rounds saves more than joining costs:
+        // whole rounds of the average tile against the line's even share.
+        const int last = tiles - dp, rounds = (last + pairs - 1) / pairs;
+        if ((rounds * pairs - last) * rest <= (int64_t)last * pairs * (JOIN_COST / deep)) {
+            dp = tiles;
+            rest = 0;
         }
         const int64_t most = max(div_small(rest, max(1, MIN_PIECE / deep)), (int64_t)(tiles - dp));
         cutters = most < 1 ? 1 : most < pairs ? (int)most : pairs;

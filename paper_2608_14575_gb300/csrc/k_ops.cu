@@ -23,7 +23,7 @@ namespace {
 constexpr int DP_THREADS = 512, DP_WARPS = DP_THREADS / 32;
 constexpr int DP_PER = 8;
 constexpr int DP_ROWS = DP_THREADS * DP_PER;
-constexpr int DP_CLUSTER = 8;
+constexpr int DP_CLUSTER = 16;   // (more than 8 is the non-portable size)
 constexpr int DP_FEW = 512;      // rows whose places are counted row against row
 
 __device__ __forceinline__ void pdl_begin() {
@@ -551,18 +551,20 @@ template <int DT>
 __device__ __forceinline__ void scale_chunk(const ClipChunk &c, float k) {
     constexpr int N = Vec<DT>::N;
     if (c.n == Vec<DT>::FULL && (((uintptr_t)c.in | (uintptr_t)c.out) & 15) == 0) {
+        // (read for the last time, written for others: neither is to push out of L2
+        // what the first pass left there)
         const uint4 *v = (const uint4 *)c.in + threadIdx.x;
         uint4 *o = (uint4 *)c.out + threadIdx.x;
         uint4 u[CL_PER];
 #pragma unroll
-        for (int i = 0; i < CL_PER; ++i) u[i] = v[i * CL_THREADS];
+        for (int i = 0; i < CL_PER; ++i) u[i] = __ldcs(v + i * CL_THREADS);
 #pragma unroll
         for (int i = 0; i < CL_PER; ++i) {
             float f[N];
             Vec<DT>::unpack(u[i], f);
 #pragma unroll
             for (int j = 0; j < N; ++j) f[j] *= k;
-            o[i * CL_THREADS] = Vec<DT>::pack(f);
+            __stcs(o + i * CL_THREADS, Vec<DT>::pack(f));
         }
         return;
     }
@@ -666,7 +668,9 @@ k_clip(const ClipChunk *table, int chunks, const float *factor) {
 
 cudaError_t ops_prepare() {
     const auto attr = cudaFuncAttributeMaxDynamicSharedMemorySize;
-    return cudaFuncSetAttribute(k_dispatch_place, attr, (int)place_smem(OPS_MAX_GROUPS));
+    cudaError_t e = cudaFuncSetAttribute(k_dispatch_place, attr, (int)place_smem(OPS_MAX_GROUPS));
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(k_dispatch_place, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    return e;
 }
 
 // Blocks and rows per block of a dispatch: whole rounds, two blocks an SM at most.
