@@ -40,8 +40,8 @@ namespace {
 using namespace umma;
 
 // warps 0-3 epilogue, 4-7 epilogue too (sorted rows) or picking rows, 8 TMA, 9
-// MMA (even CTA) or relay (odd CTA), 10 dealing the pieces
-constexpr int THREADS = 352;
+// MMA (even CTA), 10 dealing the pieces, 11 announcing picked rows
+constexpr int THREADS = 384;
 constexpr int PIECES = 4;          // pieces dealt ahead
 constexpr int GATHER_WARPS = 4;
 constexpr int A_BYTES = 128 * GP_BK * 2;
@@ -72,8 +72,8 @@ struct Work {
 
 // Shared memory behind the stages: this, then the group tables.
 struct Tables {
-    // per stage: full (even CTA: both CTAs' bytes, and the odd CTA's word), rows
-    // (this CTA's picked rows have landed), empty
+    // per stage: full (even CTA: both CTAs' bytes, and their word on picked rows),
+    // rows (this CTA's picked rows have landed), empty
     uint64_t full[MAX_STAGES], rowsf[MAX_STAGES], empty[MAX_STAGES], accf[2], acce[2], done;
     alignas(16) uint8_t out[8][OUT_BYTES];   // epilogue staging, a warp each
     int32_t rows[GP_TILE];               // the tile's rows of the output (epilogue)
@@ -88,11 +88,12 @@ struct Tables {
     int go, ready, last;
     // group tables: ng groups of the tiles, and the extension's
     int ng;
-    int ext;             // stages of the extension, where all places are in one tile (else -1)
+    int nseg;            // groups of the extension that have rows
     int64_t *iter0;      // [ng + 1] first iteration of each group (gradients)
     int32_t *offs;       // [ng + 1] first place of each group, clamped
     int32_t *tile0;      // [ng + 1] first tile of each group (rows products)
     int32_t *eoffs;      // [groups + 1] first place of each of the extension's groups
+    int32_t *seg;        // [nseg] its groups that have rows
 };
 
 static_assert(OUT_PITCH % 16 == 0 && OUT_BYTES % 16 == 0 && offsetof(Tables, out) % 16 == 0 && sizeof(Tables) % 16 == 0,
@@ -106,7 +107,7 @@ __host__ __device__ inline int ext_bytes(const GroupProduct &p) {
 
 __host__ __device__ inline int table_bytes(const GroupProduct &p) {
     const int g = p.plan.groups + 1;
-    return (int)sizeof(Tables) + (p.mode == GP_WGRAD ? g * 12 : p.shared ? g * 4 + 16 : g * 8);
+    return (int)sizeof(Tables) + (p.mode == GP_WGRAD ? g * 12 : p.shared ? g * 8 + 16 : g * 8);
 }
 
 // Waits of the unwinding (copies in flight, MMAs issued): bounded, no flags.
@@ -141,6 +142,24 @@ __device__ __forceinline__ int64_t mul_div(int64_t a, int b, int c) {
 __device__ __forceinline__ int64_t div_small(int64_t a, int64_t b) {
     if ((a | b) >> 32) return a / b;
     return (uint32_t)a / (uint32_t)b;
+}
+
+// The groups with rows in a tile, as places in the list of those with any.
+__device__ __forceinline__ void ext_groups(const Tables &t, const Work &w, int &s0, int &s1) {
+    int lo = 0, hi = t.nseg;
+    while (lo < hi) {                    // the first that ends behind the tile's first place
+        const int m = (lo + hi) >> 1;
+        if (t.eoffs[t.seg[m] + 1] > w.first) hi = m;
+        else lo = m + 1;
+    }
+    s0 = lo;
+    hi = t.nseg;
+    while (lo < hi) {                    // the first that begins behind its last
+        const int m = (lo + hi) >> 1;
+        if (t.eoffs[t.seg[m]] >= w.first + w.count) hi = m;
+        else lo = m + 1;
+    }
+    s1 = lo;
 }
 
 // Stages of the extension for n groups.
@@ -268,14 +287,9 @@ struct Walk {
             w.c1 = (int)div_small((start + w.ki) * cutters - 1, rest);
             if (p.rank && w.c0 != w.c1) {
                 // a piece takes its share of the extension
-                int all = t.ext;
-                if (all < 0) {
-                    int n = 0;
-                    for (int g = find(t.eoffs, p.plan.groups, w.first);
-                         g < p.plan.groups && t.eoffs[g] < w.first + w.count; ++g)
-                        n += max(t.eoffs[g], w.first) < min(t.eoffs[g + 1], w.first + w.count);
-                    all = ext_steps(p, n);
-                }
+                int s0, s1;
+                ext_groups(t, w, s0, s1);
+                const int all = ext_steps(p, s1 - s0);
                 w.e0 = (int)mul_div(all, w.k0, w.ki);
                 w.e1 = (int)mul_div(all, w.k1, w.ki);
             }
@@ -328,44 +342,20 @@ struct Pieces {
 struct Ext {
     const GroupProduct &p;
     const Tables &t;
-    int p0, p1, g, r0, a, b, left;
-    __device__ Ext(const GroupProduct &p_, const Tables &t_, const Work &w)
-        : p(p_), t(t_), p0(w.first), p1(w.first + w.count) {
-        g = find(t.eoffs, p.plan.groups, p0);   // eoffs[g] <= first, or g = 0
-        r0 = 0;
-        left = w.e1 - w.e0;
-        settle();
-        for (int i = 0; i < w.e0 && g < p.plan.groups; ++i)
-            for (int q = 0; q < p.ext_pack; ++q) advance();
+    int steps, i, end;            // steps of a group; this step (of all groups'), the piece's last
+    __device__ Ext(const GroupProduct &p_, const Tables &t_, const Work &w) : p(p_), t(t_) {
+        int s0, s1;
+        ext_groups(t, w, s0, s1);
+        steps = p.ext_pack > 1 ? 1 : (p.rank + GP_RC - 1) / GP_RC;
+        const int from = s0 * steps, n = (s1 - s0) * steps;
+        i = from + min(n, w.e0 * p.ext_pack);
+        end = from + (w.e1 < INT32_MAX / p.ext_pack ? min(n, w.e1 * p.ext_pack) : n);
     }
-    __device__ void settle() {
-        for (; g < p.plan.groups; ++g) {
-            if (t.eoffs[g] >= p1) break;
-            a = max(t.eoffs[g], p0);
-            b = min(t.eoffs[g + 1], p1);
-            if (a < b) return;
-        }
-        g = p.plan.groups;
-    }
-    __device__ bool here() const { return g < p.plan.groups; }
-    __device__ void advance() {          // the next group's matrix (or ranks)
-        if (!here()) return;
-        r0 += GP_RC;
-        if (r0 >= p.rank) {
-            r0 = 0;
-            ++g;
-            settle();
-        }
-    }
-    // stages: while (e.more()) { up to p.ext_pack times, while here(): ...; advance() }
-    __device__ bool more() {
-        if (left <= 0 || !here()) return false;
-        --left;
-        return true;
-    }
-    __device__ void skip() {             // a whole stage
-        for (int q = 0; q < p.ext_pack; ++q) advance();
-    }
+    __device__ bool more() const { return i < end; }
+    __device__ int here() const { return min(p.ext_pack, end - i); }       // groups of this stage
+    __device__ int group(int q) const { return t.seg[(i + q) / steps]; }
+    __device__ int rank0() const { return i % steps * GP_RC; }
+    __device__ void step() { i += p.ext_pack; }
 };
 
 template <bool F16>
@@ -446,7 +436,7 @@ __device__ void pick_rows(const GroupProduct &p, Tables &t, uint8_t *sm, int ran
         }
         // of the extension's stages only the arrival is due
         if (p.rank && ok)
-            for (Ext e(p, t, w); e.more(); e.skip(), at.step()) {
+            for (Ext e(p, t, w); e.more(); e.step(), at.step()) {
                 ok = mbar_wait(&t.empty[at.s], at.ph ^ 1, &t.abort_f, p.status);
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
@@ -473,7 +463,7 @@ k_group(const __grid_constant__ GroupMaps maps, const __grid_constant__ GroupPro
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < p.stages; ++s) {
-            mbar_init(&t.full[s], p.sorted ? 1 : 2);
+            mbar_init(&t.full[s], p.sorted ? 1 : 3);
             mbar_init(&t.rowsf[s], 32 * GATHER_WARPS);
             mbar_init(&t.empty[s], 1);
         }
@@ -484,8 +474,8 @@ k_group(const __grid_constant__ GroupMaps maps, const __grid_constant__ GroupPro
         mbar_init(&t.done, 1);
         for (int i = 0; i < PIECES; ++i) {
             mbar_init(&t.dealt[i], 1);
-            // the epilogue, the picking warps, TMA, MMA or relay
-            mbar_init(&t.taken[i], p.sorted ? 2 + (rank == 0) : 3 + GATHER_WARPS);
+            // the epilogue and TMA, the picking warps and their word, MMA
+            mbar_init(&t.taken[i], (p.sorted ? 2 : 3 + GATHER_WARPS) + (rank == 0));
         }
         t.abort_f = 0;
         t.ng = shared ? 1 : p.plan.groups;
@@ -494,6 +484,7 @@ k_group(const __grid_constant__ GroupMaps maps, const __grid_constant__ GroupPro
         t.offs = (int32_t *)(&t + 1) + (grad ? 2 * (t.ng + 1) : 0);
         t.tile0 = t.offs + t.ng + 1;
         t.eoffs = t.tile0 + t.ng + 1;
+        t.seg = t.eoffs + p.plan.groups + 1;
         fence_mbar_init();
     }
     if (warp == 9) {
@@ -555,9 +546,14 @@ k_group(const __grid_constant__ GroupMaps maps, const __grid_constant__ GroupPro
     }
     if (shared && warp == 1) {
         int n = 0;
-        for (int g = lane; g < p.plan.groups; g += 32) n += t.eoffs[g] < t.eoffs[g + 1];
-        n = __reduce_add_sync(0xffffffffu, n);
-        if (lane == 0) t.ext = t.offs[1] <= GP_TILE ? ext_steps(p, n) : -1;
+        for (int g0 = 0; g0 < p.plan.groups; g0 += 32) {
+            const int g = g0 + lane;
+            const bool any = g < p.plan.groups && t.eoffs[g] < t.eoffs[g + 1];
+            const uint32_t v = __ballot_sync(0xffffffffu, any);
+            if (any) t.seg[n + __popc(v & ((1u << lane) - 1))] = g;
+            n += __popc(v);
+        }
+        if (lane == 0) t.nseg = n;
     }
     tc_fence_before();
     __syncthreads();
@@ -567,6 +563,34 @@ k_group(const __grid_constant__ GroupMaps maps, const __grid_constant__ GroupPro
 
     if (warp == 10) {
         if (lane == 0) deal(p, t);
+        __syncwarp();
+    } else if (warp == 11) {
+        // Tells the even CTA that a stage's picked rows are here.  They are copied
+        // by threads: the fence makes them visible to the tensor cores' proxy.  (A
+        // picking thread cannot: its fence would wait for all of its copies in
+        // flight, 1.75 us a stage.  The MMA thread spent 0.2 us a stage on it.)
+        if (lane == 0 && !p.sorted) {
+            const uint32_t full0 = smem_of(&t.full[0], 0);
+            Ring at(p.stages);
+            bool ok = true;
+            Work w;
+            auto pass = [&]() {
+                ok = mbar_wait(&t.rowsf[at.s], at.ph, abort_f, p.status);
+                if (!ok) return false;
+                fence_proxy_async_smem();
+                mbar_arrive_cluster(full0 + at.s * 8);
+                at.step();
+                return true;
+            };
+            Pieces<true> pieces(p, t);
+            while (ok && pieces.next(w)) {
+                for (int kb = w.k0; kb < w.k1; ++kb)
+                    if (!pass()) break;
+                if (shared && ok)
+                    for (Ext e(p, t, w); e.more(); e.step())
+                        if (!pass()) break;
+            }
+        }
         __syncwarp();
     } else if (!p.sorted && warp >= 4 && warp < 8) {
         pick_rows(p, t, sm, rank);
@@ -634,22 +658,21 @@ k_group(const __grid_constant__ GroupMaps maps, const __grid_constant__ GroupPro
                         dense(st + dside + j * (grouped ? p.a_sub : p.b_sub), (kb * p.kk + j) * GP_BK);
                 }
                 if (shared && ok)
-                    for (Ext e(p, t, w); e.more(); at.step()) {
-                        Ext f = e;
-                        int n = 0;
-                        for (; n < p.ext_pack && f.here(); ++n) f.advance();
+                    for (Ext e(p, t, w); e.more(); e.step(), at.step()) {
+                        const int n = e.here(), r0 = e.rank0();
                         if (!claim(2 * n * ebytes + xbytes)) break;
                         uint8_t *st = sm + (size_t)at.s * p.stage_bytes;
                         for (int b = 0; b < boxes; ++b)
-                            tma_load_3d_pair(st + b * GP_ROW_BOX * 128, &maps.u, full0 + at.s * 8, e.r0 * 2,
+                            tma_load_3d_pair(st + b * GP_ROW_BOX * 128, &maps.u, full0 + at.s * 8, r0 * 2,
                                              x0 + b * GP_ROW_BOX, 0);
-                        for (int q = 0; q < n; ++q, e.advance()) {
+                        for (int q = 0; q < n; ++q) {
                             uint8_t *eb = st + p.b_off + q * ebytes;
+                            const int g = e.group(q);
                             if (p.dense_mn)
                                 for (int b = 0; b < blocks; ++b)
-                                    tma_load_3d_pair(eb + b * 4096, &maps.eb, full0 + at.s * 8, o0 + b * 64, e.r0, e.g);
+                                    tma_load_3d_pair(eb + b * 4096, &maps.eb, full0 + at.s * 8, o0 + b * 64, r0, g);
                             else
-                                tma_load_3d_pair(eb, &maps.eb, full0 + at.s * 8, e.r0, o0, e.g);
+                                tma_load_3d_pair(eb, &maps.eb, full0 + at.s * 8, r0, o0, g);
                         }
                     }
             }
@@ -667,12 +690,9 @@ k_group(const __grid_constant__ GroupMaps maps, const __grid_constant__ GroupPro
             Work w;
             const bool a_mn = grad || (grouped && p.dense_mn);
             const bool b_mn = grad || (!grad && !grouped && p.dense_mn);
-            // both CTAs' operands have landed; picked rows, copied by threads, are
-            // made visible to the tensor cores' proxy here (and by the odd CTA's relay)
+            // both CTAs' operands have landed
             auto stage_ready = [&]() {
-                if (!p.sorted && !mbar_wait(&t.rowsf[at.s], at.ph, abort_f, p.status)) return false;
                 if (!mbar_wait(&t.full[at.s], at.ph, abort_f, p.status)) return false;
-                if (!p.sorted) fence_proxy_async_smem();
                 tc_fence_after();
                 return true;
             };
@@ -707,26 +727,27 @@ k_group(const __grid_constant__ GroupMaps maps, const __grid_constant__ GroupPro
                 if (!ok) break;
                 if (shared) {
                     const uint32_t eidesc = idesc_16bit(GP_TILE, p.bn, F16, false, p.dense_mn);
-                    for (Ext e(p, t, w); e.more(); at.step()) {
+                    for (Ext e(p, t, w); e.more(); e.step(), at.step()) {
                         ok = stage_ready();
                         if (!ok) break;
                         const uint32_t st = smem_u32(sm + (size_t)at.s * p.stage_bytes);
                         const uint64_t ad = sdesc(st, 0, 1024, 2);
-                        for (int q = 0; q < p.ext_pack && e.here(); ++q, e.advance()) {
+                        const int steps = min(GP_RC, p.rank - e.rank0()) > 16 ? 2 : 1;
+                        for (int q = 0, n = e.here(); q < n; ++q) {
+                            const int g = e.group(q), a = t.eoffs[g] - w.first, z = t.eoffs[g + 1] - w.first;
                             uint32_t off[8];
 #pragma unroll
                             for (int i = 0; i < 8; ++i) {
-                                const int a = min(max(e.a - w.first - 32 * i, 0), 32);
-                                const int z = min(max(e.b - w.first - 32 * i, 0), 32);
-                                // rows [a, z) of this word take part
-                                const uint32_t below = a == 32 ? 0xffffffffu : (1u << a) - 1;
-                                const uint32_t upto = z == 32 ? 0xffffffffu : (1u << z) - 1;
-                                off[i] = ~(upto & ~below);
+                                // rows [a, z) take part
+                                off[i] = 0xffffffffu;
+                                if (i * 32 < w.count) {
+                                    const int from = max(a - 32 * i, 0), n = min(z - 32 * i, 32) - from;
+                                    if (n > 0) off[i] = ~((0xffffffffu >> (32 - n)) << from);
+                                }
                             }
                             const uint32_t eb = st + p.b_off + q * ext_bytes(p);
                             const uint64_t bd = p.dense_mn ? sdesc(eb, 4096, 1024, 2)
                                                 : p.rank <= 16 ? sdesc(eb, 0, 256, 6) : sdesc(eb, 0, 512, 4);
-                            const int steps = min(GP_RC, p.rank - e.r0) > 16 ? 2 : 1;
                             for (int k = 0; k < steps; ++k) {
                                 const uint64_t bk = bd + (p.dense_mn ? (2048 >> 4) * k : 2 * k);
                                 mma_pair_rows(d, ad + 2 * k, bk, eidesc, off);
@@ -741,28 +762,6 @@ k_group(const __grid_constant__ GroupMaps maps, const __grid_constant__ GroupPro
             }
             mma_commit_pair(&t.done);
             drain(&t.done, 0);
-        } else if (lane == 0 && !p.sorted) {
-            // odd CTA: passes on to the even one that a stage's rows are here
-            const uint32_t full0 = smem_of(&t.full[0], 0);
-            Ring at(p.stages);
-            bool ok = true;
-            Work w;
-            Pieces<true> pieces(p, t);
-            while (ok && pieces.next(w)) {
-                auto pass = [&]() {
-                    ok = mbar_wait(&t.rowsf[at.s], at.ph, abort_f, p.status);
-                    if (!ok) return false;
-                    fence_proxy_async_smem();
-                    mbar_arrive_cluster(full0 + at.s * 8);
-                    at.step();
-                    return true;
-                };
-                for (int kb = w.k0; kb < w.k1; ++kb)
-                    if (!pass()) break;
-                if (shared && ok)
-                    for (Ext e(p, t, w); e.more(); e.skip())
-                        if (!pass()) break;
-            }
         }
         __syncwarp();
     } else {
