@@ -34,6 +34,7 @@ SOURCES = {
     "ops_api.cu": [],
     "k_group.cu": [],
     "k_ops.cu": [],
+    "k_few.cu": [],
 }
 
 

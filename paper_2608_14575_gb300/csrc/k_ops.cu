@@ -403,6 +403,10 @@ k_low_few(const __grid_constant__ LowFew p) {
         float v = 0.f;
         for (int w = 0; w < LF_WARPS; ++w) v += part[w][threadIdx.x];
         v = r < p.rank && g < p.plan.groups ? v * p.scale[g] : 0.f;
+        if (p.wide) {
+            if (r < p.rank) p.wide[(int64_t)place * p.rank + r] = v;
+            return;
+        }
         // high and low terms (an infinite high one takes a zero low one)
         uint16_t *u = p.u + (int64_t)place * p.u_ld + r / GP_RC * (2 * GP_RC) + r % GP_RC;
         if (F16) {
@@ -738,7 +742,8 @@ cudaError_t launch_sort_rows(const GroupPlan &plan, const SortRows &m, int place
 cudaError_t launch_low_few(const LowFew &p, bool f16, cudaStream_t s) {
     cudaLaunchAttribute at[1];
     cudaLaunchConfig_t cfg = relaxed(p.plan.rows, LF_THREADS, 0, s, at);
-    cfg.gridDim.y = (unsigned)((p.rank + 2 * GP_RC - 1) / (2 * GP_RC) * (2 * GP_RC / LF_RANKS));
+    cfg.gridDim.y = p.wide ? (unsigned)((p.rank + LF_RANKS - 1) / LF_RANKS)
+                           : (unsigned)((p.rank + 2 * GP_RC - 1) / (2 * GP_RC) * (2 * GP_RC / LF_RANKS));
     return f16 ? cudaLaunchKernelEx(&cfg, k_low_few<true>, p) : cudaLaunchKernelEx(&cfg, k_low_few<false>, p);
 }
 

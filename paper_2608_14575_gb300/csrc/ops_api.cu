@@ -555,10 +555,10 @@ static hwr_status check_adapters(hwr_ops *c, const hwr_rows *r, const hwr_adapte
 // scale[g] M[g] x[t] (or M[g]^T x[t]) by place, as two 16-bit terms: [places]
 // [32-rank chunks][high, low], an even number of chunks.
 static hwr_status low_rank(hwr_ops *c, const hwr_rows *r, const hwr_adapters *ad, const Rows &rows, const Operand &x,
-                           const Operand &m, bool m_mn, const Operand &u) {
+                           const Operand &m, bool m_mn, const Operand &u, bool wide = false) {
     // a row reads its adapter's matrix once: few enough bytes need no tensor
     // cores (64 rows, rank 16, 4,096 columns: 27 us on them, 5 us without)
-    if (!rows.sorted && !m_mn && (int64_t)r->rows * ad->rank * x.cols <= LOW_FEW_VALUES) {
+    if (wide || (!rows.sorted && !m_mn && (int64_t)r->rows * ad->rank * x.cols <= LOW_FEW_VALUES)) {
         LowFew f;
         f.plan = rows.plan;
         f.k = x.cols;
@@ -571,6 +571,7 @@ static hwr_status low_rank(hwr_ops *c, const hwr_rows *r, const hwr_adapters *ad
         f.scale = ad->scale;
         f.u = (uint16_t *)const_cast<void *>(u.p);
         f.u_ld = u.ld;
+        f.wide = wide ? (float *)const_cast<void *>(u.p) : nullptr;
         CK(c, launch_low_few(f, r->dtype == HWR_F16, c->stream), "low-rank kernel");
         return HWR_OK;
     }
@@ -624,13 +625,35 @@ extern "C" hwr_status hwr_adapter_forward(hwr_ops *c, const hwr_rows *r, const h
     Rows rows = plan_rows(cv, r, nullptr, 0, true, false);
     Operand w = cv.operand(r->w, r->w_ld, N, K);
     Operand a = cv.operand(ad->a, K, R, K, (int64_t)R * K, G);
-    Operand b = cv.operand(ad->b, R, N, R, (int64_t)N * R, G);
+    const bool few = !rows.sorted && r->rows <= FEW_ROWS;
+    Operand b;
+    if (!few) b = cv.operand(ad->b, R, N, R, (int64_t)N * R, G);
     Operand u = packed(cv, rows, ad);
     OK(reserve(c, cv.at));
     u.p = c->ws + u.off;
     OK(sort_rows(c, &rows));
     OK(settle(c, &a));
     OK(settle(c, &w));
+    if (few) {
+        FewRows f;
+        f.plan = rows.plan;
+        f.k = K;
+        f.n = N;
+        f.x = (const uint16_t *)rows.x.p;
+        f.x_ld = rows.x.ld;
+        f.w = (const uint16_t *)w.p;
+        f.w_ld = w.ld;
+        f.out = (uint16_t *)y;
+        f.ld = y_ld;
+        f.rank = R;
+        f.u = (const float *)u.p;       // (a row of two 16-bit terms has room for it)
+        f.b = (const uint16_t *)ad->b;
+        f.b_ld = R;
+        f.b_z = (int64_t)N * R;
+        OK(low_rank(c, r, ad, rows, rows.x, a, false, u, true));
+        CK(c, launch_few_rows(f, r->dtype == HWR_F16, c->stream), "few-rows kernel");
+        return HWR_OK;
+    }
     OK(settle(c, &b));
     OK(low_rank(c, r, ad, rows, rows.x, a, false, u));
     return shared_product(c, r, ad, rows, rows.x, w, false, u, b, y, y_ld, N);

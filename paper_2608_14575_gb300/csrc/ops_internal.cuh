@@ -97,6 +97,25 @@ void group_plan(GroupProduct *p);
 size_t group_part_floats(int ctas);
 cudaError_t launch_group(const GroupProduct &p, const GroupMaps &maps, int ctas, cudaStream_t s);
 
+// ---- products of a few rows (k_few.cu) ---------------------------------------
+
+// out[t] = W x[t] + b[g(t)] u[t] for at most FEW_ROWS rows (W K-major; W and the
+// rows of x 16-byte aligned).
+constexpr int FEW_ROWS = 16;
+struct FewRows {
+    GroupPlan plan;
+    int k, n;
+    const uint16_t *x, *w;
+    int64_t x_ld, w_ld;
+    uint16_t *out;
+    int64_t ld;
+    int rank;
+    const float *u;                   // [places][rank]
+    const uint16_t *b;
+    int64_t b_ld, b_z;
+};
+cudaError_t launch_few_rows(const FewRows &p, bool f16, cudaStream_t s);
+
 // ---- dispatch, clipping, padding (k_ops.cu) ---------------------------------
 
 cudaError_t ops_prepare();
@@ -129,6 +148,7 @@ struct LowFew {
     const float *scale;
     uint16_t *u;
     int64_t u_ld;
+    float *wide;                      // or, where set, as fp32 [places][rank] here
 };
 cudaError_t launch_low_few(const LowFew &p, bool f16, cudaStream_t s);
 
