@@ -110,11 +110,17 @@ __host__ __device__ inline int table_bytes(const GroupProduct &p) {
     return (int)sizeof(Tables) + (p.mode == GP_WGRAD ? g * 12 : p.shared ? g * 8 + 16 : g * 8);
 }
 
-// Waits of the unwinding (copies in flight, MMAs issued): bounded, no flags.
+// Bounded wait for MMAs that were issued, without flags.
 __device__ __forceinline__ void drain(uint64_t *bar, uint32_t parity) {
     const long long t0 = clock64();
     while (!mbar_try_wait(bar, parity))
         if (clock64() - t0 > WAIT_CYCLES) return;
+}
+
+// Time for copies in flight to land, where a barrier cannot tell.
+__device__ __forceinline__ void linger() {
+    const long long t0 = clock64();
+    while (clock64() - t0 < 20000000) __nanosleep(1000);     // about 10 ms
 }
 
 __host__ __device__ inline int up16(int v) { return (v + 15) & ~15; }
@@ -614,7 +620,7 @@ k_group(const __grid_constant__ GroupMaps maps, const __grid_constant__ GroupPro
                 return ok;
             };
             Pieces<true> pieces(p, t);
-            while (ok && pieces.next(w)) {
+            while (!p.test_stall && ok && pieces.next(w)) {
                 if (grad) {
                     const int l0 = w.xt * GP_TILE + rank * 128, r0 = w.ot * p.bn + rank * half;
                     for (int kb = w.k0; kb < w.k1; ++kb, at.step()) {
@@ -676,10 +682,8 @@ k_group(const __grid_constant__ GroupMaps maps, const __grid_constant__ GroupPro
                         }
                     }
             }
-            // the loads still in flight land before the pair can exit
-            if (rank == 0)
-                for (uint32_t j = at.n > (uint32_t)p.stages ? at.n - p.stages : 0; j < at.n; ++j)
-                    drain(&t.full[j % p.stages], (j / p.stages) & 1);
+            // every stage loaded is waited for by the MMA thread, unless it gave up
+            if (!ok || *abort_f) linger();
         }
         __syncwarp();
     } else if (warp == 9) {
@@ -872,7 +876,7 @@ k_group(const __grid_constant__ GroupMaps maps, const __grid_constant__ GroupPro
             // Chunks of 32 columns of this thread's row.  A joined tile of a few
             // rows is dealt to all threads instead, a row's chunk at a time.
             const int chunks = pack ? (p.n + 63) / 64 * 2 : low ? (cols + 63) / 64 * 2 : (cols + 31) / 32;
-            const bool dealt = !grad && !grouped && cut && nrows <= 32;
+            const bool dealt = !grad && !grouped && cut && nrows <= 64;
             const int items = !write ? 0 : dealt ? nrows * chunks : chunks;
             // (low: both chunks of a pair in one warp)
             auto column = [&](int i) {

@@ -43,6 +43,7 @@ struct hwr_ops {
     double *sums = nullptr;      // partial sums of squares; then their arrivals and the factor
     int32_t *status_h = nullptr, *status_d = nullptr;   // mapped: bounded waits that ran out
     cudaEvent_t event = nullptr;                         // hwr_ops_after / before
+    int test_stall = 0;                                  // HWR_TEST_STALL (see hwr_api.cu)
     long fail_at = 0, allocs = 0;                        // HWR_TEST_FAIL_ALLOC
 };
 
@@ -118,6 +119,7 @@ extern "C" hwr_status hwr_ops_create(void *cuda_stream, hwr_ops **out) {
     hwr_ops *c = new (std::nothrow) hwr_ops;
     if (!c) return fail(nullptr, HWR_ERR_OOM, "host allocation failed");
     if (const char *e = getenv("HWR_TEST_FAIL_ALLOC")) c->fail_at = atol(e);
+    if (const char *e = getenv("HWR_TEST_STALL")) c->test_stall = atoi(e) != 0;
     auto body = [&]() -> hwr_status {
         int dev = 0;
         CK(c, cudaGetDevice(&dev), "cudaGetDevice");
@@ -393,6 +395,7 @@ static GroupProduct product(hwr_ops *c, const hwr_rows *r, const Rows &s) {
     p.part = c->part;
     p.count = c->count;
     p.status = c->status_d;
+    p.test_stall = c->test_stall;
     return p;
 }
 
@@ -462,6 +465,7 @@ static hwr_status check_rows(hwr_ops *c, const hwr_rows *r, bool need_x, bool ne
         return fail(c, HWR_ERR_INVALID_ARG, "rows %d, groups %d, n_in %d, n_out %d", r->rows, r->groups, r->n_in,
                     r->n_out);
     if (r->groups > OPS_MAX_GROUPS) return fail(c, HWR_ERR_UNSUPPORTED, "groups %d > %d", r->groups, OPS_MAX_GROUPS);
+    if (r->rows > INT32_MAX - 32 * OPS_MAX_GROUPS) return fail(c, HWR_ERR_UNSUPPORTED, "rows %d", r->rows);
     if (r->dtype != HWR_BF16 && r->dtype != HWR_F16)
         return fail(c, HWR_ERR_DTYPE, "dtype %d: products take bf16 or fp16", (int)r->dtype);
     if (r->rows && (!r->offsets || !r->order || (need_x && !r->x) || (need_w && !r->w)))

@@ -81,6 +81,7 @@ struct GroupProduct {
     float *part = nullptr;
     uint32_t *count = nullptr;
     int32_t *status = nullptr;
+    int test_stall = 0;               // test hook: nothing is loaded (bounded waits expire)
 };
 
 // x: the rows by place (or l and r of a gradient: the A and B side); w: the

@@ -521,6 +521,28 @@ def test_refusals(ops):
     assert torch.equal(ops.grouped_forward(x, w, plan), R.grouped_forward(x, w, c)[0].to(BF))
 
 
+@pytest.mark.parametrize("T", [40, 600])
+def test_timeout(monkeypatch, T):
+    """A producer that never loads (the test hook): the kernel's waits run out, the
+    call's failure is reported, the context is broken, and a new one works."""
+    monkeypatch.setenv("HWR_TEST_STALL", "1")
+    bad = H.Operators()
+    monkeypatch.delenv("HWR_TEST_STALL")
+    c = choices(T, 3, "any")
+    x, w = ints(T, 256), ints(3, 512, 256)
+    bad.grouped_forward(x, w, bad.dispatch(c, 3))
+    with pytest.raises(H.HwrError) as e:
+        bad.synchronize()
+    assert e.value.status == 5
+    with pytest.raises(H.HwrError) as e:
+        bad.dispatch(c, 3)
+    assert e.value.status == 6
+    bad.close()
+    good = H.Operators()
+    assert torch.equal(good.grouped_forward(x, w, good.dispatch(c, 3)), R.grouped_forward(x, w, c)[0].to(BF))
+    good.close()
+
+
 def test_allocation_failure(monkeypatch):
     monkeypatch.setenv("HWR_TEST_FAIL_ALLOC", "2")
     with pytest.raises(H.HwrError) as e:
