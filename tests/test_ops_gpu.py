@@ -548,3 +548,15 @@ def test_allocation_failure(monkeypatch):
     with pytest.raises(H.HwrError) as e:
         H.Operators()
     assert e.value.status == 3
+
+
+def test_example_learns():
+    """The example runs the operators together after a routing call."""
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "routed_layer.py")
+    spec = importlib.util.spec_from_file_location("routed_layer", path)
+    example = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(example)
+    for losses in example.main(Q=1024, width=256, steps=6, say=lambda *a: None):
+        assert all(b < a for a, b in zip(losses, losses[1:])), losses
