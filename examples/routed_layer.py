@@ -78,7 +78,7 @@ def main(Q=2048, width=512, rank=16, steps=8, say=print):
         second = fit("adapters", ops, adapters,
                      lambda a, b: ops.adapter_forward(x, shared, a, b, scale, plan),
                      lambda dy, a, b: list(ops.adapter_backward(dy, x, shared, a, b, scale, plan, need_dx=False))[1:],
-                     target, steps, 1.0, 40.0, say)
+                     target, steps, 0.2, 40.0, say)
         ops.synchronize()
         ops.close()
     return first, second

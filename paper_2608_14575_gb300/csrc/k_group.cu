@@ -60,7 +60,9 @@ __device__ __forceinline__ int staged_at(int row, int unit) {
 }
 
 // What a kernel is compiled for (the epilogue's registers are those of its kind).
-enum : int { K_GROUPED = 0, K_SHARED = 1, K_PACK = 2, K_GRAD = 3, K_LOW = 4 };
+// The last two are launched with two products (a product's parameters at an
+// address, not in the instructions, cost a single one 4 of 25 us).
+enum : int { K_GROUPED = 0, K_SHARED = 1, K_PACK = 2, K_GRAD = 3, K_LOW = 4, K_PACKS = 5, KINDS = 6 };
 
 struct Work {
     int g, xt, ot;        // group; tile of rows (gradients: of result rows); tile of columns
@@ -68,6 +70,11 @@ struct Work {
     int c0, c1;           // first and last pair with a piece of the tile
     int first, count;     // places of the tile (gradients: of the group)
     int e0, e1;           // stages of the extension that go with the piece
+};
+
+template <int N>
+struct Launch {
+    GroupCall call[N];
 };
 
 // Shared memory behind the stages: this, then the group tables.
@@ -201,8 +208,8 @@ struct Walk {
     __device__ Walk(const GroupProduct &p_, const Tables &t_) : p(p_), t(t_) {
         const bool grad = p.mode == GP_WGRAD;
         const int per = p.mtiles * p.ntiles, tiles = grad ? t.ng * per : t.tile0[t.ng];
-        me = next_tile = blockIdx.x >> 1;
-        pairs = gridDim.x >> 1;
+        me = next_tile = (blockIdx.x >> 1) - p.pair0;
+        pairs = p.pairs;
         const int deep = GP_BK * p.kk;
         kiters = (p.k + deep - 1) / deep;
         dp = tiles >= 2 * pairs ? (tiles / pairs - 1) * pairs : 0;
@@ -456,7 +463,11 @@ __device__ void pick_rows(const GroupProduct &p, Tables &t, uint8_t *sm, int ran
 
 template <bool F16, int KIND>
 __global__ void __launch_bounds__(THREADS, 1) __cluster_dims__(2, 1, 1)
-k_group(const __grid_constant__ GroupMaps maps, const __grid_constant__ GroupProduct p) {
+k_group(const __grid_constant__ Launch<KIND >= K_LOW ? 2 : 1> launch) {
+    constexpr int CALLS = KIND >= K_LOW ? 2 : 1;
+    const GroupCall &call = launch.call[CALLS > 1 && (int)(blockIdx.x >> 1) >= launch.call[CALLS - 1].p.pair0];
+    const GroupProduct &p = call.p;
+    const GroupMaps &maps = call.maps;
     extern __shared__ uint8_t smem_raw[];
     uint8_t *sm = (uint8_t *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
     Tables &t = *(Tables *)(sm + (size_t)p.stages * p.stage_bytes);
@@ -464,7 +475,8 @@ k_group(const __grid_constant__ GroupMaps maps, const __grid_constant__ GroupPro
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = cluster_rank();
     constexpr bool grad = KIND == K_GRAD || KIND == K_LOW;
-    constexpr bool grouped = KIND == K_GROUPED, shared = KIND == K_SHARED, low = KIND == K_LOW, pack = KIND == K_PACK;
+    constexpr bool grouped = KIND == K_GROUPED, shared = KIND == K_SHARED, low = KIND == K_LOW;
+    constexpr bool pack = KIND == K_PACK || KIND == K_PACKS;
     constexpr int CS = GP_TILE;      // TMEM columns of one of the two accumulators
 
     if (threadIdx.x == 0) {
@@ -859,7 +871,7 @@ k_group(const __grid_constant__ GroupMaps maps, const __grid_constant__ GroupPro
                 __threadfence();
                 named_bar_sync(1, threads);
                 if (threadIdx.x == 0) {
-                    uint32_t *count = p.count + 2 * w.c0 + rank;
+                    uint32_t *count = p.count + 2 * (p.pair0 + w.c0) + rank;
                     t.last = atomicAdd(count, 1u) == (uint32_t)(w.c1 - w.c0);
                     if (t.last) *count = 0;
                     __threadfence();
@@ -904,7 +916,7 @@ k_group(const __grid_constant__ GroupMaps maps, const __grid_constant__ GroupPro
                     for (int j = 0; j < 32; ++j) v[j] = 0.f;
 #pragma unroll 2
                     for (int o = w.c0; o <= (mine ? w.c1 : -1); ++o) {
-                        const int slot = 2 * (2 * o + rank) + (o == w.c0);
+                        const int slot = 2 * (2 * (p.pair0 + o) + rank) + (o == w.c0);
                         const float4 *src = (const float4 *)(p.part + (size_t)slot * 128 * GP_TILE) + r;
                         float4 x[8];
 #pragma unroll
@@ -1034,18 +1046,18 @@ k_group(const __grid_constant__ GroupMaps maps, const __grid_constant__ GroupPro
     }
 }
 
-using Kernel = void (*)(GroupMaps, GroupProduct);
-
-Kernel kernel_of(int f16, int kind) {
-    static const Kernel all[2][5] = {
-        {k_group<false, 0>, k_group<false, 1>, k_group<false, 2>, k_group<false, 3>, k_group<false, 4>},
-        {k_group<true, 0>, k_group<true, 1>, k_group<true, 2>, k_group<true, 3>, k_group<true, 4>}};
+const void *kernel_of(int f16, int kind) {
+    static const void *const all[2][KINDS] = {
+        {(const void *)k_group<false, 0>, (const void *)k_group<false, 1>, (const void *)k_group<false, 2>,
+         (const void *)k_group<false, 3>, (const void *)k_group<false, 4>, (const void *)k_group<false, 5>},
+        {(const void *)k_group<true, 0>, (const void *)k_group<true, 1>, (const void *)k_group<true, 2>,
+         (const void *)k_group<true, 3>, (const void *)k_group<true, 4>, (const void *)k_group<true, 5>}};
     return all[f16][kind];
 }
 
-int kind_of(const GroupProduct &p) {
+int kind_of(const GroupProduct &p, int n) {
     if (p.mode == GP_GROUPED) return K_GROUPED;
-    if (p.mode == GP_ROWS) return p.shared ? K_SHARED : K_PACK;
+    if (p.mode == GP_ROWS) return p.shared ? K_SHARED : n > 1 ? K_PACKS : K_PACK;
     return p.out_kind == GP_OUT_GROUP ? K_GRAD : K_LOW;
 }
 
@@ -1053,9 +1065,9 @@ int kind_of(const GroupProduct &p) {
 
 cudaError_t group_prepare(int nsm, int *ctas) {
     cudaError_t e = cudaSuccess;
-    for (int kind = 0; kind < 5 && e == cudaSuccess; ++kind)
+    for (int kind = 0; kind < KINDS && e == cudaSuccess; ++kind)
         for (int f16 = 0; f16 < 2 && e == cudaSuccess; ++f16)
-            e = cudaFuncSetAttribute((const void *)kernel_of(f16, kind), cudaFuncAttributeMaxDynamicSharedMemorySize,
+            e = cudaFuncSetAttribute(kernel_of(f16, kind), cudaFuncAttributeMaxDynamicSharedMemorySize,
                                      SMEM_MAX);
     if (e != cudaSuccess) return e;
     // the pairs that run at once: the walk deals its pieces to that many
@@ -1070,7 +1082,7 @@ cudaError_t group_prepare(int nsm, int *ctas) {
     cfg.attrs = at;
     cfg.numAttrs = 1;
     int pairs = 0;
-    e = cudaOccupancyMaxActiveClusters(&pairs, (const void *)kernel_of(0, K_SHARED), &cfg);
+    e = cudaOccupancyMaxActiveClusters(&pairs, kernel_of(0, K_SHARED), &cfg);
     if (e == cudaSuccess && pairs < 1) e = cudaErrorLaunchOutOfResources;
     *ctas = 2 * (pairs < nsm / 2 ? pairs : nsm / 2);
     return e;
@@ -1107,18 +1119,33 @@ void group_plan(GroupProduct *p) {
     p->mtiles = (p->m + GP_TILE - 1) / GP_TILE;
 }
 
-cudaError_t launch_group(const GroupProduct &p, const GroupMaps &maps, int ctas, cudaStream_t s) {
+cudaError_t launch_group(GroupCall *calls, int n, double share, int ctas, cudaStream_t s) {
+    const int pairs = ctas / 2, kind = kind_of(calls[0].p, n);
+    int first = pairs;
+    if (n > 1) {
+        first = (int)(share * pairs + 0.5);
+        first = first < 1 ? 1 : first > pairs - 1 ? pairs - 1 : first;
+    }
+    calls[0].p.pair0 = 0;
+    calls[0].p.pairs = first;
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.gridDim = dim3((unsigned)ctas);
     cfg.blockDim = dim3(THREADS);
-    cfg.dynamicSmemBytes = (size_t)p.smem;
+    cfg.dynamicSmemBytes = (size_t)calls[0].p.smem;
     cfg.stream = s;
     cfg.attrs = at;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, kernel_of(p.f16 != 0, kind_of(p)), maps, p);
+    Launch<2> two;
+    two.call[0] = calls[0];
+    two.call[1] = calls[n - 1];
+    two.call[1].p.pair0 = first;          // (one call: a pair that does not exist)
+    two.call[1].p.pairs = pairs - first;
+    if (n > 1 && two.call[1].p.smem > calls[0].p.smem) cfg.dynamicSmemBytes = (size_t)two.call[1].p.smem;
+    void *args[1] = {&two};               // kernels of one call take the first
+    return cudaLaunchKernelExC(&cfg, kernel_of(calls[0].p.f16 != 0, kind), args);
 }
 
 }  // namespace hwr

@@ -412,9 +412,14 @@ static hwr_status check_tiles(hwr_ops *c, const GroupProduct &p) {
     return HWR_OK;
 }
 
-// out[t] = W[g(t)] x[t] (w K-major: [out][in]) or W[g(t)]^T x[t] (w_mn).
+static hwr_status launch(hwr_ops *c, GroupCall *calls, int n = 1, double share = 1) {
+    CK(c, launch_group(calls, n, share, c->ctas, c->stream), "product kernel");
+    return HWR_OK;
+}
+
+// out[t] = W[g(t)] x[t] (w K-major: [out][in]) or W[g(t)]^T x[t] (w_mn), to be launched.
 static hwr_status rows_product(hwr_ops *c, GroupProduct p, const Operand &x, const Operand &w, bool w_mn, int n,
-                               const Operand *u, const Operand *eb) {
+                               const Operand *u, const Operand *eb, GroupCall *call) {
     p.k = x.cols;
     p.n = n;
     p.dense_mn = w_mn;
@@ -426,7 +431,8 @@ static hwr_status rows_product(hwr_ops *c, GroupProduct p, const Operand &x, con
     else p.bn = even_tiles(n, p.sorted || !p.shared ? GP_TILE : FEW_BN);
     group_plan(&p);
     OK(check_tiles(c, p));
-    GroupMaps m;
+    call->p = p;
+    GroupMaps &m = call->maps;
     memset(&m, 0, sizeof m);
     if (p.sorted) {
         OK(encode(c, &m.x, p.f16, x, 64, GP_ROW_BOX));
@@ -438,12 +444,11 @@ static hwr_status rows_product(hwr_ops *c, GroupProduct p, const Operand &x, con
         OK(w_mn ? encode(c, &m.eb, p.f16, *eb, 64, GP_RC)
                 : encode(c, &m.eb, p.f16, *eb, p.rank <= 16 ? 16 : GP_RC, p.bn / 2));
     }
-    CK(c, launch_group(p, m, c->ctas, c->stream), "product kernel");
     return HWR_OK;
 }
 
-// out[g] = sum over the rows of g of l[t] r[t]^T.
-static hwr_status grad_product(hwr_ops *c, GroupProduct p, const Operand &l, const Operand &r) {
+// out[g] = sum over the rows of g of l[t] r[t]^T, to be launched.
+static hwr_status grad_product(hwr_ops *c, GroupProduct p, const Operand &l, const Operand &r, GroupCall *call) {
     p.mode = GP_WGRAD;
     p.m = l.cols;
     p.n = r.cols;
@@ -451,11 +456,11 @@ static hwr_status grad_product(hwr_ops *c, GroupProduct p, const Operand &l, con
     group_plan(&p);
     if ((int64_t)p.plan.groups * p.mtiles * p.ntiles > INT32_MAX)
         return fail(c, HWR_ERR_UNSUPPORTED, "groups %d x %d x %d is too large", p.plan.groups, p.m, p.n);
-    GroupMaps m;
+    call->p = p;
+    GroupMaps &m = call->maps;
     memset(&m, 0, sizeof m);
     OK(encode(c, &m.x, p.f16, l, 64, GP_BK));
     OK(encode(c, &m.w, p.f16, r, 64, GP_BK));
-    CK(c, launch_group(p, m, c->ctas, c->stream), "weight gradient kernel");
     return HWR_OK;
 }
 
@@ -502,7 +507,9 @@ extern "C" hwr_status hwr_grouped_forward(hwr_ops *c, const hwr_rows *r, void *y
     p.out = y;
     p.ld = y_ld;
     p.vec = vec_ok(y, y_ld, 0);
-    return rows_product(c, p, rows.x, w, false, r->n_out, nullptr, nullptr);
+    GroupCall call;
+    OK(rows_product(c, p, rows.x, w, false, r->n_out, nullptr, nullptr, &call));
+    return launch(c, &call);
 }
 
 extern "C" hwr_status hwr_grouped_backward(hwr_ops *c, const hwr_rows *r, const void *dy, int64_t dy_ld, void *dx,
@@ -526,6 +533,7 @@ extern "C" hwr_status hwr_grouped_backward(hwr_ops *c, const hwr_rows *r, const 
     if (dx) w = cv.operand(r->w, r->w_ld, r->n_out, r->n_in, r->w_group, r->groups);
     OK(reserve(c, cv.at));
     OK(sort_rows(c, &rows));
+    GroupCall call;
     if (dx) {
         OK(settle(c, &w));
         GroupProduct p = product(c, r, rows);
@@ -534,7 +542,8 @@ extern "C" hwr_status hwr_grouped_backward(hwr_ops *c, const hwr_rows *r, const 
         p.out = dx;
         p.ld = dx_ld;
         p.vec = vec_ok(dx, dx_ld, 0);
-        OK(rows_product(c, p, rows.dy, w, true, r->n_in, nullptr, nullptr));
+        OK(rows_product(c, p, rows.dy, w, true, r->n_in, nullptr, nullptr, &call));
+        OK(launch(c, &call));
     }
     if (dw) {
         GroupProduct p = product(c, r, rows);
@@ -543,7 +552,8 @@ extern "C" hwr_status hwr_grouped_backward(hwr_ops *c, const hwr_rows *r, const 
         p.ld = r->w_ld;
         p.gstride = r->groups > 1 ? r->w_group : 0;
         p.vec = vec_ok(dw, r->w_ld, p.gstride);
-        OK(grad_product(c, p, rows.dy, rows.x));
+        OK(grad_product(c, p, rows.dy, rows.x, &call));
+        OK(launch(c, &call));
     }
     return HWR_OK;
 }
@@ -559,26 +569,7 @@ static hwr_status check_adapters(hwr_ops *c, const hwr_rows *r, const hwr_adapte
 // scale[g] M[g] x[t] (or M[g]^T x[t]) by place, as two 16-bit terms: [places]
 // [32-rank chunks][high, low], an even number of chunks.
 static hwr_status low_rank(hwr_ops *c, const hwr_rows *r, const hwr_adapters *ad, const Rows &rows, const Operand &x,
-                           const Operand &m, bool m_mn, const Operand &u, bool wide = false) {
-    // a row reads its adapter's matrix once: few enough bytes need no tensor
-    // cores (64 rows, rank 16, 4,096 columns: 27 us on them, 5 us without)
-    if (wide || (!rows.sorted && !m_mn && (int64_t)r->rows * ad->rank * x.cols <= LOW_FEW_VALUES)) {
-        LowFew f;
-        f.plan = rows.plan;
-        f.k = x.cols;
-        f.rank = ad->rank;
-        f.x = (const uint16_t *)x.p;
-        f.x_ld = x.ld;
-        f.a = (const uint16_t *)m.p;
-        f.a_ld = m.ld;
-        f.a_z = m.z;
-        f.scale = ad->scale;
-        f.u = (uint16_t *)const_cast<void *>(u.p);
-        f.u_ld = u.ld;
-        f.wide = wide ? (float *)const_cast<void *>(u.p) : nullptr;
-        CK(c, launch_low_few(f, r->dtype == HWR_F16, c->stream), "low-rank kernel");
-        return HWR_OK;
-    }
+                           const Operand &m, bool m_mn, const Operand &u, GroupCall *call) {
     GroupProduct p = product(c, r, rows);
     p.mode = GP_ROWS;
     p.out_kind = GP_OUT_PACK;
@@ -586,7 +577,29 @@ static hwr_status low_rank(hwr_ops *c, const hwr_rows *r, const hwr_adapters *ad
     p.ld = u.ld;
     p.vec = 1;
     p.scale = ad->scale;
-    return rows_product(c, p, x, m, m_mn, ad->rank, nullptr, nullptr);
+    return rows_product(c, p, x, m, m_mn, ad->rank, nullptr, nullptr, call);
+}
+
+// The same of picked rows without tensor cores, or (wide) as fp32 [places][rank]:
+// a row reads its adapter's matrix once, and so few bytes need none (64 rows, rank
+// 16, 4,096 columns: 27 us on them, 5 us without).
+static hwr_status low_rank_few(hwr_ops *c, const hwr_rows *r, const hwr_adapters *ad, const Rows &rows,
+                               const Operand &a, const Operand &u, bool wide) {
+    LowFew f;
+    f.plan = rows.plan;
+    f.k = rows.x.cols;
+    f.rank = ad->rank;
+    f.x = (const uint16_t *)rows.x.p;
+    f.a = (const uint16_t *)a.p;
+    f.x_ld = rows.x.ld;
+    f.a_ld = a.ld;
+    f.a_z = a.z;
+    f.scale = ad->scale;
+    f.u = (uint16_t *)const_cast<void *>(u.p);
+    f.u_ld = u.ld;
+    f.wide = wide ? (float *)const_cast<void *>(u.p) : nullptr;
+    CK(c, launch_low_few(f, r->dtype == HWR_F16, c->stream), "low-rank kernel");
+    return HWR_OK;
 }
 
 // The packed inner products' place in the workspace.
@@ -604,6 +617,7 @@ static Operand packed(Carver &cv, const Rows &rows, const hwr_adapters *ad) {
 static hwr_status shared_product(hwr_ops *c, const hwr_rows *r, const hwr_adapters *ad, const Rows &rows,
                                  const Operand &x, const Operand &w, bool w_mn, const Operand &u, const Operand &eb,
                                  void *out, int64_t ld, int n) {
+    GroupCall call;
     GroupProduct p = product(c, r, rows);
     p.mode = GP_ROWS;
     p.shared = 1;
@@ -612,7 +626,8 @@ static hwr_status shared_product(hwr_ops *c, const hwr_rows *r, const hwr_adapte
     p.out = out;
     p.ld = ld;
     p.vec = vec_ok(out, ld, 0);
-    return rows_product(c, p, x, w, w_mn, n, &u, &eb);
+    OK(rows_product(c, p, x, w, w_mn, n, &u, &eb, &call));
+    return launch(c, &call);
 }
 
 extern "C" hwr_status hwr_adapter_forward(hwr_ops *c, const hwr_rows *r, const hwr_adapters *ad, void *y,
@@ -654,12 +669,18 @@ extern "C" hwr_status hwr_adapter_forward(hwr_ops *c, const hwr_rows *r, const h
         f.b = (const uint16_t *)ad->b;
         f.b_ld = R;
         f.b_z = (int64_t)N * R;
-        OK(low_rank(c, r, ad, rows, rows.x, a, false, u, true));
+        OK(low_rank_few(c, r, ad, rows, a, u, true));
         CK(c, launch_few_rows(f, r->dtype == HWR_F16, c->stream), "few-rows kernel");
         return HWR_OK;
     }
     OK(settle(c, &b));
-    OK(low_rank(c, r, ad, rows, rows.x, a, false, u));
+    if (!rows.sorted && (int64_t)r->rows * R * K <= LOW_FEW_VALUES) {
+        OK(low_rank_few(c, r, ad, rows, a, u, false));
+    } else {
+        GroupCall call;
+        OK(low_rank(c, r, ad, rows, rows.x, a, false, u, &call));
+        OK(launch(c, &call));
+    }
     return shared_product(c, r, ad, rows, rows.x, w, false, u, b, y, y_ld, N);
 }
 
@@ -695,12 +716,19 @@ extern "C" hwr_status hwr_adapter_backward(hwr_ops *c, const hwr_rows *r, const 
     OK(sort_rows(c, &rows));
     if (dx) OK(settle(c, &w));
     if (dx || db) OK(settle(c, &a));
+    // v and u are independent of each other, and so are da and db: two in a launch,
+    // on shares of the SMs by what they read (a launch of its own takes 10 us)
+    GroupCall calls[2];
+    int n = 0;
     if (dx || da) {
         OK(settle(c, &b));
-        OK(low_rank(c, r, ad, rows, rows.dy, b, true, v));
+        OK(low_rank(c, r, ad, rows, rows.dy, b, true, v, &calls[n++]));
     }
-    if (db) OK(low_rank(c, r, ad, rows, rows.x, a, false, u));
+    if (db) OK(low_rank(c, r, ad, rows, rows.x, a, false, u, &calls[n++]));
+    const double by_n = (double)N / ((double)N + K);
+    OK(launch(c, calls, n, by_n));
     if (dx) OK(shared_product(c, r, ad, rows, rows.dy, w, true, v, a, dx, dx_ld, K));
+    n = 0;
     if (da) {
         GroupProduct p = product(c, r, rows);
         p.out_kind = GP_OUT_LOW_T;
@@ -708,7 +736,7 @@ extern "C" hwr_status hwr_adapter_backward(hwr_ops *c, const hwr_rows *r, const 
         p.ld = K;
         p.gstride = (int64_t)R * K;
         p.rank_out = R;
-        OK(grad_product(c, p, rows.x, v));
+        OK(grad_product(c, p, rows.x, v, &calls[n++]));
     }
     if (db) {
         GroupProduct p = product(c, r, rows);
@@ -718,9 +746,9 @@ extern "C" hwr_status hwr_adapter_backward(hwr_ops *c, const hwr_rows *r, const 
         p.gstride = (int64_t)N * R;
         p.rank_out = R;
         p.vec = vec_ok(db, R, p.gstride);
-        OK(grad_product(c, p, rows.dy, u));
+        OK(grad_product(c, p, rows.dy, u, &calls[n++]));
     }
-    return HWR_OK;
+    return n ? launch(c, calls, n, 1 - by_n) : HWR_OK;
 }
 
 // ---------------------------------------------------------------------------

@@ -82,6 +82,7 @@ struct GroupProduct {
     uint32_t *count = nullptr;
     int32_t *status = nullptr;
     int test_stall = 0;               // test hook: nothing is loaded (bounded waits expire)
+    int pair0 = 0, pairs = 0;         // the CTA pairs at work on it
 };
 
 // x: the rows by place (or l and r of a gradient: the A and B side); w: the
@@ -92,11 +93,19 @@ struct GroupMaps {
 
 constexpr int GP_ROW_BOX = 32;     // rows of a box of x and u
 
+// A product as it is launched; of the kinds with small tiles (GP_OUT_PACK,
+// GP_OUT_LOW*) two may share a launch, each on some of the pairs.
+struct GroupCall {
+    GroupMaps maps;
+    GroupProduct p;
+};
+
 cudaError_t group_prepare(int nsm, int *ctas);
 // Pipeline stages that fit beside the tables, and the counts of tiles.
 void group_plan(GroupProduct *p);
 size_t group_part_floats(int ctas);
-cudaError_t launch_group(const GroupProduct &p, const GroupMaps &maps, int ctas, cudaStream_t s);
+// n calls (1 or 2, of one kind) in a launch; share: of the pairs for the first of two.
+cudaError_t launch_group(GroupCall *calls, int n, double share, int ctas, cudaStream_t s);
 
 // ---- products of a few rows (k_few.cu) ---------------------------------------
 
