@@ -49,6 +49,7 @@ constexpr int MAX_STAGES = 24;
 constexpr int SMEM_MAX = 227 * 1024;
 constexpr int MIN_PIECE = 6 * GP_BK;   // columns of the smallest piece of a cut tile
 constexpr int JOIN_COST = 8 * GP_BK;   // columns that joining the pieces of tiles costs (about 4 us)
+constexpr int BAND = 8;            // row tiles (32: 666 us for 8,192^3, 8: 635 us)
 constexpr int WRITE_COST = 4;      // iterations that writing a gradient's tile counts for
 
 constexpr int OUT_PITCH = 64;      // bytes of a staged output row (32 columns)
@@ -272,12 +273,13 @@ struct Walk {
                 w.g = find(t.tile0, t.ng, tile);
                 const int local = tile - t.tile0[w.g];
                 const int n = t.offs[w.g + 1] - t.offs[w.g], xts = (n + GP_TILE - 1) / GP_TILE;
-                // bands of 32 row tiles, column by column: the pairs at work share
-                // columns of W and the band's rows stay in L2
-                const int band = local / (32 * p.ntiles), in = local - band * 32 * p.ntiles;
-                const int h = min(32, xts - band * 32);
+                // bands of BAND row tiles, column by column: the pairs at work are
+                // about as many columns as rows of tiles, so that each tile of W and
+                // of x that L2 serves is wanted by several at a time
+                const int band = local / (BAND * p.ntiles), in = local - band * BAND * p.ntiles;
+                const int h = min(BAND, xts - band * BAND);
                 w.ot = in / h;
-                w.xt = band * 32 + (in - w.ot * h);
+                w.xt = band * BAND + (in - w.ot * h);
                 // rows on the B side: tiles of about equal extent
                 const int width = p.mode == GP_GROUPED && xts <= 8 ? up16((n + xts - 1) / xts) : GP_TILE;
                 w.first = t.offs[w.g] + w.xt * width;

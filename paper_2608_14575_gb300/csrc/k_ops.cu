@@ -79,30 +79,6 @@ k_dispatch_few(int rows, int G, const int32_t *choice, int32_t *offsets, int32_t
     }
 }
 
-// Rows of each key in each block: hist [blocks][G + 1].
-__global__ void __launch_bounds__(DP_THREADS)
-k_dispatch_count(int rows, int G, int64_t per_block, const int32_t *choice, int32_t *hist) {
-    extern __shared__ int32_t sh[];
-    for (int i = threadIdx.x; i <= G; i += DP_THREADS) sh[i] = 0;
-    pdl_begin();
-    __syncthreads();
-    const int64_t begin = blockIdx.x * per_block;
-    const int64_t end = begin + per_block < rows ? begin + per_block : rows;
-    const int lane = threadIdx.x & 31, nbits = 32 - __clz(G + 1);
-    for (int64_t r0 = begin; r0 < end; r0 += DP_ROWS) {
-        int key[DP_PER];
-#pragma unroll
-        for (int i = 0; i < DP_PER; ++i) key[i] = key_of(choice, r0 + i * DP_THREADS + threadIdx.x, end, G);
-#pragma unroll
-        for (int i = 0; i < DP_PER; ++i) {
-            const uint32_t peers = peers_of(key[i], nbits);
-            if (key[i] <= G && lane == __ffs(peers) - 1) atomicAdd(&sh[key[i]], __popc(peers));
-        }
-    }
-    __syncthreads();
-    for (int i = threadIdx.x; i <= G; i += DP_THREADS) hist[(int64_t)blockIdx.x * (G + 1) + i] = sh[i];
-}
-
 __device__ __forceinline__ int remote_int(const int32_t *p, int rank) {
     uint32_t a;
     int v;
@@ -115,10 +91,47 @@ __device__ __forceinline__ void cluster_barrier() {
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
-// hist: counts per block of k_dispatch_count; null with one block, or with one
-// cluster of blocks of a round each.
+// Rows of each key in the blocks of a cluster before each of its blocks: hist
+// [blocks][G + 1]; then those of each whole cluster: [clusters][G + 1].
 __global__ void __launch_bounds__(DP_THREADS)
-k_dispatch_place(int rows, int G, int64_t per_block, const int32_t *choice, const int32_t *hist,
+k_dispatch_count(int rows, int G, int64_t per_block, const int32_t *choice, int32_t *hist) {
+    extern __shared__ int32_t sh[];
+    const int tid = threadIdx.x, lane = tid & 31, nbits = 32 - __clz(G + 1), G1 = G + 1;
+    for (int i = tid; i < G1; i += DP_THREADS) sh[i] = 0;
+    pdl_begin();
+    __syncthreads();
+    const int64_t begin = blockIdx.x * per_block;
+    const int64_t end = begin + per_block < rows ? begin + per_block : rows;
+    for (int64_t r0 = begin; r0 < end; r0 += DP_ROWS) {
+        int key[DP_PER];
+#pragma unroll
+        for (int i = 0; i < DP_PER; ++i) key[i] = key_of(choice, r0 + i * DP_THREADS + tid, end, G);
+#pragma unroll
+        for (int i = 0; i < DP_PER; ++i) {
+            const uint32_t peers = peers_of(key[i], nbits);
+            if (key[i] <= G && lane == __ffs(peers) - 1) atomicAdd(&sh[key[i]], __popc(peers));
+        }
+    }
+    cluster_barrier();
+    const int rank = blockIdx.x % DP_CLUSTER;
+    for (int g = tid; g < G1; g += DP_THREADS) {
+        int before = 0, all = 0;
+#pragma unroll
+        for (int b = 0; b < DP_CLUSTER; ++b) {
+            const int c = remote_int(&sh[g], b);
+            before += b < rank ? c : 0;
+            all += c;
+        }
+        hist[(int64_t)blockIdx.x * G1 + g] = before;
+        if (rank == 0) hist[((int64_t)gridDim.x + blockIdx.x / DP_CLUSTER) * G1 + g] = all;
+    }
+    cluster_barrier();       // the others may still read this block's counts
+}
+
+// hist: from k_dispatch_count, of `counted` blocks; null with one block, or with
+// one cluster of blocks of a round each.
+__global__ void __launch_bounds__(DP_THREADS)
+k_dispatch_place(int rows, int G, int64_t per_block, const int32_t *choice, const int32_t *hist, int counted,
                  int32_t *offsets, int32_t *order) {
     extern __shared__ int32_t sh[];
     const int G1 = G + 1, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, nb = gridDim.x;
@@ -159,18 +172,17 @@ k_dispatch_place(int rows, int G, int64_t per_block, const int32_t *choice, cons
         if (hist && r0 == begin) {
             // rows of each key in the blocks before this one, and in all
             pdl_begin();
-            const int subs = max(1, DP_THREADS / G1);
-            for (int j = tid; j < G1 * subs; j += DP_THREADS) {
-                const int g = j % G1, sub = j / G1;
-                int before = 0, all = 0;
+            const int clusters = counted / DP_CLUSTER, mine = blockIdx.x / DP_CLUSTER;
+            for (int g = tid; g < G1; g += DP_THREADS) {
+                int before = hist[(int64_t)blockIdx.x * G1 + g], all = 0;
 #pragma unroll 8
-                for (int b = sub; b < nb; b += subs) {
-                    const int c = hist[(int64_t)b * G1 + g];
-                    all += c;
-                    before += b < (int)blockIdx.x ? c : 0;
+                for (int c = 0; c < clusters; ++c) {
+                    const int v = hist[((int64_t)counted + c) * G1 + g];
+                    all += v;
+                    before += c < mine ? v : 0;
                 }
-                atomicAdd(&base[g], before);
-                atomicAdd(&total[g], all);
+                base[g] = before;
+                total[g] = all;
             }
         }
         __syncthreads();
@@ -674,6 +686,7 @@ cudaError_t ops_prepare() {
     const auto attr = cudaFuncAttributeMaxDynamicSharedMemorySize;
     cudaError_t e = cudaFuncSetAttribute(k_dispatch_place, attr, (int)place_smem(OPS_MAX_GROUPS));
     if (e == cudaSuccess) e = cudaFuncSetAttribute(k_dispatch_place, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(k_dispatch_count, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
     return e;
 }
 
@@ -689,7 +702,8 @@ static int dispatch_blocks(int rows, int nsm, int64_t *per_block) {
 size_t dispatch_scratch_ints(int rows, int groups, int nsm) {
     int64_t per;
     const int b = dispatch_blocks(rows, nsm, &per);
-    return b > DP_CLUSTER ? (size_t)b * (groups + 1) : 0;
+    const int counted = (b + DP_CLUSTER - 1) / DP_CLUSTER * DP_CLUSTER;
+    return b > DP_CLUSTER ? (size_t)(counted + counted / DP_CLUSTER) * (groups + 1) : 0;
 }
 
 // A launch that may begin while the kernel before it ends (it waits by itself).
@@ -716,19 +730,19 @@ cudaError_t launch_dispatch(int rows, int groups, const int32_t *choice, int32_t
     int64_t per;
     const int b = dispatch_blocks(rows, nsm, &per);
     const int32_t *hist = b > DP_CLUSTER ? scratch : nullptr;
+    const int counted = (b + DP_CLUSTER - 1) / DP_CLUSTER * DP_CLUSTER;
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.x = hist ? DP_CLUSTER : b;
+    at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
     if (hist) {
-        const cudaLaunchConfig_t cfg = relaxed(b, DP_THREADS, (groups + 1) * 4, s, at);
+        cudaLaunchConfig_t cfg = relaxed(counted, DP_THREADS, (groups + 1) * 4, s, at);
+        cfg.numAttrs = 2;
         const cudaError_t e = cudaLaunchKernelEx(&cfg, k_dispatch_count, rows, groups, per, choice, scratch);
         if (e != cudaSuccess) return e;
     }
     cudaLaunchConfig_t cfg = relaxed(b, DP_THREADS, place_smem(groups), s, at);
-    if (!hist && b > 1) {
-        at[1].id = cudaLaunchAttributeClusterDimension;
-        at[1].val.clusterDim.x = b;
-        at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
-        cfg.numAttrs = 2;
-    }
-    return cudaLaunchKernelEx(&cfg, k_dispatch_place, rows, groups, per, choice, hist, offsets, order);
+    if (!hist && b > 1) cfg.numAttrs = 2;
+    return cudaLaunchKernelEx(&cfg, k_dispatch_place, rows, groups, per, choice, hist, counted, offsets, order);
 }
 
 cudaError_t launch_sort_rows(const GroupPlan &plan, const SortRows &m, int places, int32_t *padded_offsets,
