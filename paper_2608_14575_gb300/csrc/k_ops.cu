@@ -456,14 +456,14 @@ k_pad(uint16_t *dst, int64_t dst_ld, const uint16_t *src, int64_t src_ld, int64_
 
 // ---------------------------------------------------------------------------
 // Gradient clipping: one pass sums the squares, one scales.  Both are bound by
-// HBM.  The tensors are cut into chunks of 16 KB, named by a table in device
-// memory (read from kernel parameters, the table's cache misses cost more than
-// the chunks of a small set of gradients); a block's chunks lie a grid apart,
+// HBM.  The tensors are cut into chunks, named by a table in device memory (read
+// from kernel parameters, the table's cache misses cost more than the chunks of a
+// small set of gradients); a block's chunks lie a grid apart,
 // so that the whole GPU walks the tensors in order, and the second pass walks
 // them backwards: it begins with what the first left in L2.
 
 constexpr int CL_THREADS = 256;
-constexpr int CL_PER = CLIP_CHUNK_BYTES / 16 / CL_THREADS;   // 16-byte accesses of a thread in a chunk
+static_assert(CLIP_UNIT == CL_THREADS * 16, "a 16-byte access a thread");
 
 template <int DT>
 struct Vec {
@@ -510,12 +510,12 @@ struct Vec {
         else if (DT == HWR_BF16) ((__nv_bfloat16 *)p)[i] = __float2bfloat16_rn(v);
         else ((__half *)p)[i] = __float2half_rn(v);
     }
-    static constexpr int FULL = CLIP_CHUNK_BYTES / (DT == HWR_F32 ? 4 : 2);
+    static constexpr int FULL = CLIP_UNIT / (DT == HWR_F32 ? 4 : 2);      // of a unit
 };
 
 // The squares of a thread's share of a chunk once more, in 64 bits: where
 // their fp32 sum left the range that fp32 holds well.
-template <int DT>
+template <int DT, int CL_PER>
 __device__ __noinline__ double wide_squares(const void *in, int n, bool vec) {
     double s = 0;
     auto add = [&](float f) { s += (double)f * f; };
@@ -528,10 +528,10 @@ __device__ __noinline__ double wide_squares(const void *in, int n, bool vec) {
     return s;
 }
 
-template <int DT>
+template <int DT, int CL_PER>
 __device__ __forceinline__ void sum_chunk(const ClipChunk &c, float &acc, double &wide) {
     constexpr int N = Vec<DT>::N;
-    const bool vec = c.n == Vec<DT>::FULL && ((uintptr_t)c.in & 15) == 0;
+    const bool vec = c.n == CL_PER * Vec<DT>::FULL && ((uintptr_t)c.in & 15) == 0;
     float s = 0.f;
     if (vec) {
         const uint4 *v = (const uint4 *)c.in + threadIdx.x;
@@ -560,13 +560,13 @@ __device__ __forceinline__ void sum_chunk(const ClipChunk &c, float &acc, double
         if (!any) return;
     }
     if (s >= 1e-30f && s <= 1e30f) acc += s;
-    else wide += wide_squares<DT>(c.in, c.n, vec);      // NaN and infinities too
+    else wide += wide_squares<DT, CL_PER>(c.in, c.n, vec);      // NaN and infinities too
 }
 
-template <int DT>
+template <int DT, int CL_PER>
 __device__ __forceinline__ void scale_chunk(const ClipChunk &c, float k) {
     constexpr int N = Vec<DT>::N;
-    if (c.n == Vec<DT>::FULL && (((uintptr_t)c.in | (uintptr_t)c.out) & 15) == 0) {
+    if (c.n == CL_PER * Vec<DT>::FULL && (((uintptr_t)c.in | (uintptr_t)c.out) & 15) == 0) {
         // (read for the last time, written for others: neither is to push out of L2
         // what the first pass left there)
         const uint4 *v = (const uint4 *)c.in + threadIdx.x;
@@ -611,11 +611,12 @@ k_clip_table(const __grid_constant__ ClipTable t, ClipChunk *table) {
         if (t.chunk0[m] <= i) lo = m;
         else hi = m - 1;
     }
-    table[t.at + i] = clip_chunk(t.in[lo], t.out[lo], t.count[lo], t.dtype[lo], i - t.chunk0[lo]);
+    table[t.at + i] = clip_chunk(t.in[lo], t.out[lo], t.count[lo], t.dtype[lo], t.per, i - t.chunk0[lo]);
 }
 
 // The last block to finish adds the blocks' sums, in their order, and leaves
 // the norm and the factor.
+template <int PER>
 __global__ void __launch_bounds__(CL_THREADS)
 k_square_sums(const ClipChunk *table, int chunks, ClipSums sums, float max_norm, float *norm) {
     __shared__ double w[CL_THREADS / 32];
@@ -630,9 +631,9 @@ k_square_sums(const ClipChunk *table, int chunks, ClipSums sums, float max_norm,
     for (; i < chunks; i += gridDim.x) {
         const ClipChunk now = c;
         if (i + gridDim.x < chunks) c = table[i + gridDim.x];
-        if (now.dtype == HWR_F32) sum_chunk<HWR_F32>(now, acc, wide);
-        else if (now.dtype == HWR_BF16) sum_chunk<HWR_BF16>(now, acc, wide);
-        else sum_chunk<HWR_F16>(now, acc, wide);
+        if (now.dtype == HWR_F32) sum_chunk<HWR_F32, PER>(now, acc, wide);
+        else if (now.dtype == HWR_BF16) sum_chunk<HWR_BF16, PER>(now, acc, wide);
+        else sum_chunk<HWR_F16, PER>(now, acc, wide);
     }
     const double s = warp_sum(acc, wide);
     if (lane == 0) w[warp] = s;
@@ -663,6 +664,7 @@ k_square_sums(const ClipChunk *table, int chunks, ClipSums sums, float max_norm,
     }
 }
 
+template <int PER>
 __global__ void __launch_bounds__(CL_THREADS)
 k_clip(const ClipChunk *table, int chunks, const float *factor) {
     pdl_begin();
@@ -674,9 +676,9 @@ k_clip(const ClipChunk *table, int chunks, const float *factor) {
         const ClipChunk now = c;
         if (i >= (int)gridDim.x) c = table[i - gridDim.x];
         if (k == 1.f && now.in == now.out) continue;
-        if (now.dtype == HWR_F32) scale_chunk<HWR_F32>(now, k);
-        else if (now.dtype == HWR_BF16) scale_chunk<HWR_BF16>(now, k);
-        else scale_chunk<HWR_F16>(now, k);
+        if (now.dtype == HWR_F32) scale_chunk<HWR_F32, PER>(now, k);
+        else if (now.dtype == HWR_BF16) scale_chunk<HWR_BF16, PER>(now, k);
+        else scale_chunk<HWR_F16, PER>(now, k);
     }
 }
 
@@ -782,14 +784,17 @@ cudaError_t launch_clip_table(const ClipTable &t, ClipChunk *table, cudaStream_t
     return cudaGetLastError();
 }
 
-cudaError_t launch_clip(const ClipChunk *table, int chunks, int nsm, const ClipSums &sums, float max_norm,
+cudaError_t launch_clip(const ClipChunk *table, int chunks, int per, int nsm, const ClipSums &sums, float max_norm,
                         float *norm, cudaStream_t s) {
     const int blocks = clip_blocks(chunks, nsm);
     cudaLaunchAttribute at[1];
     const cudaLaunchConfig_t cfg = relaxed(blocks, CL_THREADS, 0, s, at);
-    cudaError_t e = cudaLaunchKernelEx(&cfg, k_square_sums, table, chunks, sums, max_norm, norm);
-    if (e == cudaSuccess && chunks) e = cudaLaunchKernelEx(&cfg, k_clip, table, chunks, (const float *)sums.factor);
-    return e;
+    const float *factor = sums.factor;
+    cudaError_t e = per == 1 ? cudaLaunchKernelEx(&cfg, k_square_sums<1>, table, chunks, sums, max_norm, norm)
+                             : cudaLaunchKernelEx(&cfg, k_square_sums<CLIP_PER>, table, chunks, sums, max_norm, norm);
+    if (e != cudaSuccess || chunks == 0) return e;
+    return per == 1 ? cudaLaunchKernelEx(&cfg, k_clip<1>, table, chunks, factor)
+                    : cudaLaunchKernelEx(&cfg, k_clip<CLIP_PER>, table, chunks, factor);
 }
 
 }  // namespace hwr

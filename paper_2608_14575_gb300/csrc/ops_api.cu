@@ -755,12 +755,17 @@ extern "C" hwr_status hwr_adapter_backward(hwr_ops *c, const hwr_rows *r, const 
 
 struct hwr_gradients {
     ClipChunk *table = nullptr;
-    int chunks = 0;
+    int chunks = 0, per = 1;
 };
 
-static hwr_status check_gradients(hwr_ops *c, int32_t n, const hwr_gradient *grads, int64_t *chunks) {
+// Checks a list, and says into how many chunks of which size it is cut.
+static hwr_status check_gradients(hwr_ops *c, int32_t n, const hwr_gradient *grads, int64_t *chunks, int *per) {
     if (n < 0 || (n && !grads)) return fail(c, HWR_ERR_INVALID_ARG, "n %d or a NULL array", n);
     *chunks = 0;
+    int64_t all = 0;
+    for (int i = 0; i < n; ++i)
+        if (grads[i].n > 0 && all <= CLIP_SMALL) all += grads[i].n > CLIP_SMALL ? CLIP_SMALL + 1 : grads[i].n;
+    *per = all <= CLIP_SMALL ? 1 : CLIP_PER;
     for (int i = 0; i < n; ++i) {
         const hwr_gradient &g = grads[i];
         if (g.n < 0 || (g.n && (!g.in || !g.out)))
@@ -770,7 +775,7 @@ static hwr_status check_gradients(hwr_ops *c, int32_t n, const hwr_gradient *gra
         const uintptr_t mask = g.dtype == HWR_F32 ? 3 : 1;
         if (((uintptr_t)g.in | (uintptr_t)g.out) & mask)
             return fail(c, HWR_ERR_INVALID_ARG, "gradient %d is not aligned to its elements", i);
-        *chunks += g.n > INT64_MAX / 8 ? INT32_MAX : clip_chunks(g.n, g.dtype);
+        *chunks += g.n > INT64_MAX / 8 ? INT32_MAX : clip_chunks(g.n, g.dtype, *per);
         if (*chunks >= INT32_MAX) return fail(c, HWR_ERR_UNSUPPORTED, "too many elements");
     }
     return HWR_OK;
@@ -796,12 +801,14 @@ extern "C" hwr_status hwr_clip_gradients(hwr_ops *c, int32_t n, const hwr_gradie
     ApiRange range("hwr_clip_gradients");
     OK(ready(c));
     int64_t chunks;
-    OK(check_gradients(c, n, grads, &chunks));
+    int per;
+    OK(check_gradients(c, n, grads, &chunks, &per));
     OK(check_norm(c, max_norm, norm));
     OK(reserve(c, (size_t)chunks * sizeof(ClipChunk)));
     ClipChunk *table = (ClipChunk *)c->ws;
     ClipTable t;
     t.n = t.at = 0;
+    t.per = per;
     t.chunk0[0] = 0;
     for (int i = 0; i < n; ++i) {
         const hwr_gradient &g = grads[i];
@@ -809,13 +816,13 @@ extern "C" hwr_status hwr_clip_gradients(hwr_ops *c, int32_t n, const hwr_gradie
         t.out[t.n] = g.out;
         t.count[t.n] = g.n;
         t.dtype[t.n] = (uint8_t)g.dtype;
-        t.chunk0[t.n + 1] = t.chunk0[t.n] + (int32_t)clip_chunks(g.n, g.dtype);
+        t.chunk0[t.n + 1] = t.chunk0[t.n] + (int32_t)clip_chunks(g.n, g.dtype, per);
         if (++t.n < CLIP_TABLE && i + 1 < n) continue;
         CK(c, launch_clip_table(t, table, c->stream), "gradient table kernel");
         t.at += t.chunk0[t.n];
         t.n = 0;
     }
-    CK(c, launch_clip(table, (int)chunks, c->nsm, clip_sums(c), max_norm, norm, c->stream), "clip kernel");
+    CK(c, launch_clip(table, (int)chunks, per, c->nsm, clip_sums(c), max_norm, norm, c->stream), "clip kernel");
     return HWR_OK;
 }
 
@@ -826,15 +833,17 @@ extern "C" hwr_status hwr_gradients_create(hwr_ops *c, int32_t n, const hwr_grad
     *out = nullptr;
     OK(ready(c));
     int64_t chunks;
-    OK(check_gradients(c, n, grads, &chunks));
+    int per;
+    OK(check_gradients(c, n, grads, &chunks, &per));
     hwr_gradients *l = new (std::nothrow) hwr_gradients;
     ClipChunk *host = new (std::nothrow) ClipChunk[chunks ? chunks : 1];
     hwr_status s = l && host ? HWR_OK : fail(c, HWR_ERR_OOM, "host allocation failed");
     if (s == HWR_OK) s = alloc(c, &l->table, chunks ? chunks : 1);
     if (s == HWR_OK) {
+        l->per = per;
         for (int i = 0; i < n; ++i)
-            for (int64_t k = 0, m = clip_chunks(grads[i].n, grads[i].dtype); k < m; ++k)
-                host[l->chunks++] = clip_chunk(grads[i].in, grads[i].out, grads[i].n, grads[i].dtype, k);
+            for (int64_t k = 0, m = clip_chunks(grads[i].n, grads[i].dtype, per); k < m; ++k)
+                host[l->chunks++] = clip_chunk(grads[i].in, grads[i].out, grads[i].n, grads[i].dtype, per, k);
         cudaError_t e = cudaMemcpyAsync(l->table, host, chunks * sizeof(ClipChunk), cudaMemcpyHostToDevice, c->stream);
         if (e == cudaSuccess) e = cudaStreamSynchronize(c->stream);
         if (e != cudaSuccess) s = cuda_fail(c, e, "gradient table");
@@ -855,7 +864,7 @@ extern "C" hwr_status hwr_gradients_clip(hwr_ops *c, const hwr_gradients *l, flo
     OK(ready(c));
     if (!l) return fail(c, HWR_ERR_INVALID_ARG, "NULL list");
     OK(check_norm(c, max_norm, norm));
-    CK(c, launch_clip(l->table, l->chunks, c->nsm, clip_sums(c), max_norm, norm, c->stream), "clip kernel");
+    CK(c, launch_clip(l->table, l->chunks, l->per, c->nsm, clip_sums(c), max_norm, norm, c->stream), "clip kernel");
     return HWR_OK;
 }
 

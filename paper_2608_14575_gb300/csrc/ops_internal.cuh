@@ -167,28 +167,35 @@ cudaError_t launch_low_few(const LowFew &p, bool f16, cudaStream_t s);
 cudaError_t launch_pad(void *dst, int64_t dst_ld, const void *src, int64_t src_ld, int64_t src_z,
                        int64_t nz, int64_t rows, int cols, int nsm, cudaStream_t s);
 
-constexpr int CLIP_CHUNK_BYTES = 16384;
+// Chunks of `per` 4 KB (a 16-byte access of each of a block's threads): 4 for
+// sets of gradients that fill the GPU so, 1 for small ones, whose time is that of
+// the busiest SM (48 tensors of 2 MB in all: 12.5 us in chunks of 16 KB, 9.8 of
+// 8 KB; 475 MB: 228 and 232 us).
+constexpr int CLIP_UNIT = 4096, CLIP_PER = 4;
+constexpr int64_t CLIP_SMALL = 4 << 20;       // elements of a small set
 struct alignas(16) ClipChunk {
     const void *in;
     void *out;
     int32_t n, dtype;
     int64_t unused;
 };
-inline __host__ __device__ int clip_elems(int dtype) { return CLIP_CHUNK_BYTES / (dtype == HWR_F32 ? 4 : 2); }
-inline __host__ __device__ int64_t clip_chunks(int64_t n, int dtype) { return (n + clip_elems(dtype) - 1) / clip_elems(dtype); }
-inline __host__ __device__ ClipChunk clip_chunk(const void *in, void *out, int64_t n, int dtype, int64_t i) {
+inline __host__ __device__ int clip_elems(int dtype, int per) { return per * CLIP_UNIT / (dtype == HWR_F32 ? 4 : 2); }
+inline __host__ __device__ int64_t clip_chunks(int64_t n, int dtype, int per) {
+    return (n + clip_elems(dtype, per) - 1) / clip_elems(dtype, per);
+}
+inline __host__ __device__ ClipChunk clip_chunk(const void *in, void *out, int64_t n, int dtype, int per, int64_t i) {
     ClipChunk c;
-    const int64_t left = n - i * clip_elems(dtype);
-    c.in = (const char *)in + i * CLIP_CHUNK_BYTES;
-    c.out = (char *)out + i * CLIP_CHUNK_BYTES;
-    c.n = (int32_t)(left < clip_elems(dtype) ? left : clip_elems(dtype));
+    const int64_t left = n - i * clip_elems(dtype, per);
+    c.in = (const char *)in + i * per * CLIP_UNIT;
+    c.out = (char *)out + i * per * CLIP_UNIT;
+    c.n = (int32_t)(left < clip_elems(dtype, per) ? left : clip_elems(dtype, per));
     c.dtype = dtype;
     c.unused = 0;
     return c;
 }
 constexpr int CLIP_TABLE = 256;       // tensors of one launch of the table's kernel
 struct ClipTable {
-    int n, at;                        // tensors; first chunk of them in the table
+    int n, at, per;                   // tensors; first chunk of them in the table; chunks' size
     const void *in[CLIP_TABLE];
     void *out[CLIP_TABLE];
     int64_t count[CLIP_TABLE];
@@ -202,7 +209,7 @@ struct ClipSums {
     uint32_t *count;                  // blocks that have finished (zeroed once, self-resetting)
     float *factor;                    // what the gradients are scaled by
 };
-cudaError_t launch_clip(const ClipChunk *table, int chunks, int nsm, const ClipSums &sums, float max_norm,
+cudaError_t launch_clip(const ClipChunk *table, int chunks, int per, int nsm, const ClipSums &sums, float max_norm,
                         float *norm, cudaStream_t s);
 
 }  // namespace hwr
