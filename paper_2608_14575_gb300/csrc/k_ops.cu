@@ -24,7 +24,7 @@ constexpr int DP_THREADS = 512, DP_WARPS = DP_THREADS / 32;
 constexpr int DP_PER = 8;
 constexpr int DP_ROWS = DP_THREADS * DP_PER;
 constexpr int DP_CLUSTER = 16;   // (more than 8 is the non-portable size)
-constexpr int DP_FEW = 512;      // rows whose places are counted row against row
+constexpr int DP_FEW = 256;      // rows whose places are counted row against row
 
 __device__ __forceinline__ void pdl_begin() {
     asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -371,7 +371,7 @@ k_low_few(const __grid_constant__ LowFew p) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int place = blockIdx.x, r0 = blockIdx.y * LF_RANKS;
     pdl_begin();
-    const int row = p.plan.order[place];
+    const int row = p.by_place ? place : p.plan.order[place];
     if (warp == 0) {
         // the place's group: how many groups end at or before it
         int n = 0;

@@ -325,14 +325,15 @@ struct Rows {
 // Rows that are few are picked by index: they cost no copy, and the weights'
 // bytes bound the product (64 rows x 12 groups, 1024 -> 4096: 42 us picked).
 // More of them are copied by place once.
-constexpr int PICK_ROWS = 256;
+constexpr int PICK_GROUPED = 1024, PICK_SHARED = 256;
 // Their shared product takes narrower tiles: more pairs have a tile of their own,
 // and a tile has fewer pieces to join.
 constexpr int FEW_BN = 128;
-constexpr int64_t LOW_FEW_VALUES = 16 << 20;   // values of the adapters read by a few rows
+constexpr int64_t LOW_FEW_VALUES = 32 << 20;   // values of the adapters read by a few rows
 
 // contracted: a gradient contracts over the rows, which takes the padded plan.
-static Rows plan_rows(Carver &cv, const hwr_rows *r, const void *dy, int64_t dy_ld, bool need_x, bool contracted) {
+static Rows plan_rows(Carver &cv, const hwr_rows *r, const void *dy, int64_t dy_ld, bool need_x, bool contracted,
+                      int pick) {
     Rows s;
     s.plan.rows = s.plan.places = r->rows;
     s.plan.groups = r->groups;
@@ -348,7 +349,7 @@ static Rows plan_rows(Carver &cv, const hwr_rows *r, const void *dy, int64_t dy_
     };
     if (need_x) s.x = operand(r->x, r->x_ld, r->n_in);
     if (dy) s.dy = operand(dy, dy_ld, r->n_out);
-    s.sorted = contracted || r->rows > PICK_ROWS || (need_x && !on16(r->x, r->x_ld, 0, 1)) ||
+    s.sorted = contracted || r->rows > pick || (need_x && !on16(r->x, r->x_ld, 0, 1)) ||
                (dy && !on16(dy, dy_ld, 0, 1));
     if (!s.sorted) return s;
     if (contracted) {
@@ -496,7 +497,7 @@ extern "C" hwr_status hwr_grouped_forward(hwr_ops *c, const hwr_rows *r, void *y
     OK(check_out(c, r, y, y_ld, r->n_out, "y"));
     if (r->rows == 0) return HWR_OK;
     Carver cv;
-    Rows rows = plan_rows(cv, r, nullptr, 0, true, false);
+    Rows rows = plan_rows(cv, r, nullptr, 0, true, false, PICK_GROUPED);
     Operand w = cv.operand(r->w, r->w_ld, r->n_out, r->n_in, r->w_group, r->groups);
     OK(reserve(c, cv.at));
     OK(sort_rows(c, &rows));
@@ -528,7 +529,7 @@ extern "C" hwr_status hwr_grouped_backward(hwr_ops *c, const hwr_rows *r, const 
     }
     if (!dx && !dw) return HWR_OK;
     Carver cv;
-    Rows rows = plan_rows(cv, r, dy, dy_ld, dw != nullptr, dw != nullptr);
+    Rows rows = plan_rows(cv, r, dy, dy_ld, dw != nullptr, dw != nullptr, PICK_GROUPED);
     Operand w;
     if (dx) w = cv.operand(r->w, r->w_ld, r->n_out, r->n_in, r->w_group, r->groups);
     OK(reserve(c, cv.at));
@@ -597,6 +598,7 @@ static hwr_status low_rank_few(hwr_ops *c, const hwr_rows *r, const hwr_adapters
     f.scale = ad->scale;
     f.u = (uint16_t *)const_cast<void *>(u.p);
     f.u_ld = u.ld;
+    f.by_place = rows.sorted;
     f.wide = wide ? (float *)const_cast<void *>(u.p) : nullptr;
     CK(c, launch_low_few(f, r->dtype == HWR_F16, c->stream), "low-rank kernel");
     return HWR_OK;
@@ -641,7 +643,7 @@ extern "C" hwr_status hwr_adapter_forward(hwr_ops *c, const hwr_rows *r, const h
     if (r->rows == 0) return HWR_OK;
     const int K = r->n_in, N = r->n_out, R = ad->rank, G = r->groups;
     Carver cv;
-    Rows rows = plan_rows(cv, r, nullptr, 0, true, false);
+    Rows rows = plan_rows(cv, r, nullptr, 0, true, false, PICK_SHARED);
     Operand w = cv.operand(r->w, r->w_ld, N, K);
     Operand a = cv.operand(ad->a, K, R, K, (int64_t)R * K, G);
     const bool few = !rows.sorted && r->rows <= FEW_ROWS;
@@ -674,7 +676,7 @@ extern "C" hwr_status hwr_adapter_forward(hwr_ops *c, const hwr_rows *r, const h
         return HWR_OK;
     }
     OK(settle(c, &b));
-    if (!rows.sorted && (int64_t)r->rows * R * K <= LOW_FEW_VALUES) {
+    if ((int64_t)r->rows * R * K <= LOW_FEW_VALUES) {
         OK(low_rank_few(c, r, ad, rows, a, u, false));
     } else {
         GroupCall call;
@@ -701,7 +703,7 @@ extern "C" hwr_status hwr_adapter_backward(hwr_ops *c, const hwr_rows *r, const 
     }
     if (!dx && !da && !db) return HWR_OK;
     Carver cv;
-    Rows rows = plan_rows(cv, r, dy, dy_ld, da || db, da || db);
+    Rows rows = plan_rows(cv, r, dy, dy_ld, da || db, da || db, PICK_SHARED);
     Operand w, a, b, u, v;
     if (dx) w = cv.operand(r->w, r->w_ld, N, K);
     if (dx || db) a = cv.operand(ad->a, K, R, K, (int64_t)R * K, G);

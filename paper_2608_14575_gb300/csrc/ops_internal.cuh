@@ -159,6 +159,7 @@ struct LowFew {
     uint16_t *u;
     int64_t u_ld;
     float *wide;                      // or, where set, as fp32 [places][rank] here
+    int by_place;                     // x lies by place already
 };
 cudaError_t launch_low_few(const LowFew &p, bool f16, cudaStream_t s);
 
