@@ -23,10 +23,12 @@
  *   - Rows are row-major with a leading dimension in elements: row t of x
  *     begins at x + t * x_ld.  Weights are [out][in], group g at w + g *
  *     w_group, row n at + n * w_ld.  Any pointer aligned to its element and any
- *     leading dimension >= the row's length is accepted.  Where a pointer is
- *     not on a 16-byte boundary, or a stride is not a whole number of 16-byte
- *     units, the operand is first copied to the workspace with padded rows (an
- *     extra read and write of it, and that much workspace).
+ *     leading dimension >= the row's length is accepted.  A weight that is not
+ *     on a 16-byte boundary, or whose strides are not whole 16-byte units, is
+ *     first copied to the workspace with padded rows (an extra read and write of
+ *     it, and that much workspace).  The rows of x and dy are copied there by
+ *     group in any case, unless they are few (1,024; 256 with adapters) and so
+ *     aligned.
  *   - Sums run in fp32 on the tensor cores; each output is rounded once.
  *   - Results do not depend on timing: the same call gives the same bits.
  *   - The workspace grows (cudaMalloc) when a call needs more than any call

@@ -27,7 +27,7 @@
 // fp32 partials; the last to arrive adds them in the order of the contraction,
 // so the result does not depend on who that is.
 #include "ops_internal.cuh"
-#include "umma.cuh"
+#include "umma_pair.cuh"
 
 #include <stddef.h>
 

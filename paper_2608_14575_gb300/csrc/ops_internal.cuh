@@ -1,6 +1,7 @@
 // Internal interface between the host code of the operators that follow a
 // routing decision (ops_api.cu) and their kernels (k_group.cu: products on the
-// tensor cores; k_ops.cu: dispatch, gradient clipping, padding).
+// tensor cores; k_few.cu: of a few rows; k_ops.cu: dispatch, row copies, low-rank
+// products of a few rows, padding, gradient clipping).
 #pragma once
 
 #include <cuda.h>
@@ -26,7 +27,7 @@ enum : int {
     GP_GROUPED = 0,    // B side: out^T tile = W[g] tile (A) x rows (B): a ragged group costs
                        // whole 16s of rows
     GP_ROWS = 1,       // A side: out tile = rows x W tile
-    GP_WGRAD = 2,      // contraction: both sides are columns of gathered rows
+    GP_WGRAD = 2,      // contraction: both sides are columns of rows by place
 };
 
 // What a tile's values become.
