@@ -59,8 +59,9 @@ hwr_status hwr_ops_synchronize(hwr_ops *ops);      /* reports asynchronous failu
 const char *hwr_ops_last_error(const hwr_ops *ops); /* NULL: of hwr_ops_create */
 /* Order the context's later work after what is queued on another stream now, and
  * another stream's later work after what the context has queued (for calls whose
- * arrays belong to that stream; 1 is the legacy default stream).
- * Errors: INVALID_ARG, STATE, CUDA. */
+ * arrays belong to that stream; 1 is the legacy default stream).  A context on
+ * the default stream cannot follow a stream that is being captured (UNSUPPORTED).
+ * Errors: INVALID_ARG, UNSUPPORTED, STATE, CUDA. */
 hwr_status hwr_ops_after(hwr_ops *ops, void *cuda_stream);
 hwr_status hwr_ops_before(hwr_ops *ops, void *cuda_stream);
 /* Make the workspace at least `bytes` large.  Errors: INVALID_ARG, STATE, OOM, CUDA. */

@@ -198,6 +198,12 @@ extern "C" hwr_status hwr_ops_after(hwr_ops *c, void *stream) {
     if (!c) return HWR_ERR_INVALID_ARG;
     OK(ready(c));
     if (!stream) return fail(c, HWR_ERR_INVALID_ARG, "NULL stream");
+    if (c->stream == cudaStreamLegacy) {
+        cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
+        CK(c, cudaStreamIsCapturing((cudaStream_t)stream, &capture), "capture status");
+        if (capture != cudaStreamCaptureStatusNone)
+            return fail(c, HWR_ERR_UNSUPPORTED, "a context on the default stream cannot take part in a stream capture");
+    }
     return order_streams(c, (cudaStream_t)stream, c->stream);
 }
 

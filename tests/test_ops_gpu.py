@@ -47,7 +47,8 @@ def choices(T, G, kind, seed=0):
 
 # ---- dispatch ---------------------------------------------------------------
 
-@pytest.mark.parametrize("T", [0, 1, 31, 32, 33, 255, 8191, 8192, 8193, 50_001, 1_300_003])
+@pytest.mark.parametrize("T", [0, 1, 31, 32, 33, 255, 256, 257, 4096, 4097, 8191, 8192, 8193, 50_001, 65_536,
+                               65_537, 200_001, 1_300_003])
 @pytest.mark.parametrize("G", [1, 2, 12, 64, 1023, 1024])
 @pytest.mark.parametrize("kind", ["any", "none", "one", "holes", "outside"])
 def test_dispatch(ops, T, G, kind):
@@ -69,6 +70,8 @@ SHAPES = [   # T, G, K, N
     (128, 1, 128, 256), (129, 1, 192, 264), (300, 7, 1000, 520), (1000, 3, 128, 1024),
     (2500, 40, 256, 384), (5000, 4, 512, 776), (700, 1000, 64, 48),
     (200, 3, 1, 1), (77, 4, 33, 5), (260, 3, 101, 257), (64, 2, 4104, 40),
+    # tiles cut along long contractions: few rows and many
+    (100, 3, 4096, 512), (1000, 2, 4096, 256), (1025, 2, 4096, 256), (3000, 3, 2048, 512), (2100, 30, 328, 3000),
 ]
 
 
@@ -204,6 +207,9 @@ ADAPTERS = [   # T, G, K, N, rank
     (128, 5, 128, 256, 64), (129, 200, 64, 320, 24), (500, 3, 264, 200, 100), (1500, 4, 512, 1032, 32),
     (260, 2, 128, 64, 256), (3000, 12, 256, 512, 128), (90, 4, 33, 57, 5), (50, 2, 1, 3, 1),
     (300, 1000, 128, 64, 16),
+    # picked rows on the tensor cores, cut tiles that share out their adapters
+    (200, 3, 2048, 64, 128), (64, 40, 2048, 1024, 48), (250, 60, 1024, 2048, 16), (100, 100, 4096, 512, 8),
+    (600, 50, 2048, 1024, 40), (17, 9, 1024, 640, 24), (16, 9, 1000, 648, 24), (400, 6, 2048, 2048, 16),
 ]
 
 
@@ -362,6 +368,49 @@ def test_other_streams(ops):
     assert torch.equal(y, R.grouped_forward(x, w, c)[0].to(BF))
     side_ops.synchronize()
     side_ops.close()
+
+
+def test_graph_capture(ops):
+    """After a call of the same sizes nothing is allocated: a step can be captured and
+    replayed on new values, by a context on the capturing stream or another one.  (The
+    legacy default stream takes no part in a capture: its context says so, and stays usable.)"""
+    T, G, K, N, r = 48, 6, 256, 384, 16
+    c, x = choices(T, G, "any"), ints(T, K)
+    w, b = ints(G, N, K), ints(G, K, r, lo=-1, hi=1)
+    a, sh, s = ints(G, r, N, lo=-1, hi=1), ints(K, N, lo=-1, hi=1), torch.ones(G, device="cuda")
+    torch.cuda.synchronize()
+
+    def step(o):
+        plan = o.dispatch(c, G)
+        y = o.grouped_forward(x, w, plan)
+        g = y.clone()
+        return y, o.adapter_forward(y, sh, a, b, s, plan), o.clip_gradients([g], 1e9), g
+    side, other = torch.cuda.Stream(), torch.cuda.Stream()
+    for on in (side, other):
+        with torch.cuda.stream(on):
+            own = H.Operators()
+        with torch.cuda.stream(side):
+            step(own)
+            torch.cuda.synchronize()
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph, stream=side):
+                held = step(own)
+            for k in range(3):
+                x.copy_(ints(T, K, seed=k))
+                c.copy_(choices(T, G, "holes", seed=k))
+                graph.replay()
+                now = step(own)
+                for p, q in zip(held, now):
+                    assert torch.equal(p, q)
+                assert torch.equal(held[0], R.grouped_forward(x, w, c)[0].to(BF))
+        torch.cuda.synchronize()
+        own.close()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        with pytest.raises(H.HwrError) as e:
+            ops.dispatch(c, G)
+        assert e.value.status == 7
+    assert ops.dispatch(c, G).offsets.shape == (G + 1,)
 
 
 def test_no_rows(ops):
