@@ -404,6 +404,45 @@ __device__ __forceinline__ void store_row(uint16_t *dst, const float (&v)[32], i
     }
 }
 
+// A warp's 32 staged rows of 32 values to where they belong, V values an access
+// (what the result's rows are aligned to): 32 / V lanes write 64 bytes of a row.
+// to(j): where row j's values go (null: nowhere); left: how many of them count.
+template <int V, class To>
+__device__ __forceinline__ void flush(const uint8_t *stage, int left, To to) {
+    constexpr int LANES = 32 / V, STEPS = 32 / V;
+    const int lane = threadIdx.x & 31, e = lane % LANES * V;
+#pragma unroll
+    for (int i0 = 0; i0 < STEPS; i0 += 4) {
+        uint16_t *dst[4];
+        uint4 d[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int j = (i0 + i) * V + lane / LANES;
+            const uint8_t *src = stage + staged_at(j, e >> 3) + (e & 7) * 2;
+            if (V == 8) d[i] = *(const uint4 *)src;
+            if (V == 4) *(uint2 *)&d[i] = *(const uint2 *)src;
+            if (V == 2) d[i].x = *(const uint32_t *)src;
+            if (V == 1) d[i].x = *(const uint16_t *)src;
+            dst[i] = to(j);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (!dst[i]) continue;
+            uint16_t *o = dst[i] + e;
+            if (e + V <= left) {
+                if (V == 8) *(uint4 *)o = d[i];
+                if (V == 4) *(uint2 *)o = *(const uint2 *)&d[i];
+                if (V == 2) *(uint32_t *)o = d[i].x;
+                if (V == 1) *o = (uint16_t)d[i].x;
+            } else if (V > 1) {
+                const uint16_t *src =
+                    (const uint16_t *)(stage + staged_at((i0 + i) * V + lane / LANES, e >> 3) + (e & 7) * 2);
+                for (int k = 0; e + k < left; ++k) o[k] = src[k];
+            }
+        }
+    }
+}
+
 // Index of the row at a place of the order, -1 where there is none.
 __device__ __forceinline__ int row_at(const GroupProduct &p, int place) {
     const int r = p.plan.order[place];
@@ -799,9 +838,10 @@ k_group(const __grid_constant__ Launch<KIND >= K_LOW ? 2 : 1> launch) {
                 const int r = row_at(p, (int)pos);
                 if (r < 0) continue;
                 uint16_t *dst = out0 + (int64_t)r * p.ld;
-                if (p.vec)
+                const bool wide = p.vec == 8;
+                if (wide)
                     for (int j = lane * 8; j + 8 <= p.n; j += 256) *(uint4 *)(dst + j) = make_uint4(0, 0, 0, 0);
-                for (int j = (p.vec ? p.n & ~7 : 0) + lane; j < p.n; j += 32) dst[j] = 0;
+                for (int j = (wide ? p.n & ~7 : 0) + lane; j < p.n; j += 32) dst[j] = 0;
             }
         }
         uint32_t lt = 0;
@@ -897,12 +937,33 @@ k_group(const __grid_constant__ Launch<KIND >= K_LOW ? 2 : 1> launch) {
                 return (low ? (i >> 1) * 2 * halves + half * 2 + (i & 1) : i * halves + half) * 32;
             };
             // staged rows go out 64 bytes each, by 4 lanes: this lane's 4 rows
-            const bool staged = !low && !pack && p.vec && !dealt;
+            const bool staged = !low && !pack && p.vec == 8 && !dealt;
             const int piece = (lane & 3) * 8;
             uint16_t *base[4];
 #pragma unroll
             for (int q = 0; q < 4; ++q)
                 base[q] = staged && !grouped ? out_row(quad * 32 + q * 8 + (lane >> 2)) : nullptr;
+            // Rows that are less aligned, and those of the low-rank gradients, with
+            // narrower accesses that still run along a row: against each lane writing
+            // its own, 2 bytes at a time, the gradients of 4,096 rows in 16 groups of
+            // 1,023 x 1,025 take 140 us (242), those of 43 adapters of rank 128 346
+            // (385).  The grouped products' lanes lie along the row anyhow: 66 us so,
+            // 76 through the stage
+            auto send = [&](int left, auto to) {
+                __syncwarp();
+                if (low && p.vec == 8) flush<8>(stage, left, to);
+                else if (p.vec >= 4) flush<4>(stage, left, to);
+                else if (p.vec == 2) flush<2>(stage, left, to);
+                else flush<1>(stage, left, to);
+                __syncwarp();
+            };
+            auto stage_row = [&](const float (&v)[32]) {     // the lane's own row
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    *(uint4 *)(stage + staged_at(lane, j)) =
+                        make_uint4(pack2<F16>(v[8 * j], v[8 * j + 1]), pack2<F16>(v[8 * j + 2], v[8 * j + 3]),
+                                   pack2<F16>(v[8 * j + 4], v[8 * j + 5]), pack2<F16>(v[8 * j + 6], v[8 * j + 7]));
+            };
             float prev[32];
             uint32_t u[32];
             const bool tm = !cut && write;
@@ -953,11 +1014,7 @@ k_group(const __grid_constant__ Launch<KIND >= K_LOW ? 2 : 1> launch) {
                         for (int j = 0; j < 32; ++j)
                             *(uint16_t *)(stage + staged_at(j, lane >> 3) + (lane & 7) * 2) = (uint16_t)pack2<F16>(v[j], 0.f);
                     } else {
-#pragma unroll
-                        for (int j = 0; j < 4; ++j)
-                            *(uint4 *)(stage + staged_at(lane, j)) =
-                                make_uint4(pack2<F16>(v[8 * j], v[8 * j + 1]), pack2<F16>(v[8 * j + 2], v[8 * j + 3]),
-                                           pack2<F16>(v[8 * j + 4], v[8 * j + 5]), pack2<F16>(v[8 * j + 6], v[8 * j + 7]));
+                        stage_row(v);
                     }
                     __syncwarp();
                     const int n = grouped ? w.ot * GP_TILE + rank * 128 + quad * 32 + piece : w.ot * p.bn + c + piece;
@@ -996,23 +1053,27 @@ k_group(const __grid_constant__ Launch<KIND >= K_LOW ? 2 : 1> launch) {
                 } else if (low) {
                     // blocks of 64 columns: the products with the high terms of 32
                     // ranks, then those with the low terms
-                    const int r0 = (w.ot * p.bn + c) >> 6 << 5, left = p.rank_out - r0;
-                    if (c & 32) {
-                        uint16_t *out = out0 + w.g * p.gstride;
-                        const int64_t m = w.xt * GP_TILE + rank * 128 + row;
-#pragma unroll
-                        for (int j = 0; j < 32; ++j) v[j] += prev[j];
-                        if (mine && left > 0) {
-                            if (p.out_kind == GP_OUT_LOW)
-                                store_row<F16>(out + m * p.ld + r0, v, min(32, left), p.vec);
-                            else
-#pragma unroll
-                                for (int j = 0; j < 32; ++j)
-                                    if (j < left) out[(r0 + j) * p.ld + m] = (uint16_t)pack2<F16>(v[j], 0.f);
-                        }
-                    } else {
+                    if (!(c & 32)) {
 #pragma unroll
                         for (int j = 0; j < 32; ++j) prev[j] = v[j];
+                        continue;
+                    }
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) v[j] += prev[j];
+                    uint16_t *out = out0 + w.g * p.gstride;
+                    const int r0 = (w.ot * p.bn + c) >> 6 << 5, m = w.xt * GP_TILE + rank * 128 + quad * 32;
+                    if (p.out_kind == GP_OUT_LOW) {
+                        stage_row(v);
+                        send(p.rank_out - r0, [&](int j) -> uint16_t * {
+                            return m + j < p.m ? out + (int64_t)(m + j) * p.ld + r0 : nullptr;
+                        });
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 32; ++j)
+                            *(uint16_t *)(stage + staged_at(j, lane >> 3) + (lane & 7) * 2) = (uint16_t)pack2<F16>(v[j], 0.f);
+                        send(p.m - m, [&](int j) -> uint16_t * {
+                            return r0 + j < p.rank_out ? out + (int64_t)(r0 + j) * p.ld + m : nullptr;
+                        });
                     }
                 } else if (pack) {
                     // 32 ranks of an inner product: value = high + low term, to about
@@ -1030,9 +1091,15 @@ k_group(const __grid_constant__ Launch<KIND >= K_LOW ? 2 : 1> launch) {
                         store_row<F16>(dst, v, 32, true);
                         store_row<F16>(dst + 32, prev, 32, true);
                     }
+                } else if (!dealt) {
+                    stage_row(v);
+                    send(cols - c, [&](int j) -> uint16_t * {
+                        uint16_t *to = out_row(quad * 32 + j);
+                        return to ? to + w.ot * p.bn + c : nullptr;
+                    });
                 } else {
                     uint16_t *dst = out_row(r);
-                    if (dst) store_row<F16>(dst + w.ot * p.bn + c, v, min(32, cols - c), p.vec);
+                    if (dst) store_row<F16>(dst + w.ot * p.bn + c, v, min(32, cols - c), p.vec == 8);
                 }
             }
             if (held) release();                // (no chunk was this warp's)

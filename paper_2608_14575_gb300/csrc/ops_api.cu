@@ -316,8 +316,12 @@ static hwr_status encode(hwr_ops *c, CUtensorMap *m, bool f16, const Operand &o,
     return HWR_OK;
 }
 
-// 16-byte stores where the rows of the result allow them.
-static int vec_ok(const void *p, int64_t ld, int64_t z) { return on16(p, ld, z, 2); }
+// Values of the widest store that the rows of the result are aligned to.
+static int vec_of(const void *p, int64_t ld, int64_t z) {
+    for (int v = 8; v > 1; v /= 2)
+        if ((uintptr_t)p % (2 * v) == 0 && ld % v == 0 && z % v == 0) return v;
+    return 1;
+}
 
 // What the products of a call share: the plan and the rows of its inputs, by
 // place (copied to the workspace) or where the caller has them.
@@ -513,7 +517,7 @@ extern "C" hwr_status hwr_grouped_forward(hwr_ops *c, const hwr_rows *r, void *y
     p.out_kind = GP_OUT_ROWS;
     p.out = y;
     p.ld = y_ld;
-    p.vec = vec_ok(y, y_ld, 0);
+    p.vec = vec_of(y, y_ld, 0);
     GroupCall call;
     OK(rows_product(c, p, rows.x, w, false, r->n_out, nullptr, nullptr, &call));
     return launch(c, &call);
@@ -548,7 +552,7 @@ extern "C" hwr_status hwr_grouped_backward(hwr_ops *c, const hwr_rows *r, const 
         p.out_kind = GP_OUT_ROWS;
         p.out = dx;
         p.ld = dx_ld;
-        p.vec = vec_ok(dx, dx_ld, 0);
+        p.vec = vec_of(dx, dx_ld, 0);
         OK(rows_product(c, p, rows.dy, w, true, r->n_in, nullptr, nullptr, &call));
         OK(launch(c, &call));
     }
@@ -558,7 +562,7 @@ extern "C" hwr_status hwr_grouped_backward(hwr_ops *c, const hwr_rows *r, const 
         p.out = dw;
         p.ld = r->w_ld;
         p.gstride = r->groups > 1 ? r->w_group : 0;
-        p.vec = vec_ok(dw, r->w_ld, p.gstride);
+        p.vec = vec_of(dw, r->w_ld, p.gstride);
         OK(grad_product(c, p, rows.dy, rows.x, &call));
         OK(launch(c, &call));
     }
@@ -582,7 +586,6 @@ static hwr_status low_rank(hwr_ops *c, const hwr_rows *r, const hwr_adapters *ad
     p.out_kind = GP_OUT_PACK;
     p.out = const_cast<void *>(u.p);
     p.ld = u.ld;
-    p.vec = 1;
     p.scale = ad->scale;
     return rows_product(c, p, x, m, m_mn, ad->rank, nullptr, nullptr, call);
 }
@@ -633,7 +636,7 @@ static hwr_status shared_product(hwr_ops *c, const hwr_rows *r, const hwr_adapte
     p.out_kind = GP_OUT_ROWS;
     p.out = out;
     p.ld = ld;
-    p.vec = vec_ok(out, ld, 0);
+    p.vec = vec_of(out, ld, 0);
     OK(rows_product(c, p, x, w, w_mn, n, &u, &eb, &call));
     return launch(c, &call);
 }
@@ -744,6 +747,7 @@ extern "C" hwr_status hwr_adapter_backward(hwr_ops *c, const hwr_rows *r, const 
         p.ld = K;
         p.gstride = (int64_t)R * K;
         p.rank_out = R;
+        p.vec = vec_of(da, K, p.gstride);
         OK(grad_product(c, p, rows.x, v, &calls[n++]));
     }
     if (db) {
@@ -753,7 +757,7 @@ extern "C" hwr_status hwr_adapter_backward(hwr_ops *c, const hwr_rows *r, const 
         p.ld = R;
         p.gstride = (int64_t)N * R;
         p.rank_out = R;
-        p.vec = vec_ok(db, R, p.gstride);
+        p.vec = vec_of(db, R, p.gstride);
         OK(grad_product(c, p, rows.dy, u, &calls[n++]));
     }
     return n ? launch(c, calls, n, 1 - by_n) : HWR_OK;

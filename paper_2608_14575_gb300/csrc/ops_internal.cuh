@@ -73,7 +73,7 @@ struct GroupProduct {
     int ext_pack = 1;                 // groups in one of its stages
     // output
     int out_kind = 0;
-    int vec = 0;                      // 16-byte stores
+    int vec = 1;                      // values of an aligned store: 8, 4, 2 or 1
     void *out = nullptr;
     int64_t ld = 0, gstride = 0;
     int rank_out = 0;                 // GP_OUT_LOW*: ranks written

@@ -328,6 +328,31 @@ def test_adapter_strides(ops, pad, shift):
         assert torch.equal(g, want.to(BF))
 
 
+@pytest.mark.parametrize("K,N,r", [(72, 264, 8), (68, 300, 12), (66, 302, 6), (65, 301, 7), (300, 68, 36), (301, 65, 33)])
+@pytest.mark.parametrize("T", [7, 100, 1500])
+def test_results_of_each_alignment(ops, K, N, r, T):
+    """Rows of results that are aligned to 16, 8, 4 and 2 bytes; what lies between
+    the rows of a strided result stays."""
+    G = 5
+    c = choices(T, G, "holes")
+    x, w, a, b, gw = (ints(*s, lo=-1, hi=1, seed=i) for i, s in
+                      enumerate(((T, K), (N, K), (G, r, K), (G, N, r), (G, N, K))))
+    dy, s = ints(T, N, lo=-1, hi=1, seed=9), torch.ones(G, device="cuda")
+    plan = ops.dispatch(c, G)
+    for g, (want, _) in zip(ops.grouped_backward(dy, x, gw, plan), R.grouped_backward(dy, x, gw, c)):
+        assert torch.equal(g, want.to(BF))
+    for g, (want, _) in zip(ops.adapter_backward(dy, x, w, a, b, s, plan),
+                            R.adapter_backward(dy, x, w, a, b, s, c)):
+        assert torch.equal(g, want.to(BF))
+    for pad in (0, 1, 2, 4, 8):
+        buf = torch.full((T, N + pad), 7.0, device="cuda", dtype=BF)
+        ops.adapter_forward(x, w, a, b, s, plan, out=buf[:, :N])
+        assert torch.equal(buf[:, :N], R.adapter_forward(x, w, a, b, s, c)[0].to(BF)) and (buf[:, N:] == 7).all()
+        buf = torch.full((T, N + pad), 7.0, device="cuda", dtype=BF)
+        ops.grouped_forward(x, gw, plan, out=buf[:, :N])
+        assert torch.equal(buf[:, :N], R.grouped_forward(x, gw, c)[0].to(BF)) and (buf[:, N:] == 7).all()
+
+
 def test_same_bits_again(ops):
     """Cut tiles are joined in a fixed order: the same call gives the same bits."""
     T, G, K, N, r = 700, 5, 1024, 1040, 16
