@@ -48,7 +48,12 @@ constexpr int A_BYTES = 128 * GP_BK * 2;
 constexpr int MAX_STAGES = 24;
 constexpr int SMEM_MAX = 227 * 1024;
 constexpr int MIN_PIECE = 6 * GP_BK;   // columns of the smallest piece of a cut tile
-constexpr int JOIN_COST = 8 * GP_BK;   // columns that joining the pieces of tiles costs (about 4 us)
+// Joining a tile's pieces, in blocks of 64 columns of the contraction (about 0.3 us
+// each): so many and, by its columns, up to 36 more.  From 110 shapes with all last
+// tiles cut and with none: they break even at 22 to 25 blocks saved for tiles of a
+// few columns, 35 for 70, 45 to 60 for 200 to 256.  (256 rows through 4,096 x 1,024:
+// 17 us whole, 37 cut; through 8,192 columns 52 whole, 44 cut.)
+constexpr int JOIN_FIXED = 22, JOIN_256 = 36;
 constexpr int BAND = 8;            // row tiles (32: 666 us for 8,192^3, 8: 635 us)
 constexpr int WRITE_COST = 4;      // iterations that writing a gradient's tile counts for
 
@@ -207,7 +212,7 @@ struct Walk {
     int64_t pos, end;         // of this pair's piece of it, what is left
 
     __device__ Walk(const GroupProduct &p_, const Tables &t_) : p(p_), t(t_) {
-        const bool grad = p.mode == GP_WGRAD;
+        const bool grad = p.mode == GP_WGRAD, shared = p.rank > 0;
         const int per = p.mtiles * p.ntiles, tiles = grad ? t.ng * per : t.tile0[t.ng];
         me = next_tile = (blockIdx.x >> 1) - p.pair0;
         pairs = p.pairs;
@@ -222,21 +227,33 @@ struct Walk {
         } else {
             rest = (int64_t)(tiles - dp) * kiters;
         }
-        // Cut only where evening out the last rounds saves more than joining costs:
-        // whole rounds of the average tile against the line's even share.
         const int last = tiles - dp, rounds = (last + pairs - 1) / pairs;
-        if ((rounds * pairs - last) * rest <= (int64_t)last * pairs * (JOIN_COST / deep)) {
+        const int64_t most = max(div_small(rest, max(1, MIN_PIECE / deep)), (int64_t)last);
+        cutters = most < 1 ? 1 : most < pairs ? (int)most : pairs;
+        // Cut only where evening out the last rounds saves more than joining costs:
+        // whole rounds of the average tile against its share of the line.
+        const int64_t work = rest * p.kk + (shared && tiles ? mul_div(ext_work(), last, tiles) : 0);
+        if ((rounds * cutters - last) * work <= (int64_t)last * cutters * join_cost(tiles)) {
             dp = tiles;
             rest = 0;
+            cutters = 1;
         }
-        const int64_t most = max(div_small(rest, max(1, MIN_PIECE / deep)), (int64_t)(tiles - dp));
-        cutters = most < 1 ? 1 : most < pairs ? (int)most : pairs;
         pos = end = 0;
         if (me < cutters) {
             pos = mul_div(rest, me, cutters);
             end = mul_div(rest, me + 1, cutters);
         }
     }
+    // What joining the pieces of a tile takes, in blocks of 64 columns: writing,
+    // arriving and reading by the columns of a tile.
+    __device__ int join_cost(int tiles) const {
+        int cols = p.bn;
+        if (p.mode == GP_GROUPED) cols = (int)min(mul_div(t.offs[t.ng], p.ntiles, max(1, tiles)), (int64_t)GP_TILE);
+        else if (p.mode == GP_ROWS && p.shared) cols = p.bn * min(t.offs[1], 128) >> 7;
+        return JOIN_FIXED + (cols * JOIN_256 >> 8);
+    }
+    // The extension's steps in all of a shared product's tiles, 3/4 of a block each.
+    __device__ int64_t ext_work() const { return (int64_t)t.nseg * ext_steps(p) * p.ntiles * 3 / 4; }
     __device__ bool next(Work &w) {
         const bool grad = p.mode == GP_WGRAD;
         w.e0 = 0;
