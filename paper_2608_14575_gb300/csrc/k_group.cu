@@ -49,11 +49,11 @@ constexpr int MAX_STAGES = 24;
 constexpr int SMEM_MAX = 227 * 1024;
 constexpr int MIN_PIECE = 6 * GP_BK;   // columns of the smallest piece of a cut tile
 // Joining a tile's pieces, in blocks of 64 columns of the contraction (about 0.3 us
-// each): so many and, by its columns, up to 36 more.  From 110 shapes with all last
-// tiles cut and with none: they break even at 22 to 25 blocks saved for tiles of a
-// few columns, 35 for 70, 45 to 60 for 200 to 256.  (256 rows through 4,096 x 1,024:
-// 17 us whole, 37 cut; through 8,192 columns 52 whole, 44 cut.)
-constexpr int JOIN_FIXED = 22, JOIN_256 = 36;
+// each): leaving, arriving and the last fences (less for the inner products), and
+// what the last to arrive reads, for each piece and 64 columns of it, with eight
+// warps or four.  From 110 shapes with all last tiles cut and with none.  (256 rows
+// through 4,096 x 1,024: 17 us whole, 37 cut; through 8,192 columns 52 whole, 44 cut.)
+constexpr float JOIN_FIXED = 20.f, JOIN_LOW = 8.f, JOIN_PIECE_8 = 1.8f, JOIN_PIECE_4 = 2.7f;
 constexpr int BAND = 8;            // row tiles (32: 666 us for 8,192^3, 8: 635 us)
 constexpr int WRITE_COST = 4;      // iterations that writing a gradient's tile counts for
 
@@ -228,12 +228,25 @@ struct Walk {
             rest = (int64_t)(tiles - dp) * kiters;
         }
         const int last = tiles - dp, rounds = (last + pairs - 1) / pairs;
-        const int64_t most = max(div_small(rest, max(1, MIN_PIECE / deep)), (int64_t)last);
-        cutters = most < 1 ? 1 : most < pairs ? (int)most : pairs;
         // Cut only where evening out the last rounds saves more than joining costs:
         // whole rounds of the average tile against its share of the line.
-        const int64_t work = rest * p.kk + (shared && tiles ? mul_div(ext_work(), last, tiles) : 0);
-        if ((rounds * cutters - last) * work <= (int64_t)last * cutters * join_cost(tiles)) {
+        const float work = (float)rest * p.kk + (shared && tiles ? __fdividef((float)ext_work() * last, tiles) : 0.f);
+        const float fixed = p.mode == GP_ROWS && !p.shared ? JOIN_LOW : JOIN_FIXED;
+        bool cut = work * rounds > fixed * last;
+        cutters = 1;
+        if (cut) {
+            // Pieces of a tile that take the least time, its blocks / pieces + what a
+            // piece costs the join * pieces; whole pieces of each tile where the pairs
+            // suffice for two and more (a pair's piece of two tiles is joined twice).
+            const float piece = (p.sorted ? JOIN_PIECE_8 : JOIN_PIECE_4) / 64 * join_cols(tiles);
+            const float tile = __fdividef(work, last), best = max(1.f, sqrtf(__fdividef(tile, piece)));
+            const int most = (int)min((int64_t)pairs, max(div_small(rest, max(1, MIN_PIECE / deep)), (int64_t)last));
+            cutters = max(1, (int)min((float)most, best * last));
+            cutters = cutters >= 2 * last ? cutters / last * last : max(1, most);
+            const float pieces = max(2.f, __fdividef(cutters, last));
+            cut = tile * rounds - __fdividef(work, cutters) > fixed + piece * (pieces + 1.f);
+        }
+        if (!cut) {
             dp = tiles;
             rest = 0;
             cutters = 1;
@@ -244,16 +257,13 @@ struct Walk {
             end = mul_div(rest, me + 1, cutters);
         }
     }
-    // What joining the pieces of a tile takes, in blocks of 64 columns: writing,
-    // arriving and reading by the columns of a tile.
-    __device__ int join_cost(int tiles) const {
-        int cols = p.bn;
-        if (p.mode == GP_GROUPED) cols = (int)min(mul_div(t.offs[t.ng], p.ntiles, max(1, tiles)), (int64_t)GP_TILE);
-        else if (p.mode == GP_ROWS && p.shared) cols = p.bn * min(t.offs[1], 128) >> 7;
-        return JOIN_FIXED + (cols * JOIN_256 >> 8);
+    // Columns of a tile's partials (of a few rows as many as take the same time).
+    __device__ float join_cols(int tiles) const {
+        if (p.mode == GP_GROUPED) return max(1.f, min((float)GP_TILE, __fdividef((float)t.offs[t.ng] * p.ntiles, max(1, tiles))));
+        return p.mode == GP_ROWS && p.shared ? p.bn * max(1, min(t.offs[1], 128)) * (1.f / 128) : p.bn;
     }
-    // The extension's steps in all of a shared product's tiles, 3/4 of a block each.
-    __device__ int64_t ext_work() const { return (int64_t)t.nseg * ext_steps(p) * p.ntiles * 3 / 4; }
+    // The extension's steps in all of a shared product's tiles, about a block each.
+    __device__ int64_t ext_work() const { return (int64_t)t.nseg * ext_steps(p) * p.ntiles; }
     __device__ bool next(Work &w) {
         const bool grad = p.mode == GP_WGRAD;
         w.e0 = 0;

@@ -410,10 +410,13 @@ k_low_few(const __grid_constant__ LowFew p) {
         if (lane == 0) part[warp][r] = acc[r];
     }
     __syncthreads();
-    if (threadIdx.x < LF_RANKS) {
+    // (the last block of a row writes the zeros up to whole 64s of ranks too)
+    const int end = blockIdx.y + 1 < gridDim.y || p.wide ? LF_RANKS : (p.rank + 63) / 64 * 64 - r0;
+    if (threadIdx.x < end) {
         const int r = r0 + threadIdx.x;
         float v = 0.f;
-        for (int w = 0; w < LF_WARPS; ++w) v += part[w][threadIdx.x];
+        if (threadIdx.x < LF_RANKS)
+            for (int w = 0; w < LF_WARPS; ++w) v += part[w][threadIdx.x];
         v = r < p.rank && g < p.plan.groups ? v * p.scale[g] : 0.f;
         if (p.wide) {
             if (r < p.rank) p.wide[(int64_t)place * p.rank + r] = v;
@@ -758,8 +761,7 @@ cudaError_t launch_sort_rows(const GroupPlan &plan, const SortRows &m, int place
 cudaError_t launch_low_few(const LowFew &p, bool f16, cudaStream_t s) {
     cudaLaunchAttribute at[1];
     cudaLaunchConfig_t cfg = relaxed(p.plan.rows, LF_THREADS, 0, s, at);
-    cfg.gridDim.y = p.wide ? (unsigned)((p.rank + LF_RANKS - 1) / LF_RANKS)
-                           : (unsigned)((p.rank + 2 * GP_RC - 1) / (2 * GP_RC) * (2 * GP_RC / LF_RANKS));
+    cfg.gridDim.y = (unsigned)((p.rank + LF_RANKS - 1) / LF_RANKS);
     return f16 ? cudaLaunchKernelEx(&cfg, k_low_few<true>, p) : cudaLaunchKernelEx(&cfg, k_low_few<false>, p);
 }
 

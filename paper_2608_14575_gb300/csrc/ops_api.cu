@@ -339,7 +339,11 @@ constexpr int PICK_GROUPED = 1024, PICK_SHARED = 256;
 // Their shared product takes narrower tiles: more pairs have a tile of their own,
 // and a tile has fewer pieces to join.
 constexpr int FEW_BN = 128;
-constexpr int64_t LOW_FEW_VALUES = 32 << 20;   // values of the adapters read by a few rows
+// Inner products without tensor cores: values of the adapters that are read, and
+// blocks (a row and four ranks each).  With either twice as many the tensor cores
+// are faster, at 8 to 128 ranks and 256 to 4,096 columns (4,096 rows of rank 8 and
+// 1,024 columns: 41 us against 36; 2,048 rows: 31 against 35).
+constexpr int64_t LOW_FEW_VALUES = 64 << 20, LOW_FEW_BLOCKS = 4096;
 
 // contracted: a gradient contracts over the rows, which takes the padded plan.
 static Rows plan_rows(Carver &cv, const hwr_rows *r, const void *dy, int64_t dy_ld, bool need_x, bool contracted,
@@ -685,7 +689,7 @@ extern "C" hwr_status hwr_adapter_forward(hwr_ops *c, const hwr_rows *r, const h
         return HWR_OK;
     }
     OK(settle(c, &b));
-    if ((int64_t)r->rows * R * K <= LOW_FEW_VALUES) {
+    if ((int64_t)r->rows * R * K <= LOW_FEW_VALUES && (int64_t)r->rows * ((R + 3) / 4) <= LOW_FEW_BLOCKS) {
         OK(low_rank_few(c, r, ad, rows, a, u, false));
     } else {
         GroupCall call;
