@@ -123,6 +123,13 @@ __host__ __device__ inline int table_bytes(const GroupProduct &p) {
     return (int)sizeof(Tables) + (p.mode == GP_WGRAD ? g * 12 : p.shared ? g * 8 + 16 : g * 8);
 }
 
+// atomicAdd that orders, across the GPU, what came before it and what comes after.
+__device__ __forceinline__ uint32_t add_acq_rel(uint32_t *p, uint32_t v) {
+    uint32_t old;
+    asm volatile("atom.add.acq_rel.gpu.global.u32 %0, [%1], %2;" : "=r"(old) : "l"(p), "r"(v) : "memory");
+    return old;
+}
+
 // Bounded wait for MMAs that were issued, without flags.
 __device__ __forceinline__ void drain(uint64_t *bar, uint32_t parity) {
     const long long t0 = clock64();
@@ -960,13 +967,12 @@ k_group(const __grid_constant__ Launch<KIND >= K_LOW ? 2 : 1> launch) {
                                                    __uint_as_float(v[j + 2]), __uint_as_float(v[j + 3])));
                 }
                 release();
-                __threadfence();
                 named_bar_sync(1, threads);
                 if (threadIdx.x == 0) {
+                    // (released and acquired for all behind the barriers)
                     uint32_t *count = p.count + 2 * (p.pair0 + w.c0) + rank;
-                    t.last = atomicAdd(count, 1u) == (uint32_t)(w.c1 - w.c0);
+                    t.last = add_acq_rel(count, 1u) == (uint32_t)(w.c1 - w.c0);
                     if (t.last) *count = 0;
-                    __threadfence();
                 }
                 named_bar_sync(1, threads);
                 write = *(volatile int *)&t.last != 0;
