@@ -339,6 +339,10 @@ constexpr int PICK_GROUPED = 1024, PICK_SHARED = 256;
 // Their shared product takes narrower tiles: more pairs have a tile of their own,
 // and a tile has fewer pieces to join.
 constexpr int FEW_BN = 128;
+// So do those of up to three eighths as many tiles as pairs: 171 rows through
+// 4,992 x 576 43 -> 39 us, 263 through 3,712 x 832 46 -> 39.  (With three quarters 336
+// rows of 46 adapters take 78 us for 57; with 32 columns 35 of 57 take 41 for 36.)
+constexpr int LEAST_BN = 64;
 // Inner products without tensor cores: values of the adapters that are read, and
 // blocks (a row and four ranks each).  With either twice as many the tensor cores
 // are faster, at 8 to 128 ranks and 256 to 4,096 columns (4,096 rows of rank 8 and
@@ -420,6 +424,15 @@ static int even_tiles(int n, int most) {
     return (int)up((n + tiles - 1) / tiles, 16);
 }
 
+// Columns of a tile whose A side are rows.
+static int tile_columns(const hwr_ops *c, const GroupProduct &p, int n) {
+    int most = p.sorted || !p.shared ? GP_TILE : FEW_BN;
+    const int64_t mtiles = (p.plan.places + GP_TILE - 1) / GP_TILE;
+    while (p.shared && !p.dense_mn && most > LEAST_BN && mtiles * ((n + most / 2 - 1) / (most / 2)) * 16 <= 3 * c->ctas)
+        most /= 2;
+    return most;
+}
+
 static hwr_status check_tiles(hwr_ops *c, const GroupProduct &p) {
     if (((int64_t)p.plan.places / GP_TILE + 1) * p.plan.groups * p.ntiles > INT32_MAX)
         return fail(c, HWR_ERR_UNSUPPORTED, "rows %d x groups %d x columns %d is too large", p.plan.rows, p.plan.groups,
@@ -443,7 +456,7 @@ static hwr_status rows_product(hwr_ops *c, GroupProduct p, const Operand &x, con
         p.x_ld = x.ld;
     }
     if (p.mode == GP_GROUPED) p.bn = (int)up(p.plan.places < GP_TILE ? p.plan.places : GP_TILE, 16);
-    else p.bn = even_tiles(n, p.sorted || !p.shared ? GP_TILE : FEW_BN);
+    else p.bn = even_tiles(n, tile_columns(c, p, n));
     group_plan(&p);
     OK(check_tiles(c, p));
     call->p = p;
