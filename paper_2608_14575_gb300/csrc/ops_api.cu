@@ -332,12 +332,21 @@ struct Rows {
     size_t offsets_off = 0, order_off = 0;     // padded plan
 };
 
-// Rows that are few are picked by index: they cost no copy, and the weights'
-// bytes bound the product (64 rows x 12 groups, 1024 -> 4096: 42 us picked).
-// More of them are copied by place once.
-constexpr int PICK_GROUPED = 1024, PICK_SHARED = 256;
-// Their shared product takes narrower tiles: more pairs have a tile of their own,
-// and a tile has fewer pieces to join.
+// Whether a product picks its rows by index, or they are copied by place first.
+// Picking saves the copy (its start and the rows' bytes, in and out) and costs each
+// tile: four of the eight epilogue warps pick, and where rows are a shared product's
+// A side, all pairs' loads.  In us, from 130 shapes either way: 10,188 rows of 3,136
+// columns to 512, 49 picked, 75 copied; 10,013 of 512 to 6,528, 109 and 82; through
+// adapters 950 of 4,608 to 1,984, 53 and 69; 7,354 of 4,352 to 4,544, 336 and 229.
+static bool picks_rows(const hwr_ops *c, int64_t rows, int k, int n, bool shared) {
+    const float pairs = c->ctas / 2, copy = rows * (float)k * 4e-6f / 6;
+    const float tiles = rows * ((n + GP_TILE - 1) / GP_TILE) / (GP_TILE * pairs);      // a pair
+    if (!shared) return 2.6f * tiles <= 0.8f + 1.4f * copy;
+    return 3.3f * tiles + (tiles > 1 ? 0.25f / GP_BK * k * tiles : 0) <= 3 + 1.4f * copy;
+}
+// The shared product of one tile's picked rows takes narrower tiles: more pairs have a
+// tile of their own, and a tile has fewer pieces to join.  (3,778 rows: 79 us, 62 with
+// whole tiles.)
 constexpr int FEW_BN = 128;
 // So do those of up to three eighths as many tiles as pairs: 171 rows through
 // 4,992 x 576 43 -> 39 us, 263 through 3,712 x 832 46 -> 39.  (With three quarters 336
@@ -351,7 +360,7 @@ constexpr int64_t LOW_FEW_VALUES = 64 << 20, LOW_FEW_BLOCKS = 4096;
 
 // contracted: a gradient contracts over the rows, which takes the padded plan.
 static Rows plan_rows(Carver &cv, const hwr_rows *r, const void *dy, int64_t dy_ld, bool need_x, bool contracted,
-                      int pick) {
+                      bool pick) {
     Rows s;
     s.plan.rows = s.plan.places = r->rows;
     s.plan.groups = r->groups;
@@ -367,7 +376,7 @@ static Rows plan_rows(Carver &cv, const hwr_rows *r, const void *dy, int64_t dy_
     };
     if (need_x) s.x = operand(r->x, r->x_ld, r->n_in);
     if (dy) s.dy = operand(dy, dy_ld, r->n_out);
-    s.sorted = contracted || r->rows > pick || (need_x && !on16(r->x, r->x_ld, 0, 1)) ||
+    s.sorted = contracted || !pick || (need_x && !on16(r->x, r->x_ld, 0, 1)) ||
                (dy && !on16(dy, dy_ld, 0, 1));
     if (!s.sorted) return s;
     if (contracted) {
@@ -426,7 +435,7 @@ static int even_tiles(int n, int most) {
 
 // Columns of a tile whose A side are rows.
 static int tile_columns(const hwr_ops *c, const GroupProduct &p, int n) {
-    int most = p.sorted || !p.shared ? GP_TILE : FEW_BN;
+    int most = p.sorted || !p.shared || p.plan.places > GP_TILE ? GP_TILE : FEW_BN;
     const int64_t mtiles = (p.plan.places + GP_TILE - 1) / GP_TILE;
     while (p.shared && !p.dense_mn && most > LEAST_BN && mtiles * ((n + most / 2 - 1) / (most / 2)) * 16 <= 3 * c->ctas)
         most /= 2;
@@ -524,7 +533,7 @@ extern "C" hwr_status hwr_grouped_forward(hwr_ops *c, const hwr_rows *r, void *y
     OK(check_out(c, r, y, y_ld, r->n_out, "y"));
     if (r->rows == 0) return HWR_OK;
     Carver cv;
-    Rows rows = plan_rows(cv, r, nullptr, 0, true, false, PICK_GROUPED);
+    Rows rows = plan_rows(cv, r, nullptr, 0, true, false, picks_rows(c, r->rows, r->n_in, r->n_out, false));
     Operand w = cv.operand(r->w, r->w_ld, r->n_out, r->n_in, r->w_group, r->groups);
     OK(reserve(c, cv.at));
     OK(sort_rows(c, &rows));
@@ -556,7 +565,7 @@ extern "C" hwr_status hwr_grouped_backward(hwr_ops *c, const hwr_rows *r, const 
     }
     if (!dx && !dw) return HWR_OK;
     Carver cv;
-    Rows rows = plan_rows(cv, r, dy, dy_ld, dw != nullptr, dw != nullptr, PICK_GROUPED);
+    Rows rows = plan_rows(cv, r, dy, dy_ld, dw != nullptr, dw != nullptr, picks_rows(c, r->rows, r->n_out, r->n_in, false));
     Operand w;
     if (dx) w = cv.operand(r->w, r->w_ld, r->n_out, r->n_in, r->w_group, r->groups);
     OK(reserve(c, cv.at));
@@ -669,7 +678,7 @@ extern "C" hwr_status hwr_adapter_forward(hwr_ops *c, const hwr_rows *r, const h
     if (r->rows == 0) return HWR_OK;
     const int K = r->n_in, N = r->n_out, R = ad->rank, G = r->groups;
     Carver cv;
-    Rows rows = plan_rows(cv, r, nullptr, 0, true, false, PICK_SHARED);
+    Rows rows = plan_rows(cv, r, nullptr, 0, true, false, picks_rows(c, r->rows, K, N, true));
     Operand w = cv.operand(r->w, r->w_ld, N, K);
     Operand a = cv.operand(ad->a, K, R, K, (int64_t)R * K, G);
     const bool few = !rows.sorted && r->rows <= FEW_ROWS;
@@ -729,7 +738,7 @@ extern "C" hwr_status hwr_adapter_backward(hwr_ops *c, const hwr_rows *r, const 
     }
     if (!dx && !da && !db) return HWR_OK;
     Carver cv;
-    Rows rows = plan_rows(cv, r, dy, dy_ld, da || db, da || db, PICK_SHARED);
+    Rows rows = plan_rows(cv, r, dy, dy_ld, da || db, da || db, picks_rows(c, r->rows, N, K, true));
     Operand w, a, b, u, v;
     if (dx) w = cv.operand(r->w, r->w_ld, N, K);
     if (dx || db) a = cv.operand(ad->a, K, R, K, (int64_t)R * K, G);
