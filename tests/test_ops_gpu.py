@@ -353,6 +353,27 @@ def test_results_of_each_alignment(ops, K, N, r, T):
         assert torch.equal(buf[:, :N], R.grouped_forward(x, gw, c)[0].to(BF)) and (buf[:, N:] == 7).all()
 
 
+@pytest.mark.parametrize("T,G,K,N,r", [(5000, 3, 1024, 256, 8), (3000, 40, 2048, 200, 40), (1500, 7, 4096, 96, 96),
+                                       (1500, 5, 512, 384, 5), (700, 9, 256, 640, 33), (257, 2, 1536, 72, 16)])
+@pytest.mark.parametrize("dt", [BF, HF])
+def test_many_rows_of_narrow_products(ops, T, G, K, N, r, dt):
+    """Rows of several tiles that are picked by index, tiles in pieces, inner
+    products of many rows; also without the gradients that need a copy."""
+    c = choices(T, G, "holes")
+    x, w, a, b, gw = (ints(*s, lo=-1, hi=1, dt=dt, seed=i) for i, s in
+                      enumerate(((T, K), (N, K), (G, r, K), (G, N, r), (G, N, K))))
+    dy, s = ints(T, N, lo=-1, hi=1, dt=dt, seed=9), 2.0 ** torch.randint(-1, 2, (G,), device="cuda").float()
+    plan = ops.dispatch(c, G)
+    assert torch.equal(ops.grouped_forward(x, gw, plan), R.grouped_forward(x, gw, c)[0].to(dt))
+    want = R.grouped_backward(dy, x, gw, c)[0][0].to(dt)
+    assert torch.equal(ops.grouped_backward(dy, x, gw, plan, need_dw=False)[0], want)
+    assert torch.equal(ops.grouped_backward(dy, x, gw, plan)[0], want)
+    assert torch.equal(ops.adapter_forward(x, w, a, b, s, plan), R.adapter_forward(x, w, a, b, s, c)[0].to(dt))
+    want = R.adapter_backward(dy, x, w, a, b, s, c)[0][0].to(dt)
+    assert torch.equal(ops.adapter_backward(dy, x, w, a, b, s, plan, need_dab=False)[0], want)
+    assert torch.equal(ops.adapter_backward(dy, x, w, a, b, s, plan)[0], want)
+
+
 def test_same_bits_again(ops):
     """Cut tiles are joined in a fixed order: the same call gives the same bits."""
     T, G, K, N, r = 700, 5, 1024, 1040, 16
