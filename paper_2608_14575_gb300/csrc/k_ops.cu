@@ -254,7 +254,34 @@ k_dispatch_place(int rows, int G, int64_t per_block, const int32_t *choice, cons
 size_t place_smem(int G) { return (size_t)(DP_WARPS + 3) * (G + 1) * 4; }
 
 // ---------------------------------------------------------------------------
-// Rows by place: a warp copies a row (reads and writes of 512 bytes at a time).
+// Eight values from column 8 i on of a row of `cols` that begins anywhere: two
+// aligned loads inside the row, shifted; at its ends value by value, zeros beyond.
+__device__ __forceinline__ uint4 unit_of(const uint16_t *src, int i, int cols) {
+    const uint16_t *a = src + (int64_t)i * 8;
+    const uint32_t off = (uint32_t)(uintptr_t)a & 15;
+    const uint4 *w = (const uint4 *)((uintptr_t)a - off);
+    if (off == 0 && i * 8 + 8 <= cols) return __ldg(w);
+    if (i > 0 && i * 8 + 16 <= cols) {       // (the loads reach 7 values back and 15 on)
+        const uint4 lo = __ldg(w), hi = __ldg(w + 1);
+        uint32_t x[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+        if (off & 8)
+#pragma unroll
+            for (int j = 0; j < 6; ++j) x[j] = x[j + 2];
+        if (off & 4)
+#pragma unroll
+            for (int j = 0; j < 5; ++j) x[j] = x[j + 1];
+        const uint32_t bits = (off & 2) * 8;
+        return make_uint4(__funnelshift_r(x[0], x[1], bits), __funnelshift_r(x[1], x[2], bits),
+                          __funnelshift_r(x[2], x[3], bits), __funnelshift_r(x[3], x[4], bits));
+    }
+    uint32_t v[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = i * 8 + j < cols ? a[j] : 0;
+    return make_uint4(v[0] | v[1] << 16, v[2] | v[3] << 16, v[4] | v[5] << 16, v[6] | v[7] << 16);
+}
+
+// Rows by place: a warp copies a row, or with few rows a slice of one (reads and
+// writes of 512 bytes at a time; gridDim.y slices).
 
 constexpr int SR_THREADS = 256;
 
@@ -290,7 +317,7 @@ k_sort_rows(const __grid_constant__ GroupPlan plan, const __grid_constant__ Sort
         }
         __syncthreads();
         total = min(pad[G] + plan.rows - offs[G], places);
-        if (blockIdx.x == 0) {
+        if (blockIdx.x == 0 && blockIdx.y == 0) {
             for (int i = threadIdx.x; i <= G; i += SR_THREADS) padded_offsets[i] = pad[i];
             if (threadIdx.x == 0) padded_offsets[G + 1] = total;
         }
@@ -309,21 +336,20 @@ k_sort_rows(const __grid_constant__ GroupPlan plan, const __grid_constant__ Sort
         }
         int r = place >= 0 && place < plan.rows ? plan.order[place] : -1;
         if ((uint32_t)r >= (uint32_t)plan.rows) r = -1;
-        if (padded_offsets && lane == 0) padded_order[at] = r;
+        if (padded_offsets && lane == 0 && blockIdx.y == 0) padded_order[at] = r;
         for (int k = 0; k < m.n; ++k) {
             uint4 *dst = (uint4 *)(m.dst[k] + at * m.dst_ld[k]);
             const int units = (int)(m.dst_ld[k] / 8), cols = m.cols[k];
             const uint16_t *src = r < 0 ? nullptr : m.src[k] + r * m.src_ld[k];
-            if (src && ((uintptr_t)src & 15) == 0 && cols % 8 == 0) {
+            const int first = blockIdx.y * 32 + lane, step = gridDim.y * 32;
+            if (!src) {
+                for (int i = first; i < units; i += step) dst[i] = make_uint4(0, 0, 0, 0);
+            } else if (((uintptr_t)src & 15) == 0 && cols % 8 == 0) {
 #pragma unroll 4
-                for (int i = lane; i < units; i += 32) dst[i] = __ldg((const uint4 *)src + i);
-                continue;
-            }
-            for (int i = lane; i < units; i += 32) {
-                uint32_t v[8];
-#pragma unroll
-                for (int j = 0; j < 8; ++j) v[j] = src && i * 8 + j < cols ? src[i * 8 + j] : 0;
-                dst[i] = make_uint4(v[0] | v[1] << 16, v[2] | v[3] << 16, v[4] | v[5] << 16, v[6] | v[7] << 16);
+                for (int i = first; i < units; i += step) dst[i] = __ldg((const uint4 *)src + i);
+            } else {
+#pragma unroll 2
+                for (int i = first; i < units; i += step) dst[i] = unit_of(src, i, cols);
             }
         }
     }
@@ -444,16 +470,13 @@ k_low_few(const __grid_constant__ LowFew p) {
 __global__ void __launch_bounds__(256)
 k_pad(uint16_t *dst, int64_t dst_ld, const uint16_t *src, int64_t src_ld, int64_t src_z, int64_t rows,
       int64_t all_rows, int cols) {
-    const int64_t units = dst_ld / 8;        // 16-byte units of a row
-    for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < all_rows * units; i += gridDim.x * 256ll) {
-        const int64_t r = i / units;
-        const int c = (int)(i - r * units) * 8;
-        const uint16_t *s = src + (r / rows) * src_z + (r % rows) * src_ld + c;
-        uint32_t v[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = c + j < cols ? s[j] : 0;
-        *(uint4 *)(dst + r * dst_ld + c) = make_uint4(v[0] | v[1] << 16, v[2] | v[3] << 16,
-                                                      v[4] | v[5] << 16, v[6] | v[7] << 16);
+    const int64_t units = dst_ld / 8, all = all_rows * units;        // 16-byte units, of a row and in all
+    const bool narrow = all <= INT32_MAX;                            // (64-bit divisions cost as much as the copy)
+#pragma unroll 2
+    for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < all; i += gridDim.x * 256ll) {
+        const int64_t r = narrow ? (uint32_t)i / (uint32_t)units : i / units;
+        const int64_t z = narrow ? (uint32_t)r / (uint32_t)rows : r / rows;
+        *(uint4 *)(dst + i * 8) = unit_of(src + z * src_z + (r - z * rows) * src_ld, (int)(i - r * units), cols);
     }
 }
 
@@ -754,7 +777,12 @@ cudaError_t launch_sort_rows(const GroupPlan &plan, const SortRows &m, int place
                              int32_t *padded_order, int nsm, cudaStream_t s) {
     const int64_t want = ((int64_t)places + SR_THREADS / 32 - 1) / (SR_THREADS / 32), most = (int64_t)nsm * 8;
     cudaLaunchAttribute at[1];
-    const cudaLaunchConfig_t cfg = relaxed((int)(want < most ? want : most), SR_THREADS, (plan.groups + 1) * 8, s, at);
+    cudaLaunchConfig_t cfg = relaxed((int)(want < most ? want : most), SR_THREADS, (plan.groups + 1) * 8, s, at);
+    // slices of at least four steps of a warp
+    int64_t widest = 1;
+    for (int k = 0; k < m.n; ++k) widest = widest < m.dst_ld[k] / (8 * 32 * 4) ? m.dst_ld[k] / (8 * 32 * 4) : widest;
+    const int64_t slices = want < 1 ? 1 : most / want;
+    cfg.gridDim.y = (unsigned)(slices < 1 ? 1 : slices < widest ? slices : widest);
     return cudaLaunchKernelEx(&cfg, k_sort_rows, plan, m, places, padded_offsets, padded_order);
 }
 
