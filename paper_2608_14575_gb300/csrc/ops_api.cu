@@ -338,12 +338,21 @@ struct Rows {
 // A side, all pairs' loads.  In us, from 130 shapes either way: 10,188 rows of 3,136
 // columns to 512, 49 picked, 75 copied; 10,013 of 512 to 6,528, 109 and 82; through
 // adapters 950 of 4,608 to 1,984, 53 and 69; 7,354 of 4,352 to 4,544, 336 and 229.
-static bool picks_rows(const hwr_ops *c, int64_t rows, int k, int n, bool shared) {
-    const float pairs = c->ctas / 2, copy = rows * (float)k * 4e-6f / 6;
+// Four warps write a tile whose results are aligned to less than 16 bytes (vec: values
+// of a store) slowly: 1,000 rows of 512 columns to 1,028 over 4 experts 26 us picked, 20
+// copied; 300 rows 14 and 15.
+static bool picks_rows(const hwr_ops *c, const hwr_rows *r, int k, int n, bool shared, int vec) {
+    const float rows = (float)r->rows, pairs = c->ctas / 2, copy = rows * k * 4e-6f / 6;
     const float tiles = rows * ((n + GP_TILE - 1) / GP_TILE) / (GP_TILE * pairs);      // a pair
-    if (!shared) return 2.6f * tiles <= 0.8f + 1.4f * copy;
-    return 3.3f * tiles + (tiles > 1 ? 0.25f / GP_BK * k * tiles : 0) <= 3 + 1.4f * copy;
+    if (!shared) {
+        if (vec == 8) return 2.6f * tiles <= 0.8f + 1.4f * copy;
+        const float full = rows / r->groups / GP_TILE;                                  // of a tile's columns
+        return 12 * (tiles > 1 ? tiles : full < 1 ? full : 1) <= 3.5f + 1.4f * copy;
+    }
+    const float write = (vec == 8 ? 0.f : vec == 4 ? 1.f : vec == 2 ? 4.f : 7.f) * (rows < GP_TILE ? rows / GP_TILE : 1);
+    return 3.3f * tiles + (tiles > 1 ? 0.25f / GP_BK * k * tiles : 0) + write <= 3 + 1.4f * copy;
 }
+
 // The shared product of one tile's picked rows takes narrower tiles: more pairs have a
 // tile of their own, and a tile has fewer pieces to join.  (3,778 rows: 79 us, 62 with
 // whole tiles.)
@@ -533,7 +542,7 @@ extern "C" hwr_status hwr_grouped_forward(hwr_ops *c, const hwr_rows *r, void *y
     OK(check_out(c, r, y, y_ld, r->n_out, "y"));
     if (r->rows == 0) return HWR_OK;
     Carver cv;
-    Rows rows = plan_rows(cv, r, nullptr, 0, true, false, picks_rows(c, r->rows, r->n_in, r->n_out, false));
+    Rows rows = plan_rows(cv, r, nullptr, 0, true, false, picks_rows(c, r, r->n_in, r->n_out, false, vec_of(y, y_ld, 0)));
     Operand w = cv.operand(r->w, r->w_ld, r->n_out, r->n_in, r->w_group, r->groups);
     OK(reserve(c, cv.at));
     OK(sort_rows(c, &rows));
@@ -565,7 +574,7 @@ extern "C" hwr_status hwr_grouped_backward(hwr_ops *c, const hwr_rows *r, const 
     }
     if (!dx && !dw) return HWR_OK;
     Carver cv;
-    Rows rows = plan_rows(cv, r, dy, dy_ld, dw != nullptr, dw != nullptr, picks_rows(c, r->rows, r->n_out, r->n_in, false));
+    Rows rows = plan_rows(cv, r, dy, dy_ld, dw != nullptr, dw != nullptr, picks_rows(c, r, r->n_out, r->n_in, false, vec_of(dx, dx_ld, 0)));
     Operand w;
     if (dx) w = cv.operand(r->w, r->w_ld, r->n_out, r->n_in, r->w_group, r->groups);
     OK(reserve(c, cv.at));
@@ -678,7 +687,7 @@ extern "C" hwr_status hwr_adapter_forward(hwr_ops *c, const hwr_rows *r, const h
     if (r->rows == 0) return HWR_OK;
     const int K = r->n_in, N = r->n_out, R = ad->rank, G = r->groups;
     Carver cv;
-    Rows rows = plan_rows(cv, r, nullptr, 0, true, false, picks_rows(c, r->rows, K, N, true));
+    Rows rows = plan_rows(cv, r, nullptr, 0, true, false, picks_rows(c, r, K, N, true, vec_of(y, y_ld, 0)));
     Operand w = cv.operand(r->w, r->w_ld, N, K);
     Operand a = cv.operand(ad->a, K, R, K, (int64_t)R * K, G);
     const bool few = !rows.sorted && r->rows <= FEW_ROWS;
@@ -738,7 +747,7 @@ extern "C" hwr_status hwr_adapter_backward(hwr_ops *c, const hwr_rows *r, const 
     }
     if (!dx && !da && !db) return HWR_OK;
     Carver cv;
-    Rows rows = plan_rows(cv, r, dy, dy_ld, da || db, da || db, picks_rows(c, r->rows, N, K, true));
+    Rows rows = plan_rows(cv, r, dy, dy_ld, da || db, da || db, picks_rows(c, r, N, K, true, vec_of(dx, dx_ld, 0)));
     Operand w, a, b, u, v;
     if (dx) w = cv.operand(r->w, r->w_ld, N, K);
     if (dx || db) a = cv.operand(ad->a, K, R, K, (int64_t)R * K, G);
