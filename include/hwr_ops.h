@@ -32,8 +32,15 @@
  *   - Sums run in fp32 on the tensor cores; each output is rounded once.
  *   - Results do not depend on timing: the same call gives the same bits.
  *   - The workspace grows (cudaMalloc) when a call needs more than any call
- *     before; hwr_ops_reserve does that ahead of time, e.g. before a stream
- *     capture.
+ *     before; hwr_ops_reserve does that ahead of time.
+ *   - Stream capture: calls can be captured into graphs.  A call that would have
+ *     to grow the workspace then is refused (UNSUPPORTED, nothing is queued, the
+ *     context stays usable): make a call of the same sizes before, or reserve.  A
+ *     block that a captured call uses is kept until hwr_ops_destroy, also when a
+ *     later call takes a larger one; the context outlives its graphs.  A replay
+ *     uses the context's workspace, partial sums and counters as an eager call
+ *     does: order it with the context's other work (the same stream, or
+ *     hwr_ops_after / hwr_ops_before); two of them at a time spoil each other.
  *   - After HWR_ERR_CUDA or HWR_ERR_TIMEOUT the context is broken (hwr.h).
  */
 #ifndef HWR_OPS_H

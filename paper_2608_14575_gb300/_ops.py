@@ -17,6 +17,12 @@ Tensors are CUDA tensors of the context's device whose last dimension is
 contiguous; other strides are free.  The context is bound to the torch stream
 that is current when it is made.  A call made under another current stream is
 ordered after that stream's work so far, and that stream after the call.
+
+Calls can be captured into CUDA graphs once the workspace is large enough: after
+a call of the same sizes, or ``reserve`` (a capture in which it would have to grow
+raises HwrError).  What a graph uses of the workspace stays until ``close``.  A
+replay shares it with the context's other calls, so order them: replay on the
+context's stream, or on one that the other calls are ordered with.
 """
 from __future__ import annotations
 

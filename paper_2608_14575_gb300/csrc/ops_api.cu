@@ -4,6 +4,7 @@
 #include <cudaTypedefs.h>
 #include <math.h>
 #include <stdarg.h>
+#include <stdint.h>
 #include <stdio.h>
 #include <stdlib.h>
 #include <string.h>
@@ -31,6 +32,12 @@ struct ApiRange {
 
 }  // namespace
 
+// Device memory that a captured graph may hold, kept until the context goes.
+struct Retired {
+    void *p;
+    Retired *next;
+};
+
 struct hwr_ops {
     cudaStream_t stream = nullptr;
     bool own_stream = false, broken = false;
@@ -38,6 +45,8 @@ struct hwr_ops {
     std::string err;
     char *ws = nullptr;
     size_t ws_cap = 0;
+    bool ws_held = false;        // a captured call has its address
+    Retired *retired = nullptr;
     float *part = nullptr;       // partial tiles of the grouped products
     uint32_t *count = nullptr;   // their arrivals (zeroed once, self-resetting)
     double *sums = nullptr;      // partial sums of squares; then their arrivals and the factor
@@ -99,15 +108,46 @@ static hwr_status alloc(hwr_ops *c, T **p, size_t n) {
     return HWR_OK;
 }
 
+// Whether what the context queues now goes into a graph.
+static hwr_status capturing(hwr_ops *c, bool *yes) {
+    *yes = false;
+    if (c->stream == cudaStreamLegacy) return HWR_OK;      // (takes no part in captures)
+    cudaStreamCaptureStatus st = cudaStreamCaptureStatusNone;
+    CK(c, cudaStreamIsCapturing(c->stream, &st), "capture status");
+    *yes = st != cudaStreamCaptureStatusNone;
+    return HWR_OK;
+}
+
+static hwr_status retire(hwr_ops *c, void *p) {
+    Retired *r = new (std::nothrow) Retired{p, c->retired};
+    if (!r) return fail(c, HWR_ERR_OOM, "host allocation failed");
+    c->retired = r;
+    return HWR_OK;
+}
+
+// A block that a captured call has used stays when a larger one takes its place:
+// the graph's replays go on using it.
 static hwr_status reserve(hwr_ops *c, size_t bytes) {
-    if (bytes <= c->ws_cap) return HWR_OK;
+    bool captured;
+    OK(capturing(c, &captured));
+    if (bytes <= c->ws_cap) {
+        c->ws_held = c->ws_held || (captured && bytes);
+        return HWR_OK;
+    }
+    if (captured)
+        return fail(c, HWR_ERR_UNSUPPORTED, "the workspace cannot grow (to %zu bytes) during a stream capture", bytes);
     if (c->ws) {
-        CK(c, cudaStreamSynchronize(c->stream), "synchronize before regrow");
-        cudaFree(c->ws);
+        if (c->ws_held) {
+            OK(retire(c, c->ws));
+        } else {
+            CK(c, cudaStreamSynchronize(c->stream), "synchronize before regrow");
+            cudaFree(c->ws);
+        }
         c->ws = nullptr;
         c->ws_cap = 0;
+        c->ws_held = false;
     }
-    const size_t want = bytes + bytes / 8;
+    const size_t want = bytes <= SIZE_MAX / 2 ? bytes + bytes / 8 : bytes;
     OK(alloc(c, &c->ws, want));
     c->ws_cap = want;
     return HWR_OK;
@@ -165,6 +205,11 @@ extern "C" hwr_status hwr_ops_destroy(hwr_ops *c) {
     if (!c) return HWR_OK;
     if (c->stream) cudaStreamSynchronize(c->stream);
     cudaFree(c->ws);
+    while (Retired *r = c->retired) {
+        c->retired = r->next;
+        cudaFree(r->p);
+        delete r;
+    }
     cudaFree(c->part);
     cudaFree(c->count);
     cudaFree(c->sums);

@@ -1,0 +1,102 @@
+"""The operators in captured graphs, beside eager calls of the same context."""
+import pytest
+
+torch = pytest.importorskip("torch")
+
+import paper_2608_14575_gb300 as H
+import ops_ref as R
+from test_ops_gpu import BF, choices, ints
+
+pytestmark = pytest.mark.gpu
+UNSUPPORTED = 7
+
+
+@pytest.fixture
+def side():
+    """A context on a stream of its own."""
+    H.build()
+    stream = torch.cuda.Stream()
+    with torch.cuda.stream(stream):
+        ops = H.Operators()
+        yield ops, stream
+    torch.cuda.synchronize()
+    ops.close()
+
+
+def layer(T, G=5, K=264, N=200, r=24, seed=0):
+    c = choices(T, G, "holes", seed=seed)
+    t = [ints(*s, lo=-1, hi=1, seed=seed + i) for i, s in enumerate(((T, K), (N, K), (G, r, K), (G, N, r), (T, N)))]
+    return [c, *t, torch.ones(G, device="cuda")]
+
+
+def step(ops, c, x, w, a, b, dy, s):
+    """Everything that takes workspace: sorted rows, padded weights, inner products, a gradient table."""
+    plan = ops.dispatch(c, a.shape[0])
+    y = ops.adapter_forward(x, w, a, b, s, plan)
+    grads = ops.adapter_backward(dy, x, w, a, b, s, plan)
+    clipped = [g.clone() for g in grads]
+    return [y, *grads, ops.clip_gradients(clipped, 1.0), *clipped]
+
+
+def want(c, x, w, a, b, dy, s):
+    return [R.adapter_forward(x, w, a, b, s, c)[0].to(BF),
+            *(e.to(BF) for e, _ in R.adapter_backward(dy, x, w, a, b, s, c))]
+
+
+def test_graphs_outlive_a_larger_call(side):
+    """Graphs of growing sizes captured on one context: each keeps the workspace it was
+    captured with, also when that has given way to a larger one and other memory is taken."""
+    ops, stream = side
+    graphs = []
+    for T in (20, 300, 1500):
+        args = layer(T)
+        step(ops, *args)                        # grows the workspace: the graphs before hold theirs
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            held = step(ops, *args)
+        graphs.append((graph, held, args))
+    step(ops, *layer(6000))
+    # memory that was given back would be handed out here
+    guard = [torch.full((1 << 20,), 7, device="cuda", dtype=torch.int8) for _ in range(200)]
+    for k in range(2):
+        for graph, held, (c, x, w, a, b, dy, s) in graphs:
+            T, G = c.numel(), a.shape[0]
+            c.copy_(choices(T, G, "any", seed=50 + k))
+            x.copy_(ints(*x.shape, lo=-1, hi=1, seed=70 + k))
+            dy.copy_(ints(*dy.shape, lo=-1, hi=1, seed=90 + k))
+            graph.replay()
+            for got, exact in zip(held, want(c, x, w, a, b, dy, s)):
+                assert torch.equal(got, exact)
+            again = step(ops, c, x, w, a, b, dy, s)
+            for p, q in zip(held, again):
+                assert torch.equal(p, q)
+    assert all(bool((g == 7).all()) for g in guard)
+
+
+@pytest.mark.parametrize("mine", [True, False])
+def test_growing_in_a_capture_is_refused(side, mine):
+    """The call says so, queues nothing, and leaves the context and the capture as they
+    were; on the context's own stream and on another."""
+    ops, stream = side
+    on = stream if mine else torch.cuda.Stream()
+    small, large = layer(30), layer(3000)
+    with torch.cuda.stream(on):
+        step(ops, *small)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=on):
+            plan = ops.dispatch(large[0], 5)
+            with pytest.raises(H.HwrError) as e:
+                ops.adapter_backward(large[5], *large[1:5], large[6], plan)
+            assert e.value.status == UNSUPPORTED
+            with pytest.raises(H.HwrError) as e:
+                ops.reserve(1 << 32)
+            assert e.value.status == UNSUPPORTED
+            held = step(ops, *small)
+        graph.replay()
+        c, x, w, a, b, dy, s = small
+        for got, exact in zip(held, want(c, x, w, a, b, dy, s)):
+            assert torch.equal(got, exact)
+        for got, exact in zip(step(ops, *large), want(*large)):
+            assert torch.equal(got, exact)
