@@ -5,7 +5,8 @@ one shared library with the CUDA runtime linked statically, so that loading
 it needs no libcudart on the library path.  The output goes to
 ``_build/libhwr_<machine>.so`` next to this file (git-ignored).  The torch
 binding of the operators (csrc/ops_torch.cpp, g++) is compiled beside it into
-``_build/hwr_torch_<machine>.so``, which links the library.
+``_build/hwr_torch_<machine>.so``, which links the library; the library needs
+nvcc alone, and is built where torch is not installed too.
 """
 from __future__ import annotations
 
@@ -46,12 +47,16 @@ def torch_path() -> str:
     return os.path.join(OUT_DIR, f"hwr_torch_{platform.machine()}.so")
 
 
-def _torch_commands(out: str):
-    """Compile and link commands of the torch binding."""
+def _torch_dir():
+    """Where torch is installed; None where it is not."""
     spec = importlib.util.find_spec("torch")
     if spec is None or not spec.submodule_search_locations:
-        raise RuntimeError("torch not found: the operators' binding needs its headers")
-    torch = list(spec.submodule_search_locations)[0]
+        return None
+    return list(spec.submodule_search_locations)[0]
+
+
+def _torch_commands(torch: str, out: str):
+    """Compile and link commands of the torch binding."""
     obj = os.path.join(OUT_DIR, f"ops_torch_{platform.machine()}.o")
     compile_ = ["g++", "-O2", "-std=c++17", "-fPIC", "-fvisibility=hidden", "-I", INCLUDE,
                 "-isystem", os.path.join(torch, "include"),
@@ -72,9 +77,10 @@ def _nvcc() -> str:
 
 
 def _stale(out: str) -> bool:
-    if not os.path.exists(out) or not os.path.exists(torch_path()):
+    outs = [out] + ([torch_path()] if _torch_dir() else [])
+    if not all(os.path.exists(o) for o in outs):
         return True
-    t = min(os.path.getmtime(out), os.path.getmtime(torch_path()))
+    t = min(os.path.getmtime(o) for o in outs)
     deps = [os.path.join(CSRC, f) for f in os.listdir(CSRC)]
     deps += [os.path.join(INCLUDE, f) for f in os.listdir(INCLUDE)]
     deps.append(os.path.abspath(__file__))
@@ -82,7 +88,9 @@ def _stale(out: str) -> bool:
 
 
 def build(force: bool = False, verbose: bool = False, ptxas_info: bool = False) -> str:
-    """Compile and link libhwr; returns the path of the shared library."""
+    """Compile and link libhwr, and the torch binding where torch is installed;
+    returns the path of libhwr.  A binding that does not build leaves libhwr in
+    place (and raises)."""
     out = lib_path()
     if not force and not _stale(out):
         return out
@@ -92,35 +100,41 @@ def build(force: bool = False, verbose: bool = False, ptxas_info: bool = False) 
               "-I", INCLUDE, "-I", CSRC, *ARCH]
     if ptxas_info:
         common += ["-Xptxas", "-v"]
-    procs = []
-    objs = []
-    for src, extra in SOURCES.items():
-        obj = os.path.join(OUT_DIR, src.replace(".cu", f"_{platform.machine()}.o"))
-        objs.append(obj)
-        cmd = [nvcc, *common, *extra, "-c", os.path.join(CSRC, src), "-o", obj]
+    procs, objs = [], []
+
+    def compile_(src, cmd):
         if verbose:
             print(" ".join(cmd), flush=True)
         procs.append((src, subprocess.Popen(cmd, stdout=subprocess.PIPE,
                                             stderr=subprocess.STDOUT, text=True)))
-    torch_out = torch_path() + ".tmp"
-    torch_compile, torch_link = _torch_commands(torch_out)
-    procs.append(("ops_torch.cpp", subprocess.Popen(torch_compile, stdout=subprocess.PIPE,
-                                                    stderr=subprocess.STDOUT, text=True)))
-    errors = []
+
+    for src, extra in SOURCES.items():
+        obj = os.path.join(OUT_DIR, src.replace(".cu", f"_{platform.machine()}.o"))
+        objs.append(obj)
+        compile_(src, [nvcc, *common, *extra, "-c", os.path.join(CSRC, src), "-o", obj])
+    torch = _torch_dir()
+    if torch:
+        torch_out = torch_path() + ".tmp"
+        torch_compile, torch_link = _torch_commands(torch, torch_out)
+        compile_("ops_torch.cpp", torch_compile)
+    errors = {}
     for src, p in procs:
         text, _ = p.communicate()
         if p.returncode != 0:
-            errors.append(f"--- {src}\n{text}")
+            errors[src] = f"--- {src}\n{text}"
         elif verbose or ptxas_info:
             sys.stdout.write(text)
-    if errors:
-        raise RuntimeError("nvcc failed:\n" + "\n".join(errors))
+    if any(src in errors for src in SOURCES):
+        raise RuntimeError("nvcc failed:\n" + "\n".join(errors.values()))
     tmp = out + ".tmp"
     link = [nvcc, "-shared", *ARCH, "-cudart", "static", *objs, "-o", tmp]
     subprocess.run(link, check=True)
     os.replace(tmp, out)
-    subprocess.run(torch_link, check=True)
-    os.replace(torch_out, torch_path())
+    if errors:
+        raise RuntimeError("the operators' torch binding does not compile:\n" + "\n".join(errors.values()))
+    if torch:
+        subprocess.run(torch_link, check=True)
+        os.replace(torch_out, torch_path())
     return out
 
 
