@@ -64,8 +64,9 @@ def _torch_commands(torch: str, out: str):
                 "-isystem", sysconfig.get_paths()["include"],
                 "-c", os.path.join(CSRC, "ops_torch.cpp"), "-o", obj]
     lib = os.path.join(torch, "lib")
-    link = ["g++", "-shared", obj, "-o", out, lib_path(), "-L", lib, "-ltorch_python",
-            "-ltorch_cpu", "-lc10", "-Wl,-rpath,$ORIGIN"]
+    # (the library by its name, found beside the binding: the folder may move)
+    link = ["g++", "-shared", obj, "-o", out, "-L", OUT_DIR, "-l:" + os.path.basename(lib_path()),
+            "-L", lib, "-ltorch_python", "-ltorch_cpu", "-lc10", "-Wl,-rpath,$ORIGIN"]
     return compile_, link
 
 

@@ -1,6 +1,9 @@
 """The build script: what it makes where torch is missing or does not compile."""
 import importlib
 import os
+import shutil
+import subprocess
+import sys
 import time
 
 import pytest
@@ -35,3 +38,23 @@ def test_library_beside_a_broken_binding(small, monkeypatch):
     with pytest.raises(RuntimeError):
         build.build()
     assert os.path.exists(build.lib_path()) and not os.path.exists(build.torch_path())
+
+
+def test_binding_moves_with_its_library(tmp_path):
+    """A copy of the package loads the copy's own library, also where the first is gone."""
+    pytest.importorskip("torch")
+    build.build()
+    there = tmp_path / "moved"
+    there.mkdir()
+    for f in (build.lib_path(), build.torch_path()):
+        shutil.copy(f, there)
+    lib, binding = (str(there / os.path.basename(f)) for f in (build.lib_path(), build.torch_path()))
+    program = f"""
+import ctypes, importlib.util, torch
+ctypes.CDLL({lib!r})
+spec = importlib.util.spec_from_file_location("hwr_torch", {binding!r})
+spec.loader.exec_module(importlib.util.module_from_spec(spec))
+print(sorted({{l.split()[-1] for l in open("/proc/self/maps") if "libhwr_" in l}}))
+"""
+    out = subprocess.run([sys.executable, "-c", program], capture_output=True, text=True, check=True).stdout
+    assert eval(out) == [lib]
