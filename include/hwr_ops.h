@@ -68,6 +68,7 @@ const char *hwr_ops_last_error(const hwr_ops *ops); /* NULL: of hwr_ops_create *
  * another stream's later work after what the context has queued (for calls whose
  * arrays belong to that stream; 1 is the legacy default stream).  A context on
  * the default stream cannot follow a stream that is being captured (UNSUPPORTED).
+ * hwr_ops_before orders what a context has queued that is broken by now, too.
  * Errors: INVALID_ARG, UNSUPPORTED, STATE, CUDA. */
 hwr_status hwr_ops_after(hwr_ops *ops, void *cuda_stream);
 hwr_status hwr_ops_before(hwr_ops *ops, void *cuda_stream);

@@ -254,9 +254,10 @@ extern "C" hwr_status hwr_ops_after(hwr_ops *c, void *stream) {
 
 extern "C" hwr_status hwr_ops_before(hwr_ops *c, void *stream) {
     if (!c) return HWR_ERR_INVALID_ARG;
-    OK(ready(c));
     if (!stream) return fail(c, HWR_ERR_INVALID_ARG, "NULL stream");
-    return order_streams(c, c->stream, (cudaStream_t)stream);
+    // (a broken context's work may still be running)
+    const hwr_status s = ready(c), o = order_streams(c, c->stream, (cudaStream_t)stream);
+    return s != HWR_OK ? s : o;
 }
 
 extern "C" hwr_status hwr_ops_reserve(hwr_ops *c, uint64_t bytes) {

@@ -155,7 +155,8 @@ hwr_dtype sixteen(const at::Tensor &t, const char *name) {
 }
 
 // The call, ordered after the current stream's work and that stream after it,
-// where it is not the context's own.
+// where it is not the context's own; also when it fails (part of its work may be
+// queued, and the caller's memory goes back to the current stream).
 template <class F>
 void call(Context &c, PyObject *raw, F f) {
     void *current = address(raw);
@@ -164,7 +165,12 @@ void call(Context &c, PyObject *raw, F f) {
         if (s != HWR_OK) throw StatusError(s, hwr_ops_last_error(c.ops));
     };
     if (other) check(hwr_ops_after(c.ops, current ? current : (void *)1));
-    check(f());
+    const hwr_status s = f();
+    if (s != HWR_OK) {
+        const StatusError error(s, hwr_ops_last_error(c.ops));
+        if (other) hwr_ops_before(c.ops, current ? current : (void *)1);
+        throw error;
+    }
     if (other) check(hwr_ops_before(c.ops, current ? current : (void *)1));
 }
 
@@ -449,10 +455,9 @@ PyObject *clip(PyObject *, PyObject *const *a, Py_ssize_t n) {
         Context &c = context(a[0]);
         const std::vector<hwr_gradient> v = gradients(c, a[2], a[3]);
         const float max_norm = (float)number(a[4]);
+        const int count = narrow((int64_t)v.size(), "gradients");
         at::Tensor norm = scalar(c);
-        call(c, a[1], [&] {
-            return hwr_clip_gradients(c.ops, narrow((int64_t)v.size(), "gradients"), v.data(), max_norm, (float *)norm.data_ptr());
-        });
+        call(c, a[1], [&] { return hwr_clip_gradients(c.ops, count, v.data(), max_norm, (float *)norm.data_ptr()); });
         return wrap(std::move(norm));
     });
 }
@@ -463,8 +468,9 @@ PyObject *list_create(PyObject *, PyObject *const *a, Py_ssize_t n) {
         want(n, 4);
         Context &c = context(a[0]);
         const std::vector<hwr_gradient> v = gradients(c, a[2], a[3]);
+        const int count = narrow((int64_t)v.size(), "gradients");
         hwr_gradients *l = nullptr;
-        call(c, a[1], [&] { return hwr_gradients_create(c.ops, narrow((int64_t)v.size(), "gradients"), v.data(), &l); });
+        call(c, a[1], [&] { return hwr_gradients_create(c.ops, count, v.data(), &l); });
         return PyLong_FromVoidPtr(l);
     });
 }

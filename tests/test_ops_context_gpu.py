@@ -1,0 +1,39 @@
+"""What a context does around its calls: order, refusals, lifetimes."""
+import pytest
+
+torch = pytest.importorskip("torch")
+
+import paper_2608_14575_gb300 as H
+import ops_ref as R
+from test_ops_gpu import BF, choices, ints
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture
+def ops():
+    """A context on a stream of its own, while the default stream is current."""
+    H.build()
+    ops = H.Operators(torch.cuda.Stream())
+    yield ops
+    ops.close()
+
+
+def test_a_failed_call_is_ordered_too(ops):
+    """What the caller frees after a failed call goes to its own stream's next work,
+    which has to wait for whatever the context's stream still runs."""
+    c = choices(10, 3, "any")
+    plan = ops.dispatch(c, 3)
+    R1 = H.HWR_OPS_MAX_RANK + 1
+    args = ints(10, 16), ints(24, 16), ints(3, R1, 16), ints(3, 24, R1), torch.ones(3, device="cuda")
+    torch.cuda.synchronize()
+    with torch.cuda.stream(ops.stream):
+        torch.cuda._sleep(400_000_000)          # some 0.2 s
+    with pytest.raises(H.HwrError) as e:
+        ops.adapter_forward(*args, plan)
+    assert e.value.status == 7 and "rank" in str(e.value)
+    done = torch.cuda.Event()
+    done.record()
+    early, busy = done.query(), not ops.stream.query()
+    torch.cuda.synchronize()
+    assert busy and not early
