@@ -58,7 +58,8 @@ extern "C" {
 typedef struct hwr_ops hwr_ops;
 
 /* Create a context on cuda_stream (NULL: a non-blocking stream of its own) of
- * the current device, which must be current at every later call.
+ * the current device, which must be current at every later call (another one:
+ * INVALID_ARG, and the context stays usable).
  * Errors: INVALID_ARG, OOM, CUDA. */
 hwr_status hwr_ops_create(void *cuda_stream, hwr_ops **out);
 hwr_status hwr_ops_destroy(hwr_ops *ops);          /* synchronises; NULL is fine */

@@ -41,6 +41,7 @@ struct Retired {
 struct hwr_ops {
     cudaStream_t stream = nullptr;
     bool own_stream = false, broken = false;
+    int device = 0;
     int nsm = 1, ctas = 2;       // SMs; CTAs of the grouped products
     std::string err;
     char *ws = nullptr;
@@ -53,6 +54,7 @@ struct hwr_ops {
     int32_t *status_h = nullptr, *status_d = nullptr;   // mapped: bounded waits that ran out
     cudaEvent_t event = nullptr;                         // hwr_ops_after / before
     int test_stall = 0;                                  // HWR_TEST_STALL (see hwr_api.cu)
+    int test_device = 0;                                 // HWR_TEST_DEVICE: how far off the current device seems
     long fail_at = 0, allocs = 0;                        // HWR_TEST_FAIL_ALLOC
 };
 
@@ -87,10 +89,23 @@ static hwr_status cuda_fail(hwr_ops *c, cudaError_t e, const char *what) {
         if (s_ != HWR_OK) return s_;          \
     } while (0)
 
-static hwr_status ready(hwr_ops *c) {
+static hwr_status alive(hwr_ops *c) {
     if (c->broken) return fail(c, HWR_ERR_STATE, "context unusable after an earlier failure");
     if (*(volatile int32_t *)c->status_h != ST_OK)
         return fail(c, HWR_ERR_TIMEOUT, "a device-side wait of an earlier call gave up");
+    return HWR_OK;
+}
+
+// For calls that launch or allocate.
+static hwr_status ready(hwr_ops *c) {
+    OK(alive(c));
+    // (a launch on another device's stream would fail, and break the context)
+    int dev = c->device;
+    const cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return cuda_fail(c, e, "cudaGetDevice");
+    if (dev + c->test_device != c->device)
+        return fail(c, HWR_ERR_INVALID_ARG, "device %d is current, the context is of device %d", dev + c->test_device,
+                    c->device);
     return HWR_OK;
 }
 
@@ -160,9 +175,10 @@ extern "C" hwr_status hwr_ops_create(void *cuda_stream, hwr_ops **out) {
     if (!c) return fail(nullptr, HWR_ERR_OOM, "host allocation failed");
     if (const char *e = getenv("HWR_TEST_FAIL_ALLOC")) c->fail_at = atol(e);
     if (const char *e = getenv("HWR_TEST_STALL")) c->test_stall = atoi(e) != 0;
+    if (const char *e = getenv("HWR_TEST_DEVICE")) c->test_device = atoi(e);
     auto body = [&]() -> hwr_status {
-        int dev = 0;
-        CK(c, cudaGetDevice(&dev), "cudaGetDevice");
+        CK(c, cudaGetDevice(&c->device), "cudaGetDevice");
+        const int dev = c->device;
         CK(c, cudaDeviceGetAttribute(&c->nsm, cudaDevAttrMultiProcessorCount, dev), "device attribute");
         if (!g_encode) {
             void *fn = nullptr;
@@ -181,6 +197,7 @@ extern "C" hwr_status hwr_ops_create(void *cuda_stream, hwr_ops **out) {
             CK(c, cudaStreamCreateWithFlags(&c->stream, cudaStreamNonBlocking), "stream");
             c->own_stream = true;
         }
+        CK(c, cudaEventCreateWithFlags(&c->event, cudaEventDisableTiming), "event");
         CK(c, cudaHostAlloc((void **)&c->status_h, 64, cudaHostAllocMapped), "status word");
         memset(c->status_h, 0, 64);
         CK(c, cudaHostGetDevicePointer((void **)&c->status_d, c->status_h, 0), "status word");
@@ -225,7 +242,7 @@ extern "C" hwr_status hwr_ops_synchronize(hwr_ops *c) {
     if (!c) return HWR_ERR_INVALID_ARG;
     if (c->broken) return fail(c, HWR_ERR_STATE, "context unusable after an earlier failure");
     CK(c, cudaStreamSynchronize(c->stream), "synchronize");
-    return ready(c);
+    return alive(c);
 }
 
 extern "C" const char *hwr_ops_last_error(const hwr_ops *c) {
@@ -233,7 +250,6 @@ extern "C" const char *hwr_ops_last_error(const hwr_ops *c) {
 }
 
 static hwr_status order_streams(hwr_ops *c, cudaStream_t first, cudaStream_t then) {
-    if (!c->event) CK(c, cudaEventCreateWithFlags(&c->event, cudaEventDisableTiming), "event");
     CK(c, cudaEventRecord(c->event, first), "event record");
     CK(c, cudaStreamWaitEvent(then, c->event, 0), "stream wait");
     return HWR_OK;
@@ -241,7 +257,7 @@ static hwr_status order_streams(hwr_ops *c, cudaStream_t first, cudaStream_t the
 
 extern "C" hwr_status hwr_ops_after(hwr_ops *c, void *stream) {
     if (!c) return HWR_ERR_INVALID_ARG;
-    OK(ready(c));
+    OK(alive(c));
     if (!stream) return fail(c, HWR_ERR_INVALID_ARG, "NULL stream");
     if (c->stream == cudaStreamLegacy) {
         cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
@@ -256,7 +272,7 @@ extern "C" hwr_status hwr_ops_before(hwr_ops *c, void *stream) {
     if (!c) return HWR_ERR_INVALID_ARG;
     if (!stream) return fail(c, HWR_ERR_INVALID_ARG, "NULL stream");
     // (a broken context's work may still be running)
-    const hwr_status s = ready(c), o = order_streams(c, c->stream, (cudaStream_t)stream);
+    const hwr_status s = alive(c), o = order_streams(c, c->stream, (cudaStream_t)stream);
     return s != HWR_OK ? s : o;
 }
 

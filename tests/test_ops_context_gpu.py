@@ -37,3 +37,16 @@ def test_a_failed_call_is_ordered_too(ops):
     early, busy = done.query(), not ops.stream.query()
     torch.cuda.synchronize()
     assert busy and not early
+
+
+def test_another_current_device(monkeypatch):
+    """Refused before anything is launched, and nothing breaks.  (The test hook makes the
+    current device seem another one.)"""
+    monkeypatch.setenv("HWR_TEST_DEVICE", "1")
+    off = H.Operators()
+    monkeypatch.delenv("HWR_TEST_DEVICE")
+    for _ in range(2):
+        with pytest.raises(H.HwrError) as e:
+            off.dispatch(choices(10, 3, "any"), 3)
+        assert e.value.status == 1 and "device 1 is current" in str(e.value)
+    off.close()
