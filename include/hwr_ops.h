@@ -158,7 +158,8 @@ hwr_status hwr_clip_gradients(hwr_ops *ops, int32_t n, const hwr_gradient *grads
  * The same for gradients that stay where they are from step to step: create
  * lays their table out in device memory once (synchronises the stream); clip
  * reads and writes the arrays as they are at the call, which must still be
- * there.  destroy synchronises; NULL is fine.
+ * there.  destroy synchronises; NULL is fine.  A list goes with its context
+ * (hwr_ops_destroy), if not before.
  */
 typedef struct hwr_gradients hwr_gradients;
 hwr_status hwr_gradients_create(hwr_ops *ops, int32_t n, const hwr_gradient *grads,

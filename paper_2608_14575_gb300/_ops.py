@@ -141,7 +141,7 @@ class GradientList:
         self.handle = ops.native.list_create(ops.ctx, ops._current(), grads, out)
 
     def close(self):
-        if self.handle and self.ops.ctx:
+        if self.handle and self.ops.ctx:      # (a closed context has freed its lists)
             self.ops.native.list_destroy(self.ops.ctx, self.handle)
         self.handle = 0
 

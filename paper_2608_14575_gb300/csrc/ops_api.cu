@@ -38,6 +38,12 @@ struct Retired {
     Retired *next;
 };
 
+struct hwr_gradients {
+    ClipChunk *table = nullptr;
+    int chunks = 0, per = 1;
+    hwr_gradients *next = nullptr;      // of the context's lists
+};
+
 struct hwr_ops {
     cudaStream_t stream = nullptr;
     bool own_stream = false, broken = false;
@@ -48,6 +54,7 @@ struct hwr_ops {
     size_t ws_cap = 0;
     bool ws_held = false;        // a captured call has its address
     Retired *retired = nullptr;
+    hwr_gradients *lists = nullptr;
     float *part = nullptr;       // partial tiles of the grouped products
     uint32_t *count = nullptr;   // their arrivals (zeroed once, self-resetting)
     double *sums = nullptr;      // partial sums of squares; then their arrivals and the factor
@@ -222,6 +229,11 @@ extern "C" hwr_status hwr_ops_destroy(hwr_ops *c) {
     if (!c) return HWR_OK;
     if (c->stream) cudaStreamSynchronize(c->stream);
     cudaFree(c->ws);
+    while (hwr_gradients *l = c->lists) {
+        c->lists = l->next;
+        cudaFree(l->table);
+        delete l;
+    }
     while (Retired *r = c->retired) {
         c->retired = r->next;
         cudaFree(r->p);
@@ -862,11 +874,6 @@ extern "C" hwr_status hwr_adapter_backward(hwr_ops *c, const hwr_rows *r, const 
 
 // ---------------------------------------------------------------------------
 
-struct hwr_gradients {
-    ClipChunk *table = nullptr;
-    int chunks = 0, per = 1;
-};
-
 // Checks a list, and says into how many chunks of which size it is cut.
 static hwr_status check_gradients(hwr_ops *c, int32_t n, const hwr_gradient *grads, int64_t *chunks, int *per) {
     if (n < 0 || (n && !grads)) return fail(c, HWR_ERR_INVALID_ARG, "n %d or a NULL array", n);
@@ -963,6 +970,8 @@ extern "C" hwr_status hwr_gradients_create(hwr_ops *c, int32_t n, const hwr_grad
         delete l;
         return s;
     }
+    l->next = c->lists;
+    c->lists = l;
     *out = l;
     return HWR_OK;
 }
@@ -980,6 +989,10 @@ extern "C" hwr_status hwr_gradients_clip(hwr_ops *c, const hwr_gradients *l, flo
 extern "C" hwr_status hwr_gradients_destroy(hwr_ops *c, hwr_gradients *l) {
     if (!l) return HWR_OK;
     if (!c) return HWR_ERR_INVALID_ARG;
+    hwr_gradients **at = &c->lists;
+    while (*at && *at != l) at = &(*at)->next;
+    if (!*at) return fail(c, HWR_ERR_INVALID_ARG, "not a list of this context");
+    *at = l->next;
     cudaStreamSynchronize(c->stream);
     cudaFree(l->table);
     cudaGetLastError();

@@ -50,3 +50,27 @@ def test_another_current_device(monkeypatch):
             off.dispatch(choices(10, 3, "any"), 3)
         assert e.value.status == 1 and "device 1 is current" in str(e.value)
     off.close()
+
+
+def test_lists_go_with_their_context():
+    """A gradient list that outlives its closed context leaves no device memory behind."""
+    H.build()
+    grads = [torch.zeros(1 << 28, device="cuda", dtype=BF)]     # (a table of 1 MB)
+    norms = []
+
+    def cycle():
+        ops = H.Operators()
+        one, two = ops.gradient_list(grads), ops.gradient_list(grads)
+        norms.append(float(ops.clip_gradients(one, 1.0)) + float(ops.clip_gradients(two, 1.0)))
+        one.close()
+        ops.close()
+        two.close()
+    for _ in range(3):
+        cycle()
+    torch.cuda.synchronize()
+    before = torch.cuda.mem_get_info()[0]
+    for _ in range(40):
+        cycle()
+    torch.cuda.synchronize()
+    assert before - torch.cuda.mem_get_info()[0] < 8 << 20      # (40 MB if they stayed)
+    assert norms == [0.0] * 43
