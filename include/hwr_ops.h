@@ -35,9 +35,10 @@
  *     before; hwr_ops_reserve does that ahead of time.
  *   - Stream capture: calls can be captured into graphs.  A call that would have
  *     to grow the workspace then is refused (UNSUPPORTED, nothing is queued, the
- *     context stays usable): make a call of the same sizes before, or reserve.  A
- *     block that a captured call uses is kept until hwr_ops_destroy, also when a
- *     later call takes a larger one; the context outlives its graphs.  A replay
+ *     context stays usable): make a call of the same sizes before, or reserve.
+ *     So are hwr_ops_synchronize and hwr_gradients_create.  Workspace and lists of
+ *     gradients that a captured call uses are kept until hwr_ops_destroy, also when
+ *     a later call takes a larger block; the context outlives its graphs.  A replay
  *     uses the context's workspace, partial sums and counters as an eager call
  *     does: order it with the context's other work (the same stream, or
  *     hwr_ops_after / hwr_ops_before); two of them at a time spoil each other.

@@ -41,6 +41,7 @@ struct Retired {
 struct hwr_gradients {
     ClipChunk *table = nullptr;
     int chunks = 0, per = 1;
+    mutable bool held = false;          // a captured call has the table's address
     hwr_gradients *next = nullptr;      // of the context's lists
 };
 
@@ -253,6 +254,9 @@ extern "C" hwr_status hwr_ops_destroy(hwr_ops *c) {
 extern "C" hwr_status hwr_ops_synchronize(hwr_ops *c) {
     if (!c) return HWR_ERR_INVALID_ARG;
     if (c->broken) return fail(c, HWR_ERR_STATE, "context unusable after an earlier failure");
+    bool captured;
+    OK(capturing(c, &captured));
+    if (captured) return fail(c, HWR_ERR_UNSUPPORTED, "the stream is being captured");
     CK(c, cudaStreamSynchronize(c->stream), "synchronize");
     return alive(c);
 }
@@ -948,6 +952,9 @@ extern "C" hwr_status hwr_gradients_create(hwr_ops *c, int32_t n, const hwr_grad
     if (!out) return fail(c, HWR_ERR_INVALID_ARG, "out is NULL");
     *out = nullptr;
     OK(ready(c));
+    bool captured;
+    OK(capturing(c, &captured));
+    if (captured) return fail(c, HWR_ERR_UNSUPPORTED, "a list of gradients cannot be made during a stream capture");
     int64_t chunks;
     int per;
     OK(check_gradients(c, n, grads, &chunks, &per));
@@ -982,6 +989,9 @@ extern "C" hwr_status hwr_gradients_clip(hwr_ops *c, const hwr_gradients *l, flo
     OK(ready(c));
     if (!l) return fail(c, HWR_ERR_INVALID_ARG, "NULL list");
     OK(check_norm(c, max_norm, norm));
+    bool captured;
+    OK(capturing(c, &captured));
+    l->held = l->held || captured;
     CK(c, launch_clip(l->table, l->chunks, l->per, c->nsm, clip_sums(c), max_norm, norm, c->stream), "clip kernel");
     return HWR_OK;
 }
@@ -992,10 +1002,16 @@ extern "C" hwr_status hwr_gradients_destroy(hwr_ops *c, hwr_gradients *l) {
     hwr_gradients **at = &c->lists;
     while (*at && *at != l) at = &(*at)->next;
     if (!*at) return fail(c, HWR_ERR_INVALID_ARG, "not a list of this context");
+    bool captured;
+    OK(capturing(c, &captured));
+    if (captured || l->held) {          // (during a capture nothing is waited for or freed)
+        OK(retire(c, l->table));
+    } else {
+        cudaStreamSynchronize(c->stream);
+        cudaFree(l->table);
+        cudaGetLastError();
+    }
     *at = l->next;
-    cudaStreamSynchronize(c->stream);
-    cudaFree(l->table);
-    cudaGetLastError();
     delete l;
     return HWR_OK;
 }

@@ -100,3 +100,55 @@ def test_growing_in_a_capture_is_refused(side, mine):
             assert torch.equal(got, exact)
         for got, exact in zip(step(ops, *large), want(*large)):
             assert torch.equal(got, exact)
+
+
+def test_a_list_stays_under_its_graph(side):
+    """A gradient list that is closed after a capture leaves its table to the graph."""
+    ops, stream = side
+    grads = [ints(n, dt=torch.float32, seed=n) for n in (4000, 70_001, 33)]
+    out = [torch.zeros_like(g) for g in grads]
+    once = ops.gradient_list(grads, out)
+    ops.clip_gradients(once, 1.0)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        norm = ops.clip_gradients(once, 1.0)
+    once.close()
+    guard = [torch.full((1 << 16,), 7, device="cuda", dtype=torch.int8) for _ in range(64)]
+    others = [ops.gradient_list([torch.ones(50_000, device="cuda")]) for _ in range(8)]   # tables of their own
+    for k in range(3):
+        for i, g in enumerate(grads):
+            g.copy_(ints(g.numel(), dt=torch.float32, seed=10 * k + i))
+        graph.replay()
+        exact = sum(float(g.double().square().sum()) for g in grads) ** 0.5
+        assert abs(float(norm) - exact) <= exact * 2.0 ** -16
+        for g, o in zip(grads, out):
+            assert ((o.double() - g.double() / (exact + 1e-6)).abs() <= 2.0 ** -16 * g.double().abs() / exact).all()
+    assert all(bool((g == 7).all()) for g in guard)
+    for o in others:
+        o.close()
+
+
+def test_calls_that_wait_are_refused_in_a_capture(side):
+    """Making or closing a list and waiting for the stream; the capture and the context go on."""
+    ops, stream = side
+    g = torch.ones(5000, device="cuda")
+    once = ops.gradient_list([g.clone()])
+    small = layer(30)
+    step(ops, *small)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        plan = ops.dispatch(small[0], 5)
+        for refused in (lambda: ops.gradient_list([g]), ops.synchronize):
+            with pytest.raises(H.HwrError) as e:
+                refused()
+            assert e.value.status == UNSUPPORTED
+        once.close()
+        y = ops.adapter_forward(*small[1:5], small[6], plan)
+    graph.replay()
+    assert torch.equal(y, want(*small)[0])
+    ops.synchronize()
+    again = ops.gradient_list([g])
+    assert abs(float(ops.clip_gradients(again, 1.0)) - 5000 ** 0.5) < 1e-3
+    again.close()
