@@ -18,6 +18,12 @@ contiguous; other strides are free.  The context is bound to the torch stream
 that is current when it is made.  A call made under another current stream is
 ordered after that stream's work so far, and that stream after the call.
 
+Nothing is recorded for autograd: results have no gradient function, whatever the
+inputs require, and the ``_backward`` calls are made by hand (or from a
+``torch.autograd.Function`` of the caller's).  Tensors that a call writes in place
+(``out``, clipped gradients) count as modified, so that autograd notices where it
+had saved them.
+
 Calls can be captured into CUDA graphs once the workspace is large enough: after
 a call of the same sizes, or ``reserve`` (a capture in which it would have to grow
 raises HwrError).  What a graph uses of the workspace stays until ``close``.  A
@@ -214,7 +220,7 @@ class Operators:
         if isinstance(grads, GradientList):
             if out is not None or grads.ops is not self or not grads.handle:
                 raise ValueError("a gradient list has its outputs, its context, and is open")
-            return self.native.list_clip(self.ctx, self._current(), grads.handle, max_norm)
+            return self.native.list_clip(self.ctx, self._current(), grads.handle, max_norm, grads.out)
         grads = list(grads)
         return self.native.clip(self.ctx, self._current(), grads,
                                 grads if out is None else list(out), max_norm)

@@ -174,6 +174,15 @@ void call(Context &c, PyObject *raw, F f) {
     if (other) check(hwr_ops_before(c.ops, current ? current : (void *)1));
 }
 
+// Tell autograd that the call has written a tensor of the caller's.
+void written(const at::Tensor &t) {
+    if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
+
+void all_written(PyObject *list) {
+    for (Py_ssize_t i = 0; i < PyList_GET_SIZE(list); ++i) written(tensor(PyList_GET_ITEM(list, i), "output"));
+}
+
 PyObject *wrap(at::Tensor t) {
     PyObject *o = THPVariable_Wrap(std::move(t));
     if (!o) throw PythonError();
@@ -324,6 +333,7 @@ PyObject *grouped_forward(PyObject *, PyObject *const *a, Py_ssize_t n) {
         int64_t ld;
         at::Tensor y = output(c, a[6], r.rows, r.n_out, x, &ld);
         call(c, a[1], [&] { return hwr_grouped_forward(c.ops, &r, y.data_ptr(), ld); });
+        if (a[6] != Py_None) written(y);
         return wrap(std::move(y));
     });
 }
@@ -381,6 +391,7 @@ PyObject *adapter_forward(PyObject *, PyObject *const *a, Py_ssize_t n) {
         int64_t ld;
         at::Tensor y = output(c, a[9], r.rows, r.n_out, x, &ld);
         call(c, a[1], [&] { return hwr_adapter_forward(c.ops, &r, &ad, y.data_ptr(), ld); });
+        if (a[9] != Py_None) written(y);
         return wrap(std::move(y));
     });
 }
@@ -458,6 +469,7 @@ PyObject *clip(PyObject *, PyObject *const *a, Py_ssize_t n) {
         const int count = narrow((int64_t)v.size(), "gradients");
         at::Tensor norm = scalar(c);
         call(c, a[1], [&] { return hwr_clip_gradients(c.ops, count, v.data(), max_norm, (float *)norm.data_ptr()); });
+        all_written(a[3]);
         return wrap(std::move(norm));
     });
 }
@@ -475,15 +487,17 @@ PyObject *list_create(PyObject *, PyObject *const *a, Py_ssize_t n) {
     });
 }
 
-// handle, max_norm -> norm
+// handle, max_norm, the list's outputs -> norm
 PyObject *list_clip(PyObject *, PyObject *const *a, Py_ssize_t n) {
     return guarded([&] {
-        want(n, 4);
+        want(n, 5);
+        if (!PyList_Check(a[4])) throw TypeError("want a list of tensors");
         Context &c = context(a[0]);
         const hwr_gradients *l = (const hwr_gradients *)address(a[2]);
         const float max_norm = (float)number(a[3]);
         at::Tensor norm = scalar(c);
         call(c, a[1], [&] { return hwr_gradients_clip(c.ops, l, max_norm, (float *)norm.data_ptr()); });
+        all_written(a[4]);
         return wrap(std::move(norm));
     });
 }

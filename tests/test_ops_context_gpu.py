@@ -74,3 +74,32 @@ def test_lists_go_with_their_context():
     torch.cuda.synchronize()
     assert before - torch.cuda.mem_get_info()[0] < 8 << 20      # (40 MB if they stayed)
     assert norms == [0.0] * 43
+
+
+def test_written_tensors_count_as_modified(ops):
+    """Autograd sees what a call writes into a tensor of the caller's."""
+    for lists in (False, True):
+        for place in (False, True):
+            grads = [torch.ones(n, device="cuda") for n in (5, 70_000)]
+            out = grads if place else [torch.empty_like(g) for g in grads]
+            it = ops.gradient_list(grads, None if place else out) if lists else grads
+            before = [g._version for g in grads], [o._version for o in out]
+            ops.clip_gradients(it, 1.0, **({} if lists or place else {"out": out}))
+            assert all(o._version > v for o, v in zip(out, before[1]))
+            assert place or [g._version for g in grads] == before[0]
+    t = torch.ones(100, device="cuda", requires_grad=True)
+    z = t.exp()                                             # saved for the backward pass
+    ops.clip_gradients([z.detach()], 1.0)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        z.sum().backward()
+    c, x, w = choices(10, 3, "any"), ints(10, 16), ints(3, 24, 16)
+    a, b, s = ints(3, 4, 16), ints(3, 24, 4), torch.ones(3, device="cuda")
+    plan = ops.dispatch(c, 3)
+    for call in (lambda y: ops.grouped_forward(x, w, plan, out=y),
+                 lambda y: ops.adapter_forward(x, w[0], a, b, s, plan, out=y)):
+        y = torch.empty(10, 24, device="cuda", dtype=BF)
+        v = y._version
+        assert call(y) is y and y._version > v
+    with torch.inference_mode():                            # (no version to count)
+        g = torch.ones(10, device="cuda")
+        ops.clip_gradients([g], 1.0)
