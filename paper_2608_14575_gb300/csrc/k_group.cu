@@ -678,9 +678,10 @@ k_group(const __grid_constant__ Launch<KIND >= K_LOW ? 2 : 1> launch) {
         __syncwarp();
     } else if (warp == 11) {
         // Tells the even CTA that a stage's picked rows are here.  They are copied
-        // by threads: the fence makes them visible to the tensor cores' proxy.  (A
-        // picking thread cannot: its fence would wait for all of its copies in
-        // flight, 1.75 us a stage.  The MMA thread spent 0.2 us a stage on it.)
+        // by threads: the first fence makes them visible to the tensor cores' proxy, the
+        // second to the even CTA's MMA thread.  (A picking thread cannot: its fence
+        // would wait for all of its copies in flight, 1.75 us a stage.  The MMA
+        // thread spent 0.2 us a stage on it.)
         if (lane == 0 && !p.sorted) {
             const uint32_t full0 = smem_of(&t.full[0], 0);
             Ring at(p.stages);
@@ -690,6 +691,7 @@ k_group(const __grid_constant__ Launch<KIND >= K_LOW ? 2 : 1> launch) {
                 ok = mbar_wait(&t.rowsf[at.s], at.ph, abort_f, p.status);
                 if (!ok) return false;
                 fence_proxy_async_smem();
+                fence_release_smem();
                 mbar_arrive_cluster(full0 + at.s * 8);
                 at.step();
                 return true;
@@ -802,7 +804,12 @@ k_group(const __grid_constant__ Launch<KIND >= K_LOW ? 2 : 1> launch) {
             const bool b_mn = grad || (!grad && !grouped && p.dense_mn);
             // both CTAs' operands have landed
             auto stage_ready = [&]() {
-                if (!mbar_wait(&t.full[at.s], at.ph, abort_f, p.status)) return false;
+                if (p.sorted) {
+                    if (!mbar_wait(&t.full[at.s], at.ph, abort_f, p.status)) return false;
+                } else {
+                    if (!mbar_wait<true>(&t.full[at.s], at.ph, abort_f, p.status)) return false;
+                    fence_acquire_smem();
+                }
                 tc_fence_after();
                 return true;
             };
@@ -814,7 +821,7 @@ k_group(const __grid_constant__ Launch<KIND >= K_LOW ? 2 : 1> launch) {
                 const uint32_t d = tmem + b * CS;
                 const int N = grouped ? up16(w.count) : p.bn;
                 const uint32_t idesc = idesc_16bit(GP_TILE, N, F16, a_mn, b_mn);
-                ok = mbar_wait(&t.acce[b], ((lt >> 1) & 1) ^ 1, abort_f, p.status);
+                ok = mbar_wait<true>(&t.acce[b], ((lt >> 1) & 1) ^ 1, abort_f, p.status);
                 if (!ok) break;
                 tc_fence_after();
                 for (int kb = w.k0; kb < w.k1; ++kb, at.step()) {

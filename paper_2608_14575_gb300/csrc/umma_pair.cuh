@@ -50,12 +50,23 @@ __device__ __forceinline__ uint32_t smem_of(const void *p, uint32_t rank) {
     return a;
 }
 
-// Arrive on a barrier of any CTA of the cluster (address from smem_of).  What
-// it announces is read by the pair's MMAs alone, each SM's from its own shared
-// memory and TMEM, so CTA scope does; a cluster-scope release waits for a round
-// trip to L2 (0.5 to 1 us in a stage's loop).
+// Arrive on a barrier of any CTA of the cluster (address from smem_of).  It
+// orders execution alone (waited for with mbar_wait<true>), which is all that
+// tensor memory needs between the tcgen05 fences of both sides.  Shared memory
+// written by threads needs the two fences below too.  (An arrival that releases
+// covers global memory and waits a round trip to L2: 64 rows through 12 experts of
+// 1,024 x 4,096 took 32 us with it, 27 with the fences.)
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t addr) {
-    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(addr) : "memory");
+    asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(addr) : "memory");
+}
+
+// Before such an arrival: what this CTA's shared memory holds by then, for those
+// who wait.  After the wait: what the cluster's CTAs have released so.
+__device__ __forceinline__ void fence_release_smem() {
+    asm volatile("fence.release.sync_restrict::shared::cta.cluster;" ::: "memory");
+}
+__device__ __forceinline__ void fence_acquire_smem() {
+    asm volatile("fence.acquire.sync_restrict::shared::cluster.cluster;" ::: "memory");
 }
 
 // Tiled 3-D load into this CTA's shared memory that completes its bytes on a
