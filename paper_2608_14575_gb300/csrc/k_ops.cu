@@ -16,14 +16,16 @@ namespace {
 // that share a key find each other by votes over the warp, so a row's place
 // is its key's first place (over the blocks, rounds and warps before it) plus
 // the peers in lower lanes: no atomics decide an order.  What the blocks before
-// hold of each key comes from shared memory within a cluster (up to DP_CLUSTER
-// blocks, one launch) or from a counting pass before (more).  All of it is
+// hold of each key comes from shared memory within a cluster (up to its blocks,
+// one launch) or from a counting pass before (more).  All of it is
 // bound by latency: 4 MB of choices are read and written in 1.2 us.
 
 constexpr int DP_THREADS = 512, DP_WARPS = DP_THREADS / 32;
 constexpr int DP_PER = 8;
 constexpr int DP_ROWS = DP_THREADS * DP_PER;
-constexpr int DP_CLUSTER = 16;   // (more than 8 is the non-portable size)
+// Blocks of a cluster: 16, the non-portable size, where the device can place so many
+// (of a part of a GPU it may not), else 8.
+constexpr int DP_CLUSTER = 16, DP_CLUSTER_LEAST = 8;
 constexpr int DP_FEW = 256;      // rows whose places are counted row against row
 
 __device__ __forceinline__ void pdl_begin() {
@@ -93,6 +95,7 @@ __device__ __forceinline__ void cluster_barrier() {
 
 // Rows of each key in the blocks of a cluster before each of its blocks: hist
 // [blocks][G + 1]; then those of each whole cluster: [clusters][G + 1].
+template <int CLUSTER>
 __global__ void __launch_bounds__(DP_THREADS)
 k_dispatch_count(int rows, int G, int64_t per_block, const int32_t *choice, int32_t *hist) {
     extern __shared__ int32_t sh[];
@@ -113,26 +116,26 @@ k_dispatch_count(int rows, int G, int64_t per_block, const int32_t *choice, int3
         }
     }
     cluster_barrier();
-    const int rank = blockIdx.x % DP_CLUSTER;
+    const int rank = blockIdx.x % CLUSTER;
     for (int g = tid; g < G1; g += DP_THREADS) {
         int before = 0, all = 0;
 #pragma unroll
-        for (int b = 0; b < DP_CLUSTER; ++b) {
+        for (int b = 0; b < CLUSTER; ++b) {
             const int c = remote_int(&sh[g], b);
             before += b < rank ? c : 0;
             all += c;
         }
         hist[(int64_t)blockIdx.x * G1 + g] = before;
-        if (rank == 0) hist[((int64_t)gridDim.x + blockIdx.x / DP_CLUSTER) * G1 + g] = all;
+        if (rank == 0) hist[((int64_t)gridDim.x + blockIdx.x / CLUSTER) * G1 + g] = all;
     }
     cluster_barrier();       // the others may still read this block's counts
 }
 
-// hist: from k_dispatch_count, of `counted` blocks; null with one block, or with
-// one cluster of blocks of a round each.
+// hist: from k_dispatch_count, of `counted` blocks in clusters of `cluster`; null with
+// one block, or with one cluster of blocks of a round each.
 __global__ void __launch_bounds__(DP_THREADS)
 k_dispatch_place(int rows, int G, int64_t per_block, const int32_t *choice, const int32_t *hist, int counted,
-                 int32_t *offsets, int32_t *order) {
+                 int cluster, int32_t *offsets, int32_t *order) {
     extern __shared__ int32_t sh[];
     const int G1 = G + 1, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, nb = gridDim.x;
     const int nbits = 32 - __clz(G + 1);
@@ -172,7 +175,7 @@ k_dispatch_place(int rows, int G, int64_t per_block, const int32_t *choice, cons
         if (hist && r0 == begin) {
             // rows of each key in the blocks before this one, and in all
             pdl_begin();
-            const int clusters = counted / DP_CLUSTER, mine = blockIdx.x / DP_CLUSTER;
+            const int clusters = counted / cluster, mine = blockIdx.x / cluster;
             for (int g = tid; g < G1; g += DP_THREADS) {
                 int before = hist[(int64_t)blockIdx.x * G1 + g], all = 0;
 #pragma unroll 8
@@ -710,12 +713,29 @@ k_clip(const ClipChunk *table, int chunks, const float *factor) {
 
 }  // namespace
 
-cudaError_t ops_prepare() {
+cudaError_t ops_prepare(int *cluster) {
     const auto attr = cudaFuncAttributeMaxDynamicSharedMemorySize;
+    const auto wide = cudaFuncAttributeNonPortableClusterSizeAllowed;
     cudaError_t e = cudaFuncSetAttribute(k_dispatch_place, attr, (int)place_smem(OPS_MAX_GROUPS));
-    if (e == cudaSuccess) e = cudaFuncSetAttribute(k_dispatch_place, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
-    if (e == cudaSuccess) e = cudaFuncSetAttribute(k_dispatch_count, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
-    return e;
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(k_dispatch_place, wide, 1);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(k_dispatch_count<DP_CLUSTER>, wide, 1);
+    if (e != cudaSuccess) return e;
+    // (the larger of the two kernels)
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = DP_CLUSTER;
+    at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+    cfg.gridDim = dim3(DP_CLUSTER);
+    cfg.blockDim = dim3(DP_THREADS);
+    cfg.dynamicSmemBytes = place_smem(OPS_MAX_GROUPS);
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    int fit = 0;
+    e = cudaOccupancyMaxActiveClusters(&fit, k_dispatch_place, &cfg);
+    if (e != cudaSuccess) cudaGetLastError();        // (a size that the device does not have)
+    *cluster = e == cudaSuccess && fit > 0 ? DP_CLUSTER : DP_CLUSTER_LEAST;
+    return cudaSuccess;
 }
 
 // Blocks and rows per block of a dispatch: whole rounds, two blocks an SM at most.
@@ -727,11 +747,11 @@ static int dispatch_blocks(int rows, int nsm, int64_t *per_block) {
     return b < 1 ? 1 : (int)b;
 }
 
-size_t dispatch_scratch_ints(int rows, int groups, int nsm) {
+size_t dispatch_scratch_ints(int rows, int groups, int nsm, int cluster) {
     int64_t per;
     const int b = dispatch_blocks(rows, nsm, &per);
-    const int counted = (b + DP_CLUSTER - 1) / DP_CLUSTER * DP_CLUSTER;
-    return b > DP_CLUSTER ? (size_t)(counted + counted / DP_CLUSTER) * (groups + 1) : 0;
+    const int counted = (b + cluster - 1) / cluster * cluster;
+    return b > cluster ? (size_t)(counted + counted / cluster) * (groups + 1) : 0;
 }
 
 // A launch that may begin while the kernel before it ends (it waits by itself).
@@ -749,7 +769,7 @@ static cudaLaunchConfig_t relaxed(int grid, int block, size_t smem, cudaStream_t
 }
 
 cudaError_t launch_dispatch(int rows, int groups, const int32_t *choice, int32_t *offsets, int32_t *order,
-                            int32_t *scratch, int nsm, cudaStream_t s) {
+                            int32_t *scratch, int nsm, int cluster, cudaStream_t s) {
     cudaLaunchAttribute at[2];
     if (rows <= DP_FEW) {
         const cudaLaunchConfig_t cfg = relaxed(1, DP_FEW, 0, s, at);
@@ -757,20 +777,22 @@ cudaError_t launch_dispatch(int rows, int groups, const int32_t *choice, int32_t
     }
     int64_t per;
     const int b = dispatch_blocks(rows, nsm, &per);
-    const int32_t *hist = b > DP_CLUSTER ? scratch : nullptr;
-    const int counted = (b + DP_CLUSTER - 1) / DP_CLUSTER * DP_CLUSTER;
+    const int32_t *hist = b > cluster ? scratch : nullptr;
+    const int counted = (b + cluster - 1) / cluster * cluster;
     at[1].id = cudaLaunchAttributeClusterDimension;
-    at[1].val.clusterDim.x = hist ? DP_CLUSTER : b;
+    at[1].val.clusterDim.x = hist ? cluster : b;
     at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
     if (hist) {
         cudaLaunchConfig_t cfg = relaxed(counted, DP_THREADS, (groups + 1) * 4, s, at);
         cfg.numAttrs = 2;
-        const cudaError_t e = cudaLaunchKernelEx(&cfg, k_dispatch_count, rows, groups, per, choice, scratch);
+        const cudaError_t e = cluster == DP_CLUSTER
+            ? cudaLaunchKernelEx(&cfg, k_dispatch_count<DP_CLUSTER>, rows, groups, per, choice, scratch)
+            : cudaLaunchKernelEx(&cfg, k_dispatch_count<DP_CLUSTER_LEAST>, rows, groups, per, choice, scratch);
         if (e != cudaSuccess) return e;
     }
     cudaLaunchConfig_t cfg = relaxed(b, DP_THREADS, place_smem(groups), s, at);
     if (!hist && b > 1) cfg.numAttrs = 2;
-    return cudaLaunchKernelEx(&cfg, k_dispatch_place, rows, groups, per, choice, hist, counted, offsets, order);
+    return cudaLaunchKernelEx(&cfg, k_dispatch_place, rows, groups, per, choice, hist, counted, cluster, offsets, order);
 }
 
 cudaError_t launch_sort_rows(const GroupPlan &plan, const SortRows &m, int places, int32_t *padded_offsets,

@@ -50,6 +50,7 @@ struct hwr_ops {
     bool own_stream = false, broken = false;
     int device = 0;
     int nsm = 1, ctas = 2;       // SMs; CTAs of the grouped products
+    int cluster = 8;             // blocks of a dispatch's clusters (test hook HWR_TEST_SMALL_CLUSTERS: 8)
     std::string err;
     char *ws = nullptr;
     size_t ws_cap = 0;
@@ -198,7 +199,8 @@ extern "C" hwr_status hwr_ops_create(void *cuda_stream, hwr_ops **out) {
             g_encode = (PFN_cuTensorMapEncodeTiled_v12000)fn;
         }
         CK(c, group_prepare(c->nsm, &c->ctas), "kernel attributes");
-        CK(c, ops_prepare(), "kernel attributes");
+        CK(c, ops_prepare(&c->cluster), "kernel attributes");
+        if (getenv("HWR_TEST_SMALL_CLUSTERS")) c->cluster = 8;
         if (cuda_stream) {
             c->stream = (cudaStream_t)cuda_stream;
         } else {
@@ -309,9 +311,9 @@ extern "C" hwr_status hwr_dispatch(hwr_ops *c, int32_t rows, int32_t groups, con
     if (groups > OPS_MAX_GROUPS)
         return fail(c, HWR_ERR_UNSUPPORTED, "groups %d > %d", groups, OPS_MAX_GROUPS);
     if (!offsets || (rows && (!choice || !order))) return fail(c, HWR_ERR_INVALID_ARG, "NULL array");
-    const size_t ints = dispatch_scratch_ints(rows, groups, c->nsm);
+    const size_t ints = dispatch_scratch_ints(rows, groups, c->nsm, c->cluster);
     OK(reserve(c, ints * 4));
-    CK(c, launch_dispatch(rows, groups, choice, offsets, order, (int32_t *)c->ws, c->nsm, c->stream),
+    CK(c, launch_dispatch(rows, groups, choice, offsets, order, (int32_t *)c->ws, c->nsm, c->cluster, c->stream),
        "dispatch kernel");
     return HWR_OK;
 }

@@ -129,10 +129,10 @@ cudaError_t launch_few_rows(const FewRows &p, bool f16, cudaStream_t s);
 
 // ---- dispatch, clipping, padding (k_ops.cu) ---------------------------------
 
-cudaError_t ops_prepare();
-size_t dispatch_scratch_ints(int rows, int groups, int nsm);
+cudaError_t ops_prepare(int *cluster);       // blocks of a dispatch's clusters
+size_t dispatch_scratch_ints(int rows, int groups, int nsm, int cluster);
 cudaError_t launch_dispatch(int rows, int groups, const int32_t *choice, int32_t *offsets,
-                            int32_t *order, int32_t *scratch, int nsm, cudaStream_t s);
+                            int32_t *order, int32_t *scratch, int nsm, int cluster, cudaStream_t s);
 
 // Rows of up to two matrices by place: dst[p] = src[order[p]], zeros where the
 // order holds no row.  With padded_offsets (groups + 2 ints) the places are

@@ -103,3 +103,17 @@ def test_written_tensors_count_as_modified(ops):
     with torch.inference_mode():                            # (no version to count)
         g = torch.ones(10, device="cuda")
         ops.clip_gradients([g], 1.0)
+
+
+@pytest.mark.parametrize("T", [4097, 32_768, 32_769, 65_536, 65_537, 300_001])
+@pytest.mark.parametrize("G", [1, 64, 1024])
+def test_dispatch_where_clusters_of_16_do_not_fit(monkeypatch, T, G):
+    """With clusters of the portable size (the test hook): the same plan."""
+    monkeypatch.setenv("HWR_TEST_SMALL_CLUSTERS", "1")
+    small = H.Operators()
+    monkeypatch.delenv("HWR_TEST_SMALL_CLUSTERS")
+    c = choices(T, G, "holes")
+    offsets, order = R.dispatch(c, G)
+    plan = small.dispatch(c, G)
+    assert torch.equal(plan.order.cpu(), order.cpu()) and torch.equal(plan.offsets.cpu(), offsets)
+    small.close()
