@@ -557,8 +557,20 @@ __device__ __noinline__ double wide_squares(const void *in, int n, bool vec) {
     return s;
 }
 
+// A running sum as two fp32 values, the second what the first's roundings lost
+// (exactly, so the pair holds some 48 bits however many chunks a thread walks; the
+// GPU's few 64-bit units would take longer than the reads).
+struct Pair {
+    float hi, lo;
+    __device__ __forceinline__ void add(float v) {
+        const float t = hi + v, b = t - hi;
+        lo += (hi - (t - b)) + (v - b);
+        hi = t;
+    }
+};
+
 template <int DT, int CL_PER>
-__device__ __forceinline__ void sum_chunk(const ClipChunk &c, float &acc, double &wide) {
+__device__ __forceinline__ void sum_chunk(const ClipChunk &c, Pair &acc, double &wide) {
     constexpr int N = Vec<DT>::N;
     const bool vec = c.n == CL_PER * Vec<DT>::FULL && ((uintptr_t)c.in & 15) == 0;
     float s = 0.f;
@@ -588,7 +600,7 @@ __device__ __forceinline__ void sum_chunk(const ClipChunk &c, float &acc, double
         }
         if (!any) return;
     }
-    if (s >= 1e-30f && s <= 1e30f) acc += s;
+    if (s >= 1e-30f && s <= 1e30f) acc.add(s);
     else wide += wide_squares<DT, CL_PER>(c.in, c.n, vec);      // NaN and infinities too
 }
 
@@ -616,16 +628,16 @@ __device__ __forceinline__ void scale_chunk(const ClipChunk &c, float k) {
     for (int i = threadIdx.x; i < c.n; i += CL_THREADS) Vec<DT>::store(c.out, i, Vec<DT>::load(c.in, i) * k);
 }
 
-// Sum of fp32 values over the warp, in lane 0 as a double.  (The GPU has few
-// 64-bit units: a reduction of doubles by every warp cost more than the reads.)
-__device__ __forceinline__ double warp_sum(float v, double wide) {
-    for (int d = 16; d; d /= 2) v += __shfl_down_sync(0xffffffffu, v, d);
-    double s = v;
-    if (__any_sync(0xffffffffu, wide != 0.0)) {
-        for (int d = 16; d; d /= 2) wide += __shfl_down_sync(0xffffffffu, wide, d);
-        s += wide;
+// Sums over the warp, in lane 0.  (Tested by its bits: comparing doubles in every
+// thread would take the few 64-bit units a microsecond.)
+__device__ __forceinline__ void warp_sum(Pair &v, double &wide) {
+    for (int d = 16; d; d /= 2) {
+        const float hi = __shfl_down_sync(0xffffffffu, v.hi, d), lo = __shfl_down_sync(0xffffffffu, v.lo, d);
+        v.add(hi);
+        v.lo += lo;
     }
-    return s;
+    if (__any_sync(0xffffffffu, __double_as_longlong(wide) != 0))
+        for (int d = 16; d; d /= 2) wide += __shfl_down_sync(0xffffffffu, wide, d);
 }
 
 // The table's entries of up to CLIP_TABLE tensors (kernel parameters), from
@@ -649,9 +661,10 @@ template <int PER>
 __global__ void __launch_bounds__(CL_THREADS)
 k_square_sums(const ClipChunk *table, int chunks, ClipSums sums, float max_norm, float *norm) {
     __shared__ double w[CL_THREADS / 32];
+    __shared__ Pair narrow[CL_THREADS / 32];
     __shared__ bool last;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    float acc = 0.f;
+    Pair acc = {0.f, 0.f};
     double wide = 0;
     pdl_begin();
     int i = blockIdx.x;
@@ -664,12 +677,21 @@ k_square_sums(const ClipChunk *table, int chunks, ClipSums sums, float max_norm,
         else if (now.dtype == HWR_BF16) sum_chunk<HWR_BF16, PER>(now, acc, wide);
         else sum_chunk<HWR_F16, PER>(now, acc, wide);
     }
-    const double s = warp_sum(acc, wide);
-    if (lane == 0) w[warp] = s;
+    warp_sum(acc, wide);
+    if (lane == 0) {
+        narrow[warp] = acc;
+        w[warp] = wide;
+    }
     __syncthreads();
     if (threadIdx.x == 0) {
+        Pair n = {0.f, 0.f};
         double b = 0;
-        for (int k = 0; k < CL_THREADS / 32; ++k) b += w[k];
+        for (int k = 0; k < CL_THREADS / 32; ++k) {
+            n.add(narrow[k].hi);
+            n.lo += narrow[k].lo;
+            if (__double_as_longlong(w[k]) != 0) b += w[k];
+        }
+        b += (double)n.hi + n.lo;
         sums.part[blockIdx.x] = b;
         __threadfence();
         last = atomicAdd(sums.count, 1u) == gridDim.x - 1;
