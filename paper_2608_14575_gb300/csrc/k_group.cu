@@ -1141,11 +1141,13 @@ k_group(const __grid_constant__ Launch<KIND >= K_LOW ? 2 : 1> launch) {
                 } else if (pack) {
                     // 32 ranks of an inner product: value = high + low term, to about
                     // twice the type's precision; an infinite high term takes a zero
-                    // low one (not inf - inf)
+                    // low one (not inf - inf).  A place without a row (padding) has
+                    // zeros, also where the adapter's values make a NaN of them
                     const float sc = p.scale[w.g];
+                    const bool row_there = mine && t.rows[r] >= 0;
 #pragma unroll
                     for (int j = 0; j < 32; ++j) {
-                        v[j] = c + j < p.n ? v[j] * sc : 0.f;
+                        v[j] = row_there && c + j < p.n ? v[j] * sc : 0.f;
                         const float hi = widen<F16>((uint16_t)pack2<F16>(v[j], 0.f));
                         prev[j] = isinf(hi) ? 0.f : v[j] - hi;
                     }
