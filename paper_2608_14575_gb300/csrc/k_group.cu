@@ -19,7 +19,11 @@
 // group with rows in the tile, the tile's rows of u (two 16-bit terms a value)
 // times the group's [n][rank] matrix are accumulated with the MMA's row mask
 // into that group's rows only; no value of one group's matrix ever meets
-// another group's rows.
+// another group's rows.  The terms are bf16 whatever the rows' type: they hold 16
+// bits at any magnitude, where fp16's would overflow above 65,504 and lose bits
+// below 2^-3; an fp16 matrix is then taken as two bf16 terms too (exactly), one
+// after the other.  In the gradients of fp16 rows an inner product meets fp16 rows,
+// so its terms are fp16, scaled by a power of two of each group's own.
 //
 // The iterations (stages of the contraction) of all tiles are dealt evenly:
 // whole tiles first, one to a pair a round, then the tiles of the last rounds
@@ -114,9 +118,11 @@ static_assert(OUT_PITCH % 16 == 0 && OUT_BYTES % 16 == 0 && offsetof(Tables, out
 
 // A group's matrix in an extension stage of one CTA: 32 ranks of blocks of 64
 // columns (MN-major), or rows of 32 or, with a small rank, 16 ranks.
-__host__ __device__ inline int ext_bytes(const GroupProduct &p) {
+__host__ __device__ inline int ext_bytes(const GroupProduct &p) {      // (of one term)
     return p.dense_mn ? (p.bn / 2 + 63) / 64 * 4096 : p.bn / 2 * (p.rank <= 16 ? 32 : 64);
 }
+
+__host__ __device__ inline int ext_terms(const GroupProduct &p) { return p.f16 ? 2 : 1; }
 
 __host__ __device__ inline int table_bytes(const GroupProduct &p) {
     const int g = p.plan.groups + 1;
@@ -270,7 +276,7 @@ struct Walk {
         return p.mode == GP_ROWS && p.shared ? p.bn * max(1, min(t.offs[1], 128)) * (1.f / 128) : p.bn;
     }
     // The extension's steps in all of a shared product's tiles, about a block each.
-    __device__ int64_t ext_work() const { return (int64_t)t.nseg * ext_steps(p) * p.ntiles; }
+    __device__ int64_t ext_work() const { return (int64_t)t.nseg * ext_steps(p) * ext_terms(p) * p.ntiles; }
     __device__ bool next(Work &w) {
         const bool grad = p.mode == GP_WGRAD;
         w.e0 = 0;
@@ -571,6 +577,7 @@ k_group(const __grid_constant__ Launch<KIND >= K_LOW ? 2 : 1> launch) {
     constexpr bool grad = KIND == K_GRAD || KIND == K_LOW;
     constexpr bool grouped = KIND == K_GROUPED, shared = KIND == K_SHARED, low = KIND == K_LOW;
     constexpr bool pack = KIND == K_PACK || KIND == K_PACKS;
+    constexpr int TERMS = F16 ? 2 : 1;      // of the extension's matrices
     constexpr int CS = GP_TILE;      // TMEM columns of one of the two accumulators
 
     if (threadIdx.x == 0) {
@@ -774,19 +781,21 @@ k_group(const __grid_constant__ Launch<KIND >= K_LOW ? 2 : 1> launch) {
                 if (shared && ok)
                     for (Ext e(p, t, w); e.more(); e.step(), at.step()) {
                         const int n = e.here(), r0 = e.rank0();
-                        if (!claim(2 * n * ebytes + xbytes)) break;
+                        if (!claim(2 * n * TERMS * ebytes + xbytes)) break;
                         uint8_t *st = sm + (size_t)at.s * p.stage_bytes;
                         for (int b = 0; b < boxes; ++b)
                             tma_load_3d_pair(st + b * GP_ROW_BOX * 128, &maps.u, full0 + at.s * 8, r0 * 2,
                                              x0 + b * GP_ROW_BOX, 0);
-                        for (int q = 0; q < n; ++q) {
+                        for (int q = 0; q < n * TERMS; ++q) {
                             uint8_t *eb = st + p.b_off + q * ebytes;
-                            const int g = e.group(q);
+                            const int g = e.group(q / TERMS), term = q % TERMS;
                             if (p.dense_mn)
                                 for (int b = 0; b < blocks; ++b)
-                                    tma_load_3d_pair(eb + b * 4096, &maps.eb, full0 + at.s * 8, o0 + b * 64, r0, g);
+                                    tma_load_3d_pair(eb + b * 4096, &maps.eb, full0 + at.s * 8, o0 + b * 64,
+                                                     r0 * TERMS + term * GP_RC, g);
                             else
-                                tma_load_3d_pair(eb, &maps.eb, full0 + at.s * 8, r0, o0, g);
+                                tma_load_3d_pair(eb, &maps.eb, full0 + at.s * 8,
+                                                 r0 * TERMS + term * (p.rank <= 16 ? 16 : GP_RC), o0, g);
                         }
                     }
             }
@@ -843,7 +852,7 @@ k_group(const __grid_constant__ Launch<KIND >= K_LOW ? 2 : 1> launch) {
                 }
                 if (!ok) break;
                 if (shared) {
-                    const uint32_t eidesc = idesc_16bit(GP_TILE, p.bn, F16, false, p.dense_mn), ebytes = ext_bytes(p);
+                    const uint32_t eidesc = idesc_16bit(GP_TILE, p.bn, false, false, p.dense_mn), ebytes = ext_bytes(p);
                     const uint64_t bdesc0 = p.dense_mn ? sdesc(0, 4096, 1024, 2)
                                             : p.rank <= 16 ? sdesc(0, 0, 256, 6) : sdesc(0, 0, 512, 4);
                     for (Ext e(p, t, w); e.more(); e.step(), at.step()) {
@@ -868,12 +877,15 @@ k_group(const __grid_constant__ Launch<KIND >= K_LOW ? 2 : 1> launch) {
                                 a = t.eoffs[g];
                                 z = t.eoffs[g + 1];
                             }
-                            for (int k = 0; k < steps; ++k) {
-                                const uint64_t bk = bd + (p.dense_mn ? (2048 >> 4) * k : 2 * k);
-                                mma_pair_rows(d, ad + 2 * k, bk, eidesc, off);
-                                mma_pair_rows(d, ad + 4 + 2 * k, bk, eidesc, off);
+#pragma unroll
+                            for (int term = 0; term < TERMS; ++term) {
+                                for (int k = 0; k < steps; ++k) {
+                                    const uint64_t bk = bd + (p.dense_mn ? (2048 >> 4) * k : 2 * k);
+                                    mma_pair_rows(d, ad + 2 * k, bk, eidesc, off);
+                                    mma_pair_rows(d, ad + 4 + 2 * k, bk, eidesc, off);
+                                }
+                                bd += ebytes >> 4;
                             }
-                            bd += ebytes >> 4;
                         }
                         mma_commit_pair(&t.empty[at.s]);
                     }
@@ -1123,6 +1135,11 @@ k_group(const __grid_constant__ Launch<KIND >= K_LOW ? 2 : 1> launch) {
                     }
 #pragma unroll
                     for (int j = 0; j < 32; ++j) v[j] += prev[j];
+                    if (F16) {
+                        const float back = peak_unscale(p.peak[w.g]);
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) v[j] *= back;
+                    }
                     uint16_t *out = out0 + w.g * p.gstride;
                     const int r0 = (w.ot * p.bn + c) >> 6 << 5, m = w.xt * GP_TILE + rank * 128 + quad * 32;
                     if (p.out_kind == GP_OUT_LOW) {
@@ -1139,22 +1156,39 @@ k_group(const __grid_constant__ Launch<KIND >= K_LOW ? 2 : 1> launch) {
                         });
                     }
                 } else if (pack) {
-                    // 32 ranks of an inner product: value = high + low term, to about
-                    // twice the type's precision; an infinite high term takes a zero
-                    // low one (not inf - inf).  A place without a row (padding) has
+                    // 32 ranks of an inner product.  A place without a row (padding) has
                     // zeros, also where the adapter's values make a NaN of them
                     const float sc = p.scale[w.g];
                     const bool row_there = mine && t.rows[r] >= 0;
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) {
-                        v[j] = row_there && c + j < p.n ? v[j] * sc : 0.f;
-                        const float hi = widen<F16>((uint16_t)pack2<F16>(v[j], 0.f));
-                        prev[j] = isinf(hi) ? 0.f : v[j] - hi;
-                    }
-                    if (mine) {
-                        uint16_t *dst = out0 + (int64_t)(w.first + rank * 128 + r) * p.ld + c * 2;
-                        store_row<F16>(dst, v, 32, true);
-                        store_row<F16>(dst + 32, prev, 32, true);
+                    for (int j = 0; j < 32; ++j) v[j] = row_there && c + j < p.n ? v[j] * sc : 0.f;
+                    uint16_t *dst = out0 + (int64_t)(w.first + rank * 128 + r) * p.ld + c * 2;
+                    if (F16 && p.out_kind == GP_OUT_WIDE) {
+                        uint32_t top = 0;
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) {
+                            const uint32_t m = __float_as_uint(v[j]) & 0x7fffffffu;
+                            top = max(top, m < 0x7f800000u ? m : 0u);
+                        }
+                        if (mine)
+#pragma unroll
+                            for (int j = 0; j < 32; j += 4)
+                                *(float4 *)((float *)dst + j) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
+                        // (a maximum: the order of the arrivals is free)
+                        if (!dealt) top = __reduce_max_sync(0xffffffffu, top);
+                        if (top && (dealt || lane == 0)) atomicMax(p.peak + w.g, top);
+                    } else {
+                        // value = high + low term; an infinite high term takes a zero low
+                        // one (not inf - inf)
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) {
+                            const float hi = widen<false>((uint16_t)pack2<false>(v[j], 0.f));
+                            prev[j] = isinf(hi) ? 0.f : v[j] - hi;
+                        }
+                        if (mine) {
+                            store_row<false>(dst, v, 32, true);
+                            store_row<false>(dst + 32, prev, 32, true);
+                        }
                     }
                 } else if (!dealt) {
                     stage_row(v);
@@ -1243,7 +1277,7 @@ void group_plan(GroupProduct *p) {
     p->stage_bytes = (a + b) * p->kk;
     p->ext_pack = 1;
     if (p->rank && p->rank <= GP_RC) {
-        const int fits = b * p->kk / ext_bytes(*p);
+        const int fits = b * p->kk / (ext_bytes(*p) * ext_terms(*p));
         p->ext_pack = fits < 1 ? 1 : fits;
     }
     const int fit = room / p->stage_bytes;

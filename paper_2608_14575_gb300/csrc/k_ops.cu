@@ -296,6 +296,8 @@ k_sort_rows(const __grid_constant__ GroupPlan plan, const __grid_constant__ Sort
     int32_t *offs = sh, *pad = sh + G + 1;       // first place of each group, in either plan
     int total = plan.rows;
     pdl_begin();
+    if (blockIdx.x == 0 && blockIdx.y == 0)
+        for (int i = threadIdx.x; i < m.nzero; i += SR_THREADS) m.zero[i] = 0;
     if (padded_offsets) {
         for (int i = threadIdx.x; i <= G; i += SR_THREADS) {
             const int v = plan.offsets[i];
@@ -360,10 +362,18 @@ k_sort_rows(const __grid_constant__ GroupPlan plan, const __grid_constant__ Sort
 
 // ---------------------------------------------------------------------------
 // Low-rank inner products of a few rows: u[place] = scale[g] A[g] x[order[place]]
-// as two 16-bit terms a value, in the layout of the tensor-core kernel.  A few
+// as two bf16 terms a value, in the layout of the tensor-core kernel.  A few
 // rows read all of A once and compute little: a block takes a row and four
 // ranks, its eight warps an eighth of the columns each, so that every load of
 // the call is in flight at once.
+
+// A value as two bf16 terms; an infinite high one takes a zero low one (not inf - inf).
+__device__ __forceinline__ void bf16_terms(float v, uint16_t &high, uint16_t &low) {
+    const __nv_bfloat16 h = __float2bfloat16_rn(v);
+    const float f = __bfloat162float(h);
+    high = __bfloat16_as_ushort(h);
+    low = __bfloat16_as_ushort(__float2bfloat16_rn(isinf(f) ? 0.f : v - f));
+}
 
 constexpr int LF_THREADS = 256, LF_WARPS = LF_THREADS / 32, LF_RANKS = 4;
 
@@ -453,17 +463,83 @@ k_low_few(const __grid_constant__ LowFew p) {
         }
         // high and low terms (an infinite high one takes a zero low one)
         uint16_t *u = p.u + (int64_t)place * p.u_ld + r / GP_RC * (2 * GP_RC) + r % GP_RC;
-        if (F16) {
-            const __half h = __float2half_rn(v);
-            const float f = __half2float(h);
-            u[0] = __half_as_ushort(h);
-            u[GP_RC] = __half_as_ushort(__float2half_rn(isinf(f) ? 0.f : v - f));
-        } else {
-            const __nv_bfloat16 h = __float2bfloat16_rn(v);
-            const float f = __bfloat162float(h);
-            u[0] = __bfloat16_as_ushort(h);
-            u[GP_RC] = __bfloat16_as_ushort(__float2bfloat16_rn(isinf(f) ? 0.f : v - f));
+        bf16_terms(v, u[0], u[GP_RC]);
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Terms of inner products and of adapters (see SplitLow and launch_ext_terms).  Both
+// pass a few MB, and are bound by their launch.
+
+constexpr int SP_THREADS = 256;
+
+struct Split {
+    SplitLow of[2];
+};
+
+// A warp takes a place: 32 ranks (128 bytes) at a time.
+__global__ void __launch_bounds__(SP_THREADS)
+k_split_low(const __grid_constant__ GroupPlan plan, const __grid_constant__ Split split, int rank, int64_t ld) {
+    extern __shared__ int32_t offs[];
+    const SplitLow &s = split.of[blockIdx.y];
+    const int G = plan.groups, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    pdl_begin();
+    for (int i = threadIdx.x; i <= G; i += SP_THREADS) offs[i] = plan.offsets[i];
+    __syncthreads();
+    const int end = min(offs[G], plan.places);
+    for (int64_t at = blockIdx.x * (SP_THREADS / 32) + warp; at < end; at += (int64_t)gridDim.x * (SP_THREADS / 32)) {
+        int lo = 0, hi = G - 1;                  // last group that begins at or before the place
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) >> 1;
+            if (offs[mid] <= at) lo = mid;
+            else hi = mid - 1;
         }
+        const float scale = peak_scale(s.peak[lo]);
+        for (int64_t c = at * ld; c < at * ld + (rank + 31) / 32 * 64; c += 64) {
+            const float v = ((const float *)(s.u + c))[lane];
+            __syncwarp();                        // (the terms take the values' place)
+            const float f = v * scale;
+            const __half h = __float2half_rn(f);
+            s.u[c + lane] = __half_as_ushort(h);
+            s.u[c + 32 + lane] = __half_as_ushort(__float2half_rn(isfinite(f) ? f - __half2float(h) : 0.f));
+            if (s.ext) bf16_terms(v, s.ext[c + lane], s.ext[c + 32 + lane]);
+        }
+    }
+}
+
+// A thread takes eight values: of a row's ranks, or (MN) along the rows of one rank; 32-bit
+// divisions where they do.
+template <bool MN>
+__global__ void __launch_bounds__(SP_THREADS)
+k_ext_terms(uint16_t *dst, int64_t dst_ld, const uint16_t *src, int groups, int rows, int rank) {
+    const int wide = !MN && rank <= 16 ? 16 : GP_RC, ranks = (rank + wide - 1) / wide * wide;
+    const int units = MN ? (int)(dst_ld / 8) : ranks / 8;
+    const int64_t lines = (int64_t)groups * (MN ? ranks : rows), all = lines * units;
+    pdl_begin();
+#pragma unroll 2
+    for (int64_t i = blockIdx.x * (int64_t)SP_THREADS + threadIdx.x; i < all; i += (int64_t)gridDim.x * SP_THREADS) {
+        const int64_t line = all <= INT32_MAX ? (uint32_t)i / (uint32_t)units : i / units;
+        const int unit = (int)(i - line * units);
+        const int64_t group = !MN ? 0 : all <= INT32_MAX ? (uint32_t)line / (uint32_t)ranks : line / ranks;
+        const int r = MN ? (int)(line - group * ranks) : unit * 8;
+        uint4 v = make_uint4(0, 0, 0, 0);
+        if (r < rank)
+            v = MN ? unit_of(src + (group * rank + r) * rows, unit, rows) : unit_of(src + line * rank, unit, rank);
+        const uint32_t x[4] = {v.x, v.y, v.z, v.w};
+        uint32_t high[4], low[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            uint16_t h0, l0, h1, l1;
+            const float2 f = __half22float2(*(const __half2 *)&x[k]);
+            bf16_terms(f.x, h0, l0);
+            bf16_terms(f.y, h1, l1);
+            high[k] = h0 | (uint32_t)h1 << 16;
+            low[k] = l0 | (uint32_t)l1 << 16;
+        }
+        const int at = r / wide * (2 * wide) + r % wide;         // of the high terms
+        uint16_t *to = MN ? dst + (group * (2 * ranks) + at) * dst_ld + unit * 8 : dst + line * dst_ld + at;
+        *(uint4 *)to = make_uint4(high[0], high[1], high[2], high[3]);
+        *(uint4 *)(to + (MN ? wide * dst_ld : wide)) = make_uint4(low[0], low[1], low[2], low[3]);
     }
 }
 
@@ -828,6 +904,27 @@ cudaError_t launch_sort_rows(const GroupPlan &plan, const SortRows &m, int place
     const int64_t slices = want < 1 ? 1 : most / want;
     cfg.gridDim.y = (unsigned)(slices < 1 ? 1 : slices < widest ? slices : widest);
     return cudaLaunchKernelEx(&cfg, k_sort_rows, plan, m, places, padded_offsets, padded_order);
+}
+
+cudaError_t launch_split_low(const GroupPlan &plan, int rank, int64_t ld, const SplitLow *s, int n, int nsm,
+                             cudaStream_t st) {
+    Split split;
+    for (int i = 0; i < 2; ++i) split.of[i] = s[i < n ? i : 0];
+    const int64_t want = ((int64_t)plan.places + SP_THREADS / 32 - 1) / (SP_THREADS / 32), most = (int64_t)nsm * 8;
+    cudaLaunchAttribute at[1];
+    cudaLaunchConfig_t cfg = relaxed((int)(want < most ? want : most), SP_THREADS, (plan.groups + 1) * 4, st, at);
+    cfg.gridDim.y = (unsigned)n;
+    return cudaLaunchKernelEx(&cfg, k_split_low, plan, split, rank, ld);
+}
+
+cudaError_t launch_ext_terms(uint16_t *dst, int64_t dst_ld, const uint16_t *src, int groups, int rows, int rank, bool mn,
+                             int nsm, cudaStream_t s) {
+    const int64_t units = (int64_t)groups * (mn ? ext_terms_ranks(rank, mn) / 2 : rows) * (mn ? dst_ld / 8 : dst_ld / 16);
+    const int64_t want = (units + SP_THREADS - 1) / SP_THREADS, most = (int64_t)nsm * 8;
+    cudaLaunchAttribute at[1];
+    const cudaLaunchConfig_t cfg = relaxed((int)(want < most ? want : most), SP_THREADS, 0, s, at);
+    return mn ? cudaLaunchKernelEx(&cfg, k_ext_terms<true>, dst, dst_ld, src, groups, rows, rank)
+              : cudaLaunchKernelEx(&cfg, k_ext_terms<false>, dst, dst_ld, src, groups, rows, rank);
 }
 
 cudaError_t launch_low_few(const LowFew &p, bool f16, cudaStream_t s) {

@@ -410,6 +410,8 @@ struct Rows {
     bool sorted = false;
     Operand x, dy;
     size_t offsets_off = 0, order_off = 0;     // padded plan
+    size_t peak_off = 0;                       // words that are zeroed beside the copy
+    int peaks = 0;
 };
 
 // Whether a product picks its rows by index, or they are copied by place first.
@@ -495,6 +497,8 @@ static hwr_status sort_rows(hwr_ops *c, Rows *s) {
     }
     int32_t *offsets = s->plan.padded ? (int32_t *)(c->ws + s->offsets_off) : nullptr;
     int32_t *order = s->plan.padded ? (int32_t *)(c->ws + s->order_off) : nullptr;
+    m.zero = (uint32_t *)(c->ws + s->peak_off);
+    m.nzero = s->peaks;
     CK(c, launch_sort_rows(s->plan, m, s->plan.places, offsets, order, c->nsm, c->stream), "row copy");
     if (s->plan.padded) {
         s->plan.offsets = offsets;
@@ -565,10 +569,10 @@ static hwr_status rows_product(hwr_ops *c, GroupProduct p, const Operand &x, con
         OK(encode(c, &m.xx, p.f16, x, 64, 128));
     }
     OK(encode(c, &m.w, p.f16, w, 64, w_mn ? 64 : p.mode == GP_GROUPED ? 128 : p.bn / 2));
-    if (u) {
-        OK(encode(c, &m.u, p.f16, *u, 64, GP_ROW_BOX));
-        OK(w_mn ? encode(c, &m.eb, p.f16, *eb, 64, GP_RC)
-                : encode(c, &m.eb, p.f16, *eb, p.rank <= 16 ? 16 : GP_RC, p.bn / 2));
+    if (u) {         // (bf16 terms whatever the rows' type)
+        OK(encode(c, &m.u, false, *u, 64, GP_ROW_BOX));
+        OK(w_mn ? encode(c, &m.eb, false, *eb, 64, GP_RC)
+                : encode(c, &m.eb, false, *eb, p.rank <= 16 ? 16 : GP_RC, p.bn / 2));
     }
     return HWR_OK;
 }
@@ -692,13 +696,15 @@ static hwr_status check_adapters(hwr_ops *c, const hwr_rows *r, const hwr_adapte
     return HWR_OK;
 }
 
-// scale[g] M[g] x[t] (or M[g]^T x[t]) by place, as two 16-bit terms: [places]
-// [32-rank chunks][high, low], an even number of chunks.
+// scale[g] M[g] x[t] (or M[g]^T x[t]) by place, as two bf16 terms: [places]
+// [32-rank chunks][high, low], an even number of chunks; or, with the groups' peaks,
+// in fp32 in the same room.
 static hwr_status low_rank(hwr_ops *c, const hwr_rows *r, const hwr_adapters *ad, const Rows &rows, const Operand &x,
-                           const Operand &m, bool m_mn, const Operand &u, GroupCall *call) {
+                           const Operand &m, bool m_mn, const Operand &u, uint32_t *peak, GroupCall *call) {
     GroupProduct p = product(c, r, rows);
     p.mode = GP_ROWS;
-    p.out_kind = GP_OUT_PACK;
+    p.out_kind = peak ? GP_OUT_WIDE : GP_OUT_PACK;
+    p.peak = peak;
     p.out = const_cast<void *>(u.p);
     p.ld = u.ld;
     p.scale = ad->scale;
@@ -739,6 +745,34 @@ static Operand packed(Carver &cv, const Rows &rows, const hwr_adapters *ad) {
     return u;
 }
 
+// The adapters' matrices as the extension takes them: as they are in bf16, as two bf16
+// terms of fp16 ones.
+static Operand ext_operand(Carver &cv, const hwr_rows *r, const void *m, int rows, int rank, bool mn) {
+    const int G = r->groups;
+    if (r->dtype == HWR_BF16)
+        return mn ? cv.operand(m, rows, rank, rows, (int64_t)rank * rows, G)
+                  : cv.operand(m, rank, rows, rank, (int64_t)rows * rank, G);
+    Operand o;
+    o.p = m;
+    o.nz = G;
+    o.rows = mn ? ext_terms_ranks(rank, mn) : rows;
+    o.cols = mn ? rows : ext_terms_ranks(rank, mn);
+    o.off = cv.take((size_t)G * o.rows * up(o.cols, 8) * 2);
+    return o;
+}
+
+static hwr_status settle_ext(hwr_ops *c, const hwr_rows *r, Operand *o, int rank, bool mn) {
+    if (r->dtype == HWR_BF16) return settle(c, o);
+    const uint16_t *src = (const uint16_t *)o->p;
+    o->p = c->ws + o->off;
+    o->ld = up(o->cols, 8);
+    o->z = o->ld * o->rows;
+    CK(c, launch_ext_terms((uint16_t *)(c->ws + o->off), o->ld, src, r->groups, (int)(mn ? o->cols : o->rows), rank, mn,
+                           c->nsm, c->stream),
+       "adapters' terms");
+    return HWR_OK;
+}
+
 // W x[t] (or W^T x[t]) and the extension of t's group.
 static hwr_status shared_product(hwr_ops *c, const hwr_rows *r, const hwr_adapters *ad, const Rows &rows,
                                  const Operand &x, const Operand &w, bool w_mn, const Operand &u, const Operand &eb,
@@ -772,7 +806,7 @@ extern "C" hwr_status hwr_adapter_forward(hwr_ops *c, const hwr_rows *r, const h
     Operand a = cv.operand(ad->a, K, R, K, (int64_t)R * K, G);
     const bool few = !rows.sorted && r->rows <= FEW_ROWS;
     Operand b;
-    if (!few) b = cv.operand(ad->b, R, N, R, (int64_t)N * R, G);
+    if (!few) b = ext_operand(cv, r, ad->b, N, R, false);
     Operand u = packed(cv, rows, ad);
     OK(reserve(c, cv.at));
     u.p = c->ws + u.off;
@@ -799,12 +833,12 @@ extern "C" hwr_status hwr_adapter_forward(hwr_ops *c, const hwr_rows *r, const h
         CK(c, launch_few_rows(f, r->dtype == HWR_F16, c->stream), "few-rows kernel");
         return HWR_OK;
     }
-    OK(settle(c, &b));
+    OK(settle_ext(c, r, &b, R, false));
     if ((int64_t)r->rows * R * K <= LOW_FEW_VALUES && (int64_t)r->rows * ((R + 3) / 4) <= LOW_FEW_BLOCKS) {
         OK(low_rank_few(c, r, ad, rows, a, u, false));
     } else {
         GroupCall call;
-        OK(low_rank(c, r, ad, rows, rows.x, a, false, u, &call));
+        OK(low_rank(c, r, ad, rows, rows.x, a, false, u, nullptr, &call));
         OK(launch(c, &call));
     }
     return shared_product(c, r, ad, rows, rows.x, w, false, u, b, y, y_ld, N);
@@ -828,36 +862,57 @@ extern "C" hwr_status hwr_adapter_backward(hwr_ops *c, const hwr_rows *r, const 
     if (!dx && !da && !db) return HWR_OK;
     Carver cv;
     Rows rows = plan_rows(cv, r, dy, dy_ld, da || db, da || db, picks_rows(c, r, N, K, true, vec_of(dx, dx_ld, 0)));
-    Operand w, a, b, u, v;
+    // In fp16 the gradients take the inner products as fp16 terms that are scaled by
+    // each group's peak: they are made in fp32 and split in a pass of their own
+    const bool split = r->dtype == HWR_F16;
+    Operand w, a, b, ea, u, v, ev;
     if (dx) w = cv.operand(r->w, r->w_ld, N, K);
-    if (dx || db) a = cv.operand(ad->a, K, R, K, (int64_t)R * K, G);
+    if (dx) ea = ext_operand(cv, r, ad->a, K, R, true);
+    if (db) a = cv.operand(ad->a, K, R, K, (int64_t)R * K, G);
     if (dx || da) {
         b = cv.operand(ad->b, R, N, R, (int64_t)N * R, G);
         v = packed(cv, rows, ad);
     }
     if (db) u = packed(cv, rows, ad);
+    if (split && dx && da) ev = packed(cv, rows, ad);
+    if (split && (da || db)) {
+        rows.peaks = 2 * G;
+        rows.peak_off = cv.take((size_t)rows.peaks * 4);
+    }
     OK(reserve(c, cv.at));
     u.p = c->ws + u.off;
     v.p = c->ws + v.off;
+    ev.p = c->ws + ev.off;
+    uint32_t *const upeak = split && db ? (uint32_t *)(c->ws + rows.peak_off) : nullptr;
+    uint32_t *const vpeak = split && da ? (uint32_t *)(c->ws + rows.peak_off) + G : nullptr;
     OK(sort_rows(c, &rows));
     if (dx) OK(settle(c, &w));
-    if (dx || db) OK(settle(c, &a));
+    if (dx) OK(settle_ext(c, r, &ea, R, true));
+    if (db) OK(settle(c, &a));
     // v and u are independent of each other, and so are da and db: two in a launch,
     // on shares of the SMs by what they read (a launch of its own takes 10 us)
     GroupCall calls[2];
-    int n = 0;
+    SplitLow splits[2];
+    int n = 0, nsplit = 0;
     if (dx || da) {
         OK(settle(c, &b));
-        OK(low_rank(c, r, ad, rows, rows.dy, b, true, v, &calls[n++]));
+        OK(low_rank(c, r, ad, rows, rows.dy, b, true, v, vpeak, &calls[n++]));
+        if (vpeak) splits[nsplit++] = {(uint16_t *)(c->ws + v.off), dx ? (uint16_t *)(c->ws + ev.off) : nullptr, vpeak};
     }
-    if (db) OK(low_rank(c, r, ad, rows, rows.x, a, false, u, &calls[n++]));
+    if (db) {
+        OK(low_rank(c, r, ad, rows, rows.x, a, false, u, upeak, &calls[n++]));
+        if (upeak) splits[nsplit++] = {(uint16_t *)(c->ws + u.off), nullptr, upeak};
+    }
     const double by_n = (double)N / ((double)N + K);
     OK(launch(c, calls, n, by_n));
-    if (dx) OK(shared_product(c, r, ad, rows, rows.dy, w, true, v, a, dx, dx_ld, K));
+    if (nsplit)
+        CK(c, launch_split_low(rows.plan, R, 2 * up(R, 2 * GP_RC), splits, nsplit, c->nsm, c->stream), "terms");
+    if (dx) OK(shared_product(c, r, ad, rows, rows.dy, w, true, vpeak ? ev : v, ea, dx, dx_ld, K));
     n = 0;
     if (da) {
         GroupProduct p = product(c, r, rows);
         p.out_kind = GP_OUT_LOW_T;
+        p.peak = vpeak;
         p.out = da;
         p.ld = K;
         p.gstride = (int64_t)R * K;
@@ -868,6 +923,7 @@ extern "C" hwr_status hwr_adapter_backward(hwr_ops *c, const hwr_rows *r, const 
     if (db) {
         GroupProduct p = product(c, r, rows);
         p.out_kind = GP_OUT_LOW;
+        p.peak = upeak;
         p.out = db;
         p.ld = R;
         p.gstride = (int64_t)N * R;

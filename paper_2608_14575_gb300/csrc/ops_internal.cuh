@@ -33,11 +33,22 @@ enum : int {
 // What a tile's values become.
 enum : int {
     GP_OUT_ROWS = 0,   // out[order[p]][n], rows scattered back to their places
-    GP_OUT_PACK = 1,   // scale[g] * value as two 16-bit terms, a row per place
+    GP_OUT_PACK = 1,   // scale[g] * value as two bf16 terms, a row per place
     GP_OUT_GROUP = 2,  // out[g][m][n]
     GP_OUT_LOW = 3,    // out[g][m][r]: columns j and j + 32 of each 64 added
     GP_OUT_LOW_T = 4,  // out[g][r][m]: the same, transposed
+    GP_OUT_WIDE = 5,   // scale[g] * value in fp32, where GP_OUT_PACK has the terms; and
+                       // each group's largest finite one
 };
+
+// The largest finite magnitude of a group's inner products (its bits) as the power of
+// two that brings it into [2^14, 2^15), the end of fp16's range, and back.
+__device__ __forceinline__ int peak_exponent(uint32_t peak) {
+    const int e = peak >> 23 ? peak >> 23 : 1;
+    return peak ? (141 - e < 126 ? 141 - e : 126) : 0;
+}
+__device__ __forceinline__ float peak_scale(uint32_t peak) { return __uint_as_float((127 + peak_exponent(peak)) << 23); }
+__device__ __forceinline__ float peak_unscale(uint32_t peak) { return __uint_as_float((127 - peak_exponent(peak)) << 23); }
 
 // A plan as the products read it.  The places of its order hold the groups one
 // after the other, then the rows without a group; a padded plan (sort_rows)
@@ -78,6 +89,7 @@ struct GroupProduct {
     int64_t ld = 0, gstride = 0;
     int rank_out = 0;                 // GP_OUT_LOW*: ranks written
     const float *scale = nullptr;
+    uint32_t *peak = nullptr;         // [groups] GP_OUT_WIDE: raised; GP_OUT_LOW*: what the terms are scaled by
     // joined partial tiles and the status word
     float *part = nullptr;
     uint32_t *count = nullptr;
@@ -145,9 +157,28 @@ struct SortRows {
     int cols[2];
     uint16_t *dst[2];
     int64_t dst_ld[2];                // whole 16-byte units
+    uint32_t *zero = nullptr;         // and words to be zeroed
+    int nzero = 0;
 };
 cudaError_t launch_sort_rows(const GroupPlan &plan, const SortRows &m, int places, int32_t *padded_offsets,
                              int32_t *padded_order, int nsm, cudaStream_t s);
+
+// Inner products in fp32 (GP_OUT_WIDE) as two fp16 terms, in place, scaled by a power of
+// two of each group's own (peak_scale); where `ext` is set also as two bf16 terms there.
+struct SplitLow {
+    uint16_t *u, *ext;
+    const uint32_t *peak;
+};
+cudaError_t launch_split_low(const GroupPlan &plan, int rank, int64_t ld, const SplitLow *s, int n, int nsm,
+                             cudaStream_t st);
+
+// The adapters' matrices in fp16 as two bf16 terms, exactly (8 + 3 bits), as the
+// extension's stages take them: src [groups][rows][rank] (or, mn, [groups][rank][rows])
+// to dst [groups][rows][ext_terms_ranks] (or [groups][ext_terms_ranks][dst_ld]), where
+// a chunk of 32 ranks (16 of up to 16; mn: 32) is its high terms, then its low ones.
+inline int ext_terms_ranks(int rank, bool mn) { return rank <= 16 && !mn ? 32 : (rank + GP_RC - 1) / GP_RC * 2 * GP_RC; }
+cudaError_t launch_ext_terms(uint16_t *dst, int64_t dst_ld, const uint16_t *src, int groups, int rows, int rank, bool mn,
+                             int nsm, cudaStream_t s);
 
 // u[place] = scale[g] a[g] x[order[place]] as GP_OUT_PACK leaves it, for a few
 // rows (a 16-byte aligned, rows of x too).
