@@ -1127,14 +1127,15 @@ k_group(const __grid_constant__ Launch<KIND >= K_LOW ? 2 : 1> launch) {
                     }
                 } else if (low) {
                     // blocks of 64 columns: the products with the high terms of 32
-                    // ranks, then those with the low terms
+                    // ranks, then those with the low terms (which an infinity among the
+                    // rows would make a NaN of where they are 0)
                     if (!(c & 32)) {
 #pragma unroll
                         for (int j = 0; j < 32; ++j) prev[j] = v[j];
                         continue;
                     }
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) v[j] += prev[j];
+                    for (int j = 0; j < 32; ++j) v[j] = isfinite(prev[j]) ? prev[j] + v[j] : prev[j];
                     if (F16) {
                         const float back = peak_unscale(p.peak[w.g]);
 #pragma unroll
@@ -1178,17 +1179,22 @@ k_group(const __grid_constant__ Launch<KIND >= K_LOW ? 2 : 1> launch) {
                         if (!dealt) top = __reduce_max_sync(0xffffffffu, top);
                         if (top && (dealt || lane == 0)) atomicMax(p.peak + w.g, top);
                     } else {
-                        // value = high + low term; an infinite high term takes a zero low
-                        // one (not inf - inf)
+                        uint32_t hi[16], lo[16];
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) {
-                            const float hi = widen<false>((uint16_t)pack2<false>(v[j], 0.f));
-                            prev[j] = isinf(hi) ? 0.f : v[j] - hi;
+                        for (int j = 0; j < 32; j += 2) {
+                            uint16_t h0, l0, h1, l1;
+                            bf16_terms(v[j], h0, l0);
+                            bf16_terms(v[j + 1], h1, l1);
+                            hi[j / 2] = h0 | (uint32_t)h1 << 16;
+                            lo[j / 2] = l0 | (uint32_t)l1 << 16;
                         }
-                        if (mine) {
-                            store_row<false>(dst, v, 32, true);
-                            store_row<false>(dst + 32, prev, 32, true);
-                        }
+                        if (mine)
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) {
+                                *(uint4 *)(dst + 8 * j) = make_uint4(hi[4 * j], hi[4 * j + 1], hi[4 * j + 2], hi[4 * j + 3]);
+                                *(uint4 *)(dst + 32 + 8 * j) =
+                                    make_uint4(lo[4 * j], lo[4 * j + 1], lo[4 * j + 2], lo[4 * j + 3]);
+                            }
                     }
                 } else if (!dealt) {
                     stage_row(v);

@@ -367,14 +367,6 @@ k_sort_rows(const __grid_constant__ GroupPlan plan, const __grid_constant__ Sort
 // ranks, its eight warps an eighth of the columns each, so that every load of
 // the call is in flight at once.
 
-// A value as two bf16 terms; an infinite high one takes a zero low one (not inf - inf).
-__device__ __forceinline__ void bf16_terms(float v, uint16_t &high, uint16_t &low) {
-    const __nv_bfloat16 h = __float2bfloat16_rn(v);
-    const float f = __bfloat162float(h);
-    high = __bfloat16_as_ushort(h);
-    low = __bfloat16_as_ushort(__float2bfloat16_rn(isinf(f) ? 0.f : v - f));
-}
-
 constexpr int LF_THREADS = 256, LF_WARPS = LF_THREADS / 32, LF_RANKS = 4;
 
 template <bool F16>
@@ -461,7 +453,6 @@ k_low_few(const __grid_constant__ LowFew p) {
             if (r < p.rank) p.wide[(int64_t)place * p.rank + r] = v;
             return;
         }
-        // high and low terms (an infinite high one takes a zero low one)
         uint16_t *u = p.u + (int64_t)place * p.u_ld + r / GP_RC * (2 * GP_RC) + r % GP_RC;
         bf16_terms(v, u[0], u[GP_RC]);
     }
@@ -498,13 +489,27 @@ k_split_low(const __grid_constant__ GroupPlan plan, const __grid_constant__ Spli
         for (int64_t c = at * ld; c < at * ld + (rank + 31) / 32 * 64; c += 64) {
             const float v = ((const float *)(s.u + c))[lane];
             __syncwarp();                        // (the terms take the values' place)
+            // (a high term is zero only where the value is: what becomes of infinities is
+            // taken from the high terms alone)
             const float f = v * scale;
-            const __half h = __float2half_rn(f);
+            __half h = __float2half_rn(f);
+            if (v != 0.f && __half2float(h) == 0.f) h = __ushort_as_half(v < 0.f ? 0x8001 : 1);
             s.u[c + lane] = __half_as_ushort(h);
             s.u[c + 32 + lane] = __half_as_ushort(__float2half_rn(isfinite(f) ? f - __half2float(h) : 0.f));
             if (s.ext) bf16_terms(v, s.ext[c + lane], s.ext[c + 32 + lane]);
         }
     }
+}
+
+// As bf16_terms, of a value that one or two terms hold exactly: a value that the first
+// one holds keeps it, beside 2^-126 of its sign, which no sum of finite values notices.
+__device__ __forceinline__ void matrix_terms(float v, uint16_t &high, uint16_t &low) {
+    const uint32_t u = __float_as_uint(v), h = u & 0xffff0000u, m = u & 0x7fffffffu;
+    uint32_t l = __float_as_uint(v - __uint_as_float(h));        // (exact: its lower half is 0)
+    if (m >= 0x7f800000u) l = u;
+    else if (u == h) l = m ? (u & 0x80000000u) | 0x00800000u : u;
+    high = (uint16_t)(h >> 16);
+    low = (uint16_t)(l >> 16);
 }
 
 // A thread takes eight values: of a row's ranks, or (MN) along the rows of one rank; 32-bit
@@ -529,10 +534,10 @@ k_ext_terms(uint16_t *dst, int64_t dst_ld, const uint16_t *src, int groups, int 
         uint32_t high[4], low[4];
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            uint16_t h0, l0, h1, l1;
             const float2 f = __half22float2(*(const __half2 *)&x[k]);
-            bf16_terms(f.x, h0, l0);
-            bf16_terms(f.y, h1, l1);
+            uint16_t h0, l0, h1, l1;
+            matrix_terms(f.x, h0, l0);
+            matrix_terms(f.y, h1, l1);
             high[k] = h0 | (uint32_t)h1 << 16;
             low[k] = l0 | (uint32_t)l1 << 16;
         }

@@ -5,6 +5,7 @@
 #pragma once
 
 #include <cuda.h>
+#include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
 
@@ -40,6 +41,18 @@ enum : int {
     GP_OUT_WIDE = 5,   // scale[g] * value in fp32, where GP_OUT_PACK has the terms; and
                        // each group's largest finite one
 };
+
+// A value as two bf16 terms, high + low, that give what the value gives in a sum of
+// products with infinities too: the low term has the value's sign and is zero only
+// where the value is (0 and inf make a NaN), so the high one is cut off, strictly below
+// the value; an infinity or NaN is both terms.  16 bits of the value.
+__device__ __forceinline__ void bf16_terms(float v, uint16_t &high, uint16_t &low) {
+    const uint32_t u = __float_as_uint(v), m = u & 0x7fffffffu;
+    const uint32_t h = (m - 1 < 0x7f7fffffu ? u - 1 : u) >> 16;          // (finite, not 0)
+    const float rest = m < 0x7f800000u ? v - __uint_as_float(h << 16) : v;
+    high = (uint16_t)h;
+    low = __bfloat16_as_ushort(__float2bfloat16_rn(rest));
+}
 
 // The largest finite magnitude of a group's inner products (its bits) as the power of
 // two that brings it into [2^14, 2^15), the end of fp16's range, and back.

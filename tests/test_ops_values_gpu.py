@@ -153,3 +153,31 @@ def test_inner_products_beyond_half_precision_backward(ops, dt):
     dy, s = make(T, N, std=50.0, dt=dt, seed=3), torch.tensor([1.0, 8.0], device="cuda")
     assert float((dy.double() @ b[1].double()).abs().max()) * 8 > 65504
     check_ends(ops, x, w, a, b, s, dy, c)
+
+
+@pytest.mark.parametrize("dt", [BF, HF])
+@pytest.mark.parametrize("T,K,N,r", [(5, 64, 72, 8), (16, 72, 64, 24), (40, 72, 64, 24), (300, 65, 130, 40),
+                                     (300, 256, 320, 16), (5000, 136, 72, 8), (3000, 264, 200, 70)])
+def test_infinities_give_what_they_give_in_64_bits(ops, dt, T, K, N, r):
+    """Infinities in adapters, rows and gradients: infinite where the formula is, NaN only
+    where it is (0 times an infinity, a difference of two)."""
+    G = 7
+    c = torch.arange(T, device="cuda", dtype=torch.int32) % (G + 1) - 1
+    x, w, a, b, dy = (ints(*s, lo=-1, hi=1, dt=dt, seed=i) for i, s in
+                      enumerate(((T, K), (N, K), (G, r, K), (G, N, r), (T, N))))
+    s = 2.0 ** torch.randint(-1, 2, (G,), device="cuda").float()
+    a[1, 3, 5], a[2, r - 1, K - 1] = INF, -INF
+    b[3, 7, 2], b[4, N - 1, r - 1] = INF, -INF
+    for g, v in ((5, INF), (6, -INF)):
+        t = torch.nonzero(c == g).flatten()
+        if t.numel():
+            x[t[-1], 4], dy[t[0], 6] = v, -v
+    plan = ops.dispatch(c, G)
+    same(ops.adapter_forward(x, w, a, b, s, plan), R.adapter_forward(x, w, a, b, s, c)[0], dt)
+    for got, (want, _) in zip(ops.adapter_backward(dy, x, w, a, b, s, plan), R.adapter_backward(dy, x, w, a, b, s, c)):
+        same(got, want, dt)
+    gw = ints(G, N, K, lo=-1, hi=1, dt=dt, seed=7)
+    gw[1, 3, 5], gw[2, N - 1, K - 1] = INF, -INF
+    same(ops.grouped_forward(x, gw, plan), R.grouped_forward(x, gw, c)[0], dt)
+    for got, (want, _) in zip(ops.grouped_backward(dy, x, gw, plan), R.grouped_backward(dy, x, gw, c)):
+        same(got, want, dt)
