@@ -117,3 +117,103 @@ def test_dispatch_where_clusters_of_16_do_not_fit(monkeypatch, T, G):
     plan = small.dispatch(c, G)
     assert torch.equal(plan.order.cpu(), order.cpu()) and torch.equal(plan.offsets.cpu(), offsets)
     small.close()
+
+
+def test_two_contexts_at_work_at_once():
+    """Each has its own workspace, partial sums and counters."""
+    H.build()
+    T, G, K, N, r = 700, 5, 1024, 1040, 16
+    c = choices(T, G, "holes")
+    x, w, a, b, dy, gw = (ints(*s, lo=-1, hi=1, seed=i) for i, s in
+                          enumerate(((T, K), (N, K), (G, r, K), (G, N, r), (T, N), (G, N, K))))
+    s = torch.ones(G, device="cuda")
+    want = [R.grouped_forward(x, gw, c)[0].to(BF), *(e.to(BF) for e, _ in R.grouped_backward(dy, x, gw, c)),
+            R.adapter_forward(x, w, a, b, s, c)[0].to(BF), *(e.to(BF) for e, _ in R.adapter_backward(dy, x, w, a, b, s, c))]
+    norm = float(torch.cat([e.double().flatten() for e in want]).square().sum().sqrt())
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    both, got = [], []
+    for stream in streams:
+        with torch.cuda.stream(stream):
+            both.append(H.Operators())
+    for _ in range(8):
+        for stream, ops in zip(streams, both):
+            with torch.cuda.stream(stream):
+                plan = ops.dispatch(c, G)
+                out = [ops.grouped_forward(x, gw, plan), *ops.grouped_backward(dy, x, gw, plan),
+                       ops.adapter_forward(x, w, a, b, s, plan), *ops.adapter_backward(dy, x, w, a, b, s, plan)]
+                got.append((out, ops.clip_gradients([t.clone() for t in out], 1.0)))
+    torch.cuda.synchronize()
+    for out, n in got:
+        assert all(torch.equal(p, q) for p, q in zip(out, want))
+        assert abs(float(n) - norm) <= 1e-6 * norm
+    for ops in both:
+        ops.close()
+
+
+def test_element_offsets_beyond_32_bits(ops):
+    """Rows, weights and results 2^25 elements apart: offsets up to 2.3e9."""
+    T, G, K, N, r, far = 70, 70, 64, 72, 8, 1 << 25
+
+    def apart(n, *shape, seed=0):
+        buf = torch.empty((n - 1) * far + shape[0] * (shape[1] if len(shape) > 1 else 1) + 8, device="cuda", dtype=BF)
+        v = buf.as_strided((n, *shape), (far, *((shape[1], 1) if len(shape) > 1 else (1,))))
+        v.copy_(ints(n, *shape, lo=-1, hi=1, seed=seed))
+        return v
+    c = choices(T, G, "holes")
+    x, dy, y, gw = apart(T, K), apart(T, N, seed=1), apart(T, N, seed=2), apart(G, N, K, seed=3)
+    w, a, b, s = ints(N, K), ints(G, r, K), ints(G, N, r), torch.ones(G, device="cuda")
+    plan = ops.dispatch(c, G)
+    assert torch.equal(ops.grouped_forward(x, gw, plan, out=y), R.grouped_forward(x, gw, c)[0].to(BF))
+    for got, (want, _) in zip(ops.grouped_backward(dy, x, gw, plan), R.grouped_backward(dy, x, gw, c)):
+        assert torch.equal(got, want.to(BF))
+    del gw
+    assert torch.equal(ops.adapter_forward(x, w, a, b, s, plan, out=y), R.adapter_forward(x, w, a, b, s, c)[0].to(BF))
+    few = ops.dispatch(c[:9], G)
+    assert torch.equal(ops.adapter_forward(x[-9:], w, a, b, s, few, out=y[-9:]),
+                       R.adapter_forward(x[-9:], w, a, b, s, c[:9])[0].to(BF))
+    for got, (want, _) in zip(ops.adapter_backward(dy, x, w, a, b, s, plan), R.adapter_backward(dy, x, w, a, b, s, c)):
+        assert torch.equal(got, want.to(BF))
+
+
+@pytest.mark.parametrize("dt", [BF, torch.float16])
+def test_foreign_plans_write_nothing_beside_the_results(dt):
+    """Offsets and orders that no dispatch made: the results are wrong, but what lies beside
+    them and the inputs stay as they are (the C interface, with results in guarded buffers)."""
+    import ctypes as ct
+    from paper_2608_14575_gb300 import _hwr, _ops
+    lib = _ops.load_ops()
+    T, G, K, N, r, edge = 300, 4, 64, 72, 40, 4096
+    x, w, dy, a, b = (ints(*s, dt=dt, seed=i) for i, s in enumerate(((T, K), (G, N, K), (T, N), (G, r, K), (G, N, r))))
+    s = torch.ones(G, device="cuda")
+    inputs = x, w, dy, a, b, s
+    kept = [t.clone() for t in inputs]
+    ctx = ct.c_void_p()
+    assert lib.hwr_ops_create(None, ct.byref(ctx)) == _hwr.HWR_OK
+    guards = []
+
+    def guarded(n):
+        buf = torch.full((n + 2 * edge,), 7.0, device="cuda", dtype=dt)
+        guards.append((buf, n))
+        return ct.c_void_p(buf.data_ptr() + 2 * edge)
+    order = torch.randint(-(1 << 31), (1 << 31) - 1, (T,), device="cuda").to(torch.int32)
+    near = torch.randint(-2, T + 2, (T,), device="cuda", dtype=torch.int32)
+    for offsets in ([0, 5000, -7, 20, 1 << 30], [-5, -5, -5, -5, -5], [300, 200, 100, 50, 0], [0, 300, 0, 300, 0]):
+        o = torch.tensor(offsets, device="cuda", dtype=torch.int32)
+        for p in (order, near):
+            torch.cuda.synchronize()
+            rows = _ops.hwr_rows(T, G, K, N, H.HWR_F16 if dt is torch.float16 else _hwr.HWR_BF16, o.data_ptr(), p.data_ptr(),
+                                 x.data_ptr(), K, w.data_ptr(), K, N * K)
+            ad = _ops.hwr_adapters(r, a.data_ptr(), b.data_ptr(), s.data_ptr())
+            R_, A_, d = ct.byref(rows), ct.byref(ad), ct.c_void_p(dy.data_ptr())
+            assert lib.hwr_grouped_forward(ctx, R_, guarded(T * N), N) == 0
+            assert lib.hwr_grouped_backward(ctx, R_, d, N, guarded(T * K), K, guarded(G * N * K)) == 0
+            assert lib.hwr_grouped_backward(ctx, R_, d, N, guarded(T * K), K, None) == 0
+            assert lib.hwr_adapter_forward(ctx, R_, A_, guarded(T * N), N) == 0
+            assert lib.hwr_adapter_backward(ctx, R_, A_, d, N, guarded(T * K), K, guarded(G * r * K), guarded(G * N * r)) == 0
+            assert lib.hwr_ops_synchronize(ctx) == 0
+    for buf, n in guards:
+        assert (buf[:edge] == 7).all() and (buf[edge + n:] == 7).all()
+    for t, k in zip(inputs, kept):
+        assert torch.equal(t, k)
+    assert lib.hwr_ops_destroy(ctx) == 0
