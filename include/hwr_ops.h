@@ -27,12 +27,21 @@
  *     on a 16-byte boundary, or whose strides are not whole 16-byte units, is
  *     first copied to the workspace with padded rows (an extra read and write of
  *     it, and that much workspace).  The rows of x and dy are copied there by
- *     group in any case, unless they are few (1,024; 256 with adapters) and so
- *     aligned.
+ *     group where that is cheaper than picking each by its index, in backward
+ *     calls with weight gradients, and where they are not so aligned.
  *   - Sums run in fp32 on the tensor cores; each output is rounded once.
  *   - Results do not depend on timing: the same call gives the same bits.
  *   - The workspace grows (cudaMalloc) when a call needs more than any call
- *     before; hwr_ops_reserve does that ahead of time.
+ *     before; hwr_ops_reserve does that ahead of time.  No call needs more bytes
+ *     than, with P = rows + 15 min(rows, groups), n_in + n_out = S, rank r,
+ *       hwr_dispatch   5 (rows / 4,096 + 16) (groups + 1)
+ *       hwr_grouped_*  16,384 + 4 groups + 2 P (S + 18)
+ *                      + 2 groups n_out (n_in + 8)
+ *       hwr_adapter_*  16,384 + 12 groups + 2 P (S + 18) + 12 P (r + 63)
+ *                      + 2 n_out (n_in + 8) + 6 groups (r + 63) (S + 16)
+ *       hwr_clip_gradients  8 bytes for each 1,024 of the gradients' bytes and 32
+ *                      for each gradient
+ *     (weights that are read in place are the terms with n_out (n_in + 8) less).
  *   - Stream capture: calls can be captured into graphs.  A call that would have
  *     to grow the workspace then is refused (UNSUPPORTED, nothing is queued, the
  *     context stays usable): make a call of the same sizes before, or reserve.

@@ -1,11 +1,14 @@
 // A shared projection with low-rank terms for a few rows: decode steps, whose
 // time is that of reading W.  A block takes 16 output columns and its eight warps
 // an eighth of the contraction each, 32 columns of it in turn, so that the block
-// reads 512 consecutive bytes of each row of W and every load of the call is in
-// flight at once; nothing is staged, cut or joined through memory.  The
+// reads 512 consecutive bytes of each row of W; nothing is staged, cut or joined
+// through memory.  Bound by memory latency: a warp has at most four steps' loads in
+// flight (48 registers), and reading W waits for the inner products though only the
+// epilogue needs them (33.5 MB of W alone and with cold caches: 16.5 us, 2.0 TB/s).  The
 // multiplications are warp-level 16 x 8 x 16 MMAs: a tile of 256 rows on tcgen05
 // would be filled by 8 or 16 (one row, 4,096 -> 4,096, rank 16, with its dispatch:
-// 28.0 us there, 21.4 us here; the weights' bytes take 4.9).
+// 28.0 us there, 21.4 us here when both were measured, 19.5 by now; the weights'
+// bytes take 4.9).
 //
 // The contraction's order is free, so a lane takes eight consecutive columns of
 // its row with one 16-byte load and uses them as the column pairs (2q, 2q + 1)

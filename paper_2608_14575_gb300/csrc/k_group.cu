@@ -8,9 +8,10 @@
 // stage each CTA holds 128 rows of the A side and half of the B side, which
 // halves the B bytes that every SM takes from L2.  W comes by TMA, and so do
 // the rows of x once they lie by place; or, without a copy, each is picked by its
-// index with 16-byte cp.async (65,536 x 1024 x 2048 over 64 groups: 255 us picked,
-// 262 with the copy, 650 with TMA's row gather; 8,191 rows of a shared product of
-// 4,096 x 4,096: 334 picked, 229 with the copy, as its rows are the A side).
+// index with 16-byte cp.async (65,536 x 1024 x 2048 over 64 groups: 258 us picked,
+// 259 with the copy, 650 with TMA's row gather in an early form; 8,191 rows of a
+// shared product of 4,096 x 4,096 with adapters of rank 64: 248 picked, 230 with the
+// copy, as its rows are the A side).
 //
 // In a grouped product the rows of x are the B side, whose extent moves in
 // steps of 16: a group's last rows cost no whole tile, and a few rows of a

@@ -417,12 +417,15 @@ struct Rows {
 // Whether a product picks its rows by index, or they are copied by place first.
 // Picking saves the copy (its start and the rows' bytes, in and out) and costs each
 // tile: four of the eight epilogue warps pick, and where rows are a shared product's
-// A side, all pairs' loads.  In us, from 130 shapes either way: 10,188 rows of 3,136
-// columns to 512, 49 picked, 75 copied; 10,013 of 512 to 6,528, 109 and 82; through
-// adapters 950 of 4,608 to 1,984, 53 and 69; 7,354 of 4,352 to 4,544, 336 and 229.
+// A side, all pairs' loads.  Fitted on 130 shapes timed either way, this function
+// returning the one or the other throughout.  In us, each with its dispatch: 10,188 rows
+// of 3,136 columns to 512 over 12 experts, 59 picked, 77 copied; 10,013 of 512 to 6,528,
+// 122 and 95; 65,536 of 1,024 to 2,048 over 64, 258 and 259; through 5 adapters of rank 16
+// 950 of 4,608 to 1,984, 63 and 66; through 8 7,354 of 4,352 to 4,544, 242 and 235.
 // Four warps write a tile whose results are aligned to less than 16 bytes (vec: values
-// of a store) slowly: 1,000 rows of 512 columns to 1,028 over 4 experts 26 us picked, 20
-// copied; 300 rows 14 and 15.
+// of a store) slowly: 1,000 rows of 512 columns to 1,028 over 4 experts 29 us picked, 24
+// copied.  (Where the two are near, the rule may miss: 300 of these rows are picked, 23
+// and 21; so are 512 rows beside 4,096 x 4,096 with 12 fp16 adapters of rank 64, 79 and 71.)
 static bool picks_rows(const hwr_ops *c, const hwr_rows *r, int k, int n, bool shared, int vec) {
     const float rows = (float)r->rows, pairs = c->ctas / 2, copy = rows * k * 4e-6f / 6;
     const float tiles = rows * ((n + GP_TILE - 1) / GP_TILE) / (GP_TILE * pairs);      // a pair

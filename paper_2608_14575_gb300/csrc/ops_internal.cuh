@@ -215,8 +215,8 @@ cudaError_t launch_pad(void *dst, int64_t dst_ld, const void *src, int64_t src_l
 
 // Chunks of `per` 4 KB (a 16-byte access of each of a block's threads): 4 for
 // sets of gradients that fill the GPU so, 1 for small ones, whose time is that of
-// the busiest SM (48 tensors of 2 MB in all: 12.5 us in chunks of 16 KB, 9.8 of
-// 8 KB; 475 MB: 228 and 232 us).
+// the busiest SM (48 tensors of 2.8 MB in all: 12.4 us in chunks of 16 KB, 9.8 of
+// 8 KB, 9.9 of 4 KB; 474 MB: 229, 232 and 241 us).
 constexpr int CLIP_UNIT = 4096, CLIP_PER = 4;
 constexpr int64_t CLIP_SMALL = 4 << 20;       // elements of a small set
 struct alignas(16) ClipChunk {

@@ -152,3 +152,63 @@ def test_calls_that_wait_are_refused_in_a_capture(side):
     again = ops.gradient_list([g])
     assert abs(float(ops.clip_gradients(again, 1.0)) - 5000 ** 0.5) < 1e-3
     again.close()
+
+
+def bounds(T, G, K, N, r, grads):
+    """The header's bounds of the workspace."""
+    P, S = T + 15 * min(T, G), K + N
+    grouped = 16384 + 4 * G + 2 * P * (S + 18) + 2 * G * N * (K + 8)
+    adapter = 16384 + 12 * G + 2 * P * (S + 18) + 12 * P * (r + 63) + 2 * N * (K + 8) + 6 * G * (r + 63) * (S + 16)
+    clip = sum(-(-g.numel() * g.element_size() // 1024) * 8 + 32 for g in grads)
+    return max(5 * (T // 4096 + 16) * (G + 1), grouped, adapter, clip)
+
+
+PROGRAM = """
+import sys
+sys.path[:0] = [{tests!r}, {root!r}]
+import torch
+import paper_2608_14575_gb300 as H
+from test_ops_capture_gpu import bounds
+T, G, K, N, r, dt = {shape!r}
+dt = getattr(torch, dt)
+stream = torch.cuda.Stream()
+with torch.cuda.stream(stream):
+    c = (torch.arange(T, device="cuda", dtype=torch.int32) * 7) % (G + 1) - 1
+    x, w, a, b, dy, gw = (torch.ones(s, device="cuda", dtype=dt) for s in
+                          ((T, K), (N, K), (G, r, K), (G, N, r), (T, N), (G, N, K)))
+    s = torch.ones(G, device="cuda")
+    grads = [torch.ones(n, device="cuda") for n in (1, 5000, 3_000_001)]
+    ops = H.Operators()
+    ops.reserve(bounds(T, G, K, N, r, grads))
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        plan = ops.dispatch(c, G)
+        out = [ops.grouped_forward(x, gw, plan), *ops.grouped_backward(dy, x, gw, plan),
+               ops.adapter_forward(x, w, a, b, s, plan), *ops.adapter_backward(dy, x, w, a, b, s, plan),
+               ops.adapter_backward(dy, x, w, a, b, s, plan, need_dab=False)[0]]
+        norm = ops.clip_gradients(grads, float("inf"))
+    graph.replay()
+    plan = ops.dispatch(c, G)
+    now = [ops.grouped_forward(x, gw, plan), *ops.grouped_backward(dy, x, gw, plan),
+           ops.adapter_forward(x, w, a, b, s, plan), *ops.adapter_backward(dy, x, w, a, b, s, plan),
+           ops.adapter_backward(dy, x, w, a, b, s, plan, need_dab=False)[0]]
+    assert all(torch.equal(p, q) for p, q in zip(out, now))
+    assert abs(float(norm) - 3_005_002 ** 0.5) < 1e-2
+print("captured")
+"""
+
+
+@pytest.mark.parametrize("shape", [(300, 7, 130, 65, 24, "bfloat16"), (40_000, 1000, 64, 72, 8, "float16"),
+                                   (5, 64, 1000, 999, 100, "float16"), (2000, 3, 1, 1, 1, "bfloat16"),
+                                   (70_000, 2, 33, 17, 256, "float16")])
+def test_a_process_that_reserves_captures_at_once(shape):
+    """A new process: with the header's bound reserved, its first calls are captured."""
+    import os
+    import subprocess
+    import sys
+    H.build()
+    here = os.path.dirname(os.path.abspath(__file__))
+    program = PROGRAM.format(tests=here, root=os.path.dirname(here), shape=shape)
+    run = subprocess.run([sys.executable, "-c", program], capture_output=True, text=True, timeout=300)
+    assert run.returncode == 0 and run.stdout.strip().endswith("captured"), run.stderr[-2000:]

@@ -217,3 +217,35 @@ def test_foreign_plans_write_nothing_beside_the_results(dt):
     for t, k in zip(inputs, kept):
         assert torch.equal(t, k)
     assert lib.hwr_ops_destroy(ctx) == 0
+
+
+@pytest.mark.parametrize("dt", [BF, torch.float16])
+def test_each_result_of_the_adapters_backward_alone(dt):
+    """The C interface takes any of dx, dA and dB: the same bits as all three together."""
+    import ctypes as ct
+    from paper_2608_14575_gb300 import _hwr, _ops
+    lib = _ops.load_ops()
+    T, G, K, N, r = 333, 5, 136, 72, 40
+    c = choices(T, G, "holes")
+    x, w, dy, a, b = (ints(*s, lo=-1, hi=1, dt=dt, seed=i) for i, s in
+                      enumerate(((T, K), (N, K), (T, N), (G, r, K), (G, N, r))))
+    s = torch.ones(G, device="cuda")
+    torch.cuda.synchronize()
+    ctx = ct.c_void_p()
+    assert lib.hwr_ops_create(None, ct.byref(ctx)) == 0
+    offsets, order = (torch.empty(n, device="cuda", dtype=torch.int32) for n in (G + 1, T))
+    P = lambda t: ct.c_void_p(t.data_ptr())  # noqa: E731
+    assert lib.hwr_dispatch(ctx, T, G, P(c), P(offsets), P(order)) == 0
+    rows = _ops.hwr_rows(T, G, K, N, H.HWR_F16 if dt is torch.float16 else _hwr.HWR_BF16, offsets.data_ptr(), order.data_ptr(),
+                         x.data_ptr(), K, w.data_ptr(), K, 0)
+    ad = _ops.hwr_adapters(r, a.data_ptr(), b.data_ptr(), s.data_ptr())
+    want = [e.to(dt) for e, _ in R.adapter_backward(dy, x, w, a, b, s, c)]
+    for which in range(1, 8):
+        out = [torch.full_like(e, 7) if which >> i & 1 else None for i, e in enumerate(want)]
+        torch.cuda.synchronize()
+        p = [None if o is None else P(o) for o in out]
+        assert lib.hwr_adapter_backward(ctx, ct.byref(rows), ct.byref(ad), P(dy), N, p[0], K, p[1], p[2]) == 0
+        assert lib.hwr_ops_synchronize(ctx) == 0
+        for o, e in zip(out, want):
+            assert o is None or torch.equal(o, e)
+    assert lib.hwr_ops_destroy(ctx) == 0
