@@ -870,8 +870,9 @@ extern "C" hwr_status hwr_adapter_backward(hwr_ops *c, const hwr_rows *r, const 
     const bool split = r->dtype == HWR_F16;
     Operand w, a, b, ea, u, v, ev;
     if (dx) w = cv.operand(r->w, r->w_ld, N, K);
-    if (dx) ea = ext_operand(cv, r, ad->a, K, R, true);
     if (db) a = cv.operand(ad->a, K, R, K, (int64_t)R * K, G);
+    const bool one = db && r->dtype == HWR_BF16;       // (dx and dB take the same A)
+    if (dx && !one) ea = ext_operand(cv, r, ad->a, K, R, true);
     if (dx || da) {
         b = cv.operand(ad->b, R, N, R, (int64_t)N * R, G);
         v = packed(cv, rows, ad);
@@ -890,8 +891,9 @@ extern "C" hwr_status hwr_adapter_backward(hwr_ops *c, const hwr_rows *r, const 
     uint32_t *const vpeak = split && da ? (uint32_t *)(c->ws + rows.peak_off) + G : nullptr;
     OK(sort_rows(c, &rows));
     if (dx) OK(settle(c, &w));
-    if (dx) OK(settle_ext(c, r, &ea, R, true));
     if (db) OK(settle(c, &a));
+    if (dx && one) ea = a;
+    if (dx && !one) OK(settle_ext(c, r, &ea, R, true));
     // v and u are independent of each other, and so are da and db: two in a launch,
     // on shares of the SMs by what they read (a launch of its own takes 10 us)
     GroupCall calls[2];
