@@ -30,6 +30,16 @@ struct ApiRange {
     ApiRange &operator=(const ApiRange &) = delete;
 };
 
+// Memory is taken and given back beside captures of other streams: without this, a
+// capture that watches the thread (the usual kind) would be spoilt by it.
+struct Unwatched {
+    cudaStreamCaptureMode mode = cudaStreamCaptureModeRelaxed;
+    Unwatched() { cudaThreadExchangeStreamCaptureMode(&mode); }
+    ~Unwatched() { cudaThreadExchangeStreamCaptureMode(&mode); }
+    Unwatched(const Unwatched &) = delete;
+    Unwatched &operator=(const Unwatched &) = delete;
+};
+
 }  // namespace
 
 // Device memory that a captured graph may hold, kept until the context goes.
@@ -123,6 +133,7 @@ static hwr_status alloc(hwr_ops *c, T **p, size_t n) {
     *p = nullptr;
     if (c->fail_at > 0 && ++c->allocs == c->fail_at)
         return fail(c, HWR_ERR_OOM, "allocation %ld failed (test hook)", c->allocs);
+    const Unwatched memory;
     const cudaError_t e = cudaMalloc((void **)p, n * sizeof(T));
     if (e != cudaSuccess) {
         cudaGetLastError();
@@ -165,6 +176,7 @@ static hwr_status reserve(hwr_ops *c, size_t bytes) {
             OK(retire(c, c->ws));
         } else {
             CK(c, cudaStreamSynchronize(c->stream), "synchronize before regrow");
+            const Unwatched memory;
             cudaFree(c->ws);
         }
         c->ws = nullptr;
@@ -185,6 +197,7 @@ extern "C" hwr_status hwr_ops_create(void *cuda_stream, hwr_ops **out) {
     if (const char *e = getenv("HWR_TEST_FAIL_ALLOC")) c->fail_at = atol(e);
     if (const char *e = getenv("HWR_TEST_STALL")) c->test_stall = atoi(e) != 0;
     if (const char *e = getenv("HWR_TEST_DEVICE")) c->test_device = atoi(e);
+    const Unwatched memory;
     auto body = [&]() -> hwr_status {
         CK(c, cudaGetDevice(&c->device), "cudaGetDevice");
         const int dev = c->device;
@@ -230,6 +243,7 @@ extern "C" hwr_status hwr_ops_create(void *cuda_stream, hwr_ops **out) {
 
 extern "C" hwr_status hwr_ops_destroy(hwr_ops *c) {
     if (!c) return HWR_OK;
+    const Unwatched memory;
     if (c->stream) cudaStreamSynchronize(c->stream);
     cudaFree(c->ws);
     while (hwr_gradients *l = c->lists) {
@@ -1036,6 +1050,7 @@ extern "C" hwr_status hwr_gradients_create(hwr_ops *c, int32_t n, const hwr_grad
     }
     delete[] host;
     if (s != HWR_OK) {
+        const Unwatched memory;
         if (l) cudaFree(l->table);
         delete l;
         return s;
@@ -1070,6 +1085,7 @@ extern "C" hwr_status hwr_gradients_destroy(hwr_ops *c, hwr_gradients *l) {
     if (captured || l->held) {          // (during a capture nothing is waited for or freed)
         OK(retire(c, l->table));
     } else {
+        const Unwatched memory;
         cudaStreamSynchronize(c->stream);
         cudaFree(l->table);
         cudaGetLastError();

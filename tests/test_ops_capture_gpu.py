@@ -212,3 +212,27 @@ def test_a_process_that_reserves_captures_at_once(shape):
     program = PROGRAM.format(tests=here, root=os.path.dirname(here), shape=shape)
     run = subprocess.run([sys.executable, "-c", program], capture_output=True, text=True, timeout=300)
     assert run.returncode == 0 and run.stdout.strip().endswith("captured"), run.stderr[-2000:]
+
+
+def test_other_contexts_come_and_go_beside_a_capture(side):
+    """What a context that takes no part in a capture allocates and frees leaves it alone."""
+    ops, stream = side
+    small = layer(30)
+    step(ops, *small)
+    other = [H.Operators(torch.cuda.Stream()) for _ in range(2)]
+    g = torch.ones(5000, device="cuda")
+    lists = [o.gradient_list([g]) for o in other]
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        held = step(ops, *small)
+        lists[0].close()
+        other[1].close()
+        lists[1].close()
+        new = H.Operators(torch.cuda.Stream())
+    graph.replay()
+    for got, exact in zip(held, want(*small)):
+        assert torch.equal(got, exact)
+    for o in (other[0], new):
+        assert torch.equal(o.adapter_forward(*small[1:5], small[6], o.dispatch(small[0], 5)), want(*small)[0])
+        o.close()
