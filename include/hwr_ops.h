@@ -12,6 +12,10 @@
  *   hwr_adapter_backward    dx, dA, dB of the same (W is left as it is)
  *   hwr_clip_gradients      global norm of many tensors, and clipping
  *   hwr_gradients_clip      the same over a list that is laid out once
+ *   hwr_adamw_step          the optimizer's step over many tensors at once
+ *   hwr_expert_layer        a whole layer of experts for the few rows of a decode step
+ *   hwr_token_logprobs      log probabilities, entropies and best alternatives of the
+ *                           tokens of an answer, and (_backward) their gradient
  *
  * Conventions (those of hwr.h, and)
  *   - A context of its own (hwr_ops): one CUDA stream, one workspace.  Calls
@@ -41,12 +45,16 @@
  *                      + 2 n_out (n_in + 8) + 6 groups (r + 63) (S + 16)
  *       hwr_clip_gradients  8 bytes for each 1,024 of the gradients' bytes and 32
  *                      for each gradient
- *     (weights that are read in place are the terms with n_out (n_in + 8) less).
+ *     (weights that are read in place are the terms with n_out (n_in + 8) less),
+ *       hwr_expert_layer  1,024 + 8 rows top (hidden + 7 + 8 n_out)
+ *       hwr_token_logprobs  1,088 for each of the device's SMs
+ *     and the other calls none.
  *   - Stream capture: calls can be captured into graphs.  A call that would have
  *     to grow the workspace then is refused (UNSUPPORTED, nothing is queued, the
  *     context stays usable): make a call of the same sizes before, or reserve.
- *     So are hwr_ops_synchronize and hwr_gradients_create.  Workspace and lists of
- *     gradients that a captured call uses are kept until hwr_ops_destroy, also when
+ *     So are hwr_ops_synchronize, hwr_gradients_create and hwr_adamw_create.  Workspace,
+ *     lists of gradients and optimizers' tables that a captured call uses are kept until
+ *     hwr_ops_destroy, also when
  *     a later call takes a larger block; the context outlives its graphs.  A replay
  *     uses the context's workspace, partial sums and counters as an eager call
  *     does: order it with the context's other work (the same stream, or
@@ -64,6 +72,12 @@ extern "C" {
 
 #define HWR_OPS_MAX_GROUPS 1024 /* groups of one plan */
 #define HWR_OPS_MAX_RANK 256    /* rank of an adapter */
+#define HWR_EXPERTS_MAX_ROWS 128    /* rows of a layer of experts (beyond: dispatch and grouped products) */
+#define HWR_EXPERTS_MAX_TOP 16      /* choices of a row */
+#define HWR_EXPERTS_MAX_OUT 65536   /* width of its result, */
+#define HWR_EXPERTS_MAX_WIDTH 262144    /* of its input and of the experts' hidden layer */
+#define HWR_TOKENS_MAX_TOP 32       /* alternatives of a token */
+#define HWR_ADAMW_BLOCK 256         /* elements that share a scale where moments have 8 bits */
 
 typedef struct hwr_ops hwr_ops;
 
@@ -178,6 +192,114 @@ hwr_status hwr_gradients_create(hwr_ops *ops, int32_t n, const hwr_gradient *gra
                                 hwr_gradients **out);
 hwr_status hwr_gradients_clip(hwr_ops *ops, const hwr_gradients *list, float max_norm, float *norm);
 hwr_status hwr_gradients_destroy(hwr_ops *ops, hwr_gradients *list);
+
+/*
+ * One AdamW step over many tensors.  With g the gradients (times min(1, max_norm /
+ * (norm + 1e-6)) where a norm is given), t the step's number, from 1:
+ *   m = beta1 m + (1 - beta1) g,   v = beta2 v + (1 - beta2) g^2
+ *   param -= lr (weight_decay param + (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps))
+ * Parameters are fp32; `copy`, where it is set, gets them rounded to copy_dtype (HWR_BF16
+ * or HWR_F16), for the products.  Moments are fp32, or (bits 8) m and sqrt(v) as e4m3
+ * values times a power of two of each HWR_ADAMW_BLOCK elements in m_scale and v_scale
+ * [(n + HWR_ADAMW_BLOCK - 1) / HWR_ADAMW_BLOCK].  They are rounded up or down by 16 bits
+ * of a hash of seed, t, the tensor's number and the element's: their expectation is the
+ * value, down to 2^-17 of their block's largest; the same call gives the same bits.  A
+ * positive sqrt(v) does not become 0.  A moment that is not finite makes its block NaN.
+ * All zeros (and scale 0) is the state before the first step.
+ */
+typedef struct {
+    float *param;             /* [n] */
+    void *copy;               /* [n], may be NULL */
+    hwr_dtype copy_dtype;
+    void *m, *v;              /* [n] fp32, or bytes */
+    float *m_scale, *v_scale; /* bits 8 only */
+    int64_t n;
+} hwr_adamw_tensor;
+
+typedef struct {
+    double lr, beta1, beta2, eps, weight_decay;
+    const float *lr_device;   /* device, one float in lr's place; may be NULL */
+    const float *norm;        /* device, one float (of hwr_clip_gradients, max_norm +inf); may be NULL */
+    float max_norm;           /* with norm: > 0 */
+    uint32_t seed;
+} hwr_adamw_options;
+
+/* An optimizer over tensors that stay where they are (its table is laid out in device
+ * memory once; synchronises the stream).  `step`, device, one int32: the number of steps
+ * done, which each step counts up, so that captured steps go on counting.  It and the
+ * tensors are the caller's, to be saved and restored; they go on existing as long as the
+ * optimizer.  An optimizer goes with its context, if not before. */
+typedef struct hwr_adamw hwr_adamw;
+hwr_status hwr_adamw_create(hwr_ops *ops, int32_t n, const hwr_adamw_tensor *tensors, int32_t bits,
+                            int32_t *step, hwr_adamw **out);
+/* grads, dtypes: host arrays of a device pointer (NULL: that tensor is left as it is) and
+ * a type (any of hwr_dtype) for each tensor.  A step whose norm is not finite changes
+ * nothing, and does not count. */
+hwr_status hwr_adamw_step(hwr_ops *ops, const hwr_adamw *optimizer, const hwr_adamw_options *options,
+                          const void *const *grads, const hwr_dtype *dtypes);
+hwr_status hwr_adamw_destroy(hwr_ops *ops, hwr_adamw *optimizer); /* synchronises; NULL is fine */
+
+/*
+ * A layer of experts for a few rows:
+ *   y[t] = sum over j < top of p[t][j] W_out[e] h,   e = the j-th choice of row t,
+ *   h = act(W_in[e] x[t])                                       (gated = 0), or
+ *   h = act(W_in[e][0 .. hidden) x[t]) * (W_in[e][hidden ..) x[t])   (gated)
+ * With scores [rows][groups], the choices are the `top` largest scores of a row (ties to
+ * the lowest index; NaN and -inf are never chosen), and p the softmax over them, or
+ * (over_all) over all of the row's scores.  Without, they are choice and gates
+ * [rows][top]; a choice outside [0, groups) is none, the same one may come twice.  A row
+ * without a choice gets zeros.  Experts that no row chooses are not read.
+ * h is summed in fp32 and enters the second product as two terms within 2^-15 of it (in
+ * fp16 layers 2^-20), at any magnitude; y is rounded once.
+ */
+typedef enum { HWR_ACT_SILU = 0, HWR_ACT_GELU = 1 /* u Phi(u) */, HWR_ACT_RELU = 2 } hwr_activation;
+typedef struct {
+    int32_t rows, groups, top;
+    int32_t n_in, hidden, n_out;
+    hwr_dtype dtype;          /* HWR_BF16 or HWR_F16: x, weights and y */
+    hwr_activation activation;
+    int32_t gated, over_all;
+    const void *x;            /* [rows][n_in] */
+    int64_t x_ld;
+    const void *w_in;         /* [groups][gated ? 2 hidden : hidden][n_in] */
+    int64_t w_in_ld, w_in_group;
+    const void *w_out;        /* [groups][n_out][hidden] */
+    int64_t w_out_ld, w_out_group;
+    const float *scores;      /* may be NULL */
+    int64_t scores_ld;
+    const int32_t *choice;
+    const float *gates;
+} hwr_experts;
+hwr_status hwr_expert_layer(hwr_ops *ops, const hwr_experts *layer, void *y, int64_t y_ld);
+
+/*
+ * Rows of logits z and a token of each; with q = softmax(z):
+ *   logprob [rows]   log q[token]; 0 for a token outside [0, vocab) or no tokens at all
+ *   entropy [rows]   -sum of q log q
+ *   stats [rows][2]  the largest logit, and the log of the sum of exp(z - largest)
+ *   top_token, top_logprob [rows][top]  the most probable tokens (ties to the lowest
+ *                    index, NaN last) and their log probabilities
+ * A logit of -inf has probability 0 and adds nothing.  A row of nothing else has
+ * probabilities 0: log probabilities -inf, entropy 0.  A NaN or +inf makes its row's
+ * results NaN (top_token apart).
+ */
+typedef struct {
+    int32_t rows, vocab;
+    hwr_dtype dtype;          /* HWR_F32, HWR_BF16 or HWR_F16 */
+    const void *logits;
+    int64_t ld;
+    const int32_t *token;     /* [rows], may be NULL */
+} hwr_logits;
+hwr_status hwr_token_logprobs(hwr_ops *ops, const hwr_logits *logits, int32_t top, float *logprob,
+                              float *entropy, float *stats, int32_t *top_token, float *top_logprob);
+/* The gradient of sum over rows of dlogprob logprob + dentropy entropy (either may be
+ * NULL: zeros) with respect to the logits, in their type: with a and b a row's two,
+ *   dz[v] = a (1[v = token] - q[v]) - b q[v] (log q[v] + entropy),
+ * a = 0 for a row without a token; zeros for a row of -inf.  entropy and stats: of
+ * hwr_token_logprobs.  dlogits may be the logits themselves. */
+hwr_status hwr_token_logprobs_backward(hwr_ops *ops, const hwr_logits *logits, const float *entropy,
+                                       const float *stats, const float *dlogprob, const float *dentropy,
+                                       void *dlogits, int64_t dlogits_ld);
 
 #ifdef __cplusplus
 }

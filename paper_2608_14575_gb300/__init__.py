@@ -15,6 +15,8 @@ from ._hwr import (HwrError, Router, load, lib_path, HWR_SEQUENTIAL,
                    hwr_route_batch_noalloc, HWR_NOALLOC_MAX_Q,
                    hwr_synchronize, hwr_destroy,
                    hwr_status_string, hwr_last_error, hwr_get_stats)
-from ._ops import (Operators, Plan, GradientList, HWR_F16, HWR_OPS_MAX_GROUPS,
-                   HWR_OPS_MAX_RANK)
+from ._ops import (Operators, Plan, GradientList, TokenLogprobs, AdamWState, HWR_F16,
+                   HWR_OPS_MAX_GROUPS, HWR_OPS_MAX_RANK, HWR_EXPERTS_MAX_ROWS,
+                   HWR_EXPERTS_MAX_TOP, HWR_EXPERTS_MAX_OUT, HWR_EXPERTS_MAX_WIDTH,
+                   HWR_TOKENS_MAX_TOP, HWR_ADAMW_BLOCK)
 from .build import build

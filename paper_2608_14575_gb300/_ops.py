@@ -12,6 +12,11 @@ functions keep their names in ``load_ops()``, their structures below.
     y = ops.adapter_forward(x, w, a, b, scale, plan)    # W x + scale B (A x)
     dx, da, db = ops.adapter_backward(dy, x, w, a, b, scale, plan)
     norm = ops.clip_gradients([dw, ...], max_norm=1.0)  # in place
+    state = ops.adamw_state([w32, ...], copies=[w, ...])
+    ops.adamw_step(state, [dw, ...], lr=1e-3)           # w32 and w
+    y = ops.expert_layer(x, w_in, w_out, scores=s, top=2)   # a decode step's few rows
+    got = ops.token_logprobs(logits, token, top=5)
+    dlogits = ops.token_logprobs_backward(a, logits, token, got)
 
 Tensors are CUDA tensors of the context's device whose last dimension is
 contiguous; other strides are free.  The context is bound to the torch stream
@@ -43,13 +48,22 @@ from ._hwr import HwrError
 HWR_F16 = 2
 HWR_OPS_MAX_GROUPS = 1024
 HWR_OPS_MAX_RANK = 256
+HWR_EXPERTS_MAX_ROWS = 128
+HWR_EXPERTS_MAX_TOP = 16
+HWR_EXPERTS_MAX_OUT = 65536
+HWR_EXPERTS_MAX_WIDTH = 262144
+HWR_TOKENS_MAX_TOP = 32
+HWR_ADAMW_BLOCK = 256
+ACTIVATIONS = {"silu": 0, "gelu": 1, "relu": 2}
 
 OPS_EXPORTS = ("hwr_ops_create", "hwr_ops_destroy", "hwr_ops_synchronize",
                "hwr_ops_last_error", "hwr_ops_reserve", "hwr_ops_after", "hwr_ops_before",
                "hwr_dispatch",
                "hwr_grouped_forward", "hwr_grouped_backward", "hwr_adapter_forward",
                "hwr_adapter_backward", "hwr_clip_gradients", "hwr_gradients_create",
-               "hwr_gradients_clip", "hwr_gradients_destroy")
+               "hwr_gradients_clip", "hwr_gradients_destroy", "hwr_adamw_create",
+               "hwr_adamw_step", "hwr_adamw_destroy", "hwr_expert_layer",
+               "hwr_token_logprobs", "hwr_token_logprobs_backward")
 
 
 class hwr_rows(ct.Structure):
@@ -67,6 +81,34 @@ class hwr_adapters(ct.Structure):
 class hwr_gradient(ct.Structure):
     _fields_ = [("in_", ct.c_void_p), ("out", ct.c_void_p), ("n", ct.c_int64),
                 ("dtype", ct.c_int)]
+
+
+class hwr_adamw_tensor(ct.Structure):
+    _fields_ = [("param", ct.c_void_p), ("copy", ct.c_void_p), ("copy_dtype", ct.c_int),
+                ("m", ct.c_void_p), ("v", ct.c_void_p), ("m_scale", ct.c_void_p),
+                ("v_scale", ct.c_void_p), ("n", ct.c_int64)]
+
+
+class hwr_adamw_options(ct.Structure):
+    _fields_ = [("lr", ct.c_double), ("beta1", ct.c_double), ("beta2", ct.c_double),
+                ("eps", ct.c_double), ("weight_decay", ct.c_double), ("lr_device", ct.c_void_p),
+                ("norm", ct.c_void_p), ("max_norm", ct.c_float), ("seed", ct.c_uint32)]
+
+
+class hwr_experts(ct.Structure):
+    _fields_ = [("rows", ct.c_int32), ("groups", ct.c_int32), ("top", ct.c_int32),
+                ("n_in", ct.c_int32), ("hidden", ct.c_int32), ("n_out", ct.c_int32),
+                ("dtype", ct.c_int), ("activation", ct.c_int), ("gated", ct.c_int32),
+                ("over_all", ct.c_int32), ("x", ct.c_void_p), ("x_ld", ct.c_int64),
+                ("w_in", ct.c_void_p), ("w_in_ld", ct.c_int64), ("w_in_group", ct.c_int64),
+                ("w_out", ct.c_void_p), ("w_out_ld", ct.c_int64), ("w_out_group", ct.c_int64),
+                ("scores", ct.c_void_p), ("scores_ld", ct.c_int64), ("choice", ct.c_void_p),
+                ("gates", ct.c_void_p)]
+
+
+class hwr_logits(ct.Structure):
+    _fields_ = [("rows", ct.c_int32), ("vocab", ct.c_int32), ("dtype", ct.c_int),
+                ("logits", ct.c_void_p), ("ld", ct.c_int64), ("token", ct.c_void_p)]
 
 
 _ready = None
@@ -93,6 +135,12 @@ def load_ops():
         lib.hwr_gradients_create.argtypes = [P, I, P, ct.POINTER(P)]
         lib.hwr_gradients_clip.argtypes = [P, P, ct.c_float, P]
         lib.hwr_gradients_destroy.argtypes = [P, P]
+        lib.hwr_adamw_create.argtypes = [P, I, P, I, P, ct.POINTER(P)]
+        lib.hwr_adamw_step.argtypes = [P, P, P, P, P]
+        lib.hwr_adamw_destroy.argtypes = [P, P]
+        lib.hwr_expert_layer.argtypes = [P, P, P, L]
+        lib.hwr_token_logprobs.argtypes = [P, P, I, P, P, P, P, P]
+        lib.hwr_token_logprobs_backward.argtypes = [P, P, P, P, P, P, P, L]
         for n in OPS_EXPORTS:
             getattr(lib, n).restype = ct.c_int
         lib.hwr_ops_last_error.restype = ct.c_char_p
@@ -149,6 +197,52 @@ class GradientList:
     def close(self):
         if self.handle and self.ops.ctx:      # (a closed context has freed its lists)
             self.ops.native.list_destroy(self.ops.ctx, self.handle)
+        self.handle = 0
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+class TokenLogprobs:
+    """Of a row of logits each: ``logprob`` of its token, ``entropy``, ``stats`` [rows][2]
+    (largest logit, log of the sum of exp(z - largest)), ``top_token`` and
+    ``top_logprob`` [rows][top] (None without alternatives)."""
+    __slots__ = ("logprob", "entropy", "stats", "top_token", "top_logprob")
+
+    def __init__(self, *values):
+        self.logprob, self.entropy, self.stats, self.top_token, self.top_logprob = values
+
+
+class AdamWState:
+    """Parameters and moments of an optimizer, made by ``Operators.adamw_state``.  The
+    tensors stay where they are; save and restore them in place.  ``m`` and ``v`` are
+    fp32, or (8 bits) e4m3 values of m and sqrt(v) with a power of two for each
+    ``HWR_ADAMW_BLOCK`` elements in ``m_scale`` and ``v_scale``; ``step`` [1] int32
+    counts the steps done."""
+
+    def __init__(self, ops, params, bits, copies, m, v, m_scale, v_scale, step):
+        self.ops, self.params, self.bits, self.copies = ops, params, bits, copies
+        self.m, self.v, self.m_scale, self.v_scale, self.step = m, v, m_scale, v_scale, step
+        self.handle = 0
+        self.handle = ops.native.adamw_create(ops.ctx, ops._current(), params, copies, m, v, m_scale,
+                                              v_scale, bits, step)
+
+    def moments(self, i: int):
+        """(m, v) of tensor i in fp32."""
+        if self.bits == 32:
+            return self.m[i], self.v[i]
+
+        def wide(values, scale):
+            flat = values.float().view(-1)
+            return (flat * scale.repeat_interleave(HWR_ADAMW_BLOCK)[:flat.numel()]).view(values.shape)
+        return wide(self.m[i], self.m_scale[i]), wide(self.v[i], self.v_scale[i]).square()
+
+    def close(self):
+        if self.handle:
+            self.ops.native.adamw_destroy(self.ops.ctx, self.handle)
         self.handle = 0
 
     def __del__(self):
@@ -224,6 +318,68 @@ class Operators:
         grads = list(grads)
         return self.native.clip(self.ctx, self._current(), grads,
                                 grads if out is None else list(out), max_norm)
+
+    def adamw_state(self, params, bits: int = 32, copies=None, m=None, v=None, m_scale=None, v_scale=None,
+                    step=None) -> AdamWState:
+        """State of an AdamW run over fp32 tensors ``params``, with ``copies`` in bf16 or
+        fp16 (None, or None for some) that each step rounds them to.  Moments of ``bits`` 32 or 8,
+        zeros unless they are given (lists as in ``AdamWState``), like ``step``."""
+        import torch
+        params = list(params)
+        kind = torch.float8_e4m3fn if bits == 8 else torch.float32
+        blocks = [-(-p.numel() // HWR_ADAMW_BLOCK) for p in params]
+
+        def state(given, wanted, shapes=None, dtype=torch.float32):
+            if given is not None or not wanted:
+                return None if given is None else list(given)
+            return [torch.zeros(s, dtype=dtype, device=p.device) for s, p in zip(shapes, params)]
+        shapes = [p.shape for p in params]
+        m, v = state(m, True, shapes, kind), state(v, True, shapes, kind)
+        m_scale, v_scale = state(m_scale, bits == 8, blocks), state(v_scale, bits == 8, blocks)
+        if step is None:
+            step = torch.zeros(1, dtype=torch.int32, device=self.stream.device)
+        return AdamWState(self, params, bits, state(copies, False), m, v, m_scale, v_scale, step)
+
+    def adamw_step(self, state: AdamWState, grads, lr, betas=(0.9, 0.999), eps: float = 1e-8,
+                   weight_decay: float = 0.01, norm=None, max_norm: float = float("inf"), seed: int = 0):
+        """One step (``state.step`` counts it): ``grads`` a gradient (fp32, bf16, fp16)
+        or None for each parameter, ``lr`` a number or an fp32 tensor on the device.  With ``norm``
+        (of ``clip_gradients``, max_norm inf: left as they are) the gradients are taken times
+        min(1, max_norm / (norm + 1e-6)), and a step whose norm is not finite is left
+        out.  ``seed``: of the 8-bit moments' rounding."""
+        if state.ops is not self or not state.handle:
+            raise ValueError("a state has its context, and is open")
+        self.native.adamw_step(self.ctx, self._current(), state.handle,
+                               grads if type(grads) is list else list(grads), lr, betas[0], betas[1], eps,
+                               weight_decay, norm, max_norm, seed)
+
+    def expert_layer(self, x, w_in, w_out, scores=None, top: int = 1, over_all: bool = False, choice=None,
+                     gates=None, activation: str = "silu", out=None):
+        """A layer of experts for up to ``HWR_EXPERTS_MAX_ROWS`` rows x [rows][K]:
+        y[t] = sum of p[t, j] w_out[e] h over the row's choices e, with
+        w_in [groups][2 F][K] h = act(w_in[e][:F] x[t]) * (w_in[e][F:] x[t]), with
+        [groups][F][K] h = act(w_in[e] x[t]); w_out [groups][N][F].  ``scores``
+        [rows][groups] fp32: the ``top`` largest are the choices, p the softmax over them (``over_all``:
+        over all scores).  Or ``choice`` [rows][top] int32 (outside [0, groups): none) and
+        ``gates`` [rows][top] fp32, the p.  ``activation``: "silu", "gelu" (u Phi(u)), "relu"."""
+        if activation not in ACTIVATIONS:
+            raise ValueError(f"activation {activation!r}: want one of {', '.join(ACTIVATIONS)}")
+        y = self.native.expert_layer(self.ctx, self._current(), x, w_in, w_out, scores, top, over_all, choice,
+                                     gates, ACTIVATIONS[activation], out)
+        return y if out is None else out
+
+    def token_logprobs(self, logits, token=None, top: int = 0) -> TokenLogprobs:
+        """Log probability of each row's ``token`` [rows] int32 (0 for one outside
+        [0, vocab)) under softmax(logits [rows][vocab]), entropies, and the ``top`` most
+        probable tokens."""
+        return TokenLogprobs(*self.native.token_logprobs(self.ctx, self._current(), logits, token, top))
+
+    def token_logprobs_backward(self, dlogprob, logits, token, got: TokenLogprobs, dentropy=None, out=None):
+        """The gradient with respect to the logits of sum(dlogprob * logprob + dentropy *
+        entropy) (either may be None), in the logits' type; ``out`` may be the logits."""
+        dz = self.native.token_logprobs_backward(self.ctx, self._current(), dlogprob, logits, token, got.entropy,
+                                                 got.stats, dentropy, out)
+        return dz if out is None else out
 
     def reserve(self, nbytes: int):
         """Make the workspace at least ``nbytes`` large (before a stream capture)."""

@@ -36,6 +36,10 @@ SOURCES = {
     "k_group.cu": [],
     "k_ops.cu": [],
     "k_few.cu": [],
+    "ops_model.cu": [],
+    "k_experts.cu": [],
+    "k_tokens.cu": [],
+    "k_adamw.cu": [],
 }
 
 

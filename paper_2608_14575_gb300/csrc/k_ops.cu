@@ -1,6 +1,7 @@
 // Dispatch (stable grouping of rows by choice), gradient clipping and padding
 // copies: the memory-bound kernels beside the grouped products.
 #include "ops_internal.cuh"
+#include "values.cuh"
 
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -575,54 +576,6 @@ k_pad(uint16_t *dst, int64_t dst_ld, const uint16_t *src, int64_t src_ld, int64_
 constexpr int CL_THREADS = 256;
 static_assert(CLIP_UNIT == CL_THREADS * 16, "a 16-byte access a thread");
 
-template <int DT>
-struct Vec {
-    static constexpr int N = DT == HWR_F32 ? 4 : 8;      // values of 16 bytes
-    __device__ static void unpack(const uint4 &u, float (&f)[N]) {
-        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if (DT == HWR_F32) {
-                f[i] = __uint_as_float(w[i]);
-            } else if (DT == HWR_BF16) {
-                f[(2 * i) % N] = __uint_as_float(w[i] << 16);
-                f[(2 * i + 1) % N] = __uint_as_float(w[i] & 0xffff0000u);
-            } else {
-                const float2 v = __half22float2(*(const __half2 *)&w[i]);
-                f[(2 * i) % N] = v.x;
-                f[(2 * i + 1) % N] = v.y;
-            }
-        }
-    }
-    __device__ static uint4 pack(const float (&f)[N]) {
-        uint32_t w[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if (DT == HWR_F32) {
-                w[i] = __float_as_uint(f[i]);
-            } else if (DT == HWR_BF16) {
-                const __nv_bfloat162 v = __floats2bfloat162_rn(f[(2 * i) % N], f[(2 * i + 1) % N]);
-                w[i] = *(const uint32_t *)&v;
-            } else {
-                const __half2 v = __floats2half2_rn(f[(2 * i) % N], f[(2 * i + 1) % N]);
-                w[i] = *(const uint32_t *)&v;
-            }
-        }
-        return make_uint4(w[0], w[1], w[2], w[3]);
-    }
-    __device__ static float load(const void *p, int i) {
-        if (DT == HWR_F32) return ((const float *)p)[i];
-        if (DT == HWR_BF16) return __bfloat162float(((const __nv_bfloat16 *)p)[i]);
-        return __half2float(((const __half *)p)[i]);
-    }
-    __device__ static void store(void *p, int i, float v) {
-        if (DT == HWR_F32) ((float *)p)[i] = v;
-        else if (DT == HWR_BF16) ((__nv_bfloat16 *)p)[i] = __float2bfloat16_rn(v);
-        else ((__half *)p)[i] = __float2half_rn(v);
-    }
-    static constexpr int FULL = CLIP_UNIT / (DT == HWR_F32 ? 4 : 2);      // of a unit
-};
-
 // The squares of a thread's share of a chunk once more, in 64 bits: where
 // their fp32 sum left the range that fp32 holds well.
 template <int DT, int CL_PER>
@@ -653,7 +606,7 @@ struct Pair {
 template <int DT, int CL_PER>
 __device__ __forceinline__ void sum_chunk(const ClipChunk &c, Pair &acc, double &wide) {
     constexpr int N = Vec<DT>::N;
-    const bool vec = c.n == CL_PER * Vec<DT>::FULL && ((uintptr_t)c.in & 15) == 0;
+    const bool vec = c.n == clip_elems(DT, CL_PER) && ((uintptr_t)c.in & 15) == 0;
     float s = 0.f;
     if (vec) {
         const uint4 *v = (const uint4 *)c.in + threadIdx.x;
@@ -688,7 +641,7 @@ __device__ __forceinline__ void sum_chunk(const ClipChunk &c, Pair &acc, double 
 template <int DT, int CL_PER>
 __device__ __forceinline__ void scale_chunk(const ClipChunk &c, float k) {
     constexpr int N = Vec<DT>::N;
-    if (c.n == CL_PER * Vec<DT>::FULL && (((uintptr_t)c.in | (uintptr_t)c.out) & 15) == 0) {
+    if (c.n == clip_elems(DT, CL_PER) && (((uintptr_t)c.in | (uintptr_t)c.out) & 15) == 0) {
         // (read for the last time, written for others: neither is to push out of L2
         // what the first pass left there)
         const uint4 *v = (const uint4 *)c.in + threadIdx.x;

@@ -54,6 +54,8 @@ extern "C" hwr_status hwr_ops_create(void *cuda_stream, hwr_ops **out) {
         OK(alloc(c, &c->sums, clip_blocks(INT64_MAX, c->nsm) + 1));
         CK(c, cudaMemsetAsync(c->sums, 0, (clip_blocks(INT64_MAX, c->nsm) + 1) * sizeof(double), c->stream), "memset");
         CK(c, cudaMemsetAsync(c->count, 0, c->ctas * sizeof(uint32_t), c->stream), "memset");
+        OK(alloc(c, &c->arrivals, ARRIVALS));
+        CK(c, cudaMemsetAsync(c->arrivals, 0, ARRIVALS * sizeof(uint32_t), c->stream), "memset");
         return HWR_OK;
     };
     const hwr_status s = body();
@@ -76,6 +78,12 @@ extern "C" hwr_status hwr_ops_destroy(hwr_ops *c) {
         cudaFree(l->table);
         delete l;
     }
+    while (hwr_adamw *o = c->optimizers) {
+        c->optimizers = o->next;
+        cudaFree(o->table);
+        delete[] o->chunk0;
+        delete o;
+    }
     while (Retired *r = c->retired) {
         c->retired = r->next;
         cudaFree(r->p);
@@ -84,6 +92,7 @@ extern "C" hwr_status hwr_ops_destroy(hwr_ops *c) {
     cudaFree(c->part);
     cudaFree(c->count);
     cudaFree(c->sums);
+    cudaFree(c->arrivals);
     if (c->status_h) cudaFreeHost(c->status_h);
     if (c->event) cudaEventDestroy(c->event);
     if (c->own_stream) cudaStreamDestroy(c->stream);

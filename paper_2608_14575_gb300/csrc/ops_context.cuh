@@ -53,6 +53,19 @@ struct hwr_gradients {
     hwr_gradients *next = nullptr;      // of the context's lists
 };
 
+struct hwr_adamw {
+    AdamWChunk *table = nullptr;
+    int n = 0, bits = 32;
+    int *chunk0 = nullptr;              // host, [n + 1]: first chunk of each tensor
+    int32_t *step = nullptr;
+    mutable bool held = false;
+    hwr_adamw *next = nullptr;          // of the context's optimizers
+};
+
+// Words that blocks count their arrivals in (zeroed once, self-resetting).
+constexpr int ARRIVALS_TILES = 0, ARRIVALS_ROWS = EXPERTS_MAX_OUT / 16, ARRIVALS_STEP = ARRIVALS_ROWS + 1024,
+              ARRIVALS = ARRIVALS_STEP + 1;
+
 struct hwr_ops {
     cudaStream_t stream = nullptr;
     bool own_stream = false, broken = false;
@@ -65,6 +78,8 @@ struct hwr_ops {
     bool ws_held = false;        // a captured call has its address
     Retired *retired = nullptr;
     hwr_gradients *lists = nullptr;
+    hwr_adamw *optimizers = nullptr;
+    uint32_t *arrivals = nullptr;
     float *part = nullptr;       // partial tiles of the grouped products
     uint32_t *count = nullptr;   // their arrivals (zeroed once, self-resetting)
     double *sums = nullptr;      // partial sums of squares; then their arrivals and the factor

@@ -258,4 +258,89 @@ struct ClipSums {
 cudaError_t launch_clip(const ClipChunk *table, int chunks, int per, int nsm, const ClipSums &sums, float max_norm,
                         float *norm, cudaStream_t s);
 
+// ---- rows of logits (k_tokens.cu) --------------------------------------------
+
+constexpr int TOKENS_MAX_TOP = HWR_TOKENS_MAX_TOP;
+constexpr int TOKEN_SPLITS = 32;      // pieces of a row, at most
+struct TokenPart {                    // of a piece: the sums, and its best keys
+    float m, s, d, unused;
+    uint64_t key[32];
+};
+struct TokenRows {
+    int rows, vocab, top, splits;
+    const void *logits;
+    int64_t ld;
+    const int32_t *token;             // may be null
+    float *logprob, *entropy, *stats;
+    int32_t *top_token;
+    float *top_logprob;
+    TokenPart *part;                  // [rows][splits] where splits > 1
+    uint32_t *arrivals;               // [rows] zeroed once, self-resetting
+};
+int token_splits(int rows, int vocab, hwr_dtype dtype, int nsm);
+cudaError_t launch_token_rows(const TokenRows &p, hwr_dtype dtype, cudaStream_t s);
+struct TokenGrad {
+    int rows, vocab, splits;
+    const void *logits;
+    int64_t ld;
+    const int32_t *token;
+    const float *stats, *entropy, *da, *db;
+    void *out;
+    int64_t out_ld;
+};
+cudaError_t launch_token_grad(TokenGrad p, hwr_dtype dtype, int nsm, cudaStream_t s);
+
+// ---- the optimizer's step (k_adamw.cu) ----------------------------------------
+
+// A block's elements; with moments in 8 bits a warp's share one power of two.
+constexpr int ADAMW_CHUNK = 2048, ADAMW_BLOCK = 256;
+constexpr int ADAMW_TABLE = 256;      // tensors of one launch
+struct alignas(16) AdamWChunk {
+    float *param;
+    void *copy, *m, *v;               // copy: may be null
+    float *m_scale, *v_scale;
+    int64_t first;                    // of its elements in the tensor
+    int32_t n, tensor;
+    int32_t copy_dtype, unused[3];
+};
+struct AdamWStep {
+    const AdamWChunk *table;
+    int chunks, tensor0;              // chunks of this launch; the first of its tensors
+    uint32_t blocks;                  // of all the call's launches
+    uint32_t *arrivals;
+    int32_t *step;
+    const float *lr, *norm;           // device values, may be null
+    float rate, max_norm, b1, b2, one_b1, one_b2, log_b1, log_b2, eps, decay;
+    uint32_t seed;
+    const void *grad[ADAMW_TABLE];    // null: the tensor is left as it is
+    uint8_t dtype[ADAMW_TABLE];
+};
+int adamw_grid(int chunks, int nsm);
+cudaError_t launch_adamw(const AdamWStep &p, int bits, int grid, cudaStream_t s);
+
+// ---- a layer of experts for a few rows (k_experts.cu) ---------------------------
+
+constexpr int EXPERTS_MAX_ROWS = HWR_EXPERTS_MAX_ROWS, EXPERTS_MAX_TOP = HWR_EXPERTS_MAX_TOP;
+constexpr int EXPERTS_MAX_OUT = HWR_EXPERTS_MAX_OUT, EXPERTS_MAX_WIDTH = HWR_EXPERTS_MAX_WIDTH;
+struct Experts {
+    int rows, groups, top, n_in, hidden, n_out;
+    int gated, act, over_all;
+    const uint16_t *x, *w_in, *w_out;
+    int64_t x_ld, w_in_ld, w_in_z, w_out_ld, w_out_z;
+    const float *scores;              // null: choice and gates are given
+    int64_t scores_ld;
+    const int32_t *choice;
+    const float *gates;
+    uint16_t *y;
+    int64_t y_ld;
+    // workspace: h as two terms [rows * top][h_groups][2][8], bf16 or fp32; what each piece
+    // of the second product gives [rows * top][splits][n_out]
+    void *h;
+    int h_groups, splits;
+    float *part;
+    uint32_t *arrivals;               // [tiles of 16 outputs] zeroed once, self-resetting
+};
+int expert_splits(int rows, int groups, int top, int hidden, int n_out, int nsm);
+cudaError_t launch_experts(const Experts &p, bool f16, int nsm, cudaStream_t s);
+
 }  // namespace hwr

@@ -510,6 +510,257 @@ PyObject *list_destroy(PyObject *, PyObject *const *a, Py_ssize_t n) {
     });
 }
 
+// x, w_in, w_out, scores, top, over_all, choice, gates, activation, out
+PyObject *expert_layer(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return guarded([&] {
+        want(n, 12);
+        Context &c = context(a[0]);
+        const at::Tensor &x = tensor(a[2], "x"), &w_in = tensor(a[3], "w_in"), &w_out = tensor(a[4], "w_out");
+        const at::ScalarType dt = x.scalar_type();
+        hwr_experts e = {};
+        e.dtype = sixteen(x, "x");
+        if (x.dim() != 2) throw ValueError("x: want [rows][K]");
+        if (w_in.dim() != 3) throw ValueError("w_in: want [groups][hidden or 2 hidden][K]");
+        if (w_out.dim() != 3) throw ValueError("w_out: want [groups][N][hidden]");
+        const int64_t T = x.size(0), K = x.size(1), E = w_in.size(0), F = w_out.size(2), N = w_out.size(1);
+        const int64_t wide = w_in.size(1);
+        if (wide != F && wide != 2 * F)
+            throw ValueError("w_in: " + std::to_string(wide) + " rows for a hidden width of " + std::to_string(F));
+        e.rows = narrow(T, "rows");
+        e.groups = narrow(E, "groups");
+        e.n_in = narrow(K, "n_in");
+        e.hidden = narrow(F, "hidden");
+        e.n_out = narrow(N, "n_out");
+        e.gated = wide != F;
+        e.x_ld = rows_stride(c, x, {T, K}, dt, "x");
+        e.x = x.data_ptr();
+        e.w_in_ld = rows_stride(c, w_in, {E, wide, K}, dt, "w_in");
+        e.w_in_group = E > 1 ? w_in.stride(0) : e.w_in_ld * wide;
+        e.w_in = w_in.data_ptr();
+        e.w_out_ld = rows_stride(c, w_out, {E, N, F}, dt, "w_out");
+        e.w_out_group = E > 1 ? w_out.stride(0) : e.w_out_ld * N;
+        e.w_out = w_out.data_ptr();
+        if (a[5] != Py_None) {
+            if (a[8] != Py_None || a[9] != Py_None) throw ValueError("want scores, or choice and gates");
+            const at::Tensor &s = tensor(a[5], "scores");
+            const long long top = PyLong_AsLongLong(a[6]);
+            if (PyErr_Occurred()) throw PythonError();
+            if (top < 1 || top > E) throw ValueError("top " + std::to_string(top) + " of " + std::to_string(E) + " groups");
+            e.top = narrow(top, "top");
+            e.over_all = truth(a[7]);
+            e.scores_ld = rows_stride(c, s, {T, E}, at::kFloat, "scores");
+            e.scores = (const float *)s.data_ptr();
+        } else {
+            const at::Tensor &choice = tensor(a[8], "choice"), &gates = tensor(a[9], "gates");
+            if (choice.dim() != 2) throw ValueError("choice: want [rows][top]");
+            const int64_t top = choice.size(1);
+            if (top < 1) throw ValueError("choice: no columns");
+            e.top = narrow(top, "top");
+            e.choice = (const int32_t *)contiguous(c, choice, {T, top}, at::kInt, "choice");
+            e.gates = (const float *)contiguous(c, gates, {T, top}, at::kFloat, "gates");
+        }
+        e.activation = (hwr_activation)PyLong_AsLong(a[10]);
+        if (PyErr_Occurred()) throw PythonError();
+        int64_t ld;
+        at::Tensor y = output(c, a[11], T, N, x, &ld);
+        call(c, a[1], [&] { return hwr_expert_layer(c.ops, &e, y.data_ptr(), ld); });
+        if (a[11] != Py_None) written(y);
+        return wrap(std::move(y));
+    });
+}
+
+hwr_dtype any_float(const at::Tensor &t, const char *name) {
+    if (t.scalar_type() == at::kFloat) return HWR_F32;
+    return sixteen(t, name);
+}
+
+hwr_logits fill_logits(const Context &c, const at::Tensor &z, PyObject *token) {
+    if (z.dim() != 2) throw ValueError("logits: want [rows][vocab]");
+    hwr_logits l = {};
+    l.rows = narrow(z.size(0), "rows");
+    l.vocab = narrow(z.size(1), "vocab");
+    l.dtype = any_float(z, "logits");
+    l.ld = rows_stride(c, z, z.sizes(), z.scalar_type(), "logits");
+    l.logits = z.data_ptr();
+    if (token != Py_None) l.token = (const int32_t *)contiguous(c, tensor(token, "token"), {z.size(0)}, at::kInt, "token");
+    return l;
+}
+
+// logits, token, top -> (logprob, entropy, stats, top_token, top_logprob)
+PyObject *token_logprobs(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return guarded([&] {
+        want(n, 5);
+        Context &c = context(a[0]);
+        const at::Tensor &z = tensor(a[2], "logits");
+        const hwr_logits l = fill_logits(c, z, a[3]);
+        const long long top = PyLong_AsLongLong(a[4]);
+        if (PyErr_Occurred()) throw PythonError();
+        if (top < 0 || top > z.size(1)) throw ValueError("top " + std::to_string(top) + " of " + std::to_string(z.size(1)));
+        const int64_t T = z.size(0);
+        const at::TensorOptions f32 = z.options().dtype(at::kFloat);
+        at::Tensor logprob = at::empty({T}, f32), entropy = at::empty({T}, f32), stats = at::empty({T, 2}, f32);
+        at::Tensor top_token, top_logprob;
+        if (top > HWR_TOKENS_MAX_TOP)
+            throw StatusError(HWR_ERR_UNSUPPORTED, ("top " + std::to_string(top) + " > " + std::to_string(HWR_TOKENS_MAX_TOP)).c_str());
+        if (top) {
+            top_token = at::empty({T, top}, f32.dtype(at::kInt));
+            top_logprob = at::empty({T, top}, f32);
+        }
+        call(c, a[1], [&] {
+            return hwr_token_logprobs(c.ops, &l, (int32_t)top, (float *)logprob.data_ptr(), (float *)entropy.data_ptr(),
+                                      (float *)stats.data_ptr(), top ? (int32_t *)top_token.data_ptr() : nullptr,
+                                      top ? (float *)top_logprob.data_ptr() : nullptr);
+        });
+        return tuple({logprob, entropy, stats, top_token, top_logprob});
+    });
+}
+
+// dlogprob, logits, token, entropy, stats, dentropy, out -> dlogits
+PyObject *token_logprobs_backward(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return guarded([&] {
+        want(n, 9);
+        Context &c = context(a[0]);
+        const at::Tensor &z = tensor(a[3], "logits");
+        const hwr_logits l = fill_logits(c, z, a[4]);
+        const int64_t T = z.size(0);
+        auto row_values = [&](PyObject *o, at::IntArrayRef shape, const char *name) -> const float * {
+            return o == Py_None ? nullptr : (const float *)contiguous(c, tensor(o, name), shape, at::kFloat, name);
+        };
+        const float *da = row_values(a[2], {T}, "dlogprob"), *db = row_values(a[7], {T}, "dentropy");
+        const float *entropy = row_values(a[5], {T}, "entropy"), *stats = row_values(a[6], {T, 2}, "stats");
+        int64_t ld;
+        at::Tensor dz = output(c, a[8], T, z.size(1), z, &ld);
+        call(c, a[1], [&] {
+            return hwr_token_logprobs_backward(c.ops, &l, entropy, stats, da, db, dz.data_ptr(), ld);
+        });
+        if (a[8] != Py_None) written(dz);
+        return wrap(std::move(dz));
+    });
+}
+
+// An optimizer and the tensors that it writes.
+struct Optimizer {
+    hwr_adamw *o = nullptr;
+    std::vector<int64_t> n;
+    std::vector<at::Tensor> tensors;
+    std::vector<const void *> grads;      // of a call
+    std::vector<hwr_dtype> dtypes;
+};
+
+// params, copies, m, v, m_scale, v_scale (lists; the copies and scales may be None), bits, step -> handle
+PyObject *adamw_create(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return guarded([&] {
+        want(n, 10);
+        Context &c = context(a[0]);
+        const char *names[6] = {"params", "copies", "m", "v", "m_scale", "v_scale"};
+        const long bits = PyLong_AsLong(a[8]);
+        if (PyErr_Occurred()) throw PythonError();
+        if (bits != 8 && bits != 32) throw ValueError("bits " + std::to_string(bits) + ": want 8 or 32");
+        for (int k = 0; k < 6; ++k) {
+            const bool need = k == 0 || k == 2 || k == 3 || (k > 3 && bits == 8);
+            if (a[2 + k] == Py_None && !need) continue;
+            if (!PyList_Check(a[2 + k])) throw TypeError(std::string(names[k]) + ": want a list of tensors");
+            if (PyList_GET_SIZE(a[2 + k]) != PyList_GET_SIZE(a[2]))
+                throw ValueError(std::string(names[k]) + ": not as many as parameters");
+        }
+        const Py_ssize_t count = PyList_GET_SIZE(a[2]);
+        std::vector<hwr_adamw_tensor> v((size_t)count);
+        Optimizer o;
+        for (Py_ssize_t i = 0; i < count; ++i) {
+            hwr_adamw_tensor &e = v[(size_t)i];
+            const at::Tensor &p = tensor(PyList_GET_ITEM(a[2], i), "a parameter");
+            const auto given = [&](int k, at::IntArrayRef shape, at::ScalarType dtype) {
+                const at::Tensor &t = tensor(PyList_GET_ITEM(a[2 + k], i), names[k]);
+                void *at = const_cast<void *>(contiguous(c, t, shape, dtype, names[k]));
+                o.tensors.push_back(t);
+                return at;
+            };
+            e.n = p.numel();
+            e.param = (float *)given(0, p.sizes(), at::kFloat);
+            if (a[3] != Py_None && PyList_GET_ITEM(a[3], i) != Py_None) {
+                const at::Tensor &q = tensor(PyList_GET_ITEM(a[3], i), "a copy");
+                e.copy_dtype = sixteen(q, "a copy");
+                e.copy = given(1, p.sizes(), q.scalar_type());
+            }
+            const at::ScalarType kind = bits == 8 ? at::kFloat8_e4m3fn : at::kFloat;
+            e.m = given(2, p.sizes(), kind);
+            e.v = given(3, p.sizes(), kind);
+            if (bits == 8) {
+                const int64_t blocks = (e.n + HWR_ADAMW_BLOCK - 1) / HWR_ADAMW_BLOCK;
+                e.m_scale = (float *)given(4, {blocks}, at::kFloat);
+                e.v_scale = (float *)given(5, {blocks}, at::kFloat);
+            }
+            o.n.push_back(e.n);
+        }
+        const at::Tensor &step = tensor(a[9], "step");
+        int32_t *at = (int32_t *)const_cast<void *>(contiguous(c, step, {1}, at::kInt, "step"));
+        o.tensors.push_back(step);
+        o.grads.resize((size_t)count);
+        o.dtypes.resize((size_t)count);
+        const int m = narrow(count, "tensors");
+        call(c, a[1], [&] { return hwr_adamw_create(c.ops, m, v.data(), (int32_t)bits, at, &o.o); });
+        return PyLong_FromVoidPtr(new Optimizer(std::move(o)));
+    });
+}
+
+// handle, grads, lr (number or tensor), beta1, beta2, eps, weight_decay, norm, max_norm, seed
+PyObject *adamw_step(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return guarded([&]() -> PyObject * {
+        want(n, 12);
+        Context &c = context(a[0]);
+        Optimizer &o = *(Optimizer *)address(a[2]);
+        if (!PyList_Check(a[3])) throw TypeError("grads: want a list of tensors");
+        if ((size_t)PyList_GET_SIZE(a[3]) != o.n.size())
+            throw ValueError(std::to_string(PyList_GET_SIZE(a[3])) + " gradients for " + std::to_string(o.n.size()) + " parameters");
+        for (size_t i = 0; i < o.n.size(); ++i) {
+            PyObject *item = PyList_GET_ITEM(a[3], (Py_ssize_t)i);
+            o.grads[i] = nullptr;
+            o.dtypes[i] = HWR_F32;
+            if (item == Py_None) continue;
+            const at::Tensor &g = tensor(item, "a gradient");
+            o.dtypes[i] = any_float(g, "a gradient");
+            on_device(c, g, "a gradient");
+            if (g.numel() != o.n[i])
+                throw ValueError("gradient " + std::to_string(i) + " has " + std::to_string(g.numel()) + " elements, its parameter " + std::to_string(o.n[i]));
+            if (!g.is_contiguous()) throw ValueError("want contiguous gradients");
+            o.grads[i] = g.data_ptr();
+        }
+        const auto scalar_at = [&](PyObject *t, const char *name) {
+            const at::Tensor &s = tensor(t, name);
+            if (s.numel() != 1) throw ValueError(std::string(name) + ": want one value");
+            typed(s, at::kFloat, name);
+            on_device(c, s, name);
+            return (const float *)s.data_ptr();
+        };
+        hwr_adamw_options p = {};
+        if (THPVariable_Check(a[4])) p.lr_device = scalar_at(a[4], "lr");
+        else p.lr = number(a[4]);
+        p.beta1 = number(a[5]);
+        p.beta2 = number(a[6]);
+        p.eps = number(a[7]);
+        p.weight_decay = number(a[8]);
+        if (a[9] != Py_None) p.norm = scalar_at(a[9], "norm");
+        p.max_norm = (float)number(a[10]);
+        p.seed = (uint32_t)PyLong_AsUnsignedLongMask(a[11]);
+        if (PyErr_Occurred()) throw PythonError();
+        call(c, a[1], [&] { return hwr_adamw_step(c.ops, o.o, &p, o.grads.data(), o.dtypes.data()); });
+        for (const at::Tensor &t : o.tensors) written(t);
+        Py_RETURN_NONE;
+    });
+}
+
+// handle; the context where it is still open (or 0)
+PyObject *adamw_destroy(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return guarded([&]() -> PyObject * {
+        want(n, 2);
+        Optimizer *o = (Optimizer *)address(a[1]);
+        Context *c = (Context *)address(a[0]);
+        if (c) hwr_adamw_destroy(c->ops, o->o);      // (a closed context has freed its optimizers)
+        delete o;
+        Py_RETURN_NONE;
+    });
+}
+
 PyObject *set_error(PyObject *, PyObject *const *a, Py_ssize_t n) {
     return guarded([&]() -> PyObject * {
         want(n, 1);
@@ -524,7 +775,9 @@ PyObject *set_error(PyObject *, PyObject *const *a, Py_ssize_t n) {
 PyMethodDef methods[] = {METHOD(create), METHOD(destroy), METHOD(synchronize), METHOD(reserve), METHOD(dispatch),
                          METHOD(grouped_forward), METHOD(grouped_backward), METHOD(adapter_forward),
                          METHOD(adapter_backward), METHOD(clip), METHOD(list_create), METHOD(list_clip),
-                         METHOD(list_destroy), METHOD(set_error), {nullptr, nullptr, 0, nullptr}};
+                         METHOD(list_destroy), METHOD(expert_layer), METHOD(token_logprobs),
+                         METHOD(token_logprobs_backward), METHOD(adamw_create), METHOD(adamw_step),
+                         METHOD(adamw_destroy), METHOD(set_error), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "hwr_torch", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
