@@ -128,7 +128,8 @@ def tokens_backward(logits, token, a, b):
     at = torch.where(has, token, torch.zeros_like(token)).long()[:, None]
     g.scatter_add_(1, at, a)
     e_lq = r["e_log"][:, None] + 2.0 ** -22 * (r["dist"] + torch.where(q > 0, logq.abs(), torch.zeros_like(q)))
-    e_q = q * (e_lq + FUNC + 2.0 ** -23 * torch.where(q > 0, logq.abs(), torch.zeros_like(q)))
+    # (an exp below fp32's smallest normal number, 2^-126, counts as 0: off by less than that)
+    e_q = 2.0 ** -126 + q * (e_lq + FUNC + 2.0 ** -23 * torch.where(q > 0, logq.abs(), torch.zeros_like(q)))
     err = (e_q + q * 2.0 ** -22) * (a.abs() + b.abs() * inner.abs()) + q * b.abs() * (e_lq + eH[:, None])
     err = err + 2.0 ** -22 * a.abs() * torch.zeros_like(q).scatter_(1, at, 1.0)
     unit, floor = (U32, 2.0 ** -126) if logits.dtype == torch.float32 else (UNIT[logits.dtype], FLOOR[logits.dtype])
