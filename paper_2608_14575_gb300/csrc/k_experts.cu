@@ -1,68 +1,80 @@
 // A layer of experts for a few rows (decode steps): routing, both products, the
-// activation between them and the sum over a row's choices, in two launches.
+// activation between them and the sum over a row's choices, in two or three launches.
 //
 //   k_experts_in    h[t, j] = act(W_gate[e] x[t]) * (W_up[e] x[t])  (or act(W_in[e] x[t]))
-//   k_experts_out   y[t] = sum over j of p[t, j] W_out[e] h[t, j]
+//   k_experts_out   z[t, j] = W_out[e] h[t, j]
+//   k_experts_sum   y[t] = sum over j of p[t, j] z[t, j]
 //
+// (the last where a row has several choices, or the second product's contraction is cut).
 // Bound by HBM: of each expert that a row chooses the weights are read once (by up to
-// 8 x NB of its rows at a time), everything else stays in L2.  Every block finds the
-// choices and the experts' rows by itself from the scores (a few KB), which costs less
-// than a launch between.  A unit of work is 16 rows of a weight matrix, whole (in the
-// first product 8 gate rows and the 8 up rows that they meet, so that the activation
-// finds both in one block); the eight warps of a block share its contraction, 32
-// columns in turn, and add their sums up through shared memory.  A block walks a run
-// of consecutive units, always one step of loads ahead (32 or 64 bytes a lane of each
-// operand, across the ends of units), and the second launch begins under the first's
-// end with routing and its first weights.
+// 8 of its rows at a time, a job; an expert of more rows is read again from L2),
+// everything else stays in L2.  Every block finds the choices and the experts' rows by
+// itself from the scores (a few KB), which costs less than a launch between.  A unit of
+// work is 16 rows of a weight matrix (in the first product 8 gate rows and the 8 up rows
+// that they meet, so that the activation finds both) and a job.  A block walks a run of
+// consecutive units.  One of its warps copies the weights into a ring in shared memory,
+// some steps of up to 1,024 columns ahead and across the ends of units.  Two teams of eight
+// warps take the steps in turn; a team's warps share a step's columns, 32 at a time, and
+// load their part of the job's rows of x (or h) from L2 a step ahead.  Two more warps add
+// up the teams' sums of a unit, in a fixed order, and write its results.  (A unit a warp,
+// each with copies of its own, read 512-byte pieces all over the matrices: 4.4 TB/s.  With
+// the rows of x and h copied into the ring too the copying warp was the bound, some 50
+// cycles a copy; with one team, its latency from step to step.)
 //
 // The multiplications are warp-level MMAs: 16 rows of weights, 8 rows of x.  The
 // contraction's order is free, so a lane takes eight consecutive columns of a weight's
 // row in one 16-byte load, and the same of x.  h is summed in fp32 and enters the second
-// product as two terms that give 16 bits of it or more at any magnitude: two bf16 values
+// product as two terms that give 15 bits of it or more at any magnitude: two bf16 values
 // beside bf16 weights; beside fp16 weights, whose range is too small for it, two tf32
 // values, the weights widened to tf32 exactly.
 #include "ops_internal.cuh"
+#include "umma.cuh"
 #include "values.cuh"
 
 namespace hwr {
 namespace {
 
-constexpr int EX_THREADS = 256, EX_WARPS = EX_THREADS / 32;
-constexpr int EX_STEP = 4;                 // blocks of 32 columns that a warp loads ahead
-constexpr int EX_PAIRS = EXPERTS_MAX_ROWS * EXPERTS_MAX_TOP;
-constexpr int EX_GROUPS = OPS_MAX_GROUPS;
+using umma::bulk_g2s;
+using umma::mbar_arrive;
+using umma::mbar_arrive_expect_tx;
+using umma::mbar_init;
+using umma::mbar_wait;
+
+constexpr int EX_TEAM = 8, EX_MMA = 2 * EX_TEAM, EX_ADD = 2;      // warps that multiply, and that add up; one more copies
+constexpr int EX_WARPS = EX_MMA + 1 + EX_ADD, EX_THREADS = EX_WARPS * 32;
+constexpr int EX_SUMS = 2;                 // units whose sums are under way
+constexpr int EX_STRIDE = EX_TEAM * 32;    // columns of a step that a team takes at a time
+constexpr int EX_JOB = 8;                  // pairs of a job
+constexpr int EX_DEPTH = 8;                // steps of the ring, at most
+constexpr int EX_SMEM = 208 * 1024;        // (a block also has some of its own)
+constexpr int EX_UNIT_COST = 128;          // of a unit, in columns of its weights
+constexpr int EX_COLS = 1024;              // columns of a step, at most (of the second product: half, in fp16 a quarter)
+constexpr int SUM_THREADS = 128;
+// Shared memory of the tables and the ring, where it holds two steps: the rest is the L1
+// that keeps x and h (64 rows over 64 experts of 1,024 x 4,096 in bf16: 260 us with 110 KB,
+// 232 with 140, 288 with 206).
+constexpr int EX_RING = 140 * 1024;
+constexpr int EX_GROUPS = OPS_MAX_GROUPS, EX_EACH = (EX_GROUPS + EX_THREADS - 1) / EX_THREADS;      // groups a thread
 constexpr uint32_t ALL = 0xffffffffu;
-static_assert(EX_GROUPS == 4 * EX_THREADS, "four groups a thread");
 
 template <bool F16>
 __device__ __forceinline__ void mma16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
                                       uint32_t b1) {
     if (F16)
-        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
     else
-        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
 __device__ __forceinline__ void mma8_tf32(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
                                           uint32_t b1) {
-    asm volatile("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+    asm("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                  : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-}
-
-__device__ __forceinline__ uint4 zeros() { return make_uint4(0, 0, 0, 0); }
-
-// Read once: not kept in L1, which is x's and h's.
-__device__ __forceinline__ uint4 stream16(const void *p) {
-    uint4 v;
-    asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];"
-                 : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
-                 : "l"(p));
-    return v;
 }
 
 // The first n of eight 16-bit elements, zeros after them.
@@ -76,123 +88,282 @@ __device__ __forceinline__ uint4 first(uint4 v, int n) {
     return v;
 }
 
-// Eight elements of a row of n from column c on, zeros beyond it and for no row.  A row
-// that does not begin on a 16-byte boundary takes the two aligned units around them,
-// those that hold an element of the row, shifted into place.
-template <bool ALIGNED, bool STREAM>
-__device__ __forceinline__ uint4 eight(const uint16_t *row, int c, int n) {
-    if (!row || c >= n) return zeros();
-    const uint16_t *p = row + c;
-    uint4 v;
-    if (ALIGNED) {
-        v = STREAM ? stream16(p) : __ldg((const uint4 *)p);
-    } else {
-        const int s = (int)((uintptr_t)p & 15);
-        const uint16_t *q = (const uint16_t *)((uintptr_t)p - s);
-        const uint4 a = __ldg((const uint4 *)q);
-        const uint4 b = s && q + 8 < row + n ? __ldg((const uint4 *)q + 1) : zeros();
-        uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-        if (s & 8)
+// The 16 bytes that begin s (even) bytes into a, followed by b.
+__device__ __forceinline__ uint4 shifted(const uint4 &a, const uint4 &b, int s) {
+    uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+    if (s & 8)
 #pragma unroll
-            for (int i = 0; i < 6; ++i) w[i] = w[i + 2];
-        if (s & 4)
+        for (int i = 0; i < 6; ++i) w[i] = w[i + 2];
+    if (s & 4)
 #pragma unroll
-            for (int i = 0; i < 5; ++i) w[i] = w[i + 1];
-        const int h = (s & 2) * 8;
-        v = make_uint4(__funnelshift_r(w[0], w[1], h), __funnelshift_r(w[1], w[2], h), __funnelshift_r(w[2], w[3], h),
-                       __funnelshift_r(w[3], w[4], h));
-    }
-    return c + 8 <= n ? v : first(v, n - c);
+        for (int i = 0; i < 5; ++i) w[i] = w[i + 1];
+    const int h = (s & 2) * 8;
+    return make_uint4(__funnelshift_r(w[0], w[1], h), __funnelshift_r(w[1], w[2], h), __funnelshift_r(w[2], w[3], h),
+                      __funnelshift_r(w[3], w[4], h));
 }
+
+// Eight 16-bit elements of a row in shared memory, whose first lies s bytes behind a
+// 16-byte boundary.
+template <bool ALIGNED>
+__device__ __forceinline__ uint4 taken(const char *at, int s) {
+    const uint4 a = *(const uint4 *)at;
+    if (ALIGNED) return a;
+    const uint4 b = *(const uint4 *)(at + 16);
+    return shifted(a, b, s);
+}
+
+// Eight 16-bit elements of a row of n in global memory from column c on, zeros for no row
+// and from the row's end on, but for those of the last eight, which hold anything there
+// (masked where they are used: a mask here would wait for the load).  A row that does not
+// begin on a 16-byte boundary gives the two aligned units around them, those that hold an
+// element of the row.
+template <bool ALIGNED>
+__device__ __forceinline__ void eight(uint4 (&v)[ALIGNED ? 1 : 2], const uint16_t *row, int c, int n) {
+#pragma unroll
+    for (int i = 0; i < (ALIGNED ? 1 : 2); ++i) v[i] = make_uint4(0, 0, 0, 0);
+    if (!row || c >= n) return;
+    if (ALIGNED) {
+        v[0] = *(const uint4 *)(row + c);
+    } else {
+        const uint4 *u = (const uint4 *)((uintptr_t)(row + c) & ~(uintptr_t)15);
+        v[0] = u[0];
+        if ((const uint16_t *)(u + 1) < row + n) v[1] = u[1];
+    }
+}
+
+// A lane's row of a step's copies: the 16-byte units that hold its columns [c, c + cols)
+// of n (any alignment; a unit holds an element of the row, so none is out of bounds).
+struct Piece {
+    const char *from;
+    uint32_t bytes;
+};
+__device__ __forceinline__ Piece piece_of(const void *row, int size, int c, int cols, int n) {
+    Piece p = {nullptr, 0};
+    const int left = n - c < cols ? n - c : cols;
+    if (!row || left <= 0) return p;
+    const uintptr_t begin = (uintptr_t)row + (int64_t)c * size, end = begin + (int64_t)left * size;
+    p.from = (const char *)(begin & ~(uintptr_t)15);
+    p.bytes = (uint32_t)(((end + 15) & ~(uintptr_t)15) - (begin & ~(uintptr_t)15));
+    return p;
+}
+
+// How the weights' rows come: in boxes of 64 columns x 8 rows by tensor copies (one for all
+// of a step's columns; matrices of whole 64 columns on 16-byte boundaries), or as bulk
+// copies of rows, aligned or not.
+enum : int { W_BOXES = 0, W_ROWS = 1, W_ANY = 2 };
+
+// The weights' row that stands in row g of an MMA's eight: a quarter of a warp's 16-byte
+// loads reads 64 bytes of two rows, which lie four rows apart, so that they are 64 bytes
+// apart in the banks.
+__device__ __forceinline__ int row_of(int g) { return g >> 1 | (g & 1) << 2; }
+
+// Eight of a step's columns from k + 8 q on of a weight's row (of the first or the second
+// eight): boxes are swizzled (the 16-byte units of row i exchanged by i), rows padded by 16.
+template <int W>
+__device__ __forceinline__ uint4 weights(const char *at, int row, int q, bool second, int k, int cols, int s) {
+    if (W == W_BOXES)
+        return *(const uint4 *)(at + (second ? cols * 16 : 0) + (k >> 6) * 1024 + row * 128 + (((k >> 5 & 1) * 4 + q) ^ row) * 16);
+    return taken<W == W_ROWS>(at + (row + (second ? 8 : 0)) * (cols * 2 + 16) + (k + q * 8) * 2, s);
+}
+
+// A block's ring: `depth` steps of 16 rows of weights and some of x or h.
+struct Ring {
+    char *base;
+    uint64_t *full, *empty;               // [depth]
+    int step, depth;                      // bytes of a step
+    int slot;
+    uint32_t phase;
+    bool ok;
+    __device__ __forceinline__ void next() {
+        if (++slot == depth) {
+            slot = 0;
+            phase ^= 1;
+        }
+    }
+    // Where a wait gives up, the block goes on without waiting (or copying), and the call's
+    // results are worth nothing.
+    __device__ __forceinline__ const char *wait_full(volatile int *abort_flag, int32_t *status) {
+        ok = ok && mbar_wait(full + slot, phase, abort_flag, status);
+        return base + slot * step;
+    }
+    __device__ __forceinline__ void release() {
+        __syncwarp();                     // (read by all lanes)
+        if ((threadIdx.x & 31) == 0) mbar_arrive(empty + slot);
+        next();
+        next();                           // (the other team's)
+    }
+    // A step's copies: lane i's row of weights, or (boxes) both of its eight rows by lanes 0
+    // and 1.  False where the wait for the slot gave up.
+    template <int W>
+    __device__ __forceinline__ bool copy(const CUtensorMap *map, int y, int e, const uint16_t *row, int s, int cols, int n,
+                                         volatile int *abort_flag, int32_t *status, bool stall) {
+        const int lane = threadIdx.x & 31;
+        ok = ok && mbar_wait(empty + slot, phase ^ 1, abort_flag, status);
+        if (W != W_BOXES) ok = __all_sync(ALL, ok);
+        if (!ok) return false;
+        char *to = base + slot * step;
+        if (W == W_BOXES) {
+            if (lane < 2 && !stall) {
+                mbar_arrive_expect_tx(full + slot, cols * 16);
+                umma::tma_load_4d(to + lane * cols * 16, map, full + slot, 0, y, s * cols / 64, e);
+            }
+        } else {
+            const Piece p = lane < 16 ? piece_of(row, 2, s * cols, cols, n) : Piece{nullptr, 0};
+            const uint32_t bytes = __reduce_add_sync(ALL, p.bytes);
+            if (lane < 2 && !stall) mbar_arrive_expect_tx(full + slot, lane ? 0 : bytes);
+            __syncwarp();
+            if (p.bytes && !stall) bulk_g2s(to + lane * (cols * 2 + 16), p.from, p.bytes, full + slot);
+        }
+        next();
+        return true;
+    }
+};
 
 // ---- routing --------------------------------------------------------------------
 
 // Which rows meet which expert: pairs (row t, choice j) at t * top + j, the pairs of an
-// expert side by side in `list`, in jobs of at most 8 NB of them.
+// expert side by side in `list`, in jobs of at most 8 of them.  The first product's blocks
+// each make the tables, and one of them leaves them in memory for the launches after it.
 struct Routing {
-    float gate[EX_PAIRS];
-    int count[EX_GROUPS];
-    alignas(16) int16_t choice[EX_PAIRS + 8];             // -1: none
-    uint16_t list[EX_PAIRS], begin[EX_PAIRS], expert[EX_PAIRS];      // (jobs: begin, expert)
-    uint8_t n[EX_PAIRS];
-    int jobs, warp_jobs[EX_WARPS], warp_pairs[EX_WARPS];
-};
-
-// Order of a score among the choices: larger ones above, then lower indices; 0 for one
-// that is never chosen (-inf, NaN).
-__device__ __forceinline__ uint64_t score_key(float v, int e) {
-    if (!(v > -INFINITY)) return 0;
-    const uint32_t u = __float_as_uint(v + 0.f);
-    return (uint64_t)(u ^ (u >> 31 ? 0xffffffffu : 0x80000000u)) << 32 | (uint32_t)~e;
-}
-
-__device__ __forceinline__ uint64_t warp_max(uint64_t k) {
-    for (int d = 16; d; d /= 2) {
-        const uint64_t o = __shfl_xor_sync(ALL, k, d);
-        k = k > o ? k : o;
+    int *jobs;
+    float *gate;                          // [pairs]
+    int *count;                           // [groups]
+    int16_t *choice;                      // [pairs] -1: none
+    uint16_t *list, *begin, *expert;      // [pairs] (jobs: begin, expert)
+    uint8_t *n;                           // [jobs]
+    __device__ __forceinline__ Routing(const Experts &p, char *at) {
+        const int pairs = (p.rows * p.top + 7) & ~7;
+        jobs = (int *)at;
+        choice = (int16_t *)(at + 16);    // (16-byte aligned, read by eights)
+        gate = (float *)(choice + pairs);
+        list = (uint16_t *)(gate + pairs);
+        begin = list + pairs;
+        expert = begin + pairs;
+        n = (uint8_t *)(expert + pairs);
+        count = (int *)(n + pairs);
     }
-    return k;
+};
+// (the counts are not needed after the routing)
+inline __host__ __device__ size_t tables_bytes(const Experts &p) {
+    return 16 + (size_t)((p.rows * p.top + 7) & ~7) * (2 + 4 + 6 + 1);      // (whole words)
 }
+inline size_t routing_bytes(const Experts &p) { return (tables_bytes(p) + 16 + p.groups * 4 + 1023) / 1024 * 1024; }
+
+// Order of a score among the choices: larger ones above; 0 for one that is never chosen
+// (-inf, NaN).
+__device__ __forceinline__ uint32_t score_order(float v) {
+    const uint32_t u = __float_as_uint(v + 0.f);
+    return v > -INFINITY ? u ^ (u >> 31 ? 0xffffffffu : 0x80000000u) : 0u;
+}
+__device__ __forceinline__ float score_of(uint32_t order) {
+    return __uint_as_float(order >> 31 ? order ^ 0x80000000u : ~order);
+}
+
 __device__ __forceinline__ float warp_sum(float v) {
     for (int d = 16; d; d /= 2) v += __shfl_xor_sync(ALL, v, d);
     return v;
 }
 
-template <int NB>
-__device__ __forceinline__ void route(const Experts &p, Routing &r) {
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, pairs = p.rows * p.top, E = p.groups;
-    for (int i = tid; i < E; i += EX_THREADS) r.count[i] = 0;
-    if (p.scores) {
-        for (int t = warp; t < p.rows; t += EX_WARPS) {
-            const float *s = p.scores + t * p.scores_ld;
-            uint64_t last = ~0ull;
-            float mine = -INFINITY, top = 0.f;
-            int choice = -1;
-            for (int j = 0; j < p.top; ++j) {
-                uint64_t best = 0;
-                for (int e = lane; e < E; e += 32) {
-                    const uint64_t k = score_key(s[e], e);
-                    if (k < last && k > best) best = k;
-                }
-                last = warp_max(best);
-                if (!last) break;
-                const int e = (int)~(uint32_t)last;
-                const float v = s[e];
-                if (j == 0) top = v;
-                if (lane == j) {
-                    mine = v;
-                    choice = e;
-                }
+// A row's choices by a warp: lane j gets the j-th (-1: none) and its p.  LANE: scores that
+// a lane holds (rows of at most 32 LANE of them).
+template <int LANE>
+__device__ __forceinline__ void choose(const float *s, int E, int top, bool over_all, int &choice, float &gate) {
+    const int lane = threadIdx.x & 31;
+    uint32_t order[LANE];
+#pragma unroll
+    for (int i = 0; i < LANE; ++i) order[i] = lane + i * 32 < E ? score_order(__ldg(s + lane + i * 32)) : 0u;
+    float largest = 0.f, mine = 0.f, total = 0.f;
+    choice = -1;
+    for (int j = 0; j < top; ++j) {
+        uint32_t best = 0;
+        int at = 0;
+#pragma unroll
+        for (int i = 0; i < LANE; ++i)
+            if (order[i] > best) {
+                best = order[i];
+                at = i;
             }
-            const float w = choice >= 0 ? expf(mine - top) : 0.f;
-            float total = w;
-            if (p.over_all) {
-                total = 0.f;
-                for (int e = lane; e < E; e += 32) total += s[e] > -INFINITY ? expf(s[e] - top) : 0.f;
-            }
-            total = warp_sum(total);
-            if (lane < p.top) {
-                r.choice[t * p.top + lane] = (int16_t)choice;
-                r.gate[t * p.top + lane] = choice >= 0 ? w / total : 0.f;
-            }
+        const uint32_t most = __reduce_max_sync(ALL, best);
+        if (!most) break;
+        const uint32_t e = __reduce_min_sync(ALL, best == most ? (uint32_t)(lane + at * 32) : ~0u);
+        const float v = score_of(most);
+        if (j == 0) {
+            largest = v;
+            if (over_all)
+#pragma unroll
+                for (int i = 0; i < LANE; ++i) total += order[i] ? expf(score_of(order[i]) - largest) : 0.f;
         }
-    } else {
-        for (int i = tid; i < pairs; i += EX_THREADS) {
-            const int c = p.choice[i];
-            r.choice[i] = (int16_t)((uint32_t)c < (uint32_t)E ? c : -1);
-            r.gate[i] = p.gates[i];
+        if (lane == j) {
+            choice = (int)e;
+            mine = v;
+        }
+#pragma unroll
+        for (int i = 0; i < LANE; ++i)
+            if (e == (uint32_t)(lane + i * 32)) order[i] = 0;
+    }
+    const float w = choice >= 0 ? expf(mine - largest) : 0.f;
+    total = warp_sum(over_all ? total : w);
+    gate = choice >= 0 ? w / total : 0.f;
+}
+
+template <int LANE>
+__device__ __forceinline__ void choose_all(const Experts &p, Routing &r) {
+    const int lane = threadIdx.x & 31;
+    for (int t = threadIdx.x >> 5; t < p.rows; t += EX_WARPS) {
+        int choice;
+        float gate;
+        choose<LANE>(p.scores + t * p.scores_ld, p.groups, p.top, p.over_all, choice, gate);
+        if (lane < p.top) {
+            r.choice[t * p.top + lane] = (int16_t)choice;
+            r.gate[t * p.top + lane] = gate;
         }
     }
-    __syncthreads();
+}
+
+// Up to 32 pairs, by one warp: a stable sort by expert.
+__device__ __forceinline__ void deal_few(const Routing &r, int pairs) {
+    const int lane = threadIdx.x & 31;
+    const int mine = lane < pairs ? r.choice[lane] : -1;
+    int place = 0, rank = 0;              // among all, and among my expert's
+    for (int i = 0; i < pairs; ++i) {
+        const int c = __shfl_sync(ALL, mine, i);
+        const bool before = c == mine && i < lane;
+        rank += before;
+        place += before || (c >= 0 && c < mine);
+    }
+    const bool lead = mine >= 0 && rank % EX_JOB == 0;
+    const uint32_t same = __match_any_sync(ALL, mine);
+    int job = 0;
+    for (int i = 0; i < pairs; ++i) {
+        const int at = __shfl_sync(ALL, lead ? place : 64, i);
+        job += at < place;
+    }
+    if (mine >= 0) r.list[place] = (uint16_t)lane;
+    if (lead) {
+        const int left = __popc(same) - rank;
+        r.expert[job] = (uint16_t)mine;
+        r.begin[job] = (uint16_t)place;
+        r.n[job] = (uint8_t)(left < EX_JOB ? left : EX_JOB);
+    }
+    const uint32_t leads = __ballot_sync(ALL, lead);
+    if (lane == 0) *r.jobs = __popc(leads);
+}
+
+// Any number, by the block.
+__device__ __forceinline__ void deal(const Routing &r, int pairs, int E) {
+    __shared__ int warp_jobs[EX_WARPS], warp_pairs[EX_WARPS];
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     for (int i = tid; i < pairs; i += EX_THREADS)
         if (r.choice[i] >= 0) atomicAdd(&r.count[r.choice[i]], 1);
     __syncthreads();
-    // four experts a thread: where their pairs and jobs begin
-    int jobs = 0, all = 0, n[4];
+    // some experts a thread: where their pairs and jobs begin
+    int jobs = 0, all = 0, n[EX_EACH];
+    bool several = false;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        n[k] = tid * 4 + k < E ? r.count[tid * 4 + k] : 0;
-        jobs += (n[k] + 8 * NB - 1) / (8 * NB);
+    for (int k = 0; k < EX_EACH; ++k) {
+        n[k] = tid * EX_EACH + k < E ? r.count[tid * EX_EACH + k] : 0;
+        several |= n[k] > EX_JOB;
+        jobs += (n[k] + EX_JOB - 1) / EX_JOB;
         all += n[k];
     }
     int j = jobs, a = all;
@@ -204,33 +375,30 @@ __device__ __forceinline__ void route(const Experts &p, Routing &r) {
         }
     }
     if (lane == 31) {
-        r.warp_jobs[warp] = j;
-        r.warp_pairs[warp] = a;
+        warp_jobs[warp] = j;
+        warp_pairs[warp] = a;
     }
     __syncthreads();
     j -= jobs;
     a -= all;
     for (int w = 0; w < warp; ++w) {
-        j += r.warp_jobs[w];
-        a += r.warp_pairs[w];
+        j += warp_jobs[w];
+        a += warp_pairs[w];
     }
-    if (tid == EX_THREADS - 1) r.jobs = j + jobs;
+    if (tid == EX_THREADS - 1) *r.jobs = j + jobs;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        if (n[k]) r.count[tid * 4 + k] = a;
-        for (int b = 0; b < n[k]; b += 8 * NB, ++j) {
-            r.expert[j] = (uint16_t)(tid * 4 + k);
+    for (int k = 0; k < EX_EACH; ++k) {
+        if (n[k]) r.count[tid * EX_EACH + k] = a;
+        for (int b = 0; b < n[k]; b += EX_JOB, ++j) {
+            r.expert[j] = (uint16_t)(tid * EX_EACH + k);
             r.begin[j] = (uint16_t)(a + b);
-            r.n[j] = (uint8_t)(n[k] - b < 8 * NB ? n[k] - b : 8 * NB);
+            r.n[j] = (uint8_t)(n[k] - b < EX_JOB ? n[k] - b : EX_JOB);
         }
         a += n[k];
     }
     // Within a job pairs may lie in any order (a pair's results do not depend on its column
     // of the MMA); where an expert has several, they lie in their own order, so that every
     // block deals them out alike.
-    bool several = false;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) several |= n[k] > 8 * NB;
     several = __syncthreads_or(several);
     for (int i = tid; i < pairs; i += EX_THREADS) {
         const int e = r.choice[i];
@@ -248,29 +416,78 @@ __device__ __forceinline__ void route(const Experts &p, Routing &r) {
         for (int j = i & ~7; j < i; ++j) at += r.choice[j] == e;
         r.list[r.count[e] + at] = (uint16_t)i;
     }
+}
+
+__device__ __forceinline__ void route(const Experts &p, Routing &r, char *smem) {
+    const int tid = threadIdx.x, pairs = p.rows * p.top, E = p.groups;
+    if (pairs > 32)
+        for (int i = tid; i < E; i += EX_THREADS) r.count[i] = 0;
+    if (!p.scores) {
+        for (int i = tid; i < pairs; i += EX_THREADS) {
+            const int c = p.choice[i];
+            r.choice[i] = (int16_t)((uint32_t)c < (uint32_t)E ? c : -1);
+            r.gate[i] = p.gates[i];
+        }
+    } else if (E <= 32) {
+        choose_all<1>(p, r);
+    } else if (E <= 128) {
+        choose_all<4>(p, r);
+    } else {
+        choose_all<32>(p, r);
+    }
+    __syncthreads();
+    if (pairs > 32) deal(r, pairs, E);
+    else if (tid < 32) deal_few(r, pairs);
+    __syncthreads();
+    if (blockIdx.x == 0)
+        for (int i = tid; i < (int)tables_bytes(p) / 4; i += EX_THREADS) ((uint32_t *)p.tables)[i] = ((const uint32_t *)smem)[i];
+}
+
+// The tables that the first product has left.
+__device__ __forceinline__ void load_routing(const Experts &p, char *smem) {
+    for (int i = threadIdx.x; i < (int)tables_bytes(p) / 4; i += EX_THREADS)
+        ((uint32_t *)smem)[i] = __ldcg((const uint32_t *)p.tables + i);
     __syncthreads();
 }
 
-// A block's run of units.
-__device__ __forceinline__ void run_of(int units, int &u, int &end) {
-    u = (int)((int64_t)units * blockIdx.x / gridDim.x);
-    end = (int)((int64_t)units * (blockIdx.x + 1) / gridDim.x);
-}
-
-// Weights of a step: rows g8 and g8 + 8 of the unit.
-struct Step {
-    uint4 a[EX_STEP], d[EX_STEP];
+// A block's run of units: by job, piece of the contraction and tile of 16 rows.
+struct Walk {
+    int u, end, job, split, tile, splits, tiles;
+    __device__ __forceinline__ Walk(int jobs, int splits, int tiles) : splits(splits), tiles(tiles) {
+        const int units = jobs * splits * tiles;
+        u = (int)((int64_t)units * blockIdx.x / gridDim.x);
+        end = (int)((int64_t)units * (blockIdx.x + 1) / gridDim.x);
+        tile = u % tiles;
+        split = u / tiles % splits;
+        job = u / tiles / splits;
+    }
+    __device__ __forceinline__ bool more() const { return u < end; }
+    __device__ __forceinline__ void next() {
+        ++u;
+        if (++tile < tiles) return;
+        tile = 0;
+        if (++split < splits) return;
+        split = 0;
+        ++job;
+    }
 };
 
-template <bool ALIGNED>
-__device__ __forceinline__ void load(Step &s, const uint16_t *ra, const uint16_t *rb, int block, int end, int q, int n) {
-#pragma unroll
-    for (int i = 0; i < EX_STEP; ++i) {
-        const int b = block + i * EX_WARPS, c = b * 32 + q * 8;
-        s.a[i] = b < end ? eight<ALIGNED, true>(ra, c, n) : zeros();
-        s.d[i] = b < end ? eight<ALIGNED, true>(rb, c, n) : zeros();
+// The steps of a run, `per` (the last piece: what is left of `all`) of each unit.
+struct Steps {
+    Walk w;
+    int s, end, per, all;
+    __device__ __forceinline__ Steps(const Walk &w, int per, int all) : w(w), per(per), all(all) { begin(); }
+    __device__ __forceinline__ void begin() {
+        s = w.split * per;
+        end = min(s + per, all);
     }
-}
+    __device__ __forceinline__ bool more() const { return w.more(); }
+    __device__ __forceinline__ void next() {
+        if (++s < end) return;
+        w.next();
+        begin();
+    }
+};
 
 __device__ __forceinline__ float activated(float u, int act) {
     if (act == HWR_ACT_RELU) return u < 0.f ? 0.f : u;
@@ -286,100 +503,208 @@ __device__ __forceinline__ void tf32_terms(float v, float &high, float &low) {
     low = m < 0x7f800000u ? v - high : v;
 }
 
+// What the block shares beside the routing's tables and the ring.
+struct Shared {
+    float4 sums[EX_SUMS][EX_MMA][32];
+    uint64_t full[EX_DEPTH], empty[EX_DEPTH], added[EX_SUMS], taken[EX_SUMS];
+    int abort_flag;
+};
+
+__device__ __forceinline__ Ring ring_of(const Experts &p, char *smem, Shared &sh) {
+    Ring r;
+    r.depth = p.depth;
+    r.step = p.step;
+    r.base = smem + p.ring_at;
+    r.full = sh.full;
+    r.empty = sh.empty;
+    r.slot = 0;
+    r.phase = 0;
+    r.ok = true;
+    return r;
+}
+// (before the routing's barriers; both: teams take part in a unit)
+__device__ __forceinline__ void init(Shared &sh, bool both) {
+    if (threadIdx.x < EX_DEPTH) {
+        mbar_init(sh.full + threadIdx.x, 2);
+        mbar_init(sh.empty + threadIdx.x, EX_TEAM);
+    }
+    if (threadIdx.x < EX_SUMS) {
+        mbar_init(sh.added + threadIdx.x, both ? EX_MMA : EX_TEAM);
+        mbar_init(sh.taken + threadIdx.x, 1);
+    }
+    if (threadIdx.x == 0) sh.abort_flag = 0;
+    umma::fence_mbar_init();
+}
+
+// A warp's sums of a unit (the turn-th of the block's) go to the warps that add up ...
+__device__ __forceinline__ void give(Shared &sh, float (&c)[2][4], int turn, int place, bool &ok, int32_t *status) {
+    const int b = turn % EX_SUMS, lane = threadIdx.x & 31;
+    ok = ok && mbar_wait(sh.taken + b, (turn / EX_SUMS & 1) ^ 1, &sh.abort_flag, status);
+    sh.sums[b][place][lane] = make_float4(c[0][0] + c[1][0], c[0][1] + c[1][1], c[0][2] + c[1][2], c[0][3] + c[1][3]);
+    __syncwarp();
+    if (lane == 0) mbar_arrive(sh.added + b);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) c[i / 4][i % 4] = 0.f;
+}
+// ... which take them in the warps' order (from one team, where units have one step, or both).
+__device__ __forceinline__ bool take(Shared &sh, float (&c)[4], int turn, bool both, int32_t *status) {
+    const int b = turn % EX_SUMS, lane = threadIdx.x & 31;
+    if (!mbar_wait(sh.added + b, turn / EX_SUMS & 1, &sh.abort_flag, status)) return false;
+    float4 v = sh.sums[b][0][lane];
+#pragma unroll
+    for (int w = 1; w < EX_MMA; ++w) {
+        if (w == EX_TEAM && !both) break;
+        const float4 o = sh.sums[b][w][lane];
+        v.x += o.x;
+        v.y += o.y;
+        v.z += o.z;
+        v.w += o.w;
+    }
+    __syncwarp();
+    if (lane == 0) mbar_arrive(sh.taken + b);
+    c[0] = v.x;
+    c[1] = v.y;
+    c[2] = v.z;
+    c[3] = v.w;
+    return true;
+}
+
 // ---- the first product --------------------------------------------------------------
 
-template <bool F16, bool ALIGNED, int NB>
-__global__ void __launch_bounds__(EX_THREADS, 2)
-k_experts_in(const __grid_constant__ Experts p) {
-    __shared__ Routing r;
-    __shared__ float sums[EX_WARPS][16][8 * NB + 1];
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g8 = lane >> 2, q = lane & 3;
+template <bool F16, int W, bool X_ALIGNED>
+__global__ void __launch_bounds__(EX_THREADS)
+k_experts_in(const __grid_constant__ Experts p, const __grid_constant__ CUtensorMap map) {
+    extern __shared__ __align__(1024) char smem[];
+    __shared__ Shared sh;
+    constexpr int CH = EX_COLS / EX_STRIDE, XU = X_ALIGNED ? 1 : 2;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g8 = lane >> 2, q = lane & 3, wr = row_of(g8);
+    const int cols = p.cols, steps = (p.n_in + cols - 1) / cols;
+    const bool both = steps > 1;
+    init(sh, both);
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    route<NB>(p, r);
-    const int wide = p.gated ? 8 : 16, tiles = (p.hidden + wide - 1) / wide, blocks = (p.n_in + 31) / 32;
-    const bool x_aligned = (((uintptr_t)p.x & 15) | (p.x_ld & 7)) == 0;
-    int u, end;
-    run_of(r.jobs * tiles, u, end);
-    if (u >= end) return;
-    const uint16_t *ra, *rb;
-    auto rows = [&](int unit) {
-        const int job = unit / tiles, f = (unit - job * tiles) * wide + g8;
-        const uint16_t *w = p.w_in + r.expert[job] * p.w_in_z;
-        const int up = p.gated ? p.hidden + f : f + 8;
-        ra = f < p.hidden ? w + f * p.w_in_ld : nullptr;
-        rb = up < (p.gated ? 2 * p.hidden : p.hidden) ? w + up * p.w_in_ld : nullptr;
+    Routing r(p, smem);
+    route(p, r, smem);
+    Ring ring = ring_of(p, smem, sh);
+    const int wide = p.gated ? 8 : 16;
+    Walk w(*r.jobs, 1, (p.hidden + wide - 1) / wide);
+    const int u0 = w.u;
+    const auto weights_row = [&](const Walk &w, int i) -> const uint16_t * {
+        const int f = w.tile * wide + (p.gated ? i & 7 : i);
+        const int64_t at = p.gated && i >= 8 ? p.hidden + f : f;
+        return f < p.hidden ? p.w_in + r.expert[w.job] * p.w_in_z + at * p.w_in_ld : nullptr;
     };
-    Step now, next;
-    rows(u);
-    load<ALIGNED>(now, ra, rb, warp, blocks, q, p.n_in);
-    for (; u < end; ++u) {
-        const int job = u / tiles, n = r.n[job], begin = r.begin[job];
-        const uint16_t *x[NB];
-#pragma unroll
-        for (int b = 0; b < NB; ++b) {
-            const int at = b * 8 + g8;
-            x[b] = at < n ? p.x + r.list[begin + at] / p.top * p.x_ld : nullptr;
+    if (warp == EX_MMA) {
+        for (; w.more(); w.next()) {
+            const uint16_t *row = W != W_BOXES && lane < 16 ? weights_row(w, lane) : nullptr;
+            const int f0 = w.tile * wide, y = lane == 0 ? f0 : p.gated ? p.hidden + f0 : f0 + 8, e = r.expert[w.job];
+            for (int s = 0; s < steps; ++s)
+                if (!ring.copy<W>(&map, y, e, row, s, cols, p.n_in, &sh.abort_flag, p.status, p.test_stall)) return;
         }
-        float c[NB][4] = {};
-        for (int b0 = 0; b0 < blocks; b0 += EX_STEP * EX_WARPS) {
-            const int more = b0 + EX_STEP * EX_WARPS;
-            if (more < blocks) {
-                load<ALIGNED>(next, ra, rb, more + warp, blocks, q, p.n_in);
-            } else if (u + 1 < end) {
-                rows(u + 1);
-                load<ALIGNED>(next, ra, rb, warp, blocks, q, p.n_in);
-            }
+        return;
+    }
+    if (warp > EX_MMA) {
+        for (; w.more(); w.next()) {
+            const int turn = w.u - u0;
+            if (turn % EX_ADD != warp - EX_MMA - 1) continue;
+            const int n = r.n[w.job], begin = r.begin[w.job];
+            float c[4];
+            if (!take(sh, c, turn, both, p.status)) return;
+            // rows wr and wr + 8 of columns 2 q and 2 q + 1
 #pragma unroll
-            for (int i = 0; i < EX_STEP; ++i) {
-                const int k = b0 + warp + i * EX_WARPS;
-                if (k >= blocks) break;
-#pragma unroll
-                for (int b = 0; b < NB; ++b) {
-                    if (b * 8 >= n) break;
-                    const uint4 v = x_aligned ? eight<true, false>(x[b], k * 32 + q * 8, p.n_in)
-                                              : eight<false, false>(x[b], k * 32 + q * 8, p.n_in);
-                    mma16<F16>(c[b], now.a[i].x, now.d[i].x, now.a[i].y, now.d[i].y, v.x, v.y);
-                    mma16<F16>(c[b], now.a[i].z, now.d[i].z, now.a[i].w, now.d[i].w, v.z, v.w);
+            for (int i = 0; i < 4; ++i) {
+                const int column = 2 * q + (i & 1), f = w.tile * wide + wr + (i & 2) * 4;
+                if (column >= n || (p.gated && (i & 2)) || f >= p.hidden) continue;
+                float v = activated(c[i], p.act);
+                if (p.gated) v *= c[i | 2];
+                const int64_t to = (int64_t)r.list[begin + column] * 2 * p.h_ld + f;
+                if (F16) {
+                    float *h = (float *)p.h + to;
+                    tf32_terms(v, h[0], h[p.h_ld]);
+                } else {
+                    uint16_t *h = (uint16_t *)p.h + to;
+                    bf16_terms(v, h[0], h[p.h_ld]);
                 }
             }
-            now = next;
+            __syncwarp();
+        }
+        return;
+    }
+    const int team = warp / EX_TEAM, member = warp % EX_TEAM;
+    // my columns of x: the job's row g8
+    const uint16_t *row = nullptr;
+    int row_job = -1;
+    const auto fetch = [&](uint4(&v)[CH][XU], const Steps &at) {
+        if (at.w.job != row_job) {
+            row_job = at.w.job;
+            row = g8 < r.n[row_job] ? p.x + r.list[r.begin[row_job] + g8] / p.top * p.x_ld : nullptr;
+        }
+        const int to = min((at.s + 1) * cols, p.n_in);
+#pragma unroll
+        for (int i = 0; i < CH; ++i) eight<X_ALIGNED>(v[i], row, at.s * cols + member * 32 + i * EX_STRIDE + q * 8, to);
+    };
+    Steps ahead(w, steps, steps);         // the next step of this team, whose x is under way
+    if (team) {
+        ahead.next();
+        ring.next();
+    }
+    int given = u0;
+    float c[2][4] = {};
+    const auto give_up_to = [&](int u) {
+        for (; given < u; ++given) give(sh, c, given - u0, warp, ring.ok, p.status);
+    };
+    if (both) give_up_to(min(ahead.w.u, w.end));
+    if (!ahead.more()) return;
+    const auto take_step = [&](uint4(&now)[CH][XU], uint4(&next)[CH][XU]) {
+        const Steps at = ahead;
+        const int sx = X_ALIGNED ? 0 : (int)((uintptr_t)row & 15);
+        ahead.next();
+        if (ahead.more()) ahead.next();
+        if (ahead.more()) fetch(next, ahead);
+        int sa = 0, sb = 0;
+        if (W == W_ANY) {
+            sa = (int)((uintptr_t)weights_row(at.w, wr) & 15);
+            sb = (int)((uintptr_t)weights_row(at.w, wr + 8) & 15);
+        }
+        const char *from = ring.wait_full(&sh.abort_flag, p.status);
+        const int left = min(cols, p.n_in - at.s * cols);
+        // (all loads before the first multiplication: what is beyond the row is zero)
+        uint4 a[CH], d[CH];
+#pragma unroll
+        for (int i = 0; i < CH; ++i) {
+            const int k = member * 32 + i * EX_STRIDE;
+            a[i] = d[i] = make_uint4(0, 0, 0, 0);
+            if (k < left) {
+                a[i] = weights<W>(from, wr, q, false, k, cols, sa);
+                d[i] = weights<W>(from, wr, q, true, k, cols, sb);
+            }
+            if (W != W_BOXES && k + 32 > left) {
+                const int e = max(0, min(8, left - k - q * 8));
+                a[i] = first(a[i], e);
+                d[i] = first(d[i], e);
+            }
         }
 #pragma unroll
-        for (int b = 0; b < NB; ++b)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) sums[warp][g8 + (i >> 1) * 8][b * 8 + 2 * q + (i & 1)] = c[b][i];
-        __syncthreads();
-        const int f0 = (u - job * tiles) * wide;
-        for (int i = tid; i < wide * 8 * NB; i += EX_THREADS) {
-            const int f = i % wide, at = i / wide;
-            if (at >= n) break;
-            float v = 0.f, up = 0.f;
-#pragma unroll
-            for (int w = 0; w < EX_WARPS; ++w) {
-                v += sums[w][f][at];
-                if (p.gated) up += sums[w][f + 8][at];
-            }
-            v = activated(v, p.act);
-            if (p.gated) v *= up;
-            // (groups of eight: those of the last rows are filled up with zeros)
-            const int64_t group = (int64_t)r.list[begin + at] * p.h_groups + (f0 + f) / 8;
-            if (f0 + f >= p.h_groups * 8) continue;
-            if (F16) {
-                float *h = (float *)p.h + group * 16 + (f & 7);
-                tf32_terms(v, h[0], h[8]);
-            } else {
-                uint16_t *h = (uint16_t *)p.h + group * 16 + (f & 7);
-                bf16_terms(v, h[0], h[8]);
-            }
+        for (int i = 0; i < CH; ++i) {
+            const int k = member * 32 + i * EX_STRIDE;
+            uint4 v = X_ALIGNED ? now[i][0] : shifted(now[i][0], now[i][XU - 1], sx);
+            if (W != W_BOXES && k + 32 > left) v = first(v, max(0, min(8, left - k - q * 8)));
+            mma16<F16>(c[0], a[i].x, d[i].x, a[i].y, d[i].y, v.x, v.y);
+            mma16<F16>(c[1], a[i].z, d[i].z, a[i].w, d[i].w, v.z, v.w);
         }
-        __syncthreads();
+        ring.release();
+        if (both) give_up_to(min(ahead.w.u, w.end));
+        else give(sh, c, at.w.u - u0, member, ring.ok, p.status);
+        return ahead.more();
+    };
+    uint4 one[CH][XU], two[CH][XU];
+    fetch(one, ahead);
+    while (take_step(one, two) && take_step(two, one)) {
     }
 }
 
 // ---- the second product -----------------------------------------------------------
 
-// Rows without a choice, where no row has one.
 template <bool F16>
 __device__ __forceinline__ void store(const Experts &p, int t, int n, float v) {
     uint16_t *y = p.y + t * p.y_ld + n;
@@ -392,190 +717,313 @@ __device__ __forceinline__ uint4 widened(uint32_t lo, uint32_t hi) {
     return make_uint4(__float_as_uint(a.x), __float_as_uint(a.y), __float_as_uint(b.x), __float_as_uint(b.y));
 }
 
-template <bool F16, bool ALIGNED, int NB>
-__global__ void __launch_bounds__(EX_THREADS, 2)
-k_experts_out(const __grid_constant__ Experts p) {
-    __shared__ Routing r;
-    __shared__ float sums[EX_WARPS][16][8 * NB + 1];
-    __shared__ bool last;
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g8 = lane >> 2, q = lane & 3;
+template <bool F16, int W>
+__global__ void __launch_bounds__(EX_THREADS)
+k_experts_out(const __grid_constant__ Experts p, const __grid_constant__ CUtensorMap map) {
+    extern __shared__ __align__(1024) char smem[];
+    __shared__ Shared sh;
+    // 32 columns of h a lane: high and low terms, in 16-byte loads
+    constexpr int CH = EX_COLS / (F16 ? 4 : 2) / EX_STRIDE, TERM = F16 ? 2 : 1;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g8 = lane >> 2, q = lane & 3, wr = row_of(g8);
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    // (what this kernel reads before it waits was there before the first one began)
-    route<NB>(p, r);
-    const int tiles = (p.n_out + 15) / 16, per_tile = r.jobs * p.splits;
-    const int blocks = (p.hidden + 31) / 32, per_split = (blocks + p.splits - 1) / p.splits;
-    int u, end;
-    run_of(tiles * per_tile, u, end);
-    const uint16_t *ra = nullptr, *rb = nullptr;
-    int k0 = 0, k1 = 0;
-    auto rows = [&](int unit) {
-        const int tile = unit / per_tile, at = unit - tile * per_tile, job = at / p.splits;
-        const int o = tile * 16 + g8;
-        const uint16_t *w = p.w_out + r.expert[job] * p.w_out_z;
-        ra = o < p.n_out ? w + o * p.w_out_ld : nullptr;
-        rb = o + 8 < p.n_out ? w + (o + 8) * p.w_out_ld : nullptr;
-        k0 = (at - job * p.splits) * per_split;
-        k1 = min(k0 + per_split, blocks);
-    };
-    Step now, next;
-    if (u < end) {
-        rows(u);
-        load<ALIGNED>(now, ra, rb, k0 + warp, k1, q, p.hidden);
-    }
+    init(sh, true);
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    if (r.jobs == 0) {
-        for (int i = blockIdx.x * EX_THREADS + tid; i < p.rows * p.n_out; i += gridDim.x * EX_THREADS)
-            store<F16>(p, i / p.n_out, i % p.n_out, 0.f);
+    Routing r(p, smem);
+    load_routing(p, smem);
+    Ring ring = ring_of(p, smem, sh);
+    // pieces of the contraction, that the busiest block has the least to do
+    const int cols = p.cols, tiles = (p.n_out + 15) / 16, all = *r.jobs * tiles, all_steps = (p.hidden + cols - 1) / cols;
+    int splits = 1;
+    int64_t least = INT64_MAX;
+    for (int s = 1; s <= p.splits && s <= all_steps; s *= 2) {
+        const int64_t cost = (int64_t)((all * s + gridDim.x - 1) / gridDim.x) * ((all_steps + s - 1) / s * cols + EX_UNIT_COST);
+        if (cost < least) {
+            least = cost;
+            splits = s;
+        }
+    }
+    const int per = (all_steps + splits - 1) / splits;       // steps of a piece, and pieces with any
+    splits = (all_steps + per - 1) / per;
+    // one choice a row, taken whole: its result is the row's, and rows without one get zeros
+    const bool whole = p.top == 1 && p.splits == 1;
+    Walk w(*r.jobs, splits, tiles);
+    const int u0 = w.u;
+    if (warp == EX_MMA) {
+        for (Steps at(w, per, all_steps); at.more(); at.next()) {
+            const int o = at.w.tile * 16, e = r.expert[at.w.job];
+            const uint16_t *row = nullptr;
+            if (W != W_BOXES && lane < 16 && o + lane < p.n_out) row = p.w_out + e * p.w_out_z + (int64_t)(o + lane) * p.w_out_ld;
+            if (!ring.copy<W>(&map, o + lane * 8, e, row, at.s, cols, p.hidden, &sh.abort_flag, p.status, p.test_stall)) return;
+        }
         return;
     }
-    int done = 0;                         // units of this tile
-    for (; u < end; ++u) {
-        const int tile = u / per_tile, at0 = u - tile * per_tile, job = at0 / p.splits, split = at0 - job * p.splits;
-        const int n = r.n[job], begin = r.begin[job];
-        const uint4 *h[NB];
-#pragma unroll
-        for (int b = 0; b < NB; ++b) {
-            const int at = b * 8 + g8;
-            h[b] = at < n ? (const uint4 *)p.h + (int64_t)r.list[begin + at] * p.h_groups * (F16 ? 4 : 2) : nullptr;
+    if (warp > EX_MMA) {
+        const int i0 = tid - (EX_MMA + 1) * 32;
+        if (whole) {
+            for (int t = blockIdx.x; t < p.rows; t += gridDim.x)
+                if (r.choice[t] < 0)
+                    for (int o = i0; o < p.n_out; o += EX_ADD * 32) store<F16>(p, t, o, 0.f);
+        } else if (blockIdx.x == 0 && i0 == 0) {
+            *p.used_splits = splits;
         }
-        float c[NB][4] = {};
-        const int from = k0, to = k1;
-        int b0 = from;
-        do {
-            const int more = b0 + EX_STEP * EX_WARPS;
-            if (more < to) {
-                load<ALIGNED>(next, ra, rb, more + warp, to, q, p.hidden);
-            } else if (u + 1 < end) {
-                rows(u + 1);
-                load<ALIGNED>(next, ra, rb, k0 + warp, k1, q, p.hidden);
+        for (; w.more(); w.next()) {
+            const int turn = w.u - u0;
+            if (turn % EX_ADD != warp - EX_MMA - 1) continue;
+            const int n = r.n[w.job], begin = r.begin[w.job];
+            float c[4];
+            if (!take(sh, c, turn, true, p.status)) return;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int column = 2 * q + (i & 1), o = w.tile * 16 + wr + (i & 2) * 4;
+                if (column >= n || o >= p.n_out) continue;
+                const int pair = r.list[begin + column];
+                if (whole) store<F16>(p, pair, o, r.gate[pair] * c[i]);
+                else p.part[((int64_t)pair * splits + w.split) * p.n_out + o] = c[i];
             }
+            __syncwarp();
+        }
+        return;
+    }
+    const int team = warp / EX_TEAM, member = warp % EX_TEAM;
+    const int64_t low = p.h_ld * (F16 ? 4 : 2) / 16;
+    const uint4 *row = nullptr;
+    int row_job = -1;
+    const auto fetch = [&](uint4(&v)[CH][2 * TERM], const Steps &at) {
+        if (at.w.job != row_job) {
+            row_job = at.w.job;
+            row = nullptr;
+            if (g8 < r.n[row_job])
+                row = (const uint4 *)((const char *)p.h + (int64_t)r.list[r.begin[row_job] + g8] * 2 * p.h_ld * (F16 ? 4 : 2));
+        }
+        const int to = min((at.s + 1) * cols, p.hidden);
 #pragma unroll
-            for (int i = 0; i < EX_STEP; ++i) {
-                const int k = b0 + warp + i * EX_WARPS;
-                if (k >= to) break;
-                const bool in = k * 32 + q * 8 < p.hidden;
+        for (int i = 0; i < CH; ++i) {
+            const int c = at.s * cols + member * 32 + i * EX_STRIDE + q * 8;
+            const bool in = row && c < to;
 #pragma unroll
-                for (int b = 0; b < NB; ++b) {
-                    if (b * 8 >= n) break;
-                    const bool mine = in && h[b];
+            for (int j = 0; j < 2 * TERM; ++j) {
+                v[i][j] = make_uint4(0, 0, 0, 0);
+                if (in) v[i][j] = row[(j < TERM ? 0 : low) + c / 8 * TERM + j % TERM];
+            }
+        }
+    };
+    Steps ahead(w, per, all_steps);       // the next step of this team, whose h is under way
+    if (team) {
+        ahead.next();
+        ring.next();
+    }
+    int given = u0;
+    float c[2][4] = {};
+    const auto give_up_to = [&](int u) {
+        for (; given < u; ++given) give(sh, c, given - u0, warp, ring.ok, p.status);
+    };
+    give_up_to(min(ahead.w.u, w.end));
+    if (!ahead.more()) return;
+    const auto take_step = [&](uint4(&now)[CH][2 * TERM], uint4(&next)[CH][2 * TERM]) {
+        const Steps at = ahead;
+        ahead.next();
+        if (ahead.more()) ahead.next();
+        if (ahead.more()) fetch(next, ahead);
+        int sa = 0, sb = 0;
+        if (W == W_ANY) {
+            const uint16_t *w = p.w_out + r.expert[at.w.job] * p.w_out_z + (int64_t)(at.w.tile * 16 + wr) * p.w_out_ld;
+            sa = (int)((uintptr_t)w & 15);
+            sb = (int)((uintptr_t)(w + 8 * p.w_out_ld) & 15);
+        }
+        const char *from = ring.wait_full(&sh.abort_flag, p.status);
+        const int left = min(cols, p.hidden - at.s * cols);
+        // (all loads before the first multiplication: what is beyond the row is zero)
+        uint4 a[CH], d[CH];
+#pragma unroll
+        for (int i = 0; i < CH; ++i) {
+            const int k = member * 32 + i * EX_STRIDE;
+            a[i] = d[i] = make_uint4(0, 0, 0, 0);
+            if (k < left) {
+                a[i] = weights<W>(from, wr, q, false, k, cols, sa);
+                d[i] = weights<W>(from, wr, q, true, k, cols, sb);
+            }
+            if (W != W_BOXES && k + 32 > left) {
+                const int e = max(0, min(8, left - k - q * 8));
+                a[i] = first(a[i], e);
+                d[i] = first(d[i], e);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < CH; ++i) {
+            const int k = member * 32 + i * EX_STRIDE;
+            if (W != W_BOXES && k + 32 > left) {
+                // (the rows are filled up to whole 16 bytes with anything)
+                const int e = max(0, min(8, left - k - q * 8));
+#pragma unroll
+                for (int j = 0; j < 2 * TERM; ++j) {
                     if (F16) {
-                        const uint4 *v = h[b] + (k * 4 + q) * 4;
-                        const uint4 h0 = mine ? __ldcg(v) : zeros(), h1 = mine ? __ldcg(v + 1) : zeros();
-                        const uint4 l0 = mine ? __ldcg(v + 2) : zeros(), l1 = mine ? __ldcg(v + 3) : zeros();
-                        const uint4 a0 = widened(now.a[i].x, now.a[i].y), a1 = widened(now.a[i].z, now.a[i].w);
-                        const uint4 d0 = widened(now.d[i].x, now.d[i].y), d1 = widened(now.d[i].z, now.d[i].w);
-                        mma8_tf32(c[b], a0.x, d0.x, a0.y, d0.y, h0.x, h0.y);
-                        mma8_tf32(c[b], a0.z, d0.z, a0.w, d0.w, h0.z, h0.w);
-                        mma8_tf32(c[b], a1.x, d1.x, a1.y, d1.y, h1.x, h1.y);
-                        mma8_tf32(c[b], a1.z, d1.z, a1.w, d1.w, h1.z, h1.w);
-                        mma8_tf32(c[b], a0.x, d0.x, a0.y, d0.y, l0.x, l0.y);
-                        mma8_tf32(c[b], a0.z, d0.z, a0.w, d0.w, l0.z, l0.w);
-                        mma8_tf32(c[b], a1.x, d1.x, a1.y, d1.y, l1.x, l1.y);
-                        mma8_tf32(c[b], a1.z, d1.z, a1.w, d1.w, l1.z, l1.w);
+                        const int f = e - j % TERM * 4;
+                        if (f < 1) now[i][j].x = 0;
+                        if (f < 2) now[i][j].y = 0;
+                        if (f < 3) now[i][j].z = 0;
+                        if (f < 4) now[i][j].w = 0;
                     } else {
-                        const uint4 *v = h[b] + (k * 4 + q) * 2;
-                        const uint4 hi = mine ? __ldcg(v) : zeros(), lo = mine ? __ldcg(v + 1) : zeros();
-                        mma16<false>(c[b], now.a[i].x, now.d[i].x, now.a[i].y, now.d[i].y, hi.x, hi.y);
-                        mma16<false>(c[b], now.a[i].z, now.d[i].z, now.a[i].w, now.d[i].w, hi.z, hi.w);
-                        mma16<false>(c[b], now.a[i].x, now.d[i].x, now.a[i].y, now.d[i].y, lo.x, lo.y);
-                        mma16<false>(c[b], now.a[i].z, now.d[i].z, now.a[i].w, now.d[i].w, lo.z, lo.w);
+                        now[i][j] = first(now[i][j], e);
                     }
                 }
             }
-            now = next;
-            b0 = more;
-        } while (b0 < to);
+            if (F16) {
+                const uint4 a0 = widened(a[i].x, a[i].y), a1 = widened(a[i].z, a[i].w);
+                const uint4 d0 = widened(d[i].x, d[i].y), d1 = widened(d[i].z, d[i].w);
 #pragma unroll
-        for (int b = 0; b < NB; ++b)
+                for (int j = 0; j < 2 * TERM; j += TERM) {
+                    const uint4 v = now[i][j], w = now[i][j + TERM - 1];
+                    mma8_tf32(c[0], a0.x, d0.x, a0.y, d0.y, v.x, v.y);
+                    mma8_tf32(c[1], a0.z, d0.z, a0.w, d0.w, v.z, v.w);
+                    mma8_tf32(c[0], a1.x, d1.x, a1.y, d1.y, w.x, w.y);
+                    mma8_tf32(c[1], a1.z, d1.z, a1.w, d1.w, w.z, w.w);
+                }
+            } else {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) sums[warp][g8 + (i >> 1) * 8][b * 8 + 2 * q + (i & 1)] = c[b][i];
-        __syncthreads();
-        for (int i = tid; i < 16 * 8 * NB; i += EX_THREADS) {
-            const int o = i & 15, at = i >> 4;
-            if (at >= n) break;
-            float v = 0.f;
-#pragma unroll
-            for (int w = 0; w < EX_WARPS; ++w) v += sums[w][o][at];
-            if (tile * 16 + o < p.n_out)
-                p.part[((int64_t)r.list[begin + at] * p.splits + split) * p.n_out + tile * 16 + o] = v;
-        }
-        __syncthreads();
-        ++done;
-        if (u + 1 < end && (u + 1) / per_tile == tile) continue;
-        // the block that brings a tile's last units adds up what each row's choices gave,
-        // in their order
-        if (tid == 0) {
-            __threadfence();
-            last = atomicAdd(p.arrivals + tile, (uint32_t)done) + done == (uint32_t)per_tile;
-            if (last) p.arrivals[tile] = 0;
-            __threadfence();
-        }
-        done = 0;
-        __syncthreads();
-        if (!last) continue;
-        for (int i = tid; i < p.rows * 16; i += EX_THREADS) {
-            const int o = tile * 16 + (i & 15), t = i >> 4;
-            if (o >= p.n_out) continue;
-            float y = 0.f;
-            for (int j = 0; j < p.top; ++j) {
-                const int pair = t * p.top + j;
-                if (r.choice[pair] < 0) continue;
-                const float *part = p.part + (int64_t)pair * p.splits * p.n_out + o;
-                float v = 0.f;
-                for (int s = 0; s < p.splits; ++s) v += __ldcg(part + (int64_t)s * p.n_out);
-                y = fmaf(r.gate[pair], v, y);
+                for (int j = 0; j < 2 * TERM; ++j) {
+                    mma16<false>(c[0], a[i].x, d[i].x, a[i].y, d[i].y, now[i][j].x, now[i][j].y);
+                    mma16<false>(c[1], a[i].z, d[i].z, a[i].w, d[i].w, now[i][j].z, now[i][j].w);
+                }
             }
-            store<F16>(p, t, o, y);
         }
+        ring.release();
+        give_up_to(min(ahead.w.u, w.end));
+        return ahead.more();
+    };
+    uint4 one[CH][2 * TERM], two[CH][2 * TERM];
+    fetch(one, ahead);
+    while (take_step(one, two) && take_step(two, one)) {
     }
 }
 
-cudaLaunchConfig_t early(int grid, cudaStream_t s, cudaLaunchAttribute *at) {
+// y: what each row's choices gave, added up in their order (and the pieces of each).
+template <bool F16>
+__global__ void __launch_bounds__(SUM_THREADS)
+k_experts_sum(const __grid_constant__ Experts p) {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    const int o = blockIdx.x * SUM_THREADS + threadIdx.x, t = blockIdx.y, splits = *p.used_splits;
+    if (o >= p.n_out) return;
+    const Routing r(p, p.tables);
+    float y = 0.f;
+    for (int j = 0; j < p.top; ++j) {
+        const float gate = r.gate[t * p.top + j];
+        if (r.choice[t * p.top + j] < 0) continue;
+        const float *part = p.part + (int64_t)(t * p.top + j) * splits * p.n_out + o;
+        float v = 0.f;
+#pragma unroll 4
+        for (int i = 0; i < splits; ++i) v += part[(int64_t)i * p.n_out];
+        y = fmaf(gate, v, y);
+    }
+    store<F16>(p, t, o, y);
+}
+
+cudaLaunchConfig_t early(dim3 grid, int threads, size_t smem, cudaStream_t s, cudaLaunchAttribute *at) {
     cudaLaunchConfig_t cfg = {};
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.gridDim = dim3((unsigned)grid);
-    cfg.blockDim = dim3(EX_THREADS);
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = smem;
     cfg.stream = s;
     cfg.attrs = at;
     cfg.numAttrs = 1;
     return cfg;
 }
 
-template <bool F16, int NB>
-cudaError_t both(const Experts &p, int nsm, bool in_aligned, bool out_aligned, cudaStream_t s) {
+typedef void (*Kernel)(Experts, CUtensorMap);
+
+// Columns of a step: as even as it gets for this width, in whole boxes.
+int even_columns(int width, int most) {
+    const int steps = (width + most - 1) / most;
+    return ((width + steps - 1) / steps + 63) & ~63;
+}
+
+int step_bytes(int cols) { return 16 * (cols * 2 + 16); }
+
+cudaError_t launch(Kernel kernel, Experts p, const CUtensorMap &map, int cols, int nsm, cudaStream_t s) {
+    p.cols = cols;
+    p.step = (step_bytes(cols) + 1023) & ~1023;
+    p.ring_at = (int)routing_bytes(p);
+    // (an even number of slots, each of which belongs to one team: another team's use of it,
+    // one phase of its barriers later, could not be told from the one before)
+    const int depth = (EX_RING - p.ring_at) / p.step & ~1;
+    p.depth = depth < 2 ? 2 : depth > EX_DEPTH ? EX_DEPTH : depth;
     cudaLaunchAttribute at[1];
-    const cudaLaunchConfig_t cfg = early(2 * nsm, s, at);
-    const cudaError_t e = in_aligned ? cudaLaunchKernelEx(&cfg, k_experts_in<F16, true, NB>, p)
-                                     : cudaLaunchKernelEx(&cfg, k_experts_in<F16, false, NB>, p);
-    if (e != cudaSuccess) return e;
-    return out_aligned ? cudaLaunchKernelEx(&cfg, k_experts_out<F16, true, NB>, p)
-                       : cudaLaunchKernelEx(&cfg, k_experts_out<F16, false, NB>, p);
+    const cudaLaunchConfig_t cfg = early(dim3((unsigned)nsm), EX_THREADS, (size_t)p.ring_at + p.depth * p.step, s, at);
+    return cudaLaunchKernelEx(&cfg, kernel, p, map);
+}
+
+bool whole16(const void *p, int64_t ld, int64_t z, int groups) {
+    return (((uintptr_t)p & 15) | (ld & 7) | (groups > 1 ? z & 7 : 0)) == 0;
 }
 
 template <bool F16>
-cudaError_t by_rows(const Experts &p, int nsm, bool in_aligned, bool out_aligned, cudaStream_t s) {
-    if (p.rows <= 8) return both<F16, 1>(p, nsm, in_aligned, out_aligned, s);
-    if (p.rows <= 16) return both<F16, 2>(p, nsm, in_aligned, out_aligned, s);
-    return both<F16, 4>(p, nsm, in_aligned, out_aligned, s);
+cudaError_t both(const Experts &p, const ExpertMaps &m, int nsm, cudaStream_t s) {
+    const bool in = whole16(p.w_in, p.w_in_ld, p.w_in_z, p.groups), out = whole16(p.w_out, p.w_out_ld, p.w_out_z, p.groups);
+    const bool x = whole16(p.x, p.x_ld, 0, 1);
+    cudaError_t e = launch(m.in_boxes ? x ? k_experts_in<F16, W_BOXES, true> : k_experts_in<F16, W_BOXES, false>
+                           : in       ? x ? k_experts_in<F16, W_ROWS, true> : k_experts_in<F16, W_ROWS, false>
+                           : x        ? k_experts_in<F16, W_ANY, true>
+                                      : k_experts_in<F16, W_ANY, false>,
+                           p, m.in, m.in_cols, nsm, s);
+    if (e != cudaSuccess) return e;
+    e = launch(m.out_boxes ? k_experts_out<F16, W_BOXES> : out ? k_experts_out<F16, W_ROWS> : k_experts_out<F16, W_ANY>, p,
+               m.out, m.out_cols, nsm, s);
+    if (e != cudaSuccess || (p.top == 1 && p.splits == 1)) return e;
+    cudaLaunchAttribute at[1];
+    const cudaLaunchConfig_t cfg =
+        early(dim3((unsigned)((p.n_out + SUM_THREADS - 1) / SUM_THREADS), (unsigned)p.rows), SUM_THREADS, 0, s, at);
+    return cudaLaunchKernelEx(&cfg, k_experts_sum<F16>, p);
 }
 
 }  // namespace
 
-// Pieces of the second product's contraction: enough units for the GPU's blocks where
-// tiles and experts are few, none under two steps of 32 columns a warp.
-int expert_splits(int rows, int groups, int top, int hidden, int n_out, int nsm) {
-    const int64_t pairs = (int64_t)rows * top, jobs = pairs < groups ? pairs : groups;
-    const int64_t units = jobs * ((n_out + 15) / 16), most = ((hidden + 31) / 32) / (2 * EX_WARPS);
-    int64_t n = (4 * nsm + units - 1) / (units < 1 ? 1 : units);
-    if (n > most) n = most;
-    return (int)(n < 1 ? 1 : n > 16 ? 16 : n);
+// The most pieces of the second product's contraction: none under 512 columns.
+int expert_splits(int hidden) {
+    int n = 1;
+    while (n < 16 && n * 2 * 512 <= hidden) n *= 2;
+    return n;
 }
 
-cudaError_t launch_experts(const Experts &p, bool f16, int nsm, cudaStream_t s) {
-    const bool in = (((uintptr_t)p.w_in & 15) | (p.w_in_ld & 7) | (p.groups > 1 ? p.w_in_z & 7 : 0)) == 0;
-    const bool out = (((uintptr_t)p.w_out & 15) | (p.w_out_ld & 7) | (p.groups > 1 ? p.w_out_z & 7 : 0)) == 0;
-    return f16 ? by_rows<true>(p, nsm, in, out, s) : by_rows<false>(p, nsm, in, out, s);
+size_t expert_tables(int rows, int top) {
+    Experts p;
+    p.rows = rows;
+    p.top = top;
+    return tables_bytes(p);
+}
+
+// Columns of each product's steps.
+void expert_plan(const Experts &p, bool f16, ExpertMaps *m) {
+    m->in_cols = even_columns(p.n_in, EX_COLS);
+    m->out_cols = even_columns(p.hidden, f16 ? EX_COLS / 4 : EX_COLS / 2);
+}
+
+template <bool F16>
+static cudaError_t prepare() {
+    cudaError_t e = cudaSuccess;
+    const auto set = [&](Kernel kernel) {
+        if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, EX_SMEM);
+    };
+    set(k_experts_in<F16, W_BOXES, true>);
+    set(k_experts_in<F16, W_BOXES, false>);
+    set(k_experts_in<F16, W_ROWS, true>);
+    set(k_experts_in<F16, W_ROWS, false>);
+    set(k_experts_in<F16, W_ANY, true>);
+    set(k_experts_in<F16, W_ANY, false>);
+    set(k_experts_out<F16, W_BOXES>);
+    set(k_experts_out<F16, W_ROWS>);
+    set(k_experts_out<F16, W_ANY>);
+    return e;
+}
+
+cudaError_t experts_prepare() {
+    const cudaError_t e = prepare<true>();
+    return e == cudaSuccess ? prepare<false>() : e;
+}
+
+cudaError_t launch_experts(const Experts &p, const ExpertMaps &m, bool f16, int nsm, cudaStream_t s) {
+    return f16 ? both<true>(p, m, nsm, s) : both<false>(p, m, nsm, s);
 }
 
 }  // namespace hwr

@@ -1,18 +1,11 @@
 // C-ABI host code of the operators that follow a routing decision
 // (declarations in include/hwr_ops.h): argument checks, the workspace, tensor
 // maps, and the launches of each call on the context's stream.
-#include <cudaTypedefs.h>
 #include <math.h>
 
 #include "ops_context.cuh"
 
 using namespace hwr;
-
-namespace {
-
-PFN_cuTensorMapEncodeTiled_v12000 g_encode = nullptr;
-
-}  // namespace
 
 extern "C" hwr_status hwr_ops_create(void *cuda_stream, hwr_ops **out) {
     if (!out) return fail(nullptr, HWR_ERR_INVALID_ARG, "out is NULL");
@@ -38,6 +31,7 @@ extern "C" hwr_status hwr_ops_create(void *cuda_stream, hwr_ops **out) {
         }
         CK(c, group_prepare(c->nsm, &c->ctas), "kernel attributes");
         CK(c, ops_prepare(&c->cluster), "kernel attributes");
+        CK(c, experts_prepare(), "kernel attributes");
         if (getenv("HWR_TEST_SMALL_CLUSTERS")) c->cluster = 8;
         if (cuda_stream) {
             c->stream = (cudaStream_t)cuda_stream;

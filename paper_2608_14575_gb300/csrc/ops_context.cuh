@@ -2,6 +2,7 @@
 // errors, memory, and what a call checks before it queues anything.
 #pragma once
 
+#include <cudaTypedefs.h>
 #include <stdarg.h>
 #include <stdint.h>
 #include <stdio.h>
@@ -17,6 +18,7 @@
 
 namespace hwr {
 
+inline PFN_cuTensorMapEncodeTiled_v12000 g_encode = nullptr;
 inline thread_local std::string g_create_error;      // of hwr_ops_create
 
 struct ApiRange {
@@ -63,8 +65,7 @@ struct hwr_adamw {
 };
 
 // Words that blocks count their arrivals in (zeroed once, self-resetting).
-constexpr int ARRIVALS_TILES = 0, ARRIVALS_ROWS = EXPERTS_MAX_OUT / 16, ARRIVALS_STEP = ARRIVALS_ROWS + 1024,
-              ARRIVALS = ARRIVALS_STEP + 1;
+constexpr int ARRIVALS_ROWS = 0, ARRIVALS_STEP = 1024, ARRIVALS = ARRIVALS_STEP + 1;
 
 struct hwr_ops {
     cudaStream_t stream = nullptr;

@@ -333,14 +333,31 @@ struct Experts {
     const float *gates;
     uint16_t *y;
     int64_t y_ld;
-    // workspace: h as two terms [rows * top][h_groups][2][8], bf16 or fp32; what each piece
-    // of the second product gives [rows * top][splits][n_out]
+    // workspace: h as two terms [rows * top][2][h_ld], bf16 or fp32; what each piece of the
+    // second product gives [rows * top][splits][n_out]
     void *h;
-    int h_groups, splits;
+    int64_t h_ld;                     // whole 16-byte units
+    int splits;
     float *part;
-    uint32_t *arrivals;               // [tiles of 16 outputs] zeroed once, self-resetting
+    char *tables;                     // what the routing found, for the launches after the first
+    int32_t *used_splits;
+    int32_t *status;
+    int test_stall;                   // test hook: nothing is copied (bounded waits expire)
+    // of a launch: columns of a step; where the ring of copies begins in shared memory, the
+    // bytes of a step, and steps
+    int cols, ring_at, step, depth;
 };
-int expert_splits(int rows, int groups, int top, int hidden, int n_out, int nsm);
-cudaError_t launch_experts(const Experts &p, bool f16, int nsm, cudaStream_t s);
+int expert_splits(int hidden);            // at most
+size_t expert_tables(int rows, int top);
+cudaError_t experts_prepare();
+// The weights of both products as tensors (64, rows, columns / 64, experts) where their
+// matrices allow it (boxes of 64 x 8 x columns / 64 of a step), and the steps' columns.
+struct ExpertMaps {
+    CUtensorMap in, out;
+    bool in_boxes, out_boxes;
+    int in_cols, out_cols;
+};
+void expert_plan(const Experts &p, bool f16, ExpertMaps *m);
+cudaError_t launch_experts(const Experts &p, const ExpertMaps &m, bool f16, int nsm, cudaStream_t s);
 
 }  // namespace hwr

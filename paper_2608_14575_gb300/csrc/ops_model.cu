@@ -42,6 +42,20 @@ static hwr_status check_experts(hwr_ops *c, const hwr_experts *e, const void *y,
     return HWR_OK;
 }
 
+// Matrices [groups][rows][width] in boxes of 64 columns x 8 rows, cols / 64 of them side by
+// side; false where they cannot be mapped so.
+static bool map_weights(CUtensorMap *m, bool f16, const void *w, int64_t ld, int64_t z, int64_t rows, int width, int groups,
+                        int cols) {
+    memset(m, 0, sizeof *m);
+    if (((uintptr_t)w & 15) || ld % 8 || width % 64 || (groups > 1 && z % 8)) return false;
+    const cuuint64_t dims[4] = {64, (cuuint64_t)rows, (cuuint64_t)width / 64, (cuuint64_t)groups};
+    const cuuint64_t strides[3] = {(cuuint64_t)ld * 2, 128, (cuuint64_t)(groups > 1 ? z : ld * rows) * 2};
+    const cuuint32_t box[4] = {64, 8, (cuuint32_t)cols / 64, 1}, one[4] = {1, 1, 1, 1};
+    return g_encode(m, f16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void *>(w), dims,
+                    strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                    CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 extern "C" hwr_status hwr_expert_layer(hwr_ops *c, const hwr_experts *e, void *y, int64_t y_ld) {
     if (!c) return HWR_ERR_INVALID_ARG;
     ApiRange range("hwr_expert_layer");
@@ -72,15 +86,26 @@ extern "C" hwr_status hwr_expert_layer(hwr_ops *c, const hwr_experts *e, void *y
     p.gates = e->gates;
     p.y = (uint16_t *)y;
     p.y_ld = y_ld;
-    p.h_groups = (e->hidden + 7) / 8;
-    p.splits = expert_splits(e->rows, e->groups, e->top, e->hidden, e->n_out, c->nsm);
+    p.h_ld = (e->hidden + 7) / 8 * 8;
+    p.splits = expert_splits(e->hidden);
+    const bool whole = e->top == 1 && p.splits == 1;
     const size_t pairs = (size_t)e->rows * e->top, term = e->dtype == HWR_F16 ? 4 : 2;
-    const size_t h = (pairs * p.h_groups * 16 * term + 1023) / 1024 * 1024;
-    OK(reserve(c, h + pairs * p.splits * p.n_out * 4));
+    const size_t h = (pairs * p.h_ld * 2 * term + 1023) / 1024 * 1024;
+    const size_t used = (expert_tables(e->rows, e->top) + 16 + 1023) / 1024 * 1024;
+    OK(reserve(c, h + used + (whole ? 0 : pairs * p.splits * p.n_out * 4)));
     p.h = c->ws;
-    p.part = (float *)(c->ws + h);
-    p.arrivals = c->arrivals + ARRIVALS_TILES;
-    CK(c, launch_experts(p, e->dtype == HWR_F16, c->nsm, c->stream), "expert kernels");
+    p.used_splits = (int32_t *)(c->ws + h);
+    p.tables = c->ws + h + 16;
+    p.part = (float *)(c->ws + h + used);
+    p.status = c->status_d;
+    p.test_stall = c->test_stall;
+    const bool f16 = e->dtype == HWR_F16;
+    ExpertMaps m;
+    expert_plan(p, f16, &m);
+    m.in_boxes = map_weights(&m.in, f16, e->w_in, e->w_in_ld, e->w_in_group, e->gated ? 2 * (int64_t)e->hidden : e->hidden,
+                             e->n_in, e->groups, m.in_cols);
+    m.out_boxes = map_weights(&m.out, f16, e->w_out, e->w_out_ld, e->w_out_group, e->n_out, e->hidden, e->groups, m.out_cols);
+    CK(c, launch_experts(p, m, f16, c->nsm, c->stream), "expert kernels");
     return HWR_OK;
 }
 
