@@ -12,7 +12,7 @@
 // itself from the scores (a few KB), which costs less than a launch between.  A unit of
 // work is 16 rows of a weight matrix (in the first product 8 gate rows and the 8 up rows
 // that they meet, so that the activation finds both) and a job.  A block walks a run of
-// consecutive units.  One of its warps copies the weights into a ring in shared memory,
+// consecutive units.  Two of its warps copy the weights into a ring in shared memory,
 // some steps of up to 1,024 columns ahead and across the ends of units.  Two teams of eight
 // warps take the steps in turn; a team's warps share a step's columns, 32 at a time, and
 // load their part of the job's rows of x (or h) from L2 a step ahead.  Two more warps add
@@ -40,8 +40,8 @@ using umma::mbar_arrive_expect_tx;
 using umma::mbar_init;
 using umma::mbar_wait;
 
-constexpr int EX_TEAM = 8, EX_MMA = 2 * EX_TEAM, EX_ADD = 2;      // warps that multiply, and that add up; one more copies
-constexpr int EX_WARPS = EX_MMA + 1 + EX_ADD, EX_THREADS = EX_WARPS * 32;
+constexpr int EX_TEAM = 8, EX_MMA = 2 * EX_TEAM, EX_COPY = 2, EX_ADD = 2;      // warps that multiply, copy, add up
+constexpr int EX_WARPS = EX_MMA + EX_COPY + EX_ADD, EX_THREADS = EX_WARPS * 32;
 constexpr int EX_SUMS = 2;                 // units whose sums are under way
 constexpr int EX_STRIDE = EX_TEAM * 32;    // columns of a step that a team takes at a time
 constexpr int EX_JOB = 8;                  // pairs of a job
@@ -215,6 +215,7 @@ struct Ring {
             if (p.bytes && !stall) bulk_g2s(to + lane * (cols * 2 + 16), p.from, p.bytes, full + slot);
         }
         next();
+        next();                           // (the other copying warp's)
         return true;
     }
 };
@@ -594,19 +595,25 @@ k_experts_in(const __grid_constant__ Experts p, const __grid_constant__ CUtensor
         const int64_t at = p.gated && i >= 8 ? p.hidden + f : f;
         return f < p.hidden ? p.w_in + r.expert[w.job] * p.w_in_z + at * p.w_in_ld : nullptr;
     };
-    if (warp == EX_MMA) {
-        for (; w.more(); w.next()) {
-            const uint16_t *row = W != W_BOXES && lane < 16 ? weights_row(w, lane) : nullptr;
-            const int f0 = w.tile * wide, y = lane == 0 ? f0 : p.gated ? p.hidden + f0 : f0 + 8, e = r.expert[w.job];
-            for (int s = 0; s < steps; ++s)
-                if (!ring.copy<W>(&map, y, e, row, s, cols, p.n_in, &sh.abort_flag, p.status, p.test_stall)) return;
+    if (warp >= EX_MMA && warp < EX_MMA + EX_COPY) {
+        Steps at(w, steps, steps);
+        if (warp > EX_MMA) {
+            at.next();
+            ring.next();
+        }
+        while (at.more()) {
+            const uint16_t *row = W != W_BOXES && lane < 16 ? weights_row(at.w, lane) : nullptr;
+            const int f0 = at.w.tile * wide, y = lane == 0 ? f0 : p.gated ? p.hidden + f0 : f0 + 8;
+            if (!ring.copy<W>(&map, y, r.expert[at.w.job], row, at.s, cols, p.n_in, &sh.abort_flag, p.status, p.test_stall)) return;
+            at.next();
+            if (at.more()) at.next();
         }
         return;
     }
-    if (warp > EX_MMA) {
+    if (warp >= EX_MMA) {
         for (; w.more(); w.next()) {
             const int turn = w.u - u0;
-            if (turn % EX_ADD != warp - EX_MMA - 1) continue;
+            if (turn % EX_ADD != warp - EX_MMA - EX_COPY) continue;
             const int n = r.n[w.job], begin = r.begin[w.job];
             float c[4];
             if (!take(sh, c, turn, both, p.status)) return;
@@ -748,17 +755,24 @@ k_experts_out(const __grid_constant__ Experts p, const __grid_constant__ CUtenso
     const bool whole = p.top == 1 && p.splits == 1;
     Walk w(*r.jobs, splits, tiles);
     const int u0 = w.u;
-    if (warp == EX_MMA) {
-        for (Steps at(w, per, all_steps); at.more(); at.next()) {
+    if (warp >= EX_MMA && warp < EX_MMA + EX_COPY) {
+        Steps at(w, per, all_steps);
+        if (warp > EX_MMA) {
+            at.next();
+            ring.next();
+        }
+        while (at.more()) {
             const int o = at.w.tile * 16, e = r.expert[at.w.job];
             const uint16_t *row = nullptr;
             if (W != W_BOXES && lane < 16 && o + lane < p.n_out) row = p.w_out + e * p.w_out_z + (int64_t)(o + lane) * p.w_out_ld;
             if (!ring.copy<W>(&map, o + lane * 8, e, row, at.s, cols, p.hidden, &sh.abort_flag, p.status, p.test_stall)) return;
+            at.next();
+            if (at.more()) at.next();
         }
         return;
     }
-    if (warp > EX_MMA) {
-        const int i0 = tid - (EX_MMA + 1) * 32;
+    if (warp >= EX_MMA) {
+        const int i0 = tid - (EX_MMA + EX_COPY) * 32;
         if (whole) {
             for (int t = blockIdx.x; t < p.rows; t += gridDim.x)
                 if (r.choice[t] < 0)
@@ -768,7 +782,7 @@ k_experts_out(const __grid_constant__ Experts p, const __grid_constant__ CUtenso
         }
         for (; w.more(); w.next()) {
             const int turn = w.u - u0;
-            if (turn % EX_ADD != warp - EX_MMA - 1) continue;
+            if (turn % EX_ADD != warp - EX_MMA - EX_COPY) continue;
             const int n = r.n[w.job], begin = r.begin[w.job];
             float c[4];
             if (!take(sh, c, turn, true, p.status)) return;
