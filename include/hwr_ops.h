@@ -47,7 +47,7 @@
  *                      for each gradient
  *     (weights that are read in place are the terms with n_out (n_in + 8) less),
  *       hwr_expert_layer  1,024 + 8 rows top (hidden + 7 + 8 n_out)
- *       hwr_token_logprobs  1,088 for each of the device's SMs
+ *       hwr_token_logprobs  2,176 for each of the device's SMs
  *     and the other calls none.
  *   - Stream capture: calls can be captured into graphs.  A call that would have
  *     to grow the workspace then is refused (UNSUPPORTED, nothing is queued, the

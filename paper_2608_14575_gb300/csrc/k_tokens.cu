@@ -9,11 +9,14 @@
 // the maximum (a masked one's -inf among them) counts as exp = 0 times a finite
 // distance, so that it adds nothing, not NaN.
 //
-// Alternatives: a warp keeps its best ones sorted, one a lane, as 64-bit keys (the
-// value's order above, the index's complement below: equal values go by the lowest
-// index).  Values come in the order of their indices from one step of a warp to the
-// next, so a step in which no value is above the warp's last alternative has none to
-// offer, and costs one vote.
+// Alternatives: 64-bit keys (the value's order above, the index's complement below: equal
+// values go by the lowest index).  A block's first step has its threads' largest values,
+// and from the few largest of each warp a bound that at least `top` values reach, and few
+// more.  Values above it are gathered in shared memory, at the end (or where they get too
+// many) a key's place is the number of larger ones.  Values of later steps have higher
+// indices, so those that only equal the bound have no place.
+#include <type_traits>
+
 #include "ops_internal.cuh"
 #include "values.cuh"
 
@@ -40,12 +43,6 @@ __device__ __forceinline__ float max_nan(float a, float b) {
 
 struct Sums {
     float m, s, d;
-    __device__ __forceinline__ void raise(float to) {       // to > m
-        const float by = fmaxf(m - to, FAR), f = exp2_fast(by * LOG2E);
-        d = f * (d + by * s);
-        s *= f;
-        m = to;
-    }
     __device__ __forceinline__ void join(float om, float os, float od) {
         const float to = fmaxf(m, om);
         const float a = fmaxf(m - to, FAR), b = fmaxf(om - to, FAR);
@@ -65,51 +62,72 @@ __device__ __forceinline__ float value_of(uint32_t order) {
     return __uint_as_float(order >> 31 ? order ^ 0x80000000u : ~order);      // (0: a NaN)
 }
 
+constexpr int TK_KEYS = TK_THREADS * 8;       // of a vector of each thread
+constexpr int TK_READ = 32;                   // keys that a thread compares at a time
+constexpr int TK_ROOM = TK_KEYS + TK_READ;
+constexpr int TK_MANY = 64;                   // candidates that are sorted out before a next step
 constexpr uint32_t MASKED = 0x007fffffu;      // order_of(-inf)
 
-// A warp's sorted list: lane i has the i-th best key (0: none yet).
-struct Best {
-    uint64_t key, last;       // mine; that of the last alternative
-    __device__ __forceinline__ void insert(uint64_t k, int top, int lane) {
-        const int at = __popc(__ballot_sync(ALL, key > k));
-        const uint64_t up = __shfl_up_sync(ALL, key, 1);
-        if (lane >= at) key = lane == at ? k : up;
-        last = __shfl_sync(ALL, key, top - 1);
-    }
-    // The lanes' candidates.
-    __device__ __forceinline__ void offer(uint64_t k, bool valid, int top, int lane) {
-        for (;;) {
-            const uint32_t who = __ballot_sync(ALL, valid && k > last);
-            if (!who) return;
-            const int from = __ffs(who) - 1;
-            insert(__shfl_sync(ALL, k, from), top, lane);
-            if (lane == from) valid = false;
-        }
-    }
-    // Joined with another sorted list: the largest 32 of both form a bitonic
-    // sequence, which five exchanges sort.
-    __device__ __forceinline__ void join(uint64_t other, int lane) {
-        const uint64_t turned = __shfl_sync(ALL, other, 31 - lane);
-        key = key > turned ? key : turned;
-#pragma unroll
-        for (int d = 16; d; d /= 2) {
-            const uint64_t o = __shfl_xor_sync(ALL, key, d);
-            const bool lower = lane & d;
-            key = (key > o) != lower ? key : o;
-        }
-    }
+// Keys of a block's candidates.
+struct alignas(16) Best {
+    uint64_t key[TK_ROOM], sorted[32];
+    uint32_t most[TK_WARPS];
+    int n;                                // offered; more than there is room for: some are missing
+    uint32_t bound;
 };
 
-// The order below which none of a step's values can be among the `top` best, before the
-// list is full: the top-th largest of the lanes' maxima.
-__device__ __forceinline__ uint32_t floor_of(uint32_t mine, int top, int lane) {
-    int rank = 0;
-    for (int i = 0; i < 32; ++i) {
-        const uint32_t o = __shfl_sync(ALL, mine, i);
-        rank += o > mine || (o == mine && i < lane);
+// The least value that is above (equal: or at) the bound.
+__device__ __forceinline__ float least_of(uint32_t bound, bool equal) { return value_of(bound + (equal ? 0 : 1)); }
+
+// A thread's values at or above `least`, N from index i on, the largest of which is given.
+// (Few threads have any, after the first steps.)
+template <int N>
+__device__ __forceinline__ void offer(Best &b, const float (&z)[N], float largest, int i, float least) {
+    if (!(largest >= least)) return;
+    uint32_t mine = 0;
+#pragma unroll
+    for (int j = 0; j < N; ++j) mine |= (uint32_t)(z[j] >= least) << j;
+    int at = atomicAdd(&b.n, __popc(mine));
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+        if (mine >> j & 1) {
+            if (at < TK_ROOM) b.key[at] = (uint64_t)order_of(z[j]) << 32 | (uint32_t)~(i + j);
+            ++at;
+        }
+}
+
+// The best of the gathered keys, sorted (0: none); by the block.
+__device__ __forceinline__ void settle(Best &b, int top) {
+    __syncthreads();
+    const int n = min(b.n, TK_ROOM);
+    if (threadIdx.x < 32) b.sorted[threadIdx.x] = 0;
+    if (threadIdx.x < TK_READ && n + threadIdx.x < TK_ROOM) b.key[n + threadIdx.x] = 0;
+    __syncthreads();
+    for (int i = threadIdx.x; i < n; i += TK_THREADS) {
+        const uint64_t mine = b.key[i];
+        int place = 0;
+        for (int j = 0; j < n && place < top; j += TK_READ) {
+            const ulonglong2 *o = (const ulonglong2 *)(b.key + j);
+#pragma unroll
+            for (int k = 0; k < TK_READ / 2; ++k) {
+                const ulonglong2 v = o[k];
+                place += (v.x > mine) + (v.y > mine);
+            }
+        }
+        if (place < top && mine) b.sorted[place] = mine;
     }
-    const uint32_t who = __ballot_sync(ALL, rank == top - 1);
-    return __shfl_sync(ALL, mine, __ffs(who) - 1);
+    __syncthreads();
+}
+
+// The same, left as the only candidates; the bound is the last one's value.
+__device__ __forceinline__ void squeeze(Best &b, int top) {
+    settle(b, top);
+    if (threadIdx.x < top) b.key[threadIdx.x] = b.sorted[threadIdx.x];
+    if (threadIdx.x == 0) {
+        b.n = min(b.n, top);
+        if (b.n == top) b.bound = max(b.bound, (uint32_t)(b.sorted[top - 1] >> 32));
+    }
+    __syncthreads();
 }
 
 // Where a row's 16-byte vectors begin, and how many there are.
@@ -147,15 +165,45 @@ __device__ __forceinline__ void finish(const TokenRows &p, int64_t row, const Su
     }
 }
 
+// Two fp32 values in one register pair, for the packed additions and multiplications.
+struct Two {
+    uint64_t v;
+    __device__ __forceinline__ Two(float a, float b) { asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(a), "f"(b)); }
+    __device__ __forceinline__ explicit Two(uint64_t v) : v(v) {}
+    __device__ __forceinline__ void get(float &a, float &b) const { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+};
+__device__ __forceinline__ Two operator+(Two a, Two b) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a.v), "l"(b.v));
+    return Two(r);
+}
+__device__ __forceinline__ Two operator*(Two a, Two b) {
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a.v), "l"(b.v));
+    return Two(r);
+}
+__device__ __forceinline__ Two fma2(Two a, Two b, Two c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a.v), "l"(b.v), "l"(c.v));
+    return Two(r);
+}
+
 template <int DT, bool TOP>
 __global__ void __launch_bounds__(TK_THREADS)
 k_token_rows(const __grid_constant__ TokenRows p) {
     constexpr int N = Vec<DT>::N;
     __shared__ Sums sums[TK_WARPS];
-    __shared__ uint64_t keys[TOP ? TK_WARPS : 1][32];
+    __shared__ bool last;
+    __shared__ typename std::conditional<TOP, Best, int>::type shared_best;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, top = p.top;
     const int64_t row = blockIdx.x / (uint32_t)p.splits;
     const int piece = blockIdx.x % (uint32_t)p.splits;
+    if constexpr (TOP) {
+        if (tid == 0) {
+            shared_best.n = 0;
+            shared_best.bound = MASKED;
+        }
+    }
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const void *base = row_at(p.logits, row, p.ld, DT);
@@ -165,105 +213,172 @@ k_token_rows(const __grid_constant__ TokenRows p) {
     const uint4 *vecs = (const uint4 *)((const char *)base + (DT == HWR_F32 ? 4 : 2) * cut.head);
     const int token = p.token ? p.token[row] : -1;
     const bool has = (uint32_t)token < (uint32_t)p.vocab;
-    const float z_token = has ? Vec<DT>::load(base, token) : 0.f;
+    const float z_token = has && tid == 0 ? Vec<DT>::load(base, token) : 0.f;
 
-    Sums a = {-INFINITY, 0.f, 0.f};
-    Best best = {0, 0};
-    auto add = [&](float z, float m) {
-        const float d = max_nan(z - m, FAR), e = exp2_fast(d * LOG2E);
-        a.s += e;
-        a.d = fmaf(e, d, a.d);
+    float m = -INFINITY;
+    Two s(0.f, 0.f), d(0.f, 0.f);
+    const auto raise = [&](float to) {
+        const float by = fmaxf(m - to, FAR), f = exp2_fast(by * LOG2E);
+        d = Two(f, f) * fma2(Two(by, by), s, d);
+        s = s * Two(f, f);
+        m = to;
     };
-    // one value a lane
-    auto single = [&](int i, bool valid) {
-        const float z = valid ? Vec<DT>::load(base, i) : -INFINITY;
-        if (z > a.m) a.raise(z);
-        if (valid) add(z, a.m == -INFINITY ? 0.f : a.m);
-        if (TOP) best.offer((uint64_t)order_of(z) << 32 | (uint32_t)~i, valid, top, lane);
+    const auto add = [&](float a, float b, float base) {
+        (Two(a, b) + Two(-base, -base)).get(a, b);
+        const Two x(max_nan(a, FAR), max_nan(b, FAR));
+        (x * Two(LOG2E, LOG2E)).get(a, b);
+        const Two e(exp2_fast(a), exp2_fast(b));
+        s = s + e;
+        d = fma2(e, x, d);
     };
-    if (warp == 0 && piece == 0 && cut.head) single(lane, lane < cut.head);
+    // one value a lane of the first warp
+    const auto single = [&](int i, bool valid, float least) {
+        float z[1] = {valid ? Vec<DT>::load(base, i) : -INFINITY};
+        if (z[0] > m) raise(z[0]);
+        add(z[0], -INFINITY, m == -INFINITY ? 0.f : m);
+        if constexpr (TOP) {
+            if (valid) offer<1>(shared_best, z, z[0], i, least);
+        }
+    };
+    __syncthreads();
+    if (warp == 0 && piece == 0 && cut.head) single(lane, lane < cut.head, least_of(MASKED, false));
     for (int b = v0; b < v1; b += TK_THREADS * TK_VECS) {
         uint4 u[TK_VECS];
 #pragma unroll
         for (int k = 0; k < TK_VECS; ++k) {
             const int i = b + k * TK_THREADS + tid;
-            if (i < v1) u[k] = __ldcs(vecs + i);
+            if (i < v1) u[k] = __ldg(vecs + i);
             else u[k] = Vec<DT>::lowest();
         }
-        float z[TK_VECS][N], mx = -INFINITY;
+        float z[TK_VECS][N], largest[TK_VECS], mx = -INFINITY;
 #pragma unroll
         for (int k = 0; k < TK_VECS; ++k) {
+            largest[k] = Vec<DT>::largest(u[k]);
+            mx = fmaxf(mx, largest[k]);
             Vec<DT>::unpack(u[k], z[k]);
-#pragma unroll
-            for (int j = 0; j < N; ++j) mx = fmaxf(mx, z[k][j]);
         }
-        if (mx > a.m) a.raise(mx);
-        const float m = a.m == -INFINITY ? 0.f : a.m;
+        if (mx > m) raise(mx);
+        const float base_m = m == -INFINITY ? 0.f : m;
 #pragma unroll
         for (int k = 0; k < TK_VECS; ++k)
 #pragma unroll
-            for (int j = 0; j < N; ++j) add(z[k][j], m);
-        if (TOP) {
-            const uint32_t mine = order_of(mx);
-            uint64_t least = 0;
-            if (best.last == 0) {
-                const uint32_t f = floor_of(mine, top, lane);
-                least = f > MASKED ? (uint64_t)f << 32 : 0;      // (lanes without a number have -inf)
-            }
-            if (__any_sync(ALL, mine > (uint32_t)(best.last >> 32) || best.last == 0)) {
-#pragma unroll 1
-                for (int k = 0; k < TK_VECS; ++k) {
-                    const int i = b + k * TK_THREADS + tid;
-#pragma unroll 1
-                    for (int j = 0; j < N; ++j) {
-                        const bool valid = i < v1;
-                        const int at = cut.head + i * N + j;
-                        const float v = valid ? Vec<DT>::load(base, at) : 0.f;
-                        const uint64_t key = (uint64_t)order_of(v) << 32 | (uint32_t)~at;
-                        best.offer(key, valid && key >= least, top, lane);
-                    }
+            for (int j = 0; j < N; j += 2) add(z[k][j], z[k][j + 1], base_m);
+        if constexpr (TOP) {
+            Best &best = shared_best;
+            const bool first = b == v0;
+            if (first) {
+                // in each warp as many threads as it takes for `top` in all have a value at or
+                // above this (-inf: too few have a number)
+                uint32_t mine = order_of(mx), most = 0;
+                for (int j = 0; j < (top + TK_WARPS - 1) / TK_WARPS; ++j) {
+                    most = __reduce_max_sync(ALL, mine);
+                    const uint32_t who = __ballot_sync(ALL, mine == most);
+                    if (lane == __ffs(who) - 1) mine = 0;
                 }
+                if (lane == 0) best.most[warp] = most;
+                __syncthreads();
+                if (tid == 0) {
+                    for (int w = 0; w < TK_WARPS; ++w) most = min(most, best.most[w]);
+                    best.bound = max(most, MASKED);
+                }
+                __syncthreads();
+            }
+            const uint32_t floor = best.bound;
+            // (vectors beyond the last are -inf, below any `least`)
+            const int before = best.n, at = cut.head + (b + tid) * N;
+            const auto least = [&] { return least_of(best.bound, first && best.bound == floor && floor > MASKED); };
+            __syncthreads();
+            if (mx >= least())
+#pragma unroll
+                for (int k = 0; k < TK_VECS; ++k) offer<N>(best, z[k], largest[k], at + k * TK_THREADS * N, least());
+            __syncthreads();
+            if (best.n > TK_ROOM) {
+                // not all of them found room: once more, a vector at a time
+                __syncthreads();
+                if (tid == 0) best.n = before;
+                squeeze(best, top);
+#pragma unroll
+                for (int k = 0; k < TK_VECS; ++k) {
+                    offer<N>(best, z[k], largest[k], at + k * TK_THREADS * N, least());
+                    squeeze(best, top);
+                }
+            } else if (best.n > TK_MANY && b + TK_THREADS * TK_VECS < v1) {
+                squeeze(best, top);
             }
         }
     }
     if (warp == 0 && piece == p.splits - 1) {
         const int at = cut.head + cut.vecs * N + lane;
-        single(at, at < p.vocab);
+        float least = 0.f;
+        if constexpr (TOP) least = least_of(shared_best.bound, false);
+        single(at, at < p.vocab, least);
     }
 
-    for (int d = 16; d; d /= 2)
-        a.join(__shfl_xor_sync(ALL, a.m, d), __shfl_xor_sync(ALL, a.s, d), __shfl_xor_sync(ALL, a.d, d));
+    Sums a = {m, 0.f, 0.f};
+    {
+        float x, y;
+        s.get(x, y);
+        a.s = x + y;
+        d.get(x, y);
+        a.d = x + y;
+    }
+    for (int k = 16; k; k /= 2)
+        a.join(__shfl_xor_sync(ALL, a.m, k), __shfl_xor_sync(ALL, a.s, k), __shfl_xor_sync(ALL, a.d, k));
     if (lane == 0) sums[warp] = a;
-    if (TOP) keys[warp][lane] = lane < top ? best.key : 0;
-    __syncthreads();
-    if (warp) return;
+    if constexpr (TOP) settle(shared_best, top);
+    else __syncthreads();
     a = sums[0];
     for (int w = 1; w < TK_WARPS; ++w) a.join(sums[w].m, sums[w].s, sums[w].d);
-    if (TOP)
-        for (int w = 1; w < TK_WARPS; ++w) best.join(keys[w][lane], lane);
     if (p.splits > 1) {
         TokenPart *part = p.part + row * p.splits;
-        if (lane == 0) {
-            part[piece].m = a.m;
-            part[piece].s = a.s;
-            part[piece].d = a.d;
+        if (warp == 0) {
+            if (lane == 0) {
+                part[piece].m = a.m;
+                part[piece].s = a.s;
+                part[piece].d = a.d;
+            }
+            if constexpr (TOP) part[piece].key[lane] = shared_best.sorted[lane];
+            __threadfence();
+            __syncwarp();
+            if (lane == 0) {
+                last = atomicAdd(p.arrivals + row, 1u) == (uint32_t)p.splits - 1;
+                if (last) p.arrivals[row] = 0;
+                __threadfence();
+            }
         }
-        if (TOP) part[piece].key[lane] = best.key;
-        __threadfence();
-        __syncwarp();
-        uint32_t before = 0;
-        if (lane == 0) before = atomicAdd(p.arrivals + row, 1u);
-        if (__shfl_sync(ALL, before, 0) != (uint32_t)p.splits - 1) return;
-        if (lane == 0) p.arrivals[row] = 0;
-        __threadfence();
+        __syncthreads();
+        if (!last) return;
         a = {-INFINITY, 0.f, 0.f};
-        best.key = 0;
-        for (int i = 0; i < p.splits; ++i) {
-            a.join(__ldcg(&part[i].m), __ldcg(&part[i].s), __ldcg(&part[i].d));
-            if (TOP) best.join(__ldcg(&part[i].key[lane]), lane);
+        // (all read at once, joined in their order)
+        Sums mine = a;
+        if (lane < p.splits) mine = {__ldcg(&part[lane].m), __ldcg(&part[lane].s), __ldcg(&part[lane].d)};
+        for (int i = 0; i < p.splits; ++i)
+            a.join(__shfl_sync(ALL, mine.m, i), __shfl_sync(ALL, mine.s, i), __shfl_sync(ALL, mine.d, i));
+        if constexpr (TOP) {
+            for (int i = tid; i < p.splits * top; i += TK_THREADS) shared_best.key[i] = __ldcg(&part[i / top].key[i % top]);
+            if (tid == 0) shared_best.n = p.splits * top;
+            settle(shared_best, top);
         }
     }
-    finish<TOP>(p, row, a, best.key, z_token, has, lane);
+    if (warp) return;
+    uint64_t key = 0;
+    if constexpr (TOP) {
+        // fewer numbers than alternatives: the first masked values follow, then NaN
+        uint64_t *sorted = shared_best.sorted;
+        int found = __popc(__ballot_sync(ALL, lane < top && sorted[lane] != 0));
+        for (int kind = 0; kind < 2; ++kind)
+            for (int i = 0; found < top && i < p.vocab; i += 32) {
+                const float z = i + lane < p.vocab ? Vec<DT>::load(base, i + lane) : 0.f;
+                const bool is = i + lane < p.vocab && (kind ? z != z : z == -INFINITY);
+                const uint32_t who = __ballot_sync(ALL, is);
+                const int at = found + __popc(who & ((1u << lane) - 1));
+                if (is && at < top) sorted[at] = (uint64_t)order_of(z) << 32 | (uint32_t)~(i + lane);
+                found += __popc(who);
+            }
+        __syncwarp();
+        key = sorted[lane];
+    }
+    finish<TOP>(p, row, a, key, z_token, has, lane);
 }
 
 // dz = a (1[token] - q) - b q (log q + entropy), q = exp((z - m) - log S): bound by
@@ -329,13 +444,13 @@ k_token_grad(const __grid_constant__ TokenGrad p) {
 // step of a block.
 static int row_pieces(int rows, int vocab, int size, int blocks, int most) {
     const int64_t steps = ((int64_t)vocab * size + TK_THREADS * TK_VECS * 16 - 1) / (TK_THREADS * TK_VECS * 16);
-    int64_t n = (blocks + rows - 1) / rows;
+    int64_t n = blocks / rows;
     if (n > steps) n = steps;
     return (int)(n < 1 ? 1 : n > most ? most : n);
 }
 
 int token_splits(int rows, int vocab, hwr_dtype dtype, int nsm) {
-    return row_pieces(rows, vocab, dtype == HWR_F32 ? 4 : 2, 2 * nsm, TOKEN_SPLITS);
+    return row_pieces(rows, vocab, dtype == HWR_F32 ? 4 : 2, 4 * nsm, TOKEN_SPLITS);
 }
 
 static cudaLaunchConfig_t early(int64_t grid, cudaStream_t s, cudaLaunchAttribute *at) {

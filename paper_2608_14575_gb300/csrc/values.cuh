@@ -48,6 +48,18 @@ struct Vec {
         const uint32_t w = DT == HWR_F32 ? 0xff800000u : DT == HWR_BF16 ? 0xff80ff80u : 0xfc00fc00u;
         return make_uint4(w, w, w, w);
     }
+    __device__ static float largest(const uint4 &u) {    // (NaN left out)
+        if (DT == HWR_F32)
+            return fmaxf(fmaxf(__uint_as_float(u.x), __uint_as_float(u.y)), fmaxf(__uint_as_float(u.z), __uint_as_float(u.w)));
+        if (DT == HWR_BF16) {
+            const auto two = [](uint32_t w) { return *(const __nv_bfloat162 *)&w; };
+            const __nv_bfloat162 m = __hmax2(__hmax2(two(u.x), two(u.y)), __hmax2(two(u.z), two(u.w)));
+            return fmaxf(__low2float(m), __high2float(m));
+        }
+        const auto two = [](uint32_t w) { return *(const __half2 *)&w; };
+        const __half2 m = __hmax2(__hmax2(two(u.x), two(u.y)), __hmax2(two(u.z), two(u.w)));
+        return fmaxf(__low2float(m), __high2float(m));
+    }
     __device__ static float load(const void *p, int i) {
         if (DT == HWR_F32) return ((const float *)p)[i];
         if (DT == HWR_BF16) return __bfloat162float(((const __nv_bfloat16 *)p)[i]);
