@@ -25,6 +25,12 @@ namespace {
 
 constexpr int TK_THREADS = 256, TK_WARPS = TK_THREADS / 32;
 constexpr int TK_VECS = 4;             // 16-byte loads of a step
+// Blocks of rows alone are smaller, so that more of them are at different stages of a row:
+// 4,099 rows of 50,001 bf16 logits 77 us with 256 threads, 69 with 128; 2,048 in fp32 68 and
+// 71, and 61 where a step is loaded ahead (bf16 71, fp16 67 for 68: not done).  Alternatives
+// want few blocks, each of which finds a bound of its own: 64 rows of 131,072 with 20 take
+// 18 us with 256 threads, 24 with 128.
+__host__ __device__ constexpr int threads_of(bool top) { return top ? TK_THREADS : 128; }
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr float FAR = -1e30f;
 constexpr uint32_t ALL = 0xffffffffu;
@@ -189,10 +195,11 @@ __device__ __forceinline__ Two fma2(Two a, Two b, Two c) {
 }
 
 template <int DT, bool TOP>
-__global__ void __launch_bounds__(TK_THREADS)
+__global__ void __launch_bounds__(threads_of(TOP), TOP ? 4 : DT == HWR_F32 ? 8 : DT == HWR_BF16 ? 10 : 9)
 k_token_rows(const __grid_constant__ TokenRows p) {
-    constexpr int N = Vec<DT>::N;
-    __shared__ Sums sums[TK_WARPS];
+    constexpr int N = Vec<DT>::N, TH = threads_of(TOP);
+    constexpr bool AHEAD = !TOP && DT == HWR_F32;
+    __shared__ Sums sums[TH / 32];
     __shared__ bool last;
     __shared__ typename std::conditional<TOP, Best, int>::type shared_best;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, top = p.top;
@@ -242,14 +249,23 @@ k_token_rows(const __grid_constant__ TokenRows p) {
     };
     __syncthreads();
     if (warp == 0 && piece == 0 && cut.head) single(lane, lane < cut.head, least_of(MASKED, false));
-    for (int b = v0; b < v1; b += TK_THREADS * TK_VECS) {
-        uint4 u[TK_VECS];
+    // (32-bit values: a step's are on their way while the one before is taken)
+    uint4 next[TK_VECS];
+    const auto fetch = [&](int b) {
 #pragma unroll
         for (int k = 0; k < TK_VECS; ++k) {
-            const int i = b + k * TK_THREADS + tid;
-            if (i < v1) u[k] = __ldg(vecs + i);
-            else u[k] = Vec<DT>::lowest();
+            const int i = b + k * TH + tid;
+            next[k] = Vec<DT>::lowest();
+            if (i < v1) next[k] = __ldg(vecs + i);
         }
+    };
+    if (AHEAD) fetch(v0);
+    for (int b = v0; b < v1; b += TH * TK_VECS) {
+        uint4 u[TK_VECS];
+        if (!AHEAD) fetch(b);
+#pragma unroll
+        for (int k = 0; k < TK_VECS; ++k) u[k] = next[k];
+        if (AHEAD) fetch(b + TH * TK_VECS);
         float z[TK_VECS][N], largest[TK_VECS], mx = -INFINITY;
 #pragma unroll
         for (int k = 0; k < TK_VECS; ++k) {
@@ -290,7 +306,7 @@ k_token_rows(const __grid_constant__ TokenRows p) {
             __syncthreads();
             if (mx >= least())
 #pragma unroll
-                for (int k = 0; k < TK_VECS; ++k) offer<N>(best, z[k], largest[k], at + k * TK_THREADS * N, least());
+                for (int k = 0; k < TK_VECS; ++k) offer<N>(best, z[k], largest[k], at + k * TH * N, least());
             __syncthreads();
             if (best.n > TK_ROOM) {
                 // not all of them found room: once more, a vector at a time
@@ -299,10 +315,10 @@ k_token_rows(const __grid_constant__ TokenRows p) {
                 squeeze(best, top);
 #pragma unroll
                 for (int k = 0; k < TK_VECS; ++k) {
-                    offer<N>(best, z[k], largest[k], at + k * TK_THREADS * N, least());
+                    offer<N>(best, z[k], largest[k], at + k * TH * N, least());
                     squeeze(best, top);
                 }
-            } else if (best.n > TK_MANY && b + TK_THREADS * TK_VECS < v1) {
+            } else if (best.n > TK_MANY && b + TH * TK_VECS < v1) {
                 squeeze(best, top);
             }
         }
@@ -328,7 +344,7 @@ k_token_rows(const __grid_constant__ TokenRows p) {
     if constexpr (TOP) settle(shared_best, top);
     else __syncthreads();
     a = sums[0];
-    for (int w = 1; w < TK_WARPS; ++w) a.join(sums[w].m, sums[w].s, sums[w].d);
+    for (int w = 1; w < TH / 32; ++w) a.join(sums[w].m, sums[w].s, sums[w].d);
     if (p.splits > 1) {
         TokenPart *part = p.part + row * p.splits;
         if (warp == 0) {
@@ -355,7 +371,7 @@ k_token_rows(const __grid_constant__ TokenRows p) {
         for (int i = 0; i < p.splits; ++i)
             a.join(__shfl_sync(ALL, mine.m, i), __shfl_sync(ALL, mine.s, i), __shfl_sync(ALL, mine.d, i));
         if constexpr (TOP) {
-            for (int i = tid; i < p.splits * top; i += TK_THREADS) shared_best.key[i] = __ldcg(&part[i / top].key[i % top]);
+            for (int i = tid; i < p.splits * top; i += TH) shared_best.key[i] = __ldcg(&part[i / top].key[i % top]);
             if (tid == 0) shared_best.n = p.splits * top;
             settle(shared_best, top);
         }
@@ -442,23 +458,24 @@ k_token_grad(const __grid_constant__ TokenGrad p) {
 
 // Pieces of a row: enough blocks for the GPU where rows are few, none shorter than a
 // step of a block.
-static int row_pieces(int rows, int vocab, int size, int blocks, int most) {
-    const int64_t steps = ((int64_t)vocab * size + TK_THREADS * TK_VECS * 16 - 1) / (TK_THREADS * TK_VECS * 16);
+static int row_pieces(int rows, int vocab, int size, int threads, int blocks, int most) {
+    const int step = threads * TK_VECS * 16;
+    const int64_t steps = ((int64_t)vocab * size + step - 1) / step;
     int64_t n = blocks / rows;
     if (n > steps) n = steps;
     return (int)(n < 1 ? 1 : n > most ? most : n);
 }
 
-int token_splits(int rows, int vocab, hwr_dtype dtype, int nsm) {
-    return row_pieces(rows, vocab, dtype == HWR_F32 ? 4 : 2, 4 * nsm, TOKEN_SPLITS);
+int token_splits(int rows, int vocab, hwr_dtype dtype, bool top, int nsm) {
+    return row_pieces(rows, vocab, dtype == HWR_F32 ? 4 : 2, threads_of(top), (top ? 4 : 8) * nsm, TOKEN_SPLITS);
 }
 
-static cudaLaunchConfig_t early(int64_t grid, cudaStream_t s, cudaLaunchAttribute *at) {
+static cudaLaunchConfig_t early(int64_t grid, int threads, cudaStream_t s, cudaLaunchAttribute *at) {
     cudaLaunchConfig_t cfg = {};
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.gridDim = dim3((unsigned)grid);
-    cfg.blockDim = dim3(TK_THREADS);
+    cfg.blockDim = dim3((unsigned)threads);
     cfg.stream = s;
     cfg.attrs = at;
     cfg.numAttrs = 1;
@@ -472,16 +489,16 @@ static cudaError_t rows_of(const TokenRows &p, const cudaLaunchConfig_t &cfg) {
 
 cudaError_t launch_token_rows(const TokenRows &p, hwr_dtype dtype, cudaStream_t s) {
     cudaLaunchAttribute at[1];
-    const cudaLaunchConfig_t cfg = early((int64_t)p.rows * p.splits, s, at);
+    const cudaLaunchConfig_t cfg = early((int64_t)p.rows * p.splits, threads_of(p.top > 0), s, at);
     return dtype == HWR_F32    ? rows_of<HWR_F32>(p, cfg)
            : dtype == HWR_BF16 ? rows_of<HWR_BF16>(p, cfg)
                                : rows_of<HWR_F16>(p, cfg);
 }
 
 cudaError_t launch_token_grad(TokenGrad p, hwr_dtype dtype, int nsm, cudaStream_t s) {
-    p.splits = row_pieces(p.rows, p.vocab, dtype == HWR_F32 ? 4 : 2, 8 * nsm, 1024);
+    p.splits = row_pieces(p.rows, p.vocab, dtype == HWR_F32 ? 4 : 2, TK_THREADS, 8 * nsm, 1024);
     cudaLaunchAttribute at[1];
-    const cudaLaunchConfig_t cfg = early((int64_t)p.rows * p.splits, s, at);
+    const cudaLaunchConfig_t cfg = early((int64_t)p.rows * p.splits, TK_THREADS, s, at);
     return dtype == HWR_F32    ? cudaLaunchKernelEx(&cfg, k_token_grad<HWR_F32>, p)
            : dtype == HWR_BF16 ? cudaLaunchKernelEx(&cfg, k_token_grad<HWR_BF16>, p)
                                : cudaLaunchKernelEx(&cfg, k_token_grad<HWR_F16>, p);

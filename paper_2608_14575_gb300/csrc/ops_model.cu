@@ -147,7 +147,7 @@ extern "C" hwr_status hwr_token_logprobs(hwr_ops *c, const hwr_logits *l, int32_
     p.stats = stats;
     p.top_token = top_token;
     p.top_logprob = top_logprob;
-    p.splits = token_splits(l->rows, l->vocab, l->dtype, c->nsm);
+    p.splits = token_splits(l->rows, l->vocab, l->dtype, top > 0, c->nsm);
     if (l->rows > ARRIVALS_STEP - ARRIVALS_ROWS) p.splits = 1;
     if (p.splits > 1) OK(reserve(c, (size_t)l->rows * p.splits * sizeof(TokenPart)));
     p.part = (TokenPart *)c->ws;
