@@ -1,7 +1,7 @@
 // The AdamW step over many tensors: one launch, a pass over parameters, gradients and
 // moments, bound by HBM.  A thread takes eight consecutive elements, a block 2,048 of
-// one tensor, named by a table in device memory as in gradient clipping; the
-// gradients' addresses, which change from step to step, are kernel parameters.
+// one tensor, named by a table in device memory as in gradient clipping (read a chunk
+// ahead); the gradients' addresses, which change from step to step, are kernel parameters.
 //
 // With moments in 8 bits, 256 elements (a warp's) share a power of two: the largest
 // magnitude lies in [2^7, 2^8) of e4m3's values, and those down to 2^-16 of it keep
@@ -124,12 +124,18 @@ __device__ __forceinline__ uint32_t mixed(uint32_t x) {
     return x ^ x >> 16;
 }
 
-constexpr float UP = 0x1p120f, DOWN = 0x1p-120f;      // between e4m3's exponents and fp32's last ones
+constexpr float DOWN = 0x1p-120f;         // from e4m3's exponents to fp32's last ones
 
-__device__ __forceinline__ float value8(uint2 c, int j, float scale) {
-    const uint32_t b = (j < 4 ? c.x : c.y) >> 8 * (j & 3);
-    const float x = __uint_as_float((b & 0x7f) << 20) * UP;
-    return __fmul_rn(b & 0x80 ? -x : x, scale);
+// Eight e4m3 values times their block's power of two.
+__device__ __forceinline__ void values8(uint2 c, float scale, float (&f)[8]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint16_t pair = (uint16_t)((i < 2 ? c.x : c.y) >> 16 * (i & 1));
+        uint32_t h;
+        asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"(pair));
+        const float2 x = __half22float2(*(const __half2 *)&h);
+        (Two(x.x, x.y) * Two(scale, scale)).get(f[2 * i], f[2 * i + 1]);
+    }
 }
 
 // The power of two of a warp's block with this largest magnitude (its bits), and its inverse.
@@ -138,16 +144,10 @@ __device__ __forceinline__ uint32_t scale_field(uint32_t most) {
     return (uint32_t)(f < 1 ? 1 : f) << 23;
 }
 
-__device__ __forceinline__ uint32_t code8(float x, float inverse, uint32_t random, bool least) {
-    const uint32_t u = __float_as_uint(x);
-    const float tiny = __fmul_rn(__fmul_rn(fabsf(x), inverse), DOWN);
-    uint32_t c = (__float_as_uint(tiny) + (random << 4 | 8)) >> 20;
-    if (least && x > 0.f && c == 0) c = 1;
-    return (c & 0x7f) | (u >> 24 & 0x80);
-}
-
-__device__ __forceinline__ uint2 codes8(const float (&x)[8], float *scale, const uint32_t (&random)[8], int shift,
-                                        bool least, bool write) {
+// Bytes of eight values (root: not negative, and above 0 where the value is), rounded up or
+// down by the high or the low 16 random bits of each.
+template <bool ROOT>
+__device__ __forceinline__ uint2 codes8(const float (&x)[8], float *scale, const uint32_t (&random)[8], bool write) {
     uint32_t most = 0;
 #pragma unroll
     for (int j = 0; j < 8; ++j) most = max(most, __float_as_uint(x[j]) & 0x7fffffffu);
@@ -155,16 +155,47 @@ __device__ __forceinline__ uint2 codes8(const float (&x)[8], float *scale, const
     const uint32_t field = scale_field(most);
     const float inverse = __uint_as_float((254u << 23) - field);
     if (write) *scale = most >= 0x7f800000u ? __uint_as_float(0x7fc00000u) : __uint_as_float(field);
-    uint32_t w[2] = {0, 0};
+    // (both powers of two in one multiplication, where their product is a normal number: the
+    // result is the same, as the first one's is exact unless the second makes 0 of it)
+    const bool one = field < 134u << 23;
+    const float down = one ? __uint_as_float((134u << 23) - field) : DOWN;
+    uint32_t c[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) w[j / 4] |= code8(x[j], inverse, random[j] >> shift & 0xffffu, least) << 8 * (j & 3);
+    for (int j = 0; j < 8; j += 2) {
+        float a = fabsf(x[j]), b = fabsf(x[j + 1]);
+        if (!one) (Two(a, b) * Two(inverse, inverse)).get(a, b);
+        (Two(a, b) * Two(down, down)).get(a, b);
+        c[j] = __float_as_uint(a);
+        c[j + 1] = __float_as_uint(b);
+    }
+    uint32_t w[2];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const uint32_t bits = ROOT ? random[j] >> 12 & 0xffff0u : random[j] << 4 & 0xffff0u;
+        c[j] = (c[j] + (bits | 8)) >> 20;
+        if (ROOT) c[j] = max(c[j], min(__float_as_uint(x[j]), 1u));
+        else c[j] |= __float_as_uint(x[j]) >> 24 & 0x80u;
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+        w[i] = __byte_perm(__byte_perm(c[4 * i], c[4 * i + 1], 0x0040), __byte_perm(c[4 * i + 2], c[4 * i + 3], 0x0040), 0x5410);
     return make_uint2(w[0], w[1]);
+}
+
+// Within a unit of the last place, for values whose bits nobody keeps.
+__device__ __forceinline__ float root(float x) {
+    float y;
+    asm("sqrt.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
 }
 
 template <int BITS>
 __global__ void __launch_bounds__(AW_THREADS)
 k_adamw(const __grid_constant__ AdamWStep p) {
     const int tid = threadIdx.x, lane = tid & 31;
+    // (the tables were there before the call)
+    AdamWChunk next = {p.tensor0, 0};
+    if ((int)blockIdx.x < p.chunks) next = p.table[blockIdx.x];
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int32_t t = *p.step + 1;
@@ -180,15 +211,16 @@ k_adamw(const __grid_constant__ AdamWStep p) {
     const uint32_t key_t = mixed((uint32_t)t + p.seed * 0x9e3779b1u);
     if (!skip)
         for (int i = blockIdx.x; i < p.chunks; i += gridDim.x) {
-            const AdamWChunk c = p.table[i];
-            const void *grad = p.grad[c.tensor - p.tensor0];
+            const AdamWChunk now = next;
+            if (i + gridDim.x < p.chunks) next = p.table[i + gridDim.x];
+            const AdamWTensor c = p.tensors[now.tensor];
+            const void *grad = p.grad[now.tensor - p.tensor0];
             if (!grad) continue;
-            const int gt = p.dtype[c.tensor - p.tensor0];
-            const int own = c.n - tid * 8, n = own < 0 ? 0 : own < 8 ? own : 8;
+            const int gt = p.dtype[now.tensor - p.tensor0];
+            const int64_t at = (int64_t)now.chunk * ADAMW_CHUNK + tid * 8, own = c.n - at;
+            const int n = own < 0 ? 0 : own < 8 ? (int)own : 8;
             // (the last elements, and tensors that are not aligned to 16 bytes, go one by one)
-            const bool full = n == 8 && (((uintptr_t)c.param | (uintptr_t)c.copy | (uintptr_t)c.m | (uintptr_t)c.v |
-                                          (uintptr_t)grad) & 15) == 0;
-            const int64_t at = c.first + tid * 8;
+            const bool full = n == 8 && c.aligned && ((uintptr_t)grad & 15) == 0;
             const Raw rp = take(c.param, HWR_F32, at, n, full), rg = take(grad, gt, at, n, full);
             Raw rm, rv;
             uint2 cm, cv;
@@ -210,25 +242,21 @@ k_adamw(const __grid_constant__ AdamWStep p) {
                 widen(rm, HWR_F32, m);
                 widen(rv, HWR_F32, v);
             } else {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    m[j] = value8(cm, j, sm);
-                    const float r = value8(cv, j, sv);
-                    v[j] = __fmul_rn(r, r);
-                }
+                values8(cm, sm, m);
+                values8(cv, sv, v);
             }
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const float f = __fmul_rn(g[j], k);
+                const float f = __fmul_rn(g[j], k), old = BITS == 32 ? v[j] : __fmul_rn(v[j], v[j]);
                 m[j] = __fadd_rn(__fmul_rn(m[j], p.b1), __fmul_rn(f, p.one_b1));
-                v[j] = __fadd_rn(__fmul_rn(v[j], p.b2), __fmul_rn(__fmul_rn(f, f), p.one_b2));
+                v[j] = __fadd_rn(__fmul_rn(old, p.b2), __fmul_rn(__fmul_rn(f, f), p.one_b2));
             }
             if (BITS == 32) {
                 put32((float *)c.m + at, m, n, full);
                 put32((float *)c.v + at, v, n, full);
             }
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = __fsqrt_rn(v[j]);
+            for (int j = 0; j < 8; ++j) v[j] = BITS == 8 ? __fsqrt_rn(v[j]) : root(v[j]);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const float step = __fdividef(m[j] * by1, fmaf(v[j], by2, p.eps));
@@ -240,7 +268,7 @@ k_adamw(const __grid_constant__ AdamWStep p) {
                 else put16<HWR_F16>(c.copy, at, w, n, full);
             }
             if (BITS == 8) {
-                const uint32_t tensor = mixed(key_t + (uint32_t)(c.tensor + 1) * 0x85157af5u);
+                const uint32_t tensor = mixed(key_t + (uint32_t)(now.tensor + 1) * 0x85157af5u);
                 // (elements from 2^32 on: others' bits, turned)
                 const uint32_t key = at >> 32 ? mixed(tensor ^ (uint32_t)(at >> 32)) : tensor;
                 uint32_t random[8];
@@ -249,8 +277,8 @@ k_adamw(const __grid_constant__ AdamWStep p) {
                     random[j] = mixed((uint32_t)(at + j) * 0x9e3779b1u + key);
                     if (j >= n) m[j] = v[j] = 0.f;
                 }
-                put8(c.m, at, codes8(m, c.m_scale + block, random, 0, false, lane == 0 && n), n, full);
-                put8(c.v, at, codes8(v, c.v_scale + block, random, 16, true, lane == 0 && n), n, full);
+                put8(c.m, at, codes8<false>(m, c.m_scale + block, random, lane == 0 && n), n, full);
+                put8(c.v, at, codes8<true>(v, c.v_scale + block, random, lane == 0 && n), n, full);
             }
         }
     // the last block of the call to have read the step's number counts it up

@@ -171,29 +171,6 @@ __device__ __forceinline__ void finish(const TokenRows &p, int64_t row, const Su
     }
 }
 
-// Two fp32 values in one register pair, for the packed additions and multiplications.
-struct Two {
-    uint64_t v;
-    __device__ __forceinline__ Two(float a, float b) { asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(a), "f"(b)); }
-    __device__ __forceinline__ explicit Two(uint64_t v) : v(v) {}
-    __device__ __forceinline__ void get(float &a, float &b) const { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
-};
-__device__ __forceinline__ Two operator+(Two a, Two b) {
-    uint64_t r;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a.v), "l"(b.v));
-    return Two(r);
-}
-__device__ __forceinline__ Two operator*(Two a, Two b) {
-    uint64_t r;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a.v), "l"(b.v));
-    return Two(r);
-}
-__device__ __forceinline__ Two fma2(Two a, Two b, Two c) {
-    uint64_t r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a.v), "l"(b.v), "l"(c.v));
-    return Two(r);
-}
-
 template <int DT, bool TOP>
 __global__ void __launch_bounds__(threads_of(TOP), TOP ? 4 : DT == HWR_F32 ? 8 : DT == HWR_BF16 ? 10 : 9)
 k_token_rows(const __grid_constant__ TokenRows p) {

@@ -74,7 +74,7 @@ extern "C" hwr_status hwr_ops_destroy(hwr_ops *c) {
     }
     while (hwr_adamw *o = c->optimizers) {
         c->optimizers = o->next;
-        cudaFree(o->table);
+        cudaFree(o->tensors);
         delete[] o->chunk0;
         delete o;
     }

@@ -56,7 +56,8 @@ struct hwr_gradients {
 };
 
 struct hwr_adamw {
-    AdamWChunk *table = nullptr;
+    AdamWTensor *tensors = nullptr;     // device: the tensors, then
+    AdamWChunk *table = nullptr;        // their chunks
     int n = 0, bits = 32;
     int *chunk0 = nullptr;              // host, [n + 1]: first chunk of each tensor
     int32_t *step = nullptr;

@@ -295,15 +295,18 @@ cudaError_t launch_token_grad(TokenGrad p, hwr_dtype dtype, int nsm, cudaStream_
 // A block's elements; with moments in 8 bits a warp's share one power of two.
 constexpr int ADAMW_CHUNK = 2048, ADAMW_BLOCK = 256;
 constexpr int ADAMW_TABLE = 256;      // tensors of one launch
-struct alignas(16) AdamWChunk {
+struct alignas(64) AdamWTensor {
     float *param;
     void *copy, *m, *v;               // copy: may be null
     float *m_scale, *v_scale;
-    int64_t first;                    // of its elements in the tensor
-    int32_t n, tensor;
-    int32_t copy_dtype, unused[3];
+    int64_t n;
+    int32_t copy_dtype, aligned;      // aligned: to 16 bytes, all of them
+};
+struct AdamWChunk {
+    int32_t tensor, chunk;            // and which of its chunks
 };
 struct AdamWStep {
+    const AdamWTensor *tensors;
     const AdamWChunk *table;
     int chunks, tensor0;              // chunks of this launch; the first of its tensors
     uint32_t blocks;                  // of all the call's launches

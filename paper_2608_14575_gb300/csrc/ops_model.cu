@@ -217,44 +217,48 @@ extern "C" hwr_status hwr_adamw_create(hwr_ops *c, int32_t n, const hwr_adamw_te
         if (chunks >= INT32_MAX) return fail(c, HWR_ERR_UNSUPPORTED, "too many elements");
     }
     hwr_adamw *o = new (std::nothrow) hwr_adamw;
-    AdamWChunk *host = new (std::nothrow) AdamWChunk[chunks ? chunks : 1];
+    const size_t bytes = n * sizeof(AdamWTensor) + (chunks ? chunks : 1) * sizeof(AdamWChunk);
+    char *host = new (std::nothrow) char[bytes];
     if (o) o->chunk0 = new (std::nothrow) int[n + 1];
     hwr_status s = o && host && o->chunk0 ? HWR_OK : fail(c, HWR_ERR_OOM, "host allocation failed");
-    if (s == HWR_OK) s = alloc(c, &o->table, chunks ? chunks : 1);
+    char *device = nullptr;
+    if (s == HWR_OK) s = alloc(c, &device, bytes);
     if (s == HWR_OK) {
+        o->tensors = (AdamWTensor *)device;
+        o->table = (AdamWChunk *)(device + n * sizeof(AdamWTensor));
         o->n = n;
         o->bits = bits;
         o->step = step;
         int at = 0;
         for (int i = 0; i < n; ++i) {
             const hwr_adamw_tensor &t = tensors[i];
+            AdamWTensor d;
+            d.param = (float *)t.param;
+            d.copy = t.copy;
+            d.m = t.m;
+            d.v = t.v;
+            d.m_scale = t.m_scale;
+            d.v_scale = t.v_scale;
+            d.n = t.n;
+            d.copy_dtype = t.copy_dtype;
+            d.aligned = (((uintptr_t)t.param | (uintptr_t)t.copy | (uintptr_t)t.m | (uintptr_t)t.v) & 15) == 0;
+            memcpy(host + i * sizeof d, &d, sizeof d);
             o->chunk0[i] = at;
-            for (int64_t first = 0; first < t.n; first += ADAMW_CHUNK) {
-                AdamWChunk &k = host[at++];
-                k.param = (float *)t.param;
-                k.copy = t.copy;
-                k.m = t.m;
-                k.v = t.v;
-                k.m_scale = t.m_scale;
-                k.v_scale = t.v_scale;
-                k.first = first;
-                k.n = (int32_t)(t.n - first < ADAMW_CHUNK ? t.n - first : ADAMW_CHUNK);
-                k.tensor = i;
-                k.copy_dtype = t.copy_dtype;
+            for (int64_t k = 0; k * ADAMW_CHUNK < t.n; ++k, ++at) {
+                const AdamWChunk chunk = {i, (int32_t)k};
+                memcpy(host + n * sizeof d + at * sizeof chunk, &chunk, sizeof chunk);
             }
         }
         o->chunk0[n] = at;
-        cudaError_t e = cudaMemcpyAsync(o->table, host, chunks * sizeof(AdamWChunk), cudaMemcpyHostToDevice, c->stream);
+        cudaError_t e = cudaMemcpyAsync(device, host, bytes, cudaMemcpyHostToDevice, c->stream);
         if (e == cudaSuccess) e = cudaStreamSynchronize(c->stream);
         if (e != cudaSuccess) s = cuda_fail(c, e, "optimizer table");
     }
     delete[] host;
     if (s != HWR_OK) {
         const Unwatched memory;
-        if (o) {
-            cudaFree(o->table);
-            delete[] o->chunk0;
-        }
+        cudaFree(device);
+        if (o) delete[] o->chunk0;
         delete o;
         return s;
     }
@@ -311,6 +315,7 @@ extern "C" hwr_status hwr_adamw_step(hwr_ops *c, const hwr_adamw *o, const hwr_a
     }
     for (int k = 0; k < launches || k == 0; ++k) {
         const int t0 = k * ADAMW_TABLE, t1 = o->n < t0 + ADAMW_TABLE ? o->n : t0 + ADAMW_TABLE;
+        p.tensors = o->tensors;
         p.table = o->table + o->chunk0[t0];
         p.chunks = o->chunk0[t1] - o->chunk0[t0];
         p.tensor0 = t0;
@@ -332,11 +337,11 @@ extern "C" hwr_status hwr_adamw_destroy(hwr_ops *c, hwr_adamw *o) {
     bool captured;
     OK(capturing(c, &captured));
     if (captured || o->held) {          // (during a capture nothing is waited for or freed)
-        OK(retire(c, o->table));
+        OK(retire(c, o->tensors));
     } else {
         const Unwatched memory;
         cudaStreamSynchronize(c->stream);
-        cudaFree(o->table);
+        cudaFree(o->tensors);
         cudaGetLastError();
     }
     *at = o->next;
