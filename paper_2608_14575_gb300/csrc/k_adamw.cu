@@ -116,6 +116,13 @@ __device__ __forceinline__ void put8(void *p, int64_t i, uint2 c, int n, bool fu
         if (j < n) q[j] = (uint8_t)((j < 4 ? c.x : c.y) >> 8 * (j & 3));
 }
 
+// max(a, b), NaN where one of them is
+__device__ __forceinline__ float max_nan(float a, float b) {
+    float y;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
+    return y;
+}
+
 // A 32-bit hash of whole numbers, each output bit of which depends on every input bit
 // about evenly (tested on the rounding that it drives).
 __device__ __forceinline__ uint32_t mixed(uint32_t x) {
@@ -148,10 +155,10 @@ __device__ __forceinline__ uint32_t scale_field(uint32_t most) {
 // down by the high or the low 16 random bits of each.
 template <bool ROOT>
 __device__ __forceinline__ uint2 codes8(const float (&x)[8], float *scale, const uint32_t (&random)[8], bool write) {
-    uint32_t most = 0;
+    float largest = fabsf(x[0]);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) most = max(most, __float_as_uint(x[j]) & 0x7fffffffu);
-    most = __reduce_max_sync(0xffffffffu, most);
+    for (int j = 1; j < 8; ++j) largest = max_nan(largest, fabsf(x[j]));
+    const uint32_t most = __reduce_max_sync(0xffffffffu, __float_as_uint(largest));
     const uint32_t field = scale_field(most);
     const float inverse = __uint_as_float((254u << 23) - field);
     if (write) *scale = most >= 0x7f800000u ? __uint_as_float(0x7fc00000u) : __uint_as_float(field);
@@ -162,7 +169,7 @@ __device__ __forceinline__ uint2 codes8(const float (&x)[8], float *scale, const
     uint32_t c[8];
 #pragma unroll
     for (int j = 0; j < 8; j += 2) {
-        float a = fabsf(x[j]), b = fabsf(x[j + 1]);
+        float a = x[j], b = x[j + 1];
         if (!one) (Two(a, b) * Two(inverse, inverse)).get(a, b);
         (Two(a, b) * Two(down, down)).get(a, b);
         c[j] = __float_as_uint(a);
@@ -172,9 +179,10 @@ __device__ __forceinline__ uint2 codes8(const float (&x)[8], float *scale, const
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
         const uint32_t bits = ROOT ? random[j] >> 12 & 0xffff0u : random[j] << 4 & 0xffff0u;
+        // (the value's bits below the sign, whose place in the byte is four lower)
         c[j] = (c[j] + (bits | 8)) >> 20;
         if (ROOT) c[j] = max(c[j], min(__float_as_uint(x[j]), 1u));
-        else c[j] |= __float_as_uint(x[j]) >> 24 & 0x80u;
+        else c[j] = (c[j] & ~0x80u) | (c[j] >> 4 & 0x80u);
     }
 #pragma unroll
     for (int i = 0; i < 2; ++i)
@@ -183,19 +191,67 @@ __device__ __forceinline__ uint2 codes8(const float (&x)[8], float *scale, const
 }
 
 // Within a unit of the last place, for values whose bits nobody keeps.
+__device__ __forceinline__ float reciprocal(float x) {
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
 __device__ __forceinline__ float root(float x) {
     float y;
     asm("sqrt.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
 
+// A thread's eight elements as they lie in memory.
+template <int BITS>
+struct Chunk {
+    const void *grad;                     // null: there is nothing to do
+    int64_t at;                           // the first one's place in its tensor
+    int tensor, n;
+    bool full;
+    Raw p, g, m, v;
+    uint2 cm, cv;
+    float sm, sv;
+    __device__ __forceinline__ void load(const AdamWStep &s, const AdamWChunk &chunk) {
+        tensor = chunk.tensor;
+        const AdamWTensor &c = s.tensors[tensor];
+        grad = s.grad[tensor - s.tensor0];
+        at = (int64_t)chunk.chunk * ADAMW_CHUNK + threadIdx.x * 8;
+        const int64_t own = c.n - at;
+        n = own < 0 ? 0 : own < 8 ? (int)own : 8;
+        // (the last elements, and tensors that are not aligned to 16 bytes, go one by one)
+        full = n == 8 && c.aligned && ((uintptr_t)grad & 15) == 0;
+        if (!grad) return;
+        p = take(c.param, HWR_F32, at, n, full);
+        g = take(grad, s.dtype[tensor - s.tensor0], at, n, full);
+        if (BITS == 32) {
+            m = take(c.m, HWR_F32, at, n, full);
+            v = take(c.v, HWR_F32, at, n, full);
+        } else {
+            cm = take8(c.m, at, n, full);
+            cv = take8(c.v, at, n, full);
+            sm = n ? c.m_scale[at / ADAMW_BLOCK] : 0.f;
+            sv = n ? c.v_scale[at / ADAMW_BLOCK] : 0.f;
+        }
+    }
+    __device__ __forceinline__ void moments(float (&a)[8], float (&b)[8]) const {
+        if (BITS == 32) {
+            widen(m, HWR_F32, a);
+            widen(v, HWR_F32, b);
+        } else {
+            values8(cm, sm, a);
+            values8(cv, sv, b);
+        }
+    }
+};
+
 template <int BITS>
 __global__ void __launch_bounds__(AW_THREADS)
 k_adamw(const __grid_constant__ AdamWStep p) {
     const int tid = threadIdx.x, lane = tid & 31;
     // (the tables were there before the call)
-    AdamWChunk next = {p.tensor0, 0};
-    if ((int)blockIdx.x < p.chunks) next = p.table[blockIdx.x];
+    AdamWChunk first = {p.tensor0, 0};
+    if ((int)blockIdx.x < p.chunks) first = p.table[blockIdx.x];
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int32_t t = *p.step + 1;
@@ -209,42 +265,24 @@ k_adamw(const __grid_constant__ AdamWStep p) {
     const float c1 = -expm1f((float)t * p.log_b1), c2 = -expm1f((float)t * p.log_b2);
     const float by1 = 1.f / c1, by2 = rsqrtf(c2);
     const uint32_t key_t = mixed((uint32_t)t + p.seed * 0x9e3779b1u);
-    if (!skip)
-        for (int i = blockIdx.x; i < p.chunks; i += gridDim.x) {
-            const AdamWChunk now = next;
-            if (i + gridDim.x < p.chunks) next = p.table[i + gridDim.x];
-            const AdamWTensor c = p.tensors[now.tensor];
-            const void *grad = p.grad[now.tensor - p.tensor0];
-            if (!grad) continue;
-            const int gt = p.dtype[now.tensor - p.tensor0];
-            const int64_t at = (int64_t)now.chunk * ADAMW_CHUNK + tid * 8, own = c.n - at;
-            const int n = own < 0 ? 0 : own < 8 ? (int)own : 8;
-            // (the last elements, and tensors that are not aligned to 16 bytes, go one by one)
-            const bool full = n == 8 && c.aligned && ((uintptr_t)grad & 15) == 0;
-            const Raw rp = take(c.param, HWR_F32, at, n, full), rg = take(grad, gt, at, n, full);
-            Raw rm, rv;
-            uint2 cm, cv;
-            float sm, sv;
-            const int64_t block = at / ADAMW_BLOCK;
-            if (BITS == 32) {
-                rm = take(c.m, HWR_F32, at, n, full);
-                rv = take(c.v, HWR_F32, at, n, full);
-            } else {
-                cm = take8(c.m, at, n, full);
-                cv = take8(c.v, at, n, full);
-                sm = n ? c.m_scale[block] : 0.f;
-                sv = n ? c.v_scale[block] : 0.f;
-            }
+    Chunk<BITS> now;
+    int i = blockIdx.x;
+    if (!skip && i < p.chunks) now.load(p, first);
+    for (; !skip && i < p.chunks; i += gridDim.x) {
+        // 8 bits: the next chunk's loads are under way while this one's codes are made
+        Chunk<BITS> next;
+        const bool more = i + gridDim.x < p.chunks;
+        if (more) first = p.table[i + gridDim.x];
+        if (BITS == 8 && more) next.load(p, first);
+        if (now.grad) {
+            const AdamWTensor &c = p.tensors[now.tensor];
+            const int n = now.n;
+            const bool full = now.full;
+            const int64_t at = now.at, block = at / ADAMW_BLOCK;
             float w[8], g[8], m[8], v[8];
-            widen(rp, HWR_F32, w);
-            widen(rg, gt, g);
-            if (BITS == 32) {
-                widen(rm, HWR_F32, m);
-                widen(rv, HWR_F32, v);
-            } else {
-                values8(cm, sm, m);
-                values8(cv, sv, v);
-            }
+            widen(now.p, HWR_F32, w);
+            widen(now.g, p.dtype[now.tensor - p.tensor0], g);
+            now.moments(m, v);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const float f = __fmul_rn(g[j], k), old = BITS == 32 ? v[j] : __fmul_rn(v[j], v[j]);
@@ -259,7 +297,7 @@ k_adamw(const __grid_constant__ AdamWStep p) {
             for (int j = 0; j < 8; ++j) v[j] = BITS == 8 ? __fsqrt_rn(v[j]) : root(v[j]);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const float step = __fdividef(m[j] * by1, fmaf(v[j], by2, p.eps));
+                const float step = m[j] * by1 * reciprocal(fmaf(v[j], by2, p.eps));
                 w[j] = fmaf(-rate, fmaf(p.decay, w[j], step), w[j]);
             }
             put32(c.param + at, w, n, full);
@@ -273,14 +311,18 @@ k_adamw(const __grid_constant__ AdamWStep p) {
                 const uint32_t key = at >> 32 ? mixed(tensor ^ (uint32_t)(at >> 32)) : tensor;
                 uint32_t random[8];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    random[j] = mixed((uint32_t)(at + j) * 0x9e3779b1u + key);
-                    if (j >= n) m[j] = v[j] = 0.f;
-                }
+                for (int j = 0; j < 8; ++j) random[j] = mixed((uint32_t)(at + j) * 0x9e3779b1u + key);
+                if (n < 8)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        if (j >= n) m[j] = v[j] = 0.f;
                 put8(c.m, at, codes8<false>(m, c.m_scale + block, random, lane == 0 && n), n, full);
                 put8(c.v, at, codes8<true>(v, c.v_scale + block, random, lane == 0 && n), n, full);
             }
         }
+        if (BITS == 8) now = next;
+        else if (more) now.load(p, first);
+    }
     // the last block of the call to have read the step's number counts it up
     if (tid == 0 && atomicAdd(p.arrivals, 1u) == p.blocks - 1) {
         *p.arrivals = 0;
