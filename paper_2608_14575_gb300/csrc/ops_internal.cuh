@@ -318,7 +318,7 @@ struct AdamWStep {
     const void *grad[ADAMW_TABLE];    // null: the tensor is left as it is
     uint8_t dtype[ADAMW_TABLE];
 };
-int adamw_grid(int chunks, int nsm);
+int adamw_grid(int chunks, int bits, int nsm);
 cudaError_t launch_adamw(const AdamWStep &p, int bits, int grid, cudaStream_t s);
 
 // ---- a layer of experts for a few rows (k_experts.cu) ---------------------------

@@ -311,7 +311,7 @@ extern "C" hwr_status hwr_adamw_step(hwr_ops *c, const hwr_adamw *o, const hwr_a
     p.blocks = 0;
     for (int k = 0; k < launches || k == 0; ++k) {
         const int t0 = k * ADAMW_TABLE, t1 = o->n < t0 + ADAMW_TABLE ? o->n : t0 + ADAMW_TABLE;
-        p.blocks += adamw_grid(o->chunk0[t1] - o->chunk0[t0], c->nsm);
+        p.blocks += adamw_grid(o->chunk0[t1] - o->chunk0[t0], o->bits, c->nsm);
     }
     for (int k = 0; k < launches || k == 0; ++k) {
         const int t0 = k * ADAMW_TABLE, t1 = o->n < t0 + ADAMW_TABLE ? o->n : t0 + ADAMW_TABLE;
@@ -323,7 +323,7 @@ extern "C" hwr_status hwr_adamw_step(hwr_ops *c, const hwr_adamw *o, const hwr_a
             p.grad[i - t0] = grads[i];
             p.dtype[i - t0] = (uint8_t)dtypes[i];
         }
-        CK(c, launch_adamw(p, o->bits, adamw_grid(p.chunks, c->nsm), c->stream), "optimizer kernel");
+        CK(c, launch_adamw(p, o->bits, adamw_grid(p.chunks, o->bits, c->nsm), c->stream), "optimizer kernel");
     }
     return HWR_OK;
 }
