@@ -46,7 +46,7 @@
  *       hwr_clip_gradients  8 bytes for each 1,024 of the gradients' bytes and 32
  *                      for each gradient
  *     (weights that are read in place are the terms with n_out (n_in + 8) less),
- *       hwr_expert_layer  1,024 + 8 rows top (hidden + 7 + 8 n_out)
+ *       hwr_expert_layer  4,096 + 8 rows top (hidden + 9 + 8 n_out)
  *       hwr_token_logprobs  2,176 for each of the device's SMs
  *     and the other calls none.
  *   - Stream capture: calls can be captured into graphs.  A call that would have

@@ -44,15 +44,14 @@ constexpr int EX_TEAM = 8, EX_MMA = 2 * EX_TEAM, EX_COPY = 2, EX_ADD = 2;      /
 constexpr int EX_WARPS = EX_MMA + EX_COPY + EX_ADD, EX_THREADS = EX_WARPS * 32;
 constexpr int EX_SUMS = 2;                 // units whose sums are under way
 constexpr int EX_STRIDE = EX_TEAM * 32;    // columns of a step that a team takes at a time
+constexpr int EX_PAIRS = EXPERTS_MAX_ROWS * EXPERTS_MAX_TOP;
 constexpr int EX_JOB = 8;                  // pairs of a job
 constexpr int EX_DEPTH = 8;                // steps of the ring, at most
-constexpr int EX_SMEM = 208 * 1024;        // (a block also has some of its own)
 constexpr int EX_UNIT_COST = 128;          // of a unit, in columns of its weights
 constexpr int EX_COLS = 1024;              // columns of a step, at most (of the second product: half, in fp16 a quarter)
 constexpr int SUM_THREADS = 128;
-// Shared memory of the tables and the ring, where it holds two steps: the rest is the L1
-// that keeps x and h (64 rows over 64 experts of 1,024 x 4,096 in bf16: 260 us with 110 KB,
-// 232 with 140, 288 with 206).
+// Shared memory of the tables and the ring: the rest is the L1 that keeps x and h (64 rows
+// over 64 experts of 1,024 x 4,096 in bf16: 260 us with 110 KB, 232 with 140, 288 with 206).
 constexpr int EX_RING = 140 * 1024;
 constexpr int EX_GROUPS = OPS_MAX_GROUPS, EX_EACH = (EX_GROUPS + EX_THREADS - 1) / EX_THREADS;      // groups a thread
 constexpr uint32_t ALL = 0xffffffffu;
@@ -62,19 +61,19 @@ __device__ __forceinline__ void mma16(float (&c)[4], uint32_t a0, uint32_t a1, u
                                       uint32_t b1) {
     if (F16)
         asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                     : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-                     : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+            : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+            : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
     else
         asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                     : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-                     : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+            : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+            : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
 __device__ __forceinline__ void mma8_tf32(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
                                           uint32_t b1) {
     asm("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
 // The first n of eight 16-bit elements, zeros after them.
@@ -166,7 +165,7 @@ __device__ __forceinline__ uint4 weights(const char *at, int row, int q, bool se
     return taken<W == W_ROWS>(at + (row + (second ? 8 : 0)) * (cols * 2 + 16) + (k + q * 8) * 2, s);
 }
 
-// A block's ring: `depth` steps of 16 rows of weights and some of x or h.
+// A block's ring: `depth` steps of 16 rows of weights.
 struct Ring {
     char *base;
     uint64_t *full, *empty;               // [depth]
@@ -398,8 +397,8 @@ __device__ __forceinline__ void deal(const Routing &r, int pairs, int E) {
         a += n[k];
     }
     // Within a job pairs may lie in any order (a pair's results do not depend on its column
-    // of the MMA); where an expert has several, they lie in their own order, so that every
-    // block deals them out alike.
+    // of the MMA); where an expert has several jobs, they lie in their own order, so that
+    // every block deals them out alike.
     several = __syncthreads_or(several);
     for (int i = tid; i < pairs; i += EX_THREADS) {
         const int e = r.choice[i];
@@ -419,6 +418,8 @@ __device__ __forceinline__ void deal(const Routing &r, int pairs, int E) {
     }
 }
 
+// The tables, of every block; block 0 leaves them in memory.  (Made in each launch instead
+// of read there: one token 24.7 us for 20.8.)
 __device__ __forceinline__ void route(const Experts &p, Routing &r, char *smem) {
     const int tid = threadIdx.x, pairs = p.rows * p.top, E = p.groups;
     if (pairs > 32)
@@ -953,16 +954,17 @@ int even_columns(int width, int most) {
     return ((width + steps - 1) / steps + 63) & ~63;
 }
 
-int step_bytes(int cols) { return 16 * (cols * 2 + 16); }
+constexpr int step_bytes(int cols) { return (16 * (cols * 2 + 16) + 1023) & ~1023; }
+static_assert(2 * step_bytes(EX_COLS) + 16 + EX_PAIRS * 13 + 16 + EX_GROUPS * 4 + 1023 <= EX_RING, "tables and two steps");
 
 cudaError_t launch(Kernel kernel, Experts p, const CUtensorMap &map, int cols, int nsm, cudaStream_t s) {
     p.cols = cols;
-    p.step = (step_bytes(cols) + 1023) & ~1023;
+    p.step = step_bytes(cols);
     p.ring_at = (int)routing_bytes(p);
     // (an even number of slots, each of which belongs to one team: another team's use of it,
     // one phase of its barriers later, could not be told from the one before)
     const int depth = (EX_RING - p.ring_at) / p.step & ~1;
-    p.depth = depth < 2 ? 2 : depth > EX_DEPTH ? EX_DEPTH : depth;
+    p.depth = depth > EX_DEPTH ? EX_DEPTH : depth;
     cudaLaunchAttribute at[1];
     const cudaLaunchConfig_t cfg = early(dim3((unsigned)nsm), EX_THREADS, (size_t)p.ring_at + p.depth * p.step, s, at);
     return cudaLaunchKernelEx(&cfg, kernel, p, map);
@@ -1017,7 +1019,7 @@ template <bool F16>
 static cudaError_t prepare() {
     cudaError_t e = cudaSuccess;
     const auto set = [&](Kernel kernel) {
-        if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, EX_SMEM);
+        if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, EX_RING);
     };
     set(k_experts_in<F16, W_BOXES, true>);
     set(k_experts_in<F16, W_BOXES, false>);

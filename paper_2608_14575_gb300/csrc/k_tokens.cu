@@ -26,10 +26,10 @@ namespace {
 constexpr int TK_THREADS = 256, TK_WARPS = TK_THREADS / 32;
 constexpr int TK_VECS = 4;             // 16-byte loads of a step
 // Blocks of rows alone are smaller, so that more of them are at different stages of a row:
-// 4,099 rows of 50,001 bf16 logits 77 us with 256 threads, 69 with 128; 2,048 in fp32 68 and
-// 71, and 61 where a step is loaded ahead (bf16 71, fp16 67 for 68: not done).  Alternatives
-// want few blocks, each of which finds a bound of its own: 64 rows of 131,072 with 20 take
-// 18 us with 256 threads, 24 with 128.
+// 4,099 rows of 50,001 bf16 logits 77 us with 256 threads, 70 with 128 (5.9 TB/s); 2,048 in
+// fp32 68 and 71, and 62 (6.6 TB/s) where a step is loaded ahead (bf16 71 so, fp16 67 for 68:
+// not done).  Alternatives want few blocks, each of which finds a bound of its own: 64 rows
+// of 131,072 with 20 take 18 us with 256 threads, 24 with 128.
 __host__ __device__ constexpr int threads_of(bool top) { return top ? TK_THREADS : 128; }
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr float FAR = -1e30f;
@@ -360,12 +360,12 @@ k_token_rows(const __grid_constant__ TokenRows p) {
         uint64_t *sorted = shared_best.sorted;
         int found = __popc(__ballot_sync(ALL, lane < top && sorted[lane] != 0));
         for (int kind = 0; kind < 2; ++kind)
-            for (int i = 0; found < top && i < p.vocab; i += 32) {
-                const float z = i + lane < p.vocab ? Vec<DT>::load(base, i + lane) : 0.f;
+            for (int64_t i = 0; found < top && i < p.vocab; i += 32) {
+                const float z = i + lane < p.vocab ? Vec<DT>::load(base, (int)(i + lane)) : 0.f;
                 const bool is = i + lane < p.vocab && (kind ? z != z : z == -INFINITY);
                 const uint32_t who = __ballot_sync(ALL, is);
                 const int at = found + __popc(who & ((1u << lane) - 1));
-                if (is && at < top) sorted[at] = (uint64_t)order_of(z) << 32 | (uint32_t)~(i + lane);
+                if (is && at < top) sorted[at] = (uint64_t)order_of(z) << 32 | (uint32_t)~(uint32_t)(i + lane);
                 found += __popc(who);
             }
         __syncwarp();
@@ -425,8 +425,8 @@ k_token_grad(const __grid_constant__ TokenGrad p) {
     }
     // what the vectors leave: before them and after them
     const int left = p.vocab - vecs * N;
-    for (int i = piece * TK_THREADS + tid; i < left; i += p.splits * TK_THREADS) {
-        const int at = i < head ? i : i + vecs * N;
+    for (int64_t i = piece * TK_THREADS + tid; i < left; i += p.splits * TK_THREADS) {
+        const int at = (int)(i < head ? i : i + vecs * N);
         Vec<DT>::store(out, at, grad(Vec<DT>::load(in, at), at));
     }
 }
