@@ -282,3 +282,18 @@ def test_optimizers_go_with_their_context():
         cycle()
     torch.cuda.synchronize()
     assert before - torch.cuda.mem_get_info()[0] < 8 << 20
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_example_runs(bits):
+    """The example trains adapters on answer tokens and decodes through experts."""
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "token_training.py")
+    spec = importlib.util.spec_from_file_location("token_training", path)
+    example = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(example)
+    means, adapters, tokens = example.main(rows=200, width=64, vocab=300, groups=3, rank=4, steps=2, bits=bits, say=lambda *_: None)
+    assert len(means) == 2 and all(math.isfinite(m) and m < 0 for m in means)
+    assert all(a.isfinite().all() for a in adapters) and bool((adapters[1] != 0).any())
+    assert tokens.shape == (4,) and bool((tokens >= 0).all()) and bool((tokens < 300).all())
