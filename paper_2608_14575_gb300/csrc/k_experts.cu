@@ -6,14 +6,14 @@
 //   k_experts_sum   y[t] = sum over j of p[t, j] z[t, j]
 //
 // (the last where a row has several choices, or the second product's contraction is cut).
-// Bound by HBM: of each expert that a row chooses the weights are read once (by up to
-// 8 of its rows at a time, a job; an expert of more rows is read again from L2),
-// everything else stays in L2.  Every block finds the choices and the experts' rows by
+// Bound by HBM: of each expert that a row chooses the weights are read once (by up to 8
+// of its rows at a time, a job, or 16 where experts have many; an expert of more rows is
+// read again from L2), everything else stays in L2.  Every block finds the choices and the experts' rows by
 // itself from the scores (a few KB), which costs less than a launch between.  A unit of
 // work is 16 rows of a weight matrix (in the first product 8 gate rows and the 8 up rows
 // that they meet, so that the activation finds both) and a job.  A block walks a run of
 // consecutive units.  Two of its warps copy the weights into a ring in shared memory,
-// some steps of up to 1,024 columns ahead and across the ends of units.  Two teams of eight
+// some steps of up to 512 columns ahead and across the ends of units.  Two teams of eight
 // warps take the steps in turn; a team's warps share a step's columns, 32 at a time, and
 // load their part of the job's rows of x (or h) from L2 a step ahead.  Two more warps add
 // up the teams' sums of a unit, in a fixed order, and write its results.  (A unit a warp,
@@ -45,10 +45,11 @@ constexpr int EX_WARPS = EX_MMA + EX_COPY + EX_ADD, EX_THREADS = EX_WARPS * 32;
 constexpr int EX_SUMS = 2;                 // units whose sums are under way
 constexpr int EX_STRIDE = EX_TEAM * 32;    // columns of a step that a team takes at a time
 constexpr int EX_PAIRS = EXPERTS_MAX_ROWS * EXPERTS_MAX_TOP;
-constexpr int EX_JOB = 8;                  // pairs of a job
 constexpr int EX_DEPTH = 8;                // steps of the ring, at most
 constexpr int EX_UNIT_COST = 128;          // of a unit, in columns of its weights
-constexpr int EX_COLS = 1024;              // columns of a step, at most (of the second product: half, in fp16 a quarter)
+// Columns of a step, at most (of the second product in fp16: half).  One row of 4,096 ->
+// 2 x 8,192 over 2 of 8 experts: 76 us with 1,024, 73 with 512.
+constexpr int EX_COLS = 512;
 constexpr int SUM_THREADS = 128;
 // Shared memory of the tables and the ring: the rest is the L1 that keeps x and h (64 rows
 // over 64 experts of 1,024 x 4,096 in bf16: 260 us with 110 KB, 232 with 140, 288 with 206).
@@ -222,7 +223,7 @@ struct Ring {
 // ---- routing --------------------------------------------------------------------
 
 // Which rows meet which expert: pairs (row t, choice j) at t * top + j, the pairs of an
-// expert side by side in `list`, in jobs of at most 8 of them.  The first product's blocks
+// expert side by side in `list`, in jobs of at most 8 or 16 of them.  The first product's blocks
 // each make the tables, and one of them leaves them in memory for the launches after it.
 struct Routing {
     int *jobs;
@@ -321,6 +322,7 @@ __device__ __forceinline__ void choose_all(const Experts &p, Routing &r) {
 }
 
 // Up to 32 pairs, by one warp: a stable sort by expert.
+template <int JOB>
 __device__ __forceinline__ void deal_few(const Routing &r, int pairs) {
     const int lane = threadIdx.x & 31;
     const int mine = lane < pairs ? r.choice[lane] : -1;
@@ -331,7 +333,7 @@ __device__ __forceinline__ void deal_few(const Routing &r, int pairs) {
         rank += before;
         place += before || (c >= 0 && c < mine);
     }
-    const bool lead = mine >= 0 && rank % EX_JOB == 0;
+    const bool lead = mine >= 0 && rank % JOB == 0;
     const uint32_t same = __match_any_sync(ALL, mine);
     int job = 0;
     for (int i = 0; i < pairs; ++i) {
@@ -343,13 +345,14 @@ __device__ __forceinline__ void deal_few(const Routing &r, int pairs) {
         const int left = __popc(same) - rank;
         r.expert[job] = (uint16_t)mine;
         r.begin[job] = (uint16_t)place;
-        r.n[job] = (uint8_t)(left < EX_JOB ? left : EX_JOB);
+        r.n[job] = (uint8_t)(left < JOB ? left : JOB);
     }
     const uint32_t leads = __ballot_sync(ALL, lead);
     if (lane == 0) *r.jobs = __popc(leads);
 }
 
 // Any number, by the block.
+template <int JOB>
 __device__ __forceinline__ void deal(const Routing &r, int pairs, int E) {
     __shared__ int warp_jobs[EX_WARPS], warp_pairs[EX_WARPS];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -362,8 +365,8 @@ __device__ __forceinline__ void deal(const Routing &r, int pairs, int E) {
 #pragma unroll
     for (int k = 0; k < EX_EACH; ++k) {
         n[k] = tid * EX_EACH + k < E ? r.count[tid * EX_EACH + k] : 0;
-        several |= n[k] > EX_JOB;
-        jobs += (n[k] + EX_JOB - 1) / EX_JOB;
+        several |= n[k] > JOB;
+        jobs += (n[k] + JOB - 1) / JOB;
         all += n[k];
     }
     int j = jobs, a = all;
@@ -389,10 +392,10 @@ __device__ __forceinline__ void deal(const Routing &r, int pairs, int E) {
 #pragma unroll
     for (int k = 0; k < EX_EACH; ++k) {
         if (n[k]) r.count[tid * EX_EACH + k] = a;
-        for (int b = 0; b < n[k]; b += EX_JOB, ++j) {
+        for (int b = 0; b < n[k]; b += JOB, ++j) {
             r.expert[j] = (uint16_t)(tid * EX_EACH + k);
             r.begin[j] = (uint16_t)(a + b);
-            r.n[j] = (uint8_t)(n[k] - b < EX_JOB ? n[k] - b : EX_JOB);
+            r.n[j] = (uint8_t)(n[k] - b < JOB ? n[k] - b : JOB);
         }
         a += n[k];
     }
@@ -420,6 +423,7 @@ __device__ __forceinline__ void deal(const Routing &r, int pairs, int E) {
 
 // The tables, of every block; block 0 leaves them in memory.  (Made in each launch instead
 // of read there: one token 24.7 us for 20.8.)
+template <int JOB>
 __device__ __forceinline__ void route(const Experts &p, Routing &r, char *smem) {
     const int tid = threadIdx.x, pairs = p.rows * p.top, E = p.groups;
     if (pairs > 32)
@@ -438,8 +442,8 @@ __device__ __forceinline__ void route(const Experts &p, Routing &r, char *smem) 
         choose_all<32>(p, r);
     }
     __syncthreads();
-    if (pairs > 32) deal(r, pairs, E);
-    else if (tid < 32) deal_few(r, pairs);
+    if (pairs > 32) deal<JOB>(r, pairs, E);
+    else if (tid < 32) deal_few<JOB>(r, pairs);
     __syncthreads();
     if (blockIdx.x == 0)
         for (int i = tid; i < (int)tables_bytes(p) / 4; i += EX_THREADS) ((uint32_t *)p.tables)[i] = ((const uint32_t *)smem)[i];
@@ -506,13 +510,15 @@ __device__ __forceinline__ void tf32_terms(float v, float &high, float &low) {
 }
 
 // What the block shares beside the routing's tables and the ring.
+template <int NB>
 struct Shared {
-    float4 sums[EX_SUMS][EX_MMA][32];
+    float4 sums[EX_SUMS][EX_MMA][NB][32];
     uint64_t full[EX_DEPTH], empty[EX_DEPTH], added[EX_SUMS], taken[EX_SUMS];
     int abort_flag;
 };
 
-__device__ __forceinline__ Ring ring_of(const Experts &p, char *smem, Shared &sh) {
+template <int NB>
+__device__ __forceinline__ Ring ring_of(const Experts &p, char *smem, Shared<NB> &sh) {
     Ring r;
     r.depth = p.depth;
     r.step = p.step;
@@ -525,7 +531,8 @@ __device__ __forceinline__ Ring ring_of(const Experts &p, char *smem, Shared &sh
     return r;
 }
 // (before the routing's barriers; both: teams take part in a unit)
-__device__ __forceinline__ void init(Shared &sh, bool both) {
+template <int NB>
+__device__ __forceinline__ void init(Shared<NB> &sh, bool both) {
     if (threadIdx.x < EX_DEPTH) {
         mbar_init(sh.full + threadIdx.x, 2);
         mbar_init(sh.empty + threadIdx.x, EX_TEAM);
@@ -539,46 +546,55 @@ __device__ __forceinline__ void init(Shared &sh, bool both) {
 }
 
 // A warp's sums of a unit (the turn-th of the block's) go to the warps that add up ...
-__device__ __forceinline__ void give(Shared &sh, float (&c)[2][4], int turn, int place, bool &ok, int32_t *status) {
+template <int NB>
+__device__ __forceinline__ void give(Shared<NB> &sh, float (&c)[NB][2][4], int turn, int place, bool &ok, int32_t *status) {
     const int b = turn % EX_SUMS, lane = threadIdx.x & 31;
     ok = ok && mbar_wait(sh.taken + b, (turn / EX_SUMS & 1) ^ 1, &sh.abort_flag, status);
-    sh.sums[b][place][lane] = make_float4(c[0][0] + c[1][0], c[0][1] + c[1][1], c[0][2] + c[1][2], c[0][3] + c[1][3]);
+#pragma unroll
+    for (int j = 0; j < NB; ++j)
+        sh.sums[b][place][j][lane] = make_float4(c[j][0][0] + c[j][1][0], c[j][0][1] + c[j][1][1],
+                                                 c[j][0][2] + c[j][1][2], c[j][0][3] + c[j][1][3]);
     __syncwarp();
     if (lane == 0) mbar_arrive(sh.added + b);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) c[i / 4][i % 4] = 0.f;
+    for (int i = 0; i < NB * 8; ++i) c[i / 8][i / 4 % 2][i % 4] = 0.f;
 }
 // ... which take them in the warps' order (from one team, where units have one step, or both).
-__device__ __forceinline__ bool take(Shared &sh, float (&c)[4], int turn, bool both, int32_t *status) {
+template <int NB>
+__device__ __forceinline__ bool take(Shared<NB> &sh, float (&c)[NB][4], int turn, bool both, int32_t *status) {
     const int b = turn % EX_SUMS, lane = threadIdx.x & 31;
     if (!mbar_wait(sh.added + b, turn / EX_SUMS & 1, &sh.abort_flag, status)) return false;
-    float4 v = sh.sums[b][0][lane];
 #pragma unroll
-    for (int w = 1; w < EX_MMA; ++w) {
-        if (w == EX_TEAM && !both) break;
-        const float4 o = sh.sums[b][w][lane];
-        v.x += o.x;
-        v.y += o.y;
-        v.z += o.z;
-        v.w += o.w;
+    for (int j = 0; j < NB; ++j) {
+        float4 v = sh.sums[b][0][j][lane];
+#pragma unroll
+        for (int w = 1; w < EX_MMA; ++w) {
+            if (w == EX_TEAM && !both) break;
+            const float4 o = sh.sums[b][w][j][lane];
+            v.x += o.x;
+            v.y += o.y;
+            v.z += o.z;
+            v.w += o.w;
+        }
+        c[j][0] = v.x;
+        c[j][1] = v.y;
+        c[j][2] = v.z;
+        c[j][3] = v.w;
     }
     __syncwarp();
     if (lane == 0) mbar_arrive(sh.taken + b);
-    c[0] = v.x;
-    c[1] = v.y;
-    c[2] = v.z;
-    c[3] = v.w;
     return true;
 }
 
 // ---- the first product --------------------------------------------------------------
 
-template <bool F16, int W, bool X_ALIGNED>
+template <bool F16, int W, bool X_ALIGNED, int NB>
 __global__ void __launch_bounds__(EX_THREADS)
 k_experts_in(const __grid_constant__ Experts p, const __grid_constant__ CUtensorMap map) {
     extern __shared__ __align__(1024) char smem[];
-    __shared__ Shared sh;
+    __shared__ Shared<NB> sh;
     constexpr int CH = EX_COLS / EX_STRIDE, XU = X_ALIGNED ? 1 : 2;
+    constexpr bool TWICE = NB == 1 && W != W_ANY && X_ALIGNED;      // registers for two steps of x
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g8 = lane >> 2, q = lane & 3, wr = row_of(g8);
     const int cols = p.cols, steps = (p.n_in + cols - 1) / cols;
     const bool both = steps > 1;
@@ -586,7 +602,7 @@ k_experts_in(const __grid_constant__ Experts p, const __grid_constant__ CUtensor
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     Routing r(p, smem);
-    route(p, r, smem);
+    route<NB * 8>(p, r, smem);
     Ring ring = ring_of(p, smem, sh);
     const int wide = p.gated ? 8 : 16;
     Walk w(*r.jobs, 1, (p.hidden + wide - 1) / wide);
@@ -616,15 +632,15 @@ k_experts_in(const __grid_constant__ Experts p, const __grid_constant__ CUtensor
             const int turn = w.u - u0;
             if (turn % EX_ADD != warp - EX_MMA - EX_COPY) continue;
             const int n = r.n[w.job], begin = r.begin[w.job];
-            float c[4];
+            float c[NB][4];
             if (!take(sh, c, turn, both, p.status)) return;
             // rows wr and wr + 8 of columns 2 q and 2 q + 1
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int column = 2 * q + (i & 1), f = w.tile * wide + wr + (i & 2) * 4;
+            for (int k = 0; k < NB * 4; ++k) {
+                const int i = k % 4, column = k / 4 * 8 + 2 * q + (i & 1), f = w.tile * wide + wr + (i & 2) * 4;
                 if (column >= n || (p.gated && (i & 2)) || f >= p.hidden) continue;
-                float v = activated(c[i], p.act);
-                if (p.gated) v *= c[i | 2];
+                float v = activated(c[k / 4][i], p.act);
+                if (p.gated) v *= c[k / 4][i | 2];
                 const int64_t to = (int64_t)r.list[begin + column] * 2 * p.h_ld + f;
                 if (F16) {
                     float *h = (float *)p.h + to;
@@ -639,17 +655,26 @@ k_experts_in(const __grid_constant__ Experts p, const __grid_constant__ CUtensor
         return;
     }
     const int team = warp / EX_TEAM, member = warp % EX_TEAM;
-    // my columns of x: the job's row g8
-    const uint16_t *row = nullptr;
-    int row_job = -1;
-    const auto fetch = [&](uint4(&v)[CH][XU], const Steps &at) {
+    // My part of x: of the job's rows g8 (and g8 + 8).  It is loaded a step ahead; where that
+    // would not fit the registers, after the step before it (the other team's step is between:
+    // 7 unaligned rows 30.1 us for 27.3 so), unless it is the same again.
+    const uint16_t *row[NB] = {};
+    int row_job = -1, row_step = -1, n = 0;
+    const auto fetch = [&](uint4(&x)[CH][NB][XU], const Steps &at) {
+        if (!TWICE && at.w.job == row_job && at.s == row_step) return;
+        row_step = at.s;
         if (at.w.job != row_job) {
             row_job = at.w.job;
-            row = g8 < r.n[row_job] ? p.x + r.list[r.begin[row_job] + g8] / p.top * p.x_ld : nullptr;
+            n = r.n[row_job];
+#pragma unroll
+            for (int j = 0; j < NB; ++j)
+                row[j] = g8 + j * 8 < n ? p.x + r.list[r.begin[row_job] + g8 + j * 8] / p.top * p.x_ld : nullptr;
         }
         const int to = min((at.s + 1) * cols, p.n_in);
 #pragma unroll
-        for (int i = 0; i < CH; ++i) eight<X_ALIGNED>(v[i], row, at.s * cols + member * 32 + i * EX_STRIDE + q * 8, to);
+        for (int i = 0; i < CH; ++i)
+#pragma unroll
+            for (int j = 0; j < NB; ++j) eight<X_ALIGNED>(x[i][j], row[j], at.s * cols + member * 32 + i * EX_STRIDE + q * 8, to);
     };
     Steps ahead(w, steps, steps);         // the next step of this team, whose x is under way
     if (team) {
@@ -657,18 +682,20 @@ k_experts_in(const __grid_constant__ Experts p, const __grid_constant__ CUtensor
         ring.next();
     }
     int given = u0;
-    float c[2][4] = {};
+    float c[NB][2][4] = {};
     const auto give_up_to = [&](int u) {
         for (; given < u; ++given) give(sh, c, given - u0, warp, ring.ok, p.status);
     };
     if (both) give_up_to(min(ahead.w.u, w.end));
     if (!ahead.more()) return;
-    const auto take_step = [&](uint4(&now)[CH][XU], uint4(&next)[CH][XU]) {
+    const auto take_step = [&](uint4(&x)[CH][NB][XU], uint4(&next)[CH][NB][XU]) {
         const Steps at = ahead;
-        const int sx = X_ALIGNED ? 0 : (int)((uintptr_t)row & 15);
+        int sx[NB];
+#pragma unroll
+        for (int j = 0; j < NB; ++j) sx[j] = (int)((uintptr_t)row[j] & 15);
         ahead.next();
         if (ahead.more()) ahead.next();
-        if (ahead.more()) fetch(next, ahead);
+        if (TWICE && ahead.more()) fetch(next, ahead);
         int sa = 0, sb = 0;
         if (W == W_ANY) {
             sa = (int)((uintptr_t)weights_row(at.w, wr) & 15);
@@ -693,21 +720,33 @@ k_experts_in(const __grid_constant__ Experts p, const __grid_constant__ CUtensor
             }
         }
 #pragma unroll
-        for (int i = 0; i < CH; ++i) {
-            const int k = member * 32 + i * EX_STRIDE;
-            uint4 v = X_ALIGNED ? now[i][0] : shifted(now[i][0], now[i][XU - 1], sx);
-            if (W != W_BOXES && k + 32 > left) v = first(v, max(0, min(8, left - k - q * 8)));
-            mma16<F16>(c[0], a[i].x, d[i].x, a[i].y, d[i].y, v.x, v.y);
-            mma16<F16>(c[1], a[i].z, d[i].z, a[i].w, d[i].w, v.z, v.w);
+        for (int j = 0; j < NB; ++j) {
+            if (j && n <= j * 8) break;
+#pragma unroll
+            for (int i = 0; i < CH; ++i) {
+                const int k = member * 32 + i * EX_STRIDE;
+                uint4 v = X_ALIGNED ? x[i][j][0] : shifted(x[i][j][0], x[i][j][XU - 1], sx[j]);
+                if (W != W_BOXES && k + 32 > left) v = first(v, max(0, min(8, left - k - q * 8)));
+                mma16<F16>(c[j][0], a[i].x, d[i].x, a[i].y, d[i].y, v.x, v.y);
+                mma16<F16>(c[j][1], a[i].z, d[i].z, a[i].w, d[i].w, v.z, v.w);
+            }
         }
         ring.release();
+        if (!TWICE && ahead.more()) fetch(next, ahead);
         if (both) give_up_to(min(ahead.w.u, w.end));
         else give(sh, c, at.w.u - u0, member, ring.ok, p.status);
         return ahead.more();
     };
-    uint4 one[CH][XU], two[CH][XU];
-    fetch(one, ahead);
-    while (take_step(one, two) && take_step(two, one)) {
+    if constexpr (TWICE) {
+        uint4 one[CH][NB][XU], two[CH][NB][XU];
+        fetch(one, ahead);
+        while (take_step(one, two) && take_step(two, one)) {
+        }
+    } else {
+        uint4 x[CH][NB][XU];
+        fetch(x, ahead);
+        while (take_step(x, x)) {
+        }
     }
 }
 
@@ -725,13 +764,14 @@ __device__ __forceinline__ uint4 widened(uint32_t lo, uint32_t hi) {
     return make_uint4(__float_as_uint(a.x), __float_as_uint(a.y), __float_as_uint(b.x), __float_as_uint(b.y));
 }
 
-template <bool F16, int W>
+template <bool F16, int W, int NB>
 __global__ void __launch_bounds__(EX_THREADS)
 k_experts_out(const __grid_constant__ Experts p, const __grid_constant__ CUtensorMap map) {
     extern __shared__ __align__(1024) char smem[];
-    __shared__ Shared sh;
+    __shared__ Shared<NB> sh;
     // 32 columns of h a lane: high and low terms, in 16-byte loads
-    constexpr int CH = EX_COLS / (F16 ? 4 : 2) / EX_STRIDE, TERM = F16 ? 2 : 1;
+    constexpr int CH = EX_COLS / (F16 ? 2 : 1) / EX_STRIDE, TERM = F16 ? 2 : 1;
+    constexpr bool TWICE = NB == 1 && W != W_ANY;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g8 = lane >> 2, q = lane & 3, wr = row_of(g8);
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     init(sh, true);
@@ -750,6 +790,11 @@ k_experts_out(const __grid_constant__ Experts p, const __grid_constant__ CUtenso
             splits = s;
         }
     }
+    // Beside several columns of h, pieces of two steps, one a team, whose h stays in the
+    // registers from tile to tile (64 rows, 4 of 16 experts each, 1,024 -> 2 x 2,048, bf16:
+    // 86.7 us without, 80.9 with; in fp16, whose steps are half as wide, 90.7 and 93.5).
+    if (NB > 1 && !F16)
+        while (splits < p.splits && splits * 2 < all_steps) splits *= 2;
     const int per = (all_steps + splits - 1) / splits;       // steps of a piece, and pieces with any
     splits = (all_steps + per - 1) / per;
     // one choice a row, taken whole: its result is the row's, and rows without one get zeros
@@ -785,15 +830,15 @@ k_experts_out(const __grid_constant__ Experts p, const __grid_constant__ CUtenso
             const int turn = w.u - u0;
             if (turn % EX_ADD != warp - EX_MMA - EX_COPY) continue;
             const int n = r.n[w.job], begin = r.begin[w.job];
-            float c[4];
+            float c[NB][4];
             if (!take(sh, c, turn, true, p.status)) return;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int column = 2 * q + (i & 1), o = w.tile * 16 + wr + (i & 2) * 4;
+            for (int k = 0; k < NB * 4; ++k) {
+                const int i = k % 4, column = k / 4 * 8 + 2 * q + (i & 1), o = w.tile * 16 + wr + (i & 2) * 4;
                 if (column >= n || o >= p.n_out) continue;
                 const int pair = r.list[begin + column];
-                if (whole) store<F16>(p, pair, o, r.gate[pair] * c[i]);
-                else p.part[((int64_t)pair * splits + w.split) * p.n_out + o] = c[i];
+                if (whole) store<F16>(p, pair, o, r.gate[pair] * c[k / 4][i]);
+                else p.part[((int64_t)pair * splits + w.split) * p.n_out + o] = c[k / 4][i];
             }
             __syncwarp();
         }
@@ -801,24 +846,34 @@ k_experts_out(const __grid_constant__ Experts p, const __grid_constant__ CUtenso
     }
     const int team = warp / EX_TEAM, member = warp % EX_TEAM;
     const int64_t low = p.h_ld * (F16 ? 4 : 2) / 16;
-    const uint4 *row = nullptr;
-    int row_job = -1;
-    const auto fetch = [&](uint4(&v)[CH][2 * TERM], const Steps &at) {
+    const uint4 *row[NB] = {};
+    int row_job = -1, row_step = -1, n = 0;
+    const auto fetch = [&](uint4(&h)[CH][NB][2 * TERM], const Steps &at) {
+        if (!TWICE && at.w.job == row_job && at.s == row_step) return;
+        row_step = at.s;
         if (at.w.job != row_job) {
             row_job = at.w.job;
-            row = nullptr;
-            if (g8 < r.n[row_job])
-                row = (const uint4 *)((const char *)p.h + (int64_t)r.list[r.begin[row_job] + g8] * 2 * p.h_ld * (F16 ? 4 : 2));
+            n = r.n[row_job];
+#pragma unroll
+            for (int b = 0; b < NB; ++b) {
+                row[b] = nullptr;
+                if (g8 + b * 8 < n)
+                    row[b] = (const uint4 *)((const char *)p.h +
+                                             (int64_t)r.list[r.begin[row_job] + g8 + b * 8] * 2 * p.h_ld * (F16 ? 4 : 2));
+            }
         }
         const int to = min((at.s + 1) * cols, p.hidden);
 #pragma unroll
         for (int i = 0; i < CH; ++i) {
             const int c = at.s * cols + member * 32 + i * EX_STRIDE + q * 8;
-            const bool in = row && c < to;
 #pragma unroll
-            for (int j = 0; j < 2 * TERM; ++j) {
-                v[i][j] = make_uint4(0, 0, 0, 0);
-                if (in) v[i][j] = row[(j < TERM ? 0 : low) + c / 8 * TERM + j % TERM];
+            for (int b = 0; b < NB; ++b) {
+                const bool in = row[b] && c < to;
+#pragma unroll
+                for (int j = 0; j < 2 * TERM; ++j) {
+                    h[i][b][j] = make_uint4(0, 0, 0, 0);
+                    if (in) h[i][b][j] = row[b][(j < TERM ? 0 : low) + c / 8 * TERM + j % TERM];
+                }
             }
         }
     };
@@ -828,17 +883,17 @@ k_experts_out(const __grid_constant__ Experts p, const __grid_constant__ CUtenso
         ring.next();
     }
     int given = u0;
-    float c[2][4] = {};
+    float c[NB][2][4] = {};
     const auto give_up_to = [&](int u) {
         for (; given < u; ++given) give(sh, c, given - u0, warp, ring.ok, p.status);
     };
     give_up_to(min(ahead.w.u, w.end));
     if (!ahead.more()) return;
-    const auto take_step = [&](uint4(&now)[CH][2 * TERM], uint4(&next)[CH][2 * TERM]) {
+    const auto take_step = [&](uint4(&h)[CH][NB][2 * TERM], uint4(&next)[CH][NB][2 * TERM]) {
         const Steps at = ahead;
         ahead.next();
         if (ahead.more()) ahead.next();
-        if (ahead.more()) fetch(next, ahead);
+        if (TWICE && ahead.more()) fetch(next, ahead);
         int sa = 0, sb = 0;
         if (W == W_ANY) {
             const uint16_t *w = p.w_out + r.expert[at.w.job] * p.w_out_z + (int64_t)(at.w.tile * 16 + wr) * p.w_out_ld;
@@ -866,48 +921,64 @@ k_experts_out(const __grid_constant__ Experts p, const __grid_constant__ CUtenso
 #pragma unroll
         for (int i = 0; i < CH; ++i) {
             const int k = member * 32 + i * EX_STRIDE;
-            if (W != W_BOXES && k + 32 > left) {
-                // (the rows are filled up to whole 16 bytes with anything)
-                const int e = max(0, min(8, left - k - q * 8));
+            uint4 a0, a1, d0, d1;
+            if (F16) {
+                a0 = widened(a[i].x, a[i].y), a1 = widened(a[i].z, a[i].w);
+                d0 = widened(d[i].x, d[i].y), d1 = widened(d[i].z, d[i].w);
+            }
 #pragma unroll
-                for (int j = 0; j < 2 * TERM; ++j) {
-                    if (F16) {
-                        const int f = e - j % TERM * 4;
-                        if (f < 1) now[i][j].x = 0;
-                        if (f < 2) now[i][j].y = 0;
-                        if (f < 3) now[i][j].z = 0;
-                        if (f < 4) now[i][j].w = 0;
-                    } else {
-                        now[i][j] = first(now[i][j], e);
+            for (int b = 0; b < NB; ++b) {
+                if (b && n <= b * 8) break;
+                if (W != W_BOXES && k + 32 > left) {
+                    // (the rows are filled up to whole 16 bytes with anything)
+                    const int e = max(0, min(8, left - k - q * 8));
+#pragma unroll
+                    for (int j = 0; j < 2 * TERM; ++j) {
+                        uint4 &v = h[i][b][j];
+                        if (F16) {
+                            const int f = e - j % TERM * 4;
+                            if (f < 1) v.x = 0;
+                            if (f < 2) v.y = 0;
+                            if (f < 3) v.z = 0;
+                            if (f < 4) v.w = 0;
+                        } else {
+                            v = first(v, e);
+                        }
                     }
                 }
-            }
-            if (F16) {
-                const uint4 a0 = widened(a[i].x, a[i].y), a1 = widened(a[i].z, a[i].w);
-                const uint4 d0 = widened(d[i].x, d[i].y), d1 = widened(d[i].z, d[i].w);
+                if (F16) {
 #pragma unroll
-                for (int j = 0; j < 2 * TERM; j += TERM) {
-                    const uint4 v = now[i][j], w = now[i][j + TERM - 1];
-                    mma8_tf32(c[0], a0.x, d0.x, a0.y, d0.y, v.x, v.y);
-                    mma8_tf32(c[1], a0.z, d0.z, a0.w, d0.w, v.z, v.w);
-                    mma8_tf32(c[0], a1.x, d1.x, a1.y, d1.y, w.x, w.y);
-                    mma8_tf32(c[1], a1.z, d1.z, a1.w, d1.w, w.z, w.w);
-                }
-            } else {
+                    for (int j = 0; j < 2 * TERM; j += TERM) {
+                        const uint4 v = h[i][b][j], w = h[i][b][j + TERM - 1];
+                        mma8_tf32(c[b][0], a0.x, d0.x, a0.y, d0.y, v.x, v.y);
+                        mma8_tf32(c[b][1], a0.z, d0.z, a0.w, d0.w, v.z, v.w);
+                        mma8_tf32(c[b][0], a1.x, d1.x, a1.y, d1.y, w.x, w.y);
+                        mma8_tf32(c[b][1], a1.z, d1.z, a1.w, d1.w, w.z, w.w);
+                    }
+                } else {
 #pragma unroll
-                for (int j = 0; j < 2 * TERM; ++j) {
-                    mma16<false>(c[0], a[i].x, d[i].x, a[i].y, d[i].y, now[i][j].x, now[i][j].y);
-                    mma16<false>(c[1], a[i].z, d[i].z, a[i].w, d[i].w, now[i][j].z, now[i][j].w);
+                    for (int j = 0; j < 2 * TERM; ++j) {
+                        mma16<false>(c[b][0], a[i].x, d[i].x, a[i].y, d[i].y, h[i][b][j].x, h[i][b][j].y);
+                        mma16<false>(c[b][1], a[i].z, d[i].z, a[i].w, d[i].w, h[i][b][j].z, h[i][b][j].w);
+                    }
                 }
             }
         }
         ring.release();
+        if (!TWICE && ahead.more()) fetch(next, ahead);
         give_up_to(min(ahead.w.u, w.end));
         return ahead.more();
     };
-    uint4 one[CH][2 * TERM], two[CH][2 * TERM];
-    fetch(one, ahead);
-    while (take_step(one, two) && take_step(two, one)) {
+    if constexpr (TWICE) {
+        uint4 one[CH][NB][2 * TERM], two[CH][NB][2 * TERM];
+        fetch(one, ahead);
+        while (take_step(one, two) && take_step(two, one)) {
+        }
+    } else {
+        uint4 h[CH][NB][2 * TERM];
+        fetch(h, ahead);
+        while (take_step(h, h)) {
+        }
     }
 }
 
@@ -974,18 +1045,33 @@ bool whole16(const void *p, int64_t ld, int64_t z, int groups) {
     return (((uintptr_t)p & 15) | (ld & 7) | (groups > 1 ? z & 7 : 0)) == 0;
 }
 
+template <bool F16, int NB>
+Kernel kernel_in(int weights, bool x_aligned) {
+    return weights == W_BOXES ? x_aligned ? k_experts_in<F16, W_BOXES, true, NB> : k_experts_in<F16, W_BOXES, false, NB>
+         : weights == W_ROWS  ? x_aligned ? k_experts_in<F16, W_ROWS, true, NB> : k_experts_in<F16, W_ROWS, false, NB>
+         : x_aligned          ? k_experts_in<F16, W_ANY, true, NB>
+                              : k_experts_in<F16, W_ANY, false, NB>;
+}
+
+template <bool F16, int NB>
+Kernel kernel_out(int weights) {
+    return weights == W_BOXES  ? k_experts_out<F16, W_BOXES, NB>
+           : weights == W_ROWS ? k_experts_out<F16, W_ROWS, NB>
+                               : k_experts_out<F16, W_ANY, NB>;
+}
+
 template <bool F16>
 cudaError_t both(const Experts &p, const ExpertMaps &m, int nsm, cudaStream_t s) {
-    const bool in = whole16(p.w_in, p.w_in_ld, p.w_in_z, p.groups), out = whole16(p.w_out, p.w_out_ld, p.w_out_z, p.groups);
-    const bool x = whole16(p.x, p.x_ld, 0, 1);
-    cudaError_t e = launch(m.in_boxes ? x ? k_experts_in<F16, W_BOXES, true> : k_experts_in<F16, W_BOXES, false>
-                           : in       ? x ? k_experts_in<F16, W_ROWS, true> : k_experts_in<F16, W_ROWS, false>
-                           : x        ? k_experts_in<F16, W_ANY, true>
-                                      : k_experts_in<F16, W_ANY, false>,
-                           p, m.in, m.in_cols, nsm, s);
+    const int in = m.in_boxes ? W_BOXES : whole16(p.w_in, p.w_in_ld, p.w_in_z, p.groups) ? W_ROWS : W_ANY;
+    const int out = m.out_boxes ? W_BOXES : whole16(p.w_out, p.w_out_ld, p.w_out_z, p.groups) ? W_ROWS : W_ANY;
+    // Jobs of 16 pairs where experts have more than 8 on average (64 rows, 4 experts each,
+    // 1,024 -> 2 x 2,048, bf16, jobs of 8 and 16: over 24 experts 104 and 80 us, over 28 106 and
+    // 88; over 32 103 and 105 to 108, for what fewer rows have their registers hold half the
+    // loads under way).
+    const bool x = whole16(p.x, p.x_ld, 0, 1), two = p.rows * p.top > 8 * p.groups;
+    cudaError_t e = launch(two ? kernel_in<F16, 2>(in, x) : kernel_in<F16, 1>(in, x), p, m.in, m.in_cols, nsm, s);
     if (e != cudaSuccess) return e;
-    e = launch(m.out_boxes ? k_experts_out<F16, W_BOXES> : out ? k_experts_out<F16, W_ROWS> : k_experts_out<F16, W_ANY>, p,
-               m.out, m.out_cols, nsm, s);
+    e = launch(two ? kernel_out<F16, 2>(out) : kernel_out<F16, 1>(out), p, m.out, m.out_cols, nsm, s);
     if (e != cudaSuccess || (p.top == 1 && p.splits == 1)) return e;
     cudaLaunchAttribute at[1];
     const cudaLaunchConfig_t cfg =
@@ -1012,7 +1098,7 @@ size_t expert_tables(int rows, int top) {
 // Columns of each product's steps.
 void expert_plan(const Experts &p, bool f16, ExpertMaps *m) {
     m->in_cols = even_columns(p.n_in, EX_COLS);
-    m->out_cols = even_columns(p.hidden, f16 ? EX_COLS / 4 : EX_COLS / 2);
+    m->out_cols = even_columns(p.hidden, f16 ? EX_COLS / 2 : EX_COLS);
 }
 
 template <bool F16>
@@ -1021,15 +1107,14 @@ static cudaError_t prepare() {
     const auto set = [&](Kernel kernel) {
         if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, EX_RING);
     };
-    set(k_experts_in<F16, W_BOXES, true>);
-    set(k_experts_in<F16, W_BOXES, false>);
-    set(k_experts_in<F16, W_ROWS, true>);
-    set(k_experts_in<F16, W_ROWS, false>);
-    set(k_experts_in<F16, W_ANY, true>);
-    set(k_experts_in<F16, W_ANY, false>);
-    set(k_experts_out<F16, W_BOXES>);
-    set(k_experts_out<F16, W_ROWS>);
-    set(k_experts_out<F16, W_ANY>);
+    for (int w = W_BOXES; w <= W_ANY; ++w) {
+        for (const bool x : {true, false}) {
+            set(kernel_in<F16, 1>(w, x));
+            set(kernel_in<F16, 2>(w, x));
+        }
+        set(kernel_out<F16, 1>(w));
+        set(kernel_out<F16, 2>(w));
+    }
     return e;
 }
 

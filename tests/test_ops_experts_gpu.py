@@ -40,7 +40,9 @@ SHAPES = [   # T, E, top, D, F, N
     (1, 1, 1, 8, 8, 8), (1, 12, 2, 256, 512, 256), (2, 5, 3, 64, 72, 40), (3, 4, 4, 33, 35, 17), (1, 3, 1, 1, 1, 1),
     (8, 64, 6, 128, 176, 128), (9, 7, 2, 1000, 520, 136), (16, 16, 2, 512, 1024, 512), (17, 1024, 16, 64, 32, 24),
     (33, 2, 2, 264, 136, 264), (64, 64, 2, 256, 264, 200), (128, 40, 16, 72, 48, 72), (128, 1, 1, 128, 256, 128),
-    (100, 3, 1, 101, 257, 99), (4, 8, 2, 4104, 40, 1000), (5, 8, 2, 40, 4104, 33), (7, 12, 1, 1001, 1365, 1001),
+    (100, 3, 1, 101, 257, 99), (4, 8, 2, 4104, 40, 1000), (5, 8, 2, 40, 4104, 33), (7, 12, 1, 1001, 1365, 1001),    # experts of more than 8 rows on average, one to several steps of both products
+    (24, 2, 2, 2056, 1544, 1100), (20, 1, 1, 1030, 2054, 513), (40, 3, 2, 1088, 4104, 72), (17, 1, 1, 520, 640, 24),
+    (50, 5, 2, 192, 1088, 264),
 ]
 
 
