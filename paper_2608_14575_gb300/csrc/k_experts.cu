@@ -104,12 +104,8 @@ __device__ __forceinline__ uint4 shifted(const uint4 &a, const uint4 &b, int s) 
 
 // Eight 16-bit elements of a row in shared memory, whose first lies s bytes behind a
 // 16-byte boundary.
-template <bool ALIGNED>
 __device__ __forceinline__ uint4 taken(const char *at, int s) {
-    const uint4 a = *(const uint4 *)at;
-    if (ALIGNED) return a;
-    const uint4 b = *(const uint4 *)(at + 16);
-    return shifted(a, b, s);
+    return shifted(*(const uint4 *)at, *(const uint4 *)(at + 16), s);
 }
 
 // Eight 16-bit elements of a row of n in global memory from column c on, zeros for no row
@@ -147,10 +143,16 @@ __device__ __forceinline__ Piece piece_of(const void *row, int size, int c, int 
     return p;
 }
 
-// How the weights' rows come: in boxes of 64 columns x 8 rows by tensor copies (one for all
-// of a step's columns; matrices of whole 64 columns on 16-byte boundaries), or as bulk
-// copies of rows, aligned or not.
-enum : int { W_BOXES = 0, W_ROWS = 1, W_ANY = 2 };
+// How the weights' rows come.  BOXES: in boxes of 64 columns x 8 rows by tensor copies, one
+// for all of a step's columns, and at the end of rows that are not whole 64 columns one for
+// those before the last 64 and one for what is left; matrices whose rows begin on 16-byte
+// boundaries.  Else: as bulk copies of rows, sixteen a step of any start and length (8 rows
+// over 4 of 32 experts, 2,056 -> 2 x 2,816, bf16, in boxes and by rows: 131 and 181 us).
+
+// The map of a unit's first copy (one that is filled in).
+__device__ __forceinline__ const CUtensorMap *first_map(const WeightMaps &m, int n, int cols) {
+    return n % 64 == 0 || n >= cols ? &m.whole : &m.tail;
+}
 
 // The weights' row that stands in row g of an MMA's eight: a quarter of a warp's 16-byte
 // loads reads 64 bytes of two rows, which lie four rows apart, so that they are 64 bytes
@@ -159,11 +161,11 @@ __device__ __forceinline__ int row_of(int g) { return g >> 1 | (g & 1) << 2; }
 
 // Eight of a step's columns from k + 8 q on of a weight's row (of the first or the second
 // eight): boxes are swizzled (the 16-byte units of row i exchanged by i), rows padded by 16.
-template <int W>
+template <bool BOXES>
 __device__ __forceinline__ uint4 weights(const char *at, int row, int q, bool second, int k, int cols, int s) {
-    if (W == W_BOXES)
+    if (BOXES)
         return *(const uint4 *)(at + (second ? cols * 16 : 0) + (k >> 6) * 1024 + row * 128 + (((k >> 5 & 1) * 4 + q) ^ row) * 16);
-    return taken<W == W_ROWS>(at + (row + (second ? 8 : 0)) * (cols * 2 + 16) + (k + q * 8) * 2, s);
+    return taken(at + (row + (second ? 8 : 0)) * (cols * 2 + 16) + (k + q * 8) * 2, s);
 }
 
 // A block's ring: `depth` steps of 16 rows of weights.
@@ -194,18 +196,26 @@ struct Ring {
     }
     // A step's copies: lane i's row of weights, or (boxes) both of its eight rows by lanes 0
     // and 1.  False where the wait for the slot gave up.
-    template <int W>
-    __device__ __forceinline__ bool copy(const CUtensorMap *map, int y, int e, const uint16_t *row, int s, int cols, int n,
+    template <bool BOXES>
+    __device__ __forceinline__ bool copy(const WeightMaps &map, int y, int e, const uint16_t *row, int s, int cols, int n,
                                          volatile int *abort_flag, int32_t *status, bool stall) {
         const int lane = threadIdx.x & 31;
         ok = ok && mbar_wait(empty + slot, phase ^ 1, abort_flag, status);
-        if (W != W_BOXES) ok = __all_sync(ALL, ok);
+        if (!BOXES) ok = __all_sync(ALL, ok);
         if (!ok) return false;
         char *to = base + slot * step;
-        if (W == W_BOXES) {
+        if (BOXES) {
             if (lane < 2 && !stall) {
-                mbar_arrive_expect_tx(full + slot, cols * 16);
-                umma::tma_load_4d(to + lane * cols * 16, map, full + slot, 0, y, s * cols / 64, e);
+                to += lane * cols * 16;
+                const int box = s * cols / 64, whole = n / 64;
+                if (n % 64 == 0 || box + cols / 64 <= whole) {
+                    mbar_arrive_expect_tx(full + slot, cols * 16);
+                    umma::tma_load_4d(to, &map.whole, full + slot, 0, y, box, e);
+                } else {
+                    mbar_arrive_expect_tx(full + slot, (whole - box + 1) * 1024);
+                    if (box < whole) umma::tma_load_4d(to, &map.last, full + slot, 0, y, box, e);
+                    umma::tma_load_4d(to + (whole - box) * 1024, &map.tail, full + slot, whole * 64, y, 0, e);
+                }
             }
         } else {
             const Piece p = lane < 16 ? piece_of(row, 2, s * cols, cols, n) : Piece{nullptr, 0};
@@ -588,16 +598,17 @@ __device__ __forceinline__ bool take(Shared<NB> &sh, float (&c)[NB][4], int turn
 
 // ---- the first product --------------------------------------------------------------
 
-template <bool F16, int W, bool X_ALIGNED, int NB>
+template <bool F16, bool BOXES, bool X_ALIGNED, int NB>
 __global__ void __launch_bounds__(EX_THREADS)
-k_experts_in(const __grid_constant__ Experts p, const __grid_constant__ CUtensorMap map) {
+k_experts_in(const __grid_constant__ Experts p, const __grid_constant__ WeightMaps map) {
     extern __shared__ __align__(1024) char smem[];
     __shared__ Shared<NB> sh;
     constexpr int CH = EX_COLS / EX_STRIDE, XU = X_ALIGNED ? 1 : 2;
-    constexpr bool TWICE = NB == 1 && W != W_ANY && X_ALIGNED;      // registers for two steps of x
+    constexpr bool TWICE = NB == 1 && BOXES && X_ALIGNED;      // registers for two steps of x
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g8 = lane >> 2, q = lane & 3, wr = row_of(g8);
     const int cols = p.cols, steps = (p.n_in + cols - 1) / cols;
     const bool both = steps > 1;
+    if (BOXES && tid == 0) umma::tma_prefetch_desc(first_map(map, p.n_in, cols));
     init(sh, both);
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -619,9 +630,9 @@ k_experts_in(const __grid_constant__ Experts p, const __grid_constant__ CUtensor
             ring.next();
         }
         while (at.more()) {
-            const uint16_t *row = W != W_BOXES && lane < 16 ? weights_row(at.w, lane) : nullptr;
+            const uint16_t *row = !BOXES && lane < 16 ? weights_row(at.w, lane) : nullptr;
             const int f0 = at.w.tile * wide, y = lane == 0 ? f0 : p.gated ? p.hidden + f0 : f0 + 8;
-            if (!ring.copy<W>(&map, y, r.expert[at.w.job], row, at.s, cols, p.n_in, &sh.abort_flag, p.status, p.test_stall)) return;
+            if (!ring.copy<BOXES>(map, y, r.expert[at.w.job], row, at.s, cols, p.n_in, &sh.abort_flag, p.status, p.test_stall)) return;
             at.next();
             if (at.more()) at.next();
         }
@@ -638,9 +649,10 @@ k_experts_in(const __grid_constant__ Experts p, const __grid_constant__ CUtensor
 #pragma unroll
             for (int k = 0; k < NB * 4; ++k) {
                 const int i = k % 4, column = k / 4 * 8 + 2 * q + (i & 1), f = w.tile * wide + wr + (i & 2) * 4;
-                if (column >= n || (p.gated && (i & 2)) || f >= p.hidden) continue;
+                if (column >= n || (p.gated && (i & 2)) || f >= p.h_ld) continue;
                 float v = activated(c[k / 4][i], p.act);
                 if (p.gated) v *= c[k / 4][i | 2];
+                if (f >= p.hidden) v = 0.f;              // (the second product reads whole 16 bytes)
                 const int64_t to = (int64_t)r.list[begin + column] * 2 * p.h_ld + f;
                 if (F16) {
                     float *h = (float *)p.h + to;
@@ -697,7 +709,7 @@ k_experts_in(const __grid_constant__ Experts p, const __grid_constant__ CUtensor
         if (ahead.more()) ahead.next();
         if (TWICE && ahead.more()) fetch(next, ahead);
         int sa = 0, sb = 0;
-        if (W == W_ANY) {
+        if (!BOXES) {
             sa = (int)((uintptr_t)weights_row(at.w, wr) & 15);
             sb = (int)((uintptr_t)weights_row(at.w, wr + 8) & 15);
         }
@@ -710,10 +722,10 @@ k_experts_in(const __grid_constant__ Experts p, const __grid_constant__ CUtensor
             const int k = member * 32 + i * EX_STRIDE;
             a[i] = d[i] = make_uint4(0, 0, 0, 0);
             if (k < left) {
-                a[i] = weights<W>(from, wr, q, false, k, cols, sa);
-                d[i] = weights<W>(from, wr, q, true, k, cols, sb);
+                a[i] = weights<BOXES>(from, wr, q, false, k, cols, sa);
+                d[i] = weights<BOXES>(from, wr, q, true, k, cols, sb);
             }
-            if (W != W_BOXES && k + 32 > left) {
+            if (!BOXES && k + 32 > left) {
                 const int e = max(0, min(8, left - k - q * 8));
                 a[i] = first(a[i], e);
                 d[i] = first(d[i], e);
@@ -726,7 +738,7 @@ k_experts_in(const __grid_constant__ Experts p, const __grid_constant__ CUtensor
             for (int i = 0; i < CH; ++i) {
                 const int k = member * 32 + i * EX_STRIDE;
                 uint4 v = X_ALIGNED ? x[i][j][0] : shifted(x[i][j][0], x[i][j][XU - 1], sx[j]);
-                if (W != W_BOXES && k + 32 > left) v = first(v, max(0, min(8, left - k - q * 8)));
+                if (!BOXES && k + 32 > left) v = first(v, max(0, min(8, left - k - q * 8)));
                 mma16<F16>(c[j][0], a[i].x, d[i].x, a[i].y, d[i].y, v.x, v.y);
                 mma16<F16>(c[j][1], a[i].z, d[i].z, a[i].w, d[i].w, v.z, v.w);
             }
@@ -764,16 +776,17 @@ __device__ __forceinline__ uint4 widened(uint32_t lo, uint32_t hi) {
     return make_uint4(__float_as_uint(a.x), __float_as_uint(a.y), __float_as_uint(b.x), __float_as_uint(b.y));
 }
 
-template <bool F16, int W, int NB>
+template <bool F16, bool BOXES, int NB>
 __global__ void __launch_bounds__(EX_THREADS)
-k_experts_out(const __grid_constant__ Experts p, const __grid_constant__ CUtensorMap map) {
+k_experts_out(const __grid_constant__ Experts p, const __grid_constant__ WeightMaps map) {
     extern __shared__ __align__(1024) char smem[];
     __shared__ Shared<NB> sh;
     // 32 columns of h a lane: high and low terms, in 16-byte loads
     constexpr int CH = EX_COLS / (F16 ? 2 : 1) / EX_STRIDE, TERM = F16 ? 2 : 1;
-    constexpr bool TWICE = NB == 1 && W != W_ANY;
+    constexpr bool TWICE = NB == 1 && BOXES;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g8 = lane >> 2, q = lane & 3, wr = row_of(g8);
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    if (BOXES && tid == 0) umma::tma_prefetch_desc(first_map(map, p.hidden, p.cols));
     init(sh, true);
     asm volatile("griddepcontrol.wait;" ::: "memory");
     Routing r(p, smem);
@@ -810,8 +823,8 @@ k_experts_out(const __grid_constant__ Experts p, const __grid_constant__ CUtenso
         while (at.more()) {
             const int o = at.w.tile * 16, e = r.expert[at.w.job];
             const uint16_t *row = nullptr;
-            if (W != W_BOXES && lane < 16 && o + lane < p.n_out) row = p.w_out + e * p.w_out_z + (int64_t)(o + lane) * p.w_out_ld;
-            if (!ring.copy<W>(&map, o + lane * 8, e, row, at.s, cols, p.hidden, &sh.abort_flag, p.status, p.test_stall)) return;
+            if (!BOXES && lane < 16 && o + lane < p.n_out) row = p.w_out + e * p.w_out_z + (int64_t)(o + lane) * p.w_out_ld;
+            if (!ring.copy<BOXES>(map, o + lane * 8, e, row, at.s, cols, p.hidden, &sh.abort_flag, p.status, p.test_stall)) return;
             at.next();
             if (at.more()) at.next();
         }
@@ -895,7 +908,7 @@ k_experts_out(const __grid_constant__ Experts p, const __grid_constant__ CUtenso
         if (ahead.more()) ahead.next();
         if (TWICE && ahead.more()) fetch(next, ahead);
         int sa = 0, sb = 0;
-        if (W == W_ANY) {
+        if (!BOXES) {
             const uint16_t *w = p.w_out + r.expert[at.w.job] * p.w_out_z + (int64_t)(at.w.tile * 16 + wr) * p.w_out_ld;
             sa = (int)((uintptr_t)w & 15);
             sb = (int)((uintptr_t)(w + 8 * p.w_out_ld) & 15);
@@ -909,10 +922,10 @@ k_experts_out(const __grid_constant__ Experts p, const __grid_constant__ CUtenso
             const int k = member * 32 + i * EX_STRIDE;
             a[i] = d[i] = make_uint4(0, 0, 0, 0);
             if (k < left) {
-                a[i] = weights<W>(from, wr, q, false, k, cols, sa);
-                d[i] = weights<W>(from, wr, q, true, k, cols, sb);
+                a[i] = weights<BOXES>(from, wr, q, false, k, cols, sa);
+                d[i] = weights<BOXES>(from, wr, q, true, k, cols, sb);
             }
-            if (W != W_BOXES && k + 32 > left) {
+            if (!BOXES && k + 32 > left) {
                 const int e = max(0, min(8, left - k - q * 8));
                 a[i] = first(a[i], e);
                 d[i] = first(d[i], e);
@@ -920,7 +933,6 @@ k_experts_out(const __grid_constant__ Experts p, const __grid_constant__ CUtenso
         }
 #pragma unroll
         for (int i = 0; i < CH; ++i) {
-            const int k = member * 32 + i * EX_STRIDE;
             uint4 a0, a1, d0, d1;
             if (F16) {
                 a0 = widened(a[i].x, a[i].y), a1 = widened(a[i].z, a[i].w);
@@ -929,23 +941,6 @@ k_experts_out(const __grid_constant__ Experts p, const __grid_constant__ CUtenso
 #pragma unroll
             for (int b = 0; b < NB; ++b) {
                 if (b && n <= b * 8) break;
-                if (W != W_BOXES && k + 32 > left) {
-                    // (the rows are filled up to whole 16 bytes with anything)
-                    const int e = max(0, min(8, left - k - q * 8));
-#pragma unroll
-                    for (int j = 0; j < 2 * TERM; ++j) {
-                        uint4 &v = h[i][b][j];
-                        if (F16) {
-                            const int f = e - j % TERM * 4;
-                            if (f < 1) v.x = 0;
-                            if (f < 2) v.y = 0;
-                            if (f < 3) v.z = 0;
-                            if (f < 4) v.w = 0;
-                        } else {
-                            v = first(v, e);
-                        }
-                    }
-                }
                 if (F16) {
 #pragma unroll
                     for (int j = 0; j < 2 * TERM; j += TERM) {
@@ -1017,7 +1012,7 @@ cudaLaunchConfig_t early(dim3 grid, int threads, size_t smem, cudaStream_t s, cu
     return cfg;
 }
 
-typedef void (*Kernel)(Experts, CUtensorMap);
+typedef void (*Kernel)(Experts, WeightMaps);
 
 // Columns of a step: as even as it gets for this width, in whole boxes.
 int even_columns(int width, int most) {
@@ -1028,7 +1023,7 @@ int even_columns(int width, int most) {
 constexpr int step_bytes(int cols) { return (16 * (cols * 2 + 16) + 1023) & ~1023; }
 static_assert(2 * step_bytes(EX_COLS) + 16 + EX_PAIRS * 13 + 16 + EX_GROUPS * 4 + 1023 <= EX_RING, "tables and two steps");
 
-cudaError_t launch(Kernel kernel, Experts p, const CUtensorMap &map, int cols, int nsm, cudaStream_t s) {
+cudaError_t launch(Kernel kernel, Experts p, const WeightMaps &map, int cols, int nsm, cudaStream_t s) {
     p.cols = cols;
     p.step = step_bytes(cols);
     p.ring_at = (int)routing_bytes(p);
@@ -1041,34 +1036,27 @@ cudaError_t launch(Kernel kernel, Experts p, const CUtensorMap &map, int cols, i
     return cudaLaunchKernelEx(&cfg, kernel, p, map);
 }
 
-bool whole16(const void *p, int64_t ld, int64_t z, int groups) {
-    return (((uintptr_t)p & 15) | (ld & 7) | (groups > 1 ? z & 7 : 0)) == 0;
+bool whole16(const void *p, int64_t ld) { return (((uintptr_t)p & 15) | (ld & 7)) == 0; }
+
+template <bool F16, int NB>
+Kernel kernel_in(bool boxes, bool x_aligned) {
+    return boxes ? x_aligned ? k_experts_in<F16, true, true, NB> : k_experts_in<F16, true, false, NB>
+                 : x_aligned ? k_experts_in<F16, false, true, NB> : k_experts_in<F16, false, false, NB>;
 }
 
 template <bool F16, int NB>
-Kernel kernel_in(int weights, bool x_aligned) {
-    return weights == W_BOXES ? x_aligned ? k_experts_in<F16, W_BOXES, true, NB> : k_experts_in<F16, W_BOXES, false, NB>
-         : weights == W_ROWS  ? x_aligned ? k_experts_in<F16, W_ROWS, true, NB> : k_experts_in<F16, W_ROWS, false, NB>
-         : x_aligned          ? k_experts_in<F16, W_ANY, true, NB>
-                              : k_experts_in<F16, W_ANY, false, NB>;
-}
-
-template <bool F16, int NB>
-Kernel kernel_out(int weights) {
-    return weights == W_BOXES  ? k_experts_out<F16, W_BOXES, NB>
-           : weights == W_ROWS ? k_experts_out<F16, W_ROWS, NB>
-                               : k_experts_out<F16, W_ANY, NB>;
+Kernel kernel_out(bool boxes) {
+    return boxes ? k_experts_out<F16, true, NB> : k_experts_out<F16, false, NB>;
 }
 
 template <bool F16>
 cudaError_t both(const Experts &p, const ExpertMaps &m, int nsm, cudaStream_t s) {
-    const int in = m.in_boxes ? W_BOXES : whole16(p.w_in, p.w_in_ld, p.w_in_z, p.groups) ? W_ROWS : W_ANY;
-    const int out = m.out_boxes ? W_BOXES : whole16(p.w_out, p.w_out_ld, p.w_out_z, p.groups) ? W_ROWS : W_ANY;
+    const bool in = m.in_boxes, out = m.out_boxes;
     // Jobs of 16 pairs where experts have more than 8 on average (64 rows, 4 experts each,
     // 1,024 -> 2 x 2,048, bf16, jobs of 8 and 16: over 24 experts 104 and 80 us, over 28 106 and
     // 88; over 32 103 and 105 to 108, for what fewer rows have their registers hold half the
     // loads under way).
-    const bool x = whole16(p.x, p.x_ld, 0, 1), two = p.rows * p.top > 8 * p.groups;
+    const bool x = whole16(p.x, p.x_ld), two = p.rows * p.top > 8 * p.groups;
     cudaError_t e = launch(two ? kernel_in<F16, 2>(in, x) : kernel_in<F16, 1>(in, x), p, m.in, m.in_cols, nsm, s);
     if (e != cudaSuccess) return e;
     e = launch(two ? kernel_out<F16, 2>(out) : kernel_out<F16, 1>(out), p, m.out, m.out_cols, nsm, s);
@@ -1107,7 +1095,7 @@ static cudaError_t prepare() {
     const auto set = [&](Kernel kernel) {
         if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, EX_RING);
     };
-    for (int w = W_BOXES; w <= W_ANY; ++w) {
+    for (const bool w : {true, false}) {
         for (const bool x : {true, false}) {
             set(kernel_in<F16, 1>(w, x));
             set(kernel_in<F16, 2>(w, x));

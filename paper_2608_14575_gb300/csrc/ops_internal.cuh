@@ -353,10 +353,15 @@ struct Experts {
 int expert_splits(int hidden);            // at most
 size_t expert_tables(int rows, int top);
 cudaError_t experts_prepare();
-// The weights of both products as tensors (64, rows, columns / 64, experts) where their
-// matrices allow it (boxes of 64 x 8 x columns / 64 of a step), and the steps' columns.
+// The weights of a product as a tensor (64, rows, columns / 64, experts): boxes of 64 x 8 x
+// columns / 64 of a step, and of what the last step has of them; and as one of (columns,
+// rows, 1, experts): boxes of 64 x 8, where the columns are not whole 64.
+struct WeightMaps {
+    CUtensorMap whole, last, tail;
+};
+// Those of both products, where their matrices allow it, and the steps' columns.
 struct ExpertMaps {
-    CUtensorMap in, out;
+    WeightMaps in, out;
     bool in_boxes, out_boxes;
     int in_cols, out_cols;
 };

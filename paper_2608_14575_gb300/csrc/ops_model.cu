@@ -44,16 +44,23 @@ static hwr_status check_experts(hwr_ops *c, const hwr_experts *e, const void *y,
 
 // Matrices [groups][rows][width] in boxes of 64 columns x 8 rows, cols / 64 of them side by
 // side; false where they cannot be mapped so.
-static bool map_weights(CUtensorMap *m, bool f16, const void *w, int64_t ld, int64_t z, int64_t rows, int width, int groups,
+static bool map_weights(WeightMaps *m, bool f16, const void *w, int64_t ld, int64_t z, int64_t rows, int width, int groups,
                         int cols) {
     memset(m, 0, sizeof *m);
-    if (((uintptr_t)w & 15) || ld % 8 || width % 64 || (groups > 1 && z % 8)) return false;
-    const cuuint64_t dims[4] = {64, (cuuint64_t)rows, (cuuint64_t)width / 64, (cuuint64_t)groups};
-    const cuuint64_t strides[3] = {(cuuint64_t)ld * 2, 128, (cuuint64_t)(groups > 1 ? z : ld * rows) * 2};
-    const cuuint32_t box[4] = {64, 8, (cuuint32_t)cols / 64, 1}, one[4] = {1, 1, 1, 1};
-    return g_encode(m, f16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void *>(w), dims,
-                    strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-                    CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    if (((uintptr_t)w & 15) || ld % 8 || (groups > 1 && z % 8)) return false;
+    const int whole = width / 64, steps = (width + cols - 1) / cols, last = whole - (steps - 1) * (cols / 64);
+    const auto map = [&](CUtensorMap *to, int inner, int blocks, int of_box) {
+        const cuuint64_t dims[4] = {(cuuint64_t)inner, (cuuint64_t)rows, (cuuint64_t)blocks, (cuuint64_t)groups};
+        const cuuint64_t strides[3] = {(cuuint64_t)ld * 2, 128, (cuuint64_t)(groups > 1 ? z : ld * rows) * 2};
+        const cuuint32_t box[4] = {64, 8, (cuuint32_t)of_box, 1}, one[4] = {1, 1, 1, 1};
+        return g_encode(to, f16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void *>(w),
+                        dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                        CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    };
+    if (width % 64 == 0) return map(&m->whole, 64, whole, cols / 64);
+    // (a map that no step uses is left out)
+    return (steps == 1 || map(&m->whole, 64, whole, cols / 64)) && (last == 0 || map(&m->last, 64, whole, last)) &&
+           map(&m->tail, width, 1, 1);
 }
 
 extern "C" hwr_status hwr_expert_layer(hwr_ops *c, const hwr_experts *e, void *y, int64_t y_ld) {
@@ -102,8 +109,9 @@ extern "C" hwr_status hwr_expert_layer(hwr_ops *c, const hwr_experts *e, void *y
     const bool f16 = e->dtype == HWR_F16;
     ExpertMaps m;
     expert_plan(p, f16, &m);
-    m.in_boxes = map_weights(&m.in, f16, e->w_in, e->w_in_ld, e->w_in_group, e->gated ? 2 * (int64_t)e->hidden : e->hidden,
-                             e->n_in, e->groups, m.in_cols);
+    // (rows of x are not filled up behind their last eight columns, those of h are with zeros)
+    m.in_boxes = e->n_in % 8 == 0 && map_weights(&m.in, f16, e->w_in, e->w_in_ld, e->w_in_group,
+                                                 e->gated ? 2 * (int64_t)e->hidden : e->hidden, e->n_in, e->groups, m.in_cols);
     m.out_boxes = map_weights(&m.out, f16, e->w_out, e->w_out_ld, e->w_out_group, e->n_out, e->hidden, e->groups, m.out_cols);
     CK(c, launch_experts(p, m, f16, c->nsm, c->stream), "expert kernels");
     return HWR_OK;

@@ -149,6 +149,25 @@ def test_strides(ops, off):
     assert (big == 3.0).all()                 # nothing beside the result was written
 
 
+@pytest.mark.parametrize("shape", [(3, 4, 2, 1000, 1100, 72), (3, 4, 2, 1001, 1098, 40), (20, 2, 2, 1096, 523, 24),
+                                   (5, 3, 1, 40, 61, 8), (9, 3, 2, 576, 1089, 1000)])
+@pytest.mark.parametrize("dt", [BF, HF])
+def test_rows_that_end_before_their_stride(ops, shape, dt):
+    """Widths of any remainder on aligned rows: what lies behind them (NaN) is not part of them."""
+    T, E, top, D, F, N = shape
+    whole = lambda n: (n + 7) // 8 * 8 + 8
+    padded = []
+    for t in layer(T, E, D, F, N, True, dt):
+        big = torch.full((*t.shape[:-1], whole(t.shape[-1])), float("nan"), device="cuda", dtype=dt)
+        big[..., :t.shape[-1]] = t
+        padded.append(big[..., :t.shape[-1]])
+    x, w_in, w_out = padded
+    s = scores_of(T, E)
+    y = ops.expert_layer(x, w_in, w_out, scores=s, top=top)
+    choice, p = M.choices(s, top, False)
+    inside(y, M.expert_layer(x, w_in, w_out, choice, p, "silu"))
+
+
 def test_offsets_beyond_32_bits(ops):
     """Weights of more than 2^31 elements: the last expert's."""
     D, F, E = 4096, 4096, 140
