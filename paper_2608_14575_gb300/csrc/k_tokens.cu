@@ -12,9 +12,15 @@
 // Alternatives: 64-bit keys (the value's order above, the index's complement below: equal
 // values go by the lowest index).  A block's first step has its threads' largest values,
 // and from the few largest of each warp a bound that at least `top` values reach, and few
-// more.  Values above it are gathered in shared memory, at the end (or where they get too
-// many) a key's place is the number of larger ones.  Values of later steps have higher
-// indices, so those that only equal the bound have no place.
+// more.  Each warp gathers the values that reach it in shared memory, and says what its few
+// largest candidates are now, so that the bound rises without a barrier.  (Other warps may be
+// ahead: what equals their bound is kept.)  Where candidates get too many a key's place is the
+// number of larger ones, and the last of the best a bound of the warp's own: values of its
+// later steps have higher indices, so those that only equal it have no place.  At the end a
+// bound as in the first step, among the candidates, leaves few of them to be placed by the
+// block.  (One list for the block, with barriers in each step: 512 rows of 131,072 bf16 logits
+// with 20 alternatives 51.5 us for 48.5, 2,048 of 50,001 90.6 for 82.5.  With each warp's own
+// bound alone 64 for 48.5.)
 #include <type_traits>
 
 #include "ops_internal.cuh"
@@ -31,6 +37,10 @@ constexpr int TK_VECS = 4;             // 16-byte loads of a step
 // not done).  Alternatives want few blocks, each of which finds a bound of its own: 64 rows
 // of 131,072 with 20 take 18 us with 256 threads, 24 with 128.
 __host__ __device__ constexpr int threads_of(bool top) { return top ? TK_THREADS : 128; }
+// Blocks of rows with alternatives an SM: 3, which may use 80 registers, where all are there
+// at once, else 4 (64 rows of 131,072 in bf16, 20 alternatives: 14.4 us with 3, 16.7 with 4;
+// 512 rows 58 and 49).
+constexpr int TK_FEW = 3, TK_LOT = 4;
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr float FAR = -1e30f;
 constexpr uint32_t ALL = 0xffffffffu;
@@ -68,72 +78,136 @@ __device__ __forceinline__ float value_of(uint32_t order) {
     return __uint_as_float(order >> 31 ? order ^ 0x80000000u : ~order);      // (0: a NaN)
 }
 
-constexpr int TK_KEYS = TK_THREADS * 8;       // of a vector of each thread
-constexpr int TK_READ = 32;                   // keys that a thread compares at a time
-constexpr int TK_ROOM = TK_KEYS + TK_READ;
-constexpr int TK_MANY = 64;                   // candidates that are sorted out before a next step
+constexpr int TK_READ = 32;                   // keys that are compared at a time
+constexpr int TK_ROOM = 32 * 8 + 32;          // of a warp: a vector of each lane, beside the best
+constexpr int TK_MANY = 64;                   // candidates of a warp that are sorted out
+constexpr int TK_ALL = (TK_WARPS * TK_MANY > TOKEN_SPLITS * 32 ? TK_WARPS * TK_MANY : TOKEN_SPLITS * 32) + TK_READ;
 constexpr uint32_t MASKED = 0x007fffffu;      // order_of(-inf)
+static_assert(TK_ROOM % TK_READ == 0, "lists are filled up to whole reads");
 
-// Keys of a block's candidates.
+// Keys of a warp's candidates, and of a block's.
 struct alignas(16) Best {
-    uint64_t key[TK_ROOM], sorted[32];
-    uint32_t most[TK_WARPS];
-    int n;                                // offered; more than there is room for: some are missing
-    uint32_t bound;
+    uint64_t key[TK_WARPS][TK_ROOM], kept[TK_WARPS][32], all[TK_ALL], sorted[32];
+    uint32_t most[2][TK_WARPS];           // of the first step, and of the candidates
+    int offered[TK_WARPS];                // more than there is room for: some are missing
+    int n;
 };
 
 // The least value that is above (equal: or at) the bound.
 __device__ __forceinline__ float least_of(uint32_t bound, bool equal) { return value_of(bound + (equal ? 0 : 1)); }
 
-// A thread's values at or above `least`, N from index i on, the largest of which is given.
-// (Few threads have any, after the first steps.)
+// A thread's values at or above `least`, N from index i on, the largest of which is given,
+// to its warp's candidates.  (Few threads have any, after the first steps.)
 template <int N>
 __device__ __forceinline__ void offer(Best &b, const float (&z)[N], float largest, int i, float least) {
     if (!(largest >= least)) return;
+    const int warp = threadIdx.x >> 5;
     uint32_t mine = 0;
 #pragma unroll
     for (int j = 0; j < N; ++j) mine |= (uint32_t)(z[j] >= least) << j;
-    int at = atomicAdd(&b.n, __popc(mine));
+    int at = atomicAdd(&b.offered[warp], __popc(mine));
+    // (one, nearly always)
+#pragma unroll 1
+    for (; mine; mine &= mine - 1, ++at) {
+        const int j = __ffs(mine) - 1;
+        float v = z[0];
 #pragma unroll
-    for (int j = 0; j < N; ++j)
-        if (mine >> j & 1) {
-            if (at < TK_ROOM) b.key[at] = (uint64_t)order_of(z[j]) << 32 | (uint32_t)~(i + j);
-            ++at;
-        }
+        for (int k = 1; k < N; ++k) v = j == k ? z[k] : v;
+        if (at < TK_ROOM) b.key[warp][at] = (uint64_t)order_of(v) << 32 | (uint32_t)~(i + j);
+    }
 }
 
-// The best of the gathered keys, sorted (0: none); by the block.
+// How many of n keys (filled up with zeros) are larger, as far as `top`.
+__device__ __forceinline__ int place_of(uint64_t mine, const uint64_t *key, int n, int top) {
+    int place = 0;
+    for (int j = 0; j < n && place < top; j += TK_READ) {
+        const ulonglong2 *o = (const ulonglong2 *)(key + j);
+#pragma unroll
+        for (int k = 0; k < TK_READ / 2; ++k) {
+            const ulonglong2 v = o[k];
+            place += (v.x > mine) + (v.y > mine);
+        }
+    }
+    return place;
+}
+
+// A warp's best, left as its only candidates; the bound is the last one's value.
+__device__ __noinline__ uint32_t squeeze(Best &b, int top, uint32_t bound) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    uint64_t *key = b.key[warp], *kept = b.kept[warp];
+    __syncwarp();
+    const int n = min(b.offered[warp], TK_ROOM);
+    kept[lane] = 0;
+    if (n + lane < TK_ROOM) key[n + lane] = 0;
+    __syncwarp();
+    for (int i = lane; i < n; i += 32) {
+        const uint64_t mine = key[i];
+        const int place = place_of(mine, key, n, top);
+        if (place < top) kept[place] = mine;
+    }
+    __syncwarp();
+    key[lane] = kept[lane];
+    if (lane == 0) b.offered[warp] = min(n, top);
+    if (n >= top) bound = max(bound, (uint32_t)(kept[top - 1] >> 32));
+    __syncwarp();
+    return bound;
+}
+
+// The best of the block's keys, sorted (0: none).
 __device__ __forceinline__ void settle(Best &b, int top) {
     __syncthreads();
-    const int n = min(b.n, TK_ROOM);
+    const int n = b.n;
     if (threadIdx.x < 32) b.sorted[threadIdx.x] = 0;
-    if (threadIdx.x < TK_READ && n + threadIdx.x < TK_ROOM) b.key[n + threadIdx.x] = 0;
+    if (threadIdx.x < TK_READ) b.all[n + threadIdx.x] = 0;
     __syncthreads();
     for (int i = threadIdx.x; i < n; i += TK_THREADS) {
-        const uint64_t mine = b.key[i];
-        int place = 0;
-        for (int j = 0; j < n && place < top; j += TK_READ) {
-            const ulonglong2 *o = (const ulonglong2 *)(b.key + j);
-#pragma unroll
-            for (int k = 0; k < TK_READ / 2; ++k) {
-                const ulonglong2 v = o[k];
-                place += (v.x > mine) + (v.y > mine);
-            }
-        }
+        const uint64_t mine = b.all[i];
+        const int place = place_of(mine, b.all, n, top);
         if (place < top && mine) b.sorted[place] = mine;
     }
     __syncthreads();
 }
 
-// The same, left as the only candidates; the bound is the last one's value.
-__device__ __forceinline__ void squeeze(Best &b, int top) {
-    settle(b, top);
-    if (threadIdx.x < top) b.key[threadIdx.x] = b.sorted[threadIdx.x];
-    if (threadIdx.x == 0) {
-        b.n = min(b.n, top);
-        if (b.n == top) b.bound = max(b.bound, (uint32_t)(b.sorted[top - 1] >> 32));
+// A value that, in every warp, as many threads' keys reach as it takes for `top` in all: what
+// this warp has to say.  (0: too few have one.)
+__device__ __forceinline__ uint32_t most_of(uint32_t mine, int top) {
+    const int lane = threadIdx.x & 31;
+    uint32_t most = 0;
+    for (int j = 0; j < (top + TK_WARPS - 1) / TK_WARPS; ++j) {
+        most = __reduce_max_sync(ALL, mine);
+        const uint32_t who = __ballot_sync(ALL, mine == most);
+        if (lane == __ffs(who) - 1) mine = 0;
     }
+    return most;
+}
+__device__ __forceinline__ uint32_t least_of_all(const uint32_t (&of)[TK_WARPS]) {
+    uint32_t most = of[0];
+#pragma unroll
+    for (int w = 1; w < TK_WARPS; ++w) most = min(most, of[w]);
+    return most;
+}
+
+// The largest of a lane's part of its warp's candidates, at most TK_MANY.
+__device__ __forceinline__ uint32_t largest_of(const Best &b, int warp) {
+    const int lane = threadIdx.x & 31, n = b.offered[warp];
+    const uint32_t *high = (const uint32_t *)b.key[warp] + 1;
+    return max(lane < n ? high[2 * lane] : 0u, lane + 32 < n ? high[2 * lane + 64] : 0u);
+}
+
+// The warps' candidates that can be among the best, sorted.
+__device__ __forceinline__ void gather(Best &b, int top) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    __syncwarp();
+    if (b.offered[warp] > TK_MANY) squeeze(b, top, 0);
+    const int n = b.offered[warp];
+    const uint64_t one = lane < n ? b.key[warp][lane] : 0, two = lane + 32 < n ? b.key[warp][lane + 32] : 0;
+    const uint32_t most = most_of((uint32_t)((one > two ? one : two) >> 32), top);
+    if (lane == 0) b.most[1][warp] = most;
     __syncthreads();
+    const uint32_t bound = least_of_all(b.most[1]);
+    if (one && (uint32_t)(one >> 32) >= bound) b.all[atomicAdd(&b.n, 1)] = one;
+    if (two && (uint32_t)(two >> 32) >= bound) b.all[atomicAdd(&b.n, 1)] = two;
+    settle(b, top);
 }
 
 // Where a row's 16-byte vectors begin, and how many there are.
@@ -171,8 +245,8 @@ __device__ __forceinline__ void finish(const TokenRows &p, int64_t row, const Su
     }
 }
 
-template <int DT, bool TOP>
-__global__ void __launch_bounds__(threads_of(TOP), TOP ? 4 : DT == HWR_F32 ? 8 : DT == HWR_BF16 ? 10 : 9)
+template <int DT, bool TOP, int BLOCKS>
+__global__ void __launch_bounds__(threads_of(TOP), BLOCKS)
 k_token_rows(const __grid_constant__ TokenRows p) {
     constexpr int N = Vec<DT>::N, TH = threads_of(TOP);
     constexpr bool AHEAD = !TOP && DT == HWR_F32;
@@ -183,10 +257,8 @@ k_token_rows(const __grid_constant__ TokenRows p) {
     const int64_t row = blockIdx.x / (uint32_t)p.splits;
     const int piece = blockIdx.x % (uint32_t)p.splits;
     if constexpr (TOP) {
-        if (tid == 0) {
-            shared_best.n = 0;
-            shared_best.bound = MASKED;
-        }
+        if (tid == 0) shared_best.n = 0;
+        if (lane == 0) shared_best.offered[warp] = 0;
     }
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -199,6 +271,7 @@ k_token_rows(const __grid_constant__ TokenRows p) {
     const bool has = (uint32_t)token < (uint32_t)p.vocab;
     const float z_token = has && tid == 0 ? Vec<DT>::load(base, token) : 0.f;
 
+    uint32_t bound = MASKED;              // of my warp: values above it are candidates
     float m = -INFINITY;
     Two s(0.f, 0.f), d(0.f, 0.f);
     const auto raise = [&](float to) {
@@ -224,7 +297,7 @@ k_token_rows(const __grid_constant__ TokenRows p) {
             if (valid) offer<1>(shared_best, z, z[0], i, least);
         }
     };
-    __syncthreads();
+    __syncwarp();
     if (warp == 0 && piece == 0 && cut.head) single(lane, lane < cut.head, least_of(MASKED, false));
     // (32-bit values: a step's are on their way while the one before is taken)
     uint4 next[TK_VECS];
@@ -259,51 +332,51 @@ k_token_rows(const __grid_constant__ TokenRows p) {
         if constexpr (TOP) {
             Best &best = shared_best;
             const bool first = b == v0;
+            volatile uint32_t *said = best.most[0];
             if (first) {
-                // in each warp as many threads as it takes for `top` in all have a value at or
-                // above this (-inf: too few have a number)
-                uint32_t mine = order_of(mx), most = 0;
-                for (int j = 0; j < (top + TK_WARPS - 1) / TK_WARPS; ++j) {
-                    most = __reduce_max_sync(ALL, mine);
-                    const uint32_t who = __ballot_sync(ALL, mine == most);
-                    if (lane == __ffs(who) - 1) mine = 0;
-                }
-                if (lane == 0) best.most[warp] = most;
-                __syncthreads();
-                if (tid == 0) {
-                    for (int w = 0; w < TK_WARPS; ++w) most = min(most, best.most[w]);
-                    best.bound = max(most, MASKED);
-                }
+                const uint32_t most = most_of(order_of(mx), top);
+                if (lane == 0) said[warp] = most;
                 __syncthreads();
             }
-            const uint32_t floor = best.bound;
+            // what `top` values reach, of any index (other warps may be ahead)
+            const uint32_t floor = __reduce_min_sync(ALL, lane < TK_WARPS ? said[lane] : ~0u);
+            const float any = floor > MASKED ? value_of(floor) : -INFINITY;
             // (vectors beyond the last are -inf, below any `least`)
-            const int before = best.n, at = cut.head + (b + tid) * N;
-            const auto least = [&] { return least_of(best.bound, first && best.bound == floor && floor > MASKED); };
-            __syncthreads();
-            if (mx >= least())
+            const int at = cut.head + (b + tid) * N;
+            const float least = fmaxf(least_of(bound, false), any);
+            if (__any_sync(ALL, mx >= least)) {
+                const int before = best.offered[warp];
+                __syncwarp();
+                if (mx >= least)
 #pragma unroll
-                for (int k = 0; k < TK_VECS; ++k) offer<N>(best, z[k], largest[k], at + k * TH * N, least());
-            __syncthreads();
-            if (best.n > TK_ROOM) {
-                // not all of them found room: once more, a vector at a time
-                __syncthreads();
-                if (tid == 0) best.n = before;
-                squeeze(best, top);
+                    for (int k = 0; k < TK_VECS; ++k) offer<N>(best, z[k], largest[k], at + k * TH * N, least);
+                __syncwarp();
+                const int n = best.offered[warp];
+                if (n > TK_ROOM) {
+                    // not all of them found room: once more, a vector at a time
+                    __syncwarp();
+                    if (lane == 0) best.offered[warp] = before;
+                    bound = squeeze(best, top, bound);
 #pragma unroll
-                for (int k = 0; k < TK_VECS; ++k) {
-                    offer<N>(best, z[k], largest[k], at + k * TH * N, least());
-                    squeeze(best, top);
+                    for (int k = 0; k < TK_VECS; ++k) {
+                        offer<N>(best, z[k], largest[k], at + k * TH * N, fmaxf(least_of(bound, false), any));
+                        bound = squeeze(best, top, bound);
+                    }
+                } else if (n > TK_MANY) {
+                    bound = squeeze(best, top, bound);
                 }
-            } else if (best.n > TK_MANY && b + TH * TK_VECS < v1) {
-                squeeze(best, top);
+                if (b + TH * TK_VECS < v1) {
+                    const uint32_t most = most_of(largest_of(best, warp), top);
+                    if (lane == 0 && most > said[warp]) said[warp] = most;
+                }
             }
+            if (first) bound = max(bound, floor);
         }
     }
     if (warp == 0 && piece == p.splits - 1) {
         const int at = cut.head + cut.vecs * N + lane;
         float least = 0.f;
-        if constexpr (TOP) least = least_of(shared_best.bound, false);
+        if constexpr (TOP) least = least_of(bound, false);
         single(at, at < p.vocab, least);
     }
 
@@ -318,7 +391,7 @@ k_token_rows(const __grid_constant__ TokenRows p) {
     for (int k = 16; k; k /= 2)
         a.join(__shfl_xor_sync(ALL, a.m, k), __shfl_xor_sync(ALL, a.s, k), __shfl_xor_sync(ALL, a.d, k));
     if (lane == 0) sums[warp] = a;
-    if constexpr (TOP) settle(shared_best, top);
+    if constexpr (TOP) gather(shared_best, top);
     else __syncthreads();
     a = sums[0];
     for (int w = 1; w < TH / 32; ++w) a.join(sums[w].m, sums[w].s, sums[w].d);
@@ -348,7 +421,7 @@ k_token_rows(const __grid_constant__ TokenRows p) {
         for (int i = 0; i < p.splits; ++i)
             a.join(__shfl_sync(ALL, mine.m, i), __shfl_sync(ALL, mine.s, i), __shfl_sync(ALL, mine.d, i));
         if constexpr (TOP) {
-            for (int i = tid; i < p.splits * top; i += TH) shared_best.key[i] = __ldcg(&part[i / top].key[i % top]);
+            for (int i = tid; i < p.splits * top; i += TH) shared_best.all[i] = __ldcg(&part[i / top].key[i % top]);
             if (tid == 0) shared_best.n = p.splits * top;
             settle(shared_best, top);
         }
@@ -444,7 +517,7 @@ static int row_pieces(int rows, int vocab, int size, int threads, int blocks, in
 }
 
 int token_splits(int rows, int vocab, hwr_dtype dtype, bool top, int nsm) {
-    return row_pieces(rows, vocab, dtype == HWR_F32 ? 4 : 2, threads_of(top), (top ? 4 : 8) * nsm, TOKEN_SPLITS);
+    return row_pieces(rows, vocab, dtype == HWR_F32 ? 4 : 2, threads_of(top), (top ? TK_FEW : 8) * nsm, TOKEN_SPLITS);
 }
 
 static cudaLaunchConfig_t early(int64_t grid, int threads, cudaStream_t s, cudaLaunchAttribute *at) {
@@ -460,16 +533,19 @@ static cudaLaunchConfig_t early(int64_t grid, int threads, cudaStream_t s, cudaL
 }
 
 template <int DT>
-static cudaError_t rows_of(const TokenRows &p, const cudaLaunchConfig_t &cfg) {
-    return p.top ? cudaLaunchKernelEx(&cfg, k_token_rows<DT, true>, p) : cudaLaunchKernelEx(&cfg, k_token_rows<DT, false>, p);
+static cudaError_t rows_of(const TokenRows &p, int nsm, const cudaLaunchConfig_t &cfg) {
+    constexpr int blocks = DT == HWR_F32 ? 8 : DT == HWR_BF16 ? 10 : 9;
+    if (!p.top) return cudaLaunchKernelEx(&cfg, k_token_rows<DT, false, blocks>, p);
+    return (int64_t)p.rows * p.splits <= TK_FEW * nsm ? cudaLaunchKernelEx(&cfg, k_token_rows<DT, true, TK_FEW>, p)
+                                                      : cudaLaunchKernelEx(&cfg, k_token_rows<DT, true, TK_LOT>, p);
 }
 
-cudaError_t launch_token_rows(const TokenRows &p, hwr_dtype dtype, cudaStream_t s) {
+cudaError_t launch_token_rows(const TokenRows &p, hwr_dtype dtype, int nsm, cudaStream_t s) {
     cudaLaunchAttribute at[1];
     const cudaLaunchConfig_t cfg = early((int64_t)p.rows * p.splits, threads_of(p.top > 0), s, at);
-    return dtype == HWR_F32    ? rows_of<HWR_F32>(p, cfg)
-           : dtype == HWR_BF16 ? rows_of<HWR_BF16>(p, cfg)
-                               : rows_of<HWR_F16>(p, cfg);
+    return dtype == HWR_F32    ? rows_of<HWR_F32>(p, nsm, cfg)
+           : dtype == HWR_BF16 ? rows_of<HWR_BF16>(p, nsm, cfg)
+                               : rows_of<HWR_F16>(p, nsm, cfg);
 }
 
 cudaError_t launch_token_grad(TokenGrad p, hwr_dtype dtype, int nsm, cudaStream_t s) {

@@ -278,7 +278,7 @@ struct TokenRows {
     uint32_t *arrivals;               // [rows] zeroed once, self-resetting
 };
 int token_splits(int rows, int vocab, hwr_dtype dtype, bool top, int nsm);
-cudaError_t launch_token_rows(const TokenRows &p, hwr_dtype dtype, cudaStream_t s);
+cudaError_t launch_token_rows(const TokenRows &p, hwr_dtype dtype, int nsm, cudaStream_t s);
 struct TokenGrad {
     int rows, vocab, splits;
     const void *logits;

@@ -160,7 +160,7 @@ extern "C" hwr_status hwr_token_logprobs(hwr_ops *c, const hwr_logits *l, int32_
     if (p.splits > 1) OK(reserve(c, (size_t)l->rows * p.splits * sizeof(TokenPart)));
     p.part = (TokenPart *)c->ws;
     p.arrivals = c->arrivals + ARRIVALS_ROWS;
-    CK(c, launch_token_rows(p, l->dtype, c->stream), "token kernel");
+    CK(c, launch_token_rows(p, l->dtype, c->nsm, c->stream), "token kernel");
     return HWR_OK;
 }
 

@@ -61,7 +61,7 @@ def best_of(z, top):
 
 
 SHAPES = [(1, 1), (1, 5), (3, 7), (2, 31), (5, 32), (4, 33), (7, 255), (3, 1000), (6, 1023), (1, 4099), (2, 8192), (400, 257),
-          (1, 32_768), (9, 50_001), (1, 200_003), (700, 3001), (65, 20_000)]
+          (1, 32_768), (9, 50_001), (1, 200_003), (700, 3001), (65, 20_000), (461, 20_001), (458, 30_001)]
 
 
 @pytest.mark.parametrize("shape", SHAPES)
