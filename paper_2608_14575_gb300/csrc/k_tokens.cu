@@ -230,7 +230,8 @@ __device__ __forceinline__ const char *row_at(const void *p, int64_t row, int64_
 template <bool TOP>
 __device__ __forceinline__ void finish(const TokenRows &p, int64_t row, const Sums &a, uint64_t key, float z, bool has,
                                        int lane) {
-    const bool empty = a.m == -INFINITY;              // nothing but -inf
+    // nothing but -inf (the maximum leaves NaN out, the sums do not)
+    const bool empty = a.m == -INFINITY && a.s == 0.f;
     const float ls = empty ? -INFINITY : logf(a.s);
     if (lane == 0) {
         p.logprob[row] = !has ? 0.f : empty ? z : (z - a.m) - ls;
@@ -463,7 +464,7 @@ k_token_grad(const __grid_constant__ TokenGrad p) {
     const int token = p.token ? p.token[row] : -1;
     float m = p.stats[2 * row];
     const float ls = p.stats[2 * row + 1], h = p.entropy[row];
-    const bool empty = m == -INFINITY;
+    const bool empty = m == -INFINITY;    // (beside NaN log S is NaN, and all of the gradient)
     const float a = p.da && (uint32_t)token < (uint32_t)p.vocab && !empty ? p.da[row] : 0.f;
     const float b = p.db ? p.db[row] : 0.f;
     if (empty) m = 0.f;

@@ -257,3 +257,33 @@ def test_refusals(ops):
     with pytest.raises((TypeError, ValueError)):
         ops.token_logprobs_backward(one, z, token, got, out=torch.empty(3, 50, device="cuda"))
     assert torch.equal(ops.token_logprobs(z, token).logprob, got.logprob)
+
+
+@pytest.mark.parametrize("V", [1, 37, 3000, 200_003])
+@pytest.mark.parametrize("dt", [F32, BF, HF])
+def test_rows_of_nan_and_nothing_else(ops, V, dt):
+    """Nothing but NaN, or NaN beside masked values (in one place of the row, whose pieces
+    may have none): NaN as in any row, not the results of a row of -inf."""
+    nan = float("nan")
+    z = logits_of(6, V, dt)
+    top = min(V, 5)
+    clean = {n: ops.token_logprobs(z, None, top=n) for n in (0, top)}
+    z[1] = nan
+    z[2], z[3], z[4] = -INF, -INF, -INF
+    z[2, 0], z[3, V // 2], z[4, V - 1] = nan, nan, nan
+    token = torch.full((6,), V - 1, device="cuda", dtype=torch.int32)
+    one = torch.ones(6, device="cuda")
+    for n in (0, top):
+        got = ops.token_logprobs(z, token, top=n)
+        assert got.logprob[1:5].isnan().all() and got.entropy[1:5].isnan().all()
+        for k in ("entropy", "stats"):
+            assert torch.equal(getattr(got, k)[[0, 5]], getattr(clean[n], k)[[0, 5]])
+        if n:
+            assert got.top_logprob[1:5].isnan().all()
+            assert got.top_token[1].tolist() == list(range(n))       # (by index, and the masked ones first)
+            if V > 5:
+                assert got.top_token[2].tolist() == list(range(1, n + 1))
+                assert got.top_token[4].tolist() == list(range(n))
+        for a, b in ((one, one), (one, None), (None, one)):
+            dz = ops.token_logprobs_backward(a, z, token, got, dentropy=b)
+            assert dz[1:5].isnan().all() and dz[[0, 5]].isfinite().all()
