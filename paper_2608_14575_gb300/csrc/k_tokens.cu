@@ -88,7 +88,7 @@ static_assert(TK_ROOM % TK_READ == 0, "lists are filled up to whole reads");
 // Keys of a warp's candidates, and of a block's.
 struct alignas(16) Best {
     uint64_t key[TK_WARPS][TK_ROOM], kept[TK_WARPS][32], all[TK_ALL], sorted[32];
-    uint32_t most[2][TK_WARPS];           // of the first step, and of the candidates
+    uint32_t most[3][TK_WARPS];           // of the first step, now (raised), and of the candidates
     int offered[TK_WARPS];                // more than there is room for: some are missing
     int n;
 };
@@ -202,9 +202,9 @@ __device__ __forceinline__ void gather(Best &b, int top) {
     const int n = b.offered[warp];
     const uint64_t one = lane < n ? b.key[warp][lane] : 0, two = lane + 32 < n ? b.key[warp][lane + 32] : 0;
     const uint32_t most = most_of((uint32_t)((one > two ? one : two) >> 32), top);
-    if (lane == 0) b.most[1][warp] = most;
+    if (lane == 0) b.most[2][warp] = most;
     __syncthreads();
-    const uint32_t bound = least_of_all(b.most[1]);
+    const uint32_t bound = least_of_all(b.most[2]);
     if (one && (uint32_t)(one >> 32) >= bound) b.all[atomicAdd(&b.n, 1)] = one;
     if (two && (uint32_t)(two >> 32) >= bound) b.all[atomicAdd(&b.n, 1)] = two;
     settle(b, top);
@@ -333,10 +333,10 @@ k_token_rows(const __grid_constant__ TokenRows p) {
         if constexpr (TOP) {
             Best &best = shared_best;
             const bool first = b == v0;
-            volatile uint32_t *said = best.most[0];
+            volatile uint32_t *said = best.most[1];
             if (first) {
                 const uint32_t most = most_of(order_of(mx), top);
-                if (lane == 0) said[warp] = most;
+                if (lane == 0) best.most[0][warp] = said[warp] = most;
                 __syncthreads();
             }
             // what `top` values reach, of any index (other warps may be ahead)
@@ -371,7 +371,8 @@ k_token_rows(const __grid_constant__ TokenRows p) {
                     if (lane == 0 && most > said[warp]) said[warp] = most;
                 }
             }
-            if (first) bound = max(bound, floor);
+            // (not `floor`: a warp ahead may have raised it by values of higher indices than mine)
+            if (first) bound = max(bound, least_of_all(best.most[0]));
         }
     }
     if (warp == 0 && piece == p.splits - 1) {
