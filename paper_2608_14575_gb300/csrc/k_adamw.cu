@@ -323,7 +323,8 @@ k_adamw(const __grid_constant__ AdamWStep p) {
         if (BITS == 8) now = next;
         else if (more) now.load(p, first);
     }
-    // the last block of the call to have read the step's number counts it up
+    // the last block of the call to have read the step's number (all of its threads) counts it up
+    __syncthreads();
     if (tid == 0 && atomicAdd(p.arrivals, 1u) == p.blocks - 1) {
         *p.arrivals = 0;
         if (!skip) *p.step = t;

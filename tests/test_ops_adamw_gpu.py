@@ -297,3 +297,29 @@ def test_refusals(ops):
     assert torch.equal(p, held) and int(state.step) == 0
     ops.adamw_step(state, [g], lr=0.1)
     assert int(state.step) == 1
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_every_thread_reads_the_same_step_number(ops, bits):
+    """Early steps, whose corrections differ most from one to the next, over a few blocks that
+    end at different times (some have little to do, some no gradient): the same start gives
+    the same bits, again and again, and the number goes up by one."""
+    sizes = [2048, 1, 2047, 300, 2048 * 3 + 5]
+    start = [normal(n, seed=1) for n in sizes]
+    grads = [normal(n, seed=2) for n in sizes]
+    grads[3] = None
+    params = [p.clone() for p in start]
+    state = ops.adamw_state(params, bits=bits)
+    written = params + [t.view(torch.uint8) for t in state.m + state.v]
+    held = [t.clone() for t in written]
+    first = None
+    for _ in range(300):
+        for t, h in zip(written, held):
+            t.copy_(h)
+        state.step.zero_()
+        for n in (1, 2):
+            ops.adamw_step(state, grads, lr=0.1, seed=4)
+        got = [t.clone() for t in written] + [state.step.clone()]
+        first = first or got
+        assert all(torch.equal(a, b) for a, b in zip(got, first))
+    assert int(state.step) == 2
