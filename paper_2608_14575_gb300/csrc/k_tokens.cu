@@ -99,7 +99,7 @@ __device__ __forceinline__ float least_of(uint32_t bound, bool equal) { return v
 // A thread's values at or above `least`, N from index i on, the largest of which is given,
 // to its warp's candidates.  (Few threads have any, after the first steps.)
 template <int N>
-__device__ __forceinline__ void offer(Best &b, const float (&z)[N], float largest, int i, float least) {
+__device__ __forceinline__ void offer(Best &b, const float (&z)[N], float largest, uint32_t i, float least) {
     if (!(largest >= least)) return;
     const int warp = threadIdx.x >> 5;
     uint32_t mine = 0;
@@ -113,7 +113,7 @@ __device__ __forceinline__ void offer(Best &b, const float (&z)[N], float larges
         float v = z[0];
 #pragma unroll
         for (int k = 1; k < N; ++k) v = j == k ? z[k] : v;
-        if (at < TK_ROOM) b.key[warp][at] = (uint64_t)order_of(v) << 32 | (uint32_t)~(i + j);
+        if (at < TK_ROOM) b.key[warp][at] = (uint64_t)order_of(v) << 32 | ~(i + j);
     }
 }
 
@@ -289,9 +289,10 @@ k_token_rows(const __grid_constant__ TokenRows p) {
         s = s + e;
         d = fma2(e, x, d);
     };
-    // one value a lane of the first warp
-    const auto single = [&](int i, bool valid, float least) {
-        float z[1] = {valid ? Vec<DT>::load(base, i) : -INFINITY};
+    // one value a lane of the first warp (indices of lanes without one may pass 2^31, the most
+    // that a row has)
+    const auto single = [&](uint32_t i, bool valid, float least) {
+        float z[1] = {valid ? Vec<DT>::load(base, (int)i) : -INFINITY};
         if (z[0] > m) raise(z[0]);
         add(z[0], -INFINITY, m == -INFINITY ? 0.f : m);
         if constexpr (TOP) {
@@ -343,7 +344,7 @@ k_token_rows(const __grid_constant__ TokenRows p) {
             const uint32_t floor = __reduce_min_sync(ALL, lane < TK_WARPS ? said[lane] : ~0u);
             const float any = floor > MASKED ? value_of(floor) : -INFINITY;
             // (vectors beyond the last are -inf, below any `least`)
-            const int at = cut.head + (b + tid) * N;
+            const uint32_t at = (uint32_t)cut.head + (uint32_t)(b + tid) * N;
             const float least = fmaxf(least_of(bound, false), any);
             if (__any_sync(ALL, mx >= least)) {
                 const int before = best.offered[warp];
@@ -376,10 +377,10 @@ k_token_rows(const __grid_constant__ TokenRows p) {
         }
     }
     if (warp == 0 && piece == p.splits - 1) {
-        const int at = cut.head + cut.vecs * N + lane;
+        const uint32_t at = (uint32_t)(cut.head + cut.vecs * N) + lane;
         float least = 0.f;
         if constexpr (TOP) least = least_of(bound, false);
-        single(at, at < p.vocab, least);
+        single(at, at < (uint32_t)p.vocab, least);
     }
 
     Sums a = {m, 0.f, 0.f};

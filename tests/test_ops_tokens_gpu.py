@@ -287,3 +287,25 @@ def test_rows_of_nan_and_nothing_else(ops, V, dt):
         for a, b in ((one, one), (one, None), (None, one)):
             dz = ops.token_logprobs_backward(a, z, token, got, dentropy=b)
             assert dz[1:5].isnan().all() and dz[[0, 5]].isfinite().all()
+
+
+def test_the_longest_rows(ops):
+    """2^31 - 1 logits, the most that a row can have: seven of them behind its last vector.
+    All alike but for the last and one in the middle, q = e^{z - m} / S in closed form."""
+    V = 2 ** 31 - 1
+    z = torch.zeros(1, V, device="cuda", dtype=BF)
+    z[0, V - 1], z[0, 1 << 30] = 24.0, 23.0
+    token = torch.tensor([V - 1], device="cuda", dtype=torch.int32)
+    log_s = math.log(1 + math.exp(-1) + (V - 2) * math.exp(-24))
+    for top in (0, 4):
+        got = ops.token_logprobs(z, token, top=top)
+        # A thread's two sums count their ones exactly (fewer than 2^24).  Beside the 23 (a sum
+        # of 1 for it) each e^-23 more may be lost whole: 2^31 / (32 * 128) / 2 of them.
+        assert abs(float(got.logprob[0]) + log_s) <= 2.0 ** 18 * math.exp(-24) + 2.0 ** -19
+        if top:
+            assert got.top_token[0].tolist() == [V - 1, 1 << 30, 0, 1]
+    dz = ops.token_logprobs_backward(torch.ones(1, device="cuda"), z, token, got, out=z)
+    q = math.exp(float(got.logprob[0]))
+    assert float(dz[0, V - 1]) == pytest.approx(1 - q, rel=2.0 ** -7)
+    assert float(dz[0, 0]) == pytest.approx(-q * math.exp(-24), rel=2.0 ** -7)
+    assert float(dz[0, V - 2]) == float(dz[0, 0])
