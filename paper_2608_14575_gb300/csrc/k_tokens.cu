@@ -472,7 +472,8 @@ k_token_grad(const __grid_constant__ TokenGrad p) {
     if (empty) m = 0.f;
     auto grad = [&](float z, int at) {
         const float lq = max_nan((z - m) - ls, FAR), q = exp2_fast(lq * LOG2E);
-        const float g = -q * fmaf(b, lq + h, a);
+        // (no product with a distance where q is 0: a large b would make it infinite)
+        const float g = -q * fmaf(b, q > 0.f ? lq + h : 0.f, a);
         return at == token ? g + a : g;
     };
     // (vectors where both rows begin alike, else value by value)

@@ -309,3 +309,15 @@ def test_the_longest_rows(ops):
     assert float(dz[0, V - 1]) == pytest.approx(1 - q, rel=2.0 ** -7)
     assert float(dz[0, 0]) == pytest.approx(-q * math.exp(-24), rel=2.0 ** -7)
     assert float(dz[0, V - 2]) == float(dz[0, 0])
+
+
+@pytest.mark.parametrize("dt", [F32, BF, HF])
+def test_large_gradients_at_masked_logits(ops, dt):
+    """However large dentropy is, a logit of probability 0 has the gradient 0."""
+    z = torch.full((2, 5000), -INF, device="cuda", dtype=dt)
+    z[0, 7] = 1.0                                        # q = 1: log q + entropy = 0
+    z[1, [3, 4000]] = 2.0
+    got = ops.token_logprobs(z, None)
+    for b in (1e9, -1e30, 3e38):
+        dz = ops.token_logprobs_backward(None, z, None, got, dentropy=torch.full((2,), b, device="cuda"))
+        assert (dz[z == -INF] == 0).all() and dz[0, 7] == 0
