@@ -268,6 +268,8 @@ k_adamw(const __grid_constant__ AdamWStep p) {
     Chunk<BITS> now;
     int i = blockIdx.x;
     if (!skip && i < p.chunks) now.load(p, first);
+    // (all threads have read the step's number before thread 0 can say so below)
+    __syncthreads();
     for (; !skip && i < p.chunks; i += gridDim.x) {
         // 8 bits: the next chunk's loads are under way while this one's codes are made
         Chunk<BITS> next;
@@ -323,8 +325,7 @@ k_adamw(const __grid_constant__ AdamWStep p) {
         if (BITS == 8) now = next;
         else if (more) now.load(p, first);
     }
-    // the last block of the call to have read the step's number (all of its threads) counts it up
-    __syncthreads();
+    // the last block of the call to have read the step's number counts it up
     if (tid == 0 && atomicAdd(p.arrivals, 1u) == p.blocks - 1) {
         *p.arrivals = 0;
         if (!skip) *p.step = t;
