@@ -216,3 +216,26 @@ def test_refusals(ops):
         assert e.value.status == 7
     choice, p = M.choices(s, 2, False)
     inside(ops.expert_layer(x, w_in, w_out, **good), M.expert_layer(x, w_in, w_out, choice, p, "silu"))
+
+
+@pytest.mark.parametrize("dt", [BF, HF])
+def test_gelu_of_negative_values(ops, dt):
+    """u Phi(u) keeps its relative accuracy far below 0: one whole or half number u a row (its
+    product with 1 is exact), gates (powers of two) that bring the results near 1.  The
+    argument's two roundings (2^-24 each) move erfc(-u / sqrt 2) by u^2 2^-23 of it at most
+    (its logarithm's slope is below u^2 + 1 in u's relative change); erfcf is within 4 units
+    of the last place, two products round once each; and the hidden value's terms."""
+    u = -torch.arange(1, 25, device="cuda", dtype=torch.float64) / 2
+    T = u.numel()
+    x = torch.zeros(T, 8, device="cuda", dtype=dt)
+    x[:, 0] = u
+    w_in, w_out = torch.zeros(1, 16, 8, device="cuda", dtype=dt), torch.zeros(1, 8, 16, device="cuda", dtype=dt)
+    w_in[0, 3, 0] = w_out[0, :, 3] = 1
+    want = u * torch.special.erfc(-u * 2 ** -0.5) / 2
+    gates = torch.exp2(-torch.floor(torch.log2(want.abs())))[:, None].float()
+    y = ops.expert_layer(x, w_in, w_out, choice=torch.zeros(T, 1, device="cuda", dtype=torch.int32), gates=gates,
+                         activation="gelu").double()
+    want = (want * gates[:, 0].double())[:, None]
+    term, unit = (2.0 ** -15, 2.0 ** -8) if dt == BF else (2.0 ** -20, 2.0 ** -11)
+    rel = (u * u + 1) * 2.0 ** -23 + 16 * 2.0 ** -23 + term
+    assert ((y - want).abs() <= want.abs() * (rel[:, None] + unit * (1 + rel[:, None]))).all()
