@@ -246,9 +246,9 @@ hwr_status hwr_adamw_destroy(hwr_ops *ops, hwr_adamw *optimizer); /* synchronise
  *   h = act(W_in[e][0 .. hidden) x[t]) * (W_in[e][hidden ..) x[t])   (gated)
  * With scores [rows][groups], the choices are the `top` largest scores of a row (ties to
  * the lowest index; NaN and -inf are never chosen), and p the softmax over them, or
- * (over_all) over all of the row's scores.  Without, they are choice and gates
- * [rows][top]; a choice outside [0, groups) is none, the same one may come twice.  A row
- * without a choice gets zeros.  Experts that no row chooses are not read.
+ * (over_all) over all of the row's scores, NaN where one of those is.  Without, they are
+ * choice and gates [rows][top]; a choice outside [0, groups) is none, the same one may come
+ * twice.  A row without a choice gets zeros.  Experts that no row chooses are not read.
  * h is summed in fp32 and enters the second product as two terms within 2^-15 of it (in
  * fp16 layers 2^-20), at any magnitude; y is rounded once.
  */

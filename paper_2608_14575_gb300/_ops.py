@@ -359,9 +359,10 @@ class Operators:
         y[t] = sum of p[t, j] w_out[e] h over the row's choices e, with
         w_in [groups][2 F][K] h = act(w_in[e][:F] x[t]) * (w_in[e][F:] x[t]), with
         [groups][F][K] h = act(w_in[e] x[t]); w_out [groups][N][F].  ``scores``
-        [rows][groups] fp32: the ``top`` largest are the choices, p the softmax over them (``over_all``:
-        over all scores).  Or ``choice`` [rows][top] int32 (outside [0, groups): none) and
-        ``gates`` [rows][top] fp32, the p.  ``activation``: "silu", "gelu" (u Phi(u)), "relu"."""
+        [rows][groups] fp32: the ``top`` largest are the choices (never NaN or -inf), p the
+        softmax over them (``over_all``: over all scores, NaN where one of those is).  Or
+        ``choice`` [rows][top] int32 (outside [0, groups): none) and ``gates`` [rows][top]
+        fp32, the p.  ``activation``: "silu", "gelu" (u Phi(u)), "relu"."""
         if activation not in ACTIVATIONS:
             raise ValueError(f"activation {activation!r}: want one of {', '.join(ACTIVATIONS)}")
         y = self.native.expert_layer(self.ctx, self._current(), x, w_in, w_out, scores, top, over_all, choice,

@@ -283,9 +283,13 @@ template <int LANE>
 __device__ __forceinline__ void choose(const float *s, int E, int top, bool over_all, int &choice, float &gate) {
     const int lane = threadIdx.x & 31;
     uint32_t order[LANE];
-#pragma unroll
-    for (int i = 0; i < LANE; ++i) order[i] = lane + i * 32 < E ? score_order(__ldg(s + lane + i * 32)) : 0u;
     float largest = 0.f, mine = 0.f, total = 0.f;
+#pragma unroll
+    for (int i = 0; i < LANE; ++i) {
+        const float v = lane + i * 32 < E ? __ldg(s + lane + i * 32) : -INFINITY;
+        order[i] = score_order(v);
+        if (v != v) total = v;            // (never chosen, but part of the sum over all)
+    }
     choice = -1;
     for (int j = 0; j < top; ++j) {
         uint32_t best = 0;

@@ -239,3 +239,22 @@ def test_gelu_of_negative_values(ops, dt):
     term, unit = (2.0 ** -15, 2.0 ** -8) if dt == BF else (2.0 ** -20, 2.0 ** -11)
     rel = (u * u + 1) * 2.0 ** -23 + 16 * 2.0 ** -23 + term
     assert ((y - want).abs() <= want.abs() * (rel[:, None] + unit * (1 + rel[:, None]))).all()
+
+
+@pytest.mark.parametrize("E", [5, 40, 300])
+def test_nan_scores(ops, E):
+    """A NaN is never chosen.  Among the chosen scores there is none; a softmax over all of a
+    row's scores (over_all) has one in its sum, and the row is NaN."""
+    T, D, F, N, top = 6, 64, 48, 40, 2
+    x, w_in, w_out = layer(T, E, D, F, N, True, BF)
+    s = scores_of(T, E)
+    bad = s.clone()
+    bad[1, E - 1], bad[3, 0], bad[4] = float("nan"), float("nan"), float("nan")
+    bad[3, 1] = float("-inf")
+    masked = torch.where(bad.isnan(), torch.full_like(bad, float("-inf")), bad)
+    y = ops.expert_layer(x, w_in, w_out, scores=bad, top=top)
+    assert torch.equal(y, ops.expert_layer(x, w_in, w_out, scores=masked, top=top)) and (y[4] == 0).all()
+    y = ops.expert_layer(x, w_in, w_out, scores=bad, top=top, over_all=True)
+    assert y[1].isnan().all() and y[3].isnan().all() and (y[4] == 0).all()      # (4: no choice)
+    keep = torch.tensor([0, 2, 5], device="cuda")
+    assert torch.equal(y[keep], ops.expert_layer(x, w_in, w_out, scores=masked, top=top, over_all=True)[keep])
