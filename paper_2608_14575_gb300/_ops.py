@@ -342,8 +342,9 @@ class Operators:
 
     def adamw_step(self, state: AdamWState, grads, lr, betas=(0.9, 0.999), eps: float = 1e-8,
                    weight_decay: float = 0.01, norm=None, max_norm: float = float("inf"), seed: int = 0):
-        """One step (``state.step`` counts it): ``grads`` a gradient (fp32, bf16, fp16)
-        or None for each parameter, ``lr`` a number or an fp32 tensor on the device.  With ``norm``
+        """One step (``state.step`` counts it): ``grads`` a gradient (fp32, bf16, fp16;
+        contiguous, of its shape) or None for each parameter, ``lr`` a number or an fp32 tensor on the
+        device.  With ``norm``
         (of ``clip_gradients``, max_norm inf: left as they are) the gradients are taken times
         min(1, max_norm / (norm + 1e-6)), and a step whose norm is not finite is left
         out.  ``seed``: of the 8-bit moments' rounding."""

@@ -641,7 +641,7 @@ PyObject *token_logprobs_backward(PyObject *, PyObject *const *a, Py_ssize_t n) 
 // An optimizer and the tensors that it writes.
 struct Optimizer {
     hwr_adamw *o = nullptr;
-    std::vector<int64_t> n;
+    std::vector<std::vector<int64_t>> shapes;
     std::vector<at::Tensor> tensors;
     std::vector<const void *> grads;      // of a call
     std::vector<hwr_dtype> dtypes;
@@ -690,7 +690,7 @@ PyObject *adamw_create(PyObject *, PyObject *const *a, Py_ssize_t n) {
                 e.m_scale = (float *)given(4, {blocks}, at::kFloat);
                 e.v_scale = (float *)given(5, {blocks}, at::kFloat);
             }
-            o.n.push_back(e.n);
+            o.shapes.push_back(p.sizes().vec());
         }
         const at::Tensor &step = tensor(a[9], "step");
         int32_t *at = (int32_t *)const_cast<void *>(contiguous(c, step, {1}, at::kInt, "step"));
@@ -710,9 +710,9 @@ PyObject *adamw_step(PyObject *, PyObject *const *a, Py_ssize_t n) {
         Context &c = context(a[0]);
         Optimizer &o = *(Optimizer *)address(a[2]);
         if (!PyList_Check(a[3])) throw TypeError("grads: want a list of tensors");
-        if ((size_t)PyList_GET_SIZE(a[3]) != o.n.size())
-            throw ValueError(std::to_string(PyList_GET_SIZE(a[3])) + " gradients for " + std::to_string(o.n.size()) + " parameters");
-        for (size_t i = 0; i < o.n.size(); ++i) {
+        if ((size_t)PyList_GET_SIZE(a[3]) != o.shapes.size())
+            throw ValueError(std::to_string(PyList_GET_SIZE(a[3])) + " gradients for " + std::to_string(o.shapes.size()) + " parameters");
+        for (size_t i = 0; i < o.shapes.size(); ++i) {
             PyObject *item = PyList_GET_ITEM(a[3], (Py_ssize_t)i);
             o.grads[i] = nullptr;
             o.dtypes[i] = HWR_F32;
@@ -720,8 +720,7 @@ PyObject *adamw_step(PyObject *, PyObject *const *a, Py_ssize_t n) {
             const at::Tensor &g = tensor(item, "a gradient");
             o.dtypes[i] = any_float(g, "a gradient");
             on_device(c, g, "a gradient");
-            if (g.numel() != o.n[i])
-                throw ValueError("gradient " + std::to_string(i) + " has " + std::to_string(g.numel()) + " elements, its parameter " + std::to_string(o.n[i]));
+            shaped(g, o.shapes[i], "a gradient");
             if (!g.is_contiguous()) throw ValueError("want contiguous gradients");
             o.grads[i] = g.data_ptr();
         }

@@ -323,3 +323,18 @@ def test_every_thread_reads_the_same_step_number(ops, bits):
         first = first or got
         assert all(torch.equal(a, b) for a, b in zip(got, first))
     assert int(state.step) == 2
+
+
+def test_gradients_of_another_shape(ops):
+    """A gradient has its parameter's shape: one with as many elements (a transposed one that
+    was made contiguous) is refused, and nothing changes."""
+    p = normal(600).view(20, 30)
+    state = ops.adamw_state([p])
+    before = p.clone()
+    g = normal(600, seed=1).view(20, 30)
+    for bad in (g.t().contiguous(), g.view(-1), g.view(1, 20, 30)):
+        with pytest.raises(ValueError):
+            ops.adamw_step(state, [bad], lr=0.1)
+    assert torch.equal(p, before) and int(state.step) == 0
+    ops.adamw_step(state, [g], lr=0.1)
+    assert int(state.step) == 1 and not torch.equal(p, before)
