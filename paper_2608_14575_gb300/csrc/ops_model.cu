@@ -276,12 +276,21 @@ extern "C" hwr_status hwr_adamw_create(hwr_ops *c, int32_t n, const hwr_adamw_te
     return HWR_OK;
 }
 
+// Whether an optimizer is one of the context's.
+static bool owned(const hwr_ops *c, const hwr_adamw *o) {
+    const hwr_adamw *at = c->optimizers;
+    while (at && at != o) at = at->next;
+    return at;
+}
+
 extern "C" hwr_status hwr_adamw_step(hwr_ops *c, const hwr_adamw *o, const hwr_adamw_options *a,
                                      const void *const *grads, const hwr_dtype *dtypes) {
     if (!c) return HWR_ERR_INVALID_ARG;
     ApiRange range("hwr_adamw_step");
     OK(ready(c));
-    if (!o || !a || (o->n && (!grads || !dtypes))) return fail(c, HWR_ERR_INVALID_ARG, "NULL argument");
+    if (!o || !a) return fail(c, HWR_ERR_INVALID_ARG, "NULL argument");
+    if (!owned(c, o)) return fail(c, HWR_ERR_INVALID_ARG, "not an optimizer of this context");
+    if (o->n && (!grads || !dtypes)) return fail(c, HWR_ERR_INVALID_ARG, "NULL argument");
     if (!(a->beta1 >= 0 && a->beta1 < 1) || !(a->beta2 >= 0 && a->beta2 < 1))
         return fail(c, HWR_ERR_INVALID_ARG, "betas %g, %g", a->beta1, a->beta2);
     if (!(a->eps >= 0) || !(a->weight_decay >= 0) || (!a->lr_device && !(a->lr >= 0)))
@@ -339,9 +348,7 @@ extern "C" hwr_status hwr_adamw_step(hwr_ops *c, const hwr_adamw *o, const hwr_a
 extern "C" hwr_status hwr_adamw_destroy(hwr_ops *c, hwr_adamw *o) {
     if (!o) return HWR_OK;
     if (!c) return HWR_ERR_INVALID_ARG;
-    hwr_adamw **at = &c->optimizers;
-    while (*at && *at != o) at = &(*at)->next;
-    if (!*at) return fail(c, HWR_ERR_INVALID_ARG, "not an optimizer of this context");
+    if (!owned(c, o)) return fail(c, HWR_ERR_INVALID_ARG, "not an optimizer of this context");
     bool captured;
     OK(capturing(c, &captured));
     if (captured || o->held) {          // (during a capture nothing is waited for or freed)
@@ -352,6 +359,8 @@ extern "C" hwr_status hwr_adamw_destroy(hwr_ops *c, hwr_adamw *o) {
         cudaFree(o->tensors);
         cudaGetLastError();
     }
+    hwr_adamw **at = &c->optimizers;
+    while (*at != o) at = &(*at)->next;
     *at = o->next;
     delete[] o->chunk0;
     delete o;

@@ -338,3 +338,19 @@ def test_gradients_of_another_shape(ops):
     assert torch.equal(p, before) and int(state.step) == 0
     ops.adamw_step(state, [g], lr=0.1)
     assert int(state.step) == 1 and not torch.equal(p, before)
+
+
+def test_an_optimizer_of_another_context_is_refused(ops):
+    """By the C entry too, whose contexts have streams and counters of their own."""
+    other = H.Operators()
+    p = normal(3000)
+    state = ops.adamw_state([p])
+    before = p.clone()
+    with pytest.raises(H.HwrError) as e:
+        other.native.adamw_step(other.ctx, other._current(), state.handle, [normal(3000, seed=1)], 0.1, 0.9, 0.999, 1e-8,
+                                0.0, None, math.inf, 0)
+    assert e.value.status == 1
+    assert torch.equal(p, before) and int(state.step) == 0
+    other.adamw_step(other.adamw_state([p]), [normal(3000, seed=1)], lr=0.1)      # (it stays usable)
+    assert not torch.equal(p, before)
+    other.close()
