@@ -13,6 +13,7 @@ extern "C" hwr_status hwr_ops_create(void *cuda_stream, hwr_ops **out) {
     hwr_ops *c = new (std::nothrow) hwr_ops;
     if (!c) return fail(nullptr, HWR_ERR_OOM, "host allocation failed");
     if (const char *e = getenv("HWR_TEST_FAIL_ALLOC")) c->fail_at = atol(e);
+    if (const char *e = getenv("HWR_TEST_FAIL_LAUNCH")) c->fail_launch = atol(e);
     if (const char *e = getenv("HWR_TEST_STALL")) c->test_stall = atoi(e) != 0;
     if (const char *e = getenv("HWR_TEST_DEVICE")) c->test_device = atoi(e);
     const Unwatched memory;

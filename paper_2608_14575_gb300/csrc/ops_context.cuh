@@ -90,6 +90,7 @@ struct hwr_ops {
     int test_stall = 0;                                  // HWR_TEST_STALL (see hwr_api.cu)
     int test_device = 0;                                 // HWR_TEST_DEVICE: how far off the current device seems
     long fail_at = 0, allocs = 0;                        // HWR_TEST_FAIL_ALLOC
+    long fail_launch = 0, launches = 0;                  // HWR_TEST_FAIL_LAUNCH: of optimizers' kernels, this one fails
 };
 
 static inline hwr_status fail(hwr_ops *c, hwr_status s, const char *fmt, ...) {

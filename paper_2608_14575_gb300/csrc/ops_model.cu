@@ -340,7 +340,14 @@ extern "C" hwr_status hwr_adamw_step(hwr_ops *c, const hwr_adamw *o, const hwr_a
             p.grad[i - t0] = grads[i];
             p.dtype[i - t0] = (uint8_t)dtypes[i];
         }
-        CK(c, launch_adamw(p, o->bits, adamw_grid(p.chunks, o->bits, c->nsm), c->stream), "optimizer kernel");
+        const cudaError_t e = c->fail_launch > 0 && ++c->launches == c->fail_launch
+                                  ? cudaErrorMemoryAllocation
+                                  : launch_adamw(p, o->bits, adamw_grid(p.chunks, o->bits, c->nsm), c->stream);
+        // (whatever the reason: some tensors have made the step and others not, and the blocks'
+        // count is left between)
+        if (e != cudaSuccess && k > 0)
+            return fail(c, HWR_ERR_CUDA, "optimizer kernel, after others of the step: %s", cudaGetErrorString(e));
+        CK(c, e, "optimizer kernel");
     }
     return HWR_OK;
 }

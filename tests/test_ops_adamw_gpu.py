@@ -354,3 +354,33 @@ def test_an_optimizer_of_another_context_is_refused(ops):
     other.adamw_step(other.adamw_state([p]), [normal(3000, seed=1)], lr=0.1)      # (it stays usable)
     assert not torch.equal(p, before)
     other.close()
+
+
+def test_a_launch_that_fails(ops, monkeypatch):
+    """Of a step's several launches (over 256 tensors each): the first one's failure leaves
+    everything as it is and the context usable; a later one's, when some tensors have made the
+    step, breaks the context whatever the error, and other contexts do not notice."""
+    params = [normal(40, seed=i) for i in range(300)]
+    grads = [normal(40, seed=i + 1000) for i in range(300)]
+    for failing in (1, 2):
+        monkeypatch.setenv("HWR_TEST_FAIL_LAUNCH", str(failing))
+        own = H.Operators()
+        monkeypatch.delenv("HWR_TEST_FAIL_LAUNCH")
+        before = [p.clone() for p in params]
+        state = own.adamw_state(params)
+        with pytest.raises(H.HwrError) as e:
+            own.adamw_step(state, grads, lr=0.1)
+        assert e.value.status == (3 if failing == 1 else 4)          # out of memory, or CUDA
+        assert int(state.step) == 0
+        if failing == 1:
+            assert all(torch.equal(a, b) for a, b in zip(params, before))
+            own.adamw_step(state, grads, lr=0.1)
+            assert int(state.step) == 1 and not torch.equal(params[-1], before[-1])
+        else:
+            with pytest.raises(H.HwrError) as e:
+                own.adamw_step(state, grads, lr=0.1)
+            assert e.value.status == 6                               # unusable
+            own.close()
+    state = ops.adamw_state(params)
+    ops.adamw_step(state, grads, lr=0.1)
+    assert int(state.step) == 1
