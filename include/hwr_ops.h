@@ -228,7 +228,7 @@ typedef struct {
  * memory once; synchronises the stream).  `step`, device, one int32: the number of steps
  * done, which each step counts up, so that captured steps go on counting.  It and the
  * tensors are the caller's, to be saved and restored; they go on existing as long as the
- * optimizer.  An optimizer goes with its context, if not before. */
+ * optimizer, and none of them overlaps another (INVALID_ARG).  An optimizer goes with its context, if not before. */
 typedef struct hwr_adamw hwr_adamw;
 hwr_status hwr_adamw_create(hwr_ops *ops, int32_t n, const hwr_adamw_tensor *tensors, int32_t bits,
                             int32_t *step, hwr_adamw **out);

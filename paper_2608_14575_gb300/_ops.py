@@ -323,7 +323,8 @@ class Operators:
                     step=None) -> AdamWState:
         """State of an AdamW run over fp32 tensors ``params``, with ``copies`` in bf16 or
         fp16 (None, or None for some) that each step rounds them to.  Moments of ``bits`` 32 or 8,
-        zeros unless they are given (lists as in ``AdamWState``), like ``step``."""
+        zeros unless they are given (lists as in ``AdamWState``), like ``step``.  None of these
+        tensors may overlap another."""
         import torch
         params = list(params)
         kind = torch.float8_e4m3fn if bits == 8 else torch.float32

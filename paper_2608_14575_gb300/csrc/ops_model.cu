@@ -3,6 +3,8 @@
 // step (declarations in include/hwr_ops.h).
 #include <math.h>
 
+#include <algorithm>
+
 #include "ops_context.cuh"
 
 // ---- a layer of experts ----------------------------------------------------------
@@ -197,6 +199,35 @@ extern "C" hwr_status hwr_token_logprobs_backward(hwr_ops *c, const hwr_logits *
 
 // ---- the optimizer's step ----------------------------------------------------------------
 
+// What a step writes has to lie nowhere twice: blocks take their elements in any order.
+static hwr_status check_apart(hwr_ops *c, int32_t n, const hwr_adamw_tensor *tensors, int32_t bits, const int32_t *step) {
+    struct Range {
+        uintptr_t begin, end;
+    };
+    Range *all = new (std::nothrow) Range[6 * (size_t)n + 1];
+    if (!all) return fail(c, HWR_ERR_OOM, "host allocation failed");
+    size_t k = 0;
+    const auto add = [&](const void *p, int64_t bytes) {
+        if (p && bytes) all[k++] = {(uintptr_t)p, (uintptr_t)p + (uintptr_t)bytes};
+    };
+    add(step, 4);
+    for (int i = 0; i < n; ++i) {
+        const hwr_adamw_tensor &t = tensors[i];
+        add(t.param, t.n * 4);
+        add(t.copy, t.n * 2);
+        add(t.m, t.n * (bits / 8));
+        add(t.v, t.n * (bits / 8));
+        if (bits == 32) continue;
+        add(t.m_scale, (t.n + ADAMW_BLOCK - 1) / ADAMW_BLOCK * 4);
+        add(t.v_scale, (t.n + ADAMW_BLOCK - 1) / ADAMW_BLOCK * 4);
+    }
+    std::sort(all, all + k, [](const Range &a, const Range &b) { return a.begin < b.begin; });
+    bool apart = true;
+    for (size_t i = 1; i < k; ++i) apart = apart && all[i - 1].end <= all[i].begin;
+    delete[] all;
+    return apart ? HWR_OK : fail(c, HWR_ERR_INVALID_ARG, "tensors overlap");
+}
+
 extern "C" hwr_status hwr_adamw_create(hwr_ops *c, int32_t n, const hwr_adamw_tensor *tensors, int32_t bits,
                                        int32_t *step, hwr_adamw **out) {
     if (!c) return HWR_ERR_INVALID_ARG;
@@ -224,6 +255,7 @@ extern "C" hwr_status hwr_adamw_create(hwr_ops *c, int32_t n, const hwr_adamw_te
         chunks += t.n > INT64_MAX / 2 ? INT32_MAX : (t.n + ADAMW_CHUNK - 1) / ADAMW_CHUNK;
         if (chunks >= INT32_MAX) return fail(c, HWR_ERR_UNSUPPORTED, "too many elements");
     }
+    OK(check_apart(c, n, tensors, bits, step));
     hwr_adamw *o = new (std::nothrow) hwr_adamw;
     const size_t bytes = n * sizeof(AdamWTensor) + (chunks ? chunks : 1) * sizeof(AdamWChunk);
     char *host = new (std::nothrow) char[bytes];

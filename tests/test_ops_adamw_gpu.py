@@ -384,3 +384,22 @@ def test_a_launch_that_fails(ops, monkeypatch):
     state = ops.adamw_state(params)
     ops.adamw_step(state, grads, lr=0.1)
     assert int(state.step) == 1
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_tensors_that_overlap_are_refused(ops, bits):
+    """What a step writes lies nowhere twice: the same parameter two times, parts of one, a
+    moment in another's place (two blocks would write it, in any order)."""
+    p, q = normal(3000), normal(3000, seed=1)
+    for params in ([p, q, p], [p, p[2999:]], [p[:2000], p[1999:]]):
+        with pytest.raises(H.HwrError) as e:
+            ops.adamw_state(params, bits=bits)
+        assert e.value.status == 1
+    m = [torch.zeros(3000, device="cuda", dtype=torch.float8_e4m3fn if bits == 8 else F32) for _ in range(2)]
+    for args in (dict(m=[m[0], m[0]]), dict(m=m, v=[m[1], m[0]]), dict(copies=[q.to(BF)] * 2)):
+        with pytest.raises(H.HwrError):
+            ops.adamw_state([p, q], bits=bits, **args)
+    # side by side, and empty ones anywhere, are fine
+    state = ops.adamw_state([p[:1500], p[1500:], q, p[700:700]], bits=bits)
+    ops.adamw_step(state, [normal(n, seed=2) for n in (1500, 1500, 3000, 0)], lr=0.1)
+    assert int(state.step) == 1
