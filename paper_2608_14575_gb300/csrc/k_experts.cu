@@ -24,9 +24,13 @@
 // The multiplications are warp-level MMAs: 16 rows of weights, 8 rows of x.  The
 // contraction's order is free, so a lane takes eight consecutive columns of a weight's
 // row in one 16-byte load, and the same of x.  h is summed in fp32 and enters the second
-// product as two terms that give 15 bits of it or more at any magnitude: two bf16 values
-// beside bf16 weights; beside fp16 weights, whose range is too small for it, two tf32
-// values, the weights widened to tf32 exactly.
+// product whole: beside bf16 weights as three bf16 terms.  (As two, 16 bits of it, one
+// bf16 result in 220 differed from that of fp32 hidden values, with three one in 1,070, as
+// many as another order of fp32 sums moves; 16 rows with 6 of 64 experts of 2,048 -> 2 x 1,408
+// took 128.5 us for 133, 64 rows with 4 of 24 of 1,024 -> 2 x 2,048 83.5 for 90.)  Beside fp16
+// weights, whose range is too small for it, as two tf32 values, within 2^-20 of it, the
+// weights widened to tf32 exactly: fp16 results are rounded to 2^-11, and a third would be
+// half as many multiplications again.
 #include "ops_internal.cuh"
 #include "umma.cuh"
 #include "values.cuh"
@@ -529,6 +533,14 @@ __device__ __forceinline__ void tf32_terms(float v, float &high, float &low) {
     low = m < 0x7f800000u ? v - high : v;
 }
 
+// The high bf16 term of a value, cut off as in bf16_terms, and what it leaves: two more
+// terms take the rest exactly (16 bits at most).
+__device__ __forceinline__ float bf16_cut(float v, uint16_t &high) {
+    const uint32_t u = __float_as_uint(v), m = u & 0x7fffffffu;
+    high = (uint16_t)((m - 1 < 0x7f7fffffu ? u - 1 : u) >> 16);
+    return m < 0x7f800000u ? v - __uint_as_float((uint32_t)high << 16) : v;
+}
+
 // What the block shares beside the routing's tables and the ring.
 template <int NB>
 struct Shared {
@@ -663,13 +675,13 @@ k_experts_in(const __grid_constant__ Experts p, const __grid_constant__ WeightMa
                 float v = activated(c[k / 4][i], p.act);
                 if (p.gated) v *= c[k / 4][i | 2];
                 if (f >= p.hidden) v = 0.f;              // (the second product reads whole 16 bytes)
-                const int64_t to = (int64_t)r.list[begin + column] * 2 * p.h_ld + f;
+                const int64_t to = (int64_t)r.list[begin + column] * expert_terms(F16) * p.h_ld + f;
                 if (F16) {
                     float *h = (float *)p.h + to;
                     tf32_terms(v, h[0], h[p.h_ld]);
                 } else {
                     uint16_t *h = (uint16_t *)p.h + to;
-                    bf16_terms(v, h[0], h[p.h_ld]);
+                    bf16_terms(bf16_cut(v, h[0]), h[p.h_ld], h[2 * p.h_ld]);
                 }
             }
             __syncwarp();
@@ -791,9 +803,11 @@ __global__ void __launch_bounds__(EX_THREADS)
 k_experts_out(const __grid_constant__ Experts p, const __grid_constant__ WeightMaps map) {
     extern __shared__ __align__(1024) char smem[];
     __shared__ Shared<NB> sh;
-    // 32 columns of h a lane: high and low terms, in 16-byte loads
-    constexpr int CH = EX_COLS / (F16 ? 2 : 1) / EX_STRIDE, TERM = F16 ? 2 : 1;
-    constexpr bool TWICE = NB == 1 && BOXES;
+    // a lane's eight columns of 32: h's terms, in 16-byte loads
+    constexpr int CH = EX_COLS / (F16 ? 2 : 1) / EX_STRIDE, TERM = F16 ? 2 : 1, TERMS = expert_terms(F16), HU = TERMS * TERM;
+    // (registers: no room for two steps of three terms, 149 us for 133 so; and beside two
+    // columns of h weights are loaded as they are used)
+    constexpr bool TWICE = NB == 1 && BOXES && F16, EARLY = NB == 1 || F16;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g8 = lane >> 2, q = lane & 3, wr = row_of(g8);
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     if (BOXES && tid == 0) umma::tma_prefetch_desc(first_map(map, p.hidden, p.cols));
@@ -868,10 +882,10 @@ k_experts_out(const __grid_constant__ Experts p, const __grid_constant__ WeightM
         return;
     }
     const int team = warp / EX_TEAM, member = warp % EX_TEAM;
-    const int64_t low = p.h_ld * (F16 ? 4 : 2) / 16;
+    const int64_t next_term = p.h_ld * (F16 ? 4 : 2) / 16;
     const uint4 *row[NB] = {};
     int row_job = -1, row_step = -1, n = 0;
-    const auto fetch = [&](uint4(&h)[CH][NB][2 * TERM], const Steps &at) {
+    const auto fetch = [&](uint4(&h)[CH][NB][HU], const Steps &at) {
         if (!TWICE && at.w.job == row_job && at.s == row_step) return;
         row_step = at.s;
         if (at.w.job != row_job) {
@@ -882,7 +896,7 @@ k_experts_out(const __grid_constant__ Experts p, const __grid_constant__ WeightM
                 row[b] = nullptr;
                 if (g8 + b * 8 < n)
                     row[b] = (const uint4 *)((const char *)p.h +
-                                             (int64_t)r.list[r.begin[row_job] + g8 + b * 8] * 2 * p.h_ld * (F16 ? 4 : 2));
+                                             (int64_t)r.list[r.begin[row_job] + g8 + b * 8] * TERMS * p.h_ld * (F16 ? 4 : 2));
             }
         }
         const int to = min((at.s + 1) * cols, p.hidden);
@@ -893,9 +907,9 @@ k_experts_out(const __grid_constant__ Experts p, const __grid_constant__ WeightM
             for (int b = 0; b < NB; ++b) {
                 const bool in = row[b] && c < to;
 #pragma unroll
-                for (int j = 0; j < 2 * TERM; ++j) {
+                for (int j = 0; j < HU; ++j) {
                     h[i][b][j] = make_uint4(0, 0, 0, 0);
-                    if (in) h[i][b][j] = row[b][(j < TERM ? 0 : low) + c / 8 * TERM + j % TERM];
+                    if (in) h[i][b][j] = row[b][j / TERM * next_term + c / 8 * TERM + j % TERM];
                 }
             }
         }
@@ -912,7 +926,7 @@ k_experts_out(const __grid_constant__ Experts p, const __grid_constant__ WeightM
     };
     give_up_to(min(ahead.w.u, w.end));
     if (!ahead.more()) return;
-    const auto take_step = [&](uint4(&h)[CH][NB][2 * TERM], uint4(&next)[CH][NB][2 * TERM]) {
+    const auto take_step = [&](uint4(&h)[CH][NB][HU], uint4(&next)[CH][NB][HU]) {
         const Steps at = ahead;
         ahead.next();
         if (ahead.more()) ahead.next();
@@ -925,10 +939,9 @@ k_experts_out(const __grid_constant__ Experts p, const __grid_constant__ WeightM
         }
         const char *from = ring.wait_full(&sh.abort_flag, p.status);
         const int left = min(cols, p.hidden - at.s * cols);
-        // (all loads before the first multiplication: what is beyond the row is zero)
+        // (EARLY: all loads before the first multiplication; what is beyond the row is zero)
         uint4 a[CH], d[CH];
-#pragma unroll
-        for (int i = 0; i < CH; ++i) {
+        const auto load = [&](int i) {
             const int k = member * 32 + i * EX_STRIDE;
             a[i] = d[i] = make_uint4(0, 0, 0, 0);
             if (k < left) {
@@ -940,9 +953,13 @@ k_experts_out(const __grid_constant__ Experts p, const __grid_constant__ WeightM
                 a[i] = first(a[i], e);
                 d[i] = first(d[i], e);
             }
-        }
+        };
+        if (EARLY)
+#pragma unroll
+            for (int i = 0; i < CH; ++i) load(i);
 #pragma unroll
         for (int i = 0; i < CH; ++i) {
+            if (!EARLY) load(i);
             uint4 a0, a1, d0, d1;
             if (F16) {
                 a0 = widened(a[i].x, a[i].y), a1 = widened(a[i].z, a[i].w);
@@ -953,7 +970,7 @@ k_experts_out(const __grid_constant__ Experts p, const __grid_constant__ WeightM
                 if (b && n <= b * 8) break;
                 if (F16) {
 #pragma unroll
-                    for (int j = 0; j < 2 * TERM; j += TERM) {
+                    for (int j = 0; j < HU; j += TERM) {
                         const uint4 v = h[i][b][j], w = h[i][b][j + TERM - 1];
                         mma8_tf32(c[b][0], a0.x, d0.x, a0.y, d0.y, v.x, v.y);
                         mma8_tf32(c[b][1], a0.z, d0.z, a0.w, d0.w, v.z, v.w);
@@ -962,25 +979,25 @@ k_experts_out(const __grid_constant__ Experts p, const __grid_constant__ WeightM
                     }
                 } else {
 #pragma unroll
-                    for (int j = 0; j < 2 * TERM; ++j) {
+                    for (int j = 0; j < HU; ++j) {
                         mma16<false>(c[b][0], a[i].x, d[i].x, a[i].y, d[i].y, h[i][b][j].x, h[i][b][j].y);
                         mma16<false>(c[b][1], a[i].z, d[i].z, a[i].w, d[i].w, h[i][b][j].z, h[i][b][j].w);
                     }
                 }
             }
         }
-        ring.release();
         if (!TWICE && ahead.more()) fetch(next, ahead);
+        ring.release();
         give_up_to(min(ahead.w.u, w.end));
         return ahead.more();
     };
     if constexpr (TWICE) {
-        uint4 one[CH][NB][2 * TERM], two[CH][NB][2 * TERM];
+        uint4 one[CH][NB][HU], two[CH][NB][HU];
         fetch(one, ahead);
         while (take_step(one, two) && take_step(two, one)) {
         }
     } else {
-        uint4 h[CH][NB][2 * TERM];
+        uint4 h[CH][NB][HU];
         fetch(h, ahead);
         while (take_step(h, h)) {
         }

@@ -336,8 +336,8 @@ struct Experts {
     const float *gates;
     uint16_t *y;
     int64_t y_ld;
-    // workspace: h as two terms [rows * top][2][h_ld], bf16 or fp32; what each piece of the
-    // second product gives [rows * top][splits][n_out]
+    // workspace: h in terms [rows * top][expert_terms][h_ld], bf16 or (fp16 layers) fp32; what
+    // each piece of the second product gives [rows * top][splits][n_out]
     void *h;
     int64_t h_ld;                     // whole 16-byte units
     int splits;
@@ -350,6 +350,7 @@ struct Experts {
     // bytes of a step, and steps
     int cols, ring_at, step, depth;
 };
+__host__ __device__ constexpr int expert_terms(bool f16) { return f16 ? 2 : 3; }      // that a hidden value has
 int expert_splits(int hidden);            // at most
 size_t expert_tables(int rows, int top);
 cudaError_t experts_prepare();

@@ -99,7 +99,7 @@ extern "C" hwr_status hwr_expert_layer(hwr_ops *c, const hwr_experts *e, void *y
     p.splits = expert_splits(e->hidden);
     const bool whole = e->top == 1 && p.splits == 1;
     const size_t pairs = (size_t)e->rows * e->top, term = e->dtype == HWR_F16 ? 4 : 2;
-    const size_t h = (pairs * p.h_ld * 2 * term + 1023) / 1024 * 1024;
+    const size_t h = (pairs * p.h_ld * expert_terms(e->dtype == HWR_F16) * term + 1023) / 1024 * 1024;
     const size_t used = (expert_tables(e->rows, e->top) + 16 + 1023) / 1024 * 1024;
     OK(reserve(c, h + used + (whole ? 0 : pairs * p.splits * p.n_out * 4)));
     p.h = c->ws;

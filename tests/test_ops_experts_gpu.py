@@ -258,3 +258,25 @@ def test_nan_scores(ops, E):
     assert y[1].isnan().all() and y[3].isnan().all() and (y[4] == 0).all()      # (4: no choice)
     keep = torch.tensor([0, 2, 5], device="cuda")
     assert torch.equal(y[keep], ops.expert_layer(x, w_in, w_out, scores=masked, top=top, over_all=True)[keep])
+
+
+@pytest.mark.parametrize("T,F", [(3, 16), (8, 33), (64, 16), (64, 33)])
+def test_hidden_values_keep_24_bits(ops, T, F):
+    """Two hidden values of a bf16 layer that agree in 16 bits, taken apart: h = x1 + x2 + x3 and
+    x1 + x2, with x1 in [1/2, 1), x2 below 2^-8 and x3 below 2^-16, eight bits each.  Their
+    difference is x3, off by 2^-22 of at most 1 for each of 11 additions (model: ops_ref.ADD);
+    values of 16 bits would lose up to 2^-17."""
+    def bits(lowest):
+        g = torch.Generator(device="cuda").manual_seed(T + lowest)
+        return torch.randint(128, 256, (T,), device="cuda", generator=g).double() * 2.0 ** lowest
+    parts = [bits(-8), bits(-16), bits(-24)]
+    x = torch.zeros(T, 8, device="cuda", dtype=BF)
+    w_in, w_out = torch.zeros(1, F, 8, device="cuda", dtype=BF), torch.zeros(1, 24, F, device="cuda", dtype=BF)
+    for i, part in enumerate(parts):
+        x[:, i] = part
+        assert torch.equal(x[:, i].double(), part)
+    w_in[0, 0, :3] = w_in[0, F - 1, :2] = 1
+    w_out[0, :, 0], w_out[0, :, F - 1] = 1, -1
+    y = ops.expert_layer(x, w_in, w_out, choice=torch.zeros(T, 1, device="cuda", dtype=torch.int32),
+                         gates=torch.ones(T, 1, device="cuda"), activation="relu").double()
+    assert ((y - parts[2][:, None]).abs() <= 11 * 2.0 ** -22 + 2.0 ** -8 * parts[2][:, None]).all()
