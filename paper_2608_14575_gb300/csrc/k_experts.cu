@@ -27,7 +27,7 @@
 // product whole: beside bf16 weights as three bf16 terms.  (As two, 16 bits of it, one
 // bf16 result in 220 differed from that of fp32 hidden values, with three one in 1,070, as
 // many as another order of fp32 sums moves; 16 rows with 6 of 64 experts of 2,048 -> 2 x 1,408
-// took 128.5 us for 133, 64 rows with 4 of 24 of 1,024 -> 2 x 2,048 83.5 for 90.)  Beside fp16
+// took 128.5 us for 133, 64 rows with 4 of 24 of 1,024 -> 2 x 2,048 84 for 88.5.)  Beside fp16
 // weights, whose range is too small for it, as two tf32 values, within 2^-20 of it, the
 // weights widened to tf32 exactly: fp16 results are rounded to 2^-11, and a third would be
 // half as many multiplications again.
@@ -49,16 +49,17 @@ constexpr int EX_WARPS = EX_MMA + EX_COPY + EX_ADD, EX_THREADS = EX_WARPS * 32;
 constexpr int EX_SUMS = 2;                 // units whose sums are under way
 constexpr int EX_STRIDE = EX_TEAM * 32;    // columns of a step that a team takes at a time
 constexpr int EX_PAIRS = EXPERTS_MAX_ROWS * EXPERTS_MAX_TOP;
-constexpr int EX_DEPTH = 8;                // steps of the ring, at most
+constexpr int EX_DEPTH = 6;                // steps of the ring, at most
 constexpr int EX_UNIT_COST = 128;          // of a unit, in columns of its weights
 // Columns of a step, at most (of the second product in fp16: half).  One row of 4,096 ->
-// 2 x 8,192 over 2 of 8 experts: 76 us with 1,024, 73 with 512.
+// 2 x 8,192 over 2 of 8 experts: 76 us with 1,024, 73 with 512 (75 since h has three terms).
 constexpr int EX_COLS = 512;
 constexpr int SUM_THREADS = 128;
-// Shared memory of the tables and the ring (8 steps of 512 columns beside the tables); the
-// rest is the L1 that keeps x and h.  With 4, 6 and 8 steps 16 rows with 6 of 64 experts of
-// 2,048 -> 2 x 1,408 take 163, 154.5 and 154 us, one row with 2 of 12 of 1,024 -> 2 x 4,096
-// 21.4, 21.4 and 21.9.
+// Shared memory of the tables and the ring, at most; what the ring leaves is the L1 that keeps
+// x and h.  With 4, 6 and 8 steps 16 rows with 6 of 64 experts of 2,048 -> 2 x 1,408 (evenly spread
+// scores) take 168, 160 and 159 us, one row with 2 of 12 of 1,024 -> 2 x 4,096 21.5, 21.5 and 22.1,
+// 64 rows with 4 of 24 of 1,024 -> 2 x 2,048 87.6, 88.5 and 90.3, with 2 of 64 of 1,024 -> 2 x 4,096
+// in fp16 (a listed case) 227.8, 210.2 and 209.1.
 constexpr int EX_RING = 140 * 1024;
 constexpr int EX_GROUPS = OPS_MAX_GROUPS, EX_EACH = (EX_GROUPS + EX_THREADS - 1) / EX_THREADS;      // groups a thread
 constexpr uint32_t ALL = 0xffffffffu;
@@ -153,7 +154,7 @@ __device__ __forceinline__ Piece piece_of(const void *row, int size, int c, int 
 // for all of a step's columns, and at the end of rows that are not whole 64 columns one for
 // those before the last 64 and one for what is left; matrices whose rows begin on 16-byte
 // boundaries.  Else: as bulk copies of rows, sixteen a step of any start and length (8 rows
-// over 4 of 32 experts, 2,056 -> 2 x 2,816, bf16, in boxes and by rows: 131 and 181 us).
+// over 4 of 32 experts, 2,056 -> 2 x 2,816, bf16, in boxes and by rows: 134 and 221 us).
 
 // The map of a unit's first copy (one that is filled in).
 __device__ __forceinline__ const CUtensorMap *first_map(const WeightMaps &m, int n, int cols) {
@@ -829,7 +830,7 @@ k_experts_out(const __grid_constant__ Experts p, const __grid_constant__ WeightM
     }
     // Beside several columns of h, pieces of two steps, one a team, whose h stays in the
     // registers from tile to tile (64 rows, 4 of 16 experts each, 1,024 -> 2 x 2,048, bf16:
-    // 86.7 us without, 80.9 with; in fp16, whose steps are half as wide, 90.7 and 93.5).
+    // 109 us without, 90 with; in fp16, whose steps are half as wide, 90.7 and 93.5).
     if (NB > 1 && !F16)
         while (splits < p.splits && splits * 2 < all_steps) splits *= 2;
     const int per = (all_steps + splits - 1) / splits;       // steps of a piece, and pieces with any
@@ -1080,9 +1081,9 @@ template <bool F16>
 cudaError_t both(const Experts &p, const ExpertMaps &m, int nsm, cudaStream_t s) {
     const bool in = m.in_boxes, out = m.out_boxes;
     // Jobs of 16 pairs where experts have more than 8 on average (64 rows, 4 experts each,
-    // 1,024 -> 2 x 2,048, bf16, jobs of 8 and 16: over 24 experts 104 and 80 us, over 28 106 and
-    // 88; over 32 103 and 105 to 108, for what fewer rows have their registers hold half the
-    // loads under way).
+    // 1,024 -> 2 x 2,048, bf16, jobs of 8 and 16: over 24 experts 106 and 89 us, over 28 109 and
+    // 98; over 32 106 and 109, for what fewer rows have their registers hold half the loads
+    // under way).
     const bool x = whole16(p.x, p.x_ld), two = p.rows * p.top > 8 * p.groups;
     cudaError_t e = launch(two ? kernel_in<F16, 2>(in, x) : kernel_in<F16, 1>(in, x), p, m.in, m.in_cols, nsm, s);
     if (e != cudaSuccess) return e;
