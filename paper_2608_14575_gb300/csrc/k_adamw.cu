@@ -124,7 +124,8 @@ __device__ __forceinline__ float max_nan(float a, float b) {
 }
 
 // A 32-bit hash of whole numbers, each output bit of which depends on every input bit
-// about evenly (tested on the rounding that it drives).
+// about evenly (tested on the rounding that it drives): two multiplications between shifts, the
+// form and the first multiplier of C. Wellons, "Prospecting for Hash Functions" (2018).
 __device__ __forceinline__ uint32_t mixed(uint32_t x) {
     x = (x ^ x >> 16) * 0x7feb352du;
     x = (x ^ x >> 15) * 0x68e31da5u;

@@ -45,6 +45,9 @@ constexpr float LOG2E = 1.4426950408889634f;
 constexpr float FAR = -1e30f;
 constexpr uint32_t ALL = 0xffffffffu;
 
+// Within 2 units of the last place, 0 below 2^-126: an exp here is a term of a sum beside 1, or a
+// probability, each of which has that much from its argument's roundings already.  (Log
+// probabilities and entropies of 4,099 rows of 50,001 are 8.3e-8 off 64 bits, in a plain form 6.5e-8.)
 __device__ __forceinline__ float exp2_fast(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
