@@ -473,13 +473,14 @@ k_token_grad(const __grid_constant__ TokenGrad p) {
     const float a = p.da && (uint32_t)token < (uint32_t)p.vocab && !empty ? p.da[row] : 0.f;
     const float b = p.db ? p.db[row] : 0.f;
     if (empty) m = 0.f;
-    // With 2^7 q and 2^-7 of a and b: b's product with a distance down to where 2^7 q is 0
-    // cannot overflow, whatever b (with the distance as it is, times 0, a masked logit's gradient
-    // was NaN from 3.4e8 on; b times q first took 133 us for the training step's 130).
-    const float a7 = a * 0x1p-7f, b7 = b * 0x1p-7f;
+    // Where b is so large that its product with a distance (down to where q is 0, 127 at most)
+    // could overflow, 2^7 q and 2^-7 of a and b: 0 times infinity would make a masked logit's
+    // gradient NaN.  (b times q first costs no choice, but 133 us for the training step's 130.)
+    const bool large = fabsf(b) > 0x1p120f;
+    const float up = large ? 7.f : 0.f, down = large ? 0x1p-7f : 1.f, sa = a * down, sb = b * down;
     auto grad = [&](float z, int at) {
-        const float lq = max_nan((z - m) - ls, -127.f), q7 = exp2_fast(fmaf(lq, LOG2E, 7.f));
-        const float g = -q7 * fmaf(b7, lq + h, a7);
+        const float lq = max_nan((z - m) - ls, -127.f), q = exp2_fast(fmaf(lq, LOG2E, up));
+        const float g = -q * fmaf(sb, lq + h, sa);
         return at == token ? g + a : g;
     };
     // (vectors where both rows begin alike, else value by value)
