@@ -77,6 +77,7 @@ struct Vec {
 // both, a few results in a million show): not for values whose every bit counts.
 struct Two {
     uint64_t v;
+    Two() = default;
     __device__ __forceinline__ Two(float a, float b) { asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(a), "f"(b)); }
     __device__ __forceinline__ explicit Two(uint64_t v) : v(v) {}
     __device__ __forceinline__ void get(float &a, float &b) const { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }

@@ -321,3 +321,23 @@ def test_large_gradients_at_masked_logits(ops, dt):
     for b in (1e9, -1e30, 3e38):
         dz = ops.token_logprobs_backward(None, z, None, got, dentropy=torch.full((2,), b, device="cuda"))
         assert (dz[z == -INF] == 0).all() and dz[0, 7] == 0
+
+
+@pytest.mark.parametrize("dt", [F32, BF, HF])
+def test_small_log_probabilities(ops, dt):
+    """Nearly all of the probability on one logit, beside terms that are just too small to
+    count next to it one by one (0.89 2^-24).  A row's sum near 1 is rounded (by 2^-24 at most)
+    once a step of a block (4,096 logits, in 32 bits 2,048), four times within one, five between
+    lanes, four between halves and warps and, here, never between pieces; exp within 2^-20."""
+    T, V = 1300, 40_960
+    z = torch.full((T, V), -16.75, device="cuda", dtype=dt)
+    token = torch.arange(T, device="cuda", dtype=torch.int32) * 31 + 7
+    z[torch.arange(T, device="cuda"), token.long()] = 0.0
+    got = ops.token_logprobs(z, token)
+    want = -math.log1p((V - 1) * math.exp(-16.75))
+    steps = V // (2048 if dt == F32 else 4096)
+    assert float((got.logprob.double() - want).abs().max()) <= (steps + 14) * 2.0 ** -24 + 2.0 ** -20 * abs(want)
+    # With alternatives: blocks of twice the threads and warps, a rounding for every four logits of
+    # a thread (two pairs), once for a pair.
+    top = ops.token_logprobs(z, token, top=2)
+    assert float((top.logprob.double() - want).abs().max()) <= (V // 1024 + 14) * 2.0 ** -24 + 2.0 ** -20 * abs(want)
