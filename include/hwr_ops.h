@@ -249,8 +249,8 @@ hwr_status hwr_adamw_destroy(hwr_ops *ops, hwr_adamw *optimizer); /* synchronise
  * (over_all) over all of the row's scores, NaN where one of those is.  Without, they are
  * choice and gates [rows][top]; a choice outside [0, groups) is none, the same one may come
  * twice.  A row without a choice gets zeros.  Experts that no row chooses are not read.
- * h is summed in fp32 and enters the second product whole, as three terms (in fp16
- * layers as two, within 2^-20 of it, at any magnitude); y is rounded once.
+ * h is summed in fp32 and enters the second product whole, as three bf16 terms (from
+ * 2^-110 on; in fp16 layers as two, within 2^-20 of it, at any magnitude); y is rounded once.
  */
 typedef enum { HWR_ACT_SILU = 0, HWR_ACT_GELU = 1 /* u Phi(u) */, HWR_ACT_RELU = 2 } hwr_activation;
 typedef struct {
